@@ -3,7 +3,8 @@
 Each translation unit is compiled by its own nvcc process, in parallel, then
 linked into one shared library with the C ABI of include/pic_decode.h,
 include/pic_izpr.h, include/pic_idct.h, include/pic_fuse.h,
-include/pic_huffman.h and include/pic_measure.h.
+include/pic_huffman.h, include/pic_linear.h, include/pic_clip.h and
+include/pic_measure.h.
 """
 from __future__ import annotations
 
@@ -20,7 +21,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(BUILD, "libpic_gb300.so")
 SOURCES = ["pic_decode.cu", "k_fp32.cu", "k_fp32_any.cu", "k_fp32_sweep.cu", "k_tc.cu",
            "k_tc_tma.cu", "k_march.cu", "k_march_f32lat.cu", "k_strip.cu", "k_izpr.cu",
-           "k_idct.cu", "k_fuse.cu", "k_huffman.cu", "k_peak.cu"]
+           "k_idct.cu", "k_fuse.cu", "k_huffman.cu", "k_peak.cu", "pic_linear.cu",
+           "k_linear_simt.cu", "k_linear_grad.cu", "k_clip.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",
          "--expt-relaxed-constexpr", "-I", INCLUDE, "-I", CSRC]

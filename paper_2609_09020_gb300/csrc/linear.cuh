@@ -1,0 +1,117 @@
+// linear.cuh -- what the kernels of the linear layer (include/pic_linear.h)
+// share: element types, activations and the launch interfaces between their
+// translation units.
+#pragma once
+
+#include <cstdint>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "pic_common.cuh"
+#include "pic_linear.h"
+
+namespace pic {
+namespace lin {
+
+template <typename T>
+__device__ __forceinline__ float to_f32(T v);
+template <>
+__device__ __forceinline__ float to_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ float to_f32<__half>(__half v) { return __half2float(v); }
+template <>
+__device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+
+// Round to nearest even.
+template <typename T>
+__device__ __forceinline__ T from_f32(float v);
+template <>
+__device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// act(z), NaN for NaN.  GELU is max(z, 0) - a Phi(-a), a = |z|: no infinity
+// meets a zero.  From a = 20 on Phi(-a) is below fp32's range.
+// EXACT: with erfcf, accurate to a few ulps in the tail too (fp32 outputs);
+// else the framework's polynomial form, off by at most 5e-7, far below half
+// an ulp of a 16-bit output but for outputs below 2e-3 (fp16: 1e-3) in size.
+template <bool EXACT>
+__device__ __forceinline__ float act_value(float z, int act) {
+  if (act == PIC_ACT_NONE) return z;
+  if (act == PIC_ACT_RELU) return relu_nan(z);
+  if constexpr (EXACT) {
+    const float a = fminf(fabsf(z), 20.0f);
+    return fmaf(-0.5f * a, erfcf(a * 0.70710678118654752f), relu_nan(z));
+  } else {
+    return gelu_approx(z);
+  }
+}
+
+// dy act'(z): a derivative of zero gives zero whatever dy is.  The clamp keeps
+// z phi(z) from being infinity times zero (phi(20) is below fp32's range).
+__device__ __forceinline__ float act_grad(float dy, float z, int act) {
+  if (act == PIC_ACT_NONE) return dy;
+  if (act == PIC_ACT_RELU) return z > 0.0f ? dy : 0.0f;
+  const float c = fminf(fmaxf(z, -20.0f), 20.0f);
+  const float phi = 0.39894228040143268f * __expf(-0.5f * c * c);
+  const float d = fmaf(c, phi, 0.5f * erfcf(-0.70710678118654752f * z));
+  return dy * d;
+}
+
+// One matrix product C[i][j] = sum_k A(i, k) B(j, k) with what follows it.
+// A(i, k) is at a[i * a_i + k * a_k], B(j, k) at b[j * b_j + k * b_k]; one of
+// the two strides is 1.
+struct Product {
+  const void* a;
+  const void* b;
+  long long a_i, a_k, b_j, b_k;
+  long long I, J, K;
+  // epilogue: z = C + bias[j]; pre = z; y = act(z) + residual
+  const void* bias;
+  const void* residual;
+  long long ldr;
+  void* y;
+  long long ldy;
+  void* pre;
+  long long ldpre;
+  int act;
+};
+
+// Parts of the sum over K that one product is cut into (1: none), each a
+// multiple of `step`, so that about `target` blocks have work.
+inline int split_count(long long tiles, long long K, long long step, long long target) {
+  if (tiles >= target) return 1;
+  long long s = target / tiles;
+  const long long most = (K + step - 1) / step;
+  if (s > most) s = most;
+  return s < 1 ? 1 : static_cast<int>(s);
+}
+
+// Every function returns a pic_status; `ws` is device workspace.
+long long simt_workspace(const Product& p);
+int simt_product(const Product& p, int dtype, void* ws, cudaStream_t s);
+
+// dz[i][j] = dy act'(z), rounded (dz null: not written), and parts[b][j], the
+// column sums of the unrounded dz over the rows of block b (parts null: none).
+struct GradAct {
+  const void* dy;
+  long long lddy;
+  const void* pre;
+  long long ldpre;
+  void* dz;
+  long long lddz;
+  float* parts;
+  long long I, J;
+  int act;
+};
+long long grad_act_blocks(long long I, long long J);
+int grad_act(const GradAct& g, int dtype, cudaStream_t s);
+// out[j] = sum_b parts[b][j], b ascending within a fixed tree.
+int sum_parts(const float* parts, long long blocks, long long J, void* out, int dtype, cudaStream_t s);
+
+}  // namespace lin
+}  // namespace pic

@@ -1,0 +1,204 @@
+// pic_linear.cu -- the C ABI of include/pic_linear.h: checks of arguments, the
+// choice of kernels and the workspace's layout.
+#include <atomic>
+
+#include "linear.cuh"
+
+namespace {
+
+using pic::lin::GradAct;
+using pic::lin::Product;
+
+constexpr long long kMaxDim = 0x7fffffffLL - 256;
+
+size_t elem_bytes(int dtype) { return dtype == PIC_DTYPE_F32 ? 4 : 2; }
+
+bool type_ok(int dtype) { return dtype == PIC_DTYPE_F32 || dtype == PIC_DTYPE_F16 || dtype == PIC_DTYPE_BF16; }
+bool act_ok(int act) { return act == PIC_ACT_NONE || act == PIC_ACT_RELU || act == PIC_ACT_GELU; }
+
+bool aligned(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+// A [rows][cols] matrix of the call: present, on its element's boundary, rows
+// apart by at least a row and at most 2^40 elements.
+bool matrix_ok(const void* p, long long ld, long long rows, long long cols, int dtype) {
+  return (p || rows == 0) && aligned(p, elem_bytes(dtype)) && ld >= cols && ld <= (1LL << 40);
+}
+
+bool dims_ok(long long rows, long long in, long long out) {
+  return rows >= 0 && in >= 1 && out >= 1 && rows <= kMaxDim && in <= kMaxDim && out <= kMaxDim;
+}
+
+bool args_ok(const pic_linear_args* a) {
+  if (!a || !dims_ok(a->rows, a->in_features, a->out_features) || !type_ok(a->dtype) || !act_ok(a->act)) return false;
+  const long long M = a->rows, K = a->in_features, N = a->out_features;
+  if (!matrix_ok(a->x, a->ldx, M, K, a->dtype) || !matrix_ok(a->w, a->ldw, N, K, a->dtype) ||
+      !matrix_ok(a->y, a->ldy, M, N, a->dtype))
+    return false;
+  if (a->bias && !aligned(a->bias, elem_bytes(a->dtype))) return false;
+  if (a->residual && !matrix_ok(a->residual, a->ldr == 0 ? N : a->ldr, M, N, a->dtype)) return false;
+  if (a->residual == a->y && a->residual && a->ldr != a->ldy) return false;
+  return !a->pre || matrix_ok(a->pre, a->ldpre, M, N, a->dtype);
+}
+
+bool args_ok(const pic_linear_grad_args* a) {
+  if (!a || !dims_ok(a->rows, a->in_features, a->out_features) || !type_ok(a->dtype) || !act_ok(a->act)) return false;
+  const long long M = a->rows, K = a->in_features, N = a->out_features;
+  if (!a->dx && !a->dw && !a->db) return false;
+  if (!matrix_ok(a->dy, a->lddy, M, N, a->dtype)) return false;
+  if (a->act != PIC_ACT_NONE && !matrix_ok(a->pre, a->ldpre, M, N, a->dtype)) return false;
+  if (a->dw && (!matrix_ok(a->x, a->ldx, M, K, a->dtype) || !matrix_ok(a->dw, a->lddw, N, K, a->dtype))) return false;
+  if (a->dx && (!matrix_ok(a->w, a->ldw, N, K, a->dtype) || !matrix_ok(a->dx, a->lddx, M, K, a->dtype))) return false;
+  return !a->db || aligned(a->db, elem_bytes(a->dtype));
+}
+
+// The device must be the one that the kernels are built for; looked up once
+// per device (0: not yet, 1: it is, 2: it is not).
+int device_status() {
+  static std::atomic<int> known[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) {
+    cudaGetLastError();
+    return PIC_ERR_UNSUPPORTED;
+  }
+  if (dev < 0 || dev >= 64) return PIC_ERR_UNSUPPORTED;
+  int k = known[dev].load(std::memory_order_relaxed);
+  if (k == 0) {
+    int major = 0, minor = 0;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess) {
+      cudaGetLastError();
+      return PIC_ERR_CUDA;
+    }
+    k = major == 10 && minor == 3 ? 1 : 2;
+    known[dev].store(k, std::memory_order_relaxed);
+  }
+  return k == 1 ? PIC_OK : PIC_ERR_UNSUPPORTED;
+}
+
+// Hands out 256-byte aligned pieces of a workspace; with a null base it only
+// counts.
+struct Arena {
+  char* base;
+  long long used = 0;
+  void* take(long long bytes) {
+    void* p = base ? base + used : nullptr;
+    used += (bytes + 255) / 256 * 256;
+    return p;
+  }
+};
+
+Product forward_product(const pic_linear_args& a) {
+  Product p{};
+  p.a = a.x, p.a_i = a.ldx, p.a_k = 1;
+  p.b = a.w, p.b_j = a.ldw, p.b_k = 1;
+  p.I = a.rows, p.J = a.out_features, p.K = a.in_features;
+  p.bias = a.bias, p.residual = a.residual, p.ldr = a.ldr;
+  p.y = a.y, p.ldy = a.ldy, p.pre = a.pre, p.ldpre = a.ldpre, p.act = a.act;
+  return p;
+}
+
+int forward(const pic_linear_args& a, Arena& ws, bool launch, cudaStream_t s) {
+  if (a.rows == 0) return PIC_OK;
+  const Product p = forward_product(a);
+  void* w = ws.take(pic::lin::simt_workspace(p));
+  return launch ? pic::lin::simt_product(p, a.dtype, w, s) : PIC_OK;
+}
+
+int zero_rows(void* p, long long ld, long long rows, long long cols, int dtype, cudaStream_t s) {
+  const size_t e = elem_bytes(dtype);
+  return cudaMemset2DAsync(p, ld * e, 0, cols * e, rows, s) == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+}
+
+int backward(const pic_linear_grad_args& a, Arena& ws, bool launch, cudaStream_t s) {
+  const long long M = a.rows, K = a.in_features, N = a.out_features;
+  int rc = PIC_OK;
+  if (M == 0) {
+    if (!launch) return PIC_OK;
+    if (a.dw) rc = zero_rows(a.dw, a.lddw, N, K, a.dtype, s);
+    if (a.db && rc == PIC_OK) rc = zero_rows(a.db, N, 1, N, a.dtype, s);
+    return rc;
+  }
+  // dz: dy itself where there is no activation
+  const bool products = a.dx || a.dw;
+  const void* dz = a.dy;
+  long long lddz = a.lddy;
+  const bool own_dz = a.act != PIC_ACT_NONE && products;
+  if (own_dz) {
+    lddz = N;
+    dz = ws.take(M * lddz * static_cast<long long>(elem_bytes(a.dtype)));
+  }
+  const long long blocks = pic::lin::grad_act_blocks(M, N);
+  float* parts = a.db ? static_cast<float*>(ws.take(blocks * N * 4)) : nullptr;
+  if (launch && (own_dz || a.db)) {
+    const GradAct g{a.dy, a.lddy, a.pre, a.ldpre, own_dz ? const_cast<void*>(dz) : nullptr, lddz, parts, M, N, a.act};
+    rc = pic::lin::grad_act(g, a.dtype, s);
+    if (rc == PIC_OK && a.db) rc = pic::lin::sum_parts(parts, blocks, N, a.db, a.dtype, s);
+    if (rc != PIC_OK) return rc;
+  }
+  if (a.dx) {
+    Product p{};
+    p.a = dz, p.a_i = lddz, p.a_k = 1;
+    p.b = a.w, p.b_j = 1, p.b_k = a.ldw;
+    p.I = M, p.J = K, p.K = N;
+    p.y = a.dx, p.ldy = a.lddx, p.act = PIC_ACT_NONE;
+    void* w = ws.take(pic::lin::simt_workspace(p));
+    if (launch && (rc = pic::lin::simt_product(p, a.dtype, w, s)) != PIC_OK) return rc;
+  }
+  if (a.dw) {
+    Product p{};
+    p.a = dz, p.a_i = 1, p.a_k = lddz;
+    p.b = a.x, p.b_j = 1, p.b_k = a.ldx;
+    p.I = N, p.J = K, p.K = M;
+    p.y = a.dw, p.ldy = a.lddw, p.act = PIC_ACT_NONE;
+    void* w = ws.take(pic::lin::simt_workspace(p));
+    if (launch && (rc = pic::lin::simt_product(p, a.dtype, w, s)) != PIC_OK) return rc;
+  }
+  return PIC_OK;
+}
+
+template <typename Args, typename F>
+int64_t count_bytes(const Args* a, F f) {
+  if (!args_ok(a)) return -1;
+  Arena ws{nullptr};
+  f(*a, ws, false, nullptr);
+  return ws.used;
+}
+
+template <typename Args, typename F>
+int run(const Args* a, F f, void* workspace, size_t bytes, void* stream) {
+  const int64_t need = count_bytes(a, f);
+  if (need < 0 || bytes < static_cast<size_t>(need)) return PIC_ERR_INVALID_ARG;
+  if (need > 0 && (!workspace || !aligned(workspace, 256))) return PIC_ERR_INVALID_ARG;
+  const int rc = device_status();
+  if (rc != PIC_OK) return rc;
+  Arena ws{static_cast<char*>(workspace)};
+  const int r = f(*a, ws, true, static_cast<cudaStream_t>(stream));
+  if (r == PIC_ERR_CUDA) cudaGetLastError();
+  return r;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t pic_linear_workspace_bytes(const pic_linear_args* a) { return count_bytes(a, forward); }
+
+int pic_linear(const pic_linear_args* a, void* workspace, size_t workspace_bytes, void* stream) {
+  return run(a, forward, workspace, workspace_bytes, stream);
+}
+
+int64_t pic_linear_backward_workspace_bytes(const pic_linear_grad_args* a) { return count_bytes(a, backward); }
+
+int pic_linear_backward(const pic_linear_grad_args* a, void* workspace, size_t workspace_bytes, void* stream) {
+  return run(a, backward, workspace, workspace_bytes, stream);
+}
+
+int pic_linear_check(void* stream) {
+  if (cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+    cudaGetLastError();
+    return PIC_ERR_CUDA;
+  }
+  return PIC_OK;
+}
+
+}  // extern "C"

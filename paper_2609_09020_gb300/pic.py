@@ -42,6 +42,11 @@ PIC_OUT_U8_HWC = 2
 OUTPUTS = {"f32_chw": PIC_OUT_F32_CHW, "f32_hwc": PIC_OUT_F32_HWC, "u8_hwc": PIC_OUT_U8_HWC}
 PIC_STAGING_AUTO, PIC_STAGING_COPIES, PIC_STAGING_TMA = 0, 1, 2
 STAGINGS = {"auto": PIC_STAGING_AUTO, "copies": PIC_STAGING_COPIES, "tma": PIC_STAGING_TMA}
+PIC_ACT_NONE = 2
+LINEAR_ACTS = {"none": PIC_ACT_NONE, **ACTS}
+PIC_DTYPE_F32, PIC_DTYPE_F16, PIC_DTYPE_BF16 = 0, 1, 2
+DTYPES = {"torch.float32": PIC_DTYPE_F32, "torch.float16": PIC_DTYPE_F16,
+          "torch.bfloat16": PIC_DTYPE_BF16}
 
 
 class pic_arch(ctypes.Structure):
@@ -63,6 +68,31 @@ class pic_arch(ctypes.Structure):
 
 
 _P = ctypes.c_void_p
+
+
+def _fields(ints, *rest):
+    return [(n, ctypes.c_int64) for n in ints.split()] + list(rest)
+
+
+class pic_linear_args(ctypes.Structure):
+    _fields_ = _fields("rows in_features out_features", ("dtype", ctypes.c_int), ("act", ctypes.c_int),
+                       ("x", _P), ("ldx", ctypes.c_int64), ("w", _P), ("ldw", ctypes.c_int64),
+                       ("bias", _P), ("residual", _P), ("ldr", ctypes.c_int64), ("y", _P),
+                       ("ldy", ctypes.c_int64), ("pre", _P), ("ldpre", ctypes.c_int64))
+
+
+class pic_linear_grad_args(ctypes.Structure):
+    _fields_ = _fields("rows in_features out_features", ("dtype", ctypes.c_int), ("act", ctypes.c_int),
+                       ("dy", _P), ("lddy", ctypes.c_int64), ("x", _P), ("ldx", ctypes.c_int64),
+                       ("w", _P), ("ldw", ctypes.c_int64), ("pre", _P), ("ldpre", ctypes.c_int64),
+                       ("dx", _P), ("lddx", ctypes.c_int64), ("dw", _P), ("lddw", ctypes.c_int64),
+                       ("db", _P))
+
+
+class pic_clip_tensor(ctypes.Structure):
+    _fields_ = [("grad", _P), ("out", _P), ("count", ctypes.c_int64), ("dtype", ctypes.c_int)]
+
+
 _lib = None
 
 
@@ -126,6 +156,19 @@ def load_library():
     lib.pic_huffman_decode.restype = i
     lib.pic_huffman_status.argtypes = [_P, _P]
     lib.pic_huffman_status.restype = i
+    for name, args in (("pic_linear", pic_linear_args), ("pic_linear_backward", pic_linear_grad_args)):
+        f = getattr(lib, name)
+        f.argtypes, f.restype = [ctypes.POINTER(args), _P, ctypes.c_size_t, _P], i
+        f = getattr(lib, name + "_workspace_bytes")
+        f.argtypes, f.restype = [ctypes.POINTER(args)], i64
+    lib.pic_linear_check.argtypes = [_P]
+    lib.pic_linear_check.restype = i
+    lib.pic_clip_create.argtypes = [ctypes.POINTER(pic_clip_tensor), i, ctypes.POINTER(_P)]
+    lib.pic_clip_create.restype = i
+    lib.pic_clip.argtypes = [_P, ctypes.c_float, _P, _P]
+    lib.pic_clip.restype = i
+    lib.pic_clip_destroy.argtypes = [_P]
+    lib.pic_clip_destroy.restype = None
     lib.pic_fma_peak_flops.argtypes = [i, i]
     lib.pic_fma_peak_flops.restype = i64
     lib.pic_fma_peak_launch.argtypes = [_P, i, i, _P]
@@ -375,6 +418,240 @@ def huffman_decode(words, word_off, n_bits, tab_value, tab_len, p, sym_off, stre
         if rc != PIC_OK:
             raise PicError(rc, "pic_huffman_status")
     return out
+
+
+# ---- the linear layer, its gradient, gradient clipping ----------------------
+_dtype_codes = {}  # torch dtype -> pic_dtype
+
+
+def _dtype_code(t, name) -> int:
+    if not _dtype_codes:
+        import torch
+        for n, c in DTYPES.items():
+            _dtype_codes[getattr(torch, n.split(".")[1])] = c
+    code = _dtype_codes.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name}: must be float32, float16 or bfloat16, not {t.dtype}")
+    return code
+
+
+def _rows(t, name, cols, like, rows=None, one_row=False):
+    """(pointer, row stride) of t as a [rows][cols] matrix of ``like``'s type
+    and device.  Leading dimensions are counted as rows, which they are for
+    contiguous tensors and 2-D ones whose rows are contiguous."""
+    if t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
+    if t.dim() < 1 or t.shape[-1] != cols:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {cols} columns")
+    n = t.numel() // cols
+    if rows is not None and n != rows:
+        raise ValueError(f"{name}: {n} rows, expected {rows}")
+    if t.dim() <= 2 and n > 0:
+        ld = cols if n == 1 else t.stride(0)
+        if cols > 1 and t.stride(-1) != 1 or not (ld >= cols or one_row and ld == 0):
+            raise ValueError(f"{name}: rows must be contiguous and must not overlap")
+        return t.data_ptr(), ld
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: must be contiguous, or 2-D with contiguous rows")
+    return t.data_ptr(), cols
+
+
+def _vector(t, name, n, like):
+    if t.dtype != like.dtype or t.device != like.device or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name}: must be a contiguous [{n}] tensor of {like.dtype} on {like.device}")
+    return t.data_ptr()
+
+
+def _on_device(t, name):
+    import torch
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, must be on the current CUDA device")
+
+
+class _Allocating:
+    """Makes ``stream`` torch's current one while a call allocates: memory that
+    goes back to the allocator after the call is then used again only behind
+    the call's kernels."""
+
+    def __init__(self, stream):
+        self._ctx = None
+        if stream is not None and _stream_ptr(stream) != _current_stream():
+            import torch
+            if not isinstance(stream, torch.cuda.Stream):
+                stream = torch.cuda.ExternalStream(_stream_ptr(stream))
+            self._ctx = torch.cuda.stream(stream)
+
+    def __enter__(self):
+        if self._ctx is not None:
+            self._ctx.__enter__()
+
+    def __exit__(self, *exc):
+        if self._ctx is not None:
+            self._ctx.__exit__(*exc)
+
+
+def _call_with_workspace(name, args, device):
+    import torch
+    lib = load_library()
+    need = getattr(lib, name + "_workspace_bytes")(ctypes.byref(args))
+    if need < 0:
+        raise PicError(PIC_ERR_INVALID_ARG, name)
+    ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    rc = getattr(lib, name)(ctypes.byref(args), ws.data_ptr() if need else None, need, _current_stream())
+    if rc != PIC_OK:
+        raise PicError(rc, name)
+
+
+def _linear_act(act) -> int:
+    code = LINEAR_ACTS.get(act)
+    if code is None:
+        raise ValueError(f"act: {act!r}, must be one of {sorted(LINEAR_ACTS)}")
+    return code
+
+
+def linear(x, weight, bias=None, act="none", residual=None, out=None, save_pre=False, stream=None):
+    """act(x weight^T + bias) + residual on torch CUDA tensors: x [..., in],
+    weight [out, in], bias [out], residual [..., out] (or one row, expanded),
+    all of one type (float32, float16, bfloat16); act "none", "relu" or "gelu"
+    (erf form).  Returns y [..., out] (``out`` if given, which may be
+    ``residual``), or (y, pre) with save_pre: pre = x weight^T + bias is what
+    ``linear_backward`` reads.  x and residual may be 2-D with rows further
+    apart than their width.  Enqueued on the stream, not synchronised."""
+    import torch
+    _on_device(x, "x")
+    if weight.dim() != 2:
+        raise ValueError("weight: must be 2-D")
+    N, K = weight.shape
+    if N < 1 or K < 1:
+        raise ValueError("weight: must not be empty")
+    a = pic_linear_args()
+    a.act = _linear_act(act)
+    a.dtype = _dtype_code(x, "x")
+    M = x.numel() // K
+    a.rows, a.in_features, a.out_features = M, K, N
+    a.x, a.ldx = _rows(x, "x", K, x)
+    a.w, a.ldw = _rows(weight, "weight", K, x)
+    if bias is not None:
+        a.bias = _vector(bias, "bias", N, x)
+    if residual is not None:
+        a.residual, a.ldr = _rows(residual, "residual", N, x, M, one_row=True)
+    shape = x.shape[:-1] + (N,)
+    with _Allocating(stream):
+        if out is None:
+            out = torch.empty(shape, dtype=x.dtype, device=x.device)
+        a.y, a.ldy = _rows(out, "out", N, x, M)
+        pre = torch.empty(shape, dtype=x.dtype, device=x.device) if save_pre else None
+        if save_pre:
+            a.pre, a.ldpre = pre.data_ptr(), N
+        _call_with_workspace("pic_linear", a, x.device)
+    return (out, pre) if save_pre else out
+
+
+def linear_backward(dy, x, weight, act="none", pre=None, need=("x", "weight", "bias"), stream=None):
+    """The gradients (dx, dweight, dbias) of ``linear`` for the output gradient
+    dy [..., out]; those not named in ``need`` are None.  pre is what
+    ``linear`` returned with save_pre (not read with act "none").  The
+    residual's gradient is dy itself.  Enqueued on the stream."""
+    import torch
+    _on_device(dy, "dy")
+    if weight.dim() != 2:
+        raise ValueError("weight: must be 2-D")
+    need = tuple(need)
+    if not need or set(need) - {"x", "weight", "bias"}:
+        raise ValueError('need: must name some of "x", "weight" and "bias"')
+    N, K = weight.shape
+    if N < 1 or K < 1:
+        raise ValueError("weight: must not be empty")
+    a = pic_linear_grad_args()
+    a.act = _linear_act(act)
+    a.dtype = _dtype_code(dy, "dy")
+    M = x.numel() // K
+    a.rows, a.in_features, a.out_features = M, K, N
+    a.dy, a.lddy = _rows(dy, "dy", N, dy, M)
+    a.x, a.ldx = _rows(x, "x", K, dy)
+    a.w, a.ldw = _rows(weight, "weight", K, dy)
+    if a.act != PIC_ACT_NONE:
+        if pre is None:
+            raise ValueError(f"pre: needed for act {act!r}")
+        a.pre, a.ldpre = _rows(pre, "pre", N, dy, M)
+    dx = dw = db = None
+    with _Allocating(stream):
+        if "x" in need:
+            dx = torch.empty(x.shape, dtype=dy.dtype, device=dy.device)
+            a.dx, a.lddx = dx.data_ptr(), K
+        if "weight" in need:
+            dw = torch.empty((N, K), dtype=dy.dtype, device=dy.device)
+            a.dw, a.lddw = dw.data_ptr(), K
+        if "bias" in need:
+            db = torch.empty(N, dtype=dy.dtype, device=dy.device)
+            a.db = db.data_ptr()
+        if M > 0 or "weight" in need or "bias" in need:
+            _call_with_workspace("pic_linear_backward", a, dy.device)
+    return dx, dw, db
+
+
+def linear_check(stream=None):
+    """Synchronises the stream; raises if a bounded device-side wait of the
+    linear layer's kernels gave up since the last check."""
+    rc = load_library().pic_linear_check(_stream_ptr(stream))
+    if rc != PIC_OK:
+        raise PicError(rc, "pic_linear_check")
+
+
+class GradClip:
+    """The global norm of a fixed list of gradient tensors, and their clipping:
+    in place, or to the tensors of ``out`` (same sizes and types).  The handle
+    keeps the tensors; each must be contiguous, float32, float16 or bfloat16,
+    and on the current device."""
+
+    def __init__(self, tensors, out=None):
+        import torch
+        self.handle = None
+        tensors = list(tensors)
+        outs = tensors if out is None else list(out)
+        if len(outs) != len(tensors):
+            raise ValueError(f"out: {len(outs)} tensors, expected {len(tensors)}")
+        table = (pic_clip_tensor * max(len(tensors), 1))()
+        for i, (t, o) in enumerate(zip(tensors, outs)):
+            for name, v in ((f"tensors[{i}]", t), (f"out[{i}]", o)):
+                _on_device(v, name)
+                if not v.is_contiguous():
+                    raise ValueError(f"{name}: must be contiguous")
+            if o.dtype != t.dtype or o.numel() != t.numel():
+                raise ValueError(f"out[{i}]: {o.numel()} of {o.dtype}, expected {t.numel()} of {t.dtype}")
+            table[i] = pic_clip_tensor(t.data_ptr(), o.data_ptr(), t.numel(),
+                                       _dtype_code(t, f"tensors[{i}]"))
+        self._tensors, self._outs = tensors, outs
+        self.device = torch.cuda.current_device()
+        h = _P()
+        rc = load_library().pic_clip_create(table, len(tensors), ctypes.byref(h))
+        if rc != PIC_OK:
+            raise PicError(rc, "pic_clip_create")
+        self.handle = h.value
+
+    def clip(self, max_norm: float, stream=None):
+        """Scales the gradients by min(1, max_norm / (norm + 1e-6)); returns
+        norm, a float32 scalar on the device.  Enqueued on the stream."""
+        import torch
+        if self.handle is None:
+            raise ValueError("GradClip: closed")
+        with _Allocating(stream):
+            norm = torch.empty((), dtype=torch.float32, device=torch.device("cuda", self.device))
+            rc = load_library().pic_clip(self.handle, max_norm, norm.data_ptr(), _current_stream())
+        if rc != PIC_OK:
+            raise PicError(rc, "pic_clip")
+        return norm
+
+    def close(self):
+        if self.handle:
+            load_library().pic_clip_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 # ---- convenience wrapper over torch tensors --------------------------------
