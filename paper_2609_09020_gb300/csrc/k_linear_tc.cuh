@@ -1,0 +1,412 @@
+// k_linear_tc.cuh -- matrix products of 16-bit operands on the tensor cores,
+// with the linear layer's epilogue (include/pic_linear.h).
+//
+// C[i][j] = sum_k A(i, k) B(j, k): a CTA (CG = 1) or a pair of CTAs (CG = 2)
+// computes tiles of CG x 128 rows and BN columns, one after another, in fp32
+// accumulators in tensor memory.  Three kinds of warps work side by side:
+//   warp 0      one thread keeps a ring of STAGES slices of A and B (64 of K)
+//               filled by TMA; what lies outside the matrices reads as zero
+//   warp 1      one thread issues the MMAs, 16 of K each
+//   warps 2..5  the epilogue: accumulators, bias, pre, activation, residual,
+//               rounding, and out through shared memory and TMA stores (or
+//               plain stores where rows do not start on 16-byte boundaries)
+// There are two sets of accumulators, so that a tile's epilogue runs under the
+// next tile's MMAs.  An operand may be contiguous along K or along its rows
+// (dz and x in dw = dz^T x): TMA then brings blocks of 64 rows x 64 of K and
+// the MMA reads them transposed.  A product that has fewer tiles than the GPU
+// has SMs, or too few for whole rounds, is cut along K: each part's
+// accumulators go to the workspace in fp32, and a second kernel adds the parts
+// in order and runs the epilogue.
+//
+// Each wait is bounded: a thread whose wait runs out raises its CTA's abort
+// flag and the status word, and every role skips what is left.
+#pragma once
+
+#include "linear.cuh"
+#include "linear_ptx.cuh"
+
+namespace pic {
+namespace lin {
+
+struct alignas(64) TcMaps {
+  CUtensorMap a, b, y, pre;
+};
+
+struct TcParams {
+  Product p;             // K in elements; a and b only through the maps
+  long long tiles_i, tiles_j;
+  long long work;        // tiles x splits
+  int splits;
+  int k_blocks;          // slices of 64 in all of K
+  int part_blocks;       // slices of one part
+  int a_mn, b_mn;        // the operand is contiguous along its rows
+  int store_tma;         // y (and pre) go out by TMA
+  float* parts;          // fp32 parts, or null: the epilogue runs in the kernel
+  int* status;
+  unsigned spin_limit;
+};
+
+constexpr int kEpiWarps = 4;
+constexpr int kTcThreads = 64 + 32 * kEpiWarps;
+constexpr int kSlice = 64;           // K of one stage
+constexpr int kPanelBytes = 32 * 128;  // 32 rows x 64 columns of a 16-bit type
+constexpr int kGroupRows = 2048;     // rows of A that neighbouring tiles share the columns of B for
+
+template <int CG, int BN>
+struct TcShape {
+  static constexpr int kRows = 128 * CG;
+  static constexpr int kBRows = BN / CG;  // rows of B that one CTA holds
+  static constexpr int kABytes = 128 * 128, kBBytes = kBRows * 128;
+  static constexpr int kStageBytes = kABytes + kBBytes;
+  // BN = 64: two CTAs on an SM, else one
+  static constexpr int kStages = BN == 256 ? 6 : BN == 128 ? 5 : 3;
+  static constexpr int kOffPanels = kStages * kStageBytes;
+  static constexpr int kOffBars = kOffPanels + kEpiWarps * 2 * kPanelBytes;
+  static constexpr int kBars = 2 * kStages + 4 + 1;
+  static constexpr int kSmem = kOffBars + kBars * 8 + 16 + 1024;  // 1024: the base is rounded up
+  static constexpr int kTmemCols = 2 * BN;
+};
+
+// Row and column tile of tile t: groups of kGroupRows rows, columns outermost
+// within a group, so that the group's rows of A and one column block of B stay in L2.
+template <int ROWS>
+__device__ __forceinline__ void tile_place(long long t, long long tiles_i, long long tiles_j, long long& ti,
+                                           long long& tj) {
+  constexpr int G = kGroupRows / ROWS;
+  const long long group = t / (G * tiles_j), first = group * G;
+  const long long size = min(static_cast<long long>(G), tiles_i - first);
+  const long long in = t - group * G * tiles_j;
+  ti = first + in % size;
+  tj = in / size;
+}
+
+template <typename T>
+struct IsHalf {
+  static constexpr bool value = false;
+};
+template <>
+struct IsHalf<__half> {
+  static constexpr bool value = true;
+};
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack2_16(float lo, float hi);
+template <>
+__device__ __forceinline__ uint32_t pack2_16<__half>(float lo, float hi) {
+  return tc::pack_f16x2(lo, hi);
+}
+template <>
+__device__ __forceinline__ uint32_t pack2_16<__nv_bfloat16>(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+template <typename T>
+__device__ __forceinline__ float2 unpack2_16(uint32_t v);
+template <>
+__device__ __forceinline__ float2 unpack2_16<__half>(uint32_t v) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&v));
+}
+template <>
+__device__ __forceinline__ float2 unpack2_16<__nv_bfloat16>(uint32_t v) {
+  return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t idesc_of(int M, int N, bool a_mn, bool b_mn) {
+  return tc::idesc_16(M, N, !IsHalf<T>::value, a_mn, b_mn);
+}
+
+// One warp's panel (32 rows from row0, 64 columns from col0; this lane's row in
+// v) to global memory: into the panel buffer, swizzled as TMA and the banks
+// like it, then one TMA store, or two columns of a row per lane and row.
+template <typename T>
+__device__ __forceinline__ void put_panel(const uint32_t (&v)[32], uint32_t buf, int lane, long long row0, long long col0,
+                                          const Product& p, void* out, long long ld, const CUtensorMap* map,
+                                          bool by_tma) {
+#pragma unroll
+  for (int c = 0; c < 8; ++c)
+    tc::sts128(buf + lane * 128 + ((c ^ (lane & 7)) * 16), v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+  if (by_tma) {
+    tc::fence_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      tc::tma_store_2d(map, static_cast<int>(col0), static_cast<int>(row0), buf);
+      tc::bulk_commit();
+    }
+    return;
+  }
+  __syncwarp();
+  const long long col = col0 + 2 * lane;
+  T* o = static_cast<T*>(out) + row0 * ld + col;
+  const bool whole = ((reinterpret_cast<uintptr_t>(out) | static_cast<uintptr_t>(ld * 2)) & 3) == 0;
+  const int rows = static_cast<int>(min(32LL, p.I - row0));
+  for (int r = 0; r < rows; ++r, o += ld) {
+    uint32_t w;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(buf + r * 128 + (((lane >> 2) ^ (r & 7)) * 16) + (lane & 3) * 4));
+    if (whole && col + 1 < p.J)
+      *reinterpret_cast<uint32_t*>(o) = w;
+    else {
+      const T* h = reinterpret_cast<const T*>(&w);
+      if (col < p.J) o[0] = h[0];
+      if (col + 1 < p.J) o[1] = h[1];
+    }
+  }
+  __syncwarp();
+}
+
+// Adds 64 columns (or those of them that exist) of the bias or of a residual row to v.
+template <typename T>
+__device__ __forceinline__ void add_row(float (&v)[64], const T* r, int cols) {
+  if (cols >= 64 && (reinterpret_cast<uintptr_t>(r) & 15) == 0) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const uint4 q = *reinterpret_cast<const uint4*>(r + 8 * c);
+      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 f = unpack2_16<T>(w[e]);
+        v[8 * c + 2 * e] += f.x;
+        v[8 * c + 2 * e + 1] += f.y;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < 64; ++c)
+      if (c < cols) v[c] += to_f32(r[c]);
+  }
+}
+
+template <typename T, int CG, int BN>
+__global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kTcThreads, BN == 64 ? 2 : 1)
+    tc_kernel(const __grid_constant__ TcParams q, const __grid_constant__ TcMaps maps) {
+  using S = TcShape<CG, BN>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = tc::smem_addr(smem_raw);
+  uint8_t* smem = smem_raw + ((1024 - (raw & 1023)) & 1023);
+  const uint32_t base = tc::smem_addr(smem);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = CG == 2 ? tc::cluster_rank() : 0;
+  const uint32_t bars = base + S::kOffBars;
+  const uint32_t bar_full = bars, bar_empty = bars + 8 * S::kStages, bar_acc = bar_empty + 8 * S::kStages,
+                 bar_free = bar_acc + 16, bar_drain = bar_free + 16;
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + S::kOffBars + 8 * S::kBars);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::kOffBars + 8 * S::kBars + 4);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S::kStages; ++s) {
+      tc::mbar_init(bar_full + 8 * s, 1);
+      tc::mbar_init(bar_empty + 8 * s, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      tc::mbar_init(bar_acc + 8 * b, 1);
+      tc::mbar_init(bar_free + 8 * b, kEpiWarps * CG);
+    }
+    tc::mbar_init(bar_drain, 1);
+    *abort_flag = 0;
+    tc::fence_mbar_init();
+  }
+  if (warp == 1) tc::tmem_alloc_cg<CG>(tc::smem_addr(tmem_slot), S::kTmemCols);
+  tc::tc_fence_before();
+  __syncthreads();
+  if constexpr (CG == 2) tc::cluster_sync();
+  tc::tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
+    if (tc::mbar_test_wait(bar, parity)) return true;
+    for (uint32_t i = 0; i < q.spin_limit; ++i) {
+      if (tc::mbar_try_wait(bar, parity)) return true;
+      if ((i & 63u) == 63u) {
+        if (*abort_flag) return false;
+        if (i > 4096) __nanosleep(64);
+      }
+    }
+    *abort_flag = 1;
+    atomicOr(q.status, 1);
+    return false;
+  };
+  const long long first = blockIdx.x / CG, step = gridDim.x / CG;
+  // slices of work item w
+  auto part = [&](long long w, int& k0, int& k1) {
+    k0 = static_cast<int>(w % q.splits) * q.part_blocks;
+    k1 = min(q.k_blocks, k0 + q.part_blocks);
+  };
+
+  if (warp == 0) {
+    if (tc::elect_one()) {
+      const uint32_t lead_full = CG == 2 ? tc::map_rank(bar_full, 0) : bar_full;
+      int s = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (long long w = first; w < q.work && ok; w += step) {
+        long long ti, tj;
+        tile_place<S::kRows>(w / q.splits, q.tiles_i, q.tiles_j, ti, tj);
+        const int i0 = static_cast<int>(ti * S::kRows + rank * 128), j0 = static_cast<int>(tj * BN + rank * S::kBRows);
+        int k0, k1;
+        part(w, k0, k1);
+        for (int kb = k0; kb < k1; ++kb) {
+          if (!(ok = wait(bar_empty + 8 * s, phase ^ 1))) break;
+          if (rank == 0) tc::mbar_arrive_expect_tx(bar_full + 8 * s, CG * S::kStageBytes);
+          const uint32_t sa = base + s * S::kStageBytes, sb = sa + S::kABytes, bar = lead_full + 8 * s;
+          const int k = kb * kSlice;
+          if (q.a_mn) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) tc::tma_load_2d<CG == 2>(sa + c * 8192, &maps.a, i0 + 64 * c, k, bar);
+          } else {
+            tc::tma_load_2d<CG == 2>(sa, &maps.a, k, i0, bar);
+          }
+          if (q.b_mn) {
+#pragma unroll
+            for (int c = 0; c < S::kBRows / 64; ++c)
+              tc::tma_load_2d<CG == 2>(sb + c * 8192, &maps.b, j0 + 64 * c, k, bar);
+          } else {
+            tc::tma_load_2d<CG == 2>(sb, &maps.b, k, j0, bar);
+          }
+          if (++s == S::kStages) s = 0, phase ^= 1;
+        }
+      }
+      // aborted: the copies in flight land before shared memory goes away (a
+      // slot that was never filled is passed at once).  The other CTA of a pair
+      // may have started some that this one did not expect: both linger for
+      // far longer than a copy takes.
+      if (!ok) {
+        for (int i = 0; i < S::kStages; ++i) {
+          if (--s < 0) s = S::kStages - 1, phase ^= 1;
+          for (uint32_t n = 0; rank == 0 && n < q.spin_limit && !tc::mbar_try_wait(bar_full + 8 * s, phase); ++n) {
+          }
+        }
+        if (CG == 2) __nanosleep(200000);
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (rank == 0 && tc::elect_one()) {
+      constexpr uint32_t kM = 128 * CG;
+      const uint32_t idesc = idesc_of<T>(kM, BN, q.a_mn != 0, q.b_mn != 0);
+      // one MMA takes 16 of K: 32 bytes of a K-major row, 16 rows of an MN-major block
+      const uint32_t a_step = q.a_mn ? 2048 : 32, b_step = q.b_mn ? 2048 : 32;
+      int s = 0, buf = 0;
+      uint32_t phase = 0, free_phase = 0;
+      bool ok = true;
+      for (long long w = first; w < q.work && ok; w += step) {
+        if (!(ok = wait(bar_free + 8 * buf, free_phase ^ 1))) break;
+        tc::tc_fence_after();
+        int k0, k1;
+        part(w, k0, k1);
+        const uint32_t d = tmem + buf * BN;
+        for (int kb = k0; kb < k1; ++kb) {
+          if (!(ok = wait(bar_full + 8 * s, phase))) break;
+          tc::tc_fence_after();
+          const uint32_t sa = base + s * S::kStageBytes, sb = sa + S::kABytes;
+#pragma unroll
+          for (int kk = 0; kk < kSlice / 16; ++kk)
+            tc::mma_16<CG>(d, tc::smem_desc_sw128(sa + kk * a_step, 8192, 1024),
+                           tc::smem_desc_sw128(sb + kk * b_step, 8192, 1024), idesc, (kb > k0 || kk > 0) ? 1u : 0u);
+          tc::mma_commit_cg<CG>(bar_empty + 8 * s);
+          if (++s == S::kStages) s = 0, phase ^= 1;
+        }
+        if (!ok) break;
+        tc::mma_commit_cg<CG>(bar_acc + 8 * buf);
+        if (++buf == 2) buf = 0, free_phase ^= 1;
+      }
+      if (!ok) {  // aborted: MMAs in flight still read shared memory
+        tc::mma_commit_cg<CG>(bar_drain);
+        for (uint32_t n = 0; n < q.spin_limit && !tc::mbar_try_wait(bar_drain, 0); ++n) {
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    const int quarter = warp & 3;  // the 32 lanes of tensor memory that this warp may read
+    const Product& p = q.p;
+    const uint32_t panels = base + S::kOffPanels + quarter * 2 * kPanelBytes;
+    const uint32_t lead_free = CG == 2 ? tc::map_rank(bar_free, 0) : bar_free;
+    int buf = 0, pb = 0;
+    uint32_t phase = 0;
+    for (long long w = first; w < q.work; w += step) {
+      long long ti, tj;
+      tile_place<S::kRows>(w / q.splits, q.tiles_i, q.tiles_j, ti, tj);
+      const long long row0 = ti * S::kRows + rank * 128 + quarter * 32, j0 = tj * BN;
+      if (!__all_sync(0xffffffffu, wait(bar_acc + 8 * buf, phase))) break;
+      tc::tc_fence_after();
+      const uint32_t d = tmem + buf * BN + (static_cast<uint32_t>(quarter * 32) << 16);
+      for (int c0 = 0; c0 < BN; c0 += 64) {
+        uint32_t raw_acc[64];
+        tc::tmem_ld64_wait(d + c0, raw_acc);
+        if (c0 + 64 == BN) {
+          tc::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            if constexpr (CG == 2)
+              tc::mbar_arrive_cluster(lead_free + 8 * buf);
+            else
+              tc::mbar_arrive(bar_free + 8 * buf);
+          }
+        }
+        if (q.parts) {
+          // part w, panel c0 / 64, this warp's 32 rows: [16][32 lanes][4 columns]
+          float4* o = reinterpret_cast<float4*>(q.parts) +
+                      ((w * CG + rank) * (BN / 64) + c0 / 64) * (128 * 16) + quarter * (32 * 16) + lane;
+#pragma unroll
+          for (int c = 0; c < 16; ++c)
+            o[c * 32] = make_float4(__uint_as_float(raw_acc[4 * c]), __uint_as_float(raw_acc[4 * c + 1]),
+                                    __uint_as_float(raw_acc[4 * c + 2]), __uint_as_float(raw_acc[4 * c + 3]));
+          continue;
+        }
+        if (row0 >= p.I || j0 + c0 >= p.J) continue;  // nothing of this panel is inside
+        float v[64];
+#pragma unroll
+        for (int c = 0; c < 64; ++c) v[c] = __uint_as_float(raw_acc[c]);
+        const int cols = static_cast<int>(min(64LL, p.J - j0 - c0));
+        if (p.bias) add_row<T>(v, static_cast<const T*>(p.bias) + j0 + c0, cols);
+        uint32_t out[32];
+        if (p.pre) {
+#pragma unroll
+          for (int c = 0; c < 32; ++c) out[c] = pack2_16<T>(v[2 * c], v[2 * c + 1]);
+          if (lane == 0) tc::bulk_wait_read<1>();  // the buffer's last store has been read
+          __syncwarp();
+          put_panel<T>(out, panels + pb * kPanelBytes, lane, row0, j0 + c0, p, p.pre, p.ldpre, &maps.pre, q.store_tma);
+          pb ^= 1;
+        }
+        if (p.act == PIC_ACT_GELU) {
+#pragma unroll
+          for (int c = 0; c < 64; ++c) v[c] = act_value<false>(v[c], PIC_ACT_GELU);
+        } else if (p.act == PIC_ACT_RELU) {
+#pragma unroll
+          for (int c = 0; c < 64; ++c) v[c] = relu_nan(v[c]);
+        }
+        if (p.residual && row0 + lane < p.I)
+          add_row<T>(v, static_cast<const T*>(p.residual) + (row0 + lane) * p.ldr + j0 + c0, cols);
+#pragma unroll
+        for (int c = 0; c < 32; ++c) out[c] = pack2_16<T>(v[2 * c], v[2 * c + 1]);
+        if (lane == 0) tc::bulk_wait_read<1>();
+        __syncwarp();
+        put_panel<T>(out, panels + pb * kPanelBytes, lane, row0, j0 + c0, p, p.y, p.ldy, &maps.y, q.store_tma);
+        pb ^= 1;
+      }
+      if (++buf == 2) buf = 0, phase ^= 1;
+    }
+    if (lane == 0) tc::bulk_wait_all();
+    __syncwarp();
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  if constexpr (CG == 2) tc::cluster_sync();
+  tc::tc_fence_after();
+  if (warp == 1) tc::tmem_dealloc_cg<CG>(tmem, S::kTmemCols);
+}
+
+// The kernel for tiles of bn columns: 64 and 128 by one CTA, 256 by a pair.
+const void* tc_kernel_f16(int bn);
+const void* tc_kernel_bf16(int bn);
+
+template <typename T>
+const void* tc_kernel_of(int bn) {
+  if (bn == 256) return reinterpret_cast<const void*>(tc_kernel<T, 2, 256>);
+  if (bn == 128) return reinterpret_cast<const void*>(tc_kernel<T, 1, 128>);
+  return reinterpret_cast<const void*>(tc_kernel<T, 1, 64>);
+}
+
+}  // namespace lin
+}  // namespace pic

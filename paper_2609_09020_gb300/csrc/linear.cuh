@@ -95,6 +95,11 @@ inline int split_count(long long tiles, long long K, long long step, long long t
 long long simt_workspace(const Product& p);
 int simt_product(const Product& p, int dtype, void* ws, cudaStream_t s);
 
+// 16-bit types on the tensor cores; `status` is set to 1 if a bounded wait
+// (at most spin_limit polls) gives up.
+long long tc_workspace(const Product& p);
+int tc_product(const Product& p, int dtype, void* ws, int* status, unsigned spin_limit, cudaStream_t s);
+
 // dz[i][j] = dy act'(z), rounded (dz null: not written), and parts[b][j], the
 // column sums of the unrounded dz over the rows of block b (parts null: none).
 struct GradAct {

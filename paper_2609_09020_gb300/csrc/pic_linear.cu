@@ -75,6 +75,36 @@ int device_status() {
   return k == 1 ? PIC_OK : PIC_ERR_UNSUPPORTED;
 }
 
+// The word that a kernel sets when one of its bounded waits gives up; its
+// address on each device is looked up once.
+__device__ int lin_status;
+
+int* status_word() {
+  static std::atomic<int*> known[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
+  int* p = known[dev].load(std::memory_order_relaxed);
+  if (!p) {
+    void* v = nullptr;
+    if (cudaGetSymbolAddress(&v, lin_status) != cudaSuccess) return nullptr;
+    p = static_cast<int*>(v);
+    known[dev].store(p, std::memory_order_relaxed);
+  }
+  return p;
+}
+
+// Workspace bytes of a product, and the product: 16-bit types run on the tensor cores.
+long long product_workspace(const Product& p, int dtype) {
+  return dtype == PIC_DTYPE_F32 ? pic::lin::simt_workspace(p) : pic::lin::tc_workspace(p);
+}
+
+int product(const Product& p, int dtype, void* ws, cudaStream_t s) {
+  if (dtype == PIC_DTYPE_F32) return pic::lin::simt_product(p, dtype, ws, s);
+  int* status = status_word();
+  if (!status) return PIC_ERR_CUDA;
+  return pic::lin::tc_product(p, dtype, ws, status, pic::kWaitPolls, s);
+}
+
 // Hands out 256-byte aligned pieces of a workspace; with a null base it only
 // counts.
 struct Arena {
@@ -100,8 +130,8 @@ Product forward_product(const pic_linear_args& a) {
 int forward(const pic_linear_args& a, Arena& ws, bool launch, cudaStream_t s) {
   if (a.rows == 0) return PIC_OK;
   const Product p = forward_product(a);
-  void* w = ws.take(pic::lin::simt_workspace(p));
-  return launch ? pic::lin::simt_product(p, a.dtype, w, s) : PIC_OK;
+  void* w = ws.take(product_workspace(p, a.dtype));
+  return launch ? product(p, a.dtype, w, s) : PIC_OK;
 }
 
 int zero_rows(void* p, long long ld, long long rows, long long cols, int dtype, cudaStream_t s) {
@@ -124,7 +154,7 @@ int backward(const pic_linear_grad_args& a, Arena& ws, bool launch, cudaStream_t
   long long lddz = a.lddy;
   const bool own_dz = a.act != PIC_ACT_NONE && products;
   if (own_dz) {
-    lddz = N;
+    lddz = (N + 7) / 8 * 8;  // rows of 16-bit values on 16-byte boundaries
     dz = ws.take(M * lddz * static_cast<long long>(elem_bytes(a.dtype)));
   }
   const long long blocks = pic::lin::grad_act_blocks(M, N);
@@ -141,8 +171,8 @@ int backward(const pic_linear_grad_args& a, Arena& ws, bool launch, cudaStream_t
     p.b = a.w, p.b_j = 1, p.b_k = a.ldw;
     p.I = M, p.J = K, p.K = N;
     p.y = a.dx, p.ldy = a.lddx, p.act = PIC_ACT_NONE;
-    void* w = ws.take(pic::lin::simt_workspace(p));
-    if (launch && (rc = pic::lin::simt_product(p, a.dtype, w, s)) != PIC_OK) return rc;
+    void* w = ws.take(product_workspace(p, a.dtype));
+    if (launch && (rc = product(p, a.dtype, w, s)) != PIC_OK) return rc;
   }
   if (a.dw) {
     Product p{};
@@ -150,8 +180,8 @@ int backward(const pic_linear_grad_args& a, Arena& ws, bool launch, cudaStream_t
     p.b = a.x, p.b_j = 1, p.b_k = a.ldx;
     p.I = N, p.J = K, p.K = M;
     p.y = a.dw, p.ldy = a.lddw, p.act = PIC_ACT_NONE;
-    void* w = ws.take(pic::lin::simt_workspace(p));
-    if (launch && (rc = pic::lin::simt_product(p, a.dtype, w, s)) != PIC_OK) return rc;
+    void* w = ws.take(product_workspace(p, a.dtype));
+    if (launch && (rc = product(p, a.dtype, w, s)) != PIC_OK) return rc;
   }
   return PIC_OK;
 }
@@ -194,11 +224,16 @@ int pic_linear_backward(const pic_linear_grad_args* a, void* workspace, size_t w
 }
 
 int pic_linear_check(void* stream) {
-  if (cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  int* status = status_word();
+  int flag = 0;
+  if (!status || cudaMemcpyAsync(&flag, status, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess ||
+      cudaStreamSynchronize(s) != cudaSuccess ||
+      (flag && (cudaMemsetAsync(status, 0, sizeof(int), s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess))) {
     cudaGetLastError();
     return PIC_ERR_CUDA;
   }
-  return PIC_OK;
+  return flag ? PIC_ERR_TIMEOUT : PIC_OK;
 }
 
 }  // extern "C"

@@ -104,7 +104,8 @@ def test_strides(size, pad, shift, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 @pytest.mark.parametrize("size", [(20000, 64, 64), (9000, 40, 3), (70001, 8, 16), (4096, 512, 384),
-                                  (600, 4096, 200), (1500, 1536, 1600)], ids=str)
+                                  (600, 4096, 200), (1500, 1536, 1600), (2500, 328, 2600), (520, 2500, 2600),
+                                  (2305, 2304, 2311)], ids=str)
 def test_larger(size, dtype):
     from paper_2609_09020_gb300 import pic
     M, K, N = size
