@@ -55,9 +55,15 @@ int pic_clip_create(const pic_clip_tensor *tensors, int n, pic_clipper **out);
  * outs.  max_norm >= 0; infinity clips nothing (tensors clipped in place are
  * then only read).  Calls with one handle must not overlap on the GPU.
  * Errors: PIC_ERR_INVALID_ARG (NULL or misaligned pointers, max_norm negative
- * or NaN, a current device other than the handle's), PIC_ERR_CUDA.
+ * or NaN, a current device other than the handle's), PIC_ERR_CUDA.  The launch
+ * is cooperative: all its blocks are on the GPU at once.
  */
 int pic_clip(pic_clipper *c, float max_norm, float *norm, void *stream);
+
+/* Synchronises `stream`; PIC_OK if the blocks of every launch of this handle
+ * since the last check met in time, PIC_ERR_TIMEOUT if those of one did not (its
+ * norm is NaN then, and its outs are not all written), PIC_ERR_CUDA. */
+int pic_clip_check(pic_clipper *c, void *stream);
 
 void pic_clip_destroy(pic_clipper *c);
 

@@ -1,10 +1,20 @@
 // k_clip.cu -- the global gradient norm and clipping (include/pic_clip.h).
-// The handle cuts its tensors into chunks of kChunk elements.  Every thread
-// block of the first kernel sums the squares of its chunks: fp32 within a
-// thread's part of a chunk (at most kChunk / kThreads squares), fp64 from
-// there on.  The blocks of the second kernel each add the blocks' sums in the
-// same order, and scale their chunks: no atomics, one result.
+//
+// One launch, bound by memory: every element is read for the norm, and read
+// again and written for the clipping.  The handle cuts its tensors (those that
+// follow one another in memory joined first) into pieces of a few KB, and every
+// warp takes every so many-th piece: with one piece's eight 16-byte loads per
+// lane in flight in each of 32 warps, an SM has 128 KB under way.  Between the
+// two passes all blocks (the launch is cooperative: all are resident) meet
+// once, and each adds the blocks' sums in the same order: no atomics on values,
+// one result.  The second pass runs backwards, so that it begins with what the
+// L2 cache still holds, and with what the warp still has in registers (its last
+// 4 KB): up to 19 MB in all are read only once.
+//
+// Sums: a lane adds at most 64 squares in fp32 and goes on in fp64; where such a
+// sum leaves the range in which fp32 is good, it is added again in fp64.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 #include <new>
@@ -13,7 +23,7 @@
 #include "linear.cuh"
 #include "pic_clip.h"
 
-struct ClipChunk {
+struct ClipPiece {
   const void* grad;
   void* out;
   int count;
@@ -22,10 +32,10 @@ struct ClipChunk {
 
 struct pic_clipper {
   int device;
-  int n_chunks;
+  int n_pieces;
   int blocks;
-  ClipChunk* chunks;  // device
-  double* parts;      // device, [blocks]
+  ClipPiece* pieces;  // device
+  double* parts;      // device, [blocks]; then the barrier's counter and the status word
 };
 
 namespace {
@@ -34,80 +44,234 @@ using pic::lin::from_f32;
 using pic::lin::to_f32;
 
 constexpr int kThreads = 512;
-constexpr int kChunk = 32768;
-constexpr int kBlocks = 304;
+constexpr int kWarps = kThreads / 32;
+constexpr int kVecs = 8;                      // 16-byte loads of a lane at a time
+constexpr int kStep = 32 * kVecs * 16;        // bytes of a warp's step
+constexpr int kMaxBlocks = 304;               // two on each SM
+constexpr long long kLarge = 1LL << 30;       // from here on a piece is four steps: shorter tables
 
-__device__ __forceinline__ double block_sum(double v) {
-  __shared__ double sums[kThreads / 32];
+struct ClipParams {
+  const ClipPiece* pieces;
+  int n;
+  double* parts;
+  unsigned long long* arrived;
+  int* status;
+  float max_norm;
+  float* norm;
+  unsigned spin_limit;
+};
+
+// The elements of one 16-byte load.
+template <typename T>
+struct Vec {
+  static constexpr int kN = 16 / sizeof(T);
+  static __device__ __forceinline__ void get(const uint4& q, float (&f)[kN]) {
+    const T* t = reinterpret_cast<const T*>(&q);
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  if (threadIdx.x % 32 == 0) sums[threadIdx.x / 32] = v;
-  __syncthreads();
-  double t = 0.0;
-  for (int i = 0; i < kThreads / 32; ++i) t += sums[i];
-  __syncthreads();
-  return t;
-}
+    for (int i = 0; i < kN; ++i) f[i] = to_f32(t[i]);
+  }
+};
+
+// A piece as a lane sees it: `head` elements before the first 16-byte boundary,
+// whole vectors, `tail` elements.
+template <typename T>
+struct Cut {
+  const T* grad;
+  T* out;
+  int head, vecs, tail;
+  __device__ __forceinline__ explicit Cut(const ClipPiece& p) {
+    grad = static_cast<const T*>(p.grad);
+    out = static_cast<T*>(p.out);
+    const int to_next = static_cast<int>((16 - (reinterpret_cast<uintptr_t>(p.grad) & 15)) & 15) / static_cast<int>(sizeof(T));
+    head = min(to_next, p.count);
+    vecs = (p.count - head) / Vec<T>::kN;
+    tail = p.count - head - vecs * Vec<T>::kN;
+  }
+  // the odd element of this lane, or null: lanes 0..15 the head's, 16..31 the tail's
+  __device__ __forceinline__ int odd(int lane) const {
+    if (lane < 16) return lane < head ? lane : -1;
+    return lane - 16 < tail ? head + vecs * Vec<T>::kN + lane - 16 : -1;
+  }
+};
 
 template <typename T>
-__device__ double thread_squares(const ClipChunk& c) {
-  const T* g = static_cast<const T*>(c.grad);
-  float s = 0.0f;
-  for (int i = threadIdx.x; i < c.count; i += kThreads) {
-    const float v = to_f32(g[i]);
-    s = fmaf(v, v, s);
+__device__ __forceinline__ void load_step(uint4 (&q)[kVecs], const Cut<T>& c, int first, int lane) {
+  const uint4* v = reinterpret_cast<const uint4*>(c.grad + c.head);
+#pragma unroll
+  for (int u = 0; u < kVecs; ++u) {
+    const int i = first + u * 32 + lane;
+    q[u] = i < c.vecs ? __ldcg(v + i) : make_uint4(0, 0, 0, 0);
   }
-  // fp32 left its range: squares below 2^-126 lose bits (2^-90: none that
-  // matter beside others of the sum's size), above 2^128 it is infinite
-  if (s < 0x1p+127f && (s > 0x1p-90f)) return s;
+}
+
+// fp32 is good where no square of weight was lost below its range and the sum
+// did not leave it above; a sum of nothing but zeros is good too.
+__device__ __forceinline__ bool fp32_held(float s, bool any) { return (s > 0x1p-90f && s < 0x1p+127f) || !any; }
+
+template <typename T>
+__device__ __forceinline__ double squares(const ClipPiece& p, int lane, uint4 (&q)[kVecs]) {
+  const Cut<T> c(p);
   double d = 0.0;
-  for (int i = threadIdx.x; i < c.count; i += kThreads) {
-    const double v = to_f32(g[i]);
-    d = fma(v, v, d);
+  const int o = c.odd(lane);
+  if (o >= 0) {
+    const double v = to_f32(c.grad[o]);
+    d = v * v;
+  }
+  for (int first = 0; first < c.vecs; first += 32 * kVecs) {
+    load_step(q, c, first, lane);
+    float s = 0.0f;
+    uint32_t any = 0;
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) {
+      float f[Vec<T>::kN];
+      Vec<T>::get(q[u], f);
+      any |= q[u].x | q[u].y | q[u].z | q[u].w;
+#pragma unroll
+      for (int i = 0; i < Vec<T>::kN; ++i) s = fmaf(f[i], f[i], s);
+    }
+    if (fp32_held(s, any != 0)) {
+      d += s;
+    } else {
+#pragma unroll
+      for (int u = 0; u < kVecs; ++u) {
+        float f[Vec<T>::kN];
+        Vec<T>::get(q[u], f);
+        for (int i = 0; i < Vec<T>::kN; ++i) d = fma(static_cast<double>(f[i]), static_cast<double>(f[i]), d);
+      }
+    }
   }
   return d;
 }
 
-__global__ void __launch_bounds__(kThreads) squares_kernel(const ClipChunk* chunks, int n, double* parts) {
-  double d = 0.0;
-  for (int i = blockIdx.x; i < n; i += gridDim.x) {
-    const ClipChunk c = chunks[i];
-    if (c.dtype == PIC_DTYPE_F32)
-      d += thread_squares<float>(c);
-    else if (c.dtype == PIC_DTYPE_F16)
-      d += thread_squares<__half>(c);
+template <typename T>
+__device__ __forceinline__ void store_step(const uint4 (&q)[kVecs], const Cut<T>& c, int first, int lane, float coef) {
+  T* o = c.out + c.head;
+  const bool whole = (reinterpret_cast<uintptr_t>(o) & 15) == 0;
+#pragma unroll
+  for (int u = 0; u < kVecs; ++u) {
+    const int i = first + u * 32 + lane;
+    if (i >= c.vecs) continue;
+    float f[Vec<T>::kN];
+    Vec<T>::get(q[u], f);
+    uint4 r;
+    T* t = reinterpret_cast<T*>(&r);
+#pragma unroll
+    for (int e = 0; e < Vec<T>::kN; ++e) t[e] = from_f32<T>(f[e] * coef);
+    if (whole)
+      __stcs(reinterpret_cast<uint4*>(o) + i, r);
     else
-      d += thread_squares<__nv_bfloat16>(c);
+#pragma unroll
+      for (int e = 0; e < Vec<T>::kN; ++e) o[i * Vec<T>::kN + e] = t[e];
+  }
+}
+
+// held: q is the piece's last step as the first pass left it
+template <typename T>
+__device__ __forceinline__ void scale(const ClipPiece& p, int lane, uint4 (&q)[kVecs], bool held, float coef) {
+  const Cut<T> c(p);
+  const int o = c.odd(lane);
+  if (o >= 0) c.out[o] = from_f32<T>(to_f32(c.grad[o]) * coef);
+  int first = (c.vecs - 1) / (32 * kVecs) * (32 * kVecs);
+  if (c.vecs == 0) return;
+  for (; first >= 0; first -= 32 * kVecs) {
+    if (!held) load_step(q, c, first, lane);
+    held = false;
+    store_step(q, c, first, lane, coef);
+  }
+}
+
+// The sum over the block, in thread 0.  Everything in fp64 is left to as few
+// warps as can be: an SM does two fp64 operations a clock.
+__device__ __forceinline__ double block_sum(double v) {
+  __shared__ double sums[kWarps];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (threadIdx.x % 32 == 0) sums[threadIdx.x / 32] = v;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    v = threadIdx.x < kWarps ? sums[threadIdx.x] : 0.0;
+#pragma unroll
+    for (int o = kWarps / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  }
+  return v;
+}
+
+// All blocks of the launch arrive and leave together; false if the others did
+// not arrive in time.  The counter only ever grows, by gridDim.x a launch.
+__device__ __forceinline__ bool meet(const ClipParams& p) {
+  __shared__ int ok;
+  if (threadIdx.x == 0) {
+    __threadfence();
+    const unsigned long long old = atomicAdd(p.arrived, 1ull);
+    const unsigned long long until = (old / gridDim.x + 1) * gridDim.x;
+    ok = 0;
+    for (unsigned i = 0; i < p.spin_limit; ++i) {
+      unsigned long long now;
+      asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(now) : "l"(p.arrived) : "memory");
+      if (now >= until) {
+        ok = 1;
+        break;
+      }
+      if (i > 4096) __nanosleep(64);
+    }
+    if (!ok) atomicOr(p.status, 1);
+  }
+  __syncthreads();
+  return ok != 0;
+}
+
+__global__ void __launch_bounds__(kThreads, 2) clip_kernel(const ClipParams p) {
+  const int lane = threadIdx.x & 31, stride = gridDim.x * kWarps;
+  const int first = (threadIdx.x >> 5) * gridDim.x + blockIdx.x;
+  uint4 q[kVecs];
+  double d = 0.0;
+  int i = first;
+  for (; i < p.n; i += stride) {
+    const ClipPiece c = p.pieces[i];
+    if (c.dtype == PIC_DTYPE_F32)
+      d += squares<float>(c, lane, q);
+    else if (c.dtype == PIC_DTYPE_F16)
+      d += squares<__half>(c, lane, q);
+    else
+      d += squares<__nv_bfloat16>(c, lane, q);
   }
   d = block_sum(d);
-  if (threadIdx.x == 0) parts[blockIdx.x] = d;
-}
-
-template <typename T>
-__device__ void scale(const ClipChunk& c, float coef) {
-  const T* g = static_cast<const T*>(c.grad);
-  T* o = static_cast<T*>(c.out);
-  for (int i = threadIdx.x; i < c.count; i += kThreads) o[i] = from_f32<T>(to_f32(g[i]) * coef);
-}
-
-__global__ void __launch_bounds__(kThreads) scale_kernel(const ClipChunk* chunks, int n, const double* parts,
-                                                         int n_parts, float max_norm, float* norm_out) {
-  double d = 0.0;
-  for (int i = threadIdx.x; i < n_parts; i += kThreads) d += parts[i];
-  const float norm = static_cast<float>(sqrt(block_sum(d)));
-  if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
-  // not fminf: coef is NaN where norm is
-  float coef = max_norm / (norm + 1e-6f);
-  if (coef > 1.0f || isinf(max_norm)) coef = 1.0f;
-  for (int i = blockIdx.x; i < n; i += gridDim.x) {
-    const ClipChunk c = chunks[i];
-    if (coef == 1.0f && c.grad == c.out) continue;
+  if (threadIdx.x == 0) __stcg(p.parts + blockIdx.x, d);
+  if (!meet(p)) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.norm = __int_as_float(0x7fffffff);
+    return;
+  }
+  __shared__ float coef_s;
+  if (threadIdx.x < 32) {
+    d = 0.0;
+    for (int b = lane; b < gridDim.x; b += 32) d += __ldcg(p.parts + b);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+    if (lane == 0) {
+      const float norm = static_cast<float>(sqrt(d));
+      if (blockIdx.x == 0) *p.norm = norm;
+      // not fminf: coef is NaN where norm is
+      float c = p.max_norm / (norm + 1e-6f);
+      if (c > 1.0f || isinf(p.max_norm)) c = 1.0f;
+      coef_s = c;
+    }
+  }
+  __syncthreads();
+  const float coef = coef_s;
+  bool held = true;
+  for (i -= stride; i >= 0; i -= stride) {
+    const ClipPiece c = p.pieces[i];
+    if (coef == 1.0f && c.grad == c.out) {
+      held = false;
+      continue;
+    }
     if (c.dtype == PIC_DTYPE_F32)
-      scale<float>(c, coef);
+      scale<float>(c, lane, q, held, coef);
     else if (c.dtype == PIC_DTYPE_F16)
-      scale<__half>(c, coef);
+      scale<__half>(c, lane, q, held, coef);
     else
-      scale<__nv_bfloat16>(c, coef);
+      scale<__nv_bfloat16>(c, lane, q, held, coef);
+    held = false;
   }
 }
 
@@ -137,6 +301,50 @@ bool outputs_disjoint(const pic_clip_tensor* t, int n) {
     if (a.out) out_end = std::max(out_end, a.hi);
   }
   return true;
+}
+
+// Tensors that follow one another in memory, gradients and outputs alike, as one.
+std::vector<pic_clip_tensor> joined(const pic_clip_tensor* t, int n) {
+  std::vector<pic_clip_tensor> v;
+  for (int i = 0; i < n; ++i)
+    if (t[i].count > 0) v.push_back(t[i]);
+  std::sort(v.begin(), v.end(), [](const pic_clip_tensor& a, const pic_clip_tensor& b) {
+    return reinterpret_cast<uintptr_t>(a.grad) < reinterpret_cast<uintptr_t>(b.grad);
+  });
+  size_t k = 0;
+  for (size_t i = 1; i < v.size(); ++i) {
+    const long long bytes = v[k].count * elem_bytes(v[k].dtype);
+    if (v[i].dtype == v[k].dtype && v[i].grad == static_cast<const char*>(v[k].grad) + bytes &&
+        v[i].out == static_cast<char*>(v[k].out) + bytes)
+      v[k].count += v[i].count;
+    else
+      v[++k] = v[i];
+  }
+  if (!v.empty()) v.resize(k + 1);
+  return v;
+}
+
+// Pieces of whole steps, on 16-byte boundaries but for a run's first and last;
+// long ones first, which evens out what the warps get.
+std::vector<ClipPiece> cut(const std::vector<pic_clip_tensor>& runs) {
+  long long total = 0;
+  for (const pic_clip_tensor& t : runs) total += t.count * elem_bytes(t.dtype);
+  const long long step = total >= kLarge ? 4 * kStep : kStep;
+  std::vector<ClipPiece> pieces;
+  pieces.reserve(static_cast<size_t>(total / step) + 2 * runs.size());
+  for (const pic_clip_tensor& t : runs) {
+    const long long e = elem_bytes(t.dtype);
+    const long long head = (16 - reinterpret_cast<uintptr_t>(t.grad) % 16) % 16 / e;
+    for (long long at = 0; at < t.count;) {
+      const long long n = std::min(t.count - at, step / e + (at == 0 ? head : 0));
+      pieces.push_back({static_cast<const char*>(t.grad) + at * e, static_cast<char*>(t.out) + at * e,
+                        static_cast<int>(n), t.dtype});
+      at += n;
+    }
+  }
+  std::stable_partition(pieces.begin(), pieces.end(),
+                        [&](const ClipPiece& p) { return p.count * elem_bytes(p.dtype) >= step; });
+  return pieces;
 }
 
 }  // namespace
@@ -169,28 +377,30 @@ int pic_clip_create(const pic_clip_tensor* tensors, int n, pic_clipper** out) {
   if (major != 10 || minor != 3) return PIC_ERR_UNSUPPORTED;
   try {
     if (!outputs_disjoint(tensors, n)) return PIC_ERR_INVALID_ARG;
-    std::vector<ClipChunk> chunks;
-    for (int i = 0; i < n; ++i) {
-      const pic_clip_tensor& t = tensors[i];
-      const long long e = elem_bytes(t.dtype);
-      for (long long at = 0; at < t.count; at += kChunk) {
-        if (chunks.size() >= 0x7fffffffu) return PIC_ERR_INVALID_ARG;
-        chunks.push_back({static_cast<const char*>(t.grad) + at * e, static_cast<char*>(t.out) + at * e,
-                          static_cast<int>(std::min<long long>(kChunk, t.count - at)), t.dtype});
-      }
+    std::vector<pic_clip_tensor> runs = joined(tensors, n);
+    const std::vector<ClipPiece> pieces = cut(runs);
+    if (pieces.size() > 0x3fffffffu) return PIC_ERR_INVALID_ARG;
+    int per_sm = 0, sms = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, clip_kernel, kThreads, 0) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+      cudaGetLastError();
+      return PIC_ERR_CUDA;
     }
     pic_clipper* c = new pic_clipper{};
     c->device = dev;
-    c->n_chunks = static_cast<int>(chunks.size());
-    c->blocks = std::max(1, std::min(kBlocks, c->n_chunks));
-    const size_t bytes = chunks.size() * sizeof(ClipChunk);
-    if (cudaMalloc(&c->parts, c->blocks * sizeof(double)) != cudaSuccess ||
-        (bytes && cudaMalloc(&c->chunks, bytes) != cudaSuccess)) {
+    c->n_pieces = static_cast<int>(pieces.size());
+    // a warp of its own for each piece where there are few: the fewer blocks meet, the sooner
+    c->blocks = std::max(1, std::min({kMaxBlocks, per_sm * sms, (c->n_pieces + kWarps - 1) / kWarps}));
+    const size_t bytes = pieces.size() * sizeof(ClipPiece);
+    if (cudaMalloc(&c->parts, (c->blocks + 2) * sizeof(double)) != cudaSuccess ||
+        (bytes && cudaMalloc(&c->pieces, bytes) != cudaSuccess)) {
       cudaGetLastError();
       pic_clip_destroy(c);
       return PIC_ERR_ALLOC;
     }
-    if (bytes && cudaMemcpy(c->chunks, chunks.data(), bytes, cudaMemcpyHostToDevice) != cudaSuccess) {
+    if (cudaMemset(c->parts, 0, (c->blocks + 2) * sizeof(double)) != cudaSuccess ||
+        (bytes && cudaMemcpy(c->pieces, pieces.data(), bytes, cudaMemcpyHostToDevice) != cudaSuccess) ||
+        cudaDeviceSynchronize() != cudaSuccess) {
       cudaGetLastError();
       pic_clip_destroy(c);
       return PIC_ERR_CUDA;
@@ -213,14 +423,41 @@ int pic_clip(pic_clipper* c, float max_norm, float* norm, void* stream) {
   }
   if (dev != c->device) return PIC_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  squares_kernel<<<c->blocks, kThreads, 0, s>>>(c->chunks, c->n_chunks, c->parts);
-  scale_kernel<<<c->blocks, kThreads, 0, s>>>(c->chunks, c->n_chunks, c->parts, c->blocks, max_norm, norm);
-  return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+  ClipParams p{};
+  p.pieces = c->pieces;
+  p.n = c->n_pieces;
+  p.parts = c->parts;
+  p.arrived = reinterpret_cast<unsigned long long*>(c->parts + c->blocks);
+  p.status = reinterpret_cast<int*>(c->parts + c->blocks + 1);
+  p.max_norm = max_norm;
+  p.norm = norm;
+  p.spin_limit = pic::kWaitPolls;
+  void* args[] = {&p};
+  if (cudaLaunchCooperativeKernel(reinterpret_cast<const void*>(clip_kernel), dim3(c->blocks), dim3(kThreads), args, 0,
+                                  s) != cudaSuccess) {
+    cudaGetLastError();
+    return PIC_ERR_CUDA;
+  }
+  return PIC_OK;
+}
+
+int pic_clip_check(pic_clipper* c, void* stream) {
+  if (!c) return PIC_ERR_INVALID_ARG;
+  int flag = 0;
+  int* status = reinterpret_cast<int*>(c->parts + c->blocks + 1);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (cudaMemcpyAsync(&flag, status, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess ||
+      cudaStreamSynchronize(s) != cudaSuccess ||
+      (flag && (cudaMemsetAsync(status, 0, sizeof(int), s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess))) {
+    cudaGetLastError();
+    return PIC_ERR_CUDA;
+  }
+  return flag ? PIC_ERR_TIMEOUT : PIC_OK;
 }
 
 void pic_clip_destroy(pic_clipper* c) {
   if (!c) return;
-  cudaFree(c->chunks);
+  cudaFree(c->pieces);
   cudaFree(c->parts);
   delete c;
 }

@@ -28,7 +28,7 @@
 namespace pic {
 namespace lin {
 
-struct alignas(64) TcMaps {
+struct TcMaps {
   CUtensorMap a, b, y, pre;
 };
 

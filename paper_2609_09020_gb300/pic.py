@@ -167,6 +167,8 @@ def load_library():
     lib.pic_clip_create.restype = i
     lib.pic_clip.argtypes = [_P, ctypes.c_float, _P, _P]
     lib.pic_clip.restype = i
+    lib.pic_clip_check.argtypes = [_P, _P]
+    lib.pic_clip_check.restype = i
     lib.pic_clip_destroy.argtypes = [_P]
     lib.pic_clip_destroy.restype = None
     lib.pic_fma_peak_flops.argtypes = [i, i]
@@ -641,6 +643,12 @@ class GradClip:
         if rc != PIC_OK:
             raise PicError(rc, "pic_clip")
         return norm
+
+    def check(self, stream=None):
+        """Synchronises the stream; raises if the blocks of a launch did not meet in time."""
+        rc = load_library().pic_clip_check(self.handle, _stream_ptr(stream))
+        if rc != PIC_OK:
+            raise PicError(rc, "pic_clip_check")
 
     def close(self):
         if self.handle:
