@@ -1,86 +1,170 @@
 // k_linear_grad.cu -- the elementwise part of the linear layer's gradient:
-// dz = dy act'(z) and its column sums db.  A block takes 32 columns and a run
-// of rows, eight at a time; its column sums go to the workspace and a second
-// kernel adds the blocks' sums in a fixed order.
+// dz = dy act'(z) and its column sums db.  Bound by memory: dy and z are read
+// and dz is written once.  A thread takes V neighbouring columns (16 bytes of
+// them where every row starts on a 16-byte boundary, else one) of every so
+// many-th row of a block's run of rows, with kUnroll rows' loads in flight; the
+// block adds its threads' column sums in shared memory and writes them to the
+// workspace, and a second kernel adds the blocks' sums in a fixed order.
 #include "linear.cuh"
 
 namespace pic {
 namespace lin {
 namespace {
 
-constexpr int kCols = 32, kRows = 8;
-constexpr int kRun = 512;  // rows of one block
+constexpr int kThreads = 256;
+constexpr int kUnroll = 4;
+constexpr int kBlocks = 1216;  // 8 per SM
 
-template <typename T>
-__global__ void __launch_bounds__(kCols* kRows) grad_act_kernel(const GradAct g) {
-  __shared__ float sums[kRows][kCols];
-  const int tx = threadIdx.x % kCols, ty = threadIdx.x / kCols;
-  const long long col_blocks = (g.J + kCols - 1) / kCols;
-  const long long row_block = blockIdx.x / col_blocks;
-  const long long j = blockIdx.x % col_blocks * kCols + tx;
-  const long long i0 = row_block * kRun;
-  const long long i1 = min(g.I, i0 + kRun);
-  float sum = 0.0f;
-  if (j < g.J)
-    for (long long i = i0 + ty; i < i1; i += kRows) {
-      float d = to_f32(static_cast<const T*>(g.dy)[i * g.lddy + j]);
-      if (g.act != PIC_ACT_NONE) d = act_grad(d, to_f32(static_cast<const T*>(g.pre)[i * g.ldpre + j]), g.act);
-      if (g.dz) static_cast<T*>(g.dz)[i * g.lddz + j] = from_f32<T>(d);
-      sum += d;
+// How a [I][J] matrix is shared out: tx threads across columns, blocks of `run` rows.
+struct Share {
+  int v, tx;
+  long long col_blocks, row_blocks, run;
+};
+
+Share share(const GradAct& g, int elem) {
+  const auto on16 = [&](const void* p, long long ld) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (ld * elem % 16 == 0 || g.I == 1);
+  };
+  Share s;
+  const bool wide = on16(g.dy, g.lddy) && (g.act == PIC_ACT_NONE || on16(g.pre, g.ldpre)) &&
+                    (!g.dz || on16(g.dz, g.lddz)) && g.J % (16 / elem) == 0;
+  s.v = wide ? 16 / elem : 1;
+  const long long across = (g.J + s.v - 1) / s.v;
+  s.tx = 1;
+  while (s.tx < across && s.tx < 32) s.tx *= 2;
+  s.col_blocks = (across + s.tx - 1) / s.tx;
+  const int ty = kThreads / s.tx;
+  long long want = (kBlocks + s.col_blocks - 1) / s.col_blocks;
+  if (want > 304) want = 304;  // more sums per column than that take longer to add than they save
+  const long long least = static_cast<long long>(ty) * kUnroll;
+  s.run = (g.I + want - 1) / want;
+  s.run = (s.run + least - 1) / least * least;
+  s.row_blocks = (g.I + s.run - 1) / s.run;
+  return s;
+}
+
+template <typename T, int V>
+struct Load {
+  uint32_t w[V * sizeof(T) / 4 ? V * sizeof(T) / 4 : 1];
+  __device__ __forceinline__ void get(const T* p) {
+    if constexpr (V * sizeof(T) == 16) {
+      const uint4 q = *reinterpret_cast<const uint4*>(p);
+      w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+    } else {
+      *reinterpret_cast<T*>(w) = *p;
     }
+  }
+  __device__ __forceinline__ float at(int i) const { return to_f32(reinterpret_cast<const T*>(w)[i]); }
+};
+
+template <typename T, int V>
+__global__ void __launch_bounds__(kThreads) grad_act_kernel(const GradAct g, const Share s) {
+  extern __shared__ float sums[];  // [ty][tx * V]
+  const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx, rows = kThreads / s.tx;
+  const long long col_block = blockIdx.x % s.col_blocks, row_block = blockIdx.x / s.col_blocks;
+  const long long j = (col_block * s.tx + tx) * V;
+  const long long i0 = row_block * s.run, i1 = min(g.I, i0 + s.run);
+  float sum[V] = {};
+  if (j < g.J) {
+    const T* dy = static_cast<const T*>(g.dy) + j;
+    const T* pre = static_cast<const T*>(g.pre) + j;
+    T* dz = static_cast<T*>(g.dz) + j;
+    for (long long i = i0 + ty; i < i1; i += rows * kUnroll) {
+      Load<T, V> a[kUnroll], z[kUnroll];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const long long r = i + u * rows;
+        if (r < i1) {
+          a[u].get(dy + r * g.lddy);
+          if (g.act != PIC_ACT_NONE) z[u].get(pre + r * g.ldpre);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const long long r = i + u * rows;
+        if (r >= i1) break;
+        Load<T, V> out;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          float d = a[u].at(e);
+          if (g.act != PIC_ACT_NONE) d = act_grad<sizeof(T) == 4>(d, z[u].at(e), g.act);
+          sum[e] += d;
+          reinterpret_cast<T*>(out.w)[e] = from_f32<T>(d);
+        }
+        if (g.dz) {
+          if constexpr (V * sizeof(T) == 16)
+            *reinterpret_cast<uint4*>(dz + r * g.lddz) = make_uint4(out.w[0], out.w[1], out.w[2], out.w[3]);
+          else
+            dz[r * g.lddz] = *reinterpret_cast<T*>(out.w);
+        }
+      }
+    }
+  }
   if (!g.parts) return;
-  sums[ty][tx] = sum;
+  const int width = s.tx * V;
+#pragma unroll
+  for (int e = 0; e < V; ++e) sums[ty * width + tx * V + e] = sum[e];
   __syncthreads();
-  if (ty == 0 && j < g.J) {
-    for (int r = 1; r < kRows; ++r) sum += sums[r][tx];
-    g.parts[row_block * g.J + j] = sum;
+  for (int c = threadIdx.x; c < width; c += kThreads) {
+    const long long col = col_block * width + c;
+    if (col >= g.J) break;
+    float t = 0.0f;
+    for (int r = 0; r < rows; ++r) t += sums[r * width + c];
+    g.parts[row_block * g.J + col] = t;
   }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(1024) sum_parts_kernel(const float* parts, long long blocks, long long J, T* out) {
-  __shared__ float sums[32][33];
-  const int tx = threadIdx.x % 32, ty = threadIdx.x / 32;
-  const long long j = blockIdx.x * 32LL + tx;
+__global__ void __launch_bounds__(1024) sum_parts_kernel(const float* parts, int blocks, long long J, T* out) {
+  __shared__ float sums[64][17];
+  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+  const long long j = blockIdx.x * 16LL + tx;
   float sum = 0.0f;
-  if (j < J)
-    for (long long b = ty; b < blocks; b += 32) sum += parts[b * J + j];
+  if (j < J) {
+#pragma unroll 5
+    for (int b = ty; b < blocks; b += 64) sum += parts[b * J + j];
+  }
   sums[ty][tx] = sum;
   __syncthreads();
   if (ty == 0 && j < J) {
-    for (int r = 1; r < 32; ++r) sum += sums[r][tx];
+#pragma unroll
+    for (int r = 1; r < 64; ++r) sum += sums[r][tx];
     out[j] = from_f32<T>(sum);
   }
 }
 
-}  // namespace
-
-long long grad_act_blocks(long long I, long long J) {
-  (void)J;
-  return (I + kRun - 1) / kRun;
-}
-
-int grad_act(const GradAct& g, int dtype, cudaStream_t s) {
-  const long long blocks = grad_act_blocks(g.I, g.J) * ((g.J + kCols - 1) / kCols);
+template <typename T>
+int run(const GradAct& g, cudaStream_t stream) {
+  const Share s = share(g, sizeof(T));
+  const long long blocks = s.col_blocks * s.row_blocks;
   if (blocks > 0x7fffffffLL) return PIC_ERR_INVALID_ARG;
-  const unsigned grid = static_cast<unsigned>(blocks);
-  if (dtype == PIC_DTYPE_F32)
-    grad_act_kernel<float><<<grid, kCols * kRows, 0, s>>>(g);
-  else if (dtype == PIC_DTYPE_F16)
-    grad_act_kernel<__half><<<grid, kCols * kRows, 0, s>>>(g);
+  const int smem = g.parts ? kThreads * s.v * 4 : 0;
+  if (s.v == 1)
+    grad_act_kernel<T, 1><<<static_cast<unsigned>(blocks), kThreads, smem, stream>>>(g, s);
   else
-    grad_act_kernel<__nv_bfloat16><<<grid, kCols * kRows, 0, s>>>(g);
+    grad_act_kernel<T, 16 / sizeof(T)><<<static_cast<unsigned>(blocks), kThreads, smem, stream>>>(g, s);
   return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
 }
 
+}  // namespace
+
+long long grad_act_blocks(const GradAct& g, int dtype) { return share(g, dtype == PIC_DTYPE_F32 ? 4 : 2).row_blocks; }
+
+int grad_act(const GradAct& g, int dtype, cudaStream_t s) {
+  if (dtype == PIC_DTYPE_F32) return run<float>(g, s);
+  if (dtype == PIC_DTYPE_F16) return run<__half>(g, s);
+  return run<__nv_bfloat16>(g, s);
+}
+
 int sum_parts(const float* parts, long long blocks, long long J, void* out, int dtype, cudaStream_t s) {
-  const unsigned grid = static_cast<unsigned>((J + 31) / 32);
+  const unsigned grid = static_cast<unsigned>((J + 15) / 16);
+  const int n = static_cast<int>(blocks);
   if (dtype == PIC_DTYPE_F32)
-    sum_parts_kernel<<<grid, 1024, 0, s>>>(parts, blocks, J, static_cast<float*>(out));
+    sum_parts_kernel<<<grid, 1024, 0, s>>>(parts, n, J, static_cast<float*>(out));
   else if (dtype == PIC_DTYPE_F16)
-    sum_parts_kernel<<<grid, 1024, 0, s>>>(parts, blocks, J, static_cast<__half*>(out));
+    sum_parts_kernel<<<grid, 1024, 0, s>>>(parts, n, J, static_cast<__half*>(out));
   else
-    sum_parts_kernel<<<grid, 1024, 0, s>>>(parts, blocks, J, static_cast<__nv_bfloat16*>(out));
+    sum_parts_kernel<<<grid, 1024, 0, s>>>(parts, n, J, static_cast<__nv_bfloat16*>(out));
   return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
 }
 

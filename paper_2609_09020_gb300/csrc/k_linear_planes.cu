@@ -1,0 +1,281 @@
+// k_linear_planes.cu -- large products of fp32 matrices on the tensor cores.  A
+// first kernel cuts each matrix into three planes of bfloat16 pieces (cut3.cuh),
+// once, in the workspace; the product then is the one of k_linear_tc.cuh for a
+// pair of CTAs, with three planes of each operand in a stage and six MMAs for
+// every 16 of K.  (k_linear_reg.cu cuts on the way into shared memory instead,
+// again for every tile: better where a matrix is used by one tile or two.)
+//
+// Roles: warp 0 TMA, warp 1 MMAs, warps 2..9 epilogue: 32 rows x 64 columns
+// each, which takes the accumulators over after every kTakeover slices.
+//
+// An infinite or NaN value would meet the zero pieces of others (inf 0 = NaN), so
+// the first kernel marks the blocks that have one, and an epilogue warp whose
+// rows or columns are marked computes its sums again with FP32 FMAs.
+#include "cut3.cuh"
+#include "k_linear_planes.cuh"
+
+namespace pic {
+namespace lin {
+namespace {
+
+constexpr int kEpi = 8;
+constexpr int kThreads = 64 + 32 * kEpi;
+constexpr int kTakeover = 2;
+constexpr int kABytes = 128 * 128, kBBytes = kPlCols / 2 * 128;  // one plane of one CTA
+constexpr int kStageBytes = kPieces * (kABytes + kBBytes);
+constexpr int kStages = 2;
+constexpr int kOffPanels = kStages * kStageBytes;
+constexpr int kOffBars = kOffPanels + kEpi * kPanelBytes;
+constexpr int kBars = 2 * kStages + 4 + 1;
+constexpr int kSmem = kOffBars + kBars * 8 + 16 + 1024;
+constexpr int kTmemCols = 2 * kPlCols;
+
+__global__ void __launch_bounds__(256) cut_kernel(const float* m, long long ld, long long rows, long long cols,
+                                                  uint16_t* planes, long long ld_out, int* marks, int col_blocks) {
+  const long long r0 = blockIdx.x / col_blocks * static_cast<long long>(kPlBlock);
+  const long long c0 = blockIdx.x % col_blocks * static_cast<long long>(kPlBlock);
+  const long long plane = rows * ld_out;
+  // 16 quads of four columns for each thread: a warp takes a row's 128 columns
+  const long long col = c0 + threadIdx.x % 32 * 4;
+  const bool vec = reinterpret_cast<uintptr_t>(m) % 16 == 0 && ld % 4 == 0;
+  uint32_t largest = 0;
+#pragma unroll 4
+  for (int u = 0; u < kPlBlock / 8; ++u) {
+    const long long r = r0 + threadIdx.x / 32 + u * 8;
+    if (r >= rows || col >= cols) continue;
+    uint32_t w[4];
+    const float* p = m + r * ld + col;
+    if (vec && col + 4 <= cols) {
+      const uint4 q = __ldg(reinterpret_cast<const uint4*>(p));
+      w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = col + i < cols ? __ldg(reinterpret_cast<const uint32_t*>(p) + i) : 0u;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) largest = max(largest, w[i] & 0x7fffffffu);
+    uint32_t h0, m0, l0, h1, m1, l1;
+    cut3(w[0], w[1], h0, m0, l0);
+    cut3(w[2], w[3], h1, m1, l1);
+    // rows are a multiple of eight places: the four are there
+    uint16_t* o = planes + r * ld_out + col;
+    *reinterpret_cast<uint2*>(o) = make_uint2(h0, h1);
+    *reinterpret_cast<uint2*>(o + plane) = make_uint2(m0, m1);
+    *reinterpret_cast<uint2*>(o + 2 * plane) = make_uint2(l0, l1);
+  }
+  const int bad = __syncthreads_or(largest >= 0x7f800000u);
+  if (threadIdx.x == 0) marks[blockIdx.x] = bad;
+}
+
+// Whether a block of the 128 rows (or columns of B) `group` and of slices
+// [k0, k1) of K is marked.
+__device__ __forceinline__ bool marked(const PlOperand& o, bool mn, long long group, long long groups, int k0, int k1,
+                                       int lane) {
+  if (group >= groups) return false;
+  bool bad = false;
+  for (int b = k0 / 2 + lane; b <= (k1 - 1) / 2; b += 32)
+    bad |= o.marks[mn ? b * static_cast<long long>(o.col_blocks) + group : group * o.col_blocks + b] != 0;
+  return __any_sync(0xffffffffu, bad);
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+    planes_kernel(const __grid_constant__ TcParams q, const __grid_constant__ TcMaps maps,
+                  const __grid_constant__ PlOperands o) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = tc::smem_addr(smem_raw);
+  uint8_t* smem = smem_raw + ((1024 - (raw & 1023)) & 1023);
+  const uint32_t base = tc::smem_addr(smem);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = tc::cluster_rank();
+  const uint32_t bars = base + kOffBars;
+  const uint32_t bar_full = bars, bar_empty = bars + 8 * kStages, bar_acc = bar_empty + 8 * kStages,
+                 bar_free = bar_acc + 16, bar_drain = bar_free + 16;
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kOffBars + 8 * kBars);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kOffBars + 8 * kBars + 4);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      tc::mbar_init(bar_full + 8 * s, 1);
+      tc::mbar_init(bar_empty + 8 * s, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      tc::mbar_init(bar_acc + 8 * b, 1);
+      tc::mbar_init(bar_free + 8 * b, kEpi * 2);
+    }
+    tc::mbar_init(bar_drain, 1);
+    *abort_flag = 0;
+    tc::fence_mbar_init();
+  }
+  if (warp == 1) tc::tmem_alloc_cg<2>(tc::smem_addr(tmem_slot), kTmemCols);
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::cluster_sync();
+  tc::tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const Product& p = q.p;
+  auto wait = [&](uint32_t bar, uint32_t parity) { return wait_bounded(bar, parity, abort_flag, q.status, q.spin_limit); };
+  const long long first = blockIdx.x / 2, step = gridDim.x / 2;
+  auto part = [&](long long w, int& k0, int& k1) {
+    k0 = static_cast<int>(w % q.splits) * q.part_blocks;
+    k1 = min(q.k_blocks, k0 + q.part_blocks);
+  };
+  // one plane is kABytes (kBBytes) of rows along K; of an operand along its rows
+  // each block of 64 rows has its three planes of 8 KB
+  const int a_plane = q.a_mn ? 8192 : kABytes, b_plane = q.b_mn ? 8192 : kBBytes;
+
+  if (warp == 0) {
+    if (tc::elect_one()) {
+      const uint32_t lead_full = tc::map_rank(bar_full, 0);
+      int s = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (long long w = first; w < q.work && ok; w += step) {
+        long long ti, tj;
+        tile_place<kPlRows>(w / q.splits, q.tiles_i, q.tiles_j, ti, tj);
+        const int i0 = static_cast<int>(ti * kPlRows + rank * 128), j0 = static_cast<int>(tj * kPlCols + rank * 64);
+        int k0, k1;
+        part(w, k0, k1);
+        for (int kb = k0; kb < k1; ++kb) {
+          if (!(ok = wait(bar_empty + 8 * s, phase ^ 1))) break;
+          if (rank == 0) tc::mbar_arrive_expect_tx(bar_full + 8 * s, 2 * kStageBytes);
+          const uint32_t sa = base + s * kStageBytes, sb = sa + kPieces * kABytes, bar = lead_full + 8 * s;
+          const int k = kb * kSlice;
+          if (q.a_mn) {
+            tc::tma_load_planes_pair(sa, &maps.a, i0, k, bar);
+            tc::tma_load_planes_pair(sa + kPieces * 8192, &maps.a, i0 + 64, k, bar);
+          } else {
+            tc::tma_load_planes_pair(sa, &maps.a, k, i0, bar);
+          }
+          if (q.b_mn)
+            tc::tma_load_planes_pair(sb, &maps.b, j0, k, bar);
+          else
+            tc::tma_load_planes_pair(sb, &maps.b, k, j0, bar);
+          if (++s == kStages) s = 0, phase ^= 1;
+        }
+      }
+      // aborted: as in k_linear_tc.cuh, the copies in flight land first
+      if (!ok) {
+        for (int i = 0; i < kStages; ++i) {
+          if (--s < 0) s = kStages - 1, phase ^= 1;
+          for (uint32_t n = 0; rank == 0 && n < q.spin_limit && !tc::mbar_try_wait(bar_full + 8 * s, phase); ++n) {
+          }
+        }
+        __nanosleep(200000);
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (rank == 0 && tc::elect_one()) {
+      const uint32_t idesc = tc::idesc_16(256, kPlCols, true, q.a_mn != 0, q.b_mn != 0);
+      const uint32_t a_step = q.a_mn ? 2048 : 32, b_step = q.b_mn ? 2048 : 32;
+      int s = 0, buf = 0;
+      uint32_t phase = 0, free_phase = 0;
+      bool ok = true;
+      for (long long w = first; w < q.work && ok; w += step) {
+        int k0, k1;
+        part(w, k0, k1);
+        for (int c0 = k0; c0 < k1 && ok; c0 += kTakeover) {
+          if (!(ok = wait(bar_free + 8 * buf, free_phase ^ 1))) break;
+          tc::tc_fence_after();
+          const uint32_t d = tmem + buf * kPlCols;
+          const int c1 = min(k1, c0 + kTakeover);
+          for (int kb = c0; kb < c1; ++kb) {
+            if (!(ok = wait(bar_full + 8 * s, phase))) break;
+            tc::tc_fence_after();
+            const uint32_t sa = base + s * kStageBytes, sb = sa + kPieces * kABytes;
+#pragma unroll
+            for (int t = 0; t < 6; ++t)
+#pragma unroll
+              for (int kk = 0; kk < kSlice / 16; ++kk)
+                tc::mma_16<2>(d, tc::smem_desc_sw128(sa + cut_a(t) * a_plane + kk * a_step, kPieces * 8192, 1024),
+                              tc::smem_desc_sw128(sb + cut_b(t) * b_plane + kk * b_step, kPieces * 8192, 1024), idesc,
+                              (kb > c0 || t > 0 || kk > 0) ? 1u : 0u);
+            tc::mma_commit_cg<2>(bar_empty + 8 * s);
+            if (++s == kStages) s = 0, phase ^= 1;
+          }
+          if (!ok) break;
+          tc::mma_commit_cg<2>(bar_acc + 8 * buf);
+          if (++buf == 2) buf = 0, free_phase ^= 1;
+        }
+      }
+      if (!ok) {  // aborted: MMAs in flight still read shared memory
+        tc::mma_commit_cg<2>(bar_drain);
+        for (uint32_t i = 0; i < q.spin_limit && !tc::mbar_try_wait(bar_drain, 0); ++i) {
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    const uint32_t panel = base + kOffPanels + (warp - 2) * kPanelBytes;
+    const uint32_t lead_free = tc::map_rank(bar_free, 0);
+    const long long a_groups = (p.I + 127) / 128, b_groups = (p.J + 127) / 128;
+    int buf = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (long long w = first; w < q.work && ok; w += step) {
+      long long ti, tj;
+      tile_place<kPlRows>(w / q.splits, q.tiles_i, q.tiles_j, ti, tj);
+      const long long row0 = ti * kPlRows + rank * 128 + quarter * 32, col0 = tj * kPlCols + half * 64;
+      int k0, k1;
+      part(w, k0, k1);
+      float v[64];
+      for (int c0 = k0; c0 < k1; c0 += kTakeover) {
+        ok = __all_sync(0xffffffffu, wait(bar_acc + 8 * buf, phase));
+        if (!ok) break;
+        tc::tc_fence_after();
+        const uint32_t d = tmem + buf * kPlCols + half * 64 + (static_cast<uint32_t>(quarter * 32) << 16);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t r[32];
+          tc::tmem_ld32_wait(d + 32 * h, r);
+#pragma unroll
+          for (int c = 0; c < 32; ++c)
+            v[32 * h + c] = c0 == k0 ? __uint_as_float(r[c]) : v[32 * h + c] + __uint_as_float(r[c]);
+        }
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive_cluster(lead_free + 8 * buf);
+        if (++buf == 2) buf = 0, phase ^= 1;
+      }
+      if (!ok) break;
+      if (marked(o.a, q.a_mn, ti * 2 + rank, a_groups, k0, k1, lane) || marked(o.b, q.b_mn, tj, b_groups, k0, k1, lane)) {
+        float u[64];
+        sum_again<64>(u, o.a.m, q.a_mn ? 1 : o.a.ld, q.a_mn ? o.a.ld : 1, o.b.m, q.b_mn ? 1 : o.b.ld, q.b_mn ? o.b.ld : 1,
+                      row0 + lane, p.I, col0, p.J, k0 * 64LL, min(p.K, k1 * 64LL));
+#pragma unroll
+        for (int c = 0; c < 64; ++c) v[c] = u[c];
+      }
+      if (q.parts) {
+        float4* out = reinterpret_cast<float4*>(q.parts) + ((w * 2 + rank) * 2 + half) * (128 * 16) + quarter * (32 * 16) + lane;
+#pragma unroll
+        for (int c = 0; c < 16; ++c) out[c * 32] = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+        continue;
+      }
+      if (row0 >= p.I || col0 >= p.J) continue;
+      finish_rows(v, p, maps, panel, lane, row0, col0, q.store_tma);
+    }
+    if (lane == 0) tc::bulk_wait_all();
+    __syncwarp();
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::cluster_sync();
+  tc::tc_fence_after();
+  if (warp == 1) tc::tmem_dealloc_cg<2>(tmem, kTmemCols);
+}
+
+}  // namespace
+
+PlKernel planes_kernel_info() { return {reinterpret_cast<const void*>(planes_kernel), kThreads, kSmem}; }
+
+int cut_planes(const float* m, long long ld, long long rows, long long cols, void* planes, long long ld_out, int* marks,
+               cudaStream_t s) {
+  const long long row_blocks = (rows + kPlBlock - 1) / kPlBlock, col_blocks = (cols + kPlBlock - 1) / kPlBlock;
+  cut_kernel<<<static_cast<unsigned>(row_blocks * col_blocks), 256, 0, s>>>(m, ld, rows, cols, static_cast<uint16_t*>(planes),
+                                                                            ld_out, marks, static_cast<int>(col_blocks));
+  return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+}
+
+}  // namespace lin
+}  // namespace pic

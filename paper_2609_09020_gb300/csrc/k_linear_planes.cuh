@@ -1,0 +1,35 @@
+// k_linear_planes.cuh -- what the launch of k_linear_planes.cu's kernels needs.
+#pragma once
+
+#include "k_linear_tc.cuh"
+
+namespace pic {
+namespace lin {
+
+// Tiles of 256 rows (128 for each CTA of a pair) and 128 columns.
+constexpr int kPlRows = 256, kPlCols = 128;
+constexpr int kPlBlock = 128;  // rows and columns of a stored matrix that share a mark
+
+// An fp32 matrix as it was, and the marks of its blocks.
+struct PlOperand {
+  const float* m;
+  long long ld;       // elements from one stored row to the next
+  const int* marks;   // [row blocks][col_blocks], nonzero: the block has an infinite or NaN value
+  int col_blocks;
+};
+struct PlOperands {
+  PlOperand a, b;
+};
+
+struct PlKernel {
+  const void* fn;  // takes (TcParams, TcMaps, PlOperands); a and b are maps of three planes
+  int threads, smem;
+};
+PlKernel planes_kernel_info();
+
+// planes[3][rows][ld_out] (bfloat16) and marks from the fp32 matrix m [rows][cols].
+int cut_planes(const float* m, long long ld, long long rows, long long cols, void* planes, long long ld_out, int* marks,
+               cudaStream_t s);
+
+}  // namespace lin
+}  // namespace pic

@@ -6,7 +6,8 @@
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
-#include "k_linear_tc.cuh"
+#include "k_linear_planes.cuh"
+#include "k_linear_reg.cuh"
 
 namespace pic {
 namespace lin {
@@ -14,14 +15,37 @@ namespace {
 
 constexpr int kSms = 152;
 
-// A matrix whose rows start on 16-byte boundaries, from one whose do not.
+// A matrix whose rows start on 16-byte boundaries, from one whose do not: a
+// thread puts eight elements together from the aligned words that hold them.
+// Bound by memory: it reads and writes each element once.
 __global__ void __launch_bounds__(256) repack_kernel(const uint16_t* src, long long ld, long long rows, int cols,
-                                                     uint16_t* dst, int ld_out) {
-  const long long n = rows * ld_out;
+                                                     uint4* dst, int chunks) {
+  const long long n = rows * chunks;
   for (long long e = blockIdx.x * 256LL + threadIdx.x; e < n; e += gridDim.x * 256LL) {
-    const long long r = e / ld_out;
-    const int c = static_cast<int>(e % ld_out);
-    if (c < cols) dst[e] = src[r * ld + c];
+    const long long r = n <= 0x7fffffffLL ? static_cast<int>(e) / chunks : e / chunks;
+    const int c = static_cast<int>(e - r * chunks) * 8;
+    const uint16_t* p = src + r * ld + c;
+    uint32_t w[4] = {};
+    const bool odd = (reinterpret_cast<uintptr_t>(p) & 2) != 0;
+    // the words' last half belongs to the element after the eight
+    if (c + 8 + (odd && r + 1 == rows ? 1 : 0) <= cols) {
+      if (odd) {
+        const uint32_t* q = reinterpret_cast<const uint32_t*>(p - 1);
+        uint32_t v[5];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) v[i] = __ldg(q + i);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(v[i], v[i + 1], 16);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __ldg(reinterpret_cast<const uint32_t*>(p) + i);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (c + i < cols) w[i / 2] |= static_cast<uint32_t>(__ldg(p + i)) << (16 * (i & 1));
+    }
+    dst[e] = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
@@ -32,38 +56,32 @@ struct JoinParams {
   int splits, rows, bn;  // rows and columns of a tile
 };
 
-// A thread adds the parts of four columns of a row, in order, and runs the epilogue.
+// A block finishes 32 items (four columns of a row each): its warps add every
+// eighth part, then the first warp the warps' sums.
 template <typename T, int ROWS>
 __global__ void __launch_bounds__(256) join_kernel(const JoinParams q) {
-  const Product& p = q.p;
-  const long long per_tile = static_cast<long long>(ROWS) * q.bn / 4;
-  const long long n = q.tiles_i * q.tiles_j * per_tile;
-  for (long long e = blockIdx.x * 256LL + threadIdx.x; e < n; e += gridDim.x * 256LL) {
-    const long long tile = e / per_tile;
-    const int in = static_cast<int>(e % per_tile);
-    // [rank][panel][quarter][16][32 lanes]
-    const int lane = in & 31, c4 = in >> 5 & 15, quarter = in >> 9 & 3, rest = in >> 11;
-    const int panel = rest % (q.bn / 64), rank = rest / (q.bn / 64);
-    long long ti, tj;
-    tile_place<ROWS>(tile, q.tiles_i, q.tiles_j, ti, tj);
-    const long long i = ti * ROWS + rank * 128 + quarter * 32 + lane, j = tj * q.bn + panel * 64 + c4 * 4;
-    if (i >= p.I || j >= p.J) continue;
-    float v[4] = {};
-    for (int s = 0; s < q.splits; ++s) {
-      const float4 f = q.parts[(tile * q.splits + s) * per_tile + in];
-      v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
-    }
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      if (j + c >= p.J) break;
-      float z = v[c];
-      if (p.bias) z += to_f32(static_cast<const T*>(p.bias)[j + c]);
-      if (p.pre) static_cast<T*>(p.pre)[i * p.ldpre + j + c] = from_f32<T>(z);
-      z = act_value<false>(z, p.act);
-      if (p.residual) z += to_f32(static_cast<const T*>(p.residual)[i * p.ldr + j + c]);
-      static_cast<T*>(p.y)[i * p.ldy + j + c] = from_f32<T>(z);
-    }
+  __shared__ float4 sums[8][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int per_tile = ROWS * q.bn / 4;
+  const long long tile = blockIdx.x / (per_tile / 32);
+  const int in = static_cast<int>(blockIdx.x % (per_tile / 32)) * 32 + lane;
+  const float4* parts = q.parts + tile * q.splits * per_tile + ((in & ~511) | (in & 15) << 5 | (in >> 4 & 31));
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+  for (int s = warp; s < q.splits; s += 8) {
+    const float4 f = __ldcg(parts + static_cast<long long>(s) * per_tile);
+    v.x += f.x, v.y += f.y, v.z += f.z, v.w += f.w;
   }
+  sums[warp][lane] = v;
+  __syncthreads();
+  if (warp > 0) return;
+#pragma unroll
+  for (int w = 1; w < 8; ++w) {
+    const float4 f = sums[w][lane];
+    v.x += f.x, v.y += f.y, v.z += f.z, v.w += f.w;
+  }
+  const float partial[4] = {v.x, v.y, v.z, v.w};
+  join_item<T, ROWS>(q.p, nullptr, 0, q.bn, q.tiles_i, q.tiles_j, tile, in, partial);
 }
 
 struct Operand {
@@ -72,44 +90,81 @@ struct Operand {
   long long ld_packed;
 };
 
-Operand operand(const void* m, long long s_row, long long s_k, long long rows, long long K) {
-  Operand o;
+Operand operand(const void* m, long long s_row, long long s_k, long long rows, long long K, bool fp32) {
+  Operand o{};
   o.mn = s_k != 1;
   o.rows = o.mn ? K : rows;
   o.cols = o.mn ? rows : K;
   o.ld = o.mn ? s_k : s_row;
   o.ld_packed = (o.cols + 7) / 8 * 8;
   if (o.rows == 1) o.ld = o.ld_packed;  // not used
+  if (fp32) return o;
   o.repack = reinterpret_cast<uintptr_t>(m) % 16 != 0 || o.ld % 8 != 0 || o.ld * 2 >= (1LL << 40);
   return o;
 }
 
 struct Plan {
   Operand a, b;
+  bool reg;     // fp32 operands through registers
+  bool planes;  // fp32 operands cut into planes first
   int cg, bn;
   long long tiles_i, tiles_j;
   int k_blocks, part_blocks, splits;
+  bool join;  // in the kernel, by clusters of `splits` CTAs
   long long a_bytes, b_bytes, part_bytes;
 };
 
 long long round256(long long v) { return (v + 255) / 256 * 256; }
 
-Plan plan(const Product& p) {
+long long planes_bytes(const Operand& o) { return round256(3 * o.rows * o.ld_packed * 2); }
+long long mark_cols(const Operand& o) { return (o.cols + kPlBlock - 1) / kPlBlock; }
+long long marks_bytes(const Operand& o) { return round256((o.rows + kPlBlock - 1) / kPlBlock * mark_cols(o) * 4); }
+
+Plan plan(const Product& p, int dtype) {
   Plan r{};
-  r.a = operand(p.a, p.a_i, p.a_k, p.I, p.K);
-  r.b = operand(p.b, p.b_j, p.b_k, p.J, p.K);
+  const bool fp32 = dtype == PIC_DTYPE_F32;
+  r.a = operand(p.a, p.a_i, p.a_k, p.I, p.K, fp32);
+  r.b = operand(p.b, p.b_j, p.b_k, p.J, p.K, fp32);
+  // fp32: cutting the operands first costs 10 bytes of traffic an element, cutting
+  // them on the way costs twice the MMAs' time for every tile
+  r.planes = fp32 && p.I >= 256 && p.J >= 256;
+  r.reg = fp32 && !r.planes;
   const long long big = ((p.I + 255) / 256) * ((p.J + 255) / 256);
-  r.bn = p.J <= 64 ? 64 : p.J <= 128 || big < kSms / 2 ? 128 : 256;
-  r.cg = r.bn == 256 ? 2 : 1;
+  const long long mid = ((p.I + 127) / 128) * ((p.J + 127) / 128);
+  r.bn = p.J <= 64 || mid < kSms / 2 ? 64 : p.J <= 128 || big < kSms / 2 ? 128 : 256;
+  if (r.reg) r.bn = kRegTile;
+  if (r.planes) r.bn = kPlCols;
+  r.cg = r.bn == 256 || r.planes ? 2 : 1;
   const int rows = 128 * r.cg;
   r.tiles_i = (p.I + rows - 1) / rows;
   r.tiles_j = (p.J + r.bn - 1) / r.bn;
   r.k_blocks = static_cast<int>((p.K + kSlice - 1) / kSlice);
-  const int splits = split_count(r.tiles_i * r.tiles_j, r.k_blocks, 4, kSms);
+  const long long tiles = r.tiles_i * r.tiles_j;
+  int splits = split_count(tiles, r.k_blocks, fp32 ? 4 : 16, r.bn == 64 ? 2 * kSms : kSms / r.cg);
+  if (splits > 1 && r.cg == 1 && tiles * 8 >= kSms / 2) {
+    // the parts of a tile as a cluster
+    while (splits & (splits - 1)) splits &= splits - 1;
+    if (splits > 8) splits = 8;
+    r.join = splits > 1;
+  }
   r.part_blocks = (r.k_blocks + splits - 1) / splits;
   r.splits = (r.k_blocks + r.part_blocks - 1) / r.part_blocks;
+  if (r.join && r.splits != splits) {  // a part would be empty: as many as are whole
+    r.splits = 1, r.part_blocks = r.k_blocks, r.join = false;
+    for (int c = splits / 2; c > 1; c /= 2) {
+      const int n = (r.k_blocks + c - 1) / c;
+      if ((r.k_blocks + n - 1) / n == c) {
+        r.splits = c, r.part_blocks = n, r.join = true;
+        break;
+      }
+    }
+  }
   if (r.a.repack) r.a_bytes = round256(r.a.rows * r.a.ld_packed * 2);
   if (r.b.repack) r.b_bytes = round256(r.b.rows * r.b.ld_packed * 2);
+  if (r.planes) {
+    r.a_bytes = planes_bytes(r.a) + marks_bytes(r.a);
+    r.b_bytes = planes_bytes(r.b) + marks_bytes(r.b);
+  }
   if (r.splits > 1) r.part_bytes = r.tiles_i * r.tiles_j * r.splits * rows * r.bn * 4;
   return r;
 }
@@ -128,27 +183,43 @@ PFN_cuTensorMapEncodeTiled_v12000 encoder() {
   return fn;
 }
 
-// A [rows][cols] matrix of 16-bit values in boxes of 64 columns and box_rows
-// rows, 128-byte swizzled.
-bool encode(CUtensorMap* map, const void* m, long long rows, long long cols, long long ld, int box_rows, bool bf16) {
+// A [rows][cols] matrix in boxes of 128 bytes of columns and box_rows rows,
+// 128-byte swizzled.
+bool encode(CUtensorMap* map, const void* m, long long rows, long long cols, long long ld, int box_rows, int dtype) {
   const PFN_cuTensorMapEncodeTiled_v12000 enc = encoder();
   if (!enc) return false;
+  const unsigned e = dtype == PIC_DTYPE_F32 ? 4 : 2;
+  const CUtensorMapDataType type = dtype == PIC_DTYPE_F32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : dtype == PIC_DTYPE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                            : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   const cuuint64_t dim[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
-  const cuuint64_t stride[1] = {static_cast<cuuint64_t>(ld * 2)};
-  const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(box_rows)};
+  const cuuint64_t stride[1] = {static_cast<cuuint64_t>(ld * e)};
+  const cuuint32_t box[2] = {128u / e, static_cast<cuuint32_t>(box_rows)};
   const cuuint32_t elem[2] = {1, 1};
-  return enc(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(m), dim,
-             stride, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return enc(map, type, 2, const_cast<void*>(m), dim, stride, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The three planes of a matrix, in boxes of 64 columns, box_rows rows and all planes.
+bool encode_planes(CUtensorMap* map, const void* m, long long rows, long long cols, long long ld, int box_rows) {
+  const PFN_cuTensorMapEncodeTiled_v12000 enc = encoder();
+  if (!enc) return false;
+  const cuuint64_t dim[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), 3};
+  const cuuint64_t stride[2] = {static_cast<cuuint64_t>(ld * 2), static_cast<cuuint64_t>(rows * ld * 2)};
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_rows), 3};
+  const cuuint32_t elem[3] = {1, 1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(m), dim, stride, box, elem,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 const void* repacked(const void* m, const Operand& o, void* ws, cudaStream_t s) {
   if (!o.repack) return m;
-  long long b = (o.rows * o.ld_packed + 1023) / 1024;
+  const int chunks = static_cast<int>(o.ld_packed / 8);
+  long long b = (o.rows * chunks + 255) / 256;
   if (b > 16 * kSms) b = 16 * kSms;
   repack_kernel<<<static_cast<unsigned>(b), 256, 0, s>>>(static_cast<const uint16_t*>(m), o.ld, o.rows,
-                                                         static_cast<int>(o.cols), static_cast<uint16_t*>(ws),
-                                                         static_cast<int>(o.ld_packed));
+                                                         static_cast<int>(o.cols), static_cast<uint4*>(ws), chunks);
   return ws;
 }
 
@@ -159,7 +230,7 @@ int smem_of() {
 
 // The kernel's shared-memory attribute, set once per device.
 int set_up(const void* fn, int slot, int smem) {
-  static std::atomic<uint64_t> done[6];
+  static std::atomic<uint64_t> done[8];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return PIC_ERR_CUDA;
   const uint64_t bit = 1ull << (dev & 63);
@@ -171,66 +242,108 @@ int set_up(const void* fn, int slot, int smem) {
 
 template <typename T>
 int join(const JoinParams& q, cudaStream_t s) {
-  long long b = (q.tiles_i * q.tiles_j * q.rows * q.bn / 4 + 255) / 256;
-  if (b > 16 * kSms) b = 16 * kSms;
+  const unsigned blocks = static_cast<unsigned>(q.tiles_i * q.tiles_j * q.rows * q.bn / 4 / 32);
   if (q.rows == 128)
-    join_kernel<T, 128><<<static_cast<unsigned>(b), 256, 0, s>>>(q);
+    join_kernel<T, 128><<<blocks, 256, 0, s>>>(q);
   else
-    join_kernel<T, 256><<<static_cast<unsigned>(b), 256, 0, s>>>(q);
+    join_kernel<T, 256><<<blocks, 256, 0, s>>>(q);
   return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
 }
 
 }  // namespace
 
-long long tc_workspace(const Product& p) {
-  const Plan r = plan(p);
+long long tc_workspace(const Product& p, int dtype) {
+  const Plan r = plan(p, dtype);
   return r.a_bytes + r.b_bytes + r.part_bytes;
 }
 
 int tc_product(const Product& p, int dtype, void* ws, int* status, unsigned spin_limit, cudaStream_t s) {
-  const Plan r = plan(p);
-  const bool bf16 = dtype == PIC_DTYPE_BF16;
+  const Plan r = plan(p, dtype);
+  const long long elem = dtype == PIC_DTYPE_F32 ? 4 : 2;
   char* w = static_cast<char*>(ws);
   const void* a = repacked(p.a, r.a, w, s);
   const void* b = repacked(p.b, r.b, w + r.a_bytes, s);
-  float* parts = r.splits > 1 ? reinterpret_cast<float*>(w + r.a_bytes + r.b_bytes) : nullptr;
 
   TcParams q{};
   TcMaps maps;
+  RegOperands o{};
+  PlOperands pl{};
   q.p = p;
   q.tiles_i = r.tiles_i, q.tiles_j = r.tiles_j;
   q.splits = r.splits, q.k_blocks = r.k_blocks, q.part_blocks = r.part_blocks;
   q.work = r.tiles_i * r.tiles_j * r.splits;
   q.a_mn = r.a.mn, q.b_mn = r.b.mn;
-  q.parts = parts;
+  q.parts = r.splits > 1 ? reinterpret_cast<float*>(w + r.a_bytes + r.b_bytes) : nullptr;
+  q.join = r.join;
   q.status = status;
   q.spin_limit = spin_limit;
-  const auto fits = [](const void* m, long long ld, long long rows) {
-    return reinterpret_cast<uintptr_t>(m) % 16 == 0 && ((ld % 8 == 0 && ld * 2 < (1LL << 40)) || rows == 1);
+  const auto fits = [&](const void* m, long long ld, long long rows) {
+    return reinterpret_cast<uintptr_t>(m) % 16 == 0 && ((ld * elem % 16 == 0 && ld * elem < (1LL << 40)) || rows == 1);
   };
-  q.store_tma = !parts && fits(p.y, p.ldy, p.I) && (!p.pre || fits(p.pre, p.ldpre, p.I));
-  // of an operand that lies along its rows a box is 64 of them by 64 of K
-  const int b_rows = r.bn / r.cg;
-  bool ok = encode(&maps.a, a, r.a.rows, r.a.cols, r.a.repack ? r.a.ld_packed : r.a.ld, r.a.mn ? 64 : 128, bf16) &&
-            encode(&maps.b, b, r.b.rows, r.b.cols, r.b.repack ? r.b.ld_packed : r.b.ld, r.b.mn ? 64 : b_rows, bf16);
+  q.store_tma = !q.parts && fits(p.y, p.ldy, p.I) && (!p.pre || fits(p.pre, p.ldpre, p.I));
   const auto out_ld = [&](long long ld) { return p.I == 1 ? (p.J + 7) / 8 * 8 : ld; };
-  if (q.store_tma) ok = ok && encode(&maps.y, p.y, p.I, p.J, out_ld(p.ldy), 32, bf16);
-  if (q.store_tma && p.pre) ok = ok && encode(&maps.pre, p.pre, p.I, p.J, out_ld(p.ldpre), 32, bf16);
+  bool ok = true;
+  if (r.reg) {
+    o.a = p.a, o.b = p.b;
+    o.lda = r.a.ld, o.ldb = r.b.ld;
+    const auto vec = [&](const void* m, const Operand& x) {
+      return reinterpret_cast<uintptr_t>(m) % (4 * elem) == 0 && (x.ld % 4 == 0 || x.rows == 1);
+    };
+    o.vec_a = vec(p.a, r.a), o.vec_b = vec(p.b, r.b);
+  } else if (r.planes) {
+    const auto cut = [&](const void* m, const Operand& x, char* at, PlOperand& out, CUtensorMap* map, int box_rows) {
+      int* marks = reinterpret_cast<int*>(at + planes_bytes(x));
+      out = {static_cast<const float*>(m), x.ld, marks, static_cast<int>(mark_cols(x))};
+      return cut_planes(out.m, x.ld, x.rows, x.cols, at, x.ld_packed, marks, s) == PIC_OK &&
+             encode_planes(map, at, x.rows, x.cols, x.ld_packed, box_rows);
+    };
+    ok = cut(p.a, r.a, w, pl.a, &maps.a, r.a.mn ? 64 : 128) && cut(p.b, r.b, w + r.a_bytes, pl.b, &maps.b, 64);
+  } else {
+    // of an operand that lies along its rows a box is 64 of them by 64 of K
+    ok = encode(&maps.a, a, r.a.rows, r.a.cols, r.a.repack ? r.a.ld_packed : r.a.ld, r.a.mn ? 64 : 128, dtype) &&
+         encode(&maps.b, b, r.b.rows, r.b.cols, r.b.repack ? r.b.ld_packed : r.b.ld, r.b.mn ? 64 : r.bn / r.cg, dtype);
+  }
+  if (q.store_tma) ok = ok && encode(&maps.y, p.y, p.I, p.J, out_ld(p.ldy), 32, dtype);
+  if (q.store_tma && p.pre) ok = ok && encode(&maps.pre, p.pre, p.I, p.J, out_ld(p.ldpre), 32, dtype);
   if (!ok) return PIC_ERR_CUDA;
 
-  const void* fn = bf16 ? tc_kernel_bf16(r.bn) : tc_kernel_f16(r.bn);
-  const int shape = r.bn == 256 ? 2 : r.bn == 128 ? 1 : 0;
-  const int smem = shape == 2 ? smem_of<2, 256>() : shape == 1 ? smem_of<1, 128>() : smem_of<1, 64>();
-  if (set_up(fn, shape + (bf16 ? 3 : 0), smem) != PIC_OK) return PIC_ERR_CUDA;
+  const void* fn;
+  int slot, smem, threads = kTcThreads;
+  if (r.reg) {
+    const RegKernel k = reg_kernel_info();
+    fn = k.fn, threads = k.threads, smem = k.smem;
+    slot = 6;
+  } else if (r.planes) {
+    const PlKernel k = planes_kernel_info();
+    fn = k.fn, threads = k.threads, smem = k.smem;
+    slot = 7;
+  } else {
+    fn = dtype == PIC_DTYPE_BF16 ? tc_kernel_bf16(r.bn) : tc_kernel_f16(r.bn);
+    const int shape = r.bn == 256 ? 2 : r.bn == 128 ? 1 : 0;
+    slot = shape + (dtype == PIC_DTYPE_BF16 ? 3 : 0);
+    smem = shape == 2 ? smem_of<2, 256>() : shape == 1 ? smem_of<1, 128>() : smem_of<1, 64>();
+  }
+  if (set_up(fn, slot, smem) != PIC_OK) return PIC_ERR_CUDA;
   long long grid = q.work * r.cg;
   const long long most = r.bn == 64 ? 2 * kSms : kSms;
-  if (grid > most) grid = most;
-  void* args[] = {&q, &maps};
-  if (cudaLaunchKernel(fn, dim3(static_cast<unsigned>(grid)), dim3(kTcThreads), args, smem, s) != cudaSuccess)
-    return PIC_ERR_CUDA;
-  if (parts) {
-    const JoinParams j{p, reinterpret_cast<const float4*>(parts), r.tiles_i, r.tiles_j, r.splits, 128 * r.cg, r.bn};
-    return bf16 ? join<__nv_bfloat16>(j, s) : join<__half>(j, s);
+  if (grid > most && !r.join) grid = most;  // joined: one tile a cluster
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = r.join ? r.splits : r.cg;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  void* args[] = {&q, &maps, r.planes ? static_cast<void*>(&pl) : &o};  // 16-bit kernels take the first two
+  if (cudaLaunchKernelExC(&cfg, fn, args) != cudaSuccess) return PIC_ERR_CUDA;
+  if (q.parts && !r.join) {
+    const JoinParams j{p, reinterpret_cast<const float4*>(q.parts), r.tiles_i, r.tiles_j, r.splits, 128 * r.cg, r.bn};
+    if (dtype == PIC_DTYPE_F32) return join<float>(j, s);
+    return dtype == PIC_DTYPE_BF16 ? join<__nv_bfloat16>(j, s) : join<__half>(j, s);
   }
   return PIC_OK;
 }

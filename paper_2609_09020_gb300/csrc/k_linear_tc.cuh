@@ -14,9 +14,10 @@
 // next tile's MMAs.  An operand may be contiguous along K or along its rows
 // (dz and x in dw = dz^T x): TMA then brings blocks of 64 rows x 64 of K and
 // the MMA reads them transposed.  A product that has fewer tiles than the GPU
-// has SMs, or too few for whole rounds, is cut along K: each part's
-// accumulators go to the workspace in fp32, and a second kernel adds the parts
-// in order and runs the epilogue.
+// has SMs is cut along K: each part's accumulators go to the workspace in fp32.
+// Up to 8 parts of a tile are a cluster, whose CTAs meet once and then each add
+// a share of the tile's parts, in order, and run the epilogue on it; more parts
+// (dw over many rows) are added by a second kernel.
 //
 // Each wait is bounded: a thread whose wait runs out raises its CTA's abort
 // flag and the status word, and every role skips what is left.
@@ -42,6 +43,7 @@ struct TcParams {
   int a_mn, b_mn;        // the operand is contiguous along its rows
   int store_tma;         // y (and pre) go out by TMA
   float* parts;          // fp32 parts, or null: the epilogue runs in the kernel
+  int join;              // the CTAs of a tile's parts are a cluster and join them
   int* status;
   unsigned spin_limit;
 };
@@ -51,6 +53,23 @@ constexpr int kTcThreads = 64 + 32 * kEpiWarps;
 constexpr int kSlice = 64;           // K of one stage
 constexpr int kPanelBytes = 32 * 128;  // 32 rows x 64 columns of a 16-bit type
 constexpr int kGroupRows = 2048;     // rows of A that neighbouring tiles share the columns of B for
+
+// At most `limit` polls; false (with the flags raised) if the phase does not
+// complete in time or another thread has given up.
+__device__ __forceinline__ bool wait_bounded(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status,
+                                             unsigned limit) {
+  if (tc::mbar_test_wait(bar, parity)) return true;
+  for (uint32_t i = 0; i < limit; ++i) {
+    if (tc::mbar_try_wait(bar, parity)) return true;
+    if ((i & 63u) == 63u) {
+      if (*abort_flag) return false;
+      if (i > 4096) __nanosleep(64);
+    }
+  }
+  *abort_flag = 1;
+  atomicOr(status, 1);
+  return false;
+}
 
 template <int CG, int BN>
 struct TcShape {
@@ -102,7 +121,9 @@ __device__ __forceinline__ uint32_t pack2_16<__nv_bfloat16>(float lo, float hi) 
   return d;
 }
 template <typename T>
-__device__ __forceinline__ float2 unpack2_16(uint32_t v);
+__device__ __forceinline__ float2 unpack2_16(uint32_t v) {
+  return make_float2(0.0f, 0.0f);
+}
 template <>
 __device__ __forceinline__ float2 unpack2_16<__half>(uint32_t v) {
   return __half22float2(*reinterpret_cast<const __half2*>(&v));
@@ -117,9 +138,9 @@ __device__ __forceinline__ uint32_t idesc_of(int M, int N, bool a_mn, bool b_mn)
   return tc::idesc_16(M, N, !IsHalf<T>::value, a_mn, b_mn);
 }
 
-// One warp's panel (32 rows from row0, 64 columns from col0; this lane's row in
-// v) to global memory: into the panel buffer, swizzled as TMA and the banks
-// like it, then one TMA store, or two columns of a row per lane and row.
+// One warp's panel (32 rows from row0, 128 bytes of columns from col0; this
+// lane's row in v) to global memory: into the panel buffer, swizzled as TMA and
+// the banks like it, then one TMA store, or one word of a row per lane and row.
 template <typename T>
 __device__ __forceinline__ void put_panel(const uint32_t (&v)[32], uint32_t buf, int lane, long long row0, long long col0,
                                           const Product& p, void* out, long long ld, const CUtensorMap* map,
@@ -137,48 +158,136 @@ __device__ __forceinline__ void put_panel(const uint32_t (&v)[32], uint32_t buf,
     return;
   }
   __syncwarp();
-  const long long col = col0 + 2 * lane;
+  constexpr int kPer = 4 / sizeof(T);  // columns of a word
+  const long long col = col0 + kPer * lane;
   T* o = static_cast<T*>(out) + row0 * ld + col;
-  const bool whole = ((reinterpret_cast<uintptr_t>(out) | static_cast<uintptr_t>(ld * 2)) & 3) == 0;
+  const bool whole = ((reinterpret_cast<uintptr_t>(out) | static_cast<uintptr_t>(ld * sizeof(T))) & 3) == 0;
   const int rows = static_cast<int>(min(32LL, p.I - row0));
+#pragma unroll 4
   for (int r = 0; r < rows; ++r, o += ld) {
     uint32_t w;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(buf + r * 128 + (((lane >> 2) ^ (r & 7)) * 16) + (lane & 3) * 4));
-    if (whole && col + 1 < p.J)
+    if (whole && col + kPer <= p.J) {
       *reinterpret_cast<uint32_t*>(o) = w;
-    else {
+    } else {
       const T* h = reinterpret_cast<const T*>(&w);
-      if (col < p.J) o[0] = h[0];
-      if (col + 1 < p.J) o[1] = h[1];
+#pragma unroll
+      for (int c = 0; c < kPer; ++c)
+        if (col + c < p.J) o[c] = h[c];
     }
   }
   __syncwarp();
 }
 
 // Adds 64 columns (or those of them that exist) of the bias or of a residual row to v.
-template <typename T>
-__device__ __forceinline__ void add_row(float (&v)[64], const T* r, int cols) {
-  if (cols >= 64 && (reinterpret_cast<uintptr_t>(r) & 15) == 0) {
+template <typename T, int N = 64>
+__device__ __forceinline__ void add_row(float (&v)[N], const T* r, int cols) {
+  constexpr int kVec = 16 / sizeof(T);
+  if (cols >= N && (reinterpret_cast<uintptr_t>(r) & 15) == 0) {
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      const uint4 q = *reinterpret_cast<const uint4*>(r + 8 * c);
+    for (int c = 0; c < N / kVec; ++c) {
+      const uint4 q = *reinterpret_cast<const uint4*>(r + kVec * c);
       const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float2 f = unpack2_16<T>(w[e]);
-        v[8 * c + 2 * e] += f.x;
-        v[8 * c + 2 * e + 1] += f.y;
+        if constexpr (sizeof(T) == 4) {
+          v[4 * c + e] += __uint_as_float(w[e]);
+        } else {
+          const float2 f = unpack2_16<T>(w[e]);
+          v[8 * c + 2 * e] += f.x;
+          v[8 * c + 2 * e + 1] += f.y;
+        }
       }
     }
   } else {
 #pragma unroll
-    for (int c = 0; c < 64; ++c)
+    for (int c = 0; c < N; ++c)
       if (c < cols) v[c] += to_f32(r[c]);
   }
 }
 
+// The epilogue of a lane's row and 64 columns of fp32 sums: bias, pre, activation,
+// residual, and out through the warp's one panel buffer.
+__device__ __forceinline__ void finish_rows(float (&v)[64], const Product& p, const TcMaps& maps, uint32_t panel, int lane,
+                                            long long row0, long long col0, bool by_tma) {
+  const int cols = static_cast<int>(min(64LL, p.J - col0));
+  if (p.bias) add_row<float>(v, static_cast<const float*>(p.bias) + col0, cols);
+  const auto put = [&](void* out, long long ld, const CUtensorMap* map) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (32 * h >= cols) break;
+      uint32_t r[32];
+#pragma unroll
+      for (int c = 0; c < 32; ++c) r[c] = __float_as_uint(v[h * 32 + c]);
+      if (lane == 0) tc::bulk_wait_read<0>();
+      __syncwarp();
+      put_panel<float>(r, panel, lane, row0, col0 + h * 32, p, out, ld, map, by_tma);
+    }
+  };
+  if (p.pre) put(p.pre, p.ldpre, &maps.pre);
+  if (p.act != PIC_ACT_NONE) {
+#pragma unroll
+    for (int c = 0; c < 64; ++c) v[c] = act_value<true>(v[c], p.act);
+  }
+  if (p.residual && row0 + lane < p.I)
+    add_row<float>(v, static_cast<const float*>(p.residual) + (row0 + lane) * p.ldr + col0, cols);
+  put(p.y, p.ldy, &maps.y);
+}
+
+// Four columns (item `in` of `tile`) of a product cut along K: adds the parts in
+// order and runs the epilogue.  A part is [rank][panel][quarter][16][32 rows][4
+// columns]; neighbouring items are neighbouring columns.
+template <typename T, int ROWS>
+__device__ __forceinline__ void join_item(const Product& p, const float4* parts, int splits, int bn, long long tiles_i,
+                                          long long tiles_j, long long tile, int in, const float* partial = nullptr) {
+  const int c4 = in & 15, row = in >> 4 & 31, quarter = in >> 9 & 3, rest = in >> 11;
+  const int panel = rest % (bn / 64), rank = rest / (bn / 64);
+  long long ti, tj;
+  tile_place<ROWS>(tile, tiles_i, tiles_j, ti, tj);
+  const long long i = ti * ROWS + rank * 128 + quarter * 32 + row, j = tj * bn + panel * 64 + c4 * 4;
+  if (i >= p.I || j >= p.J) return;
+  float v[4] = {};
+  if (partial) {
+    for (int c = 0; c < 4; ++c) v[c] = partial[c];
+  } else {
+    const int per_tile = ROWS * bn / 4;
+    const float4* q = parts + tile * splits * per_tile + (rest << 11 | quarter << 9 | c4 << 5 | row);
+    for (int s = 0; s < splits; ++s) {
+      const float4 f = __ldcg(q + static_cast<long long>(s) * per_tile);
+      v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
+    }
+  }
+  T y[4], pre[4];
+  const int cols = static_cast<int>(min(4LL, p.J - j));
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    if (c >= cols) break;
+    float z = v[c];
+    if (p.bias) z += to_f32(static_cast<const T*>(p.bias)[j + c]);
+    pre[c] = from_f32<T>(z);
+    z = act_value<sizeof(T) == 4>(z, p.act);
+    if (p.residual) z += to_f32(static_cast<const T*>(p.residual)[i * p.ldr + j + c]);
+    y[c] = from_f32<T>(z);
+  }
+  const auto put = [&](void* out, long long ld, const T (&t)[4]) {
+    T* o = static_cast<T*>(out) + i * ld + j;
+    if (cols == 4 && reinterpret_cast<uintptr_t>(o) % (4 * sizeof(T)) == 0) {
+      struct alignas(4 * sizeof(T)) Four {
+        T t[4];
+      };
+      *reinterpret_cast<Four*>(o) = {t[0], t[1], t[2], t[3]};
+    } else {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (c < cols) o[c] = t[c];
+    }
+  };
+  if (p.pre) put(p.pre, p.ldpre, pre);
+  put(p.y, p.ldy, y);
+}
+
 template <typename T, int CG, int BN>
-__global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kTcThreads, BN == 64 ? 2 : 1)
+__global__ void __launch_bounds__(kTcThreads, BN == 64 ? 2 : 1)
     tc_kernel(const __grid_constant__ TcParams q, const __grid_constant__ TcMaps maps) {
   using S = TcShape<CG, BN>;
   extern __shared__ uint8_t smem_raw[];
@@ -213,19 +322,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kTcThreads, BN == 6
   tc::tc_fence_after();
   const uint32_t tmem = *tmem_slot;
 
-  auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
-    if (tc::mbar_test_wait(bar, parity)) return true;
-    for (uint32_t i = 0; i < q.spin_limit; ++i) {
-      if (tc::mbar_try_wait(bar, parity)) return true;
-      if ((i & 63u) == 63u) {
-        if (*abort_flag) return false;
-        if (i > 4096) __nanosleep(64);
-      }
-    }
-    *abort_flag = 1;
-    atomicOr(q.status, 1);
-    return false;
-  };
+  auto wait = [&](uint32_t bar, uint32_t parity) { return wait_bounded(bar, parity, abort_flag, q.status, q.spin_limit); };
   const long long first = blockIdx.x / CG, step = gridDim.x / CG;
   // slices of work item w
   auto part = [&](long long w, int& k0, int& k1) {
@@ -392,9 +489,15 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kTcThreads, BN == 6
   }
   tc::tc_fence_before();
   __syncthreads();
-  if constexpr (CG == 2) tc::cluster_sync();
+  if (CG == 2 || q.join) tc::cluster_sync();  // the pair is done; all parts are written
   tc::tc_fence_after();
   if (warp == 1) tc::tmem_dealloc_cg<CG>(tmem, S::kTmemCols);
+  if (CG == 1 && q.join) {
+    const long long tile = blockIdx.x / q.splits;
+    for (int in = static_cast<int>(blockIdx.x % q.splits) * kTcThreads + threadIdx.x; in < 128 * BN / 4;
+         in += q.splits * kTcThreads)
+      join_item<T, 128>(q.p, reinterpret_cast<const float4*>(q.parts), q.splits, BN, q.tiles_i, q.tiles_j, tile, in);
+  }
 }
 
 // The kernel for tiles of bn columns: 64 and 128 by one CTA, 256 by a pair.

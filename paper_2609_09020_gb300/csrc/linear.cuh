@@ -10,6 +10,7 @@
 #include <cuda_runtime.h>
 
 #include "pic_common.cuh"
+#include "pic_gelu_grad.cuh"
 #include "pic_linear.h"
 
 namespace pic {
@@ -51,15 +52,29 @@ __device__ __forceinline__ float act_value(float z, int act) {
   }
 }
 
-// dy act'(z): a derivative of zero gives zero whatever dy is.  The clamp keeps
-// z phi(z) from being infinity times zero (phi(20) is below fp32's range).
+// dy act'(z): a derivative of zero gives zero whatever dy is; act' is NaN for
+// NaN.  EXACT: with erfcf and expf (fp32); else the polynomial form, off by at
+// most 5e-7, far below the rounding of dz to 16 bits, and half its cost.
+template <bool EXACT>
 __device__ __forceinline__ float act_grad(float dy, float z, int act) {
   if (act == PIC_ACT_NONE) return dy;
   if (act == PIC_ACT_RELU) return z > 0.0f ? dy : 0.0f;
-  const float c = fminf(fmaxf(z, -20.0f), 20.0f);
-  const float phi = 0.39894228040143268f * __expf(-0.5f * c * c);
-  const float d = fmaf(c, phi, 0.5f * erfcf(-0.70710678118654752f * z));
-  return dy * d;
+  float d;
+  if constexpr (EXACT) {
+    // the clamp keeps z phi(z) from being infinity times zero (phi(20) is below fp32's range)
+    const float c = fminf(fmaxf(z, -20.0f), 20.0f);
+    const float phi = 0.39894228040143268f * expf(-0.5f * c * c);
+    d = fmaf(c, phi, 0.5f * erfcf(-0.70710678118654752f * z));
+  } else {
+    float a;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(fabsf(z)), "f"(kGeluGradA));
+    float p = gelu_grad_c(0);
+#pragma unroll
+    for (int i = 1; i <= kGeluGradDeg; ++i) p = fmaf(p, a, gelu_grad_c(i));
+    const float t = a >= kGeluGradA ? 0.0f : p * ex2_approx(a * a * kGeluGradPower);
+    d = z < 0.0f ? t : 1.0f - t;
+  }
+  return d == 0.0f ? 0.0f : dy * d;
 }
 
 // One matrix product C[i][j] = sum_k A(i, k) B(j, k) with what follows it.
@@ -95,10 +110,16 @@ inline int split_count(long long tiles, long long K, long long step, long long t
 long long simt_workspace(const Product& p);
 int simt_product(const Product& p, int dtype, void* ws, cudaStream_t s);
 
-// 16-bit types on the tensor cores; `status` is set to 1 if a bounded wait
+// On the tensor cores; `status` is set to 1 if a bounded wait
 // (at most spin_limit polls) gives up.
-long long tc_workspace(const Product& p);
+long long tc_workspace(const Product& p, int dtype);
 int tc_product(const Product& p, int dtype, void* ws, int* status, unsigned spin_limit, cudaStream_t s);
+
+// 16-bit types with at most kFewRows rows of A, which must lie along K: every
+// element of B is read once, straight into the operands of warp-level MMAs.
+constexpr int kFewRows = 15;
+bool few_takes(const Product& p);
+int few_product(const Product& p, int dtype, cudaStream_t s);
 
 // dz[i][j] = dy act'(z), rounded (dz null: not written), and parts[b][j], the
 // column sums of the unrounded dz over the rows of block b (parts null: none).
@@ -113,7 +134,7 @@ struct GradAct {
   long long I, J;
   int act;
 };
-long long grad_act_blocks(long long I, long long J);
+long long grad_act_blocks(const GradAct& g, int dtype);  // rows of parts (parts itself may be null still)
 int grad_act(const GradAct& g, int dtype, cudaStream_t s);
 // out[j] = sum_b parts[b][j], b ascending within a fixed tree.
 int sum_parts(const float* parts, long long blocks, long long J, void* out, int dtype, cudaStream_t s);

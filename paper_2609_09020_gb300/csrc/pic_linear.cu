@@ -93,13 +93,13 @@ int* status_word() {
   return p;
 }
 
-// Workspace bytes of a product, and the product: 16-bit types run on the tensor cores.
+// Workspace bytes of a product, and the product.
 long long product_workspace(const Product& p, int dtype) {
-  return dtype == PIC_DTYPE_F32 ? pic::lin::simt_workspace(p) : pic::lin::tc_workspace(p);
+  return dtype != PIC_DTYPE_F32 && pic::lin::few_takes(p) ? 0 : pic::lin::tc_workspace(p, dtype);
 }
 
 int product(const Product& p, int dtype, void* ws, cudaStream_t s) {
-  if (dtype == PIC_DTYPE_F32) return pic::lin::simt_product(p, dtype, ws, s);
+  if (dtype != PIC_DTYPE_F32 && pic::lin::few_takes(p)) return pic::lin::few_product(p, dtype, s);
   int* status = status_word();
   if (!status) return PIC_ERR_CUDA;
   return pic::lin::tc_product(p, dtype, ws, status, pic::kWaitPolls, s);
@@ -157,14 +157,16 @@ int backward(const pic_linear_grad_args& a, Arena& ws, bool launch, cudaStream_t
     lddz = (N + 7) / 8 * 8;  // rows of 16-bit values on 16-byte boundaries
     dz = ws.take(M * lddz * static_cast<long long>(elem_bytes(a.dtype)));
   }
-  const long long blocks = pic::lin::grad_act_blocks(M, N);
-  float* parts = a.db ? static_cast<float*>(ws.take(blocks * N * 4)) : nullptr;
-  if (launch && (own_dz || a.db)) {
-    const GradAct g{a.dy, a.lddy, a.pre, a.ldpre, own_dz ? const_cast<void*>(dz) : nullptr, lddz, parts, M, N, a.act};
+  GradAct g{a.dy, a.lddy, a.pre, a.ldpre, own_dz ? const_cast<void*>(dz) : nullptr, lddz, nullptr, M, N, a.act};
+  if (a.db) {
+    const long long blocks = pic::lin::grad_act_blocks(g, a.dtype);
+    g.parts = static_cast<float*>(ws.take(blocks * N * 4));
+    if (launch) rc = pic::lin::grad_act(g, a.dtype, s);
+    if (launch && rc == PIC_OK) rc = pic::lin::sum_parts(g.parts, blocks, N, a.db, a.dtype, s);
+  } else if (launch && own_dz) {
     rc = pic::lin::grad_act(g, a.dtype, s);
-    if (rc == PIC_OK && a.db) rc = pic::lin::sum_parts(parts, blocks, N, a.db, a.dtype, s);
-    if (rc != PIC_OK) return rc;
   }
+  if (rc != PIC_OK) return rc;
   if (a.dx) {
     Product p{};
     p.a = dz, p.a_i = lddz, p.a_k = 1;

@@ -1,0 +1,84 @@
+"""Generates the polynomial behind the 16-bit GELU derivative of the linear
+layer (csrc/pic_gelu_grad.cuh).
+
+GELU'(z) = Phi(z) + z phi(z).  With a = |z| and t(a) = Phi(-a) - a phi(a),
+
+    GELU'(z) = t(a) for z < 0, 1 - t(a) else,
+    t(a) = 2^(-a^2 log2(e) / 2) p(a),   p(a) = phi(0) (M(a) - a),
+
+M(a) = Phi(-a) / phi(a) Mills' ratio, which is smooth: p is fitted by a
+polynomial of degree 9 on 0 <= a <= A, A = 6, with the power as its weight
+(beyond A, |t| < 4e-8 is taken as 0).  Lawson's reweighting turns the least-
+squares fit on Chebyshev nodes into a minimax one.  The kernels take one 2^x,
+nine multiply-adds and a few operations more, against erfc and an exponential.
+
+Run:  python -m paper_2609_09020_gb300.gen_gelu_grad  (prints the header)
+"""
+from __future__ import annotations
+
+import numpy as np
+from numpy.polynomial import chebyshev, polynomial
+from scipy.special import erfcx, ndtr
+
+A = 6.0
+DEG = 9
+PASSES = 200
+HALF_LOG2E = -0.5 / np.log(2.0)
+
+
+def fit():
+    """Coefficients of p, lowest degree first."""
+    a = 0.5 * A * (1 - np.cos(np.linspace(0, np.pi, 4001)))
+    w = np.exp(-0.5 * a * a)
+    f = (np.sqrt(np.pi / 2) * erfcx(a / np.sqrt(2)) - a) / np.sqrt(2 * np.pi)
+    v = chebyshev.chebvander(2 * a / A - 1, DEG)
+    lw = np.ones_like(a)
+    for _ in range(PASSES):
+        wt = w * np.sqrt(lw)
+        c, *_ = np.linalg.lstsq(v * wt[:, None], f * wt, rcond=None)
+        e = np.abs(w * (v @ c - f))
+        lw *= e / e.max() + 1e-3
+        lw /= lw.mean()
+    p, power = np.zeros(1), np.ones(1)
+    for k in chebyshev.cheb2poly(c):
+        p = polynomial.polyadd(p, k * power)
+        power = polynomial.polymul(power, [-1.0, 2 / A])
+    return p
+
+
+def grad_fp32(z, c):
+    """fp32 emulation of the kernels' evaluation (the power correctly rounded)."""
+    f32 = np.float32
+    z = np.asarray(z, f32)
+    a = np.minimum(np.abs(z), f32(A))
+    p = np.full_like(a, f32(c[-1]))
+    for k in c[-2::-1]:
+        p = (a.astype(np.float64) * p + float(f32(k))).astype(f32)
+    e = np.exp2(((a * a).astype(f32) * f32(HALF_LOG2E)).astype(f32).astype(np.float64)).astype(f32)
+    t = np.where(a >= f32(A), f32(0), (e * p).astype(f32))
+    return np.where(z < 0, t, f32(1) - t)
+
+
+def max_error(c) -> float:
+    z = np.linspace(-12, 12, 1_200_001)
+    ref = ndtr(z) + z * np.exp(-0.5 * z * z) / np.sqrt(2 * np.pi)
+    return float(np.max(np.abs(grad_fp32(z, c).astype(np.float64) - ref)))
+
+
+def header(c) -> str:
+    lines = ["// Generated by paper_2609_09020_gb300/gen_gelu_grad.py -- do not edit.",
+             f"// Phi(-a) - a phi(a) ~= 2^(kGeluGradPower a^2) p(a) on 0 <= a <= {A:g}; max error of GELU' in",
+             f"// fp32 ~ {max_error(c):.1e}.",
+             "#pragma once", "", "namespace pic {", "",
+             f"constexpr float kGeluGradA = {float(np.float32(A))!r}f;",
+             f"constexpr float kGeluGradPower = {float(np.float32(HALF_LOG2E))!r}f;",
+             f"constexpr int kGeluGradDeg = {DEG};", "",
+             "// Coefficients of p, highest degree first (Horner order).",
+             "__host__ __device__ constexpr float gelu_grad_c(int i) {", "  constexpr float c[] = {"]
+    lines += [f"      {float(np.float32(k))!r}f," for k in c[::-1]]
+    lines += ["  };", "  return c[i];", "}", "", "}  // namespace pic", ""]
+    return "\n".join(lines)
+
+
+if __name__ == "__main__":
+    print(header(fit()), end="")

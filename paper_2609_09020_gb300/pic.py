@@ -441,16 +441,21 @@ def _rows(t, name, cols, like, rows=None, one_row=False):
     """(pointer, row stride) of t as a [rows][cols] matrix of ``like``'s type
     and device.  Leading dimensions are counted as rows, which they are for
     contiguous tensors and 2-D ones whose rows are contiguous."""
-    if t.dtype != like.dtype or t.device != like.device:
+    if t.dtype is not like.dtype or t.get_device() != like.get_device():
         raise ValueError(f"{name}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
-    if t.dim() < 1 or t.shape[-1] != cols:
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {cols} columns")
-    n = t.numel() // cols
+    shape = t.shape
+    if len(shape) == 2:
+        n = shape[0]
+    else:
+        n = t.numel() // cols
+    if not shape or shape[-1] != cols:
+        raise ValueError(f"{name}: shape {tuple(shape)}, expected {cols} columns")
     if rows is not None and n != rows:
         raise ValueError(f"{name}: {n} rows, expected {rows}")
-    if t.dim() <= 2 and n > 0:
-        ld = cols if n == 1 else t.stride(0)
-        if cols > 1 and t.stride(-1) != 1 or not (ld >= cols or one_row and ld == 0):
+    if len(shape) <= 2 and n > 0:
+        strides = t.stride()
+        ld = cols if n == 1 else strides[0]
+        if cols > 1 and strides[-1] != 1 or not (ld >= cols or one_row and ld == 0):
             raise ValueError(f"{name}: rows must be contiguous and must not overlap")
         return t.data_ptr(), ld
     if not t.is_contiguous():
@@ -459,14 +464,14 @@ def _rows(t, name, cols, like, rows=None, one_row=False):
 
 
 def _vector(t, name, n, like):
-    if t.dtype != like.dtype or t.device != like.device or t.shape != (n,) or not t.is_contiguous():
+    if (t.dtype is not like.dtype or t.get_device() != like.get_device() or t.shape != (n,)
+            or not t.is_contiguous()):
         raise ValueError(f"{name}: must be a contiguous [{n}] tensor of {like.dtype} on {like.device}")
     return t.data_ptr()
 
 
 def _on_device(t, name):
-    import torch
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+    if not t.is_cuda or t.get_device() != _current_device():
         raise ValueError(f"{name}: on {t.device}, must be on the current CUDA device")
 
 
@@ -492,16 +497,27 @@ class _Allocating:
             self._ctx.__exit__(*exc)
 
 
-def _call_with_workspace(name, args, device):
-    import torch
+def _call_with_workspace(name, args, like):
     lib = load_library()
-    need = getattr(lib, name + "_workspace_bytes")(ctypes.byref(args))
+    call, workspace_bytes = _linear_calls[name] if _linear_calls else _find_linear_calls(lib, name)
+    ref = ctypes.byref(args)
+    need = workspace_bytes(ref)
     if need < 0:
         raise PicError(PIC_ERR_INVALID_ARG, name)
-    ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    rc = getattr(lib, name)(ctypes.byref(args), ws.data_ptr() if need else None, need, _current_stream())
+    # in units of the call's type: new_empty takes fewer steps than torch.empty
+    ws = like.new_empty(-(-need // like.element_size())) if need else None
+    rc = call(ref, ws.data_ptr() if need else None, need, _current_stream())
     if rc != PIC_OK:
         raise PicError(rc, name)
+
+
+_linear_calls = {}
+
+
+def _find_linear_calls(lib, name):
+    for n in ("pic_linear", "pic_linear_backward"):
+        _linear_calls[n] = getattr(lib, n), getattr(lib, n + "_workspace_bytes")
+    return _linear_calls[name]
 
 
 def _linear_act(act) -> int:
@@ -519,7 +535,6 @@ def linear(x, weight, bias=None, act="none", residual=None, out=None, save_pre=F
     ``residual``), or (y, pre) with save_pre: pre = x weight^T + bias is what
     ``linear_backward`` reads.  x and residual may be 2-D with rows further
     apart than their width.  Enqueued on the stream, not synchronised."""
-    import torch
     _on_device(x, "x")
     if weight.dim() != 2:
         raise ValueError("weight: must be 2-D")
@@ -537,15 +552,17 @@ def linear(x, weight, bias=None, act="none", residual=None, out=None, save_pre=F
         a.bias = _vector(bias, "bias", N, x)
     if residual is not None:
         a.residual, a.ldr = _rows(residual, "residual", N, x, M, one_row=True)
-    shape = x.shape[:-1] + (N,)
+    shape = (M, N) if x.dim() == 2 else x.shape[:-1] + (N,)
     with _Allocating(stream):
         if out is None:
-            out = torch.empty(shape, dtype=x.dtype, device=x.device)
-        a.y, a.ldy = _rows(out, "out", N, x, M)
-        pre = torch.empty(shape, dtype=x.dtype, device=x.device) if save_pre else None
+            out = x.new_empty(shape)
+            a.y, a.ldy = out.data_ptr(), N
+        else:
+            a.y, a.ldy = _rows(out, "out", N, x, M)
         if save_pre:
+            pre = x.new_empty(shape)
             a.pre, a.ldpre = pre.data_ptr(), N
-        _call_with_workspace("pic_linear", a, x.device)
+        _call_with_workspace("pic_linear", a, x)
     return (out, pre) if save_pre else out
 
 
@@ -554,7 +571,6 @@ def linear_backward(dy, x, weight, act="none", pre=None, need=("x", "weight", "b
     dy [..., out]; those not named in ``need`` are None.  pre is what
     ``linear`` returned with save_pre (not read with act "none").  The
     residual's gradient is dy itself.  Enqueued on the stream."""
-    import torch
     _on_device(dy, "dy")
     if weight.dim() != 2:
         raise ValueError("weight: must be 2-D")
@@ -579,16 +595,16 @@ def linear_backward(dy, x, weight, act="none", pre=None, need=("x", "weight", "b
     dx = dw = db = None
     with _Allocating(stream):
         if "x" in need:
-            dx = torch.empty(x.shape, dtype=dy.dtype, device=dy.device)
+            dx = dy.new_empty(x.shape)
             a.dx, a.lddx = dx.data_ptr(), K
         if "weight" in need:
-            dw = torch.empty((N, K), dtype=dy.dtype, device=dy.device)
+            dw = dy.new_empty((N, K))
             a.dw, a.lddw = dw.data_ptr(), K
         if "bias" in need:
-            db = torch.empty(N, dtype=dy.dtype, device=dy.device)
+            db = dy.new_empty(N)
             a.db = db.data_ptr()
         if M > 0 or "weight" in need or "bias" in need:
-            _call_with_workspace("pic_linear_backward", a, dy.device)
+            _call_with_workspace("pic_linear_backward", a, dy)
     return dx, dw, db
 
 
@@ -725,6 +741,18 @@ def _buffers_fit(need: dict, device, latents, steps, weights, out) -> bool:
                 and out.nbytes >= need["out"])
     except (AttributeError, RuntimeError):
         return False
+
+
+_raw_device = None  # () -> the current device
+
+
+def _current_device() -> int:
+    global _raw_device
+    if _raw_device is None:
+        import torch
+        torch.cuda.current_device()  # initialises CUDA, which the raw getter does not
+        _raw_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return _raw_device()
 
 
 _raw_stream = None  # () -> the current stream of the current device

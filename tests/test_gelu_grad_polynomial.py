@@ -1,0 +1,29 @@
+"""The generated polynomial of GELU': its header is the generator's, its error
+is the one stated, and it ends where it should."""
+import os
+import re
+
+import numpy as np
+
+from paper_2609_09020_gb300 import gen_gelu_grad as gen
+
+HEADER = os.path.join(os.path.dirname(os.path.abspath(gen.__file__)), "csrc", "pic_gelu_grad.cuh")
+
+
+def coefficients():
+    text = open(HEADER).read()
+    body = text[text.index("c[] = {"):text.index("return c[i]")]
+    return np.array([float(v) for v in re.findall(r"(-?[\d.]+(?:e-?\d+)?)f", body)][::-1])
+
+
+def test_header_is_generated():
+    # the fit may differ in the last digits from one linear algebra library to another
+    assert np.allclose(coefficients(), gen.fit(), rtol=1e-3, atol=1e-6)
+
+
+def test_error():
+    c = coefficients()
+    assert gen.max_error(c) < 5e-7
+    assert np.all(gen.grad_fp32(np.array([6.0, 10.0, 1e30, np.inf]), c) == 1)
+    assert np.all(gen.grad_fp32(np.array([-6.0, -10.0, -1e30, -np.inf]), c) == 0)
+    assert abs(float(gen.grad_fp32(np.array([0.0]), c)[0]) - 0.5) < 5e-7

@@ -124,6 +124,26 @@ def test_larger(size, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("size", [(1, 4096, 4096), (1, 16384, 16), (3, 4104, 1000), (9, 2048, 4096), (16, 512, 16384),
+                                  (24, 4096, 600), (25, 5000, 2000), (32, 2048, 2056), (32, 16384, 96), (32, 1, 5000),
+                                  (33, 4096, 512), (2, 8192, 24)], ids=str)
+def test_few_rows(size, dtype):
+    """Weights read once: K in many turns, over the CTAs of a cluster, ends inside a turn."""
+    from paper_2609_09020_gb300 import pic
+    M, K, N = size
+    x, w = normal((M, K), dtype, 1), normal((N, K), dtype, 2, 1.4 / math.sqrt(K))
+    b, r, dy = normal((N,), dtype, 3, 0.1), normal((M, N), dtype, 4), normal((M, N), dtype, 5, 0.1)
+    y, z = pic.linear(x, w, b, act="gelu", residual=r, save_pre=True)
+    want_y, want_z = ref.forward(x, w, b, "gelu", r)
+    ref.check(y, want_y, "y")
+    ref.check(z, want_z, "pre")
+    got = pic.linear_backward(dy, x, w, act="gelu", pre=z)
+    for g, v, name in zip(got, ref.backward(dy, x, w, z, "gelu"), ("dx", "dw", "db")):
+        ref.check(g, v, name)
+    pic.linear_check()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 def test_no_rows(dtype):
     from paper_2609_09020_gb300 import pic
     x, w, b = normal((0, 24), dtype, 1), normal((8, 24), dtype, 2), normal((8,), dtype, 3)
@@ -162,6 +182,31 @@ def test_leading_dimensions(dtype):
     one = pic.linear(x[0, 0], w)
     assert one.shape == (24,)
     ref.check(one.view(1, 24), ref.forward(x[0, :1], w, None, "none", None)[0])
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_infinities_in_large_products(dtype):
+    """One infinite or NaN value in a product of many tiles and a long sum: what
+    IEEE arithmetic gives, in its row, its column and nowhere else."""
+    from paper_2609_09020_gb300 import pic
+    M, K, N = 400, 700, 300
+    x, w = normal((M, K), dtype, 1), normal((N, K), dtype, 2, 0.1)
+    dy, z = normal((M, N), dtype, 3), normal((M, N), dtype, 4)
+    (want, tol), _ = ref.forward(x, w, None, "none", None)
+    x[301, 650], x[5, 2], w[77, 300] = math.inf, math.nan, -math.inf
+    y = pic.linear(x, w)
+    assert bool(torch.isnan(y[5]).all())
+    assert torch.equal(y[301][:77], torch.sign(w[:77, 650]) * math.inf)
+    keep_r = torch.ones(M, dtype=torch.bool, device="cuda")
+    keep_r[301] = keep_r[5] = False
+    assert torch.equal(y[keep_r, 77], torch.sign(x[keep_r, 300]) * -math.inf)
+    cols = torch.ones(N, dtype=torch.bool, device="cuda")
+    cols[77] = False
+    ref.check(y[keep_r][:, cols], (want[keep_r][:, cols], tol[keep_r][:, cols]))
+    dy[17, 33] = math.inf
+    dx, dw, db = pic.linear_backward(dy, x.clamp(-4, 4).nan_to_num(), w.clamp(-4, 4), need=("x", "weight", "bias"))
+    assert bool(dx[17].isinf().all()) and bool(dw[33].isinf().all()) and float(db[33]) == math.inf
+    assert not bool(dx[:17].isinf().any()) and int(dw.isinf().any(1).sum()) == 1 and not bool(dw.isnan().any())
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
