@@ -33,7 +33,10 @@ constexpr int kSms = 152;
 // The few rows in shared memory.  More would leave an SM a single CTA and take
 // longer to read than the weights: 4 rows of 16384 to 4096 columns 51 us (tiles of
 // 128 rows on tcgen05: 35), 15 rows of 4096, which this just allows, 19 (25).
-constexpr int kMaxRowBytes = 124 * 1024;
+constexpr int kAlongRowBytes = 124 * 1024;
+// Across, a row is read four bytes at a time: 8 rows of dz, 16384 to 4096 columns 43
+// us with 64 KB (tiles: 36), 15 rows 81; 4096 to 4096 with 31 KB 15 us (25).
+constexpr int kAcrossRowBytes = 48 * 1024;
 
 struct FewParams {
   Product p;
@@ -330,7 +333,7 @@ Plan plan(const Product& p) {
   r.cluster = 1;
   while (r.cluster < 8 && groups * r.cluster * 2 <= 2 * kSms && p.K >= 2LL * r.cluster * turn * warps) r.cluster *= 2;
   const long long stride = row_bytes(r.cluster);
-  if (p.I * stride > kMaxRowBytes) return r;
+  if (p.I * stride > (r.along ? kAlongRowBytes : kAcrossRowBytes)) return r;
   r.stride = static_cast<int>(stride);
   r.tiles = r.along ? static_cast<int>((p.I + 7) / 8) : 1;
   const int sums = r.along ? kAlongWarps * r.tiles * 8 * kAlongStride : kAcrossWarps * 16 * kAcrossStride;

@@ -1,0 +1,545 @@
+// k_linear_narrow.cu -- the whole gradient of a narrow layer (a hidden layer of a
+// synthesis net, over the pixels of images) in one pass over the rows:
+//
+//   dz = dy act'(z),  dx = dz w,  dw += dz^T x,  db += dz
+//
+// Bound by memory: dy, z and x are read once and dx is written once, where
+// separate products would write dz and read it twice.  A CTA stays on its SM and
+// takes tiles of 128 rows.  One tile of dz in shared memory (64 columns to a row
+// of 128 bytes, swizzled) is both operands: read along its rows it is A of
+// dx = dz w, read across them A of dw = dz^T x.  dw stays in tensor memory from
+// tile to tile; at the end each CTA writes its dw and db, and a small second kernel
+// adds the CTAs' in order.
+//
+// Up to 128 columns on each side for 16-bit types, 64 for fp32, whose values are
+// cut into three bfloat16 pieces as in cut3.cuh (dw is then taken over into
+// registers after every tile).
+//
+// Roles of the 16 warps: 0..3 dx out of tensor memory, 4 and 5 (fp32) take dw
+// over, 6 issues the MMAs, 8..15 load: 4 x 16 bytes of dy, z and x per thread at a
+// time, x of this tile under way while dz is computed, dy and z of the next while
+// x is written to shared memory.
+//
+// An infinite or NaN value among fp32 pieces would spread (inf 0 = NaN): its tile
+// is marked, and dx and dw of that tile are computed again on the FP32 cores.
+#include "cut3.cuh"
+#include "k_linear_tc.cuh"
+
+namespace pic {
+namespace lin {
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kLoadWarp = 8, kLoaders = 256;
+constexpr int kMmaWarp = 6;
+constexpr int kTile = 128;
+constexpr int kMarks = 8;  // more tiles than the loaders can be ahead of the others
+constexpr int kSms = 152;
+
+struct NarrowParams {
+  NarrowGrad g;
+  long long tiles;
+  int vec_dy, vec_z, vec_x, store_tma;
+  float* parts;  // [CTAs][N K + N]
+  int* status;
+  unsigned spin_limit;
+};
+
+// T: element; WIDE: up to 128 columns (16-bit types), else 64.
+template <typename T, bool WIDE>
+struct Shape {
+  static constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
+  static constexpr int kPer = 16 / sizeof(T);          // elements of a load
+  static constexpr int kBlocks = WIDE ? 2 : 1;         // of 64 columns
+  static constexpr int kCols = 64 * kBlocks;
+  static constexpr int kVecs = kCols / kPer;           // loads of a row
+  static constexpr int kPassRows = kLoaders / kVecs;   // rows that the loaders cover at once
+  static constexpr int kUnitRows = 4 * kPassRows;      // rows of a unit: four loads of each matrix per thread
+  static constexpr int kUnits = kTile / kUnitRows;
+  static constexpr int kBlockBytes = kTile * 128;
+  static constexpr int kPlaneBytes = kBlocks * kBlockBytes;
+  static constexpr int kStageBytes = 2 * kPlanes * kPlaneBytes;  // dz, x
+  static constexpr int kStages = sizeof(T) == 4 ? 1 : WIDE ? 2 : 4;
+  static constexpr int kWBlock = kCols * 128, kWPlane = kBlocks * kWBlock;
+  static constexpr int kOffW = kStages * kStageBytes;
+  static constexpr int kOffPanels = kOffW + kPlanes * kWPlane;
+  static constexpr int kOffSums = kOffPanels + 4 * 2 * kPanelBytes;
+  static constexpr int kOffBars = kOffSums + kLoaders * kPer * 4;
+  // full, empty; dx ready, free; dw ready, free; drain
+  static constexpr int kBars = 2 * kStages + 4 + 4 + 1;
+  static constexpr int kOffMarks = kOffBars + kBars * 8 + 8;
+  static constexpr int kSmem = kOffMarks + (kMarks + 1) * 4 + 8 + 1024;
+  static constexpr int kTmemDw = 2 * kCols;  // columns: two buffers of dx, then dw (fp32: two)
+  static constexpr int kTmemCols = WIDE ? 512 : 256;
+};
+
+template <typename T>
+struct Vec16 {
+  static constexpr int kPer = 16 / sizeof(T);
+  uint32_t w[4];
+  __device__ __forceinline__ void get(const T* p, int n, bool vec) {
+    if (n >= kPer && vec) {
+      const uint4 q = __ldg(reinterpret_cast<const uint4*>(p));
+      w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = 0;
+    if (n <= 0) return;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < n) w[i] = __ldg(reinterpret_cast<const uint32_t*>(p) + i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < n) w[i / 2] |= static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t*>(p) + i)) << (16 * (i & 1));
+    }
+  }
+  __device__ __forceinline__ void widen(float (&f)[kPer]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) {
+        f[i] = __uint_as_float(w[i]);
+      } else {
+        const float2 v = unpack2_16<T>(w[i]);
+        f[2 * i] = v.x;
+        f[2 * i + 1] = v.y;
+      }
+    }
+  }
+};
+
+// 16 bytes' worth of elements at (row, first column col) of a tile whose blocks of
+// 64 columns are `block` bytes apart: one store, or three of half the size.
+template <typename T>
+__device__ __forceinline__ uint32_t put_vec(uint32_t tile, int block, int plane, int row, int col, const uint32_t (&w)[4]) {
+  const uint32_t at = tile + (col >> 6) * block + row * 128 + ((((col & 63) >> 3) ^ (row & 7)) << 4);
+  if constexpr (sizeof(T) == 4) {
+    uint32_t h0, m0, l0, h1, m1, l1;
+    cut3(w[0], w[1], h0, m0, l0);
+    cut3(w[2], w[3], h1, m1, l1);
+    const uint32_t a = at + (col & 4) * 2;
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(a), "r"(h0), "r"(h1) : "memory");
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(a + plane), "r"(m0), "r"(m1) : "memory");
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(a + 2 * plane), "r"(l0), "r"(l1) : "memory");
+    return max(max(w[0] & 0x7fffffffu, w[1] & 0x7fffffffu), max(w[2] & 0x7fffffffu, w[3] & 0x7fffffffu));
+  } else {
+    tc::sts128(at, w[0], w[1], w[2], w[3]);
+    return 0;
+  }
+}
+
+__device__ __forceinline__ float dz_again(const NarrowGrad& g, long long i, int n) {
+  const float d = static_cast<const float*>(g.dy)[i * g.lddy + n];
+  return g.act == PIC_ACT_NONE ? d : act_grad<true>(d, static_cast<const float*>(g.pre)[i * g.ldpre + n], g.act);
+}
+// dx of a row, and a tile's part of a row of dw, on the FP32 cores (fp32 only).
+__device__ __noinline__ void dx_again(float* v, const NarrowGrad& g, long long i) {
+  for (int k = 0; k < 64; ++k) {
+    float s = 0.0f;
+    if (i < g.I && k < g.K)
+      for (int n = 0; n < g.N; ++n) s = fmaf(dz_again(g, i, n), static_cast<const float*>(g.w)[n * g.ldw + k], s);
+    v[k] = s;
+  }
+}
+__device__ __noinline__ void dw_again(float* v, const NarrowGrad& g, long long i0, int n) {
+  for (int k = 0; k < 64; ++k) {
+    float s = 0.0f;
+    if (n < g.N && k < g.K)
+      for (long long i = i0; i < min(g.I, i0 + kTile); ++i)
+        s = fmaf(dz_again(g, i, n), static_cast<const float*>(g.x)[i * g.ldx + k], s);
+    v[k] = s;
+  }
+}
+
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(kThreads, 1)
+    narrow_kernel(const __grid_constant__ NarrowParams q, const __grid_constant__ CUtensorMap dx_map) {
+  using S = Shape<T, WIDE>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = tc::smem_addr(smem_raw);
+  uint8_t* smem = smem_raw + ((1024 - (raw & 1023)) & 1023);
+  const uint32_t base = tc::smem_addr(smem);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const NarrowGrad& g = q.g;
+  const uint32_t bars = base + S::kOffBars;
+  const uint32_t bar_full = bars, bar_empty = bars + 8 * S::kStages, bar_dx = bar_empty + 8 * S::kStages,
+                 bar_dx_free = bar_dx + 16, bar_dw = bar_dx_free + 16, bar_dw_free = bar_dw + 16, bar_drain = bar_dw_free + 16;
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + S::kOffBars + 8 * S::kBars);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::kOffBars + 8 * S::kBars + 4);
+  // mark t % kMarks holds t + 1 if this CTA's t-th tile has an infinite or NaN
+  // operand; the last one is w's
+  volatile int* marks = reinterpret_cast<volatile int*>(smem + S::kOffMarks);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S::kStages; ++s) {
+      tc::mbar_init(bar_full + 8 * s, kLoaders / 32);
+      tc::mbar_init(bar_empty + 8 * s, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      tc::mbar_init(bar_dx + 8 * b, 1);
+      tc::mbar_init(bar_dx_free + 8 * b, 4);
+      tc::mbar_init(bar_dw + 8 * b, 1);
+      tc::mbar_init(bar_dw_free + 8 * b, 2);
+    }
+    tc::mbar_init(bar_drain, 1);
+    *abort_flag = 0;
+    for (int m = 0; m <= kMarks; ++m) marks[m] = 0;
+    tc::fence_mbar_init();
+  }
+  if (warp == kMmaWarp) tc::tmem_alloc_cg<1>(tc::smem_addr(tmem_slot), S::kTmemCols);
+  __syncthreads();
+  // w [N][K], zero to whole blocks
+  if (g.dx) {
+    uint32_t largest = 0;
+    const bool vec = reinterpret_cast<uintptr_t>(g.w) % 16 == 0 && g.ldw % S::kPer == 0;
+    for (int e = threadIdx.x; e < S::kCols * S::kVecs; e += kThreads) {
+      const int row = e / S::kVecs, col = e % S::kVecs * S::kPer;
+      Vec16<T> v;
+      v.get(static_cast<const T*>(g.w) + row * g.ldw + col, row < g.N ? g.K - col : 0, vec);
+      largest = max(largest, put_vec<T>(base + S::kOffW, S::kWBlock, S::kWPlane, row, col, v.w));
+    }
+    if (largest >= 0x7f800000u) marks[kMarks] = 1;
+  }
+  tc::fence_async_smem();
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  auto wait = [&](uint32_t bar, uint32_t parity) { return wait_bounded(bar, parity, abort_flag, q.status, q.spin_limit); };
+  float* my_parts = q.parts + blockIdx.x * static_cast<long long>(g.N * g.K + g.N);
+
+  if (warp >= kLoadWarp) {
+    const int tid = threadIdx.x - 32 * kLoadWarp;
+    const int row = tid / S::kVecs, col = tid % S::kVecs * S::kPer;
+    const T* dy = static_cast<const T*>(g.dy) + col;
+    const T* z = static_cast<const T*>(g.pre) + col;
+    const T* x = static_cast<const T*>(g.x) + col;
+    const int n_dz = g.N - col, n_x = g.dw ? g.K - col : 0;
+    const bool has_act = g.act != PIC_ACT_NONE;
+    Vec16<T> vy[4], vz[4], vx[4];
+    auto load_dz = [&](long long i0) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const long long i = i0 + row + u * S::kPassRows;
+        vy[u].get(dy + i * g.lddy, i < g.I ? n_dz : 0, q.vec_dy);
+        if (has_act) vz[u].get(z + i * g.ldpre, i < g.I ? n_dz : 0, q.vec_z);
+      }
+    };
+    float sum[S::kPer] = {};
+    int s = 0, count = 0;
+    uint32_t phase = 0;
+    if (blockIdx.x < q.tiles) load_dz(blockIdx.x * static_cast<long long>(kTile));
+    for (long long tile = blockIdx.x; tile < q.tiles; tile += gridDim.x, ++count) {
+      uint32_t largest = 0;
+      bool ok = true;
+#pragma unroll
+      for (int unit = 0; unit < S::kUnits; ++unit) {
+        const long long i0 = tile * kTile + unit * S::kUnitRows;
+        if (n_x > 0) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const long long i = i0 + row + u * S::kPassRows;
+            vx[u].get(x + i * g.ldx, i < g.I ? n_x : 0, q.vec_x);
+          }
+        }
+        // dz in the place of dy
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          float d[S::kPer], v[S::kPer];
+          vy[u].widen(d);
+          if (has_act) {
+            vz[u].widen(v);
+#pragma unroll
+            for (int e = 0; e < S::kPer; ++e) d[e] = act_grad<sizeof(T) == 4>(d[e], v[e], g.act);
+          }
+#pragma unroll
+          for (int e = 0; e < S::kPer; ++e) sum[e] += d[e];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 4)
+              vy[u].w[i] = __float_as_uint(d[i]);
+            else
+              vy[u].w[i] = pack2_16<T>(d[2 * i], d[2 * i + 1]);
+          }
+        }
+        if (unit == 0) ok = __all_sync(0xffffffffu, wait(bar_empty + 8 * s, phase ^ 1));
+        if (!ok) break;
+        const uint32_t sdz = base + s * S::kStageBytes, sx = sdz + S::kPlanes * S::kPlaneBytes;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          largest = max(largest, put_vec<T>(sdz, S::kBlockBytes, S::kPlaneBytes, unit * S::kUnitRows + row + u * S::kPassRows, col, vy[u].w));
+        if (unit + 1 < S::kUnits)
+          load_dz(i0 + S::kUnitRows);
+        else if (tile + gridDim.x < q.tiles)
+          load_dz((tile + gridDim.x) * kTile);
+        if (g.dw) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            if (n_x <= 0) vx[u].w[0] = vx[u].w[1] = vx[u].w[2] = vx[u].w[3] = 0;
+            largest = max(largest, put_vec<T>(sx, S::kBlockBytes, S::kPlaneBytes, unit * S::kUnitRows + row + u * S::kPassRows, col, vx[u].w));
+          }
+        }
+      }
+      if (!ok) break;
+      if (largest >= 0x7f800000u) marks[count % kMarks] = count + 1;
+      tc::fence_async_smem();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(bar_full + 8 * s);
+      if (++s == S::kStages) s = 0, phase ^= 1;
+    }
+    // db: the threads of a column
+    __syncwarp();
+    if (g.db) {
+      float* sums = reinterpret_cast<float*>(smem + S::kOffSums);
+#pragma unroll
+      for (int e = 0; e < S::kPer; ++e) sums[row * S::kCols + col + e] = sum[e];
+      tc::named_bar(1, kLoaders);
+      if (tid < g.N) {
+        float t = 0.0f;
+        for (int r = 0; r < S::kPassRows; ++r) t += sums[r * S::kCols + tid];
+        my_parts[g.N * g.K + tid] = t;
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    if (tc::elect_one()) {
+      const int k_pad = (g.K + 15) / 16 * 16, n_steps = (g.N + 15) / 16;
+      const uint32_t idesc_dx = idesc_of<T>(128, k_pad, false, true), idesc_dw = idesc_of<T>(128, k_pad, true, true);
+      // of a dz of one block the MMA's rows 64..127 are rows 0..63 again, not looked at
+      const uint32_t dz_lbo = WIDE && g.N > 64 ? S::kBlockBytes : 0;
+      int s = 0, buf = 0;
+      uint32_t phase = 0, free_phase = 0;
+      bool ok = true, first = true;
+      for (long long tile = blockIdx.x; tile < q.tiles && ok; tile += gridDim.x) {
+        if (!(ok = wait(bar_full + 8 * s, phase))) break;
+        tc::tc_fence_after();
+        const uint32_t sdz = base + s * S::kStageBytes, sx = sdz + S::kPlanes * S::kPlaneBytes, sw = base + S::kOffW;
+        constexpr int kProducts = S::kPlanes == 3 ? 6 : 1;
+        if (g.dx) {
+          if (!(ok = wait(bar_dx_free + 8 * buf, free_phase ^ 1))) break;
+          tc::tc_fence_after();
+#pragma unroll
+          for (int t = 0; t < kProducts; ++t) {
+            const int pa = kProducts == 6 ? cut_a(t) : 0, pb = kProducts == 6 ? cut_b(t) : 0;
+            for (int kk = 0; kk < n_steps; ++kk)
+              tc::mma_16<1>(tmem + buf * S::kCols,
+                            tc::smem_desc_sw128(sdz + pa * S::kPlaneBytes + (kk >> 2) * S::kBlockBytes + (kk & 3) * 32, 8192, 1024),
+                            tc::smem_desc_sw128(sw + pb * S::kWPlane + kk * 2048, S::kWBlock, 1024), idesc_dx,
+                            (t > 0 || kk > 0) ? 1u : 0u);
+          }
+          tc::mma_commit(bar_dx + 8 * buf);
+        }
+        if (g.dw) {
+          const uint32_t d = tmem + S::kTmemDw + (S::kPlanes == 3 ? buf * S::kCols : 0);
+          if (S::kPlanes == 3) {
+            if (!(ok = wait(bar_dw_free + 8 * buf, free_phase ^ 1))) break;
+            tc::tc_fence_after();
+          }
+#pragma unroll
+          for (int t = 0; t < kProducts; ++t) {
+            const int pa = kProducts == 6 ? cut_a(t) : 0, pb = kProducts == 6 ? cut_b(t) : 0;
+#pragma unroll
+            for (int kk = 0; kk < kTile / 16; ++kk)
+              tc::mma_16<1>(d, tc::smem_desc_sw128(sdz + pa * S::kPlaneBytes + kk * 2048, dz_lbo, 1024),
+                            tc::smem_desc_sw128(sx + pb * S::kPlaneBytes + kk * 2048, S::kBlockBytes, 1024), idesc_dw,
+                            ((S::kPlanes == 1 && !first) || t > 0 || kk > 0) ? 1u : 0u);
+          }
+          if (S::kPlanes == 3) tc::mma_commit(bar_dw + 8 * buf);
+          first = false;
+        }
+        tc::mma_commit(bar_empty + 8 * s);
+        if (++s == S::kStages) s = 0, phase ^= 1;
+        if (++buf == 2) buf = 0, free_phase ^= 1;
+      }
+      if (!ok) {  // aborted: MMAs in flight still read shared memory
+        tc::mma_commit(bar_drain);
+        for (uint32_t i = 0; i < q.spin_limit && !tc::mbar_try_wait(bar_drain, 0); ++i) {
+        }
+      } else if (S::kPlanes == 1 && g.dw) {
+        tc::mma_commit(bar_dw);
+      }
+    }
+    __syncwarp();
+  } else if (warp < 4) {
+    const uint32_t panels = base + S::kOffPanels + warp * 2 * kPanelBytes;
+    const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
+    Product p{};  // what put_panel looks at
+    p.I = g.I, p.J = g.K;
+    int buf = 0, pb = 0, count = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (long long tile = blockIdx.x; g.dx && tile < q.tiles; tile += gridDim.x, ++count) {
+      ok = __all_sync(0xffffffffu, wait(bar_dx + 8 * buf, phase));
+      if (!ok) break;
+      tc::tc_fence_after();
+      const long long row0 = tile * kTile + warp * 32;
+#pragma unroll
+      for (int b = 0; b < S::kBlocks; ++b) {
+        uint32_t r[64];
+        if (64 * b < g.K) tc::tmem_ld64_wait(tmem + buf * S::kCols + 64 * b + lanes, r);
+        if (b + 1 == S::kBlocks) {
+          tc::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(bar_dx_free + 8 * buf);
+        }
+        if (64 * b >= g.K || row0 >= g.I) continue;
+        if constexpr (sizeof(T) == 4) {
+          if (marks[count % kMarks] == count + 1 || marks[kMarks]) {
+            float v[64];
+            dx_again(v, g, row0 + lane);
+#pragma unroll
+            for (int c = 0; c < 64; ++c) r[c] = __float_as_uint(v[c]);
+          }
+        }
+        constexpr int kPanels = sizeof(T) == 4 ? 2 : 1;
+#pragma unroll
+        for (int h = 0; h < kPanels; ++h) {
+          if (64 * b + 32 * h * (kPanels - 1) >= g.K) break;
+          uint32_t out[32];
+#pragma unroll
+          for (int c = 0; c < 32; ++c) {
+            if constexpr (sizeof(T) == 4)
+              out[c] = r[32 * h + c];
+            else
+              out[c] = pack2_16<T>(__uint_as_float(r[2 * c]), __uint_as_float(r[2 * c + 1]));
+          }
+          if (lane == 0) tc::bulk_wait_read<1>();
+          __syncwarp();
+          put_panel<T>(out, panels + pb * kPanelBytes, lane, row0, 64 * b + 32 * h, p, g.dx, g.lddx, &dx_map, q.store_tma);
+          pb ^= 1;
+        }
+      }
+      if (++buf == 2) buf = 0, phase ^= 1;
+    }
+    if (lane == 0) tc::bulk_wait_all();
+    __syncwarp();
+    if (S::kPlanes == 1 && g.dw && ok && __all_sync(0xffffffffu, wait(bar_dw, 0))) {
+      tc::tc_fence_after();
+      const int n = warp * 32 + lane;
+#pragma unroll
+      for (int b = 0; b < S::kBlocks; ++b) {
+        if (64 * b >= g.K || warp * 32 >= g.N) break;
+        uint32_t r[64];
+        tc::tmem_ld64_wait(tmem + S::kTmemDw + 64 * b + lanes, r);
+        if (n < g.N)
+#pragma unroll
+          for (int c = 0; c < 64; ++c)
+            if (64 * b + c < g.K) my_parts[n * g.K + 64 * b + c] = __uint_as_float(r[c]);
+      }
+    }
+    __syncwarp();
+  } else if (S::kPlanes == 3 && warp < 6 && g.dw) {
+    const int n = (warp - 4) * 32 + lane;
+    const uint32_t lanes = static_cast<uint32_t>((warp - 4) * 32) << 16;
+    float v[64] = {};
+    int buf = 0, count = 0;
+    uint32_t phase = 0;
+    for (long long tile = blockIdx.x; tile < q.tiles; tile += gridDim.x, ++count) {
+      if (!__all_sync(0xffffffffu, wait(bar_dw + 8 * buf, phase))) break;
+      tc::tc_fence_after();
+      if (marks[count % kMarks] == count + 1) {
+        float u[64];
+        dw_again(u, g, tile * kTile, n);
+#pragma unroll
+        for (int c = 0; c < 64; ++c) v[c] += u[c];
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t r[32];
+          tc::tmem_ld32_wait(tmem + S::kTmemDw + buf * S::kCols + 32 * h + lanes, r);
+#pragma unroll
+          for (int c = 0; c < 32; ++c) v[32 * h + c] += __uint_as_float(r[c]);
+        }
+      }
+      tc::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(bar_dw_free + 8 * buf);
+      if (++buf == 2) buf = 0, phase ^= 1;
+    }
+    if (n < g.N)
+#pragma unroll
+      for (int c = 0; c < 64; ++c)
+        if (c < g.K) my_parts[n * g.K + c] = v[c];
+    __syncwarp();
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  if (warp == kMmaWarp) tc::tmem_dealloc_cg<1>(tmem, S::kTmemCols);
+}
+
+// dw and db from the CTAs' parts: a block finishes 32 values, its warps add every
+// eighth part, the first warp the warps' sums.
+template <typename T>
+__global__ void __launch_bounds__(256) add_parts_kernel(const float* parts, int n_parts, const NarrowGrad g) {
+  __shared__ float sums[8][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nk = g.N * g.K, per = nk + g.N;
+  const int e = blockIdx.x * 32 + lane;
+  float v = 0.0f;
+  if (e < per) {
+#pragma unroll 5
+    for (int s = warp; s < n_parts; s += 8) v += __ldcg(parts + s * static_cast<long long>(per) + e);
+  }
+  sums[warp][lane] = v;
+  __syncthreads();
+  if (warp > 0 || e >= per) return;
+#pragma unroll
+  for (int w = 1; w < 8; ++w) v += sums[w][lane];
+  if (e >= nk) {
+    if (g.db) static_cast<T*>(g.db)[e - nk] = from_f32<T>(v);
+  } else if (g.dw) {
+    static_cast<T*>(g.dw)[e / g.K * g.lddw + e % g.K] = from_f32<T>(v);
+  }
+}
+
+int ctas(const NarrowGrad& g) {
+  const long long tiles = (g.I + kTile - 1) / kTile;
+  return static_cast<int>(tiles < kSms ? tiles : kSms);
+}
+
+template <typename T, bool WIDE>
+int run(const NarrowGrad& g, NarrowParams& q, const CUtensorMap& map, int slot, cudaStream_t s) {
+  const void* fn = reinterpret_cast<const void*>(narrow_kernel<T, WIDE>);
+  const int smem = Shape<T, WIDE>::kSmem, grid = ctas(g);
+  static_assert(Shape<T, WIDE>::kSmem <= 227 * 1024, "shared memory of an SM");
+  if (allow_smem(fn, slot, smem) != PIC_OK) return PIC_ERR_CUDA;
+  void* args[] = {&q, const_cast<CUtensorMap*>(&map)};
+  if (cudaLaunchKernel(fn, dim3(grid), dim3(kThreads), args, smem, s) != cudaSuccess) return PIC_ERR_CUDA;
+  if (g.dw || g.db) {
+    const int per = g.N * g.K + g.N;
+    add_parts_kernel<T><<<(per + 31) / 32, 256, 0, s>>>(q.parts, grid, g);
+  }
+  return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+}
+
+}  // namespace
+
+bool narrow_takes(const NarrowGrad& g, int dtype) {
+  const int most = dtype == PIC_DTYPE_F32 ? 64 : 128;
+  return (g.dx || g.dw) && g.N <= most && g.K <= most && g.I >= 1024;
+}
+
+long long narrow_workspace(const NarrowGrad& g) { return ctas(g) * static_cast<long long>(g.N * g.K + g.N) * 4; }
+
+int narrow_grad(const NarrowGrad& g, int dtype, void* ws, int* status, unsigned spin_limit, cudaStream_t s) {
+  NarrowParams q{};
+  const int elem = dtype == PIC_DTYPE_F32 ? 4 : 2;
+  const auto on16 = [&](const void* m, long long ld) { return reinterpret_cast<uintptr_t>(m) % 16 == 0 && ld * elem % 16 == 0; };
+  q.g = g;
+  q.tiles = (g.I + kTile - 1) / kTile;
+  q.vec_dy = on16(g.dy, g.lddy), q.vec_z = on16(g.pre, g.ldpre), q.vec_x = on16(g.x, g.ldx);
+  q.store_tma = g.dx && on16(g.dx, g.lddx) && g.lddx * elem < (1LL << 40);
+  q.parts = static_cast<float*>(ws);
+  q.status = status;
+  q.spin_limit = spin_limit;
+  CUtensorMap map{};
+  if (q.store_tma && !encode(&map, g.dx, g.I, g.K, g.lddx, 32, dtype)) return PIC_ERR_CUDA;
+  const bool wide = g.N > 64 || g.K > 64;
+  if (dtype == PIC_DTYPE_F32) return run<float, false>(g, q, map, 8, s);
+  if (dtype == PIC_DTYPE_F16) return wide ? run<__half, true>(g, q, map, 9, s) : run<__half, false>(g, q, map, 10, s);
+  return wide ? run<__nv_bfloat16, true>(g, q, map, 11, s) : run<__nv_bfloat16, false>(g, q, map, 12, s);
+}
+
+}  // namespace lin
+}  // namespace pic

@@ -183,23 +183,6 @@ PFN_cuTensorMapEncodeTiled_v12000 encoder() {
   return fn;
 }
 
-// A [rows][cols] matrix in boxes of 128 bytes of columns and box_rows rows,
-// 128-byte swizzled.
-bool encode(CUtensorMap* map, const void* m, long long rows, long long cols, long long ld, int box_rows, int dtype) {
-  const PFN_cuTensorMapEncodeTiled_v12000 enc = encoder();
-  if (!enc) return false;
-  const unsigned e = dtype == PIC_DTYPE_F32 ? 4 : 2;
-  const CUtensorMapDataType type = dtype == PIC_DTYPE_F32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
-                                   : dtype == PIC_DTYPE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
-                                                            : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-  const cuuint64_t dim[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
-  const cuuint64_t stride[1] = {static_cast<cuuint64_t>(ld * e)};
-  const cuuint32_t box[2] = {128u / e, static_cast<cuuint32_t>(box_rows)};
-  const cuuint32_t elem[2] = {1, 1};
-  return enc(map, type, 2, const_cast<void*>(m), dim, stride, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 // The three planes of a matrix, in boxes of 64 columns, box_rows rows and all planes.
 bool encode_planes(CUtensorMap* map, const void* m, long long rows, long long cols, long long ld, int box_rows) {
   const PFN_cuTensorMapEncodeTiled_v12000 enc = encoder();
@@ -228,18 +211,6 @@ int smem_of() {
   return TcShape<CG, BN>::kSmem;
 }
 
-// The kernel's shared-memory attribute, set once per device.
-int set_up(const void* fn, int slot, int smem) {
-  static std::atomic<uint64_t> done[8];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return PIC_ERR_CUDA;
-  const uint64_t bit = 1ull << (dev & 63);
-  if (done[slot].load(std::memory_order_acquire) & bit) return PIC_OK;
-  if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return PIC_ERR_CUDA;
-  done[slot].fetch_or(bit, std::memory_order_release);
-  return PIC_OK;
-}
-
 template <typename T>
 int join(const JoinParams& q, cudaStream_t s) {
   const unsigned blocks = static_cast<unsigned>(q.tiles_i * q.tiles_j * q.rows * q.bn / 4 / 32);
@@ -251,6 +222,32 @@ int join(const JoinParams& q, cudaStream_t s) {
 }
 
 }  // namespace
+
+bool encode(CUtensorMap* map, const void* m, long long rows, long long cols, long long ld, int box_rows, int dtype) {
+  const PFN_cuTensorMapEncodeTiled_v12000 enc = encoder();
+  if (!enc) return false;
+  const unsigned e = dtype == PIC_DTYPE_F32 ? 4 : 2;
+  const CUtensorMapDataType type = dtype == PIC_DTYPE_F32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : dtype == PIC_DTYPE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                            : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  const cuuint64_t dim[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t stride[1] = {static_cast<cuuint64_t>(ld * e)};
+  const cuuint32_t box[2] = {128u / e, static_cast<cuuint32_t>(box_rows)};
+  const cuuint32_t elem[2] = {1, 1};
+  return enc(map, type, 2, const_cast<void*>(m), dim, stride, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int allow_smem(const void* fn, int slot, int smem) {
+  static std::atomic<uint64_t> done[kSmemSlots];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return PIC_ERR_CUDA;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (done[slot].load(std::memory_order_acquire) & bit) return PIC_OK;
+  if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return PIC_ERR_CUDA;
+  done[slot].fetch_or(bit, std::memory_order_release);
+  return PIC_OK;
+}
 
 long long tc_workspace(const Product& p, int dtype) {
   const Plan r = plan(p, dtype);
@@ -323,7 +320,7 @@ int tc_product(const Product& p, int dtype, void* ws, int* status, unsigned spin
     slot = shape + (dtype == PIC_DTYPE_BF16 ? 3 : 0);
     smem = shape == 2 ? smem_of<2, 256>() : shape == 1 ? smem_of<1, 128>() : smem_of<1, 64>();
   }
-  if (set_up(fn, slot, smem) != PIC_OK) return PIC_ERR_CUDA;
+  if (allow_smem(fn, slot, smem) != PIC_OK) return PIC_ERR_CUDA;
   long long grid = q.work * r.cg;
   const long long most = r.bn == 64 ? 2 * kSms : kSms;
   if (grid > most && !r.join) grid = most;  // joined: one tile a cluster

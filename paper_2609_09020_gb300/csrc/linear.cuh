@@ -136,6 +136,28 @@ struct GradAct {
 };
 long long grad_act_blocks(const GradAct& g, int dtype);  // rows of parts (parts itself may be null still)
 int grad_act(const GradAct& g, int dtype, cudaStream_t s);
+// The whole gradient of a narrow layer over many rows, in one pass.
+struct NarrowGrad {
+  const void* dy;
+  long long lddy;
+  const void* pre;
+  long long ldpre;
+  const void* x;
+  long long ldx;
+  const void* w;
+  long long ldw;
+  void* dx;  // null: not asked for, as for dw and db
+  long long lddx;
+  void* dw;
+  long long lddw;
+  void* db;
+  long long I;
+  int N, K, act;
+};
+bool narrow_takes(const NarrowGrad& g, int dtype);
+long long narrow_workspace(const NarrowGrad& g);
+int narrow_grad(const NarrowGrad& g, int dtype, void* ws, int* status, unsigned spin_limit, cudaStream_t s);
+
 // out[j] = sum_b parts[b][j], b ascending within a fixed tree.
 int sum_parts(const float* parts, long long blocks, long long J, void* out, int dtype, cudaStream_t s);
 

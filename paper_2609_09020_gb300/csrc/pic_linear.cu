@@ -148,6 +148,16 @@ int backward(const pic_linear_grad_args& a, Arena& ws, bool launch, cudaStream_t
     if (a.db && rc == PIC_OK) rc = zero_rows(a.db, N, 1, N, a.dtype, s);
     return rc;
   }
+  if (N <= 128 && K <= 128) {
+    const pic::lin::NarrowGrad g{a.dy, a.lddy, a.pre, a.ldpre, a.x, a.ldx, a.w, a.ldw, a.dx, a.lddx,
+                                 a.dw, a.lddw, a.db, M, static_cast<int>(N), static_cast<int>(K), a.act};
+    if (pic::lin::narrow_takes(g, a.dtype)) {
+      void* w = ws.take(pic::lin::narrow_workspace(g));
+      int* status = launch ? status_word() : nullptr;
+      if (!launch) return PIC_OK;
+      return status ? pic::lin::narrow_grad(g, a.dtype, w, status, pic::kWaitPolls, s) : PIC_ERR_CUDA;
+    }
+  }
   // dz: dy itself where there is no activation
   const bool products = a.dx || a.dw;
   const void* dz = a.dy;

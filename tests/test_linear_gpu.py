@@ -144,6 +144,63 @@ def test_few_rows(size, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("act", ["none", "relu", "gelu"])
+@pytest.mark.parametrize("size", [(1024, 3, 3), (1030, 128, 128), (2049, 65, 128), (3000, 100, 65), (1300, 64, 17),
+                                  (1024, 1, 64), (30011, 64, 64), (25000, 7, 40), (40000, 128, 96)], ids=str)
+def test_narrow_gradient(size, act, dtype):
+    """Layers of synthesis nets over many rows: all of the gradient, and each part
+    by itself; contiguous, and with NaN between the rows."""
+    from paper_2609_09020_gb300 import pic
+    M, K, N = size
+    for pad, shift in ((0, 0), (3, 1), (8, 8)):
+        x, w = wide(M, K, dtype, 1, pad, shift), wide(N, K, dtype, 2, pad, shift, 1.4 / math.sqrt(K))
+        dy, z = wide(M, N, dtype, 5, pad, shift, 0.1), wide(M, N, dtype, 6, pad, shift, 1.4)
+        want = ref.backward(dy, x, w, z, act)
+        got = pic.linear_backward(dy, x, w, act=act, pre=z)
+        for g, v, name in zip(got, want, ("dx", "dw", "db")):
+            ref.check(g, v, name)
+        if pad == 0:
+            again = pic.linear_backward(dy, x, w, act=act, pre=z)
+            assert all(torch.equal(a, b) for a, b in zip(got, again))
+            for need in (("x",), ("weight",), ("x", "bias"), ("weight", "bias")):
+                some = pic.linear_backward(dy, x, w, act=act, pre=z, need=need)
+                for i, name in enumerate(("x", "weight", "bias")):
+                    assert (some[i] is not None) == (name in need)
+                    if name in need:
+                        ref.check(some[i], want[i], name)
+    pic.linear_check()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_narrow_infinities(dtype):
+    """Infinite and NaN values reach what depends on them, as in IEEE arithmetic,
+    and nothing else."""
+    from paper_2609_09020_gb300 import pic
+    M, K, N = 5000, 24, 40
+    x, w = normal((M, K), dtype, 1), normal((N, K), dtype, 2, 0.2)
+    dy, z = normal((M, N), dtype, 5, 0.1), normal((M, N), dtype, 6, 1.4)
+    clean = ref.backward(dy, x, w, z, "gelu")
+    dy[1700, 11], dy[1701, 12], x[4000, 5] = math.inf, math.nan, -math.inf
+    dx, dw, db = pic.linear_backward(dy, x, w, act="gelu", pre=z)
+    keep = torch.ones(M, dtype=torch.bool, device="cuda")
+    keep[1700] = keep[1701] = False
+    ref.check(dx[keep], (clean[0][0][keep], clean[0][1][keep]), "dx")
+    d = ref.act_grad64(z[1700, 11].double(), "gelu")
+    assert torch.equal(dx[1700], (torch.sign(d * w[11].double()) * math.inf).to(dtype))
+    assert bool(dx[1701].isnan().all())
+    rows = [n for n in range(N) if n not in (11, 12)]
+    cols = [k for k in range(K) if k != 5]
+    ref.check(dw[rows][:, cols], (clean[1][0][rows][:, cols], clean[1][1][rows][:, cols]), "dw")
+    assert bool(dw[rows][:, 5].isinf().all()) and bool(dw[12].isnan().all()) and bool(dw[11][cols].isinf().all())
+    ref.check(db[rows], (clean[2][0][rows], clean[2][1][rows]), "db")
+    assert bool(db[11].isinf()) and bool(db[12].isnan())
+    # a weight: every row of dx, nothing of dw
+    w[3, 9] = math.inf
+    dx, dw, _ = pic.linear_backward(normal((M, N), dtype, 5, 0.1), normal((M, K), dtype, 1), w, act="none")
+    assert bool(dx[:, 9].isinf().all()) and int((~dx.isfinite()).any(0).sum()) == 1 and bool(dw.isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 def test_no_rows(dtype):
     from paper_2609_09020_gb300 import pic
     x, w, b = normal((0, 24), dtype, 1), normal((8, 24), dtype, 2), normal((8,), dtype, 3)
