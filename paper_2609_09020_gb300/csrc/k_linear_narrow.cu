@@ -16,9 +16,12 @@
 // registers after every tile).
 //
 // Roles of the 16 warps: 0..3 dx out of tensor memory, 4 and 5 (fp32) take dw
-// over, 6 issues the MMAs, 8..15 load: 4 x 16 bytes of dy, z and x per thread at a
-// time, x of this tile under way while dz is computed, dy and z of the next while
-// x is written to shared memory.
+// over, 6 issues the MMAs, 8..15 make dz and db.  Rows of 16-bit values on 16-byte
+// boundaries, up to 64 of them, come by TMA (warp 7) into a ring of three tiles of
+// dy, z and x, 48 KB each; x is an operand as it lands, and dz takes the place of
+// dy.  Else warps 8..15 load 4 x 16 bytes of dy, z and x per thread at a time, x of
+// this tile under way while dz is computed, dy and z of the next while x is written
+// to shared memory: any stride and alignment, but less in flight.
 //
 // An infinite or NaN value among fp32 pieces would spread (inf 0 = NaN): its tile
 // is marked, and dx and dw of that tile are computed again on the FP32 cores.
@@ -31,7 +34,7 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kLoadWarp = 8, kLoaders = 256;
-constexpr int kMmaWarp = 6;
+constexpr int kMmaWarp = 6, kTmaWarp = 7;
 constexpr int kTile = 128;
 constexpr int kMarks = 8;  // more tiles than the loaders can be ahead of the others
 constexpr int kSms = 152;
@@ -45,8 +48,8 @@ struct NarrowParams {
   unsigned spin_limit;
 };
 
-// T: element; WIDE: up to 128 columns (16-bit types), else 64.
-template <typename T, bool WIDE>
+// T: element; WIDE: up to 128 columns (16-bit types), else 64; TMA: dy, z and x come by TMA.
+template <typename T, bool WIDE, bool TMA>
 struct Shape {
   static constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
   static constexpr int kPer = 16 / sizeof(T);          // elements of a load
@@ -56,17 +59,18 @@ struct Shape {
   static constexpr int kPassRows = kLoaders / kVecs;   // rows that the loaders cover at once
   static constexpr int kUnitRows = 4 * kPassRows;      // rows of a unit: four loads of each matrix per thread
   static constexpr int kUnits = kTile / kUnitRows;
+  static_assert(kUnits * kUnitRows == kTile, "whole units");
   static constexpr int kBlockBytes = kTile * 128;
   static constexpr int kPlaneBytes = kBlocks * kBlockBytes;
-  static constexpr int kStageBytes = 2 * kPlanes * kPlaneBytes;  // dz, x
-  static constexpr int kStages = sizeof(T) == 4 ? 1 : WIDE ? 2 : 4;
+  static constexpr int kStageBytes = (TMA ? 3 : 2 * kPlanes) * kPlaneBytes;  // dz, x (and z)
+  static constexpr int kStages = sizeof(T) == 4 ? 1 : WIDE ? 2 : TMA ? 3 : 4;
   static constexpr int kWBlock = kCols * 128, kWPlane = kBlocks * kWBlock;
   static constexpr int kOffW = kStages * kStageBytes;
   static constexpr int kOffPanels = kOffW + kPlanes * kWPlane;
   static constexpr int kOffSums = kOffPanels + 4 * 2 * kPanelBytes;
   static constexpr int kOffBars = kOffSums + kLoaders * kPer * 4;
-  // full, empty; dx ready, free; dw ready, free; drain
-  static constexpr int kBars = 2 * kStages + 4 + 4 + 1;
+  // full, empty, landed; dx ready, free; dw ready, free; drain
+  static constexpr int kBars = 3 * kStages + 4 + 4 + 1;
   static constexpr int kOffMarks = kOffBars + kBars * 8 + 8;
   static constexpr int kSmem = kOffMarks + (kMarks + 1) * 4 + 8 + 1024;
   static constexpr int kTmemDw = 2 * kCols;  // columns: two buffers of dx, then dw (fp32: two)
@@ -153,10 +157,14 @@ __device__ __noinline__ void dw_again(float* v, const NarrowGrad& g, long long i
   }
 }
 
-template <typename T, bool WIDE>
+struct NarrowMaps {
+  CUtensorMap dx, dy, z, x;
+};
+
+template <typename T, bool WIDE, bool TMA>
 __global__ void __launch_bounds__(kThreads, 1)
-    narrow_kernel(const __grid_constant__ NarrowParams q, const __grid_constant__ CUtensorMap dx_map) {
-  using S = Shape<T, WIDE>;
+    narrow_kernel(const __grid_constant__ NarrowParams q, const __grid_constant__ NarrowMaps maps) {
+  using S = Shape<T, WIDE, TMA>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = tc::smem_addr(smem_raw);
   uint8_t* smem = smem_raw + ((1024 - (raw & 1023)) & 1023);
@@ -164,7 +172,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const NarrowGrad& g = q.g;
   const uint32_t bars = base + S::kOffBars;
-  const uint32_t bar_full = bars, bar_empty = bars + 8 * S::kStages, bar_dx = bar_empty + 8 * S::kStages,
+  const uint32_t bar_full = bars, bar_empty = bars + 8 * S::kStages, bar_landed = bar_empty + 8 * S::kStages,
+                 bar_dx = bar_landed + 8 * S::kStages,
                  bar_dx_free = bar_dx + 16, bar_dw = bar_dx_free + 16, bar_dw_free = bar_dw + 16, bar_drain = bar_dw_free + 16;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + S::kOffBars + 8 * S::kBars);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::kOffBars + 8 * S::kBars + 4);
@@ -176,6 +185,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int s = 0; s < S::kStages; ++s) {
       tc::mbar_init(bar_full + 8 * s, kLoaders / 32);
       tc::mbar_init(bar_empty + 8 * s, 1);
+      tc::mbar_init(bar_landed + 8 * s, 1);
     }
     for (int b = 0; b < 2; ++b) {
       tc::mbar_init(bar_dx + 8 * b, 1);
@@ -230,6 +240,44 @@ __global__ void __launch_bounds__(kThreads, 1)
     float sum[S::kPer] = {};
     int s = 0, count = 0;
     uint32_t phase = 0;
+    if constexpr (TMA) {
+      for (long long tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
+        if (!__all_sync(0xffffffffu, wait(bar_landed + 8 * s, phase))) break;
+        const uint32_t sdz = base + s * S::kStageBytes, sz = sdz + 2 * S::kPlaneBytes;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int r = row + u * S::kPassRows;
+          const uint32_t at = r * 128 + (((col >> 3) ^ (r & 7)) << 4);
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                       : "=r"(vy[u].w[0]), "=r"(vy[u].w[1]), "=r"(vy[u].w[2]), "=r"(vy[u].w[3])
+                       : "r"(sdz + at));
+          if (has_act)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(vz[u].w[0]), "=r"(vz[u].w[1]), "=r"(vz[u].w[2]), "=r"(vz[u].w[3])
+                         : "r"(sz + at));
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          float d[S::kPer], v[S::kPer];
+          vy[u].widen(d);
+          if (has_act) {
+            vz[u].widen(v);
+#pragma unroll
+            for (int e = 0; e < S::kPer; ++e) d[e] = act_grad<false>(d[e], v[e], g.act);
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = pack2_16<T>(d[2 * i], d[2 * i + 1]);
+            put_vec<T>(sdz, S::kBlockBytes, S::kPlaneBytes, row + u * S::kPassRows, col, w);
+          }
+#pragma unroll
+          for (int e = 0; e < S::kPer; ++e) sum[e] += d[e];
+        }
+        tc::fence_async_smem();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(bar_full + 8 * s);
+        if (++s == S::kStages) s = 0, phase ^= 1;
+      }
+    } else {
     if (blockIdx.x < q.tiles) load_dz(blockIdx.x * static_cast<long long>(kTile));
     for (long long tile = blockIdx.x; tile < q.tiles; tile += gridDim.x, ++count) {
       uint32_t largest = 0;
@@ -289,6 +337,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0) tc::mbar_arrive(bar_full + 8 * s);
       if (++s == S::kStages) s = 0, phase ^= 1;
     }
+    }
     // db: the threads of a column
     __syncwarp();
     if (g.db) {
@@ -312,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t phase = 0, free_phase = 0;
       bool ok = true, first = true;
       for (long long tile = blockIdx.x; tile < q.tiles && ok; tile += gridDim.x) {
-        if (!(ok = wait(bar_full + 8 * s, phase))) break;
+        if (!(ok = wait(bar_full + 8 * s, phase) && (!TMA || wait(bar_landed + 8 * s, phase)))) break;
         tc::tc_fence_after();
         const uint32_t sdz = base + s * S::kStageBytes, sx = sdz + S::kPlanes * S::kPlaneBytes, sw = base + S::kOffW;
         constexpr int kProducts = S::kPlanes == 3 ? 6 : 1;
@@ -361,6 +410,31 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
     __syncwarp();
+  } else if (TMA && warp == kTmaWarp) {
+    if (tc::elect_one()) {
+      const bool has_z = g.act != PIC_ACT_NONE;
+      const uint32_t bytes = S::kPlaneBytes * (1 + (g.dw ? 1 : 0) + (has_z ? 1 : 0));
+      int s = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (long long tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
+        if (!(ok = wait(bar_empty + 8 * s, phase ^ 1))) break;
+        const uint32_t at = base + s * S::kStageBytes, bar = bar_landed + 8 * s;
+        const int i = static_cast<int>(tile * kTile);
+        tc::mbar_arrive_expect_tx(bar, bytes);
+        tc::tma_load_2d<false>(at, &maps.dy, 0, i, bar);
+        if (has_z) tc::tma_load_2d<false>(at + 2 * S::kPlaneBytes, &maps.z, 0, i, bar);
+        if (g.dw) tc::tma_load_2d<false>(at + S::kPlaneBytes, &maps.x, 0, i, bar);
+        if (++s == S::kStages) s = 0, phase ^= 1;
+      }
+      if (!ok)  // aborted: the copies in flight land before shared memory goes away
+        for (int i = 0; i < S::kStages; ++i) {
+          if (--s < 0) s = S::kStages - 1, phase ^= 1;
+          for (uint32_t n = 0; n < q.spin_limit && !tc::mbar_try_wait(bar_landed + 8 * s, phase); ++n) {
+          }
+        }
+    }
+    __syncwarp();
   } else if (warp < 4) {
     const uint32_t panels = base + S::kOffPanels + warp * 2 * kPanelBytes;
     const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
@@ -406,7 +480,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           if (lane == 0) tc::bulk_wait_read<1>();
           __syncwarp();
-          put_panel<T>(out, panels + pb * kPanelBytes, lane, row0, 64 * b + 32 * h, p, g.dx, g.lddx, &dx_map, q.store_tma);
+          put_panel<T>(out, panels + pb * kPanelBytes, lane, row0, 64 * b + 32 * h, p, g.dx, g.lddx, &maps.dx, q.store_tma);
           pb ^= 1;
         }
       }
@@ -498,13 +572,13 @@ int ctas(const NarrowGrad& g) {
   return static_cast<int>(tiles < kSms ? tiles : kSms);
 }
 
-template <typename T, bool WIDE>
-int run(const NarrowGrad& g, NarrowParams& q, const CUtensorMap& map, int slot, cudaStream_t s) {
-  const void* fn = reinterpret_cast<const void*>(narrow_kernel<T, WIDE>);
-  const int smem = Shape<T, WIDE>::kSmem, grid = ctas(g);
-  static_assert(Shape<T, WIDE>::kSmem <= 227 * 1024, "shared memory of an SM");
+template <typename T, bool WIDE, bool TMA>
+int run(const NarrowGrad& g, NarrowParams& q, NarrowMaps& maps, int slot, cudaStream_t s) {
+  const void* fn = reinterpret_cast<const void*>(narrow_kernel<T, WIDE, TMA>);
+  const int smem = Shape<T, WIDE, TMA>::kSmem, grid = ctas(g);
+  static_assert(Shape<T, WIDE, TMA>::kSmem <= 227 * 1024, "shared memory of an SM");
   if (allow_smem(fn, slot, smem) != PIC_OK) return PIC_ERR_CUDA;
-  void* args[] = {&q, const_cast<CUtensorMap*>(&map)};
+  void* args[] = {&q, &maps};
   if (cudaLaunchKernel(fn, dim3(grid), dim3(kThreads), args, smem, s) != cudaSuccess) return PIC_ERR_CUDA;
   if (g.dw || g.db) {
     const int per = g.N * g.K + g.N;
@@ -529,16 +603,28 @@ int narrow_grad(const NarrowGrad& g, int dtype, void* ws, int* status, unsigned 
   q.g = g;
   q.tiles = (g.I + kTile - 1) / kTile;
   q.vec_dy = on16(g.dy, g.lddy), q.vec_z = on16(g.pre, g.ldpre), q.vec_x = on16(g.x, g.ldx);
-  q.store_tma = g.dx && on16(g.dx, g.lddx) && g.lddx * elem < (1LL << 40);
+  q.store_tma = g.dx && g.K * elem % 16 == 0 && on16(g.dx, g.lddx) && g.lddx * elem < (1LL << 40);
   q.parts = static_cast<float*>(ws);
   q.status = status;
   q.spin_limit = spin_limit;
-  CUtensorMap map{};
-  if (q.store_tma && !encode(&map, g.dx, g.I, g.K, g.lddx, 32, dtype)) return PIC_ERR_CUDA;
-  const bool wide = g.N > 64 || g.K > 64;
-  if (dtype == PIC_DTYPE_F32) return run<float, false>(g, q, map, 8, s);
-  if (dtype == PIC_DTYPE_F16) return wide ? run<__half, true>(g, q, map, 9, s) : run<__half, false>(g, q, map, 10, s);
-  return wide ? run<__nv_bfloat16, true>(g, q, map, 11, s) : run<__nv_bfloat16, false>(g, q, map, 12, s);
+  NarrowMaps maps{};
+  const auto far = [&](long long ld) { return ld * elem >= (1LL << 40); };
+  if (q.store_tma && !encode(&maps.dx, g.dx, g.I, g.K, g.lddx, 32, dtype)) return PIC_ERR_CUDA;
+  const bool wide = g.N > 64 || g.K > 64, has_z = g.act != PIC_ACT_NONE;
+  const bool tma = dtype != PIC_DTYPE_F32 && !wide && q.vec_dy && !far(g.lddy) && (!has_z || (q.vec_z && !far(g.ldpre))) &&
+                   (!g.dw || (q.vec_x && !far(g.ldx)));
+  if (tma && !(encode(&maps.dy, g.dy, g.I, g.N, g.lddy, kTile, dtype) &&
+               (!has_z || encode(&maps.z, g.pre, g.I, g.N, g.ldpre, kTile, dtype)) &&
+               (!g.dw || encode(&maps.x, g.x, g.I, g.K, g.ldx, kTile, dtype))))
+    return PIC_ERR_CUDA;
+  if (dtype == PIC_DTYPE_F32) return run<float, false, false>(g, q, maps, 8, s);
+  if (dtype == PIC_DTYPE_F16)
+    return wide  ? run<__half, true, false>(g, q, maps, 9, s)
+           : tma ? run<__half, false, true>(g, q, maps, 10, s)
+                 : run<__half, false, false>(g, q, maps, 11, s);
+  return wide  ? run<__nv_bfloat16, true, false>(g, q, maps, 12, s)
+         : tma ? run<__nv_bfloat16, false, true>(g, q, maps, 13, s)
+               : run<__nv_bfloat16, false, false>(g, q, maps, 14, s);
 }
 
 }  // namespace lin

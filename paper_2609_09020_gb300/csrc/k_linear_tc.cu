@@ -277,7 +277,9 @@ int tc_product(const Product& p, int dtype, void* ws, int* status, unsigned spin
   const auto fits = [&](const void* m, long long ld, long long rows) {
     return reinterpret_cast<uintptr_t>(m) % 16 == 0 && ((ld * elem % 16 == 0 && ld * elem < (1LL << 40)) || rows == 1);
   };
-  q.store_tma = !q.parts && fits(p.y, p.ldy, p.I) && (!p.pre || fits(p.pre, p.ldpre, p.I));
+  // a TMA store ends on a 16-byte boundary of the row: columns that do not would
+  // have their neighbours overwritten
+  q.store_tma = !q.parts && p.J * elem % 16 == 0 && fits(p.y, p.ldy, p.I) && (!p.pre || fits(p.pre, p.ldpre, p.I));
   const auto out_ld = [&](long long ld) { return p.I == 1 ? (p.J + 7) / 8 * 8 : ld; };
   bool ok = true;
   if (r.reg) {

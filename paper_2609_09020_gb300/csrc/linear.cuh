@@ -53,27 +53,20 @@ __device__ __forceinline__ float act_value(float z, int act) {
 }
 
 // dy act'(z): a derivative of zero gives zero whatever dy is; act' is NaN for
-// NaN.  EXACT: with erfcf and expf (fp32); else the polynomial form, off by at
-// most 5e-7, far below the rounding of dz to 16 bits, and half its cost.
+// NaN.  EXACT (fp32): off by the roundings of the evaluation, about 1e-7; else by
+// at most 5e-7, far below the rounding of dz to 16 bits.
 template <bool EXACT>
 __device__ __forceinline__ float act_grad(float dy, float z, int act) {
   if (act == PIC_ACT_NONE) return dy;
   if (act == PIC_ACT_RELU) return z > 0.0f ? dy : 0.0f;
-  float d;
-  if constexpr (EXACT) {
-    // the clamp keeps z phi(z) from being infinity times zero (phi(20) is below fp32's range)
-    const float c = fminf(fmaxf(z, -20.0f), 20.0f);
-    const float phi = 0.39894228040143268f * expf(-0.5f * c * c);
-    d = fmaf(c, phi, 0.5f * erfcf(-0.70710678118654752f * z));
-  } else {
-    float a;
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(fabsf(z)), "f"(kGeluGradA));
-    float p = gelu_grad_c(0);
+  float a;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(fabsf(z)), "f"(kGeluGradA));
+  float p = EXACT ? gelu_grad_c32(0) : gelu_grad_c(0);
 #pragma unroll
-    for (int i = 1; i <= kGeluGradDeg; ++i) p = fmaf(p, a, gelu_grad_c(i));
-    const float t = a >= kGeluGradA ? 0.0f : p * ex2_approx(a * a * kGeluGradPower);
-    d = z < 0.0f ? t : 1.0f - t;
-  }
+  for (int i = 1; i <= (EXACT ? kGeluGradDeg32 : kGeluGradDeg); ++i)
+    p = fmaf(p, a, EXACT ? gelu_grad_c32(i) : gelu_grad_c(i));
+  const float t = a >= kGeluGradA ? 0.0f : p * ex2_approx(a * a * kGeluGradPower);
+  const float d = z < 0.0f ? t : 1.0f - t;
   return d == 0.0f ? 0.0f : dy * d;
 }
 
@@ -96,12 +89,12 @@ struct Product {
   int act;
 };
 
-// Parts of the sum over K that one product is cut into (1: none), each a
-// multiple of `step`, so that about `target` blocks have work.
+// Parts of the sum over K that one product is cut into (1: none), each at least
+// `step`, so that about `target` blocks have work.
 inline int split_count(long long tiles, long long K, long long step, long long target) {
   if (tiles >= target) return 1;
   long long s = target / tiles;
-  const long long most = (K + step - 1) / step;
+  const long long most = K / step;
   if (s > most) s = most;
   return s < 1 ? 1 : static_cast<int>(s);
 }

@@ -1,6 +1,6 @@
 // Generated by paper_2609_09020_gb300/gen_gelu_grad.py -- do not edit.
 // Phi(-a) - a phi(a) ~= 2^(kGeluGradPower a^2) p(a) on 0 <= a <= 6; max error of GELU' in
-// fp32 ~ 3.6e-07.
+// fp32 ~ 3.6e-07 (degree 9), 1.2e-07 (degree 11).
 #pragma once
 
 namespace pic {
@@ -8,6 +8,7 @@ namespace pic {
 constexpr float kGeluGradA = 6.0f;
 constexpr float kGeluGradPower = -0.7213475108146667f;
 constexpr int kGeluGradDeg = 9;
+constexpr int kGeluGradDeg32 = 11;
 
 // Coefficients of p, highest degree first (Horner order).
 __host__ __device__ constexpr float gelu_grad_c(int i) {
@@ -22,6 +23,23 @@ __host__ __device__ constexpr float gelu_grad_c(int i) {
       0.24975229799747467f,
       -0.7978649139404297f,
       0.4999997317790985f,
+  };
+  return c[i];
+}
+__host__ __device__ constexpr float gelu_grad_c32(int i) {
+  constexpr float c[] = {
+      -3.155438150770351e-07f,
+      7.70879523770418e-06f,
+      -8.477114170091227e-05f,
+      0.0005636534770019352f,
+      -0.0025900928303599358f,
+      0.009003852494060993f,
+      -0.025471823289990425f,
+      0.06192393600940704f,
+      -0.13280579447746277f,
+      0.24997256696224213f,
+      -0.7978828549385071f,
+      0.4999999701976776f,
   };
   return c[i];
 }

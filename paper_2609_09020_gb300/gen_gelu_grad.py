@@ -7,10 +7,12 @@ GELU'(z) = Phi(z) + z phi(z).  With a = |z| and t(a) = Phi(-a) - a phi(a),
     t(a) = 2^(-a^2 log2(e) / 2) p(a),   p(a) = phi(0) (M(a) - a),
 
 M(a) = Phi(-a) / phi(a) Mills' ratio, which is smooth: p is fitted by a
-polynomial of degree 9 on 0 <= a <= A, A = 6, with the power as its weight
-(beyond A, |t| < 4e-8 is taken as 0).  Lawson's reweighting turns the least-
-squares fit on Chebyshev nodes into a minimax one.  The kernels take one 2^x,
-nine multiply-adds and a few operations more, against erfc and an exponential.
+polynomial on 0 <= a <= A, A = 6, with the power as its weight (beyond A,
+|t| < 4e-8 is taken as 0), of degree 9 for gradients that are rounded to 16
+bits and of degree 11 for fp32, where the roundings of the evaluation are what
+is left.  Lawson's reweighting turns the least-squares fit on Chebyshev nodes
+into a minimax one.  The kernels take one 2^x, nine (eleven) multiply-adds and a
+few operations more, against erfc and an exponential with their branches.
 
 Run:  python -m paper_2609_09020_gb300.gen_gelu_grad  (prints the header)
 """
@@ -22,16 +24,17 @@ from scipy.special import erfcx, ndtr
 
 A = 6.0
 DEG = 9
+DEG_FP32 = 11
 PASSES = 200
 HALF_LOG2E = -0.5 / np.log(2.0)
 
 
-def fit():
+def fit(deg=DEG):
     """Coefficients of p, lowest degree first."""
     a = 0.5 * A * (1 - np.cos(np.linspace(0, np.pi, 4001)))
     w = np.exp(-0.5 * a * a)
     f = (np.sqrt(np.pi / 2) * erfcx(a / np.sqrt(2)) - a) / np.sqrt(2 * np.pi)
-    v = chebyshev.chebvander(2 * a / A - 1, DEG)
+    v = chebyshev.chebvander(2 * a / A - 1, deg)
     lw = np.ones_like(a)
     for _ in range(PASSES):
         wt = w * np.sqrt(lw)
@@ -65,20 +68,21 @@ def max_error(c) -> float:
     return float(np.max(np.abs(grad_fp32(z, c).astype(np.float64) - ref)))
 
 
-def header(c) -> str:
+def header(c, c32) -> str:
     lines = ["// Generated by paper_2609_09020_gb300/gen_gelu_grad.py -- do not edit.",
              f"// Phi(-a) - a phi(a) ~= 2^(kGeluGradPower a^2) p(a) on 0 <= a <= {A:g}; max error of GELU' in",
-             f"// fp32 ~ {max_error(c):.1e}.",
+             f"// fp32 ~ {max_error(c):.1e} (degree {DEG}), {max_error(c32):.1e} (degree {DEG_FP32}).",
              "#pragma once", "", "namespace pic {", "",
              f"constexpr float kGeluGradA = {float(np.float32(A))!r}f;",
              f"constexpr float kGeluGradPower = {float(np.float32(HALF_LOG2E))!r}f;",
-             f"constexpr int kGeluGradDeg = {DEG};", "",
-             "// Coefficients of p, highest degree first (Horner order).",
-             "__host__ __device__ constexpr float gelu_grad_c(int i) {", "  constexpr float c[] = {"]
-    lines += [f"      {float(np.float32(k))!r}f," for k in c[::-1]]
-    lines += ["  };", "  return c[i];", "}", "", "}  // namespace pic", ""]
-    return "\n".join(lines)
+             f"constexpr int kGeluGradDeg = {DEG};", f"constexpr int kGeluGradDeg32 = {DEG_FP32};", "",
+             "// Coefficients of p, highest degree first (Horner order)."]
+    for name, k in (("gelu_grad_c", c), ("gelu_grad_c32", c32)):
+        lines += [f"__host__ __device__ constexpr float {name}(int i) {{", "  constexpr float c[] = {"]
+        lines += [f"      {float(np.float32(v))!r}f," for v in k[::-1]]
+        lines += ["  };", "  return c[i];", "}"]
+    return "\n".join(lines + ["", "}  // namespace pic", ""])
 
 
 if __name__ == "__main__":
-    print(header(fit()), end="")
+    print(header(fit(), fit(DEG_FP32)), end="")

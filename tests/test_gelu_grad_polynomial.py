@@ -10,8 +10,9 @@ from paper_2609_09020_gb300 import gen_gelu_grad as gen
 HEADER = os.path.join(os.path.dirname(os.path.abspath(gen.__file__)), "csrc", "pic_gelu_grad.cuh")
 
 
-def coefficients():
+def coefficients(name="gelu_grad_c"):
     text = open(HEADER).read()
+    text = text[text.index(name + "(int"):]
     body = text[text.index("c[] = {"):text.index("return c[i]")]
     return np.array([float(v) for v in re.findall(r"(-?[\d.]+(?:e-?\d+)?)f", body)][::-1])
 
@@ -27,3 +28,10 @@ def test_error():
     assert np.all(gen.grad_fp32(np.array([6.0, 10.0, 1e30, np.inf]), c) == 1)
     assert np.all(gen.grad_fp32(np.array([-6.0, -10.0, -1e30, -np.inf]), c) == 0)
     assert abs(float(gen.grad_fp32(np.array([0.0]), c)[0]) - 0.5) < 5e-7
+
+
+def test_fp32_polynomial():
+    c = coefficients("gelu_grad_c32")
+    assert len(c) == gen.DEG_FP32 + 1 and len(coefficients()) == gen.DEG + 1
+    assert gen.max_error(c) < 1.5e-7
+    assert np.all(gen.grad_fp32(np.array([6.0, np.inf]), c) == 1) and np.all(gen.grad_fp32(np.array([-6.0, -np.inf]), c) == 0)

@@ -103,6 +103,32 @@ def test_strides(size, pad, shift, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("size", [(40, 65, 61), (300, 1001, 515), (1, 301, 69), (700, 259, 1501), (2000, 61, 35), (1500, 5, 1),
+                                  (1100, 70, 121)], ids=str)
+def test_rows_that_end_inside_16_bytes(size, dtype):
+    """Rows that start on 16-byte boundaries, but whose width is no multiple of 16
+    bytes: the NaN behind the last column stays out, and nothing is written there."""
+    from paper_2609_09020_gb300 import pic
+    M, K, N = size
+
+    def padded(rows, cols, seed, std=1.0):
+        return wide(rows, cols, dtype, seed, -cols % 8 + 8, 0, std)
+
+    x, w, r = padded(M, K, 1), padded(N, K, 2, 1.4 / math.sqrt(K)), padded(M, N, 3)
+    buf = torch.full((M + 1, (N + 7) // 8 * 8), 7.0, dtype=dtype, device="cuda")
+    for act, res in (("none", None), ("gelu", r)):
+        y = pic.linear(x, w, act=act, residual=res, out=buf[:M, :N])
+        ref.check(y, ref.forward(x, w, None, act, res)[0], "y")
+        assert bool((buf[:, N:] == 7).all()) and bool((buf[M] == 7).all())
+    dy, z = padded(M, N, 5, 0.1), padded(M, N, 6, 1.4)
+    for act in ("none", "gelu"):
+        got = pic.linear_backward(dy, x, w, act=act, pre=z)
+        for g, v, name in zip(got, ref.backward(dy, x, w, z, act), ("dx", "dw", "db")):
+            ref.check(g, v, name)
+    pic.linear_check()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 @pytest.mark.parametrize("size", [(20000, 64, 64), (9000, 40, 3), (70001, 8, 16), (4096, 512, 384),
                                   (600, 4096, 200), (1500, 1536, 1600), (2500, 328, 2600), (520, 2500, 2600),
                                   (2305, 2304, 2311)], ids=str)
