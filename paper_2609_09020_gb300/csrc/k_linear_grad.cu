@@ -14,6 +14,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kUnroll = 4;
 constexpr int kBlocks = 1216;  // 8 per SM
+constexpr int kOneBlockRows = 128;  // up to here a block takes all rows, and db needs no second kernel
 
 // How a [I][J] matrix is shared out: tx threads across columns, blocks of `run` rows.
 struct Share {
@@ -36,6 +37,7 @@ Share share(const GradAct& g, int elem) {
   const int ty = kThreads / s.tx;
   long long want = (kBlocks + s.col_blocks - 1) / s.col_blocks;
   if (want > 304) want = 304;  // more sums per column than that take longer to add than they save
+  if (g.I <= kOneBlockRows) want = 1;
   const long long least = static_cast<long long>(ty) * kUnroll;
   s.run = (g.I + want - 1) / want;
   s.run = (s.run + least - 1) / least * least;
@@ -100,7 +102,7 @@ __global__ void __launch_bounds__(kThreads) grad_act_kernel(const GradAct g, con
       }
     }
   }
-  if (!g.parts) return;
+  if (!g.db) return;
   const int width = s.tx * V;
 #pragma unroll
   for (int e = 0; e < V; ++e) sums[ty * width + tx * V + e] = sum[e];
@@ -110,7 +112,10 @@ __global__ void __launch_bounds__(kThreads) grad_act_kernel(const GradAct g, con
     if (col >= g.J) break;
     float t = 0.0f;
     for (int r = 0; r < rows; ++r) t += sums[r * width + c];
-    g.parts[row_block * g.J + col] = t;
+    if (s.row_blocks == 1)
+      static_cast<T*>(g.db)[col] = from_f32<T>(t);
+    else
+      g.parts[row_block * g.J + col] = t;
   }
 }
 
@@ -138,34 +143,28 @@ int run(const GradAct& g, cudaStream_t stream) {
   const Share s = share(g, sizeof(T));
   const long long blocks = s.col_blocks * s.row_blocks;
   if (blocks > 0x7fffffffLL) return PIC_ERR_INVALID_ARG;
-  const int smem = g.parts ? kThreads * s.v * 4 : 0;
+  const int smem = g.db ? kThreads * s.v * 4 : 0;
   if (s.v == 1)
     grad_act_kernel<T, 1><<<static_cast<unsigned>(blocks), kThreads, smem, stream>>>(g, s);
   else
     grad_act_kernel<T, 16 / sizeof(T)><<<static_cast<unsigned>(blocks), kThreads, smem, stream>>>(g, s);
+  if (g.db && s.row_blocks > 1)
+    sum_parts_kernel<<<static_cast<unsigned>((g.J + 15) / 16), 1024, 0, stream>>>(
+        g.parts, static_cast<int>(s.row_blocks), g.J, static_cast<T*>(g.db));
   return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
 }
 
 }  // namespace
 
-long long grad_act_blocks(const GradAct& g, int dtype) { return share(g, dtype == PIC_DTYPE_F32 ? 4 : 2).row_blocks; }
+long long grad_act_workspace(const GradAct& g, int dtype) {
+  const long long blocks = share(g, dtype == PIC_DTYPE_F32 ? 4 : 2).row_blocks;
+  return g.db && blocks > 1 ? blocks * g.J * 4 : 0;
+}
 
 int grad_act(const GradAct& g, int dtype, cudaStream_t s) {
   if (dtype == PIC_DTYPE_F32) return run<float>(g, s);
   if (dtype == PIC_DTYPE_F16) return run<__half>(g, s);
   return run<__nv_bfloat16>(g, s);
-}
-
-int sum_parts(const float* parts, long long blocks, long long J, void* out, int dtype, cudaStream_t s) {
-  const unsigned grid = static_cast<unsigned>((J + 15) / 16);
-  const int n = static_cast<int>(blocks);
-  if (dtype == PIC_DTYPE_F32)
-    sum_parts_kernel<<<grid, 1024, 0, s>>>(parts, n, J, static_cast<float*>(out));
-  else if (dtype == PIC_DTYPE_F16)
-    sum_parts_kernel<<<grid, 1024, 0, s>>>(parts, n, J, static_cast<__half*>(out));
-  else
-    sum_parts_kernel<<<grid, 1024, 0, s>>>(parts, n, J, static_cast<__nv_bfloat16*>(out));
-  return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
 }
 
 }  // namespace lin

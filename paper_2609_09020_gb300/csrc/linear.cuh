@@ -114,8 +114,8 @@ constexpr int kFewRows = 15;
 bool few_takes(const Product& p);
 int few_product(const Product& p, int dtype, cudaStream_t s);
 
-// dz[i][j] = dy act'(z), rounded (dz null: not written), and parts[b][j], the
-// column sums of the unrounded dz over the rows of block b (parts null: none).
+// dz[i][j] = dy act'(z), rounded (dz null: not written), and db[j], the sums of
+// the unrounded dz over the rows (db null: none); parts is workspace.
 struct GradAct {
   const void* dy;
   long long lddy;
@@ -123,12 +123,14 @@ struct GradAct {
   long long ldpre;
   void* dz;
   long long lddz;
+  void* db;
   float* parts;
   long long I, J;
   int act;
 };
-long long grad_act_blocks(const GradAct& g, int dtype);  // rows of parts (parts itself may be null still)
+long long grad_act_workspace(const GradAct& g, int dtype);
 int grad_act(const GradAct& g, int dtype, cudaStream_t s);
+
 // The whole gradient of a narrow layer over many rows, in one pass.
 struct NarrowGrad {
   const void* dy;
@@ -150,9 +152,6 @@ struct NarrowGrad {
 bool narrow_takes(const NarrowGrad& g, int dtype);
 long long narrow_workspace(const NarrowGrad& g);
 int narrow_grad(const NarrowGrad& g, int dtype, void* ws, int* status, unsigned spin_limit, cudaStream_t s);
-
-// out[j] = sum_b parts[b][j], b ascending within a fixed tree.
-int sum_parts(const float* parts, long long blocks, long long J, void* out, int dtype, cudaStream_t s);
 
 }  // namespace lin
 }  // namespace pic

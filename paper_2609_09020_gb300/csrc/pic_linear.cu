@@ -167,16 +167,11 @@ int backward(const pic_linear_grad_args& a, Arena& ws, bool launch, cudaStream_t
     lddz = (N + 7) / 8 * 8;  // rows of 16-bit values on 16-byte boundaries
     dz = ws.take(M * lddz * static_cast<long long>(elem_bytes(a.dtype)));
   }
-  GradAct g{a.dy, a.lddy, a.pre, a.ldpre, own_dz ? const_cast<void*>(dz) : nullptr, lddz, nullptr, M, N, a.act};
-  if (a.db) {
-    const long long blocks = pic::lin::grad_act_blocks(g, a.dtype);
-    g.parts = static_cast<float*>(ws.take(blocks * N * 4));
-    if (launch) rc = pic::lin::grad_act(g, a.dtype, s);
-    if (launch && rc == PIC_OK) rc = pic::lin::sum_parts(g.parts, blocks, N, a.db, a.dtype, s);
-  } else if (launch && own_dz) {
-    rc = pic::lin::grad_act(g, a.dtype, s);
+  GradAct g{a.dy, a.lddy, a.pre, a.ldpre, own_dz ? const_cast<void*>(dz) : nullptr, lddz, a.db, nullptr, M, N, a.act};
+  if (own_dz || a.db) {
+    g.parts = static_cast<float*>(ws.take(pic::lin::grad_act_workspace(g, a.dtype)));
+    if (launch && (rc = pic::lin::grad_act(g, a.dtype, s)) != PIC_OK) return rc;
   }
-  if (rc != PIC_OK) return rc;
   if (a.dx) {
     Product p{};
     p.a = dz, p.a_i = lddz, p.a_k = 1;

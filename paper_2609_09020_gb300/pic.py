@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -44,6 +45,7 @@ PIC_STAGING_AUTO, PIC_STAGING_COPIES, PIC_STAGING_TMA = 0, 1, 2
 STAGINGS = {"auto": PIC_STAGING_AUTO, "copies": PIC_STAGING_COPIES, "tma": PIC_STAGING_TMA}
 PIC_ACT_NONE = 2
 LINEAR_ACTS = {"none": PIC_ACT_NONE, **ACTS}
+_GRADIENTS = frozenset(("x", "weight", "bias"))
 PIC_DTYPE_F32, PIC_DTYPE_F16, PIC_DTYPE_BF16 = 0, 1, 2
 DTYPES = {"torch.float32": PIC_DTYPE_F32, "torch.float16": PIC_DTYPE_F16,
           "torch.bfloat16": PIC_DTYPE_BF16}
@@ -497,16 +499,23 @@ class _Allocating:
             self._ctx.__exit__(*exc)
 
 
-def _call_with_workspace(name, args, like):
+# pic_linear_args and pic_linear_grad_args as their fields in order: packing the
+# bytes takes a tenth of the time of filling the structure
+_LINEAR_ARGS = struct.Struct("@3q2iPqPqPPqPqPq")
+_LINEAR_GRAD_ARGS = struct.Struct("@3q2iPqPqPqPqPqPqP")
+
+
+def _call_with_workspace(name, packed, torch, device):
     lib = load_library()
     call, workspace_bytes = _linear_calls[name] if _linear_calls else _find_linear_calls(lib, name)
-    ref = ctypes.byref(args)
-    need = workspace_bytes(ref)
-    if need < 0:
-        raise PicError(PIC_ERR_INVALID_ARG, name)
-    # in units of the call's type: new_empty takes fewer steps than torch.empty
-    ws = like.new_empty(-(-need // like.element_size())) if need else None
-    rc = call(ref, ws.data_ptr() if need else None, need, _current_stream())
+    stream = _current_stream()
+    # a call that needs workspace refuses to do without: nothing is launched then
+    rc = call(packed, None, 0, stream)
+    if rc == PIC_ERR_INVALID_ARG:
+        need = workspace_bytes(packed)
+        if need > 0:
+            ws = torch.empty(need, dtype=torch.uint8, device=device)
+            rc = call(packed, ws.data_ptr(), need, stream)
     if rc != PIC_OK:
         raise PicError(rc, name)
 
@@ -515,8 +524,11 @@ _linear_calls = {}
 
 
 def _find_linear_calls(lib, name):
+    """The C functions with untyped pointers, which ctypes passes bytes to."""
     for n in ("pic_linear", "pic_linear_backward"):
-        _linear_calls[n] = getattr(lib, n), getattr(lib, n + "_workspace_bytes")
+        f = ctypes.CFUNCTYPE(ctypes.c_int, _P, _P, ctypes.c_size_t, _P)((n, lib))
+        g = ctypes.CFUNCTYPE(ctypes.c_int64, _P)((n + "_workspace_bytes", lib))
+        _linear_calls[n] = f, g
     return _linear_calls[name]
 
 
@@ -535,34 +547,35 @@ def linear(x, weight, bias=None, act="none", residual=None, out=None, save_pre=F
     ``residual``), or (y, pre) with save_pre: pre = x weight^T + bias is what
     ``linear_backward`` reads.  x and residual may be 2-D with rows further
     apart than their width.  Enqueued on the stream, not synchronised."""
+    if stream is not None:
+        with _Allocating(stream):
+            return linear(x, weight, bias, act, residual, out, save_pre)
+    import torch
     _on_device(x, "x")
     if weight.dim() != 2:
         raise ValueError("weight: must be 2-D")
     N, K = weight.shape
     if N < 1 or K < 1:
         raise ValueError("weight: must not be empty")
-    a = pic_linear_args()
-    a.act = _linear_act(act)
-    a.dtype = _dtype_code(x, "x")
-    M = x.numel() // K
-    a.rows, a.in_features, a.out_features = M, K, N
-    a.x, a.ldx = _rows(x, "x", K, x)
-    a.w, a.ldw = _rows(weight, "weight", K, x)
-    if bias is not None:
-        a.bias = _vector(bias, "bias", N, x)
-    if residual is not None:
-        a.residual, a.ldr = _rows(residual, "residual", N, x, M, one_row=True)
-    shape = (M, N) if x.dim() == 2 else x.shape[:-1] + (N,)
-    with _Allocating(stream):
-        if out is None:
-            out = x.new_empty(shape)
-            a.y, a.ldy = out.data_ptr(), N
-        else:
-            a.y, a.ldy = _rows(out, "out", N, x, M)
-        if save_pre:
-            pre = x.new_empty(shape)
-            a.pre, a.ldpre = pre.data_ptr(), N
-        _call_with_workspace("pic_linear", a, x)
+    act_code, dtype, device = _linear_act(act), x.dtype, x.device
+    shape = x.shape
+    M = shape[0] if len(shape) == 2 else x.numel() // K
+    px, ldx = _rows(x, "x", K, x)
+    pw, ldw = _rows(weight, "weight", K, x)
+    pb = 0 if bias is None else _vector(bias, "bias", N, x)
+    pr, ldr = (0, 0) if residual is None else _rows(residual, "residual", N, x, M, one_row=True)
+    shape = (M, N) if len(shape) == 2 else shape[:-1] + (N,)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=device)
+        py, ldy = out.data_ptr(), N
+    else:
+        py, ldy = _rows(out, "out", N, x, M)
+    pre, pp = None, 0
+    if save_pre:
+        pre = torch.empty(shape, dtype=dtype, device=device)
+        pp = pre.data_ptr()
+    _call_with_workspace("pic_linear", _LINEAR_ARGS.pack(M, K, N, _dtype_code(x, "x"), act_code, px, ldx, pw, ldw,
+                                                         pb, pr, ldr, py, ldy, pp, N), torch, device)
     return (out, pre) if save_pre else out
 
 
@@ -571,40 +584,44 @@ def linear_backward(dy, x, weight, act="none", pre=None, need=("x", "weight", "b
     dy [..., out]; those not named in ``need`` are None.  pre is what
     ``linear`` returned with save_pre (not read with act "none").  The
     residual's gradient is dy itself.  Enqueued on the stream."""
+    if stream is not None:
+        with _Allocating(stream):
+            return linear_backward(dy, x, weight, act, pre, need)
+    import torch
     _on_device(dy, "dy")
     if weight.dim() != 2:
         raise ValueError("weight: must be 2-D")
     need = tuple(need)
-    if not need or set(need) - {"x", "weight", "bias"}:
+    if not need or not _GRADIENTS.issuperset(need):
         raise ValueError('need: must name some of "x", "weight" and "bias"')
     N, K = weight.shape
     if N < 1 or K < 1:
         raise ValueError("weight: must not be empty")
-    a = pic_linear_grad_args()
-    a.act = _linear_act(act)
-    a.dtype = _dtype_code(dy, "dy")
+    act_code, dtype, device = _linear_act(act), dy.dtype, dy.device
     M = x.numel() // K
-    a.rows, a.in_features, a.out_features = M, K, N
-    a.dy, a.lddy = _rows(dy, "dy", N, dy, M)
-    a.x, a.ldx = _rows(x, "x", K, dy)
-    a.w, a.ldw = _rows(weight, "weight", K, dy)
-    if a.act != PIC_ACT_NONE:
+    pdy, lddy = _rows(dy, "dy", N, dy, M)
+    px, ldx = _rows(x, "x", K, dy)
+    pw, ldw = _rows(weight, "weight", K, dy)
+    pz = ldz = 0
+    if act_code != PIC_ACT_NONE:
         if pre is None:
             raise ValueError(f"pre: needed for act {act!r}")
-        a.pre, a.ldpre = _rows(pre, "pre", N, dy, M)
+        pz, ldz = _rows(pre, "pre", N, dy, M)
     dx = dw = db = None
-    with _Allocating(stream):
-        if "x" in need:
-            dx = dy.new_empty(x.shape)
-            a.dx, a.lddx = dx.data_ptr(), K
-        if "weight" in need:
-            dw = dy.new_empty((N, K))
-            a.dw, a.lddw = dw.data_ptr(), K
-        if "bias" in need:
-            db = dy.new_empty(N)
-            a.db = db.data_ptr()
-        if M > 0 or "weight" in need or "bias" in need:
-            _call_with_workspace("pic_linear_backward", a, dy)
+    pdx = pdw = pdb = 0
+    if "x" in need:
+        dx = torch.empty(x.shape, dtype=dtype, device=device)
+        pdx = dx.data_ptr()
+    if "weight" in need:
+        dw = torch.empty((N, K), dtype=dtype, device=device)
+        pdw = dw.data_ptr()
+    if "bias" in need:
+        db = torch.empty(N, dtype=dtype, device=device)
+        pdb = db.data_ptr()
+    if M > 0 or pdw or pdb:
+        _call_with_workspace("pic_linear_backward",
+                             _LINEAR_GRAD_ARGS.pack(M, K, N, _dtype_code(dy, "dy"), act_code, pdy, lddy, px, ldx,
+                                                    pw, ldw, pz, ldz, pdx, K, pdw, K, pdb), torch, device)
     return dx, dw, db
 
 

@@ -141,3 +141,14 @@ def test_rows_describes_matrices(pic):
         pic._rows(t, "t", 11, like)
     with pytest.raises(ValueError):
         pic._rows(t, "t", 10, like, rows=5)
+
+
+def test_packed_arguments_are_the_structures(pic):
+    a = forward_args(pic, bias=P + 64, residual=P + 128, ldr=24, pre=P + 192, ldpre=25)
+    b = bytes(pic._LINEAR_ARGS.pack(8, 16, 24, pic.PIC_DTYPE_F16, pic.PIC_ACT_NONE, P, 16, P, 16, P + 64, P + 128, 24,
+                                    P + 4096, 24, P + 192, 25))
+    assert b == bytes(a) and len(b) == ctypes.sizeof(a)
+    a = backward_args(pic)
+    b = bytes(pic._LINEAR_GRAD_ARGS.pack(8, 16, 24, pic.PIC_DTYPE_F16, pic.PIC_ACT_GELU, P, 24, P, 16, P, 16, P, 24,
+                                         P + 4096, 16, P + 8192, 16, P + 16384))
+    assert b == bytes(a) and len(b) == ctypes.sizeof(a)
