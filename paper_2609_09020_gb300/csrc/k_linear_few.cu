@@ -382,19 +382,8 @@ int few_product(const Product& p, int dtype, cudaStream_t s) {
                         : (vec ? kernel_of<__half, true>(r) : kernel_of<__half, false>(r));
   const int slot = ((bf16 ? 2 : 0) + (vec ? 1 : 0)) * 3 + (r.along ? r.tiles : 0);
   if (set_up(fn, slot) != PIC_OK) return PIC_ERR_CUDA;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = r.cluster;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(r.grid);
-  cfg.blockDim = dim3(r.along ? 32 * kAlongWarps : 32 * kAcrossWarps);
-  cfg.dynamicSmemBytes = r.smem;
-  cfg.stream = s;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
   void* args[] = {&q};
-  return cudaLaunchKernelExC(&cfg, fn, args) == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+  return launch_kernel(fn, r.grid, 32 * (r.along ? kAlongWarps : kAcrossWarps), r.smem, r.cluster, args, s);
 }
 
 }  // namespace lin

@@ -86,12 +86,25 @@ __global__ void __launch_bounds__(kThreads) grad_act_kernel(const GradAct g, con
         const long long r = i + u * rows;
         if (r >= i1) break;
         Load<T, V> out;
+        float d[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) d[e] = a[u].at(e);
+        if (g.act != PIC_ACT_NONE) {
+          if constexpr (V > 1) {
+#pragma unroll
+            for (int e = 0; e < V; e += 2) {
+              const float2 r = act_grad2<sizeof(T) == 4>(make_float2(d[e], d[e + 1]), make_float2(z[u].at(e), z[u].at(e + 1)), g.act);
+              d[e] = r.x;
+              d[e + 1] = r.y;
+            }
+          } else {
+            d[0] = act_grad<sizeof(T) == 4>(d[0], z[u].at(0), g.act);
+          }
+        }
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          float d = a[u].at(e);
-          if (g.act != PIC_ACT_NONE) d = act_grad<sizeof(T) == 4>(d, z[u].at(e), g.act);
-          sum[e] += d;
-          reinterpret_cast<T*>(out.w)[e] = from_f32<T>(d);
+          sum[e] += d[e];
+          reinterpret_cast<T*>(out.w)[e] = from_f32<T>(d[e]);
         }
         if (g.dz) {
           if constexpr (V * sizeof(T) == 16)

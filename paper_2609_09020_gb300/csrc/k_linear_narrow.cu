@@ -134,6 +134,22 @@ __device__ __forceinline__ uint32_t put_vec(uint32_t tile, int block, int plane,
   }
 }
 
+// d *= act'(v)
+template <bool EXACT, int N>
+__device__ __forceinline__ void times_act_grad(float (&d)[N], const float (&v)[N], int act) {
+  if (act == PIC_ACT_RELU) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) d[e] = v[e] > 0.0f ? d[e] : 0.0f;
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; e += 2) {
+      const float2 r = act_grad2<EXACT>(make_float2(d[e], d[e + 1]), make_float2(v[e], v[e + 1]), PIC_ACT_GELU);
+      d[e] = r.x;
+      d[e + 1] = r.y;
+    }
+  }
+}
+
 __device__ __forceinline__ float dz_again(const NarrowGrad& g, long long i, int n) {
   const float d = static_cast<const float*>(g.dy)[i * g.lddy + n];
   return g.act == PIC_ACT_NONE ? d : act_grad<true>(d, static_cast<const float*>(g.pre)[i * g.ldpre + n], g.act);
@@ -262,8 +278,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           vy[u].widen(d);
           if (has_act) {
             vz[u].widen(v);
-#pragma unroll
-            for (int e = 0; e < S::kPer; ++e) d[e] = act_grad<false>(d[e], v[e], g.act);
+            times_act_grad<sizeof(T) == 4, S::kPer>(d, v, g.act);
             uint32_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[i] = pack2_16<T>(d[2 * i], d[2 * i + 1]);
@@ -299,8 +314,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           vy[u].widen(d);
           if (has_act) {
             vz[u].widen(v);
-#pragma unroll
-            for (int e = 0; e < S::kPer; ++e) d[e] = act_grad<sizeof(T) == 4>(d[e], v[e], g.act);
+            times_act_grad<sizeof(T) == 4, S::kPer>(d, v, g.act);
           }
 #pragma unroll
           for (int e = 0; e < S::kPer; ++e) sum[e] += d[e];
@@ -544,22 +558,25 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // dw and db from the CTAs' parts: a block finishes 32 values, its warps add every
-// eighth part, the first warp the warps' sums.
+// 32nd part, the first warp the warps' sums.
 template <typename T>
-__global__ void __launch_bounds__(256) add_parts_kernel(const float* parts, int n_parts, const NarrowGrad g) {
-  __shared__ float sums[8][32];
+__global__ void __launch_bounds__(1024) add_parts_kernel(const float* parts, int n_parts, const NarrowGrad g) {
+  __shared__ float sums[32][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nk = g.N * g.K, per = nk + g.N;
   const int e = blockIdx.x * 32 + lane;
   float v = 0.0f;
   if (e < per) {
-#pragma unroll 5
-    for (int s = warp; s < n_parts; s += 8) v += __ldcg(parts + s * static_cast<long long>(per) + e);
+#pragma unroll
+    for (int i = 0; i < (kSms + 31) / 32; ++i) {
+      const int s = warp + 32 * i;
+      if (s < n_parts) v += __ldcg(parts + s * static_cast<long long>(per) + e);
+    }
   }
   sums[warp][lane] = v;
   __syncthreads();
   if (warp > 0 || e >= per) return;
 #pragma unroll
-  for (int w = 1; w < 8; ++w) v += sums[w][lane];
+  for (int w = 1; w < 32; ++w) v += sums[w][lane];
   if (e >= nk) {
     if (g.db) static_cast<T*>(g.db)[e - nk] = from_f32<T>(v);
   } else if (g.dw) {
@@ -582,7 +599,7 @@ int run(const NarrowGrad& g, NarrowParams& q, NarrowMaps& maps, int slot, cudaSt
   if (cudaLaunchKernel(fn, dim3(grid), dim3(kThreads), args, smem, s) != cudaSuccess) return PIC_ERR_CUDA;
   if (g.dw || g.db) {
     const int per = g.N * g.K + g.N;
-    add_parts_kernel<T><<<(per + 31) / 32, 256, 0, s>>>(q.parts, grid, g);
+    add_parts_kernel<T><<<(per + 31) / 32, 1024, 0, s>>>(q.parts, grid, g);
   }
   return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
 }

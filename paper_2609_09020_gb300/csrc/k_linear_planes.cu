@@ -30,10 +30,20 @@ constexpr int kBars = 2 * kStages + 4 + 1;
 constexpr int kSmem = kOffBars + kBars * 8 + 16 + 1024;
 constexpr int kTmemCols = 2 * kPlCols;
 
-__global__ void __launch_bounds__(256) cut_kernel(const float* m, long long ld, long long rows, long long cols,
-                                                  uint16_t* planes, long long ld_out, int* marks, int col_blocks) {
-  const long long r0 = blockIdx.x / col_blocks * static_cast<long long>(kPlBlock);
-  const long long c0 = blockIdx.x % col_blocks * static_cast<long long>(kPlBlock);
+struct CutPair {
+  CutMatrix m[2];
+  unsigned blocks0;  // blocks of the first matrix
+};
+
+__global__ void __launch_bounds__(256) cut_kernel(const CutPair q) {
+  const int which = blockIdx.x < q.blocks0 ? 0 : 1;
+  const unsigned block = which ? blockIdx.x - q.blocks0 : blockIdx.x;
+  const float* m = q.m[which].m;
+  const long long ld = q.m[which].ld, rows = q.m[which].rows, cols = q.m[which].cols, ld_out = q.m[which].ld_out;
+  uint16_t* planes = static_cast<uint16_t*>(q.m[which].planes);
+  const unsigned col_blocks = static_cast<unsigned>((cols + kPlBlock - 1) / kPlBlock);
+  const long long r0 = block / col_blocks * static_cast<long long>(kPlBlock);
+  const long long c0 = block % col_blocks * static_cast<long long>(kPlBlock);
   const long long plane = rows * ld_out;
   // 16 quads of four columns for each thread: a warp takes a row's 128 columns
   const long long col = c0 + threadIdx.x % 32 * 4;
@@ -64,7 +74,7 @@ __global__ void __launch_bounds__(256) cut_kernel(const float* m, long long ld, 
     *reinterpret_cast<uint2*>(o + 2 * plane) = make_uint2(l0, l1);
   }
   const int bad = __syncthreads_or(largest >= 0x7f800000u);
-  if (threadIdx.x == 0) marks[blockIdx.x] = bad;
+  if (threadIdx.x == 0) q.m[which].marks[block] = bad;
 }
 
 // Whether a block of the 128 rows (or columns of B) `group` and of slices
@@ -269,11 +279,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 PlKernel planes_kernel_info() { return {reinterpret_cast<const void*>(planes_kernel), kThreads, kSmem}; }
 
-int cut_planes(const float* m, long long ld, long long rows, long long cols, void* planes, long long ld_out, int* marks,
-               cudaStream_t s) {
-  const long long row_blocks = (rows + kPlBlock - 1) / kPlBlock, col_blocks = (cols + kPlBlock - 1) / kPlBlock;
-  cut_kernel<<<static_cast<unsigned>(row_blocks * col_blocks), 256, 0, s>>>(m, ld, rows, cols, static_cast<uint16_t*>(planes),
-                                                                            ld_out, marks, static_cast<int>(col_blocks));
+int cut_planes(const CutMatrix (&m)[2], cudaStream_t s) {
+  const auto blocks = [](const CutMatrix& c) {
+    return static_cast<unsigned>((c.rows + kPlBlock - 1) / kPlBlock * ((c.cols + kPlBlock - 1) / kPlBlock));
+  };
+  const CutPair q{{m[0], m[1]}, blocks(m[0])};
+  cut_kernel<<<q.blocks0 + blocks(m[1]), 256, 0, s>>>(q);
   return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
 }
 

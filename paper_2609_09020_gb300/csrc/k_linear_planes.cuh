@@ -27,9 +27,15 @@ struct PlKernel {
 };
 PlKernel planes_kernel_info();
 
-// planes[3][rows][ld_out] (bfloat16) and marks from the fp32 matrix m [rows][cols].
-int cut_planes(const float* m, long long ld, long long rows, long long cols, void* planes, long long ld_out, int* marks,
-               cudaStream_t s);
+// planes[3][rows][ld_out] (bfloat16) and marks, from the fp32 matrix m [rows][cols].
+struct CutMatrix {
+  const float* m;
+  long long ld, rows, cols;
+  void* planes;
+  long long ld_out;
+  int* marks;
+};
+int cut_planes(const CutMatrix (&m)[2], cudaStream_t s);
 
 }  // namespace lin
 }  // namespace pic

@@ -15,13 +15,26 @@ namespace {
 
 constexpr int kSms = 152;
 
-// A matrix whose rows start on 16-byte boundaries, from one whose do not: a
-// thread puts eight elements together from the aligned words that hold them.
-// Bound by memory: it reads and writes each element once.
-__global__ void __launch_bounds__(256) repack_kernel(const uint16_t* src, long long ld, long long rows, int cols,
-                                                     uint4* dst, int chunks) {
+// Up to two matrices whose rows start on 16-byte boundaries, from ones whose do
+// not: a thread puts eight elements together from the aligned words that hold
+// them.  Bound by memory: it reads and writes each element once.
+struct Repack {
+  const uint16_t* src[2];
+  uint4* dst[2];
+  long long ld[2], rows[2];
+  int cols[2], chunks[2];  // chunks of eight elements in a row
+  unsigned blocks0;        // blocks that work on the first matrix
+};
+
+__global__ void __launch_bounds__(256) repack_kernel(const Repack q) {
+  const int m = blockIdx.x < q.blocks0 ? 0 : 1;
+  const unsigned block = m ? blockIdx.x - q.blocks0 : blockIdx.x, blocks = m ? gridDim.x - q.blocks0 : q.blocks0;
+  const uint16_t* src = q.src[m];
+  uint4* dst = q.dst[m];
+  const long long ld = q.ld[m], rows = q.rows[m];
+  const int cols = q.cols[m], chunks = q.chunks[m];
   const long long n = rows * chunks;
-  for (long long e = blockIdx.x * 256LL + threadIdx.x; e < n; e += gridDim.x * 256LL) {
+  for (long long e = block * 256LL + threadIdx.x; e < n; e += blocks * 256LL) {
     const long long r = n <= 0x7fffffffLL ? static_cast<int>(e) / chunks : e / chunks;
     const int c = static_cast<int>(e - r * chunks) * 8;
     const uint16_t* p = src + r * ld + c;
@@ -30,12 +43,12 @@ __global__ void __launch_bounds__(256) repack_kernel(const uint16_t* src, long l
     // the words' last half belongs to the element after the eight
     if (c + 8 + (odd && r + 1 == rows ? 1 : 0) <= cols) {
       if (odd) {
-        const uint32_t* q = reinterpret_cast<const uint32_t*>(p - 1);
-        uint32_t v[5];
+        const uint32_t* v = reinterpret_cast<const uint32_t*>(p - 1);
+        uint32_t h[5];
 #pragma unroll
-        for (int i = 0; i < 5; ++i) v[i] = __ldg(q + i);
+        for (int i = 0; i < 5; ++i) h[i] = __ldg(v + i);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(v[i], v[i + 1], 16);
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(h[i], h[i + 1], 16);
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = __ldg(reinterpret_cast<const uint32_t*>(p) + i);
@@ -196,14 +209,25 @@ bool encode_planes(CUtensorMap* map, const void* m, long long rows, long long co
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-const void* repacked(const void* m, const Operand& o, void* ws, cudaStream_t s) {
-  if (!o.repack) return m;
-  const int chunks = static_cast<int>(o.ld_packed / 8);
-  long long b = (o.rows * chunks + 255) / 256;
-  if (b > 16 * kSms) b = 16 * kSms;
-  repack_kernel<<<static_cast<unsigned>(b), 256, 0, s>>>(static_cast<const uint16_t*>(m), o.ld, o.rows,
-                                                         static_cast<int>(o.cols), static_cast<uint4*>(ws), chunks);
-  return ws;
+// The operands where TMA can read them: as they are, or laid out in the workspace.
+void lay_out(const Product& p, const Plan& r, char* w, const void** a, const void** b, cudaStream_t s) {
+  Repack q{};
+  unsigned blocks[2] = {0, 0};
+  int n = 0;
+  const auto add = [&](const void* m, const Operand& o, char* at) {
+    if (!o.repack) return m;
+    q.src[n] = static_cast<const uint16_t*>(m);
+    q.dst[n] = reinterpret_cast<uint4*>(at);
+    q.ld[n] = o.ld, q.rows[n] = o.rows;
+    q.cols[n] = static_cast<int>(o.cols), q.chunks[n] = static_cast<int>(o.ld_packed / 8);
+    const long long want = (o.rows * q.chunks[n] + 255) / 256;
+    blocks[n++] = static_cast<unsigned>(want < 16 * kSms ? want : 16 * kSms);
+    return static_cast<const void*>(at);
+  };
+  *a = add(p.a, r.a, w);
+  *b = add(p.b, r.b, w + r.a_bytes);
+  q.blocks0 = blocks[0];
+  if (n > 0) repack_kernel<<<blocks[0] + blocks[1], 256, 0, s>>>(q);
 }
 
 template <int CG, int BN>
@@ -258,8 +282,8 @@ int tc_product(const Product& p, int dtype, void* ws, int* status, unsigned spin
   const Plan r = plan(p, dtype);
   const long long elem = dtype == PIC_DTYPE_F32 ? 4 : 2;
   char* w = static_cast<char*>(ws);
-  const void* a = repacked(p.a, r.a, w, s);
-  const void* b = repacked(p.b, r.b, w + r.a_bytes, s);
+  const void *a, *b;
+  lay_out(p, r, w, &a, &b, s);
 
   TcParams q{};
   TcMaps maps;
@@ -290,13 +314,14 @@ int tc_product(const Product& p, int dtype, void* ws, int* status, unsigned spin
     };
     o.vec_a = vec(p.a, r.a), o.vec_b = vec(p.b, r.b);
   } else if (r.planes) {
-    const auto cut = [&](const void* m, const Operand& x, char* at, PlOperand& out, CUtensorMap* map, int box_rows) {
-      int* marks = reinterpret_cast<int*>(at + planes_bytes(x));
-      out = {static_cast<const float*>(m), x.ld, marks, static_cast<int>(mark_cols(x))};
-      return cut_planes(out.m, x.ld, x.rows, x.cols, at, x.ld_packed, marks, s) == PIC_OK &&
-             encode_planes(map, at, x.rows, x.cols, x.ld_packed, box_rows);
+    CutMatrix m[2];
+    const auto add = [&](CutMatrix& c, const void* from, const Operand& x, char* at, PlOperand& out, CUtensorMap* map, int box) {
+      c = {static_cast<const float*>(from), x.ld, x.rows, x.cols, at, x.ld_packed, reinterpret_cast<int*>(at + planes_bytes(x))};
+      out = {c.m, x.ld, c.marks, static_cast<int>(mark_cols(x))};
+      return encode_planes(map, at, x.rows, x.cols, x.ld_packed, box);
     };
-    ok = cut(p.a, r.a, w, pl.a, &maps.a, r.a.mn ? 64 : 128) && cut(p.b, r.b, w + r.a_bytes, pl.b, &maps.b, 64);
+    ok = add(m[0], p.a, r.a, w, pl.a, &maps.a, r.a.mn ? 64 : 128) &&
+         add(m[1], p.b, r.b, w + r.a_bytes, pl.b, &maps.b, 64) && cut_planes(m, s) == PIC_OK;
   } else {
     // of an operand that lies along its rows a box is 64 of them by 64 of K
     ok = encode(&maps.a, a, r.a.rows, r.a.cols, r.a.repack ? r.a.ld_packed : r.a.ld, r.a.mn ? 64 : 128, dtype) &&
@@ -326,19 +351,8 @@ int tc_product(const Product& p, int dtype, void* ws, int* status, unsigned spin
   long long grid = q.work * r.cg;
   const long long most = r.bn == 64 ? 2 * kSms : kSms;
   if (grid > most && !r.join) grid = most;  // joined: one tile a cluster
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = r.join ? r.splits : r.cg;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(grid));
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
   void* args[] = {&q, &maps, r.planes ? static_cast<void*>(&pl) : &o};  // 16-bit kernels take the first two
-  if (cudaLaunchKernelExC(&cfg, fn, args) != cudaSuccess) return PIC_ERR_CUDA;
+  if (launch_kernel(fn, grid, threads, smem, r.join ? r.splits : r.cg, args, s) != PIC_OK) return PIC_ERR_CUDA;
   if (q.parts && !r.join) {
     const JoinParams j{p, reinterpret_cast<const float4*>(q.parts), r.tiles_i, r.tiles_j, r.splits, 128 * r.cg, r.bn};
     if (dtype == PIC_DTYPE_F32) return join<float>(j, s);

@@ -138,6 +138,21 @@ __device__ __forceinline__ uint32_t idesc_of(int M, int N, bool a_mn, bool b_mn)
   return tc::idesc_16(M, N, !IsHalf<T>::value, a_mn, b_mn);
 }
 
+// Word `i` of row r of a panel buffer.
+__device__ __forceinline__ uint32_t panel_at(uint32_t buf, int r, int i) {
+  return buf + r * 128 + (((i >> 2) ^ (r & 7)) * 16) + (i & 3) * 4;
+}
+__device__ __forceinline__ uint32_t panel_word(uint32_t buf, int r, int i) {
+  uint32_t w;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(panel_at(buf, r, i)) : "memory");
+  return w;
+}
+// Whether every row of a matrix starts on a 16-byte boundary from column col0 on.
+template <typename T>
+__device__ __forceinline__ bool rows_on16(const void* m, long long ld, long long col0) {
+  return ((reinterpret_cast<uintptr_t>(m) + col0 * sizeof(T)) | static_cast<uintptr_t>(ld * sizeof(T))) % 16 == 0;
+}
+
 // One warp's panel (32 rows from row0, 128 bytes of columns from col0; this
 // lane's row in v) to global memory: into the panel buffer, swizzled as TMA and
 // the banks like it, then one TMA store, or one word of a row per lane and row.
@@ -158,22 +173,74 @@ __device__ __forceinline__ void put_panel(const uint32_t (&v)[32], uint32_t buf,
     return;
   }
   __syncwarp();
-  constexpr int kPer = 4 / sizeof(T);  // columns of a word
-  const long long col = col0 + kPer * lane;
-  T* o = static_cast<T*>(out) + row0 * ld + col;
-  const bool whole = ((reinterpret_cast<uintptr_t>(out) | static_cast<uintptr_t>(ld * sizeof(T))) & 3) == 0;
+  const int n = static_cast<int>(min(static_cast<long long>(128 / sizeof(T)), p.J - col0));  // columns that exist
   const int rows = static_cast<int>(min(32LL, p.I - row0));
+  T* o = static_cast<T*>(out) + row0 * ld + col0;
 #pragma unroll 4
   for (int r = 0; r < rows; ++r, o += ld) {
-    uint32_t w;
-    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(buf + r * 128 + (((lane >> 2) ^ (r & 7)) * 16) + (lane & 3) * 4));
-    if (whole && col + kPer <= p.J) {
-      *reinterpret_cast<uint32_t*>(o) = w;
+    const uint32_t w = panel_word(buf, r, lane);
+    if constexpr (sizeof(T) == 4) {
+      if (lane < n) reinterpret_cast<uint32_t*>(o)[lane] = w;
     } else {
-      const T* h = reinterpret_cast<const T*>(&w);
+      // words of two columns where the row's words lie: columns 2 l, 2 l + 1, or
+      // 2 l + 1, 2 l + 2 of a row that starts in the middle of one
+      uint16_t* h = reinterpret_cast<uint16_t*>(o) + 2 * lane;
+      if ((reinterpret_cast<uintptr_t>(o) & 2) == 0) {
+        if (2 * lane + 1 < n)
+          *reinterpret_cast<uint32_t*>(h) = w;
+        else if (2 * lane < n)
+          h[0] = static_cast<uint16_t>(w);
+      } else {
+        const uint32_t next = __shfl_down_sync(0xffffffffu, w, 1);
+        if (lane == 0) h[0] = static_cast<uint16_t>(w);
+        if (lane < 31 && 2 * lane + 2 < n)
+          *reinterpret_cast<uint32_t*>(h + 1) = w >> 16 | next << 16;
+        else if (2 * lane + 1 < n)
+          h[1] = static_cast<uint16_t>(w >> 16);
+      }
+    }
+  }
+  __syncwarp();
+}
+
+// The other way round: adds 128 bytes of columns from col0 of 32 rows of a matrix
+// whose rows lanes cannot read 16 bytes at a time, each lane its row's to v.
+template <typename T, int N>
+__device__ __forceinline__ void add_panel(float* v, uint32_t buf, int lane, long long row0, long long col0, const Product& p,
+                                          const void* m, long long ld) {
+  const int n = static_cast<int>(min(static_cast<long long>(N), p.J - col0));
+  const int rows = static_cast<int>(min(32LL, p.I - row0));
+  const T* o = static_cast<const T*>(m) + row0 * ld + col0;
+  __syncwarp();
+#pragma unroll 8
+  for (int r = 0; r < rows; ++r, o += ld) {
+    uint32_t w = 0;
+    if constexpr (sizeof(T) == 4) {
+      if (lane < n) w = reinterpret_cast<const uint32_t*>(o)[lane];
+    } else {
+      const uint16_t* h = reinterpret_cast<const uint16_t*>(o) + 2 * lane;
+      if (2 * lane < n) w = h[0];
+      if (2 * lane + 1 < n) w |= static_cast<uint32_t>(h[1]) << 16;
+    }
+    asm volatile("st.shared.b32 [%0], %1;" ::"r"(panel_at(buf, r, lane)), "r"(w) : "memory");
+  }
+  __syncwarp();
 #pragma unroll
-      for (int c = 0; c < kPer; ++c)
-        if (col + c < p.J) o[c] = h[c];
+  for (int c = 0; c < 8; ++c) {
+    uint32_t w[4];
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                 : "r"(buf + lane * 128 + ((c ^ (lane & 7)) * 16))
+                 : "memory");
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (sizeof(T) == 4) {
+        v[4 * c + e] += __uint_as_float(w[e]);
+      } else {
+        const float2 f = unpack2_16<T>(w[e]);
+        v[8 * c + 2 * e] += f.x;
+        v[8 * c + 2 * e + 1] += f.y;
+      }
     }
   }
   __syncwarp();
@@ -229,8 +296,15 @@ __device__ __forceinline__ void finish_rows(float (&v)[64], const Product& p, co
 #pragma unroll
     for (int c = 0; c < 64; ++c) v[c] = act_value<true>(v[c], p.act);
   }
-  if (p.residual && row0 + lane < p.I)
-    add_row<float>(v, static_cast<const float*>(p.residual) + (row0 + lane) * p.ldr + col0, cols);
+  if (p.residual) {
+    if (cols == 64 && rows_on16<float>(p.residual, p.ldr, col0)) {
+      if (row0 + lane < p.I) add_row<float>(v, static_cast<const float*>(p.residual) + (row0 + lane) * p.ldr + col0, 64);
+    } else {
+      if (lane == 0) tc::bulk_wait_read<0>();
+      add_panel<float, 32>(v, panel, lane, row0, col0, p, p.residual, p.ldr);
+      if (cols > 32) add_panel<float, 32>(v + 32, panel, lane, row0, col0 + 32, p, p.residual, p.ldr);
+    }
+  }
   put(p.y, p.ldy, &maps.y);
 }
 
@@ -468,17 +542,26 @@ __global__ void __launch_bounds__(kTcThreads, BN == 64 ? 2 : 1)
         }
         if (p.act == PIC_ACT_GELU) {
 #pragma unroll
-          for (int c = 0; c < 64; ++c) v[c] = act_value<false>(v[c], PIC_ACT_GELU);
+          for (int c = 0; c < 64; c += 2) {
+            const float2 r = unpack2(gelu_approx2(pack2(v[c], v[c + 1])));
+            v[c] = r.x;
+            v[c + 1] = r.y;
+          }
         } else if (p.act == PIC_ACT_RELU) {
 #pragma unroll
           for (int c = 0; c < 64; ++c) v[c] = relu_nan(v[c]);
         }
-        if (p.residual && row0 + lane < p.I)
-          add_row<T>(v, static_cast<const T*>(p.residual) + (row0 + lane) * p.ldr + j0 + c0, cols);
-#pragma unroll
-        for (int c = 0; c < 32; ++c) out[c] = pack2_16<T>(v[2 * c], v[2 * c + 1]);
         if (lane == 0) tc::bulk_wait_read<1>();
         __syncwarp();
+        if (p.residual) {
+          if (cols == 64 && rows_on16<T>(p.residual, p.ldr, j0 + c0)) {
+            if (row0 + lane < p.I) add_row<T>(v, static_cast<const T*>(p.residual) + (row0 + lane) * p.ldr + j0 + c0, 64);
+          } else {
+            add_panel<T, 64>(v, panels + pb * kPanelBytes, lane, row0, j0 + c0, p, p.residual, p.ldr);
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < 32; ++c) out[c] = pack2_16<T>(v[2 * c], v[2 * c + 1]);
         put_panel<T>(out, panels + pb * kPanelBytes, lane, row0, j0 + c0, p, p.y, p.ldy, &maps.y, q.store_tma);
         pb ^= 1;
       }

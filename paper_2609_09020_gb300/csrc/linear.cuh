@@ -70,6 +70,28 @@ __device__ __forceinline__ float act_grad(float dy, float z, int act) {
   return d == 0.0f ? 0.0f : dy * d;
 }
 
+// The same for two values: the polynomial runs on both in packed instructions.
+template <bool EXACT>
+__device__ __forceinline__ float2 act_grad2(float2 dy, float2 z, int act) {
+  if (act != PIC_ACT_GELU) return make_float2(act_grad<EXACT>(dy.x, z.x, act), act_grad<EXACT>(dy.y, z.y, act));
+  float2 a;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(a.x) : "f"(fabsf(z.x)), "f"(kGeluGradA));
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(a.y) : "f"(fabsf(z.y)), "f"(kGeluGradA));
+  const unsigned long long a2 = pack2(a.x, a.y);
+  const float c0 = EXACT ? gelu_grad_c32(0) : gelu_grad_c(0);
+  unsigned long long p = pack2(c0, c0);
+#pragma unroll
+  for (int i = 1; i <= (EXACT ? kGeluGradDeg32 : kGeluGradDeg); ++i) {
+    const float c = EXACT ? gelu_grad_c32(i) : gelu_grad_c(i);
+    p = fma2(p, a2, pack2(c, c));
+  }
+  const float2 e = unpack2(mul2(mul2(a2, a2), pack2(kGeluGradPower, kGeluGradPower)));
+  const float2 t2 = unpack2(mul2(p, pack2(ex2_approx(e.x), ex2_approx(e.y))));
+  const float tx = a.x >= kGeluGradA ? 0.0f : t2.x, ty = a.y >= kGeluGradA ? 0.0f : t2.y;
+  const float dx = z.x < 0.0f ? tx : 1.0f - tx, dz = z.y < 0.0f ? ty : 1.0f - ty;
+  return make_float2(dx == 0.0f ? 0.0f : dy.x * dx, dz == 0.0f ? 0.0f : dy.y * dz);
+}
+
 // One matrix product C[i][j] = sum_k A(i, k) B(j, k) with what follows it.
 // A(i, k) is at a[i * a_i + k * a_k], B(j, k) at b[j * b_j + k * b_k]; one of
 // the two strides is 1.
@@ -97,6 +119,24 @@ inline int split_count(long long tiles, long long K, long long step, long long t
   const long long most = K / step;
   if (s > most) s = most;
   return s < 1 ? 1 : static_cast<int>(s);
+}
+
+// Launches a kernel in clusters of `cluster` CTAs along x.
+inline int launch_kernel(const void* fn, long long grid, int threads, int smem, int cluster, void** args, cudaStream_t s) {
+  const dim3 g(static_cast<unsigned>(grid)), b(threads);
+  if (cluster == 1) return cudaLaunchKernel(fn, g, b, args, smem, s) == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = cluster;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = g;
+  cfg.blockDim = b;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelExC(&cfg, fn, args) == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
 }
 
 // Every function returns a pic_status; `ws` is device workspace.
