@@ -22,7 +22,7 @@ LIB = os.path.join(BUILD, "libpic_gb300.so")
 SOURCES = ["pic_decode.cu", "k_fp32.cu", "k_fp32_any.cu", "k_fp32_sweep.cu", "k_tc.cu",
            "k_tc_tma.cu", "k_march.cu", "k_march_f32lat.cu", "k_strip.cu", "k_izpr.cu",
            "k_idct.cu", "k_fuse.cu", "k_huffman.cu", "k_peak.cu", "pic_linear.cu",
-           "k_linear_simt.cu", "k_linear_grad.cu", "k_linear_tc.cu", "k_linear_tc_f16.cu",
+           "k_linear_grad.cu", "k_linear_tc.cu", "k_linear_tc_f16.cu",
            "k_linear_tc_bf16.cu", "k_linear_reg.cu",
            "k_linear_planes.cu", "k_linear_narrow.cu", "k_linear_few.cu", "k_clip.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

@@ -301,15 +301,8 @@ __global__ void __launch_bounds__(kRegThreads, 1)
   }
   tc::tc_fence_before();
   __syncthreads();
-  if (q.join) tc::cluster_sync();  // all parts are written
   tc::tc_fence_after();
   if (warp == kMmaWarp) tc::tmem_dealloc_cg<1>(tmem, kTmemCols);
-  if (q.join) {
-    const long long tile = blockIdx.x / q.splits;
-    for (int in = static_cast<int>(blockIdx.x % q.splits) * kRegThreads + threadIdx.x; in < 128 * kRegTile / 4;
-         in += q.splits * kRegThreads)
-      join_item<float, 128>(q.p, reinterpret_cast<const float4*>(q.parts), q.splits, kRegTile, q.tiles_i, q.tiles_j, tile, in);
-  }
 }
 
 }  // namespace

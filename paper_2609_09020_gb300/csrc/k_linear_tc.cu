@@ -22,7 +22,7 @@ struct Repack {
   const uint16_t* src[2];
   uint4* dst[2];
   long long ld[2], rows[2];
-  int cols[2], chunks[2];  // chunks of eight elements in a row
+  int cols[2], chunks[2], ld_out[2];  // chunks of eight elements in a row and from row to row
   unsigned blocks0;        // blocks that work on the first matrix
 };
 
@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(256) repack_kernel(const Repack q) {
       for (int i = 0; i < 8; ++i)
         if (c + i < cols) w[i / 2] |= static_cast<uint32_t>(__ldg(p + i)) << (16 * (i & 1));
     }
-    dst[e] = make_uint4(w[0], w[1], w[2], w[3]);
+    dst[r * q.ld_out[m] + c / 8] = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
@@ -69,32 +69,55 @@ struct JoinParams {
   int splits, rows, bn;  // rows and columns of a tile
 };
 
-// A block finishes 32 items (four columns of a row each): its warps add every
-// eighth part, then the first warp the warps' sums.
+// A thread finishes an item (four columns of a row), where there are few parts.
+template <typename T, int ROWS>
+__global__ void __launch_bounds__(256) join_few_kernel(const JoinParams q) {
+  const int per_tile = ROWS * q.bn / 4;
+  const long long tile = blockIdx.x / (per_tile / 256);
+  long long ti, tj;
+  tile_place<ROWS>(tile, q.tiles_i, q.tiles_j, ti, tj);
+  const JoinItem m = join_place<ROWS>(static_cast<int>(blockIdx.x % (per_tile / 256)) * 256 + threadIdx.x, q.bn, ti, tj);
+  if (m.i >= q.p.I || m.j >= q.p.J) return;
+  const float4* parts = q.parts + tile * q.splits * per_tile + m.at;
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+  for (int s = 0; s < q.splits; ++s) {
+    const float4 f = __ldcg(parts + static_cast<long long>(s) * per_tile);
+    v.x += f.x, v.y += f.y, v.z += f.z, v.w += f.w;
+  }
+  finish_item<T>(q.p, m, v);
+}
+
+// A block finishes 32 items, where there are many parts: its warps add every
+// eighth, then the first warp the warps' sums.
 template <typename T, int ROWS>
 __global__ void __launch_bounds__(256) join_kernel(const JoinParams q) {
   __shared__ float4 sums[8][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int per_tile = ROWS * q.bn / 4;
   const long long tile = blockIdx.x / (per_tile / 32);
-  const int in = static_cast<int>(blockIdx.x % (per_tile / 32)) * 32 + lane;
-  const float4* parts = q.parts + tile * q.splits * per_tile + ((in & ~511) | (in & 15) << 5 | (in >> 4 & 31));
+  long long ti, tj;
+  tile_place<ROWS>(tile, q.tiles_i, q.tiles_j, ti, tj);
+  const JoinItem m = join_place<ROWS>(static_cast<int>(blockIdx.x % (per_tile / 32)) * 32 + lane, q.bn, ti, tj);
+  const bool inside = m.i < q.p.I && m.j < q.p.J;
+  const float4* parts = q.parts + tile * q.splits * per_tile + m.at;
   float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  if (inside) {
 #pragma unroll 4
-  for (int s = warp; s < q.splits; s += 8) {
-    const float4 f = __ldcg(parts + static_cast<long long>(s) * per_tile);
-    v.x += f.x, v.y += f.y, v.z += f.z, v.w += f.w;
+    for (int s = warp; s < q.splits; s += 8) {
+      const float4 f = __ldcg(parts + static_cast<long long>(s) * per_tile);
+      v.x += f.x, v.y += f.y, v.z += f.z, v.w += f.w;
+    }
   }
   sums[warp][lane] = v;
   __syncthreads();
-  if (warp > 0) return;
+  if (warp > 0 || !inside) return;
 #pragma unroll
   for (int w = 1; w < 8; ++w) {
     const float4 f = sums[w][lane];
     v.x += f.x, v.y += f.y, v.z += f.z, v.w += f.w;
   }
-  const float partial[4] = {v.x, v.y, v.z, v.w};
-  join_item<T, ROWS>(q.p, nullptr, 0, q.bn, q.tiles_i, q.tiles_j, tile, in, partial);
+  finish_item<T>(q.p, m, v);
 }
 
 struct Operand {
@@ -109,7 +132,7 @@ Operand operand(const void* m, long long s_row, long long s_k, long long rows, l
   o.rows = o.mn ? K : rows;
   o.cols = o.mn ? rows : K;
   o.ld = o.mn ? s_k : s_row;
-  o.ld_packed = (o.cols + 7) / 8 * 8;
+  o.ld_packed = (o.cols + 63) / 64 * 64;  // rows on 128-byte lines
   if (o.rows == 1) o.ld = o.ld_packed;  // not used
   if (fp32) return o;
   o.repack = reinterpret_cast<uintptr_t>(m) % 16 != 0 || o.ld % 8 != 0 || o.ld * 2 >= (1LL << 40);
@@ -123,7 +146,6 @@ struct Plan {
   int cg, bn;
   long long tiles_i, tiles_j;
   int k_blocks, part_blocks, splits;
-  bool join;  // in the kernel, by clusters of `splits` CTAs
   long long a_bytes, b_bytes, part_bytes;
 };
 
@@ -133,45 +155,72 @@ long long planes_bytes(const Operand& o) { return round256(3 * o.rows * o.ld_pac
 long long mark_cols(const Operand& o) { return (o.cols + kPlBlock - 1) / kPlBlock; }
 long long marks_bytes(const Operand& o) { return round256((o.rows + kPlBlock - 1) / kPlBlock * mark_cols(o) * 4); }
 
+// What a tile shape costs, in microseconds, as measured on products of 64..4096
+// rows, K of 256..16384 and 256..4096 columns (bf16; fp32 for the last two).
+struct ShapeCost {
+  int bn, cg;
+  int slots;         // CTAs or pairs that run at once
+  double fixed;      // launch, first loads, last epilogue
+  double slice;      // 64 of K of a tile
+  double tile;       // a tile's epilogue, which the next one's slices hide
+};
+constexpr ShapeCost kShape64{64, 1, 2 * kSms, 4.2, 0.20, 3.0};
+constexpr ShapeCost kShape128{128, 1, kSms, 4.5, 0.19, 2.2};
+constexpr ShapeCost kShape256{256, 2, kSms / 2, 6.8, 0.26, 3.4};
+constexpr ShapeCost kShapeReg{kRegTile, 1, kSms, 6.0, 3.0, 3.0};
+constexpr ShapeCost kShapePlanes{kPlCols, 2, kSms / 2, 8.0, 0.85, 3.4};
+
+// The shape and the number of parts of K with the least estimated time, parts at
+// least `least` slices long: rounds of tiles, and for parts the second kernel, which
+// costs 2 us and their fp32 traffic at 2.6 TB/s.  For instance, in us (measured):
+// 1024 x 1024 -> 1024 128/1 7.6 (7.7), 1024 x 4096 -> 1024 128/1 16.7 (16.5) and
+// 128/4 19.0 (19.0), 512 x 16384 -> 512 128/8 15.8 (15.2), 64/8 (20), 256/8 (19.3).
+// Rows that are not whole 128-byte lines make slices of 64 and 128 columns half as
+// slow again (720 x 12632 -> 496 128/4 25.9 (25.7), 256/8 21.9 (21.2)).
+void choose(Plan& r, const Product& p, const ShapeCost* shapes, int n_shapes, int least, bool lines) {
+  double best = 1e30;
+  for (int c = 0; c < n_shapes; ++c) {
+    const ShapeCost& h = shapes[c];
+    const int rows = 128 * h.cg;
+    const long long ti = (p.I + rows - 1) / rows, tj = (p.J + h.bn - 1) / h.bn, tiles = ti * tj;
+    double slice = h.slice;
+    if (!lines) slice *= h.bn == 256 ? 1.25 : 1.75;
+    for (int want = 1; want <= 2 * kSms; want = want < 8 ? want + 1 : want + want / 8) {
+      if (want > 1 && (tiles * want > h.slots || r.k_blocks / want < least)) break;
+      const int part = (r.k_blocks + want - 1) / want;
+      const int splits = (r.k_blocks + part - 1) / part;
+      const long long work = tiles * splits, rounds = (work + h.slots - 1) / h.slots;
+      const bool shared = h.bn == 64 && work > kSms;  // two CTAs on an SM
+      const double each = part * slice * (shared ? 1.5 : 1.0);
+      double t = h.fixed + (rounds > 1 && each < h.tile ? rounds * h.tile : rounds * each);
+      if (splits > 1) t += 2.0 + 4.0 * rows * h.bn * static_cast<double>(work) / 2.6e6;
+      if (t < best) {
+        best = t;
+        r.bn = h.bn, r.cg = h.cg, r.tiles_i = ti, r.tiles_j = tj;
+        r.part_blocks = part, r.splits = splits;
+      }
+    }
+  }
+}
+
 Plan plan(const Product& p, int dtype) {
   Plan r{};
   const bool fp32 = dtype == PIC_DTYPE_F32;
   r.a = operand(p.a, p.a_i, p.a_k, p.I, p.K, fp32);
   r.b = operand(p.b, p.b_j, p.b_k, p.J, p.K, fp32);
   // fp32: cutting the operands first costs 10 bytes of traffic an element, cutting
-  // them on the way costs twice the MMAs' time for every tile
+  // them on the way three times the MMAs' time for every tile
   r.planes = fp32 && p.I >= 256 && p.J >= 256;
   r.reg = fp32 && !r.planes;
-  const long long big = ((p.I + 255) / 256) * ((p.J + 255) / 256);
-  const long long mid = ((p.I + 127) / 128) * ((p.J + 127) / 128);
-  r.bn = p.J <= 64 || mid < kSms / 2 ? 64 : p.J <= 128 || big < kSms / 2 ? 128 : 256;
-  if (r.reg) r.bn = kRegTile;
-  if (r.planes) r.bn = kPlCols;
-  r.cg = r.bn == 256 || r.planes ? 2 : 1;
-  const int rows = 128 * r.cg;
-  r.tiles_i = (p.I + rows - 1) / rows;
-  r.tiles_j = (p.J + r.bn - 1) / r.bn;
   r.k_blocks = static_cast<int>((p.K + kSlice - 1) / kSlice);
-  const long long tiles = r.tiles_i * r.tiles_j;
-  int splits = split_count(tiles, r.k_blocks, fp32 ? 4 : 16, r.bn == 64 ? 2 * kSms : kSms / r.cg);
-  if (splits > 1 && r.cg == 1 && tiles * 8 >= kSms / 2) {
-    // the parts of a tile as a cluster
-    while (splits & (splits - 1)) splits &= splits - 1;
-    if (splits > 8) splits = 8;
-    r.join = splits > 1;
+  if (fp32) {
+    choose(r, p, r.reg ? &kShapeReg : &kShapePlanes, 1, 4, true);
+  } else {
+    const ShapeCost shapes[] = {kShape64, kShape128, kShape256};
+    const auto lines = [](const Operand& o) { return o.repack || o.ld % 64 == 0; };
+    choose(r, p, shapes, 3, 4, lines(r.a) && lines(r.b));
   }
-  r.part_blocks = (r.k_blocks + splits - 1) / splits;
-  r.splits = (r.k_blocks + r.part_blocks - 1) / r.part_blocks;
-  if (r.join && r.splits != splits) {  // a part would be empty: as many as are whole
-    r.splits = 1, r.part_blocks = r.k_blocks, r.join = false;
-    for (int c = splits / 2; c > 1; c /= 2) {
-      const int n = (r.k_blocks + c - 1) / c;
-      if ((r.k_blocks + n - 1) / n == c) {
-        r.splits = c, r.part_blocks = n, r.join = true;
-        break;
-      }
-    }
-  }
+  const int rows = 128 * r.cg;
   if (r.a.repack) r.a_bytes = round256(r.a.rows * r.a.ld_packed * 2);
   if (r.b.repack) r.b_bytes = round256(r.b.rows * r.b.ld_packed * 2);
   if (r.planes) {
@@ -219,7 +268,8 @@ void lay_out(const Product& p, const Plan& r, char* w, const void** a, const voi
     q.src[n] = static_cast<const uint16_t*>(m);
     q.dst[n] = reinterpret_cast<uint4*>(at);
     q.ld[n] = o.ld, q.rows[n] = o.rows;
-    q.cols[n] = static_cast<int>(o.cols), q.chunks[n] = static_cast<int>(o.ld_packed / 8);
+    q.cols[n] = static_cast<int>(o.cols), q.chunks[n] = static_cast<int>((o.cols + 7) / 8);
+    q.ld_out[n] = static_cast<int>(o.ld_packed / 8);
     const long long want = (o.rows * q.chunks[n] + 255) / 256;
     blocks[n++] = static_cast<unsigned>(want < 16 * kSms ? want : 16 * kSms);
     return static_cast<const void*>(at);
@@ -237,11 +287,20 @@ int smem_of() {
 
 template <typename T>
 int join(const JoinParams& q, cudaStream_t s) {
-  const unsigned blocks = static_cast<unsigned>(q.tiles_i * q.tiles_j * q.rows * q.bn / 4 / 32);
-  if (q.rows == 128)
-    join_kernel<T, 128><<<blocks, 256, 0, s>>>(q);
-  else
-    join_kernel<T, 256><<<blocks, 256, 0, s>>>(q);
+  const long long items = q.tiles_i * q.tiles_j * q.rows * q.bn / 4;
+  if (q.splits <= 16) {
+    const unsigned blocks = static_cast<unsigned>(items / 256);
+    if (q.rows == 128)
+      join_few_kernel<T, 128><<<blocks, 256, 0, s>>>(q);
+    else
+      join_few_kernel<T, 256><<<blocks, 256, 0, s>>>(q);
+  } else {
+    const unsigned blocks = static_cast<unsigned>(items / 32);
+    if (q.rows == 128)
+      join_kernel<T, 128><<<blocks, 256, 0, s>>>(q);
+    else
+      join_kernel<T, 256><<<blocks, 256, 0, s>>>(q);
+  }
   return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
 }
 
@@ -295,7 +354,6 @@ int tc_product(const Product& p, int dtype, void* ws, int* status, unsigned spin
   q.work = r.tiles_i * r.tiles_j * r.splits;
   q.a_mn = r.a.mn, q.b_mn = r.b.mn;
   q.parts = r.splits > 1 ? reinterpret_cast<float*>(w + r.a_bytes + r.b_bytes) : nullptr;
-  q.join = r.join;
   q.status = status;
   q.spin_limit = spin_limit;
   const auto fits = [&](const void* m, long long ld, long long rows) {
@@ -350,10 +408,10 @@ int tc_product(const Product& p, int dtype, void* ws, int* status, unsigned spin
   if (allow_smem(fn, slot, smem) != PIC_OK) return PIC_ERR_CUDA;
   long long grid = q.work * r.cg;
   const long long most = r.bn == 64 ? 2 * kSms : kSms;
-  if (grid > most && !r.join) grid = most;  // joined: one tile a cluster
+  if (grid > most) grid = most;
   void* args[] = {&q, &maps, r.planes ? static_cast<void*>(&pl) : &o};  // 16-bit kernels take the first two
-  if (launch_kernel(fn, grid, threads, smem, r.join ? r.splits : r.cg, args, s) != PIC_OK) return PIC_ERR_CUDA;
-  if (q.parts && !r.join) {
+  if (launch_kernel(fn, grid, threads, smem, r.cg, args, s) != PIC_OK) return PIC_ERR_CUDA;
+  if (q.parts) {
     const JoinParams j{p, reinterpret_cast<const float4*>(q.parts), r.tiles_i, r.tiles_j, r.splits, 128 * r.cg, r.bn};
     if (dtype == PIC_DTYPE_F32) return join<float>(j, s);
     return dtype == PIC_DTYPE_BF16 ? join<__nv_bfloat16>(j, s) : join<__half>(j, s);

@@ -14,10 +14,8 @@
 // next tile's MMAs.  An operand may be contiguous along K or along its rows
 // (dz and x in dw = dz^T x): TMA then brings blocks of 64 rows x 64 of K and
 // the MMA reads them transposed.  A product that has fewer tiles than the GPU
-// has SMs is cut along K: each part's accumulators go to the workspace in fp32.
-// Up to 8 parts of a tile are a cluster, whose CTAs meet once and then each add
-// a share of the tile's parts, in order, and run the epilogue on it; more parts
-// (dw over many rows) are added by a second kernel.
+// has SMs is cut along K: each part's accumulators go to the workspace in fp32,
+// and a second kernel adds the parts in order and runs the epilogue.
 //
 // Each wait is bounded: a thread whose wait runs out raises its CTA's abort
 // flag and the status word, and every role skips what is left.
@@ -43,7 +41,6 @@ struct TcParams {
   int a_mn, b_mn;        // the operand is contiguous along its rows
   int store_tma;         // y (and pre) go out by TMA
   float* parts;          // fp32 parts, or null: the epilogue runs in the kernel
-  int join;              // the CTAs of a tile's parts are a cluster and join them
   int* status;
   unsigned spin_limit;
 };
@@ -308,47 +305,59 @@ __device__ __forceinline__ void finish_rows(float (&v)[64], const Product& p, co
   put(p.y, p.ldy, &maps.y);
 }
 
-// Four columns (item `in` of `tile`) of a product cut along K: adds the parts in
-// order and runs the epilogue.  A part is [rank][panel][quarter][16][32 rows][4
-// columns]; neighbouring items are neighbouring columns.
-template <typename T, int ROWS>
-__device__ __forceinline__ void join_item(const Product& p, const float4* parts, int splits, int bn, long long tiles_i,
-                                          long long tiles_j, long long tile, int in, const float* partial = nullptr) {
+// A product cut along K: a tile's parts are [rank][panel][quarter][16][32 rows][4
+// columns] of fp32 each; an item is four columns of a row, and neighbouring items
+// are neighbouring columns.
+struct JoinItem {
+  long long i, j;
+  int at;  // in a part, in float4
+};
+template <int ROWS>
+__device__ __forceinline__ JoinItem join_place(int in, int bn, long long ti, long long tj) {
   const int c4 = in & 15, row = in >> 4 & 31, quarter = in >> 9 & 3, rest = in >> 11;
   const int panel = rest % (bn / 64), rank = rest / (bn / 64);
-  long long ti, tj;
-  tile_place<ROWS>(tile, tiles_i, tiles_j, ti, tj);
-  const long long i = ti * ROWS + rank * 128 + quarter * 32 + row, j = tj * bn + panel * 64 + c4 * 4;
-  if (i >= p.I || j >= p.J) return;
-  float v[4] = {};
-  if (partial) {
-    for (int c = 0; c < 4; ++c) v[c] = partial[c];
-  } else {
-    const int per_tile = ROWS * bn / 4;
-    const float4* q = parts + tile * splits * per_tile + (rest << 11 | quarter << 9 | c4 << 5 | row);
-    for (int s = 0; s < splits; ++s) {
-      const float4 f = __ldcg(q + static_cast<long long>(s) * per_tile);
-      v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
+  return {ti * ROWS + rank * 128 + quarter * 32 + row, tj * bn + panel * 64 + c4 * 4,
+          rest << 11 | quarter << 9 | c4 << 5 | row};
+}
+
+// The epilogue of an item's sums.
+template <typename T>
+__device__ __forceinline__ void finish_item(const Product& p, const JoinItem& m, const float4& sum) {
+  const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+  T y[4], pre[4];
+  const int cols = static_cast<int>(min(4LL, p.J - m.j));
+  struct alignas(4 * sizeof(T)) Four {
+    T t[4];
+  };
+  const T* bias = static_cast<const T*>(p.bias) + m.j;
+  const T* res = static_cast<const T*>(p.residual) + m.i * p.ldr + m.j;
+  Four b{}, r{};
+  if (p.bias) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (c < cols) b.t[c] = bias[c];
+  }
+  if (p.residual) {
+    if (cols == 4 && reinterpret_cast<uintptr_t>(res) % sizeof(Four) == 0) {
+      r = *reinterpret_cast<const Four*>(res);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (c < cols) r.t[c] = res[c];
     }
   }
-  T y[4], pre[4];
-  const int cols = static_cast<int>(min(4LL, p.J - j));
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
-    if (c >= cols) break;
     float z = v[c];
-    if (p.bias) z += to_f32(static_cast<const T*>(p.bias)[j + c]);
+    if (p.bias) z += to_f32(b.t[c]);
     pre[c] = from_f32<T>(z);
     z = act_value<sizeof(T) == 4>(z, p.act);
-    if (p.residual) z += to_f32(static_cast<const T*>(p.residual)[i * p.ldr + j + c]);
+    if (p.residual) z += to_f32(r.t[c]);
     y[c] = from_f32<T>(z);
   }
   const auto put = [&](void* out, long long ld, const T (&t)[4]) {
-    T* o = static_cast<T*>(out) + i * ld + j;
-    if (cols == 4 && reinterpret_cast<uintptr_t>(o) % (4 * sizeof(T)) == 0) {
-      struct alignas(4 * sizeof(T)) Four {
-        T t[4];
-      };
+    T* o = static_cast<T*>(out) + m.i * ld + m.j;
+    if (cols == 4 && reinterpret_cast<uintptr_t>(o) % sizeof(Four) == 0) {
       *reinterpret_cast<Four*>(o) = {t[0], t[1], t[2], t[3]};
     } else {
 #pragma unroll
@@ -572,15 +581,9 @@ __global__ void __launch_bounds__(kTcThreads, BN == 64 ? 2 : 1)
   }
   tc::tc_fence_before();
   __syncthreads();
-  if (CG == 2 || q.join) tc::cluster_sync();  // the pair is done; all parts are written
+  if constexpr (CG == 2) tc::cluster_sync();
   tc::tc_fence_after();
   if (warp == 1) tc::tmem_dealloc_cg<CG>(tmem, S::kTmemCols);
-  if (CG == 1 && q.join) {
-    const long long tile = blockIdx.x / q.splits;
-    for (int in = static_cast<int>(blockIdx.x % q.splits) * kTcThreads + threadIdx.x; in < 128 * BN / 4;
-         in += q.splits * kTcThreads)
-      join_item<T, 128>(q.p, reinterpret_cast<const float4*>(q.parts), q.splits, BN, q.tiles_i, q.tiles_j, tile, in);
-  }
 }
 
 // A [rows][cols] matrix in boxes of 128 bytes of columns and box_rows rows,

@@ -111,16 +111,6 @@ struct Product {
   int act;
 };
 
-// Parts of the sum over K that one product is cut into (1: none), each at least
-// `step`, so that about `target` blocks have work.
-inline int split_count(long long tiles, long long K, long long step, long long target) {
-  if (tiles >= target) return 1;
-  long long s = target / tiles;
-  const long long most = K / step;
-  if (s > most) s = most;
-  return s < 1 ? 1 : static_cast<int>(s);
-}
-
 // Launches a kernel in clusters of `cluster` CTAs along x.
 inline int launch_kernel(const void* fn, long long grid, int threads, int smem, int cluster, void** args, cudaStream_t s) {
   const dim3 g(static_cast<unsigned>(grid)), b(threads);
@@ -140,9 +130,6 @@ inline int launch_kernel(const void* fn, long long grid, int threads, int smem, 
 }
 
 // Every function returns a pic_status; `ws` is device workspace.
-long long simt_workspace(const Product& p);
-int simt_product(const Product& p, int dtype, void* ws, cudaStream_t s);
-
 // On the tensor cores; `status` is set to 1 if a bounded wait
 // (at most spin_limit polls) gives up.
 long long tc_workspace(const Product& p, int dtype);

@@ -164,7 +164,7 @@ int backward(const pic_linear_grad_args& a, Arena& ws, bool launch, cudaStream_t
   long long lddz = a.lddy;
   const bool own_dz = a.act != PIC_ACT_NONE && products;
   if (own_dz) {
-    lddz = (N + 7) / 8 * 8;  // rows of 16-bit values on 16-byte boundaries
+    lddz = (N + 63) / 64 * 64;  // rows of 16-bit values on 128-byte lines
     dz = ws.take(M * lddz * static_cast<long long>(elem_bytes(a.dtype)));
   }
   GradAct g{a.dy, a.lddy, a.pre, a.ldpre, own_dz ? const_cast<void*>(dz) : nullptr, lddz, a.db, nullptr, M, N, a.act};
