@@ -16,7 +16,7 @@
  * fp32 (PIC_DTYPE_F32), IEEE half (PIC_DTYPE_F16) or bfloat16
  * (PIC_DTYPE_BF16).  Sums are held in fp32; outputs are rounded once, to
  * nearest.  In the backward pass of a 16-bit type, dz is rounded to that type
- * before the two products.
+ * before the products (but for db, and for dw of up to 15 rows).
  *
  * Conventions as in pic_decode.h: device pointers owned by the caller and
  * aligned to their element, asynchronous on `stream`, pic_status codes, no

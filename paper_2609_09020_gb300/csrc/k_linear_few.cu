@@ -44,7 +44,7 @@ struct FewParams {
   int cluster;  // CTAs that share K
   int k_part;   // K of one of them, a multiple of 32
   int stride;   // bytes from row to row in shared memory
-  int a_vec;    // A's rows start on 16-byte boundaries
+  int a_vec, pre_vec;  // A's (and a_pre's) rows start on 16-byte boundaries
 };
 
 // ---- m16n8k16, fp32 accumulators ----------------------------------------------
@@ -87,6 +87,23 @@ __device__ __forceinline__ uint4 load8(const T* p, int n) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// Eight elements of a row of A, or of dz = dy act'(z) rounded to its type.
+template <typename T>
+__device__ __forceinline__ uint4 load_a(const FewParams& q, int r, long long k, int n) {
+  const Product& p = q.p;
+  const T* a = static_cast<const T*>(p.a) + r * p.a_i + k;
+  const uint4 w = q.a_vec ? load8<T, true>(a, n) : load8<T, false>(a, n);
+  if (!p.a_pre) return w;
+  const T* z = static_cast<const T*>(p.a_pre) + r * p.a_pre_i + k;
+  const uint4 v = q.pre_vec ? load8<T, true>(z, n) : load8<T, false>(z, n);
+  uint4 out;
+  const T *d = reinterpret_cast<const T*>(&w), *e = reinterpret_cast<const T*>(&v);
+  T* o = reinterpret_cast<T*>(&out);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o[i] = from_f32<T>(act_grad<false>(to_f32(d[i]), to_f32(e[i]), p.a_act));
+  return out;
+}
+
 // This CTA's part of K of A's rows into shared memory, zero past K's end.
 template <typename T>
 __device__ __forceinline__ void load_rows(uint8_t* s, const FewParams& q, int k0) {
@@ -96,11 +113,7 @@ __device__ __forceinline__ void load_rows(uint8_t* s, const FewParams& q, int k0
     const int r = e / vecs, v = e % vecs;
     const long long left = p.K - k0 - v * 8;
     uint4 w = make_uint4(0, 0, 0, 0);
-    if (left > 0) {
-      const T* a = static_cast<const T*>(p.a) + r * p.a_i + k0 + v * 8;
-      const int n = static_cast<int>(left < 8 ? left : 8);
-      w = q.a_vec ? load8<T, true>(a, n) : load8<T, false>(a, n);
-    }
+    if (left > 0) w = load_a<T>(q, r, k0 + v * 8, static_cast<int>(left < 8 ? left : 8));
     *reinterpret_cast<uint4*>(s + r * q.stride + v * 16) = w;
   }
 }
@@ -373,9 +386,10 @@ bool few_takes(const Product& p) { return plan(p).ok; }
 
 int few_product(const Product& p, int dtype, cudaStream_t s) {
   const Plan r = plan(p);
-  FewParams q{p, r.groups, r.cluster, r.k_part, r.stride, 0};
+  FewParams q{p, r.groups, r.cluster, r.k_part, r.stride, 0, 0};
   const auto on16 = [](const void* m, long long ld) { return reinterpret_cast<uintptr_t>(m) % 16 == 0 && ld % 8 == 0; };
   q.a_vec = reinterpret_cast<uintptr_t>(p.a) % 16 == 0 && (p.I == 1 || p.a_i % 8 == 0);
+  q.pre_vec = reinterpret_cast<uintptr_t>(p.a_pre) % 16 == 0 && (p.I == 1 || p.a_pre_i % 8 == 0);
   const bool vec = on16(p.b, r.along ? p.b_j : p.b_k);
   const bool bf16 = dtype == PIC_DTYPE_BF16;
   const void* fn = bf16 ? (vec ? kernel_of<__nv_bfloat16, true>(r) : kernel_of<__nv_bfloat16, false>(r))

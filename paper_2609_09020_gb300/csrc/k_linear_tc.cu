@@ -17,49 +17,61 @@ constexpr int kSms = 152;
 
 // Up to two matrices whose rows start on 16-byte boundaries, from ones whose do
 // not: a thread puts eight elements together from the aligned words that hold
-// them.  Bound by memory: it reads and writes each element once.
+// them, of four rows at a time.  Bound by memory: it reads and writes each element
+// once.
 struct Repack {
   const uint16_t* src[2];
   uint4* dst[2];
   long long ld[2], rows[2];
-  int cols[2], chunks[2], ld_out[2];  // chunks of eight elements in a row and from row to row
+  int cols[2], ld_out[2];  // ld_out: chunks of eight elements from row to row
+  int tx[2];               // threads along a row, a power of two
   unsigned blocks0;        // blocks that work on the first matrix
 };
+constexpr int kRepackRows = 4;
 
 __global__ void __launch_bounds__(256) repack_kernel(const Repack q) {
   const int m = blockIdx.x < q.blocks0 ? 0 : 1;
   const unsigned block = m ? blockIdx.x - q.blocks0 : blockIdx.x, blocks = m ? gridDim.x - q.blocks0 : q.blocks0;
-  const uint16_t* src = q.src[m];
-  uint4* dst = q.dst[m];
   const long long ld = q.ld[m], rows = q.rows[m];
-  const int cols = q.cols[m], chunks = q.chunks[m];
-  const long long n = rows * chunks;
-  for (long long e = block * 256LL + threadIdx.x; e < n; e += blocks * 256LL) {
-    const long long r = n <= 0x7fffffffLL ? static_cast<int>(e) / chunks : e / chunks;
-    const int c = static_cast<int>(e - r * chunks) * 8;
-    const uint16_t* p = src + r * ld + c;
-    uint32_t w[4] = {};
-    const bool odd = (reinterpret_cast<uintptr_t>(p) & 2) != 0;
-    // the words' last half belongs to the element after the eight
-    if (c + 8 + (odd && r + 1 == rows ? 1 : 0) <= cols) {
-      if (odd) {
-        const uint32_t* v = reinterpret_cast<const uint32_t*>(p - 1);
-        uint32_t h[5];
+  const int cols = q.cols[m], chunks = (cols + 7) / 8, tx = q.tx[m], ty = 256 / tx;
+  const int x = threadIdx.x & (tx - 1), y = threadIdx.x / tx;
+  for (long long r0 = static_cast<long long>(block) * ty * kRepackRows; r0 < rows;
+       r0 += static_cast<long long>(blocks) * ty * kRepackRows)
+    for (int chunk = x; chunk < chunks; chunk += tx) {
+      const int c = chunk * 8;
+      uint32_t h[kRepackRows][5];
+      bool odd[kRepackRows];
 #pragma unroll
-        for (int i = 0; i < 5; ++i) h[i] = __ldg(v + i);
+      for (int u = 0; u < kRepackRows; ++u) {
+        const long long r = r0 + u * ty + y;
+        const uint16_t* p = q.src[m] + r * ld + c;
+        odd[u] = (reinterpret_cast<uintptr_t>(p) & 2) != 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(h[i], h[i + 1], 16);
-      } else {
+        for (int i = 0; i < 5; ++i) h[u][i] = 0;
+        if (r >= rows) continue;
+        // the words' last half belongs to the element after the eight
+        if (c + 8 + (odd[u] && r + 1 == rows ? 1 : 0) <= cols) {
+          const uint32_t* v = reinterpret_cast<const uint32_t*>(p - (odd[u] ? 1 : 0));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __ldg(reinterpret_cast<const uint32_t*>(p) + i);
+          for (int i = 0; i < 4; ++i) h[u][i] = __ldg(v + i);
+          if (odd[u]) h[u][4] = __ldg(v + 4);
+        } else {
+          odd[u] = false;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (c + i < cols) h[u][i / 2] |= static_cast<uint32_t>(__ldg(p + i)) << (16 * (i & 1));
+        }
       }
-    } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (c + i < cols) w[i / 2] |= static_cast<uint32_t>(__ldg(p + i)) << (16 * (i & 1));
+      for (int u = 0; u < kRepackRows; ++u) {
+        const long long r = r0 + u * ty + y;
+        if (r >= rows) continue;
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = odd[u] ? __funnelshift_r(h[u][i], h[u][i + 1], 16) : h[u][i];
+        q.dst[m][r * q.ld_out[m] + chunk] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
     }
-    dst[r * q.ld_out[m] + c / 8] = make_uint4(w[0], w[1], w[2], w[3]);
-  }
 }
 
 struct JoinParams {
@@ -268,9 +280,11 @@ void lay_out(const Product& p, const Plan& r, char* w, const void** a, const voi
     q.src[n] = static_cast<const uint16_t*>(m);
     q.dst[n] = reinterpret_cast<uint4*>(at);
     q.ld[n] = o.ld, q.rows[n] = o.rows;
-    q.cols[n] = static_cast<int>(o.cols), q.chunks[n] = static_cast<int>((o.cols + 7) / 8);
+    q.cols[n] = static_cast<int>(o.cols);
     q.ld_out[n] = static_cast<int>(o.ld_packed / 8);
-    const long long want = (o.rows * q.chunks[n] + 255) / 256;
+    q.tx[n] = 1;
+    while (q.tx[n] < (o.cols + 7) / 8 && q.tx[n] < 256) q.tx[n] *= 2;
+    const long long per_block = 256 / q.tx[n] * kRepackRows, want = (o.rows + per_block - 1) / per_block;
     blocks[n++] = static_cast<unsigned>(want < 16 * kSms ? want : 16 * kSms);
     return static_cast<const void*>(at);
   };
@@ -278,11 +292,6 @@ void lay_out(const Product& p, const Plan& r, char* w, const void** a, const voi
   *b = add(p.b, r.b, w + r.a_bytes);
   q.blocks0 = blocks[0];
   if (n > 0) repack_kernel<<<blocks[0] + blocks[1], 256, 0, s>>>(q);
-}
-
-template <int CG, int BN>
-int smem_of() {
-  return TcShape<CG, BN>::kSmem;
 }
 
 template <typename T>
@@ -390,7 +399,7 @@ int tc_product(const Product& p, int dtype, void* ws, int* status, unsigned spin
   if (!ok) return PIC_ERR_CUDA;
 
   const void* fn;
-  int slot, smem, threads = kTcThreads;
+  int slot, smem, threads;
   if (r.reg) {
     const RegKernel k = reg_kernel_info();
     fn = k.fn, threads = k.threads, smem = k.smem;
@@ -403,7 +412,8 @@ int tc_product(const Product& p, int dtype, void* ws, int* status, unsigned spin
     fn = dtype == PIC_DTYPE_BF16 ? tc_kernel_bf16(r.bn) : tc_kernel_f16(r.bn);
     const int shape = r.bn == 256 ? 2 : r.bn == 128 ? 1 : 0;
     slot = shape + (dtype == PIC_DTYPE_BF16 ? 3 : 0);
-    smem = shape == 2 ? smem_of<2, 256>() : shape == 1 ? smem_of<1, 128>() : smem_of<1, 64>();
+    smem = shape == 2 ? TcShape<2, 256>::kSmem : shape == 1 ? TcShape<1, 128>::kSmem : TcShape<1, 64>::kSmem;
+    threads = shape == 2 ? TcShape<2, 256>::kThreads : shape == 1 ? TcShape<1, 128>::kThreads : TcShape<1, 64>::kThreads;
   }
   if (allow_smem(fn, slot, smem) != PIC_OK) return PIC_ERR_CUDA;
   long long grid = q.work * r.cg;

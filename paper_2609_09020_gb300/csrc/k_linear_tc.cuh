@@ -7,7 +7,7 @@
 //   warp 0      one thread keeps a ring of STAGES slices of A and B (64 of K)
 //               filled by TMA; what lies outside the matrices reads as zero
 //   warp 1      one thread issues the MMAs, 16 of K each
-//   warps 2..5  the epilogue: accumulators, bias, pre, activation, residual,
+//   the others  the epilogue (8 warps, 4 for 64 columns): accumulators, bias, pre, activation, residual,
 //               rounding, and out through shared memory and TMA stores (or
 //               plain stores where rows do not start on 16-byte boundaries)
 // There are two sets of accumulators, so that a tile's epilogue runs under the
@@ -45,8 +45,6 @@ struct TcParams {
   unsigned spin_limit;
 };
 
-constexpr int kEpiWarps = 4;
-constexpr int kTcThreads = 64 + 32 * kEpiWarps;
 constexpr int kSlice = 64;           // K of one stage
 constexpr int kPanelBytes = 32 * 128;  // 32 rows x 64 columns of a 16-bit type
 constexpr int kGroupRows = 2048;     // rows of A that neighbouring tiles share the columns of B for
@@ -76,8 +74,15 @@ struct TcShape {
   static constexpr int kStageBytes = kABytes + kBBytes;
   // BN = 64: two CTAs on an SM, else one
   static constexpr int kStages = BN == 256 ? 6 : BN == 128 ? 5 : 3;
+  // Epilogue warps: 32 rows and BN, or half of BN, columns each.  With four, a
+  // tile of 128 x 128 that also writes pre took 5 us, longer than its slices up to
+  // K = 1536.
+  static constexpr int kEpi = BN == 64 ? 4 : 8;
+  static constexpr int kThreads = 64 + 32 * kEpi;
+  static constexpr int kColumns = BN == 64 ? 64 : BN / 2;
+  static constexpr int kPanels = BN == 64 ? 2 : 1;  // buffers of a warp
   static constexpr int kOffPanels = kStages * kStageBytes;
-  static constexpr int kOffBars = kOffPanels + kEpiWarps * 2 * kPanelBytes;
+  static constexpr int kOffBars = kOffPanels + kEpi * kPanels * kPanelBytes;
   static constexpr int kBars = 2 * kStages + 4 + 1;
   static constexpr int kSmem = kOffBars + kBars * 8 + 16 + 1024;  // 1024: the base is rounded up
   static constexpr int kTmemCols = 2 * BN;
@@ -370,7 +375,7 @@ __device__ __forceinline__ void finish_item(const Product& p, const JoinItem& m,
 }
 
 template <typename T, int CG, int BN>
-__global__ void __launch_bounds__(kTcThreads, BN == 64 ? 2 : 1)
+__global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
     tc_kernel(const __grid_constant__ TcParams q, const __grid_constant__ TcMaps maps) {
   using S = TcShape<CG, BN>;
   extern __shared__ uint8_t smem_raw[];
@@ -392,7 +397,7 @@ __global__ void __launch_bounds__(kTcThreads, BN == 64 ? 2 : 1)
     }
     for (int b = 0; b < 2; ++b) {
       tc::mbar_init(bar_acc + 8 * b, 1);
-      tc::mbar_init(bar_free + 8 * b, kEpiWarps * CG);
+      tc::mbar_init(bar_free + 8 * b, S::kEpi * CG);
     }
     tc::mbar_init(bar_drain, 1);
     *abort_flag = 0;
@@ -500,7 +505,8 @@ __global__ void __launch_bounds__(kTcThreads, BN == 64 ? 2 : 1)
   } else {
     const int quarter = warp & 3;  // the 32 lanes of tensor memory that this warp may read
     const Product& p = q.p;
-    const uint32_t panels = base + S::kOffPanels + quarter * 2 * kPanelBytes;
+    const int from = (warp - 2) / 4 * S::kColumns, to = from + S::kColumns;  // columns of the tile
+    const uint32_t panels = base + S::kOffPanels + (warp - 2) * S::kPanels * kPanelBytes;
     const uint32_t lead_free = CG == 2 ? tc::map_rank(bar_free, 0) : bar_free;
     int buf = 0, pb = 0;
     uint32_t phase = 0;
@@ -511,10 +517,10 @@ __global__ void __launch_bounds__(kTcThreads, BN == 64 ? 2 : 1)
       if (!__all_sync(0xffffffffu, wait(bar_acc + 8 * buf, phase))) break;
       tc::tc_fence_after();
       const uint32_t d = tmem + buf * BN + (static_cast<uint32_t>(quarter * 32) << 16);
-      for (int c0 = 0; c0 < BN; c0 += 64) {
+      for (int c0 = from; c0 < to; c0 += 64) {
         uint32_t raw_acc[64];
         tc::tmem_ld64_wait(d + c0, raw_acc);
-        if (c0 + 64 == BN) {
+        if (c0 + 64 == to) {
           tc::tc_fence_before();
           __syncwarp();
           if (lane == 0) {
@@ -544,10 +550,10 @@ __global__ void __launch_bounds__(kTcThreads, BN == 64 ? 2 : 1)
         if (p.pre) {
 #pragma unroll
           for (int c = 0; c < 32; ++c) out[c] = pack2_16<T>(v[2 * c], v[2 * c + 1]);
-          if (lane == 0) tc::bulk_wait_read<1>();  // the buffer's last store has been read
+          if (lane == 0) tc::bulk_wait_read<S::kPanels - 1>();  // the buffer's last store has been read
           __syncwarp();
           put_panel<T>(out, panels + pb * kPanelBytes, lane, row0, j0 + c0, p, p.pre, p.ldpre, &maps.pre, q.store_tma);
-          pb ^= 1;
+          if (++pb == S::kPanels) pb = 0;
         }
         if (p.act == PIC_ACT_GELU) {
 #pragma unroll
@@ -560,7 +566,7 @@ __global__ void __launch_bounds__(kTcThreads, BN == 64 ? 2 : 1)
 #pragma unroll
           for (int c = 0; c < 64; ++c) v[c] = relu_nan(v[c]);
         }
-        if (lane == 0) tc::bulk_wait_read<1>();
+        if (lane == 0) tc::bulk_wait_read<S::kPanels - 1>();
         __syncwarp();
         if (p.residual) {
           if (cols == 64 && rows_on16<T>(p.residual, p.ldr, j0 + c0)) {
@@ -572,7 +578,7 @@ __global__ void __launch_bounds__(kTcThreads, BN == 64 ? 2 : 1)
 #pragma unroll
         for (int c = 0; c < 32; ++c) out[c] = pack2_16<T>(v[2 * c], v[2 * c + 1]);
         put_panel<T>(out, panels + pb * kPanelBytes, lane, row0, j0 + c0, p, p.y, p.ldy, &maps.y, q.store_tma);
-        pb ^= 1;
+        if (++pb == S::kPanels) pb = 0;
       }
       if (++buf == 2) buf = 0, phase ^= 1;
     }

@@ -109,6 +109,10 @@ struct Product {
   void* pre;
   long long ldpre;
   int act;
+  // A(i, k) = a(i, k) act'(a_pre(i, k)), where there is an a_pre (few_product only)
+  const void* a_pre;
+  long long a_pre_i;
+  int a_act;
 };
 
 // Launches a kernel in clusters of `cluster` CTAs along x.
@@ -140,6 +144,27 @@ int tc_product(const Product& p, int dtype, void* ws, int* status, unsigned spin
 constexpr int kFewRows = 15;
 bool few_takes(const Product& p);
 int few_product(const Product& p, int dtype, cudaStream_t s);
+
+// The same for fp32 and at most kFewRows32 rows, on the FP32 cores.
+constexpr int kFewRows32 = 8;
+bool few32_takes(const Product& p);
+int few32_product(const Product& p, cudaStream_t s);
+
+// dw = dz^T x and db of at most kFewRows rows, dz = dy act'(z) not rounded before.
+struct OuterGrad {
+  const void* dy;
+  long long lddy;
+  const void* pre;
+  long long ldpre;
+  const void* x;
+  long long ldx;
+  void* dw;  // null: not asked for, as for db
+  long long lddw;
+  void* db;
+  long long I, N, K;
+  int act;
+};
+int outer_grad(const OuterGrad& g, int dtype, cudaStream_t s);
 
 // dz[i][j] = dy act'(z), rounded (dz null: not written), and db[j], the sums of
 // the unrounded dz over the rows (db null: none); parts is workspace.

@@ -93,13 +93,17 @@ int* status_word() {
   return p;
 }
 
-// Workspace bytes of a product, and the product.
-long long product_workspace(const Product& p, int dtype) {
-  return dtype != PIC_DTYPE_F32 && pic::lin::few_takes(p) ? 0 : pic::lin::tc_workspace(p, dtype);
+// Whether the kernels for few rows take a product (they need no workspace), its
+// workspace bytes, and the product.
+bool few(const Product& p, int dtype) {
+  return dtype == PIC_DTYPE_F32 ? pic::lin::few32_takes(p) : pic::lin::few_takes(p);
 }
 
+long long product_workspace(const Product& p, int dtype) { return few(p, dtype) ? 0 : pic::lin::tc_workspace(p, dtype); }
+
 int product(const Product& p, int dtype, void* ws, cudaStream_t s) {
-  if (dtype != PIC_DTYPE_F32 && pic::lin::few_takes(p)) return pic::lin::few_product(p, dtype, s);
+  if (few(p, dtype))
+    return dtype == PIC_DTYPE_F32 ? pic::lin::few32_product(p, s) : pic::lin::few_product(p, dtype, s);
   int* status = status_word();
   if (!status) return PIC_ERR_CUDA;
   return pic::lin::tc_product(p, dtype, ws, status, pic::kWaitPolls, s);
@@ -158,30 +162,48 @@ int backward(const pic_linear_grad_args& a, Arena& ws, bool launch, cudaStream_t
       return status ? pic::lin::narrow_grad(g, a.dtype, w, status, pic::kWaitPolls, s) : PIC_ERR_CUDA;
     }
   }
-  // dz: dy itself where there is no activation
-  const bool products = a.dx || a.dw;
-  const void* dz = a.dy;
-  long long lddz = a.lddy;
-  const bool own_dz = a.act != PIC_ACT_NONE && products;
-  if (own_dz) {
-    lddz = (N + 63) / 64 * 64;  // rows of 16-bit values on 128-byte lines
-    dz = ws.take(M * lddz * static_cast<long long>(elem_bytes(a.dtype)));
-  }
-  GradAct g{a.dy, a.lddy, a.pre, a.ldpre, own_dz ? const_cast<void*>(dz) : nullptr, lddz, a.db, nullptr, M, N, a.act};
-  if (own_dz || a.db) {
-    g.parts = static_cast<float*>(ws.take(pic::lin::grad_act_workspace(g, a.dtype)));
-    if (launch && (rc = pic::lin::grad_act(g, a.dtype, s)) != PIC_OK) return rc;
-  }
-  if (a.dx) {
+  const auto dx_product = [&](const void* dz, long long lddz) {
     Product p{};
     p.a = dz, p.a_i = lddz, p.a_k = 1;
     p.b = a.w, p.b_j = 1, p.b_k = a.ldw;
     p.I = M, p.J = K, p.K = N;
     p.y = a.dx, p.ldy = a.lddx, p.act = PIC_ACT_NONE;
+    return p;
+  };
+  bool dx = a.dx != nullptr, dw = a.dw != nullptr, db = a.db != nullptr;
+  // few rows: dw and db by an outer product, dx from the weights straight, each with dz made on the way
+  if (M <= pic::lin::kFewRows) {
+    if (dw || db) {
+      const pic::lin::OuterGrad g{a.dy, a.lddy, a.pre, a.ldpre, a.x, a.ldx, a.dw, a.lddw, a.db, M, N, K, a.act};
+      if (launch && (rc = pic::lin::outer_grad(g, a.dtype, s)) != PIC_OK) return rc;
+      dw = db = false;
+    }
+    Product p = dx_product(a.dy, a.lddy);
+    if (a.act != PIC_ACT_NONE) p.a_pre = a.pre, p.a_pre_i = a.ldpre, p.a_act = a.act;
+    if (dx && few(p, a.dtype)) {
+      if (launch && (rc = product(p, a.dtype, nullptr, s)) != PIC_OK) return rc;
+      dx = false;
+    }
+  }
+  // dz: dy itself where there is no activation
+  const void* dz = a.dy;
+  long long lddz = a.lddy;
+  const bool own_dz = a.act != PIC_ACT_NONE && (dx || dw);
+  if (own_dz) {
+    lddz = (N + 63) / 64 * 64;  // rows of 16-bit values on 128-byte lines
+    dz = ws.take(M * lddz * static_cast<long long>(elem_bytes(a.dtype)));
+  }
+  if (own_dz || db) {
+    GradAct g{a.dy, a.lddy, a.pre, a.ldpre, own_dz ? const_cast<void*>(dz) : nullptr, lddz, db ? a.db : nullptr, nullptr, M, N, a.act};
+    g.parts = static_cast<float*>(ws.take(pic::lin::grad_act_workspace(g, a.dtype)));
+    if (launch && (rc = pic::lin::grad_act(g, a.dtype, s)) != PIC_OK) return rc;
+  }
+  if (dx) {
+    const Product p = dx_product(dz, lddz);
     void* w = ws.take(product_workspace(p, a.dtype));
     if (launch && (rc = product(p, a.dtype, w, s)) != PIC_OK) return rc;
   }
-  if (a.dw) {
+  if (dw) {
     Product p{};
     p.a = dz, p.a_i = 1, p.a_k = lddz;
     p.b = a.x, p.b_j = 1, p.b_k = a.ldx;

@@ -68,7 +68,7 @@ def test_null_and_small_workspace(pic):
     lib = pic.load_library()
     assert lib.pic_linear_workspace_bytes(None) == -1
     assert lib.pic_linear(None, None, 0, None) == pic.PIC_ERR_INVALID_ARG
-    a = backward_args(pic)
+    a = backward_args(pic, rows=100)  # a few rows need none
     need = lib.pic_linear_backward_workspace_bytes(ctypes.byref(a))
     assert need > 0
     for ws, n in ((P, need - 1), (None, need), (P + 128, need)):
