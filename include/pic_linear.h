@@ -103,6 +103,16 @@ int pic_linear_backward(const pic_linear_grad_args *a, void *workspace, size_t w
  * did (its outputs are unspecified), PIC_ERR_CUDA. */
 int pic_linear_check(void *stream);
 
+/*
+ * Test hook of the bounded device-side waits, as pic_decode_test_wait_fault:
+ * while withhold_arrival = 1, one warp of the first tile of every tensor-memory
+ * kernel skips one mbarrier arrival, so that a later wait of that CTA runs out
+ * (after spin_limit polls, where that is not 0) and the kernel takes its abort
+ * path.  pic_linear_test_wait_fault(0, 0) restores production behaviour.
+ * Errors: PIC_ERR_INVALID_ARG (withhold_arrival not 0 or 1).
+ */
+int pic_linear_test_wait_fault(int withhold_arrival, unsigned spin_limit);
+
 #ifdef __cplusplus
 }
 #endif

@@ -79,12 +79,10 @@ __device__ __forceinline__ uint4 load8(const T* p, int n) {
                  : "l"(p));
     return q;
   }
-  uint32_t w[4] = {};
-  const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+  uint32_t e[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (i < n) w[i / 2] |= static_cast<uint32_t>(__ldg(h + i)) << (16 * (i & 1));
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  for (int i = 0; i < 8; ++i) e[i] = load_if(reinterpret_cast<const uint16_t*>(p) + i, i < n);
+  return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
 }
 
 // Eight elements of a row of A, or of dz = dy act'(z) rounded to its type.

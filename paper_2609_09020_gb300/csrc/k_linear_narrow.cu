@@ -44,8 +44,7 @@ struct NarrowParams {
   long long tiles;
   int vec_dy, vec_z, vec_x, store_tma;
   float* parts;  // [CTAs][N K + N]
-  int* status;
-  unsigned spin_limit;
+  Waits waits;
 };
 
 // T: element; WIDE: up to 128 columns (16-bit types), else 64; TMA: dy, z and x come by TMA.
@@ -87,17 +86,15 @@ struct Vec16 {
       w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
       return;
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = 0;
-    if (n <= 0) return;
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (i < n) w[i] = __ldg(reinterpret_cast<const uint32_t*>(p) + i);
+      for (int i = 0; i < 4; ++i) w[i] = load_if(reinterpret_cast<const uint32_t*>(p) + i, i < n);
     } else {
+      uint32_t e[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < n) w[i / 2] |= static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t*>(p) + i)) << (16 * (i & 1));
+      for (int i = 0; i < 8; ++i) e[i] = load_if(reinterpret_cast<const uint16_t*>(p) + i, i < n);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = e[2 * i] | e[2 * i + 1] << 16;
     }
   }
   __device__ __forceinline__ void widen(float (&f)[kPer]) const {
@@ -233,8 +230,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   tc::tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  auto wait = [&](uint32_t bar, uint32_t parity) { return wait_bounded(bar, parity, abort_flag, q.status, q.spin_limit); };
+  auto wait = [&](uint32_t bar, uint32_t parity) { return wait_bounded(bar, parity, abort_flag, q.waits); };
   float* my_parts = q.parts + blockIdx.x * static_cast<long long>(g.N * g.K + g.N);
+
+  const bool elected = (warp == kMmaWarp || warp == kTmaWarp) && tc::elect_one();
+  // the TMA thread's place in the ring of stages
+  int ring_s = 0;
+  uint32_t ring_phase = 0;
 
   if (warp >= kLoadWarp) {
     const int tid = threadIdx.x - 32 * kLoadWarp;
@@ -366,7 +368,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
   } else if (warp == kMmaWarp) {
-    if (tc::elect_one()) {
+    if (elected) {
       const int k_pad = (g.K + 15) / 16 * 16, n_steps = (g.N + 15) / 16;
       const uint32_t idesc_dx = idesc_of<T>(128, k_pad, false, true), idesc_dw = idesc_of<T>(128, k_pad, true, true);
       // of a dz of one block the MMA's rows 64..127 are rows 0..63 again, not looked at
@@ -415,38 +417,23 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (++s == S::kStages) s = 0, phase ^= 1;
         if (++buf == 2) buf = 0, free_phase ^= 1;
       }
-      if (!ok) {  // aborted: MMAs in flight still read shared memory
-        tc::mma_commit(bar_drain);
-        for (uint32_t i = 0; i < q.spin_limit && !tc::mbar_try_wait(bar_drain, 0); ++i) {
-        }
-      } else if (S::kPlanes == 1 && g.dw) {
-        tc::mma_commit(bar_dw);
-      }
+      if (ok && S::kPlanes == 1 && g.dw) tc::mma_commit(bar_dw);
     }
     __syncwarp();
   } else if (TMA && warp == kTmaWarp) {
-    if (tc::elect_one()) {
+    if (elected) {
       const bool has_z = g.act != PIC_ACT_NONE;
       const uint32_t bytes = S::kPlaneBytes * (1 + (g.dw ? 1 : 0) + (has_z ? 1 : 0));
-      int s = 0;
-      uint32_t phase = 0;
-      bool ok = true;
       for (long long tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
-        if (!(ok = wait(bar_empty + 8 * s, phase ^ 1))) break;
-        const uint32_t at = base + s * S::kStageBytes, bar = bar_landed + 8 * s;
+        if (!wait(bar_empty + 8 * ring_s, ring_phase ^ 1)) break;
+        const uint32_t at = base + ring_s * S::kStageBytes, bar = bar_landed + 8 * ring_s;
         const int i = static_cast<int>(tile * kTile);
         tc::mbar_arrive_expect_tx(bar, bytes);
         tc::tma_load_2d<false>(at, &maps.dy, 0, i, bar);
         if (has_z) tc::tma_load_2d<false>(at + 2 * S::kPlaneBytes, &maps.z, 0, i, bar);
         if (g.dw) tc::tma_load_2d<false>(at + S::kPlaneBytes, &maps.x, 0, i, bar);
-        if (++s == S::kStages) s = 0, phase ^= 1;
+        if (++ring_s == S::kStages) ring_s = 0, ring_phase ^= 1;
       }
-      if (!ok)  // aborted: the copies in flight land before shared memory goes away
-        for (int i = 0; i < S::kStages; ++i) {
-          if (--s < 0) s = S::kStages - 1, phase ^= 1;
-          for (uint32_t n = 0; n < q.spin_limit && !tc::mbar_try_wait(bar_landed + 8 * s, phase); ++n) {
-          }
-        }
     }
     __syncwarp();
   } else if (warp < 4) {
@@ -469,7 +456,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (b + 1 == S::kBlocks) {
           tc::tc_fence_before();
           __syncwarp();
-          if (lane == 0) tc::mbar_arrive(bar_dx_free + 8 * buf);
+          if (lane == 0 && !(q.waits.test_fault && tile == 0 && warp == 0)) tc::mbar_arrive(bar_dx_free + 8 * buf);
         }
         if (64 * b >= g.K || row0 >= g.I) continue;
         if constexpr (sizeof(T) == 4) {
@@ -553,6 +540,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   tc::tc_fence_before();
   __syncthreads();
+  if (*abort_flag) {  // copies and MMAs in flight use shared and tensor memory
+    if (TMA && elected && warp == kTmaWarp) drain_loads(bar_landed, S::kStages, ring_s, ring_phase, q.waits);
+    if (elected && warp == kMmaWarp) drain_mmas<1>(bar_drain, q.waits);
+    __syncthreads();
+  }
   tc::tc_fence_after();
   if (warp == kMmaWarp) tc::tmem_dealloc_cg<1>(tmem, S::kTmemCols);
 }
@@ -613,7 +605,7 @@ bool narrow_takes(const NarrowGrad& g, int dtype) {
 
 long long narrow_workspace(const NarrowGrad& g) { return ctas(g) * static_cast<long long>(g.N * g.K + g.N) * 4; }
 
-int narrow_grad(const NarrowGrad& g, int dtype, void* ws, int* status, unsigned spin_limit, cudaStream_t s) {
+int narrow_grad(const NarrowGrad& g, int dtype, void* ws, const Waits& waits, cudaStream_t s) {
   NarrowParams q{};
   const int elem = dtype == PIC_DTYPE_F32 ? 4 : 2;
   const auto on16 = [&](const void* m, long long ld) { return reinterpret_cast<uintptr_t>(m) % 16 == 0 && ld * elem % 16 == 0; };
@@ -622,8 +614,7 @@ int narrow_grad(const NarrowGrad& g, int dtype, void* ws, int* status, unsigned 
   q.vec_dy = on16(g.dy, g.lddy), q.vec_z = on16(g.pre, g.ldpre), q.vec_x = on16(g.x, g.ldx);
   q.store_tma = g.dx && g.K * elem % 16 == 0 && on16(g.dx, g.lddx) && g.lddx * elem < (1LL << 40);
   q.parts = static_cast<float*>(ws);
-  q.status = status;
-  q.spin_limit = spin_limit;
+  q.waits = waits;
   NarrowMaps maps{};
   const auto far = [&](long long ld) { return ld * elem >= (1LL << 40); };
   if (q.store_tma && !encode(&maps.dx, g.dx, g.I, g.K, g.lddx, 32, dtype)) return PIC_ERR_CUDA;

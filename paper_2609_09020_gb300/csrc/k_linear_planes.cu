@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc::tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   const Product& p = q.p;
-  auto wait = [&](uint32_t bar, uint32_t parity) { return wait_bounded(bar, parity, abort_flag, q.status, q.spin_limit); };
+  auto wait = [&](uint32_t bar, uint32_t parity) { return wait_bounded(bar, parity, abort_flag, q.waits); };
   const long long first = blockIdx.x / 2, step = gridDim.x / 2;
   auto part = [&](long long w, int& k0, int& k1) {
     k0 = static_cast<int>(w % q.splits) * q.part_blocks;
@@ -133,12 +133,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   // each block of 64 rows has its three planes of 8 KB
   const int a_plane = q.a_mn ? 8192 : kABytes, b_plane = q.b_mn ? 8192 : kBBytes;
 
+  // the TMA or MMA thread, and its place in the ring of stages
+  const bool elected = warp < 2 && tc::elect_one();
+  int s = 0;
+  uint32_t phase = 0;
+  bool ok = true;
   if (warp == 0) {
-    if (tc::elect_one()) {
+    if (elected) {
       const uint32_t lead_full = tc::map_rank(bar_full, 0);
-      int s = 0;
-      uint32_t phase = 0;
-      bool ok = true;
       for (long long w = first; w < q.work && ok; w += step) {
         long long ti, tj;
         tile_place<kPlRows>(w / q.splits, q.tiles_i, q.tiles_j, ti, tj);
@@ -163,24 +165,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (++s == kStages) s = 0, phase ^= 1;
         }
       }
-      // aborted: as in k_linear_tc.cuh, the copies in flight land first
-      if (!ok) {
-        for (int i = 0; i < kStages; ++i) {
-          if (--s < 0) s = kStages - 1, phase ^= 1;
-          for (uint32_t n = 0; rank == 0 && n < q.spin_limit && !tc::mbar_try_wait(bar_full + 8 * s, phase); ++n) {
-          }
-        }
-        __nanosleep(200000);
-      }
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (rank == 0 && tc::elect_one()) {
+    if (rank == 0 && elected) {
       const uint32_t idesc = tc::idesc_16(256, kPlCols, true, q.a_mn != 0, q.b_mn != 0);
       const uint32_t a_step = q.a_mn ? 2048 : 32, b_step = q.b_mn ? 2048 : 32;
-      int s = 0, buf = 0;
-      uint32_t phase = 0, free_phase = 0;
-      bool ok = true;
+      int buf = 0;
+      uint32_t free_phase = 0;
       for (long long w = first; w < q.work && ok; w += step) {
         int k0, k1;
         part(w, k0, k1);
@@ -208,11 +200,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (++buf == 2) buf = 0, free_phase ^= 1;
         }
       }
-      if (!ok) {  // aborted: MMAs in flight still read shared memory
-        tc::mma_commit_cg<2>(bar_drain);
-        for (uint32_t i = 0; i < q.spin_limit && !tc::mbar_try_wait(bar_drain, 0); ++i) {
-        }
-      }
     }
     __syncwarp();
   } else {
@@ -221,8 +208,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t lead_free = tc::map_rank(bar_free, 0);
     const long long a_groups = (p.I + 127) / 128, b_groups = (p.J + 127) / 128;
     int buf = 0;
-    uint32_t phase = 0;
-    bool ok = true;
     for (long long w = first; w < q.work && ok; w += step) {
       long long ti, tj;
       tile_place<kPlRows>(w / q.splits, q.tiles_i, q.tiles_j, ti, tj);
@@ -245,7 +230,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         tc::tc_fence_before();
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive_cluster(lead_free + 8 * buf);
+        if (lane == 0 && !(q.waits.test_fault && w == 0 && rank == 0 && warp == 2)) tc::mbar_arrive_cluster(lead_free + 8 * buf);
         if (++buf == 2) buf = 0, phase ^= 1;
       }
       if (!ok) break;
@@ -270,6 +255,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   tc::tc_fence_before();
   __syncthreads();
+  if (*abort_flag) {  // as in k_linear_tc.cuh
+    if (elected && warp == 0 && rank == 0) drain_loads(bar_full, kStages, s, phase, q.waits);
+    if (elected && warp == 1 && rank == 0) drain_mmas<2>(bar_drain, q.waits);
+    __nanosleep(200000);
+    __syncthreads();
+  }
   tc::cluster_sync();
   tc::tc_fence_after();
   if (warp == 1) tc::tmem_dealloc_cg<2>(tmem, kTmemCols);

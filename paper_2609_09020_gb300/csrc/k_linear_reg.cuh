@@ -6,7 +6,7 @@
 namespace pic {
 namespace lin {
 
-constexpr int kRegTile = 128;
+constexpr int kRegRows = 128, kRegCols = 64;  // a tile
 
 // Operands as the loaders read them, beside the launch's TcParams.
 struct RegOperands {

@@ -46,20 +46,21 @@ __global__ void __launch_bounds__(256) repack_kernel(const Repack q) {
         const long long r = r0 + u * ty + y;
         const uint16_t* p = q.src[m] + r * ld + c;
         odd[u] = (reinterpret_cast<uintptr_t>(p) & 2) != 0;
-#pragma unroll
-        for (int i = 0; i < 5; ++i) h[u][i] = 0;
-        if (r >= rows) continue;
         // the words' last half belongs to the element after the eight
-        if (c + 8 + (odd[u] && r + 1 == rows ? 1 : 0) <= cols) {
+        const bool words = r < rows && c + 8 + (odd[u] && r + 1 == rows ? 1 : 0) <= cols;
+        if (words || r >= rows) {
           const uint32_t* v = reinterpret_cast<const uint32_t*>(p - (odd[u] ? 1 : 0));
 #pragma unroll
-          for (int i = 0; i < 4; ++i) h[u][i] = __ldg(v + i);
-          if (odd[u]) h[u][4] = __ldg(v + 4);
+          for (int i = 0; i < 4; ++i) h[u][i] = load_if(v + i, words);
+          h[u][4] = load_if(v + 4, words && odd[u]);
         } else {
           odd[u] = false;
+          uint32_t e[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (c + i < cols) h[u][i / 2] |= static_cast<uint32_t>(__ldg(p + i)) << (16 * (i & 1));
+          for (int i = 0; i < 8; ++i) e[i] = load_if(p + i, c + i < cols);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) h[u][i] = e[2 * i] | e[2 * i + 1] << 16;
+          h[u][4] = 0;
         }
       }
 #pragma unroll
@@ -179,7 +180,7 @@ struct ShapeCost {
 constexpr ShapeCost kShape64{64, 1, 2 * kSms, 4.2, 0.20, 3.0};
 constexpr ShapeCost kShape128{128, 1, kSms, 4.5, 0.19, 2.2};
 constexpr ShapeCost kShape256{256, 2, kSms / 2, 6.8, 0.26, 3.4};
-constexpr ShapeCost kShapeReg{kRegTile, 1, kSms, 6.0, 3.0, 3.0};
+constexpr ShapeCost kShapeReg{kRegCols, 1, kSms, 6.0, 1.9, 2.0};
 constexpr ShapeCost kShapePlanes{kPlCols, 2, kSms / 2, 8.0, 0.85, 3.4};
 
 // The shape and the number of parts of K with the least estimated time, parts at
@@ -202,7 +203,7 @@ void choose(Plan& r, const Product& p, const ShapeCost* shapes, int n_shapes, in
       const int part = (r.k_blocks + want - 1) / want;
       const int splits = (r.k_blocks + part - 1) / part;
       const long long work = tiles * splits, rounds = (work + h.slots - 1) / h.slots;
-      const bool shared = h.bn == 64 && work > kSms;  // two CTAs on an SM
+      const bool shared = h.slots > kSms && work > kSms;  // two CTAs on an SM
       const double each = part * slice * (shared ? 1.5 : 1.0);
       double t = h.fixed + (rounds > 1 && each < h.tile ? rounds * h.tile : rounds * each);
       if (splits > 1) t += 2.0 + 4.0 * rows * h.bn * static_cast<double>(work) / 2.6e6;
@@ -346,7 +347,7 @@ long long tc_workspace(const Product& p, int dtype) {
   return r.a_bytes + r.b_bytes + r.part_bytes;
 }
 
-int tc_product(const Product& p, int dtype, void* ws, int* status, unsigned spin_limit, cudaStream_t s) {
+int tc_product(const Product& p, int dtype, void* ws, const Waits& waits, cudaStream_t s) {
   const Plan r = plan(p, dtype);
   const long long elem = dtype == PIC_DTYPE_F32 ? 4 : 2;
   char* w = static_cast<char*>(ws);
@@ -363,8 +364,7 @@ int tc_product(const Product& p, int dtype, void* ws, int* status, unsigned spin
   q.work = r.tiles_i * r.tiles_j * r.splits;
   q.a_mn = r.a.mn, q.b_mn = r.b.mn;
   q.parts = r.splits > 1 ? reinterpret_cast<float*>(w + r.a_bytes + r.b_bytes) : nullptr;
-  q.status = status;
-  q.spin_limit = spin_limit;
+  q.waits = waits;
   const auto fits = [&](const void* m, long long ld, long long rows) {
     return reinterpret_cast<uintptr_t>(m) % 16 == 0 && ((ld * elem % 16 == 0 && ld * elem < (1LL << 40)) || rows == 1);
   };
@@ -417,7 +417,7 @@ int tc_product(const Product& p, int dtype, void* ws, int* status, unsigned spin
   }
   if (allow_smem(fn, slot, smem) != PIC_OK) return PIC_ERR_CUDA;
   long long grid = q.work * r.cg;
-  const long long most = r.bn == 64 ? 2 * kSms : kSms;
+  const long long most = r.bn == 64 && !r.reg ? 2 * kSms : kSms;
   if (grid > most) grid = most;
   void* args[] = {&q, &maps, r.planes ? static_cast<void*>(&pl) : &o};  // 16-bit kernels take the first two
   if (launch_kernel(fn, grid, threads, smem, r.cg, args, s) != PIC_OK) return PIC_ERR_CUDA;

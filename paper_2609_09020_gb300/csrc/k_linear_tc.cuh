@@ -41,20 +41,18 @@ struct TcParams {
   int a_mn, b_mn;        // the operand is contiguous along its rows
   int store_tma;         // y (and pre) go out by TMA
   float* parts;          // fp32 parts, or null: the epilogue runs in the kernel
-  int* status;
-  unsigned spin_limit;
+  Waits waits;
 };
 
 constexpr int kSlice = 64;           // K of one stage
 constexpr int kPanelBytes = 32 * 128;  // 32 rows x 64 columns of a 16-bit type
 constexpr int kGroupRows = 2048;     // rows of A that neighbouring tiles share the columns of B for
 
-// At most `limit` polls; false (with the flags raised) if the phase does not
+// At most limit polls; false (with the flags raised) if the phase does not
 // complete in time or another thread has given up.
-__device__ __forceinline__ bool wait_bounded(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status,
-                                             unsigned limit) {
+__device__ __forceinline__ bool wait_bounded(uint32_t bar, uint32_t parity, volatile int* abort_flag, const Waits& w) {
   if (tc::mbar_test_wait(bar, parity)) return true;
-  for (uint32_t i = 0; i < limit; ++i) {
+  for (uint32_t i = 0; i < w.spin_limit; ++i) {
     if (tc::mbar_try_wait(bar, parity)) return true;
     if ((i & 63u) == 63u) {
       if (*abort_flag) return false;
@@ -62,8 +60,25 @@ __device__ __forceinline__ bool wait_bounded(uint32_t bar, uint32_t parity, vola
     }
   }
   *abort_flag = 1;
-  atomicOr(status, 1);
+  atomicOr(w.status, 1);
   return false;
+}
+// After an abort: until what this CTA has started completes, for as long as a wait
+// at most.  The MMAs that the calling thread has issued:
+template <int CG>
+__device__ __forceinline__ void drain_mmas(uint32_t bar_drain, const Waits& w) {
+  tc::mma_commit_cg<CG>(bar_drain);
+  for (uint32_t i = 0; i < w.spin_limit && !tc::mbar_try_wait(bar_drain, 0); ++i) {
+  }
+}
+// TMA loads: the last of a ring of `stages`, the next of which would go to stage s
+// in phase `phase` (a stage that was never filled is passed at once).
+__device__ __forceinline__ void drain_loads(uint32_t bar_full, int stages, int s, uint32_t phase, const Waits& w) {
+  for (int k = 0; k < stages; ++k) {
+    if (--s < 0) s = stages - 1, phase ^= 1;
+    for (uint32_t i = 0; i < w.spin_limit && !tc::mbar_try_wait(bar_full + 8 * s, phase); ++i) {
+    }
+  }
 }
 
 template <int CG, int BN>
@@ -155,6 +170,13 @@ __device__ __forceinline__ bool rows_on16(const void* m, long long ld, long long
   return ((reinterpret_cast<uintptr_t>(m) + col0 * sizeof(T)) | static_cast<uintptr_t>(ld * sizeof(T))) % 16 == 0;
 }
 
+// Whether 32 rows of a matrix from a multiple of 32 on are one run of memory on a
+// 16-byte boundary: narrow rows without gaps, whatever their width.
+template <typename T>
+__device__ __forceinline__ bool packed_rows(const void* m, long long ld, const Product& p) {
+  return ld == p.J && p.J <= 128 / static_cast<int>(sizeof(T)) && reinterpret_cast<uintptr_t>(m) % 16 == 0;
+}
+
 // One warp's panel (32 rows from row0, 128 bytes of columns from col0; this
 // lane's row in v) to global memory: into the panel buffer, swizzled as TMA and
 // the banks like it, then one TMA store, or one word of a row per lane and row.
@@ -162,6 +184,30 @@ template <typename T>
 __device__ __forceinline__ void put_panel(const uint32_t (&v)[32], uint32_t buf, int lane, long long row0, long long col0,
                                           const Product& p, void* out, long long ld, const CUtensorMap* map,
                                           bool by_tma) {
+  if (!by_tma && row0 + 32 <= p.I && packed_rows<T>(out, ld, p)) {
+    // as the rows lie in memory, and out in one copy
+    const int n = static_cast<int>(p.J);
+    const uint32_t row = buf + lane * n * sizeof(T);
+    if (sizeof(T) == 4 || n % 2 == 0) {
+#pragma unroll
+      for (int c = 0; c < 32; ++c)
+        if (c * static_cast<int>(4 / sizeof(T)) < n) asm volatile("st.shared.b32 [%0], %1;" ::"r"(row + 4 * c), "r"(v[c]) : "memory");
+    } else {
+#pragma unroll
+      for (int c = 0; c < 32; ++c) {
+        if (2 * c < n) asm volatile("st.shared.u16 [%0], %1;" ::"r"(row + 4 * c), "h"(static_cast<uint16_t>(v[c])) : "memory");
+        if (2 * c + 1 < n)
+          asm volatile("st.shared.u16 [%0], %1;" ::"r"(row + 4 * c + 2), "h"(static_cast<uint16_t>(v[c] >> 16)) : "memory");
+      }
+    }
+    tc::fence_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      tc::bulk_store(static_cast<T*>(out) + row0 * n, buf, 32 * n * sizeof(T));
+      tc::bulk_commit();
+    }
+    return;
+  }
 #pragma unroll
   for (int c = 0; c < 8; ++c)
     tc::sts128(buf + lane * 128 + ((c ^ (lane & 7)) * 16), v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
@@ -178,7 +224,7 @@ __device__ __forceinline__ void put_panel(const uint32_t (&v)[32], uint32_t buf,
   const int n = static_cast<int>(min(static_cast<long long>(128 / sizeof(T)), p.J - col0));  // columns that exist
   const int rows = static_cast<int>(min(32LL, p.I - row0));
   T* o = static_cast<T*>(out) + row0 * ld + col0;
-#pragma unroll 4
+#pragma unroll 8
   for (int r = 0; r < rows; ++r, o += ld) {
     const uint32_t w = panel_word(buf, r, lane);
     if constexpr (sizeof(T) == 4) {
@@ -203,50 +249,109 @@ __device__ __forceinline__ void put_panel(const uint32_t (&v)[32], uint32_t buf,
     }
   }
   __syncwarp();
+  if (lane == 0) tc::bulk_commit();  // an empty group: every panel has one, so that waits can count them
 }
 
-// The other way round: adds 128 bytes of columns from col0 of 32 rows of a matrix
-// whose rows lanes cannot read 16 bytes at a time, each lane its row's to v.
-template <typename T, int N>
-__device__ __forceinline__ void add_panel(float* v, uint32_t buf, int lane, long long row0, long long col0, const Product& p,
-                                          const void* m, long long ld) {
-  const int n = static_cast<int>(min(static_cast<long long>(N), p.J - col0));
-  const int rows = static_cast<int>(min(32LL, p.I - row0));
-  const T* o = static_cast<const T*>(m) + row0 * ld + col0;
-  __syncwarp();
-#pragma unroll 8
-  for (int r = 0; r < rows; ++r, o += ld) {
-    uint32_t w = 0;
-    if constexpr (sizeof(T) == 4) {
-      if (lane < n) w = reinterpret_cast<const uint32_t*>(o)[lane];
+// 128 bytes of columns of a warp's 32 rows of a residual, loaded before they are
+// wanted: where rows lie on 16-byte boundaries each lane has its own row's; where
+// the rows are one run of memory, 16 bytes here and there of it; else word `lane`
+// of every row.
+template <typename T>
+struct Residual {
+  static constexpr int kCols = 128 / sizeof(T);
+  uint32_t w[32];
+  int mode;  // 0: this lane's row, 1: a run, 2: a word of every row
+  int n;     // columns that exist
+
+  __device__ __forceinline__ void load(const Product& p, long long row0, long long col0, int lane) {
+    n = static_cast<int>(min(static_cast<long long>(kCols), p.J - col0));
+    const int rows = static_cast<int>(min(32LL, p.I - row0));
+    const T* o = static_cast<const T*>(p.residual) + row0 * p.ldr + col0;
+    mode = n == kCols && rows_on16<T>(p.residual, p.ldr, col0) ? 0 : rows == 32 && packed_rows<T>(p.residual, p.ldr, p) ? 1 : 2;
+    if (mode == 0) {
+      const uint4* v = reinterpret_cast<const uint4*>(o + lane * p.ldr);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const uint4 q = lane < rows ? v[c] : make_uint4(0, 0, 0, 0);
+        w[4 * c] = q.x, w[4 * c + 1] = q.y, w[4 * c + 2] = q.z, w[4 * c + 3] = q.w;
+      }
+    } else if (mode == 1) {
+      const uint4* v = reinterpret_cast<const uint4*>(o);
+      const int count = 32 * n * static_cast<int>(sizeof(T)) / 16;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const uint4 q = c * 32 + lane < count ? v[c * 32 + lane] : make_uint4(0, 0, 0, 0);
+        w[4 * c] = q.x, w[4 * c + 1] = q.y, w[4 * c + 2] = q.z, w[4 * c + 3] = q.w;
+      }
     } else {
-      const uint16_t* h = reinterpret_cast<const uint16_t*>(o) + 2 * lane;
-      if (2 * lane < n) w = h[0];
-      if (2 * lane + 1 < n) w |= static_cast<uint32_t>(h[1]) << 16;
-    }
-    asm volatile("st.shared.b32 [%0], %1;" ::"r"(panel_at(buf, r, lane)), "r"(w) : "memory");
-  }
-  __syncwarp();
-#pragma unroll
-  for (int c = 0; c < 8; ++c) {
-    uint32_t w[4];
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                 : "r"(buf + lane * 128 + ((c ^ (lane & 7)) * 16))
-                 : "memory");
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
       if constexpr (sizeof(T) == 4) {
-        v[4 * c + e] += __uint_as_float(w[e]);
+#pragma unroll
+        for (int r = 0; r < 32; ++r, o += p.ldr)
+          w[r] = load_if(reinterpret_cast<const uint32_t*>(o) + lane, r < rows && lane < n);
       } else {
-        const float2 f = unpack2_16<T>(w[e]);
-        v[8 * c + 2 * e] += f.x;
-        v[8 * c + 2 * e + 1] += f.y;
+        uint32_t high[32];
+#pragma unroll
+        for (int r = 0; r < 32; ++r, o += p.ldr) {
+          const uint16_t* h = reinterpret_cast<const uint16_t*>(o) + 2 * lane;
+          w[r] = load_if(h, r < rows && 2 * lane < n);
+          high[r] = load_if(h + 1, r < rows && 2 * lane + 1 < n);
+        }
+#pragma unroll
+        for (int r = 0; r < 32; ++r) w[r] |= high[r] << 16;
       }
     }
   }
-  __syncwarp();
-}
+  // adds this lane's row to v, through the panel buffer where it has to be turned
+  __device__ __forceinline__ void add(float* v, uint32_t buf, int lane) {
+    if (mode == 1) {
+      __syncwarp();
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        tc::sts128(buf + (c * 32 + lane) * 16, w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+      __syncwarp();
+      const uint32_t row = buf + lane * n * sizeof(T);
+      if (sizeof(T) == 4 || n % 2 == 0) {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+          w[c] = 0;
+          if (c * static_cast<int>(4 / sizeof(T)) < n) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[c]) : "r"(row + 4 * c) : "memory");
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+          uint16_t lo = 0, hi = 0;
+          if (2 * c < n) asm volatile("ld.shared.u16 %0, [%1];" : "=h"(lo) : "r"(row + 4 * c) : "memory");
+          if (2 * c + 1 < n) asm volatile("ld.shared.u16 %0, [%1];" : "=h"(hi) : "r"(row + 4 * c + 2) : "memory");
+          w[c] = lo | static_cast<uint32_t>(hi) << 16;
+        }
+      }
+      __syncwarp();
+    } else if (mode == 2) {
+      __syncwarp();
+#pragma unroll
+      for (int r = 0; r < 32; ++r)
+        asm volatile("st.shared.b32 [%0], %1;" ::"r"(panel_at(buf, r, lane)), "r"(w[r]) : "memory");
+      __syncwarp();
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(w[4 * c]), "=r"(w[4 * c + 1]), "=r"(w[4 * c + 2]), "=r"(w[4 * c + 3])
+                     : "r"(buf + lane * 128 + ((c ^ (lane & 7)) * 16))
+                     : "memory");
+      __syncwarp();
+    }
+#pragma unroll
+    for (int c = 0; c < 32; ++c) {
+      if constexpr (sizeof(T) == 4) {
+        v[c] += __uint_as_float(w[c]);
+      } else {
+        const float2 f = unpack2_16<T>(w[c]);
+        v[2 * c] += f.x;
+        v[2 * c + 1] += f.y;
+      }
+    }
+  }
+};
 
 // Adds 64 columns (or those of them that exist) of the bias or of a residual row to v.
 template <typename T, int N = 64>
@@ -299,12 +404,13 @@ __device__ __forceinline__ void finish_rows(float (&v)[64], const Product& p, co
     for (int c = 0; c < 64; ++c) v[c] = act_value<true>(v[c], p.act);
   }
   if (p.residual) {
-    if (cols == 64 && rows_on16<float>(p.residual, p.ldr, col0)) {
-      if (row0 + lane < p.I) add_row<float>(v, static_cast<const float*>(p.residual) + (row0 + lane) * p.ldr + col0, 64);
-    } else {
-      if (lane == 0) tc::bulk_wait_read<0>();
-      add_panel<float, 32>(v, panel, lane, row0, col0, p, p.residual, p.ldr);
-      if (cols > 32) add_panel<float, 32>(v + 32, panel, lane, row0, col0 + 32, p, p.residual, p.ldr);
+    if (lane == 0) tc::bulk_wait_read<0>();
+    Residual<float> res;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (32 * h >= cols) break;
+      res.load(p, row0, col0 + 32 * h, lane);
+      res.add(v + 32 * h, panel, lane);
     }
   }
   put(p.y, p.ldy, &maps.y);
@@ -410,7 +516,7 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
   tc::tc_fence_after();
   const uint32_t tmem = *tmem_slot;
 
-  auto wait = [&](uint32_t bar, uint32_t parity) { return wait_bounded(bar, parity, abort_flag, q.status, q.spin_limit); };
+  auto wait = [&](uint32_t bar, uint32_t parity) { return wait_bounded(bar, parity, abort_flag, q.waits); };
   const long long first = blockIdx.x / CG, step = gridDim.x / CG;
   // slices of work item w
   auto part = [&](long long w, int& k0, int& k1) {
@@ -418,12 +524,14 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
     k1 = min(q.k_blocks, k0 + q.part_blocks);
   };
 
+  // the TMA or MMA thread, and its place in the ring of stages
+  const bool elected = warp < 2 && tc::elect_one();
+  int s = 0;
+  uint32_t phase = 0;
+  bool ok = true;
   if (warp == 0) {
-    if (tc::elect_one()) {
+    if (elected) {
       const uint32_t lead_full = CG == 2 ? tc::map_rank(bar_full, 0) : bar_full;
-      int s = 0;
-      uint32_t phase = 0;
-      bool ok = true;
       for (long long w = first; w < q.work && ok; w += step) {
         long long ti, tj;
         tile_place<S::kRows>(w / q.splits, q.tiles_i, q.tiles_j, ti, tj);
@@ -451,29 +559,16 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
           if (++s == S::kStages) s = 0, phase ^= 1;
         }
       }
-      // aborted: the copies in flight land before shared memory goes away (a
-      // slot that was never filled is passed at once).  The other CTA of a pair
-      // may have started some that this one did not expect: both linger for
-      // far longer than a copy takes.
-      if (!ok) {
-        for (int i = 0; i < S::kStages; ++i) {
-          if (--s < 0) s = S::kStages - 1, phase ^= 1;
-          for (uint32_t n = 0; rank == 0 && n < q.spin_limit && !tc::mbar_try_wait(bar_full + 8 * s, phase); ++n) {
-          }
-        }
-        if (CG == 2) __nanosleep(200000);
-      }
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (rank == 0 && tc::elect_one()) {
+    if (rank == 0 && elected) {
       constexpr uint32_t kM = 128 * CG;
       const uint32_t idesc = idesc_of<T>(kM, BN, q.a_mn != 0, q.b_mn != 0);
       // one MMA takes 16 of K: 32 bytes of a K-major row, 16 rows of an MN-major block
       const uint32_t a_step = q.a_mn ? 2048 : 32, b_step = q.b_mn ? 2048 : 32;
-      int s = 0, buf = 0;
-      uint32_t phase = 0, free_phase = 0;
-      bool ok = true;
+      int buf = 0;
+      uint32_t free_phase = 0;
       for (long long w = first; w < q.work && ok; w += step) {
         if (!(ok = wait(bar_free + 8 * buf, free_phase ^ 1))) break;
         tc::tc_fence_after();
@@ -495,11 +590,6 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
         tc::mma_commit_cg<CG>(bar_acc + 8 * buf);
         if (++buf == 2) buf = 0, free_phase ^= 1;
       }
-      if (!ok) {  // aborted: MMAs in flight still read shared memory
-        tc::mma_commit_cg<CG>(bar_drain);
-        for (uint32_t n = 0; n < q.spin_limit && !tc::mbar_try_wait(bar_drain, 0); ++n) {
-        }
-      }
     }
     __syncwarp();
   } else {
@@ -509,11 +599,13 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
     const uint32_t panels = base + S::kOffPanels + (warp - 2) * S::kPanels * kPanelBytes;
     const uint32_t lead_free = CG == 2 ? tc::map_rank(bar_free, 0) : bar_free;
     int buf = 0, pb = 0;
-    uint32_t phase = 0;
     for (long long w = first; w < q.work; w += step) {
       long long ti, tj;
       tile_place<S::kRows>(w / q.splits, q.tiles_i, q.tiles_j, ti, tj);
       const long long row0 = ti * S::kRows + rank * 128 + quarter * 32, j0 = tj * BN;
+      Residual<T> res;
+      const bool add_res = p.residual && !q.parts;
+      if (add_res && row0 < p.I && j0 + from < p.J) res.load(p, row0, j0 + from, lane);
       if (!__all_sync(0xffffffffu, wait(bar_acc + 8 * buf, phase))) break;
       tc::tc_fence_after();
       const uint32_t d = tmem + buf * BN + (static_cast<uint32_t>(quarter * 32) << 16);
@@ -523,7 +615,7 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
         if (c0 + 64 == to) {
           tc::tc_fence_before();
           __syncwarp();
-          if (lane == 0) {
+          if (lane == 0 && !(q.waits.test_fault && w == 0 && rank == 0 && quarter == 0)) {
             if constexpr (CG == 2)
               tc::mbar_arrive_cluster(lead_free + 8 * buf);
             else
@@ -541,6 +633,7 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
           continue;
         }
         if (row0 >= p.I || j0 + c0 >= p.J) continue;  // nothing of this panel is inside
+        if (add_res && c0 > from) res.load(p, row0, j0 + c0, lane);
         float v[64];
 #pragma unroll
         for (int c = 0; c < 64; ++c) v[c] = __uint_as_float(raw_acc[c]);
@@ -568,13 +661,7 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
         }
         if (lane == 0) tc::bulk_wait_read<S::kPanels - 1>();
         __syncwarp();
-        if (p.residual) {
-          if (cols == 64 && rows_on16<T>(p.residual, p.ldr, j0 + c0)) {
-            if (row0 + lane < p.I) add_row<T>(v, static_cast<const T*>(p.residual) + (row0 + lane) * p.ldr + j0 + c0, 64);
-          } else {
-            add_panel<T, 64>(v, panels + pb * kPanelBytes, lane, row0, j0 + c0, p, p.residual, p.ldr);
-          }
-        }
+        if (p.residual) res.add(v, panels + pb * kPanelBytes, lane);
 #pragma unroll
         for (int c = 0; c < 32; ++c) out[c] = pack2_16<T>(v[2 * c], v[2 * c + 1]);
         put_panel<T>(out, panels + pb * kPanelBytes, lane, row0, j0 + c0, p, p.y, p.ldy, &maps.y, q.store_tma);
@@ -587,6 +674,15 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
   }
   tc::tc_fence_before();
   __syncthreads();
+  if (*abort_flag) {
+    // the copies and MMAs in flight use shared and tensor memory.  The other CTA of a
+    // pair may have started copies that this one did not expect: it lingers for far
+    // longer than a copy takes.
+    if (elected && warp == 0 && rank == 0) drain_loads(bar_full, S::kStages, s, phase, q.waits);
+    if (elected && warp == 1 && rank == 0) drain_mmas<CG>(bar_drain, q.waits);
+    if (CG == 2) __nanosleep(200000);
+    __syncthreads();
+  }
   if constexpr (CG == 2) tc::cluster_sync();
   tc::tc_fence_after();
   if (warp == 1) tc::tmem_dealloc_cg<CG>(tmem, S::kTmemCols);

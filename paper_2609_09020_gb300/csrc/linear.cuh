@@ -25,6 +25,24 @@ __device__ __forceinline__ float to_f32<__half>(__half v) { return __half2float(
 template <>
 __device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
 
+// A 16- or 32-bit load under a predicate, 0 where it is off, without a branch: the
+// loads around it need not wait for it.  (With branches, eight elements that are
+// put together are eight memory latencies.)
+__device__ __forceinline__ uint32_t load_if(const uint16_t* p, bool on) {
+  uint16_t v;
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\tmov.u16 %0, 0;\n\t@q ld.global.u16 %0, [%1];\n\t}"
+               : "=h"(v)
+               : "l"(p), "r"(static_cast<uint32_t>(on)));
+  return v;
+}
+__device__ __forceinline__ uint32_t load_if(const uint32_t* p, bool on) {
+  uint32_t v;
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\tmov.u32 %0, 0;\n\t@q ld.global.u32 %0, [%1];\n\t}"
+               : "=r"(v)
+               : "l"(p), "r"(static_cast<uint32_t>(on)));
+  return v;
+}
+
 // Round to nearest even.
 template <typename T>
 __device__ __forceinline__ T from_f32(float v);
@@ -134,10 +152,18 @@ inline int launch_kernel(const void* fn, long long grid, int threads, int smem, 
 }
 
 // Every function returns a pic_status; `ws` is device workspace.
-// On the tensor cores; `status` is set to 1 if a bounded wait
-// (at most spin_limit polls) gives up.
+// What the kernels' bounded waits share: polls that one makes, the device word that
+// is set to 1 when one gives up, and the test hook, which has one epilogue warp of
+// the first tile withhold an arrival.
+struct Waits {
+  int* status;
+  unsigned spin_limit;
+  int test_fault;
+};
+
+// On the tensor cores.
 long long tc_workspace(const Product& p, int dtype);
-int tc_product(const Product& p, int dtype, void* ws, int* status, unsigned spin_limit, cudaStream_t s);
+int tc_product(const Product& p, int dtype, void* ws, const Waits& waits, cudaStream_t s);
 
 // 16-bit types with at most kFewRows rows of A, which must lie along K: every
 // element of B is read once, straight into the operands of warp-level MMAs.
@@ -203,7 +229,7 @@ struct NarrowGrad {
 };
 bool narrow_takes(const NarrowGrad& g, int dtype);
 long long narrow_workspace(const NarrowGrad& g);
-int narrow_grad(const NarrowGrad& g, int dtype, void* ws, int* status, unsigned spin_limit, cudaStream_t s);
+int narrow_grad(const NarrowGrad& g, int dtype, void* ws, const Waits& waits, cudaStream_t s);
 
 }  // namespace lin
 }  // namespace pic

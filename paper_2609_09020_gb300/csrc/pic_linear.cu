@@ -93,6 +93,17 @@ int* status_word() {
   return p;
 }
 
+// pic_linear_test_wait_fault's: nonzero only while a test makes a wait run out.
+std::atomic<int> test_fault{0};
+std::atomic<unsigned> test_spin_limit{0};
+
+// False if the status word has no address.
+bool waits(pic::lin::Waits& w) {
+  const unsigned limit = test_spin_limit.load(std::memory_order_relaxed);
+  w = {status_word(), limit ? limit : pic::kWaitPolls, test_fault.load(std::memory_order_relaxed)};
+  return w.status != nullptr;
+}
+
 // Whether the kernels for few rows take a product (they need no workspace), its
 // workspace bytes, and the product.
 bool few(const Product& p, int dtype) {
@@ -104,9 +115,8 @@ long long product_workspace(const Product& p, int dtype) { return few(p, dtype) 
 int product(const Product& p, int dtype, void* ws, cudaStream_t s) {
   if (few(p, dtype))
     return dtype == PIC_DTYPE_F32 ? pic::lin::few32_product(p, s) : pic::lin::few_product(p, dtype, s);
-  int* status = status_word();
-  if (!status) return PIC_ERR_CUDA;
-  return pic::lin::tc_product(p, dtype, ws, status, pic::kWaitPolls, s);
+  pic::lin::Waits w;
+  return waits(w) ? pic::lin::tc_product(p, dtype, ws, w, s) : PIC_ERR_CUDA;
 }
 
 // Hands out 256-byte aligned pieces of a workspace; with a null base it only
@@ -157,9 +167,9 @@ int backward(const pic_linear_grad_args& a, Arena& ws, bool launch, cudaStream_t
                                  a.dw, a.lddw, a.db, M, static_cast<int>(N), static_cast<int>(K), a.act};
     if (pic::lin::narrow_takes(g, a.dtype)) {
       void* w = ws.take(pic::lin::narrow_workspace(g));
-      int* status = launch ? status_word() : nullptr;
       if (!launch) return PIC_OK;
-      return status ? pic::lin::narrow_grad(g, a.dtype, w, status, pic::kWaitPolls, s) : PIC_ERR_CUDA;
+      pic::lin::Waits wt;
+      return waits(wt) ? pic::lin::narrow_grad(g, a.dtype, w, wt, s) : PIC_ERR_CUDA;
     }
   }
   const auto dx_product = [&](const void* dz, long long lddz) {
@@ -263,6 +273,13 @@ int pic_linear_check(void* stream) {
     return PIC_ERR_CUDA;
   }
   return flag ? PIC_ERR_TIMEOUT : PIC_OK;
+}
+
+int pic_linear_test_wait_fault(int withhold_arrival, unsigned spin_limit) {
+  if (withhold_arrival != 0 && withhold_arrival != 1) return PIC_ERR_INVALID_ARG;
+  test_spin_limit.store(spin_limit, std::memory_order_relaxed);
+  test_fault.store(withhold_arrival, std::memory_order_relaxed);
+  return PIC_OK;
 }
 
 }  // extern "C"

@@ -165,6 +165,8 @@ def load_library():
         f.argtypes, f.restype = [ctypes.POINTER(args)], i64
     lib.pic_linear_check.argtypes = [_P]
     lib.pic_linear_check.restype = i
+    lib.pic_linear_test_wait_fault.argtypes = [i, ctypes.c_uint]
+    lib.pic_linear_test_wait_fault.restype = i
     lib.pic_clip_create.argtypes = [ctypes.POINTER(pic_clip_tensor), i, ctypes.POINTER(_P)]
     lib.pic_clip_create.restype = i
     lib.pic_clip.argtypes = [_P, ctypes.c_float, _P, _P]
@@ -446,12 +448,11 @@ def _rows(t, name, cols, like, rows=None, one_row=False):
     if t.dtype is not like.dtype or t.get_device() != like.get_device():
         raise ValueError(f"{name}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
     shape = t.shape
-    if len(shape) == 2:
-        n = shape[0]
-    else:
-        n = t.numel() // cols
+    if len(shape) == 2 and shape[1] == cols and t.is_contiguous() and (rows is None or shape[0] == rows):
+        return t.data_ptr(), cols
     if not shape or shape[-1] != cols:
         raise ValueError(f"{name}: shape {tuple(shape)}, expected {cols} columns")
+    n = t.numel() // cols
     if rows is not None and n != rows:
         raise ValueError(f"{name}: {n} rows, expected {rows}")
     if len(shape) <= 2 and n > 0:

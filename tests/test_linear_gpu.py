@@ -129,6 +129,27 @@ def test_rows_that_end_inside_16_bytes(size, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("N", [1, 3, 17, 31, 32, 49, 63])
+@pytest.mark.parametrize("rows", [64, 70, 5000])
+def test_narrow_outputs(rows, N, dtype):
+    """Outputs and residuals whose rows lie end to end, in strides, and one of each;
+    several tiles a CTA, and a last one that is not whole."""
+    from paper_2609_09020_gb300 import pic
+    K = 33
+    x, w, b = normal((rows, K), dtype, 1), normal((N, K), dtype, 2, 0.2), normal((N,), dtype, 3)
+    flat, gaps = normal((rows, N), dtype, 4), wide(rows, N, dtype, 4, 6, 1)
+    want_y, want_z = ref.forward(x, w, b, "relu", flat)
+    buf = torch.full((rows, N + 5), 7.0, dtype=dtype, device="cuda")
+    for res in (flat, gaps):
+        for out in (None, buf[:, 2:2 + N]):
+            y, z = pic.linear(x, w, b, act="relu", residual=res, out=out, save_pre=True)
+            ref.check(y, want_y, "y")
+            ref.check(z, want_z, "pre")
+    assert bool((buf[:, :2] == 7).all()) and bool((buf[:, 2 + N:] == 7).all())
+    pic.linear_check()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 @pytest.mark.parametrize("size", [(20000, 64, 64), (9000, 40, 3), (70001, 8, 16), (4096, 512, 384),
                                   (600, 4096, 200), (1500, 1536, 1600), (2500, 328, 2600), (520, 2500, 2600),
                                   (2305, 2304, 2311)], ids=str)
