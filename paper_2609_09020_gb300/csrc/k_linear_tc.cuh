@@ -289,15 +289,18 @@ struct Residual {
         for (int r = 0; r < 32; ++r, o += p.ldr)
           w[r] = load_if(reinterpret_cast<const uint32_t*>(o) + lane, r < rows && lane < n);
       } else {
-        uint32_t high[32];
 #pragma unroll
-        for (int r = 0; r < 32; ++r, o += p.ldr) {
-          const uint16_t* h = reinterpret_cast<const uint16_t*>(o) + 2 * lane;
-          w[r] = load_if(h, r < rows && 2 * lane < n);
-          high[r] = load_if(h + 1, r < rows && 2 * lane + 1 < n);
+        for (int half = 0; half < 32; half += 16) {
+          uint32_t high[16];
+#pragma unroll
+          for (int r = 0; r < 16; ++r, o += p.ldr) {
+            const uint16_t* h = reinterpret_cast<const uint16_t*>(o) + 2 * lane;
+            w[half + r] = load_if(h, half + r < rows && 2 * lane < n);
+            high[r] = load_if(h + 1, half + r < rows && 2 * lane + 1 < n);
+          }
+#pragma unroll
+          for (int r = 0; r < 16; ++r) w[half + r] |= high[r] << 16;
         }
-#pragma unroll
-        for (int r = 0; r < 32; ++r) w[r] |= high[r] << 16;
       }
     }
   }
@@ -603,9 +606,11 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
       long long ti, tj;
       tile_place<S::kRows>(w / q.splits, q.tiles_i, q.tiles_j, ti, tj);
       const long long row0 = ti * S::kRows + rank * 128 + quarter * 32, j0 = tj * BN;
+      // tiles of 64 columns wait for memory: their residual is on its way before they
+      // are summed (for larger tiles that would take registers that they need)
       Residual<T> res;
-      const bool add_res = p.residual && !q.parts;
-      if (add_res && row0 < p.I && j0 + from < p.J) res.load(p, row0, j0 + from, lane);
+      constexpr bool kEarly = BN == 64;
+      if (kEarly && p.residual && !q.parts && row0 < p.I && j0 < p.J) res.load(p, row0, j0, lane);
       if (!__all_sync(0xffffffffu, wait(bar_acc + 8 * buf, phase))) break;
       tc::tc_fence_after();
       const uint32_t d = tmem + buf * BN + (static_cast<uint32_t>(quarter * 32) << 16);
@@ -633,7 +638,6 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
           continue;
         }
         if (row0 >= p.I || j0 + c0 >= p.J) continue;  // nothing of this panel is inside
-        if (add_res && c0 > from) res.load(p, row0, j0 + c0, lane);
         float v[64];
 #pragma unroll
         for (int c = 0; c < 64; ++c) v[c] = __uint_as_float(raw_acc[c]);
@@ -661,7 +665,10 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
         }
         if (lane == 0) tc::bulk_wait_read<S::kPanels - 1>();
         __syncwarp();
-        if (p.residual) res.add(v, panels + pb * kPanelBytes, lane);
+        if (p.residual) {
+          if (!kEarly) res.load(p, row0, j0 + c0, lane);
+          res.add(v, panels + pb * kPanelBytes, lane);
+        }
 #pragma unroll
         for (int c = 0; c < 32; ++c) out[c] = pack2_16<T>(v[2 * c], v[2 * c + 1]);
         put_panel<T>(out, panels + pb * kPanelBytes, lane, row0, j0 + c0, p, p.y, p.ldy, &maps.y, q.store_tma);

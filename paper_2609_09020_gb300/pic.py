@@ -580,14 +580,17 @@ def linear(x, weight, bias=None, act="none", residual=None, out=None, save_pre=F
     return (out, pre) if save_pre else out
 
 
-def linear_backward(dy, x, weight, act="none", pre=None, need=("x", "weight", "bias"), stream=None):
+def linear_backward(dy, x, weight, act="none", pre=None, need=("x", "weight", "bias"), dx=None, dweight=None,
+                    dbias=None, stream=None):
     """The gradients (dx, dweight, dbias) of ``linear`` for the output gradient
     dy [..., out]; those not named in ``need`` are None.  pre is what
     ``linear`` returned with save_pre (not read with act "none").  The
-    residual's gradient is dy itself.  Enqueued on the stream."""
+    gradients are new tensors, or are written to those given (a slice of a
+    gradient buffer, say).  The residual's gradient is dy itself.  Enqueued on
+    the stream."""
     if stream is not None:
         with _Allocating(stream):
-            return linear_backward(dy, x, weight, act, pre, need)
+            return linear_backward(dy, x, weight, act, pre, need, dx, dweight, dbias)
     import torch
     _on_device(dy, "dy")
     if weight.dim() != 2:
@@ -608,22 +611,33 @@ def linear_backward(dy, x, weight, act="none", pre=None, need=("x", "weight", "b
         if pre is None:
             raise ValueError(f"pre: needed for act {act!r}")
         pz, ldz = _rows(pre, "pre", N, dy, M)
-    dx = dw = db = None
     pdx = pdw = pdb = 0
-    if "x" in need:
+    lddx = lddw = K
+    if "x" not in need:
+        dx = None
+    elif dx is None:
         dx = torch.empty(x.shape, dtype=dtype, device=device)
         pdx = dx.data_ptr()
-    if "weight" in need:
-        dw = torch.empty((N, K), dtype=dtype, device=device)
-        pdw = dw.data_ptr()
-    if "bias" in need:
-        db = torch.empty(N, dtype=dtype, device=device)
-        pdb = db.data_ptr()
+    else:
+        pdx, lddx = _rows(dx, "dx", K, dy, M)
+    if "weight" not in need:
+        dweight = None
+    elif dweight is None:
+        dweight = torch.empty((N, K), dtype=dtype, device=device)
+        pdw = dweight.data_ptr()
+    else:
+        pdw, lddw = _rows(dweight, "dweight", K, dy, N)
+    if "bias" not in need:
+        dbias = None
+    else:
+        if dbias is None:
+            dbias = torch.empty(N, dtype=dtype, device=device)
+        pdb = _vector(dbias, "dbias", N, dy)
     if M > 0 or pdw or pdb:
         _call_with_workspace("pic_linear_backward",
                              _LINEAR_GRAD_ARGS.pack(M, K, N, _dtype_code(dy, "dy"), act_code, pdy, lddy, px, ldx,
-                                                    pw, ldw, pz, ldz, pdx, K, pdw, K, pdb), torch, device)
-    return dx, dw, db
+                                                    pw, ldw, pz, ldz, pdx, lddx, pdw, lddw, pdb), torch, device)
+    return dx, dweight, dbias
 
 
 def linear_check(stream=None):
