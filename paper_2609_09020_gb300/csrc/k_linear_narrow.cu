@@ -233,7 +233,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto wait = [&](uint32_t bar, uint32_t parity) { return wait_bounded(bar, parity, abort_flag, q.waits); };
   float* my_parts = q.parts + blockIdx.x * static_cast<long long>(g.N * g.K + g.N);
 
-  const bool elected = (warp == kMmaWarp || warp == kTmaWarp) && tc::elect_one();
   // the TMA thread's place in the ring of stages
   int ring_s = 0;
   uint32_t ring_phase = 0;
@@ -368,7 +367,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
   } else if (warp == kMmaWarp) {
-    if (elected) {
+    if (tc::elect_one()) {
       const int k_pad = (g.K + 15) / 16 * 16, n_steps = (g.N + 15) / 16;
       const uint32_t idesc_dx = idesc_of<T>(128, k_pad, false, true), idesc_dw = idesc_of<T>(128, k_pad, true, true);
       // of a dz of one block the MMA's rows 64..127 are rows 0..63 again, not looked at
@@ -421,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncwarp();
   } else if (TMA && warp == kTmaWarp) {
-    if (elected) {
+    if (tc::elect_one()) {
       const bool has_z = g.act != PIC_ACT_NONE;
       const uint32_t bytes = S::kPlaneBytes * (1 + (g.dw ? 1 : 0) + (has_z ? 1 : 0));
       for (long long tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
@@ -541,8 +540,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc::tc_fence_before();
   __syncthreads();
   if (*abort_flag) {  // copies and MMAs in flight use shared and tensor memory
-    if (TMA && elected && warp == kTmaWarp) drain_loads(bar_landed, S::kStages, ring_s, ring_phase, q.waits);
-    if (elected && warp == kMmaWarp) drain_mmas<1>(bar_drain, q.waits);
+    if (TMA && warp == kTmaWarp && tc::elect_one()) drain_loads(bar_landed, S::kStages, ring_s, ring_phase, q.waits);
+    if (warp == kMmaWarp && tc::elect_one()) drain_mmas<1>(bar_drain, q.waits);
     __syncthreads();
   }
   tc::tc_fence_after();

@@ -133,13 +133,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   // each block of 64 rows has its three planes of 8 KB
   const int a_plane = q.a_mn ? 8192 : kABytes, b_plane = q.b_mn ? 8192 : kBBytes;
 
-  // the TMA or MMA thread, and its place in the ring of stages
-  const bool elected = warp < 2 && tc::elect_one();
+  // the TMA and the MMA thread's place in the ring of stages (elect_one picks the
+  // same lane each time)
   int s = 0;
   uint32_t phase = 0;
   bool ok = true;
   if (warp == 0) {
-    if (elected) {
+    if (tc::elect_one()) {
       const uint32_t lead_full = tc::map_rank(bar_full, 0);
       for (long long w = first; w < q.work && ok; w += step) {
         long long ti, tj;
@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (rank == 0 && elected) {
+    if (rank == 0 && tc::elect_one()) {
       const uint32_t idesc = tc::idesc_16(256, kPlCols, true, q.a_mn != 0, q.b_mn != 0);
       const uint32_t a_step = q.a_mn ? 2048 : 32, b_step = q.b_mn ? 2048 : 32;
       int buf = 0;
@@ -256,8 +256,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc::tc_fence_before();
   __syncthreads();
   if (*abort_flag) {  // as in k_linear_tc.cuh
-    if (elected && warp == 0 && rank == 0) drain_loads(bar_full, kStages, s, phase, q.waits);
-    if (elected && warp == 1 && rank == 0) drain_mmas<2>(bar_drain, q.waits);
+    if (warp == 0 && rank == 0 && tc::elect_one()) drain_loads(bar_full, kStages, s, phase, q.waits);
+    if (warp == 1 && rank == 0 && tc::elect_one()) drain_mmas<2>(bar_drain, q.waits);
     __nanosleep(200000);
     __syncthreads();
   }

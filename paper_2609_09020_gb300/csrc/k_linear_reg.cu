@@ -133,7 +133,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   const float* ma = static_cast<const float*>(o.a);
   const float* mb = static_cast<const float*>(o.b);
   auto wait = [&](uint32_t bar, uint32_t parity) { return wait_bounded(bar, parity, abort_flag, q.waits); };
-  const bool elected = warp == kMmaWarp && tc::elect_one();
   auto part = [&](long long w, int& k0, int& k1) {
     k0 = static_cast<int>(w % q.splits) * q.part_blocks;
     k1 = min(q.k_blocks, k0 + q.part_blocks);
@@ -211,7 +210,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (++s == kStages) s = 0, phase ^= 1;
     __syncwarp();
   } else if (warp == kMmaWarp) {
-    if (elected) {
+    if (tc::elect_one()) {
       const uint32_t a_step = q.a_mn ? 2048 : 32, b_step = q.b_mn ? 2048 : 32;
       int s = 0, buf = 0;
       uint32_t phase = 0, free_phase = 0;
@@ -304,7 +303,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc::tc_fence_before();
   __syncthreads();
   if (*abort_flag) {  // MMAs in flight still read shared memory
-    if (elected) drain_mmas<1>(bar_drain, q.waits);
+    if (warp == kMmaWarp && tc::elect_one()) drain_mmas<1>(bar_drain, q.waits);
     __syncthreads();
   }
   tc::tc_fence_after();

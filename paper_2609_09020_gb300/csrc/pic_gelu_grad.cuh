@@ -1,6 +1,8 @@
 // Generated by paper_2609_09020_gb300/gen_gelu_grad.py -- do not edit.
 // Phi(-a) - a phi(a) ~= 2^(kGeluGradPower a^2) p(a) on 0 <= a <= 6; max error of GELU' in
 // fp32 ~ 3.6e-07 (degree 9), 1.2e-07 (degree 11).
+// a Phi(-a) ~= 2^(kGeluGradPower a^2) r(a); max error of GELU on |z| < 12, the rounding of the
+// result included, ~ 2.5e-07.
 #pragma once
 
 namespace pic {
@@ -9,8 +11,9 @@ constexpr float kGeluGradA = 6.0f;
 constexpr float kGeluGradPower = -0.7213475108146667f;
 constexpr int kGeluGradDeg = 9;
 constexpr int kGeluGradDeg32 = 11;
+constexpr int kGeluDeg32 = 12;
 
-// Coefficients of p, highest degree first (Horner order).
+// Coefficients of p and of r, highest degree first (Horner order).
 __host__ __device__ constexpr float gelu_grad_c(int i) {
   constexpr float c[] = {
       -8.06307161838049e-06f,
@@ -40,6 +43,24 @@ __host__ __device__ constexpr float gelu_grad_c32(int i) {
       0.24997256696224213f,
       -0.7978828549385071f,
       0.4999999701976776f,
+  };
+  return c[i];
+}
+__host__ __device__ constexpr float gelu_c32(int i) {
+  constexpr float c[] = {
+      -1.750784974774433e-07f,
+      4.73991076432867e-06f,
+      -5.789172791992314e-05f,
+      0.00042691887938417494f,
+      -0.002159194787964225f,
+      0.008129028603434563f,
+      -0.024318480864167213f,
+      0.06095236539840698f,
+      -0.13230448961257935f,
+      0.24982641637325287f,
+      -0.3989199697971344f,
+      0.4999990165233612f,
+      0.0f,
   };
   return c[i];
 }

@@ -35,3 +35,15 @@ def test_fp32_polynomial():
     assert len(c) == gen.DEG_FP32 + 1 and len(coefficients()) == gen.DEG + 1
     assert gen.max_error(c) < 1.5e-7
     assert np.all(gen.grad_fp32(np.array([6.0, np.inf]), c) == 1) and np.all(gen.grad_fp32(np.array([-6.0, -np.inf]), c) == 0)
+
+
+def test_gelu_polynomial():
+    c = coefficients("gelu_c32")
+    assert len(c) == gen.DEG_GELU + 1 and c[0] == 0
+    z = np.linspace(-12, 12, 300_001).astype(np.float32)
+    from scipy.special import ndtr
+    want = z.astype(np.float64) * ndtr(z.astype(np.float64))
+    # half an ulp of the result, and 1e-7 of the polynomial and its evaluation
+    assert np.all(np.abs(gen.gelu_fp32(z, c) - want) <= 1e-7 + 2.0 ** -24 * np.abs(want))
+    assert np.all(gen.gelu_fp32(np.array([-6.0, -30.0, -np.inf]), c) == 0)
+    assert gen.gelu_fp32(np.array([np.inf]), c)[0] == np.inf and gen.gelu_fp32(np.array([0.0]), c)[0] == 0
