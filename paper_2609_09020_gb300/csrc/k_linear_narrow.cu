@@ -195,6 +195,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   volatile int* marks = reinterpret_cast<volatile int*>(smem + S::kOffMarks);
 
   if (threadIdx.x == 0) {
+    if (TMA) tc::prefetch_map(&maps.dy);
     for (int s = 0; s < S::kStages; ++s) {
       tc::mbar_init(bar_full + 8 * s, kLoaders / 32);
       tc::mbar_init(bar_empty + 8 * s, 1);

@@ -500,6 +500,8 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::kOffBars + 8 * S::kBars + 4);
 
   if (threadIdx.x == 0) {
+    tc::prefetch_map(&maps.a);
+    tc::prefetch_map(&maps.b);
     for (int s = 0; s < S::kStages; ++s) {
       tc::mbar_init(bar_full + 8 * s, 1);
       tc::mbar_init(bar_empty + 8 * s, 1);

@@ -28,6 +28,10 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// Fetches a tensor map ahead of its first use.
+__device__ __forceinline__ void prefetch_map(const void* tmap) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tmap)) : "memory");
+}
 // TMA load of the box at (x, y), x along the contiguous dimension.  PAIR: the
 // mbarrier may be the other CTA's of the pair.
 template <bool PAIR>

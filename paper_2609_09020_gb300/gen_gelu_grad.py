@@ -77,8 +77,8 @@ def grad_fp32(z, c):
     for k in c[-2::-1]:
         p = (a.astype(np.float64) * p + float(f32(k))).astype(f32)
     e = np.exp2(((a * a).astype(f32) * f32(HALF_LOG2E)).astype(f32).astype(np.float64)).astype(f32)
-    t = np.where(a >= f32(A), f32(0), (e * p).astype(f32))
-    return np.where(z < 0, t, f32(1) - t)
+    t = (e * p).astype(f32)
+    return np.where(z <= f32(-A), f32(0), np.where(z < 0, t, f32(1) - t))
 
 
 def gelu_fp32(z, c):

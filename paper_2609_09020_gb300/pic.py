@@ -678,16 +678,19 @@ class GradClip:
         if rc != PIC_OK:
             raise PicError(rc, "pic_clip_create")
         self.handle = h.value
+        self._call, self._empty_like = load_library().pic_clip, torch.empty_like
+        self._scalar = torch.empty((), dtype=torch.float32, device=torch.device("cuda", self.device))
 
     def clip(self, max_norm: float, stream=None):
         """Scales the gradients by min(1, max_norm / (norm + 1e-6)); returns
         norm, a float32 scalar on the device.  Enqueued on the stream."""
-        import torch
+        if stream is not None:
+            with _Allocating(stream):
+                return self.clip(max_norm)
         if self.handle is None:
             raise ValueError("GradClip: closed")
-        with _Allocating(stream):
-            norm = torch.empty((), dtype=torch.float32, device=torch.device("cuda", self.device))
-            rc = load_library().pic_clip(self.handle, max_norm, norm.data_ptr(), _current_stream())
+        norm = self._empty_like(self._scalar)
+        rc = self._call(self.handle, max_norm, norm.data_ptr(), _current_stream())
         if rc != PIC_OK:
             raise PicError(rc, "pic_clip")
         return norm
