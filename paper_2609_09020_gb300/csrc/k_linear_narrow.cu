@@ -19,7 +19,9 @@
 // over, 6 issues the MMAs, 8..15 make dz and db.  Rows of 16-bit values on 16-byte
 // boundaries, up to 64 of them, come by TMA (warp 7) into a ring of three tiles of
 // dy, z and x, 48 KB each; x is an operand as it lands, and dz takes the place of
-// dy.  Else warps 8..15 load 4 x 16 bytes of dy, z and x per thread at a time, x of
+// dy.  Rows that lie end to end, whatever their width, are runs of memory: warp 7
+// copies a tile's run of each matrix as it is, a tile or more ahead, and warps 8..15
+// pick their elements out of it.  Else warps 8..15 load 4 x 16 bytes of dy, z and x per thread at a time, x of
 // this tile under way while dz is computed, dy and z of the next while x is written
 // to shared memory: any stride and alignment, but less in flight.
 //
@@ -43,12 +45,18 @@ struct NarrowParams {
   NarrowGrad g;
   long long tiles;
   int vec_dy, vec_z, vec_x, store_tma;
+  int raw_ring, raw_bytes;  // kRun: copies in flight, and the room of one
+  int raw_z, raw_x;         // where z and x begin in it
   float* parts;  // [CTAs][N K + N]
   Waits waits;
 };
 
-// T: element; WIDE: up to 128 columns (16-bit types), else 64; TMA: dy, z and x come by TMA.
-template <typename T, bool WIDE, bool TMA>
+// How dy, z and x arrive: through registers, by TMA, as runs of memory.
+enum Source { kReg, kTma, kRun };
+constexpr int kMaxRing = 4;
+
+// T: element; WIDE: up to 128 columns (16-bit types), else 64.
+template <typename T, bool WIDE, Source SRC>
 struct Shape {
   static constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
   static constexpr int kPer = 16 / sizeof(T);          // elements of a load
@@ -61,17 +69,19 @@ struct Shape {
   static_assert(kUnits * kUnitRows == kTile, "whole units");
   static constexpr int kBlockBytes = kTile * 128;
   static constexpr int kPlaneBytes = kBlocks * kBlockBytes;
-  static constexpr int kStageBytes = (TMA ? 3 : 2 * kPlanes) * kPlaneBytes;  // dz, x (and z)
-  static constexpr int kStages = sizeof(T) == 4 ? 1 : WIDE ? 2 : TMA ? 3 : 4;
+  static constexpr int kStageBytes = (SRC == kTma ? 3 : 2 * kPlanes) * kPlaneBytes;  // dz, x (and z)
+  static constexpr int kStages = sizeof(T) == 4 ? 1 : SRC == kRun ? (WIDE ? 1 : 2) : WIDE ? 2 : SRC == kTma ? 3 : 4;
+  static constexpr int kPanels = sizeof(T) == 4 && SRC == kRun ? 1 : 2;  // buffers of a dx warp
   static constexpr int kWBlock = kCols * 128, kWPlane = kBlocks * kWBlock;
   static constexpr int kOffW = kStages * kStageBytes;
   static constexpr int kOffPanels = kOffW + kPlanes * kWPlane;
-  static constexpr int kOffSums = kOffPanels + 4 * 2 * kPanelBytes;
+  static constexpr int kOffSums = kOffPanels + 4 * kPanels * kPanelBytes;
   static constexpr int kOffBars = kOffSums + kLoaders * kPer * 4;
-  // full, empty, landed; dx ready, free; dw ready, free; drain
-  static constexpr int kBars = 3 * kStages + 4 + 4 + 1;
+  // full, empty; landed, taken; dx ready, free; dw ready, free; drain
+  static constexpr int kBars = 2 * kStages + 2 * kMaxRing + 4 + 4 + 1;
   static constexpr int kOffMarks = kOffBars + kBars * 8 + 8;
-  static constexpr int kSmem = kOffMarks + (kMarks + 1) * 4 + 8 + 1024;
+  static constexpr int kOffRaw = (kOffMarks + (kMarks + 1) * 4 + 127) / 128 * 128;
+  static constexpr int kSmem = kOffRaw + 1024;  // 1024: the base is rounded up
   static constexpr int kTmemDw = 2 * kCols;  // columns: two buffers of dx, then dw (fp32: two)
   static constexpr int kTmemCols = WIDE ? 512 : 256;
 };
@@ -95,6 +105,28 @@ struct Vec16 {
       for (int i = 0; i < 8; ++i) e[i] = load_if(reinterpret_cast<const uint16_t*>(p) + i, i < n);
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[i] = e[2 * i] | e[2 * i + 1] << 16;
+    }
+  }
+  // the same from an element of shared memory on
+  __device__ __forceinline__ void get_shared(uint32_t at, int n) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        w[i] = 0;
+        if (i < n) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[i]) : "r"(at + 4 * i) : "memory");
+      }
+    } else {
+      // the words that hold them; what they hold of others goes
+      uint32_t h[5] = {};
+      if (n > 0) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(h[i]) : "r"((at & ~3u) + 4 * i) : "memory");
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t v = (at & 2) ? __funnelshift_r(h[i], h[i + 1], 16) : h[i];
+        w[i] = 2 * i + 1 < n ? v : 2 * i < n ? v & 0xffffu : 0u;
+      }
     }
   }
   __device__ __forceinline__ void widen(float (&f)[kPer]) const {
@@ -174,10 +206,10 @@ struct NarrowMaps {
   CUtensorMap dx, dy, z, x;
 };
 
-template <typename T, bool WIDE, bool TMA>
+template <typename T, bool WIDE, Source SRC>
 __global__ void __launch_bounds__(kThreads, 1)
     narrow_kernel(const __grid_constant__ NarrowParams q, const __grid_constant__ NarrowMaps maps) {
-  using S = Shape<T, WIDE, TMA>;
+  using S = Shape<T, WIDE, SRC>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = tc::smem_addr(smem_raw);
   uint8_t* smem = smem_raw + ((1024 - (raw & 1023)) & 1023);
@@ -186,7 +218,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const NarrowGrad& g = q.g;
   const uint32_t bars = base + S::kOffBars;
   const uint32_t bar_full = bars, bar_empty = bars + 8 * S::kStages, bar_landed = bar_empty + 8 * S::kStages,
-                 bar_dx = bar_landed + 8 * S::kStages,
+                 bar_taken = bar_landed + 8 * kMaxRing, bar_dx = bar_taken + 8 * kMaxRing,
                  bar_dx_free = bar_dx + 16, bar_dw = bar_dx_free + 16, bar_dw_free = bar_dw + 16, bar_drain = bar_dw_free + 16;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + S::kOffBars + 8 * S::kBars);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::kOffBars + 8 * S::kBars + 4);
@@ -195,11 +227,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   volatile int* marks = reinterpret_cast<volatile int*>(smem + S::kOffMarks);
 
   if (threadIdx.x == 0) {
-    if (TMA) tc::prefetch_map(&maps.dy);
+    if (SRC == kTma) tc::prefetch_map(&maps.dy);
     for (int s = 0; s < S::kStages; ++s) {
       tc::mbar_init(bar_full + 8 * s, kLoaders / 32);
       tc::mbar_init(bar_empty + 8 * s, 1);
-      tc::mbar_init(bar_landed + 8 * s, 1);
+    }
+    for (int r = 0; r < kMaxRing; ++r) {
+      tc::mbar_init(bar_landed + 8 * r, 1);
+      tc::mbar_init(bar_taken + 8 * r, kLoaders / 32);
     }
     for (int b = 0; b < 2; ++b) {
       tc::mbar_init(bar_dx + 8 * b, 1);
@@ -258,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     float sum[S::kPer] = {};
     int s = 0, count = 0;
     uint32_t phase = 0;
-    if constexpr (TMA) {
+    if constexpr (SRC == kTma) {
       for (long long tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
         if (!__all_sync(0xffffffffu, wait(bar_landed + 8 * s, phase))) break;
         const uint32_t sdz = base + s * S::kStageBytes, sz = sdz + 2 * S::kPlaneBytes;
@@ -295,14 +330,33 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (++s == S::kStages) s = 0, phase ^= 1;
       }
     } else {
-    if (blockIdx.x < q.tiles) load_dz(blockIdx.x * static_cast<long long>(kTile));
+    if (SRC == kReg && blockIdx.x < q.tiles) load_dz(blockIdx.x * static_cast<long long>(kTile));
+    int raw = 0;
+    uint32_t raw_phase = 0;
     for (long long tile = blockIdx.x; tile < q.tiles; tile += gridDim.x, ++count) {
       uint32_t largest = 0;
       bool ok = true;
+      if (SRC == kRun && !__all_sync(0xffffffffu, wait(bar_landed + 8 * raw, raw_phase))) break;
 #pragma unroll
       for (int unit = 0; unit < S::kUnits; ++unit) {
         const long long i0 = tile * kTile + unit * S::kUnitRows;
-        if (n_x > 0) {
+        if constexpr (SRC == kRun) {
+          const uint32_t from = base + S::kOffRaw + raw * q.raw_bytes;
+          constexpr int kElem = sizeof(T);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int r = unit * S::kUnitRows + row + u * S::kPassRows;
+            const bool here = tile * kTile + r < g.I;
+            vy[u].get_shared(from + (r * g.N + col) * kElem, here ? n_dz : 0);
+            if (has_act) vz[u].get_shared(from + q.raw_z + (r * g.N + col) * kElem, here ? n_dz : 0);
+            if (g.dw) vx[u].get_shared(from + q.raw_x + (r * g.K + col) * kElem, here ? n_x : 0);
+          }
+          if (unit + 1 == S::kUnits) {
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(bar_taken + 8 * raw);
+            if (++raw == q.raw_ring) raw = 0, raw_phase ^= 1;
+          }
+        } else if (n_x > 0) {
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             const long long i = i0 + row + u * S::kPassRows;
@@ -334,7 +388,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int u = 0; u < 4; ++u)
           largest = max(largest, put_vec<T>(sdz, S::kBlockBytes, S::kPlaneBytes, unit * S::kUnitRows + row + u * S::kPassRows, col, vy[u].w));
-        if (unit + 1 < S::kUnits)
+        if (SRC == kRun) {
+        } else if (unit + 1 < S::kUnits)
           load_dz(i0 + S::kUnitRows);
         else if (tile + gridDim.x < q.tiles)
           load_dz((tile + gridDim.x) * kTile);
@@ -377,7 +432,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t phase = 0, free_phase = 0;
       bool ok = true, first = true;
       for (long long tile = blockIdx.x; tile < q.tiles && ok; tile += gridDim.x) {
-        if (!(ok = wait(bar_full + 8 * s, phase) && (!TMA || wait(bar_landed + 8 * s, phase)))) break;
+        if (!(ok = wait(bar_full + 8 * s, phase) && (SRC != kTma || wait(bar_landed + 8 * s, phase)))) break;
         tc::tc_fence_after();
         const uint32_t sdz = base + s * S::kStageBytes, sx = sdz + S::kPlanes * S::kPlaneBytes, sw = base + S::kOffW;
         constexpr int kProducts = S::kPlanes == 3 ? 6 : 1;
@@ -420,7 +475,39 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (ok && S::kPlanes == 1 && g.dw) tc::mma_commit(bar_dw);
     }
     __syncwarp();
-  } else if (TMA && warp == kTmaWarp) {
+  } else if (SRC == kRun && warp == kTmaWarp) {
+    if (tc::elect_one()) {
+      constexpr long long kElem = sizeof(T);
+      for (long long tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
+        if (!wait(bar_taken + 8 * ring_s, ring_phase ^ 1)) break;
+        const uint32_t at = base + S::kOffRaw + ring_s * q.raw_bytes, bar = bar_landed + 8 * ring_s;
+        const long long rows = min(static_cast<long long>(kTile), g.I - tile * kTile);
+        uint32_t bytes = 0;
+        // whole 16 bytes by an asynchronous copy; the last tile's last few by themselves
+        const auto copy = [&](const void* m, long long cols, uint32_t to, bool go) {
+          const char* from = static_cast<const char*>(m) + tile * kTile * cols * kElem;
+          const int all = static_cast<int>(rows * cols * kElem), whole = all / 16 * 16;
+          if (!go) {
+            bytes += whole;
+            for (int e = whole; e < all; e += 2) {
+              const uint16_t v = *reinterpret_cast<const uint16_t*>(from + e);
+              asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + e), "h"(v) : "memory");
+            }
+          } else if (whole > 0) {
+            tc::bulk_load(to, from, whole, bar);
+          }
+        };
+        for (int go = 0; go < 2; ++go) {
+          copy(g.dy, g.N, at, go);
+          if (g.act != PIC_ACT_NONE) copy(g.pre, g.N, at + q.raw_z, go);
+          if (g.dw) copy(g.x, g.K, at + q.raw_x, go);
+          if (!go) tc::mbar_arrive_expect_tx(bar, bytes);
+        }
+        if (++ring_s == q.raw_ring) ring_s = 0, ring_phase ^= 1;
+      }
+    }
+    __syncwarp();
+  } else if (SRC == kTma && warp == kTmaWarp) {
     if (tc::elect_one()) {
       const bool has_z = g.act != PIC_ACT_NONE;
       const uint32_t bytes = S::kPlaneBytes * (1 + (g.dw ? 1 : 0) + (has_z ? 1 : 0));
@@ -437,7 +524,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncwarp();
   } else if (warp < 4) {
-    const uint32_t panels = base + S::kOffPanels + warp * 2 * kPanelBytes;
+    const uint32_t panels = base + S::kOffPanels + warp * S::kPanels * kPanelBytes;
     const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
     Product p{};  // what put_panel looks at
     p.I = g.I, p.J = g.K;
@@ -479,10 +566,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             else
               out[c] = pack2_16<T>(__uint_as_float(r[2 * c]), __uint_as_float(r[2 * c + 1]));
           }
-          if (lane == 0) tc::bulk_wait_read<1>();
+          if (lane == 0) tc::bulk_wait_read<S::kPanels - 1>();
           __syncwarp();
           put_panel<T>(out, panels + pb * kPanelBytes, lane, row0, 64 * b + 32 * h, p, g.dx, g.lddx, &maps.dx, q.store_tma);
-          pb ^= 1;
+          if (++pb == S::kPanels) pb = 0;
         }
       }
       if (++buf == 2) buf = 0, phase ^= 1;
@@ -541,7 +628,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc::tc_fence_before();
   __syncthreads();
   if (*abort_flag) {  // copies and MMAs in flight use shared and tensor memory
-    if (TMA && warp == kTmaWarp && tc::elect_one()) drain_loads(bar_landed, S::kStages, ring_s, ring_phase, q.waits);
+    if (SRC != kReg && warp == kTmaWarp && tc::elect_one())
+      drain_loads(bar_landed, SRC == kRun ? q.raw_ring : S::kStages, ring_s, ring_phase, q.waits);
     if (warp == kMmaWarp && tc::elect_one()) drain_mmas<1>(bar_drain, q.waits);
     __syncthreads();
   }
@@ -581,11 +669,27 @@ int ctas(const NarrowGrad& g) {
   return static_cast<int>(tiles < kSms ? tiles : kSms);
 }
 
-template <typename T, bool WIDE, bool TMA>
+// The run mode's room for copies: a tile's dy, z and x, each on a 16-byte boundary
+// with some bytes to read past its end; as many tiles as fit, false if none does.
+template <typename T, bool WIDE>
+bool plan_runs(NarrowParams& q) {
+  const NarrowGrad& g = q.g;
+  const int dz = (kTile * g.N * static_cast<int>(sizeof(T)) + 47) / 16 * 16;
+  const int x = (kTile * g.K * static_cast<int>(sizeof(T)) + 47) / 16 * 16;
+  q.raw_z = dz;
+  q.raw_x = g.act != PIC_ACT_NONE ? 2 * dz : dz;
+  q.raw_bytes = (q.raw_x + (g.dw ? x : 0) + 127) / 128 * 128;
+  q.raw_ring = (227 * 1024 - Shape<T, WIDE, kRun>::kSmem) / q.raw_bytes;
+  if (q.raw_ring > kMaxRing) q.raw_ring = kMaxRing;
+  return q.raw_ring > 0;
+}
+
+template <typename T, bool WIDE, Source SRC>
 int run(const NarrowGrad& g, NarrowParams& q, NarrowMaps& maps, int slot, cudaStream_t s) {
-  const void* fn = reinterpret_cast<const void*>(narrow_kernel<T, WIDE, TMA>);
-  const int smem = Shape<T, WIDE, TMA>::kSmem, grid = ctas(g);
-  static_assert(Shape<T, WIDE, TMA>::kSmem <= 227 * 1024, "shared memory of an SM");
+  const void* fn = reinterpret_cast<const void*>(narrow_kernel<T, WIDE, SRC>);
+  const int fixed = Shape<T, WIDE, SRC>::kSmem, grid = ctas(g);
+  const int smem = SRC == kRun ? 227 * 1024 : fixed;  // the attribute is set once, for runs of any width
+  static_assert(Shape<T, WIDE, SRC>::kSmem <= 227 * 1024, "shared memory of an SM");
   if (allow_smem(fn, slot, smem) != PIC_OK) return PIC_ERR_CUDA;
   void* args[] = {&q, &maps};
   if (cudaLaunchKernel(fn, dim3(grid), dim3(kThreads), args, smem, s) != cudaSuccess) return PIC_ERR_CUDA;
@@ -625,14 +729,20 @@ int narrow_grad(const NarrowGrad& g, int dtype, void* ws, const Waits& waits, cu
                (!has_z || encode(&maps.z, g.pre, g.I, g.N, g.ldpre, kTile, dtype)) &&
                (!g.dw || encode(&maps.x, g.x, g.I, g.K, g.ldx, kTile, dtype))))
     return PIC_ERR_CUDA;
-  if (dtype == PIC_DTYPE_F32) return run<float, false, false>(g, q, maps, 8, s);
-  if (dtype == PIC_DTYPE_F16)
-    return wide  ? run<__half, true, false>(g, q, maps, 9, s)
-           : tma ? run<__half, false, true>(g, q, maps, 10, s)
-                 : run<__half, false, false>(g, q, maps, 11, s);
-  return wide  ? run<__nv_bfloat16, true, false>(g, q, maps, 12, s)
-         : tma ? run<__nv_bfloat16, false, true>(g, q, maps, 13, s)
-               : run<__nv_bfloat16, false, false>(g, q, maps, 14, s);
+  // rows end to end, from a 16-byte boundary on
+  const auto packed = [](const void* m, long long ld, int cols) { return ld == cols && reinterpret_cast<uintptr_t>(m) % 16 == 0; };
+  const bool runs = !tma && packed(g.dy, g.lddy, g.N) && (!has_z || packed(g.pre, g.ldpre, g.N)) && (!g.dw || packed(g.x, g.ldx, g.K));
+  if (dtype == PIC_DTYPE_F32)
+    return runs && plan_runs<float, false>(q) ? run<float, false, kRun>(g, q, maps, 15, s) : run<float, false, kReg>(g, q, maps, 8, s);
+  if (dtype == PIC_DTYPE_F16) {
+    if (tma) return run<__half, false, kTma>(g, q, maps, 10, s);
+    if (wide) return runs && plan_runs<__half, true>(q) ? run<__half, true, kRun>(g, q, maps, 16, s) : run<__half, true, kReg>(g, q, maps, 9, s);
+    return runs && plan_runs<__half, false>(q) ? run<__half, false, kRun>(g, q, maps, 17, s) : run<__half, false, kReg>(g, q, maps, 11, s);
+  }
+  using B = __nv_bfloat16;
+  if (tma) return run<B, false, kTma>(g, q, maps, 13, s);
+  if (wide) return runs && plan_runs<B, true>(q) ? run<B, true, kRun>(g, q, maps, 18, s) : run<B, true, kReg>(g, q, maps, 12, s);
+  return runs && plan_runs<B, false>(q) ? run<B, false, kRun>(g, q, maps, 19, s) : run<B, false, kReg>(g, q, maps, 14, s);
 }
 
 }  // namespace lin

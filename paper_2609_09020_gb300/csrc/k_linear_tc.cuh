@@ -703,7 +703,7 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
 bool encode(CUtensorMap* map, const void* m, long long rows, long long cols, long long ld, int box_rows, int dtype);
 // Allows a kernel `smem` bytes of shared memory, once per device; each kernel of
 // these files has a slot of its own below kSmemSlots.
-constexpr int kSmemSlots = 15;
+constexpr int kSmemSlots = 20;
 int allow_smem(const void* fn, int slot, int smem);
 
 // The kernel for tiles of bn columns: 64 and 128 by one CTA, 256 by a pair.

@@ -64,6 +64,13 @@ __device__ __forceinline__ void tma_store_2d(const void* tmap, int x, int y, uin
                "r"(x), "r"(y), "r"(src)
                : "memory");
 }
+// Copies `bytes` (a multiple of 16) from global to shared memory, both on 16-byte
+// boundaries, completing them on the mbarrier bar.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
 // Copies `bytes` (a multiple of 16) from shared to global memory, both on 16-byte boundaries.
 __device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t bytes) {
   asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
