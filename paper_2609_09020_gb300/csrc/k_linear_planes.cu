@@ -25,7 +25,7 @@ constexpr int kABytes = 128 * 128, kBBytes = kPlCols / 2 * 128;  // one plane of
 constexpr int kStageBytes = kPieces * (kABytes + kBBytes);
 constexpr int kStages = 2;
 constexpr int kOffPanels = kStages * kStageBytes;
-constexpr int kOffBars = kOffPanels + kEpi * kPanelBytes;
+constexpr int kOffBars = kOffPanels + kEpi * kTurnBytes;
 constexpr int kBars = 2 * kStages + 4 + 1;
 constexpr int kSmem = kOffBars + kBars * 8 + 16 + 1024;
 constexpr int kTmemCols = 2 * kPlCols;
@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncwarp();
   } else {
     const int quarter = warp & 3, half = (warp - 2) >> 2;
-    const uint32_t panel = base + kOffPanels + (warp - 2) * kPanelBytes;
+    float* turn = reinterpret_cast<float*>(smem + kOffPanels + (warp - 2) * kTurnBytes);
     const uint32_t lead_free = tc::map_rank(bar_free, 0);
     const long long a_groups = (p.I + 127) / 128, b_groups = (p.J + 127) / 128;
     int buf = 0;
@@ -250,9 +250,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         continue;
       }
       if (row0 >= p.I || col0 >= p.J) continue;
-      finish_rows(v, p, maps, panel, lane, row0, col0, q.store_tma);
+      finish_rows(v, p, turn, lane, row0, col0);
     }
-    if (lane == 0) tc::bulk_wait_all();
     __syncwarp();
   }
   tc::tc_fence_before();

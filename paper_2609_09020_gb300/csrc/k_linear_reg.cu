@@ -28,7 +28,7 @@ constexpr int kAPlane = kRegRows * 128, kBPlane = kRegCols * 128;  // bytes
 constexpr int kStageBytes = kPieces * (kAPlane + kBPlane);
 constexpr int kStages = 2;
 constexpr int kOffPanels = kStages * kStageBytes;
-constexpr int kOffBars = kOffPanels + kEpiWarps * kPanelBytes;
+constexpr int kOffBars = kOffPanels + kEpiWarps * kTurnBytes;
 constexpr int kBars = 2 * kStages + 4 + 1;
 constexpr int kOffMarks = kOffBars + kBars * 8 + 8;
 constexpr int kSmem = kOffMarks + kMarks * 4 + 8 + 1024;  // 1024: the base is rounded up
@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncwarp();
   } else {
     const int quarter = warp;
-    const uint32_t panel = base + kOffPanels + warp * kPanelBytes;
+    float* turn = reinterpret_cast<float*>(smem + kOffPanels + warp * kTurnBytes);
     int buf = 0, tile = 0;
     uint32_t phase = 0;
     bool ok = true;
@@ -295,9 +295,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         continue;
       }
       if (row0 >= p.I) continue;
-      finish_rows(v, p, maps, panel, lane, row0, col0, q.store_tma);
+      finish_rows(v, p, turn, lane, row0, col0);
     }
-    if (lane == 0) tc::bulk_wait_all();
     __syncwarp();
   }
   tc::tc_fence_before();

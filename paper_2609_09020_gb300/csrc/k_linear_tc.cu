@@ -180,7 +180,7 @@ struct ShapeCost {
 constexpr ShapeCost kShape64{64, 1, 2 * kSms, 4.2, 0.20, 3.0};
 constexpr ShapeCost kShape128{128, 1, kSms, 4.5, 0.19, 2.2};
 constexpr ShapeCost kShape256{256, 2, kSms / 2, 6.8, 0.26, 3.4};
-constexpr ShapeCost kShapeReg{kRegCols, 1, kSms, 6.0, 1.9, 2.0};
+constexpr ShapeCost kShapeReg{kRegCols, 1, kSms, 6.0, 1.7, 4.0};
 constexpr ShapeCost kShapePlanes{kPlCols, 2, kSms / 2, 8.0, 0.85, 3.4};
 
 // The shape and the number of parts of K with the least estimated time, parts at
@@ -370,7 +370,7 @@ int tc_product(const Product& p, int dtype, void* ws, const Waits& waits, cudaSt
   };
   // a TMA store ends on a 16-byte boundary of the row: columns that do not would
   // have their neighbours overwritten
-  q.store_tma = !q.parts && p.J * elem % 16 == 0 && fits(p.y, p.ldy, p.I) && (!p.pre || fits(p.pre, p.ldpre, p.I));
+  q.store_tma = !q.parts && elem == 2 && p.J * elem % 16 == 0 && fits(p.y, p.ldy, p.I) && (!p.pre || fits(p.pre, p.ldpre, p.I));
   const auto out_ld = [&](long long ld) { return p.I == 1 ? (p.J + 7) / 8 * 8 : ld; };
   bool ok = true;
   if (r.reg) {

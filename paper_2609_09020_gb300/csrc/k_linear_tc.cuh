@@ -383,40 +383,67 @@ __device__ __forceinline__ void add_row(float (&v)[N], const T* r, int cols) {
   }
 }
 
-// The epilogue of a lane's row and 64 columns of fp32 sums: bias, pre, activation,
-// residual, and out through the warp's one panel buffer.
-__device__ __forceinline__ void finish_rows(float (&v)[64], const Product& p, const TcMaps& maps, uint32_t panel, int lane,
-                                            long long row0, long long col0, bool by_tma) {
-  const int cols = static_cast<int>(min(64LL, p.J - col0));
-  if (p.bias) add_row<float>(v, static_cast<const float*>(p.bias) + col0, cols);
-  const auto put = [&](void* out, long long ld, const CUtensorMap* map) {
+// The fp32 epilogue of a warp's 32 rows x 64 columns of sums, a row in each lane's v:
+// they are turned in shared memory (kTurnBytes), and then the lanes walk down the
+// columns, so that every load and store is a run of 128 bytes whatever the strides.
+// A warp or two of an SM's quarter do this for every tile, so it counts instructions:
+// pointers move by a row, whole tiles ask for no row's existence, and a column of a
+// residual's 32 loads are under way together.
+constexpr int kTurnStride = 65;  // floats: no bank conflicts either way
+constexpr int kTurnBytes = 32 * kTurnStride * 4;
+
+// One column (of every lane) down the rows.
+template <bool WHOLE>
+__device__ __forceinline__ void finish_column(const Product& p, const float* turn, int c, long long row0, long long col,
+                                              int rows, const float (&q)[32]) {
+  const float bias = p.bias ? static_cast<const float*>(p.bias)[col] : 0.0f;
+  float* pre = p.pre ? static_cast<float*>(p.pre) + row0 * p.ldpre + col : nullptr;
+  float* y = static_cast<float*>(p.y) + row0 * p.ldy + col;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (32 * h >= cols) break;
-      uint32_t r[32];
+  for (int r0 = 0; r0 < 32; r0 += 8) {
+    if (!WHOLE && r0 >= rows) break;
+    float z[8];
 #pragma unroll
-      for (int c = 0; c < 32; ++c) r[c] = __float_as_uint(v[h * 32 + c]);
-      if (lane == 0) tc::bulk_wait_read<0>();
-      __syncwarp();
-      put_panel<float>(r, panel, lane, row0, col0 + h * 32, p, out, ld, map, by_tma);
+    for (int u = 0; u < 8; ++u) z[u] = turn[(r0 + u) * kTurnStride + c] + bias;
+    if (pre) {
+#pragma unroll
+      for (int u = 0; u < 8; ++u, pre += p.ldpre)
+        if (WHOLE || r0 + u < rows) *pre = z[u];
     }
-  };
-  if (p.pre) put(p.pre, p.ldpre, &maps.pre);
-  if (p.act != PIC_ACT_NONE) {
+    if (p.act == PIC_ACT_RELU) {
 #pragma unroll
-    for (int c = 0; c < 64; ++c) v[c] = act_value<true>(v[c], p.act);
-  }
-  if (p.residual) {
-    if (lane == 0) tc::bulk_wait_read<0>();
-    Residual<float> res;
+      for (int u = 0; u < 8; ++u) z[u] = relu_nan(z[u]);
+    } else if (p.act == PIC_ACT_GELU) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (32 * h >= cols) break;
-      res.load(p, row0, col0 + 32 * h, lane);
-      res.add(v + 32 * h, panel, lane);
+      for (int u = 0; u < 8; ++u) z[u] = act_value<true>(z[u], PIC_ACT_GELU);
     }
+#pragma unroll
+    for (int u = 0; u < 8; ++u, y += p.ldy)
+      if (WHOLE || r0 + u < rows) *y = z[u] + q[r0 + u];
   }
-  put(p.y, p.ldy, &maps.y);
+}
+
+__device__ __forceinline__ void finish_rows(const float (&v)[64], const Product& p, float* turn, int lane, long long row0,
+                                            long long col0) {
+  __syncwarp();
+#pragma unroll
+  for (int c = 0; c < 64; ++c) turn[lane * kTurnStride + c] = v[c];
+  __syncwarp();
+  const int rows = static_cast<int>(min(32LL, p.I - row0));
+#pragma unroll 1
+  for (int c = lane; c < 64; c += 32) {
+    if (col0 + c >= p.J) break;
+    float q[32] = {};
+    if (p.residual) {
+      const float* res = static_cast<const float*>(p.residual) + row0 * p.ldr + col0 + c;
+#pragma unroll
+      for (int r = 0; r < 32; ++r, res += p.ldr) q[r] = __uint_as_float(load_if(reinterpret_cast<const uint32_t*>(res), r < rows));
+    }
+    if (rows == 32)
+      finish_column<true>(p, turn, c, row0, col0 + c, rows, q);
+    else
+      finish_column<false>(p, turn, c, row0, col0 + c, rows, q);
+  }
 }
 
 // A product cut along K: a tile's parts are [rank][panel][quarter][16][32 rows][4
