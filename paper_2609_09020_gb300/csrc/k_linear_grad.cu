@@ -60,7 +60,7 @@ struct Load {
 };
 
 template <typename T, int V>
-__global__ void __launch_bounds__(kThreads) grad_act_kernel(const GradAct g, const Share s) {
+__global__ void __launch_bounds__(kThreads, 4) grad_act_kernel(const GradAct g, const Share s) {
   extern __shared__ float sums[];  // [ty][tx * V]
   const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx, rows = kThreads / s.tx;
   const long long col_block = blockIdx.x % s.col_blocks, row_block = blockIdx.x / s.col_blocks;

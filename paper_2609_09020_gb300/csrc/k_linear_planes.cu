@@ -5,6 +5,9 @@
 // every 16 of K.  (k_linear_reg.cu cuts on the way into shared memory instead,
 // again for every tile: better where a matrix is used by one tile or two.)
 //
+// A stage is 32 of K: four stages of 36 KB keep 108 KB of loads under way, where two
+// of 64 of K kept 72 (2048 x 1024 -> 4096: 86 us, the tensor pipe busy half of it).
+//
 // Roles: warp 0 TMA, warp 1 MMAs, warps 2..9 epilogue: 32 rows x 64 columns
 // each, which takes the accumulators over after every kTakeover slices.
 //
@@ -21,14 +24,17 @@ namespace {
 constexpr int kEpi = 8;
 constexpr int kThreads = 64 + 32 * kEpi;
 constexpr int kTakeover = 2;
-constexpr int kABytes = 128 * 128, kBBytes = kPlCols / 2 * 128;  // one plane of one CTA
+constexpr int kHalf = 32;  // K of a stage, half a slice
+constexpr int kABytes = 128 * 2 * kHalf, kBBytes = kPlCols / 2 * 2 * kHalf;  // one plane of one CTA
+constexpr int kBlock = kHalf * 128;  // 64 rows of an operand that lies along them
 constexpr int kStageBytes = kPieces * (kABytes + kBBytes);
-constexpr int kStages = 2;
+constexpr int kStages = 4;
 constexpr int kOffPanels = kStages * kStageBytes;
 constexpr int kOffBars = kOffPanels + kEpi * kTurnBytes;
-constexpr int kBars = 2 * kStages + 4 + 1;
+constexpr int kBufs = 4;  // accumulators: their way to the epilogue and back is longer than a slice's MMAs
+constexpr int kBars = 2 * kStages + 2 * kBufs + 1;
 constexpr int kSmem = kOffBars + kBars * 8 + 16 + 1024;
-constexpr int kTmemCols = 2 * kPlCols;
+constexpr int kTmemCols = kBufs * kPlCols;
 
 struct CutPair {
   CutMatrix m[2];
@@ -99,7 +105,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t rank = tc::cluster_rank();
   const uint32_t bars = base + kOffBars;
   const uint32_t bar_full = bars, bar_empty = bars + 8 * kStages, bar_acc = bar_empty + 8 * kStages,
-                 bar_free = bar_acc + 16, bar_drain = bar_free + 16;
+                 bar_free = bar_acc + 8 * kBufs, bar_drain = bar_free + 8 * kBufs;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kOffBars + 8 * kBars);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kOffBars + 8 * kBars + 4);
 
@@ -110,7 +116,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc::mbar_init(bar_full + 8 * s, 1);
       tc::mbar_init(bar_empty + 8 * s, 1);
     }
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < kBufs; ++b) {
       tc::mbar_init(bar_acc + 8 * b, 1);
       tc::mbar_init(bar_free + 8 * b, kEpi * 2);
     }
@@ -131,9 +137,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     k0 = static_cast<int>(w % q.splits) * q.part_blocks;
     k1 = min(q.k_blocks, k0 + q.part_blocks);
   };
-  // one plane is kABytes (kBBytes) of rows along K; of an operand along its rows
-  // each block of 64 rows has its three planes of 8 KB
-  const int a_plane = q.a_mn ? 8192 : kABytes, b_plane = q.b_mn ? 8192 : kBBytes;
+  // one plane is kABytes (kBBytes) of rows along K (64 bytes each); of an operand
+  // along its rows each block of 64 rows has its three planes of kBlock bytes
+  const int a_plane = q.a_mn ? kBlock : kABytes, b_plane = q.b_mn ? kBlock : kBBytes;
 
   // the TMA and the MMA thread's place in the ring of stages (elect_one picks the
   // same lane each time)
@@ -149,14 +155,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int i0 = static_cast<int>(ti * kPlRows + rank * 128), j0 = static_cast<int>(tj * kPlCols + rank * 64);
         int k0, k1;
         part(w, k0, k1);
-        for (int kb = k0; kb < k1; ++kb) {
+        for (int kh = 2 * k0; kh < 2 * k1; ++kh) {
           if (!(ok = wait(bar_empty + 8 * s, phase ^ 1))) break;
           if (rank == 0) tc::mbar_arrive_expect_tx(bar_full + 8 * s, 2 * kStageBytes);
           const uint32_t sa = base + s * kStageBytes, sb = sa + kPieces * kABytes, bar = lead_full + 8 * s;
-          const int k = kb * kSlice;
+          const int k = kh * kHalf;
           if (q.a_mn) {
             tc::tma_load_planes_pair(sa, &maps.a, i0, k, bar);
-            tc::tma_load_planes_pair(sa + kPieces * 8192, &maps.a, i0 + 64, k, bar);
+            tc::tma_load_planes_pair(sa + kPieces * kBlock, &maps.a, i0 + 64, k, bar);
           } else {
             tc::tma_load_planes_pair(sa, &maps.a, k, i0, bar);
           }
@@ -182,24 +188,26 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!(ok = wait(bar_free + 8 * buf, free_phase ^ 1))) break;
           tc::tc_fence_after();
           const uint32_t d = tmem + buf * kPlCols;
-          const int c1 = min(k1, c0 + kTakeover);
-          for (int kb = c0; kb < c1; ++kb) {
+          const int h0 = 2 * c0, h1 = 2 * min(k1, c0 + kTakeover);
+          for (int kh = h0; kh < h1; ++kh) {
             if (!(ok = wait(bar_full + 8 * s, phase))) break;
             tc::tc_fence_after();
             const uint32_t sa = base + s * kStageBytes, sb = sa + kPieces * kABytes;
 #pragma unroll
             for (int t = 0; t < 6; ++t)
 #pragma unroll
-              for (int kk = 0; kk < kSlice / 16; ++kk)
-                tc::mma_16<2>(d, tc::smem_desc_sw128(sa + cut_a(t) * a_plane + kk * a_step, kPieces * 8192, 1024),
-                              tc::smem_desc_sw128(sb + cut_b(t) * b_plane + kk * b_step, kPieces * 8192, 1024), idesc,
-                              (kb > c0 || t > 0 || kk > 0) ? 1u : 0u);
+              for (int kk = 0; kk < kHalf / 16; ++kk) {
+                const uint32_t a = sa + cut_a(t) * a_plane + kk * a_step, b = sb + cut_b(t) * b_plane + kk * b_step;
+                tc::mma_16<2>(d, q.a_mn ? tc::smem_desc_sw128(a, kPieces * kBlock, 1024) : tc::smem_desc_sw64(a),
+                              q.b_mn ? tc::smem_desc_sw128(b, kPieces * kBlock, 1024) : tc::smem_desc_sw64(b), idesc,
+                              (kh > h0 || t > 0 || kk > 0) ? 1u : 0u);
+              }
             tc::mma_commit_cg<2>(bar_empty + 8 * s);
             if (++s == kStages) s = 0, phase ^= 1;
           }
           if (!ok) break;
           tc::mma_commit_cg<2>(bar_acc + 8 * buf);
-          if (++buf == 2) buf = 0, free_phase ^= 1;
+          if (++buf == kBufs) buf = 0, free_phase ^= 1;
         }
       }
     }
@@ -233,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc::tc_fence_before();
         __syncwarp();
         if (lane == 0 && !(q.waits.test_fault && w == 0 && rank == 0 && warp == 2)) tc::mbar_arrive_cluster(lead_free + 8 * buf);
-        if (++buf == 2) buf = 0, phase ^= 1;
+        if (++buf == kBufs) buf = 0, phase ^= 1;
       }
       if (!ok) break;
       if (marked(o.a, q.a_mn, ti * 2 + rank, a_groups, k0, k1, lane) || marked(o.b, q.b_mn, tj, b_groups, k0, k1, lane)) {

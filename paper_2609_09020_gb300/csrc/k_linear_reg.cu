@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kEpiWarps = 4, kLoadWarps = 8, kMmaWarp = kEpiWarps + kLoadWarps;
 constexpr int kThreads = 32 * (kMmaWarp + 1), kLoaders = 32 * kLoadWarps;
-constexpr int kMarks = 8;  // more than the tiles that the loaders can be ahead of the epilogue
+constexpr int kMarks = 16;  // more than the tiles that the loaders can be ahead of the epilogue
 constexpr int kChunk = 2;  // slices of 64 between two takeovers of the accumulators
 
 constexpr int kAPlane = kRegRows * 128, kBPlane = kRegCols * 128;  // bytes
@@ -29,10 +29,11 @@ constexpr int kStageBytes = kPieces * (kAPlane + kBPlane);
 constexpr int kStages = 2;
 constexpr int kOffPanels = kStages * kStageBytes;
 constexpr int kOffBars = kOffPanels + kEpiWarps * kTurnBytes;
-constexpr int kBars = 2 * kStages + 4 + 1;
+constexpr int kBufs = 4;  // accumulators
+constexpr int kBars = 2 * kStages + 2 * kBufs + 1;
 constexpr int kOffMarks = kOffBars + kBars * 8 + 8;
 constexpr int kSmem = kOffMarks + kMarks * 4 + 8 + 1024;  // 1024: the base is rounded up
-constexpr int kTmemCols = 2 * kRegCols;
+constexpr int kTmemCols = kBufs * kRegCols;
 
 struct Quad {
   uint32_t w[4];
@@ -104,7 +105,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t bars = base + kOffBars;
   const uint32_t bar_full = bars, bar_empty = bars + 8 * kStages, bar_acc = bar_empty + 8 * kStages,
-                 bar_free = bar_acc + 16, bar_drain = bar_free + 16;
+                 bar_free = bar_acc + 8 * kBufs, bar_drain = bar_free + 8 * kBufs;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kOffBars + 8 * kBars);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kOffBars + 8 * kBars + 4);
   // mark t % kMarks holds t + 1 if this CTA's t-th tile has an infinite or NaN operand
@@ -115,7 +116,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc::mbar_init(bar_full + 8 * s, kLoadWarps);
       tc::mbar_init(bar_empty + 8 * s, 1);
     }
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < kBufs; ++b) {
       tc::mbar_init(bar_acc + 8 * b, 1);
       tc::mbar_init(bar_free + 8 * b, kEpiWarps);
     }
@@ -244,7 +245,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           if (!ok) break;
           tc::mma_commit(bar_acc + 8 * buf);
-          if (++buf == 2) buf = 0, free_phase ^= 1;
+          if (++buf == kBufs) buf = 0, free_phase ^= 1;
         }
       }
     }
@@ -278,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc::tc_fence_before();
         __syncwarp();
         if (lane == 0 && !(q.waits.test_fault && w == 0 && quarter == 0)) tc::mbar_arrive(bar_free + 8 * buf);
-        if (++buf == 2) buf = 0, phase ^= 1;
+        if (++buf == kBufs) buf = 0, phase ^= 1;
       }
       if (!ok) break;
       if (marks[tile % kMarks] == tile + 1) {

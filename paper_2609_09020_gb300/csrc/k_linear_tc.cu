@@ -181,7 +181,7 @@ constexpr ShapeCost kShape64{64, 1, 2 * kSms, 4.2, 0.20, 3.0};
 constexpr ShapeCost kShape128{128, 1, kSms, 4.5, 0.19, 2.2};
 constexpr ShapeCost kShape256{256, 2, kSms / 2, 6.8, 0.26, 3.4};
 constexpr ShapeCost kShapeReg{kRegCols, 1, kSms, 6.0, 1.7, 4.0};
-constexpr ShapeCost kShapePlanes{kPlCols, 2, kSms / 2, 8.0, 0.85, 3.4};
+constexpr ShapeCost kShapePlanes{kPlCols, 2, kSms / 2, 8.0, 0.95, 3.4};
 
 // The shape and the number of parts of K with the least estimated time, parts at
 // least `least` slices long: rounds of tiles, and for parts the second kernel, which
@@ -258,17 +258,18 @@ PFN_cuTensorMapEncodeTiled_v12000 encoder() {
   return fn;
 }
 
-// The three planes of a matrix, in boxes of 64 columns, box_rows rows and all planes.
-bool encode_planes(CUtensorMap* map, const void* m, long long rows, long long cols, long long ld, int box_rows) {
+// The three planes of a matrix, in boxes of box_cols columns (64, 128-byte swizzled,
+// or 32, 64-byte swizzled), box_rows rows and all planes.
+bool encode_planes(CUtensorMap* map, const void* m, long long rows, long long cols, long long ld, int box_cols, int box_rows) {
   const PFN_cuTensorMapEncodeTiled_v12000 enc = encoder();
   if (!enc) return false;
   const cuuint64_t dim[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), 3};
   const cuuint64_t stride[2] = {static_cast<cuuint64_t>(ld * 2), static_cast<cuuint64_t>(rows * ld * 2)};
-  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_rows), 3};
+  const cuuint32_t box[3] = {static_cast<cuuint32_t>(box_cols), static_cast<cuuint32_t>(box_rows), 3};
   const cuuint32_t elem[3] = {1, 1, 1};
   return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(m), dim, stride, box, elem,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+             CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // The operands where TMA can read them: as they are, or laid out in the workspace.
@@ -382,12 +383,14 @@ int tc_product(const Product& p, int dtype, void* ws, const Waits& waits, cudaSt
     o.vec_a = vec(p.a, r.a), o.vec_b = vec(p.b, r.b);
   } else if (r.planes) {
     CutMatrix m[2];
-    const auto add = [&](CutMatrix& c, const void* from, const Operand& x, char* at, PlOperand& out, CUtensorMap* map, int box) {
+    const auto add = [&](CutMatrix& c, const void* from, const Operand& x, char* at, PlOperand& out, CUtensorMap* map, int tile) {
       c = {static_cast<const float*>(from), x.ld, x.rows, x.cols, at, x.ld_packed, reinterpret_cast<int*>(at + planes_bytes(x))};
       out = {c.m, x.ld, c.marks, static_cast<int>(mark_cols(x))};
-      return encode_planes(map, at, x.rows, x.cols, x.ld_packed, box);
+      // 32 of K: along K a box of the CTA's rows, else blocks of 64 rows
+      return x.mn ? encode_planes(map, at, x.rows, x.cols, x.ld_packed, 64, 32)
+                  : encode_planes(map, at, x.rows, x.cols, x.ld_packed, 32, tile);
     };
-    ok = add(m[0], p.a, r.a, w, pl.a, &maps.a, r.a.mn ? 64 : 128) &&
+    ok = add(m[0], p.a, r.a, w, pl.a, &maps.a, 128) &&
          add(m[1], p.b, r.b, w + r.a_bytes, pl.b, &maps.b, 64) && cut_planes(m, s) == PIC_OK;
   } else {
     // of an operand that lies along its rows a box is 64 of them by 64 of K

@@ -97,6 +97,17 @@ __device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t saddr, uint32_t lbo
   return d;
 }
 
+// The same with the 64-byte swizzle, K-major: rows of 32 16-bit values of K, 512
+// bytes from one group of 8 rows to the next.
+__device__ __forceinline__ uint64_t smem_desc_sw64(uint32_t saddr) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>(512 >> 4) << 32;
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= static_cast<uint64_t>(4) << 61;  // layout type: 64-byte swizzle
+  return d;
+}
+
 // Instruction descriptor, kind::f16, fp32 D.  bf16: A and B are bfloat16, else
 // half; a_mn, b_mn: the operand is MN-major.
 __host__ __device__ constexpr uint32_t idesc_16(int M, int N, bool bf16, bool a_mn, bool b_mn) {
