@@ -9,13 +9,13 @@
 // the three left out are below 3 x 2^-24 of the product.  Six MMAs of bfloat16 at
 // 2.25 PFLOP/s nominal are 375 TFLOP/s of fp32, five times what the FP32 cores do.
 //
-// A tensor core truncates when it adds to an accumulator.  So within the K of a
-// stage the products of small pieces come first (cut_a, cut_b), which leaves few
+// A tensor core truncates when it adds to an accumulator.  So within a slice of 64
+// of K the products of small pieces come first (cut_a, cut_b), which leaves few
 // truncations at the sum's full size, and after every 128 of K the accumulators are
 // taken over into registers and added there to nearest.  Measured on 2048 x 1024 ->
 // 4096 (root mean square error, relative): 2.1e-6 with all products of 16 of K
 // together and takeovers every 256; 7e-7 as it is; 1.6e-7 with takeovers every 64,
-// which take a fifth more time; fp32 FMAs in order give 6.2e-7.
+// which take a quarter more time; fp32 FMAs in order give 6.2e-7.
 #pragma once
 
 #include <cstdint>

@@ -7,9 +7,10 @@
 //   warp 0      one thread keeps a ring of STAGES slices of A and B (64 of K)
 //               filled by TMA; what lies outside the matrices reads as zero
 //   warp 1      one thread issues the MMAs, 16 of K each
-//   the others  the epilogue (8 warps, 4 for 64 columns): accumulators, bias, pre, activation, residual,
-//               rounding, and out through shared memory and TMA stores (or
-//               plain stores where rows do not start on 16-byte boundaries)
+//   the others  the epilogue (8 warps, 4 for 64 columns): accumulators, bias, pre,
+//               activation, residual, rounding, and out through shared memory: by
+//               TMA where rows start and end on 16-byte boundaries, in one run
+//               where narrow rows lie end to end, else by plain stores
 // There are two sets of accumulators, so that a tile's epilogue runs under the
 // next tile's MMAs.  An operand may be contiguous along K or along its rows
 // (dz and x in dw = dz^T x): TMA then brings blocks of 64 rows x 64 of K and
@@ -252,13 +253,13 @@ __device__ __forceinline__ void put_panel(const uint32_t (&v)[32], uint32_t buf,
   if (lane == 0) tc::bulk_commit();  // an empty group: every panel has one, so that waits can count them
 }
 
-// 128 bytes of columns of a warp's 32 rows of a residual, loaded before they are
+// 64 columns of a warp's 32 rows of a residual of a 16-bit type, loaded before they are
 // wanted: where rows lie on 16-byte boundaries each lane has its own row's; where
 // the rows are one run of memory, 16 bytes here and there of it; else word `lane`
 // of every row.
 template <typename T>
 struct Residual {
-  static constexpr int kCols = 128 / sizeof(T);
+  static constexpr int kCols = 64;
   uint32_t w[32];
   int mode;  // 0: this lane's row, 1: a run, 2: a word of every row
   int n;     // columns that exist
@@ -284,23 +285,17 @@ struct Residual {
         w[4 * c] = q.x, w[4 * c + 1] = q.y, w[4 * c + 2] = q.z, w[4 * c + 3] = q.w;
       }
     } else {
-      if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int r = 0; r < 32; ++r, o += p.ldr)
-          w[r] = load_if(reinterpret_cast<const uint32_t*>(o) + lane, r < rows && lane < n);
-      } else {
+      for (int half = 0; half < 32; half += 16) {
+        uint32_t high[16];
 #pragma unroll
-        for (int half = 0; half < 32; half += 16) {
-          uint32_t high[16];
-#pragma unroll
-          for (int r = 0; r < 16; ++r, o += p.ldr) {
-            const uint16_t* h = reinterpret_cast<const uint16_t*>(o) + 2 * lane;
-            w[half + r] = load_if(h, half + r < rows && 2 * lane < n);
-            high[r] = load_if(h + 1, half + r < rows && 2 * lane + 1 < n);
-          }
-#pragma unroll
-          for (int r = 0; r < 16; ++r) w[half + r] |= high[r] << 16;
+        for (int r = 0; r < 16; ++r, o += p.ldr) {
+          const uint16_t* h = reinterpret_cast<const uint16_t*>(o) + 2 * lane;
+          w[half + r] = load_if(h, half + r < rows && 2 * lane < n);
+          high[r] = load_if(h + 1, half + r < rows && 2 * lane + 1 < n);
         }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w[half + r] |= high[r] << 16;
       }
     }
   }
@@ -313,11 +308,11 @@ struct Residual {
         tc::sts128(buf + (c * 32 + lane) * 16, w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
       __syncwarp();
       const uint32_t row = buf + lane * n * sizeof(T);
-      if (sizeof(T) == 4 || n % 2 == 0) {
+      if (n % 2 == 0) {
 #pragma unroll
         for (int c = 0; c < 32; ++c) {
           w[c] = 0;
-          if (c * static_cast<int>(4 / sizeof(T)) < n) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[c]) : "r"(row + 4 * c) : "memory");
+          if (2 * c < n) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[c]) : "r"(row + 4 * c) : "memory");
         }
       } else {
 #pragma unroll
@@ -345,40 +340,31 @@ struct Residual {
     }
 #pragma unroll
     for (int c = 0; c < 32; ++c) {
-      if constexpr (sizeof(T) == 4) {
-        v[c] += __uint_as_float(w[c]);
-      } else {
-        const float2 f = unpack2_16<T>(w[c]);
-        v[2 * c] += f.x;
-        v[2 * c + 1] += f.y;
-      }
+      const float2 f = unpack2_16<T>(w[c]);
+      v[2 * c] += f.x;
+      v[2 * c + 1] += f.y;
     }
   }
 };
 
-// Adds 64 columns (or those of them that exist) of the bias or of a residual row to v.
-template <typename T, int N = 64>
-__device__ __forceinline__ void add_row(float (&v)[N], const T* r, int cols) {
-  constexpr int kVec = 16 / sizeof(T);
-  if (cols >= N && (reinterpret_cast<uintptr_t>(r) & 15) == 0) {
+// Adds 64 columns (or those of them that exist) of the bias to v.
+template <typename T>
+__device__ __forceinline__ void add_row(float (&v)[64], const T* r, int cols) {
+  if (cols >= 64 && (reinterpret_cast<uintptr_t>(r) & 15) == 0) {
 #pragma unroll
-    for (int c = 0; c < N / kVec; ++c) {
-      const uint4 q = *reinterpret_cast<const uint4*>(r + kVec * c);
+    for (int c = 0; c < 8; ++c) {
+      const uint4 q = *reinterpret_cast<const uint4*>(r + 8 * c);
       const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if constexpr (sizeof(T) == 4) {
-          v[4 * c + e] += __uint_as_float(w[e]);
-        } else {
-          const float2 f = unpack2_16<T>(w[e]);
-          v[8 * c + 2 * e] += f.x;
-          v[8 * c + 2 * e + 1] += f.y;
-        }
+        const float2 f = unpack2_16<T>(w[e]);
+        v[8 * c + 2 * e] += f.x;
+        v[8 * c + 2 * e + 1] += f.y;
       }
     }
   } else {
 #pragma unroll
-    for (int c = 0; c < N; ++c)
+    for (int c = 0; c < 64; ++c)
       if (c < cols) v[c] += to_f32(r[c]);
   }
 }
@@ -389,7 +375,7 @@ __device__ __forceinline__ void add_row(float (&v)[N], const T* r, int cols) {
 // A warp or two of an SM's quarter do this for every tile, so it counts instructions:
 // pointers move by a row, whole tiles ask for no row's existence, and a column of a
 // residual's 32 loads are under way together.
-constexpr int kTurnStride = 65;  // floats: no bank conflicts either way
+constexpr int kTurnStride = 33;  // floats, 32 columns at a time: no bank conflicts either way
 constexpr int kTurnBytes = 32 * kTurnStride * 4;
 
 // One column (of every lane) down the rows.
@@ -425,24 +411,26 @@ __device__ __forceinline__ void finish_column(const Product& p, const float* tur
 
 __device__ __forceinline__ void finish_rows(const float (&v)[64], const Product& p, float* turn, int lane, long long row0,
                                             long long col0) {
-  __syncwarp();
-#pragma unroll
-  for (int c = 0; c < 64; ++c) turn[lane * kTurnStride + c] = v[c];
-  __syncwarp();
   const int rows = static_cast<int>(min(32LL, p.I - row0));
-#pragma unroll 1
-  for (int c = lane; c < 64; c += 32) {
-    if (col0 + c >= p.J) break;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (col0 + 32 * h >= p.J) break;
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 32; ++c) turn[lane * kTurnStride + c] = v[32 * h + c];
+    __syncwarp();
+    const long long col = col0 + 32 * h + lane;
+    if (col >= p.J) continue;
     float q[32] = {};
     if (p.residual) {
-      const float* res = static_cast<const float*>(p.residual) + row0 * p.ldr + col0 + c;
+      const float* res = static_cast<const float*>(p.residual) + row0 * p.ldr + col;
 #pragma unroll
       for (int r = 0; r < 32; ++r, res += p.ldr) q[r] = __uint_as_float(load_if(reinterpret_cast<const uint32_t*>(res), r < rows));
     }
     if (rows == 32)
-      finish_column<true>(p, turn, c, row0, col0 + c, rows, q);
+      finish_column<true>(p, turn, lane, row0, col, rows, q);
     else
-      finish_column<false>(p, turn, c, row0, col0 + c, rows, q);
+      finish_column<false>(p, turn, lane, row0, col, rows, q);
   }
 }
 
