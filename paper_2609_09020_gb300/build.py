@@ -25,6 +25,8 @@ SOURCES = ["pic_decode.cu", "k_fp32.cu", "k_fp32_any.cu", "k_fp32_sweep.cu", "k_
            "k_linear_grad.cu", "k_linear_tc.cu", "k_linear_tc_f16.cu",
            "k_linear_tc_bf16.cu", "k_linear_reg.cu",
            "k_linear_planes.cu", "k_linear_narrow.cu", "k_linear_few.cu", "k_linear_few32.cu",
+           "k_linear_thin.cu", "k_linear_thin_f16.cu", "k_linear_thin_bf16.cu",
+           "k_linear_thin_f32.cu",
            "k_linear_outer.cu", "k_clip.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",

@@ -135,7 +135,7 @@ struct Vec16 {
       if constexpr (sizeof(T) == 4) {
         f[i] = __uint_as_float(w[i]);
       } else {
-        const float2 v = unpack2_16<T>(w[i]);
+        const float2 v = unpack2_of<T>(w[i]);
         f[2 * i] = v.x;
         f[2 * i + 1] = v.y;
       }
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             times_act_grad<sizeof(T) == 4, S::kPer>(d, v, g.act);
             uint32_t w[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = pack2_16<T>(d[2 * i], d[2 * i + 1]);
+            for (int i = 0; i < 4; ++i) w[i] = pack2_of<T>(d[2 * i], d[2 * i + 1]);
             put_vec<T>(sdz, S::kBlockBytes, S::kPlaneBytes, row + u * S::kPassRows, col, w);
           }
 #pragma unroll
@@ -379,7 +379,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if constexpr (sizeof(T) == 4)
               vy[u].w[i] = __float_as_uint(d[i]);
             else
-              vy[u].w[i] = pack2_16<T>(d[2 * i], d[2 * i + 1]);
+              vy[u].w[i] = pack2_of<T>(d[2 * i], d[2 * i + 1]);
           }
         }
         if (unit == 0) ok = __all_sync(0xffffffffu, wait(bar_empty + 8 * s, phase ^ 1));
@@ -564,7 +564,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if constexpr (sizeof(T) == 4)
               out[c] = r[32 * h + c];
             else
-              out[c] = pack2_16<T>(__uint_as_float(r[2 * c]), __uint_as_float(r[2 * c + 1]));
+              out[c] = pack2_of<T>(__uint_as_float(r[2 * c]), __uint_as_float(r[2 * c + 1]));
           }
           if (lane == 0) tc::bulk_wait_read<S::kPanels - 1>();
           __syncwarp();

@@ -118,42 +118,8 @@ __device__ __forceinline__ void tile_place(long long t, long long tiles_i, long 
 }
 
 template <typename T>
-struct IsHalf {
-  static constexpr bool value = false;
-};
-template <>
-struct IsHalf<__half> {
-  static constexpr bool value = true;
-};
-
-template <typename T>
-__device__ __forceinline__ uint32_t pack2_16(float lo, float hi);
-template <>
-__device__ __forceinline__ uint32_t pack2_16<__half>(float lo, float hi) {
-  return tc::pack_f16x2(lo, hi);
-}
-template <>
-__device__ __forceinline__ uint32_t pack2_16<__nv_bfloat16>(float lo, float hi) {
-  uint32_t d;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-  return d;
-}
-template <typename T>
-__device__ __forceinline__ float2 unpack2_16(uint32_t v) {
-  return make_float2(0.0f, 0.0f);
-}
-template <>
-__device__ __forceinline__ float2 unpack2_16<__half>(uint32_t v) {
-  return __half22float2(*reinterpret_cast<const __half2*>(&v));
-}
-template <>
-__device__ __forceinline__ float2 unpack2_16<__nv_bfloat16>(uint32_t v) {
-  return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
-}
-
-template <typename T>
 __device__ __forceinline__ uint32_t idesc_of(int M, int N, bool a_mn, bool b_mn) {
-  return tc::idesc_16(M, N, !IsHalf<T>::value, a_mn, b_mn);
+  return tc::idesc_16(M, N, !std::is_same<T, __half>::value, a_mn, b_mn);
 }
 
 // Word `i` of row r of a panel buffer.
@@ -340,7 +306,7 @@ struct Residual {
     }
 #pragma unroll
     for (int c = 0; c < 32; ++c) {
-      const float2 f = unpack2_16<T>(w[c]);
+      const float2 f = unpack2_of<T>(w[c]);
       v[2 * c] += f.x;
       v[2 * c + 1] += f.y;
     }
@@ -357,7 +323,7 @@ __device__ __forceinline__ void add_row(float (&v)[64], const T* r, int cols) {
       const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float2 f = unpack2_16<T>(w[e]);
+        const float2 f = unpack2_of<T>(w[e]);
         v[8 * c + 2 * e] += f.x;
         v[8 * c + 2 * e + 1] += f.y;
       }
@@ -664,7 +630,7 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
         uint32_t out[32];
         if (p.pre) {
 #pragma unroll
-          for (int c = 0; c < 32; ++c) out[c] = pack2_16<T>(v[2 * c], v[2 * c + 1]);
+          for (int c = 0; c < 32; ++c) out[c] = pack2_of<T>(v[2 * c], v[2 * c + 1]);
           if (lane == 0) tc::bulk_wait_read<S::kPanels - 1>();  // the buffer's last store has been read
           __syncwarp();
           put_panel<T>(out, panels + pb * kPanelBytes, lane, row0, j0 + c0, p, p.pre, p.ldpre, &maps.pre, q.store_tma);
@@ -688,7 +654,7 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
           res.add(v, panels + pb * kPanelBytes, lane);
         }
 #pragma unroll
-        for (int c = 0; c < 32; ++c) out[c] = pack2_16<T>(v[2 * c], v[2 * c + 1]);
+        for (int c = 0; c < 32; ++c) out[c] = pack2_of<T>(v[2 * c], v[2 * c + 1]);
         put_panel<T>(out, panels + pb * kPanelBytes, lane, row0, j0 + c0, p, p.y, p.ldy, &maps.y, q.store_tma);
         if (++pb == S::kPanels) pb = 0;
       }

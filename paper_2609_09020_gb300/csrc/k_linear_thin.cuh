@@ -1,0 +1,465 @@
+// k_linear_thin.cuh -- products of at most 128 columns over at most 128 of K: a
+// layer of a synthesis net over the pixels of an image.  y and x are all that
+// there is to move, a few hundred bytes a row against some thousand operations, so
+// the kernel is a stream: a warp takes 16 rows at a time, by itself, from memory
+// straight into the fragments of warp-level MMAs (m16n8k16) and from their
+// accumulators straight back.  The weights, in the order of the fragments, are in
+// shared memory.  (Tiles of 128 rows through TMA, tensor memory and panels cost a
+// CTA some 3 us each for 14 KB, and rows off 16-byte boundaries a copy before.)
+//
+// Which of K's elements a lane holds in which fragment is free as long as both
+// operands agree, and so is which column a fragment's column is.  So a lane has 16
+// bytes in a row of x in each load, four lanes the row's next 64 bytes; and a lane
+// ends up with neighbouring columns of y (16 bytes, 8 for the last 16 columns of a
+// 16-bit type).  Rows of x off 16-byte boundaries: the two aligned pieces that
+// have the 16 bytes, shifted (a piece that has an element of the row is in the
+// row's allocation).  Rows of y, pre and the residual off them: if they lie end to
+// end the warp's 16 rows are a run on a boundary, turned in shared memory; else
+// element by element.
+//
+// fp32 values are cut into three bfloat16 pieces (cut3.cuh) in registers, with six
+// MMAs for every 16 of K; rows with an infinite or NaN value, or any if a weight is
+// one, are computed again with FP32 FMAs.
+//
+// While a step (128 bytes of each row) is multiplied, the next, of this tile or the
+// warp's next, is on its way.
+#pragma once
+
+#include "cut3.cuh"
+#include "linear.cuh"
+#include "linear_ptx.cuh"
+
+namespace pic {
+namespace lin {
+
+constexpr int kThinMost = 128;  // columns, and K
+constexpr int kThinThreads = 256, kThinWarps = kThinThreads / 32, kThinRows = 16;
+
+enum ThinMode { kThinVector = 0, kThinRun = 1, kThinElements = 2 };
+
+struct ThinParams {
+  Product p;
+  int steps, pieces;        // of 128 and 64 bytes along K
+  int y_mode, pre_mode, res_mode;  // a FAST kernel's are kThinVector
+  int panel_at, panel_bytes;  // a warp's 16 rows in shared memory, where a mode is kThinRun
+  long long tiles;
+};
+
+// Groups of neighbouring columns: 32 of a 16-bit type (the last may have 16), 16 of fp32.
+template <typename T, int NT>
+struct ThinShape {
+  static constexpr int kElem = static_cast<int>(sizeof(T));
+  static constexpr bool kWide = kElem == 4;
+  static constexpr int kGroup = kWide ? 2 : 4;  // MMA columns of 8 in a group
+  static constexpr int kGroups = (NT + kGroup - 1) / kGroup;
+  static constexpr int kPiece = 16 / kElem;  // elements of a load
+  // a lane's weights for a piece and 8 columns: 8 of a 16-bit type, or 3 x 4 pieces of bfloat16
+  static constexpr int kWords = kWide ? 6 : 4;
+  static constexpr int kStepBytes = 2 * NT * 32 * kWords * 4;
+  __host__ __device__ static constexpr int in_group(int g) { return NT - g * kGroup < kGroup ? NT - g * kGroup : kGroup; }
+  // first column of lane group t in group g, and what MMA column nn of MMA tile j is
+  __device__ static int column(int g, int t) { return g * kGroup * 8 + 2 * in_group(g) * t; }
+  __device__ static int column_of(int j, int nn) {
+    const int g = j / kGroup;
+    return column(g, nn / 2) + 2 * (j - g * kGroup) + nn % 2;
+  }
+};
+
+__device__ __forceinline__ uint4 thin_load(const void* p, bool on) {
+  uint4 v;
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %5, 0;\n\tmov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t"
+      "@q ld.global.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+      : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+      : "l"(p), "r"(static_cast<uint32_t>(on)));
+  return v;
+}
+
+template <typename T>
+__device__ __forceinline__ void thin_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+  if constexpr (sizeof(T) == 2 && !std::is_same<T, __nv_bfloat16>::value)
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// A lane's 16 bytes of a row as loaded: one aligned piece (FAST), or the two that have them.
+template <bool FAST>
+struct ThinPiece {
+  uint4 lo, hi;
+  __device__ __forceinline__ void load(const char* at, int bytes) {  // bytes of the row from `at` on, may be <= 0
+    if constexpr (FAST) {
+      lo = thin_load(at, bytes > 0);
+    } else {
+      const int m = static_cast<int>(reinterpret_cast<uintptr_t>(at) & 15);
+      lo = thin_load(at - m, bytes > 0);
+      hi = thin_load(at - m + 16, m + min(bytes, 16) > 16);
+    }
+  }
+  // the 16 bytes from byte `m` of the two on
+  template <typename T>
+  __device__ __forceinline__ void get(int m, uint32_t (&w)[4]) const {
+    if constexpr (FAST) {
+      w[0] = lo.x, w[1] = lo.y, w[2] = lo.z, w[3] = lo.w;
+    } else {
+      const uint32_t v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+      const bool by2 = (m & 8) != 0, by1 = (m & 4) != 0;
+      uint32_t u[6], s[5];
+#pragma unroll
+      for (int i = 0; i < 6; ++i) u[i] = by2 ? v[i + 2] : v[i];
+#pragma unroll
+      for (int i = 0; i < 5; ++i) s[i] = by1 ? u[i + 1] : u[i];
+      const uint32_t bits = (m & 2) * 8;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = sizeof(T) == 4 ? s[i] : __funnelshift_r(s[i], s[i + 1], bits);
+    }
+  }
+};
+
+// Keeps `bytes` bytes of w, from its beginning.
+template <typename T>
+__device__ __forceinline__ void thin_keep(uint32_t (&w)[4], int bytes) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    w[i] = bytes >= 4 * i + 4 ? w[i] : sizeof(T) == 2 && bytes >= 4 * i + 2 ? w[i] & 0xffffu : 0u;
+}
+
+// The sums of a lane's places, on the FP32 cores.
+template <int NT>
+__device__ __noinline__ void thin_again(const Product& p, long long row, int t, float* u) {
+  using S = ThinShape<float, NT>;
+  const float *a = static_cast<const float*>(p.a), *b = static_cast<const float*>(p.b);
+  for (int e = 0; e < NT * 4; ++e) {
+    const long long i = row + (e & 2) * 4, j = S::column_of(e >> 2, 2 * t + (e & 1));
+    float s = 0.0f;
+    if (i < p.I && j < p.J)
+      for (long long k = 0; k < p.K; ++k) s = fmaf(a[i * p.a_i + k], b[j * p.b_j + k * p.b_k], s);
+    u[e] = s;
+  }
+}
+
+// CTAs on an SM: what the registers of a kernel with NT x 8 columns leave room for.
+template <typename T, int NT, bool FAST>
+constexpr int thin_ctas() {
+  if (sizeof(T) == 4) return NT <= 8 ? 2 : 1;
+  return NT <= 4 ? (FAST ? 4 : 3) : NT <= 8 ? (FAST ? 3 : 2) : FAST ? 2 : 1;
+}
+
+// FAST: rows of every matrix on 16-byte boundaries, and J a multiple of 16 bytes.
+template <typename T, int NT, bool FAST>
+__global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_kernel(const __grid_constant__ ThinParams q) {
+  using S = ThinShape<T, NT>;
+  constexpr int E = S::kElem;
+  extern __shared__ __align__(16) uint8_t thin_smem[];
+  __shared__ float bias[NT * 8];
+  const Product& p = q.p;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int J = static_cast<int>(p.J), K = static_cast<int>(p.K);
+
+  // the weights, zero outside
+  uint32_t* frag = reinterpret_cast<uint32_t*>(thin_smem);
+  bool bad_w = false;
+  for (int e = threadIdx.x; e < q.steps * 2 * NT * 32; e += kThinThreads) {
+    const int l = e & 31, j = e / 32 % NT, piece = e / 32 / NT;
+    const int n = S::column_of(j, l >> 2), k0 = piece * (S::kPiece * 4) + (l & 3) * S::kPiece;
+    const T* w = static_cast<const T*>(p.b) + n * p.b_j + k0 * p.b_k;
+    if constexpr (S::kWide) {
+      uint32_t v[4], o[6];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = load_if(reinterpret_cast<const uint32_t*>(w + i * p.b_k), n < p.J && k0 + i < K);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) bad_w |= (v[i] & 0x7fffffffu) >= 0x7f800000u;
+      cut3(v[0], v[1], o[0], o[2], o[4]);
+      cut3(v[2], v[3], o[1], o[3], o[5]);
+      uint2* out = reinterpret_cast<uint2*>(frag) + ((piece * NT + j) * 3) * 32 + l;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) out[i * 32] = make_uint2(o[2 * i], o[2 * i + 1]);
+    } else {
+      uint32_t v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = load_if(reinterpret_cast<const uint16_t*>(w + i * p.b_k), n < p.J && k0 + i < K);
+      reinterpret_cast<uint4*>(frag)[e] =
+          make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+    }
+  }
+  for (int e = threadIdx.x; e < NT * 8; e += kThinThreads) {
+    const int n = S::column_of(e / 8, e % 8);
+    bias[e] = p.bias && n < p.J ? to_f32(static_cast<const T*>(p.bias)[n]) : 0.0f;
+  }
+  bad_w = __syncthreads_or(bad_w);
+
+  const long long first = blockIdx.x * static_cast<long long>(kThinWarps) + warp;
+  const long long stride = gridDim.x * static_cast<long long>(kThinWarps);
+  const char* a = static_cast<const char*>(p.a);
+  const long long lda = p.a_i * E;
+  const int k_bytes = K * E;
+  uint8_t* panel = thin_smem + q.panel_at + warp * q.panel_bytes;
+
+  ThinPiece<FAST> next[2][2];  // rows g and g + 8; the pieces of a step
+  const auto fetch = [&](long long tile, int step) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const long long row = tile * kThinRows + g + 8 * h;
+      const char* r = a + row * lda;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int at = step * 128 + c * 64 + t * 16;
+        next[h][c].load(r + at, row < p.I ? k_bytes - at : 0);
+      }
+    }
+  };
+  if (first < q.tiles) fetch(first, 0);
+  for (long long tile = first; tile < q.tiles; tile += stride) {
+    const long long row0 = tile * kThinRows, row = row0 + g;
+    float acc[NT][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[j][e] = 0.0f;
+    uint32_t res[2][NT * E / 2];
+    bool bad = bad_w;
+    for (int step = 0; step < q.steps; ++step) {
+      uint32_t x[2][2][4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int m = FAST ? 0 : static_cast<int>(reinterpret_cast<uintptr_t>(a + (row + 8 * h) * lda) & 15);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          next[h][c].template get<T>(m, x[h][c]);
+          const int left = k_bytes - (step * 128 + c * 64 + t * 16);
+          if (step == q.steps - 1) thin_keep<T>(x[h][c], row + 8 * h < p.I ? left : 0);
+        }
+      }
+      const bool last = step + 1 == q.steps;
+      const long long next_tile = last ? tile + stride : tile;
+      if (next_tile < q.tiles) fetch(next_tile, last ? 0 : step + 1);
+      if (last && p.residual) {
+        // the residual: each lane's places, or 16 bytes here and there of the run
+        const T* r = static_cast<const T*>(p.residual);
+        if (!FAST && q.res_mode == kThinRun && row0 + kThinRows <= p.I) {
+          const uint4* v = reinterpret_cast<const uint4*>(r + row0 * p.J);
+          const int count = kThinRows * J * E / 16;
+#pragma unroll
+          for (int i = 0; i < NT * E / 4; ++i) {
+            const uint4 w = thin_load(v + i * 32 + lane, i * 32 + lane < count);
+            uint32_t* o = &res[0][0] + 4 * i;
+            o[0] = w.x, o[1] = w.y, o[2] = w.z, o[3] = w.w;
+          }
+        } else {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int gi = 0; gi < S::kGroups; ++gi) {
+              constexpr int G = S::kGroup;
+              const int cols = 2 * S::in_group(gi), col = S::column(gi, t);
+              const T* at = r + (row + 8 * h) * p.ldr + col;
+              uint32_t* o = &res[h][gi * G * E / 2];
+              const bool there = row + 8 * h < p.I && (!FAST || col < J);
+              if (FAST || (q.res_mode == kThinVector && col + cols <= J)) {
+                if (cols * E == 16) {
+                  const uint4 w = thin_load(at, there);
+                  o[0] = w.x, o[1] = w.y, o[2] = w.z, o[3] = w.w;
+                } else {
+                  o[0] = load_if(reinterpret_cast<const uint32_t*>(at), there);
+                  o[1] = load_if(reinterpret_cast<const uint32_t*>(at) + 1, there);
+                }
+              } else {
+#pragma unroll
+                for (int i = 0; i < cols * E / 4; ++i) {
+                  if constexpr (S::kWide) {
+                    o[i] = load_if(reinterpret_cast<const uint32_t*>(at) + i, there && col + i < J);
+                  } else {
+                    const uint16_t* u = reinterpret_cast<const uint16_t*>(at) + 2 * i;
+                    o[i] = load_if(u, there && col + 2 * i < J) |
+                           load_if(u + 1, there && col + 2 * i + 1 < J) << 16;
+                  }
+                }
+              }
+            }
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        if (step * 2 + c >= q.pieces) break;
+        if constexpr (S::kWide) {
+          uint32_t y[2][6];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) bad |= (x[h][c][i] & 0x7fffffffu) >= 0x7f800000u;
+            cut3(x[h][c][0], x[h][c][1], y[h][0], y[h][2], y[h][4]);
+            cut3(x[h][c][2], x[h][c][3], y[h][1], y[h][3], y[h][5]);
+          }
+          const uint2* b = reinterpret_cast<const uint2*>(frag) + (step * 2 + c) * NT * 3 * 32 + lane;
+#pragma unroll
+          for (int j = 0; j < NT; j += 2) {
+            uint2 w[2][3];
+#pragma unroll
+            for (int i = 0; i < 6; ++i) w[i / 3][i % 3] = b[(j * 3 + i) * 32];
+#pragma unroll
+            for (int k = 0; k < 6; ++k)
+#pragma unroll
+              for (int jj = 0; jj < 2; ++jj)
+                thin_mma<T>(acc[j + jj], y[0][2 * cut_a(k)], y[1][2 * cut_a(k)], y[0][2 * cut_a(k) + 1],
+                            y[1][2 * cut_a(k) + 1], w[jj][cut_b(k)].x, w[jj][cut_b(k)].y);
+          }
+        } else {
+          const uint4* b = reinterpret_cast<const uint4*>(frag) + (step * 2 + c) * NT * 32 + lane;
+#pragma unroll
+          for (int j = 0; j < NT; ++j) {
+            const uint4 w = b[j * 32];
+            thin_mma<T>(acc[j], x[0][c][0], x[1][c][0], x[0][c][1], x[1][c][1], w.x, w.y);
+            thin_mma<T>(acc[j], x[0][c][2], x[1][c][2], x[0][c][3], x[1][c][3], w.z, w.w);
+          }
+        }
+      }
+    }
+    if constexpr (S::kWide) {
+      if (__any_sync(0xffffffffu, bad)) {
+        float u[NT * 4];
+        thin_again<NT>(p, row, t, u);
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[j][e] = u[4 * j + e];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const float2 b = *reinterpret_cast<const float2*>(bias + j * 8 + 2 * t);
+      acc[j][0] += b.x, acc[j][1] += b.y, acc[j][2] += b.x, acc[j][3] += b.y;
+    }
+    // this lane's places of the 16 rows, rounded
+    const auto put = [&](void* out, long long ld, int mode) {
+      const bool run = !FAST && mode == kThinRun && row0 + kThinRows <= p.I;
+      if (run) __syncwarp();
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int gi = 0; gi < S::kGroups; ++gi) {
+          const int cols = 2 * S::in_group(gi), col = S::column(gi, t);
+          uint32_t w[4];
+#pragma unroll
+          for (int i = 0; i < cols / 2; ++i) {
+            const float u = acc[gi * S::kGroup + i][2 * h], v = acc[gi * S::kGroup + i][2 * h + 1];
+            if constexpr (S::kWide)
+              w[2 * i] = __float_as_uint(u), w[2 * i + 1] = __float_as_uint(v);
+            else
+              w[i] = pack2_of<T>(u, v);
+          }
+          if (run) {
+            uint8_t* o = panel + ((g + 8 * h) * J + col) * E;
+#pragma unroll
+            for (int i = 0; i < cols; ++i) {
+              if (col + i >= J) continue;
+              if constexpr (S::kWide)
+                reinterpret_cast<uint32_t*>(o)[i] = w[i];
+              else
+                reinterpret_cast<uint16_t*>(o)[i] = static_cast<uint16_t>(w[i / 2] >> (i % 2 * 16));
+            }
+            continue;
+          }
+          if (row + 8 * h >= p.I || col >= J) continue;
+          T* o = static_cast<T*>(out) + (row + 8 * h) * ld + col;
+          if (FAST || (mode == kThinVector && col + cols <= J)) {
+            if (cols * E == 16)
+              *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
+            else
+              *reinterpret_cast<uint2*>(o) = make_uint2(w[0], w[1]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < cols; ++i) {
+              if (col + i >= J) continue;
+              if constexpr (S::kWide)
+                reinterpret_cast<uint32_t*>(o)[i] = w[i];
+              else
+                reinterpret_cast<uint16_t*>(o)[i] = static_cast<uint16_t>(w[i / 2] >> (i % 2 * 16));
+            }
+          }
+        }
+      if (run) {
+        __syncwarp();
+        const int count = kThinRows * J * E / 16;
+        uint4* o = reinterpret_cast<uint4*>(static_cast<T*>(out) + row0 * p.J);
+        for (int i = lane; i < count; i += 32) o[i] = reinterpret_cast<const uint4*>(panel)[i];
+      }
+    };
+    if (p.pre) put(p.pre, p.ldpre, q.pre_mode);
+    if (p.act != PIC_ACT_NONE) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[j][e] = act_value<S::kWide>(acc[j][e], p.act);
+    }
+    if (p.residual) {
+      if (!FAST && q.res_mode == kThinRun && row0 + kThinRows <= p.I) {
+        __syncwarp();
+        const int count = kThinRows * J * E / 16;
+#pragma unroll
+        for (int i = 0; i < NT * E / 4; ++i) {
+          const uint32_t* o = &res[0][0] + 4 * i;
+          if (i * 32 + lane < count)
+            reinterpret_cast<uint4*>(panel)[i * 32 + lane] = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int col = S::column_of(j, 2 * t + e);
+              if (col < J)
+                acc[j][2 * h + e] += to_f32(reinterpret_cast<const T*>(panel)[(g + 8 * h) * J + col]);
+            }
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) {
+            if constexpr (S::kWide) {
+              acc[j][2 * h] += __uint_as_float(res[h][2 * j]);
+              acc[j][2 * h + 1] += __uint_as_float(res[h][2 * j + 1]);
+            } else {
+              const float2 f = unpack2_of<T>(res[h][j]);
+              acc[j][2 * h] += f.x, acc[j][2 * h + 1] += f.y;
+            }
+          }
+      }
+    }
+    put(p.y, p.ldy, q.y_mode);
+  }
+}
+
+// The kernel for a type, by the number of 8-column tiles.
+struct ThinKernel {
+  const void* fn;
+  int tiles, step_bytes, ctas;
+};
+template <typename T, int NT>
+ThinKernel thin_kernel_at(bool fast) {
+  return {fast ? reinterpret_cast<const void*>(thin_kernel<T, NT, true>) : reinterpret_cast<const void*>(thin_kernel<T, NT, false>),
+          NT, ThinShape<T, NT>::kStepBytes, fast ? thin_ctas<T, NT, true>() : thin_ctas<T, NT, false>()};
+}
+template <typename T>
+ThinKernel thin_kernel_of(int columns, bool fast) {
+  if (columns <= 16) return thin_kernel_at<T, 2>(fast);
+  if (columns <= 32) return thin_kernel_at<T, 4>(fast);
+  if (columns <= 48) return thin_kernel_at<T, 6>(fast);
+  if (columns <= 64) return thin_kernel_at<T, 8>(fast);
+  if (columns <= 96) return thin_kernel_at<T, 12>(fast);
+  return thin_kernel_at<T, 16>(fast);
+}
+ThinKernel thin_kernel_f32(int columns, bool fast);
+ThinKernel thin_kernel_f16(int columns, bool fast);
+ThinKernel thin_kernel_bf16(int columns, bool fast);
+
+}  // namespace lin
+}  // namespace pic

@@ -4,6 +4,7 @@
 #pragma once
 
 #include <cstdint>
+#include <type_traits>
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -52,6 +53,24 @@ template <>
 __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// Two values of a 16-bit type in a word, the first in the low half.
+template <typename T>
+__device__ __forceinline__ uint32_t pack2_of(float lo, float hi) {
+  uint32_t d;
+  if constexpr (std::is_same<T, __half>::value)
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  else
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+template <typename T>
+__device__ __forceinline__ float2 unpack2_of(uint32_t v) {
+  if constexpr (std::is_same<T, __half>::value)
+    return __half22float2(*reinterpret_cast<const __half2*>(&v));
+  else
+    return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+}
 
 // act(z), NaN for NaN.  GELU is max(z, 0) - a Phi(-a), a = |z|: no infinity
 // meets a zero.  EXACT (fp32 outputs): a Phi(-a) is a power times a polynomial, off
@@ -178,6 +197,10 @@ int few_product(const Product& p, int dtype, cudaStream_t s);
 constexpr int kFewRows32 = 8;
 bool few32_takes(const Product& p);
 int few32_product(const Product& p, cudaStream_t s);
+
+// Narrow matrices of any number of rows: at most 128 columns and 128 of K, A along K.
+bool thin_takes(const Product& p);
+int thin_product(const Product& p, int dtype, cudaStream_t s);
 
 // dw = dz^T x and db of at most kFewRows rows, dz = dy act'(z) not rounded before.
 struct OuterGrad {

@@ -32,7 +32,7 @@ def normal(shape, dtype, seed, std=1.0):
 H, F = torch.float16, torch.float32
 # tiles of one CTA, one after another (64 and 128 columns), of a pair; fp32 through
 # registers and in planes
-FORWARD = [(150000, 64, 64, H), (70000, 72, 128, H), (8192, 128, 8192, H), (30000, 512, 64, F), (6000, 1024, 2048, F)]
+FORWARD = [(150000, 192, 64, H), (70000, 136, 128, H), (8192, 128, 8192, H), (30000, 512, 64, F), (6000, 1024, 2048, F)]
 # narrow gradients by TMA and through registers, fp32
 NARROW = [(80000, 64, 64, H), (80000, 31, 64, H), (80000, 100, 64, H), (80000, 40, 40, F)]
 
