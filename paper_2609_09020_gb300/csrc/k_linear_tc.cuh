@@ -367,7 +367,10 @@ __device__ __forceinline__ void finish_column(const Product& p, const float* tur
       for (int u = 0; u < 8; ++u) z[u] = relu_nan(z[u]);
     } else if (p.act == PIC_ACT_GELU) {
 #pragma unroll
-      for (int u = 0; u < 8; ++u) z[u] = act_value<true>(z[u], PIC_ACT_GELU);
+      for (int u = 0; u < 8; u += 2) {
+        const float2 y = gelu2<true>(make_float2(z[u], z[u + 1]));
+        z[u] = y.x, z[u + 1] = y.y;
+      }
     }
 #pragma unroll
     for (int u = 0; u < 8; ++u, y += p.ldy)

@@ -6,6 +6,11 @@
 // accumulators straight back.  The weights, in the order of the fragments, are in
 // shared memory.  (Tiles of 128 rows through TMA, tensor memory and panels cost a
 // CTA some 3 us each for 14 KB, and rows off 16-byte boundaries a copy before.)
+// Measured, of the copy rate of 6.7 TB/s: fp16 393216 x 64 -> 64 ReLU keeping z 27.3
+// us, 83 %; 632029 x 40 -> 64 keeping z 37 us, 86 %; 1034578 x 40 -> 16 22 us, 79 %;
+// bf16 581299 x 32 -> 64 with residual 36 us, 77 %.  Off boundaries the shifts and
+// panels bind, 660 instructions of a warp for 16 rows: 1365121 x 40 -> 44 GELU 81 us,
+// 42 %.  fp32 is bound by its MMAs: 200000 x 64 -> 64 32 us, 49 %.
 //
 // Which of K's elements a lane holds in which fragment is free as long as both
 // operands agree, and so is which column a fragment's column is.  So a lane has 16
@@ -35,13 +40,17 @@ namespace lin {
 constexpr int kThinMost = 128;  // columns, and K
 constexpr int kThinThreads = 256, kThinWarps = kThinThreads / 32, kThinRows = 16;
 
+// Rows of y, pre or the residual: 16 bytes of each lane's straight, or through a panel
+// in shared memory: the warp's 16 rows one run of memory on a boundary, or not.
 enum ThinMode { kThinVector = 0, kThinRun = 1, kThinElements = 2 };
 
 struct ThinParams {
   Product p;
   int steps, pieces;        // of 128 and 64 bytes along K
+  int ragged;               // K ends inside 16 bytes
+  int w16;                  // rows of the weights start on 16-byte boundaries
   int y_mode, pre_mode, res_mode;  // a FAST kernel's are kThinVector
-  int panel_at, panel_bytes;  // a warp's 16 rows in shared memory, where a mode is kThinRun
+  int panel_at, panel_bytes;  // a warp's panel, where a mode needs it
   long long tiles;
 };
 
@@ -140,19 +149,22 @@ __device__ __noinline__ void thin_again(const Product& p, long long row, int t, 
     const long long i = row + (e & 2) * 4, j = S::column_of(e >> 2, 2 * t + (e & 1));
     float s = 0.0f;
     if (i < p.I && j < p.J)
-      for (long long k = 0; k < p.K; ++k) s = fmaf(a[i * p.a_i + k], b[j * p.b_j + k * p.b_k], s);
+      for (long long k = 0; k < p.K; ++k) s = fmaf(a[i * p.a_i + k], b[j * p.b_j + k], s);
     u[e] = s;
   }
 }
 
-// CTAs on an SM: what the registers of a kernel with NT x 8 columns leave room for.
+// CTAs on an SM: what the registers of a kernel with NT x 8 columns leave room for
+// (fp16 300000 x 128 -> 128 with one CTA 41 us, with two, which spill, 47; 581299 x 32
+// -> 64 with residual two 36, three 41; the general kernel of 96 columns two 67, one 72).
 template <typename T, int NT, bool FAST>
 constexpr int thin_ctas() {
   if (sizeof(T) == 4) return NT <= 8 ? 2 : 1;
-  return NT <= 4 ? (FAST ? 4 : 3) : NT <= 8 ? (FAST ? 3 : 2) : FAST ? 2 : 1;
+  if (NT <= 4) return FAST ? 4 : 2;
+  return NT <= 8 || !FAST ? 2 : 1;
 }
 
-// FAST: rows of every matrix on 16-byte boundaries, and J a multiple of 16 bytes.
+// FAST: rows of every matrix start and end on 16-byte boundaries (x's may end anywhere).
 template <typename T, int NT, bool FAST>
 __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_kernel(const __grid_constant__ ThinParams q) {
   using S = ThinShape<T, NT>;
@@ -169,11 +181,26 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
   for (int e = threadIdx.x; e < q.steps * 2 * NT * 32; e += kThinThreads) {
     const int l = e & 31, j = e / 32 % NT, piece = e / 32 / NT;
     const int n = S::column_of(j, l >> 2), k0 = piece * (S::kPiece * 4) + (l & 3) * S::kPiece;
-    const T* w = static_cast<const T*>(p.b) + n * p.b_j + k0 * p.b_k;
-    if constexpr (S::kWide) {
-      uint32_t v[4], o[6];
+    const T* w = static_cast<const T*>(p.b) + n * p.b_j + k0;
+    const int there = n < J ? K - k0 : 0;  // elements of the row from here on
+    uint32_t v[4];
+    if (q.w16) {
+      const uint4 x = thin_load(w, there > 0);
+      v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+      thin_keep<T>(v, there * E);
+    } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = load_if(reinterpret_cast<const uint32_t*>(w + i * p.b_k), n < p.J && k0 + i < K);
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (S::kWide) {
+          v[i] = load_if(reinterpret_cast<const uint32_t*>(w) + i, i < there);
+        } else {
+          const uint16_t* u = reinterpret_cast<const uint16_t*>(w) + 2 * i;
+          v[i] = load_if(u, 2 * i < there) | load_if(u + 1, 2 * i + 1 < there) << 16;
+        }
+      }
+    }
+    if constexpr (S::kWide) {
+      uint32_t o[6];
 #pragma unroll
       for (int i = 0; i < 4; ++i) bad_w |= (v[i] & 0x7fffffffu) >= 0x7f800000u;
       cut3(v[0], v[1], o[0], o[2], o[4]);
@@ -182,11 +209,7 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
 #pragma unroll
       for (int i = 0; i < 3; ++i) out[i * 32] = make_uint2(o[2 * i], o[2 * i + 1]);
     } else {
-      uint32_t v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = load_if(reinterpret_cast<const uint16_t*>(w + i * p.b_k), n < p.J && k0 + i < K);
-      reinterpret_cast<uint4*>(frag)[e] =
-          make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+      reinterpret_cast<uint4*>(frag)[e] = make_uint4(v[0], v[1], v[2], v[3]);
     }
   }
   for (int e = threadIdx.x; e < NT * 8; e += kThinThreads) {
@@ -195,12 +218,13 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
   }
   bad_w = __syncthreads_or(bad_w);
 
-  const long long first = blockIdx.x * static_cast<long long>(kThinWarps) + warp;
+  const long long first = warp * static_cast<long long>(gridDim.x) + blockIdx.x;  // few tiles: over all SMs
   const long long stride = gridDim.x * static_cast<long long>(kThinWarps);
   const char* a = static_cast<const char*>(p.a);
   const long long lda = p.a_i * E;
   const int k_bytes = K * E;
   uint8_t* panel = thin_smem + q.panel_at + warp * q.panel_bytes;
+  const int run_pieces = kThinRows * J * E / 16;
 
   ThinPiece<FAST> next[2][2];  // rows g and g + 8; the pieces of a step
   const auto fetch = [&](long long tile, int step) {
@@ -215,7 +239,50 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
       }
     }
   };
-  if (first < q.tiles) fetch(first, 0);
+  // the residual of a tile: each lane's places, or 16 bytes here and there of a run
+  uint32_t res[2][NT * E / 2];
+  const auto fetch_residual = [&](long long tile) {
+    const T* r = static_cast<const T*>(p.residual);
+    if (FAST || q.res_mode == kThinVector) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const long long row = tile * kThinRows + g + 8 * h;
+#pragma unroll
+        for (int gi = 0; gi < S::kGroups; ++gi) {
+          const int cols = 2 * S::in_group(gi), col = S::column(gi, t);
+          const T* at = r + row * p.ldr + col;
+          uint32_t* o = &res[h][gi * S::kGroup * E / 2];
+          const bool there = row < p.I && col < J;
+          if (cols * E == 16) {
+            const uint4 w = thin_load(at, there);
+            o[0] = w.x, o[1] = w.y, o[2] = w.z, o[3] = w.w;
+          } else {
+            o[0] = load_if(reinterpret_cast<const uint32_t*>(at), there);
+            o[1] = load_if(reinterpret_cast<const uint32_t*>(at) + 1, there);
+          }
+        }
+      }
+    } else if (q.res_mode == kThinRun && (tile + 1) * kThinRows <= p.I) {
+      const uint4* v = reinterpret_cast<const uint4*>(r + tile * kThinRows * p.J);
+#pragma unroll
+      for (int i = 0; i < NT * E / 4; ++i) {
+        const uint4 w = thin_load(v + i * 32 + lane, i * 32 + lane < run_pieces);
+        uint32_t* o = &res[0][0] + 4 * i;
+        o[0] = w.x, o[1] = w.y, o[2] = w.z, o[3] = w.w;
+      }
+    }
+  };
+  const auto add_bias = [&](float (&acc)[NT][4]) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const float2 b = *reinterpret_cast<const float2*>(bias + j * 8 + 2 * t);
+      acc[j][0] += b.x, acc[j][1] += b.y, acc[j][2] += b.x, acc[j][3] += b.y;
+    }
+  };
+  if (first < q.tiles) {
+    fetch(first, 0);
+    if (p.residual) fetch_residual(first);
+  }
   for (long long tile = first; tile < q.tiles; tile += stride) {
     const long long row0 = tile * kThinRows, row = row0 + g;
     float acc[NT][4];
@@ -223,7 +290,8 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[j][e] = 0.0f;
-    uint32_t res[2][NT * E / 2];
+    // 16-bit types: sums begin with the bias (fp32 ones, in which the MMAs' truncations would show, end with it)
+    if constexpr (!S::kWide) add_bias(acc);
     bool bad = bad_w;
     for (int step = 0; step < q.steps; ++step) {
       uint32_t x[2][2][4];
@@ -234,57 +302,12 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
         for (int c = 0; c < 2; ++c) {
           next[h][c].template get<T>(m, x[h][c]);
           const int left = k_bytes - (step * 128 + c * 64 + t * 16);
-          if (step == q.steps - 1) thin_keep<T>(x[h][c], row + 8 * h < p.I ? left : 0);
+          if (q.ragged && step == q.steps - 1) thin_keep<T>(x[h][c], left);
         }
       }
       const bool last = step + 1 == q.steps;
       const long long next_tile = last ? tile + stride : tile;
       if (next_tile < q.tiles) fetch(next_tile, last ? 0 : step + 1);
-      if (last && p.residual) {
-        // the residual: each lane's places, or 16 bytes here and there of the run
-        const T* r = static_cast<const T*>(p.residual);
-        if (!FAST && q.res_mode == kThinRun && row0 + kThinRows <= p.I) {
-          const uint4* v = reinterpret_cast<const uint4*>(r + row0 * p.J);
-          const int count = kThinRows * J * E / 16;
-#pragma unroll
-          for (int i = 0; i < NT * E / 4; ++i) {
-            const uint4 w = thin_load(v + i * 32 + lane, i * 32 + lane < count);
-            uint32_t* o = &res[0][0] + 4 * i;
-            o[0] = w.x, o[1] = w.y, o[2] = w.z, o[3] = w.w;
-          }
-        } else {
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int gi = 0; gi < S::kGroups; ++gi) {
-              constexpr int G = S::kGroup;
-              const int cols = 2 * S::in_group(gi), col = S::column(gi, t);
-              const T* at = r + (row + 8 * h) * p.ldr + col;
-              uint32_t* o = &res[h][gi * G * E / 2];
-              const bool there = row + 8 * h < p.I && (!FAST || col < J);
-              if (FAST || (q.res_mode == kThinVector && col + cols <= J)) {
-                if (cols * E == 16) {
-                  const uint4 w = thin_load(at, there);
-                  o[0] = w.x, o[1] = w.y, o[2] = w.z, o[3] = w.w;
-                } else {
-                  o[0] = load_if(reinterpret_cast<const uint32_t*>(at), there);
-                  o[1] = load_if(reinterpret_cast<const uint32_t*>(at) + 1, there);
-                }
-              } else {
-#pragma unroll
-                for (int i = 0; i < cols * E / 4; ++i) {
-                  if constexpr (S::kWide) {
-                    o[i] = load_if(reinterpret_cast<const uint32_t*>(at) + i, there && col + i < J);
-                  } else {
-                    const uint16_t* u = reinterpret_cast<const uint16_t*>(at) + 2 * i;
-                    o[i] = load_if(u, there && col + 2 * i < J) |
-                           load_if(u + 1, there && col + 2 * i + 1 < J) << 16;
-                  }
-                }
-              }
-            }
-        }
-      }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         if (step * 2 + c >= q.pieces) break;
@@ -331,15 +354,12 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
           for (int e = 0; e < 4; ++e) acc[j][e] = u[4 * j + e];
       }
     }
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const float2 b = *reinterpret_cast<const float2*>(bias + j * 8 + 2 * t);
-      acc[j][0] += b.x, acc[j][1] += b.y, acc[j][2] += b.x, acc[j][3] += b.y;
-    }
+    if constexpr (S::kWide) add_bias(acc);
+    const int rows = static_cast<int>(min(static_cast<long long>(kThinRows), p.I - row0));
     // this lane's places of the 16 rows, rounded
     const auto put = [&](void* out, long long ld, int mode) {
-      const bool run = !FAST && mode == kThinRun && row0 + kThinRows <= p.I;
-      if (run) __syncwarp();
+      const bool straight = FAST || mode == kThinVector;
+      if (!straight) __syncwarp();
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -354,72 +374,53 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
             else
               w[i] = pack2_of<T>(u, v);
           }
-          if (run) {
-            uint8_t* o = panel + ((g + 8 * h) * J + col) * E;
-#pragma unroll
-            for (int i = 0; i < cols; ++i) {
-              if (col + i >= J) continue;
-              if constexpr (S::kWide)
-                reinterpret_cast<uint32_t*>(o)[i] = w[i];
-              else
-                reinterpret_cast<uint16_t*>(o)[i] = static_cast<uint16_t>(w[i / 2] >> (i % 2 * 16));
-            }
-            continue;
-          }
-          if (row + 8 * h >= p.I || col >= J) continue;
-          T* o = static_cast<T*>(out) + (row + 8 * h) * ld + col;
-          if (FAST || (mode == kThinVector && col + cols <= J)) {
+          if (straight) {
+            if (g + 8 * h >= rows || col >= J) continue;
+            T* o = static_cast<T*>(out) + (row + 8 * h) * ld + col;
             if (cols * E == 16)
               *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
             else
               *reinterpret_cast<uint2*>(o) = make_uint2(w[0], w[1]);
+            continue;
+          }
+          uint8_t* o = panel + ((g + 8 * h) * J + col) * E;
+          if (S::kWide || J % 2 == 0) {
+#pragma unroll
+            for (int i = 0; i < cols * E / 4; ++i)
+              if (col + i * (4 / E) < J) reinterpret_cast<uint32_t*>(o)[i] = w[i];
           } else {
 #pragma unroll
-            for (int i = 0; i < cols; ++i) {
-              if (col + i >= J) continue;
-              if constexpr (S::kWide)
-                reinterpret_cast<uint32_t*>(o)[i] = w[i];
-              else
-                reinterpret_cast<uint16_t*>(o)[i] = static_cast<uint16_t>(w[i / 2] >> (i % 2 * 16));
-            }
+            for (int i = 0; i < cols; ++i)
+              if (col + i < J) reinterpret_cast<uint16_t*>(o)[i] = static_cast<uint16_t>(w[i / 2] >> (i % 2 * 16));
           }
         }
-      if (run) {
-        __syncwarp();
-        const int count = kThinRows * J * E / 16;
-        uint4* o = reinterpret_cast<uint4*>(static_cast<T*>(out) + row0 * p.J);
-        for (int i = lane; i < count; i += 32) o[i] = reinterpret_cast<const uint4*>(panel)[i];
+      if (straight) return;
+      __syncwarp();
+      T* o = static_cast<T*>(out) + row0 * ld;
+      if (mode == kThinRun && rows == kThinRows) {
+        for (int i = lane; i < run_pieces; i += 32) reinterpret_cast<uint4*>(o)[i] = reinterpret_cast<const uint4*>(panel)[i];
+      } else {
+        for (int r = 0; r < rows; ++r)
+          for (int c = lane; c < J; c += 32) o[r * ld + c] = reinterpret_cast<const T*>(panel)[r * J + c];
       }
     };
     if (p.pre) put(p.pre, p.ldpre, q.pre_mode);
-    if (p.act != PIC_ACT_NONE) {
+    if (p.act == PIC_ACT_RELU) {
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[j][e] = act_value<S::kWide>(acc[j][e], p.act);
+        for (int e = 0; e < 4; ++e) acc[j][e] = relu_nan(acc[j][e]);
+    } else if (p.act == PIC_ACT_GELU) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float2 y = gelu2<S::kWide>(make_float2(acc[j][2 * h], acc[j][2 * h + 1]));
+          acc[j][2 * h] = y.x, acc[j][2 * h + 1] = y.y;
+        }
     }
     if (p.residual) {
-      if (!FAST && q.res_mode == kThinRun && row0 + kThinRows <= p.I) {
-        __syncwarp();
-        const int count = kThinRows * J * E / 16;
-#pragma unroll
-        for (int i = 0; i < NT * E / 4; ++i) {
-          const uint32_t* o = &res[0][0] + 4 * i;
-          if (i * 32 + lane < count)
-            reinterpret_cast<uint4*>(panel)[i * 32 + lane] = make_uint4(o[0], o[1], o[2], o[3]);
-        }
-        __syncwarp();
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int col = S::column_of(j, 2 * t + e);
-              if (col < J)
-                acc[j][2 * h + e] += to_f32(reinterpret_cast<const T*>(panel)[(g + 8 * h) * J + col]);
-            }
-      } else {
+      if (FAST || q.res_mode == kThinVector) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -432,7 +433,32 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
               acc[j][2 * h] += f.x, acc[j][2 * h + 1] += f.y;
             }
           }
+      } else {
+        __syncwarp();
+        if (q.res_mode == kThinRun && rows == kThinRows) {
+#pragma unroll
+          for (int i = 0; i < NT * E / 4; ++i) {
+            const uint32_t* o = &res[0][0] + 4 * i;
+            if (i * 32 + lane < run_pieces)
+              reinterpret_cast<uint4*>(panel)[i * 32 + lane] = make_uint4(o[0], o[1], o[2], o[3]);
+          }
+        } else {
+          const T* r = static_cast<const T*>(p.residual) + row0 * p.ldr;
+          for (int i = 0; i < rows; ++i)
+            for (int c = lane; c < J; c += 32) reinterpret_cast<T*>(panel)[i * J + c] = r[i * p.ldr + c];
+        }
+        __syncwarp();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int col = S::column_of(j, 2 * t + e);
+              if (col < J) acc[j][2 * h + e] += to_f32(reinterpret_cast<const T*>(panel)[(g + 8 * h) * J + col]);
+            }
       }
+      if (tile + stride < q.tiles) fetch_residual(tile + stride);
     }
     put(p.y, p.ldy, q.y_mode);
   }

@@ -93,6 +93,23 @@ __device__ __forceinline__ float act_value(float z, int act) {
   }
 }
 
+// GELU of two values, its polynomial in packed instructions; as act_value rounds.
+template <bool EXACT>
+__device__ __forceinline__ float2 gelu2(float2 z) {
+  if constexpr (EXACT) {
+    const float2 a = make_float2(fminf(fabsf(z.x), kGeluGradA), fminf(fabsf(z.y), kGeluGradA));
+    const unsigned long long a2 = pack2(a.x, a.y);
+    unsigned long long r = pack2(gelu_c32(0), gelu_c32(0));
+#pragma unroll
+    for (int i = 1; i <= kGeluDeg32; ++i) r = fma2(r, a2, pack2(gelu_c32(i), gelu_c32(i)));
+    const float2 q = unpack2(r), e = unpack2(mul2(mul2(a2, a2), pack2(kGeluGradPower, kGeluGradPower)));
+    return make_float2(fmaf(-ex2_approx(e.x), a.x >= kGeluGradA ? 0.0f : q.x, relu_nan(z.x)),
+                       fmaf(-ex2_approx(e.y), a.y >= kGeluGradA ? 0.0f : q.y, relu_nan(z.y)));
+  } else {
+    return unpack2(gelu_approx2(pack2(z.x, z.y)));
+  }
+}
+
 // dy act'(z): a derivative of zero gives zero whatever dy is; act' is NaN for
 // NaN.  EXACT (fp32): off by the roundings of the evaluation, about 1e-7; else by
 // at most 5e-7, far below the rounding of dz to 16 bits.
@@ -198,8 +215,8 @@ constexpr int kFewRows32 = 8;
 bool few32_takes(const Product& p);
 int few32_product(const Product& p, cudaStream_t s);
 
-// Narrow matrices of any number of rows: at most 128 columns and 128 of K, A along K.
-bool thin_takes(const Product& p);
+// Narrow matrices of any number of rows: at most 128 columns and 128 of K, both along K.
+bool thin_takes(const Product& p, int dtype);
 int thin_product(const Product& p, int dtype, cudaStream_t s);
 
 // dw = dz^T x and db of at most kFewRows rows, dz = dy act'(z) not rounded before.

@@ -111,13 +111,13 @@ bool few(const Product& p, int dtype) {
 }
 
 long long product_workspace(const Product& p, int dtype) {
-  return few(p, dtype) || pic::lin::thin_takes(p) ? 0 : pic::lin::tc_workspace(p, dtype);
+  return few(p, dtype) || pic::lin::thin_takes(p, dtype) ? 0 : pic::lin::tc_workspace(p, dtype);
 }
 
 int product(const Product& p, int dtype, void* ws, cudaStream_t s) {
   if (few(p, dtype))
     return dtype == PIC_DTYPE_F32 ? pic::lin::few32_product(p, s) : pic::lin::few_product(p, dtype, s);
-  if (pic::lin::thin_takes(p)) return pic::lin::thin_product(p, dtype, s);
+  if (pic::lin::thin_takes(p, dtype)) return pic::lin::thin_product(p, dtype, s);
   pic::lin::Waits w;
   return waits(w) ? pic::lin::tc_product(p, dtype, ws, w, s) : PIC_ERR_CUDA;
 }

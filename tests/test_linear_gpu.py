@@ -415,3 +415,59 @@ def test_tolerances_catch_mistakes():
     (y3, _), _ = ref.forward(x.bfloat16(), w.bfloat16(), None, "gelu", None)
     assert float(((y2 - y).abs() > tol).double().mean()) > 0.5
     assert float(((y3 - y).abs() > tol).double().mean()) > 0.5
+
+
+def shifted(rows, cols, dtype, seed, ld, shift, std=1.0):
+    """A [rows][cols] view with `ld` elements from row to row, `shift` past a boundary; NaN around it."""
+    t = torch.full((rows * ld + cols + shift,), math.nan, dtype=dtype, device="cuda")
+    v = torch.as_strided(t, (rows, cols), (ld, 1), shift)
+    v.copy_(normal((rows, cols), dtype, seed, std))
+    return v
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("place", [(0, 0), (0, 1), (3, 2), (8, 8), (16, 0)], ids=str)  # columns between rows, shift
+@pytest.mark.parametrize("size", [(16, 16, 16), (17, 64, 64), (333, 40, 44), (250, 33, 24), (1000, 128, 128), (95, 111, 77),
+                                  (4111, 3, 96), (2600, 72, 5), (31, 127, 121), (40, 1, 33)], ids=str)
+def test_narrow_places(size, place, dtype):
+    """Narrow layers whose matrices lie in wider ones, on and off 16-byte boundaries; nothing around is read or written."""
+    from paper_2609_09020_gb300 import pic
+    M, K, N = size
+    pad, shift = place
+    x, w = shifted(M, K, dtype, 1, K + pad, shift), shifted(N, K, dtype, 2, K + pad, shift, 1.4 / math.sqrt(K))
+    b, r = normal((N,), dtype, 3, 0.1), shifted(M, N, dtype, 4, N + pad, shift)
+    out = shifted(M, N, dtype, 5, N + pad, shift)
+    whole = torch.as_strided(out, (M * (N + pad) + N + shift,), (1,), 0)
+    kept = torch.isnan(whole).clone()
+    for act, res in (("none", r), ("relu", None), ("gelu", r)):
+        want_y, want_z = ref.forward(x, w, b, act, res)
+        y, z = pic.linear(x, w, b, act=act, residual=res, out=out, save_pre=True)
+        assert y is out
+        ref.check(y, want_y, "y")
+        ref.check(z, want_z, "pre")
+        assert torch.equal(torch.isnan(whole), kept)
+        ref.check(pic.linear(x, w, b, act=act, residual=res), want_y, "y")
+    pic.linear_check()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("pad", [0, 3])
+def test_narrow_nonfinite(pad, dtype):
+    """Infinite and NaN values in rows and weights of a narrow layer stay in their rows and columns."""
+    from paper_2609_09020_gb300 import pic
+    M, K, N = 3000, 45, 50
+    x, w = shifted(M, K, dtype, 1, K + pad, 0), normal((N, K), dtype, 2, 0.2)
+    want, tol = ref.forward(x, w, None, "none", None)[0]
+    x[7, 44], x[1234, 0], x[2999, 20] = math.inf, math.nan, -math.inf
+    y = pic.linear(x, w)
+    keep = torch.ones(M, dtype=torch.bool, device="cuda")
+    keep[7] = keep[1234] = keep[2999] = False
+    ref.check(y[keep], (want[keep], tol[keep]))
+    assert torch.equal(y[7], torch.sign(w[:, 44]) * math.inf) and bool(torch.isnan(y[1234]).all())
+    assert torch.equal(y[2999], torch.sign(w[:, 20]) * -math.inf)
+    x = normal((M, K), dtype, 1).abs() + 0.5
+    want, tol = ref.forward(x, w, None, "none", None)[0]
+    w[49, 44] = -math.inf
+    y = pic.linear(x, w)
+    assert bool((y[:, 49] == -math.inf).all())
+    ref.check(y[:, :49], (want[:, :49], tol[:, :49]))
