@@ -175,49 +175,6 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int J = static_cast<int>(p.J), K = static_cast<int>(p.K);
 
-  // the weights, zero outside
-  uint32_t* frag = reinterpret_cast<uint32_t*>(thin_smem);
-  bool bad_w = false;
-  for (int e = threadIdx.x; e < q.steps * 2 * NT * 32; e += kThinThreads) {
-    const int l = e & 31, j = e / 32 % NT, piece = e / 32 / NT;
-    const int n = S::column_of(j, l >> 2), k0 = piece * (S::kPiece * 4) + (l & 3) * S::kPiece;
-    const T* w = static_cast<const T*>(p.b) + n * p.b_j + k0;
-    const int there = n < J ? K - k0 : 0;  // elements of the row from here on
-    uint32_t v[4];
-    if (q.w16) {
-      const uint4 x = thin_load(w, there > 0);
-      v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
-      thin_keep<T>(v, there * E);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (S::kWide) {
-          v[i] = load_if(reinterpret_cast<const uint32_t*>(w) + i, i < there);
-        } else {
-          const uint16_t* u = reinterpret_cast<const uint16_t*>(w) + 2 * i;
-          v[i] = load_if(u, 2 * i < there) | load_if(u + 1, 2 * i + 1 < there) << 16;
-        }
-      }
-    }
-    if constexpr (S::kWide) {
-      uint32_t o[6];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) bad_w |= (v[i] & 0x7fffffffu) >= 0x7f800000u;
-      cut3(v[0], v[1], o[0], o[2], o[4]);
-      cut3(v[2], v[3], o[1], o[3], o[5]);
-      uint2* out = reinterpret_cast<uint2*>(frag) + ((piece * NT + j) * 3) * 32 + l;
-#pragma unroll
-      for (int i = 0; i < 3; ++i) out[i * 32] = make_uint2(o[2 * i], o[2 * i + 1]);
-    } else {
-      reinterpret_cast<uint4*>(frag)[e] = make_uint4(v[0], v[1], v[2], v[3]);
-    }
-  }
-  for (int e = threadIdx.x; e < NT * 8; e += kThinThreads) {
-    const int n = S::column_of(e / 8, e % 8);
-    bias[e] = p.bias && n < p.J ? to_f32(static_cast<const T*>(p.bias)[n]) : 0.0f;
-  }
-  bad_w = __syncthreads_or(bad_w);
-
   const long long first = warp * static_cast<long long>(gridDim.x) + blockIdx.x;  // few tiles: over all SMs
   const long long stride = gridDim.x * static_cast<long long>(kThinWarps);
   const char* a = static_cast<const char*>(p.a);
@@ -272,6 +229,53 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
       }
     }
   };
+  if (first < q.tiles) {
+    fetch(first, 0);
+    if (p.residual) fetch_residual(first);
+  }
+  // the weights, zero outside, while the first rows are on their way
+  uint32_t* frag = reinterpret_cast<uint32_t*>(thin_smem);
+  bool bad_w = false;
+  for (int e = threadIdx.x; e < q.steps * 2 * NT * 32; e += kThinThreads) {
+    const int l = e & 31, j = e / 32 % NT, piece = e / 32 / NT;
+    const int n = S::column_of(j, l >> 2), k0 = piece * (S::kPiece * 4) + (l & 3) * S::kPiece;
+    const T* w = static_cast<const T*>(p.b) + n * p.b_j + k0;
+    const int there = n < J ? K - k0 : 0;  // elements of the row from here on
+    uint32_t v[4];
+    if (q.w16) {
+      const uint4 x = thin_load(w, there > 0);
+      v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+      thin_keep<T>(v, there * E);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (S::kWide) {
+          v[i] = load_if(reinterpret_cast<const uint32_t*>(w) + i, i < there);
+        } else {
+          const uint16_t* u = reinterpret_cast<const uint16_t*>(w) + 2 * i;
+          v[i] = load_if(u, 2 * i < there) | load_if(u + 1, 2 * i + 1 < there) << 16;
+        }
+      }
+    }
+    if constexpr (S::kWide) {
+      uint32_t o[6];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) bad_w |= (v[i] & 0x7fffffffu) >= 0x7f800000u;
+      cut3(v[0], v[1], o[0], o[2], o[4]);
+      cut3(v[2], v[3], o[1], o[3], o[5]);
+      uint2* out = reinterpret_cast<uint2*>(frag) + ((piece * NT + j) * 3) * 32 + l;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) out[i * 32] = make_uint2(o[2 * i], o[2 * i + 1]);
+    } else {
+      reinterpret_cast<uint4*>(frag)[e] = make_uint4(v[0], v[1], v[2], v[3]);
+    }
+  }
+  for (int e = threadIdx.x; e < NT * 8; e += kThinThreads) {
+    const int n = S::column_of(e / 8, e % 8);
+    bias[e] = p.bias && n < p.J ? to_f32(static_cast<const T*>(p.bias)[n]) : 0.0f;
+  }
+  bad_w = __syncthreads_or(bad_w);
+
   const auto add_bias = [&](float (&acc)[NT][4]) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
@@ -279,10 +283,6 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
       acc[j][0] += b.x, acc[j][1] += b.y, acc[j][2] += b.x, acc[j][3] += b.y;
     }
   };
-  if (first < q.tiles) {
-    fetch(first, 0);
-    if (p.residual) fetch_residual(first);
-  }
   for (long long tile = first; tile < q.tiles; tile += stride) {
     const long long row0 = tile * kThinRows, row = row0 + g;
     float acc[NT][4];
