@@ -190,7 +190,8 @@ constexpr ShapeCost kShapePlanes{kPlCols, 2, kSms / 2, 8.0, 0.95, 3.4};
 // 128/4 19.0 (19.0), 512 x 16384 -> 512 128/8 15.8 (15.2), 64/8 (20), 256/8 (19.3).
 // Rows that are not whole 128-byte lines make slices of 64 and 128 columns half as
 // slow again (720 x 12632 -> 496 128/4 25.9 (25.7), 256/8 21.9 (21.2)).
-void choose(Plan& r, const Product& p, const ShapeCost* shapes, int n_shapes, int least, bool lines) {
+// The estimate is returned.
+double choose(Plan& r, const Product& p, const ShapeCost* shapes, int n_shapes, int least, bool lines) {
   double best = 1e30;
   for (int c = 0; c < n_shapes; ++c) {
     const ShapeCost& h = shapes[c];
@@ -214,6 +215,26 @@ void choose(Plan& r, const Product& p, const ShapeCost* shapes, int n_shapes, in
       }
     }
   }
+  return best;
+}
+
+// fp32: operands cut into planes first, or on the way, again for every tile.  The
+// first costs 4 us and 10 bytes of traffic an element at 5 TB/s; the second takes
+// longer for rows off 16-byte boundaries.  us, planes / on the way: 200 x 4096 -> 8192
+// 137 / 229, 4000 x 2686 -> 221 58 / 87, 200 x 500 -> 8192 25 / 46; 100 x 4096 -> 2048 45
+// / 34, 500 x 500 -> 150 20 / 14, 16000 x 512 -> 16 32 / 18.
+void choose_fp32(Plan& r, const Product& p, bool rows16) {
+  Plan other = r;
+  ShapeCost reg = kShapeReg;
+  if (!rows16) reg.slice *= 1.15;
+  const double on_the_way = choose(r, p, &reg, 1, 4, true);
+  const double elements = static_cast<double>(p.K) * static_cast<double>(p.I + p.J);
+  const double first = choose(other, p, &kShapePlanes, 1, 4, true) + 4.0 + elements * 10.0 / 5e6;
+  if (first < on_the_way) {
+    r = other;
+    r.planes = true;
+  }
+  r.reg = !r.planes;
 }
 
 Plan plan(const Product& p, int dtype) {
@@ -221,13 +242,10 @@ Plan plan(const Product& p, int dtype) {
   const bool fp32 = dtype == PIC_DTYPE_F32;
   r.a = operand(p.a, p.a_i, p.a_k, p.I, p.K, fp32);
   r.b = operand(p.b, p.b_j, p.b_k, p.J, p.K, fp32);
-  // fp32: cutting the operands first costs 10 bytes of traffic an element, cutting
-  // them on the way three times the MMAs' time for every tile
-  r.planes = fp32 && p.I >= 256 && p.J >= 256;
-  r.reg = fp32 && !r.planes;
   r.k_blocks = static_cast<int>((p.K + kSlice - 1) / kSlice);
   if (fp32) {
-    choose(r, p, r.reg ? &kShapeReg : &kShapePlanes, 1, 4, true);
+    const auto rows16 = [](const void* m, const Operand& o) { return reinterpret_cast<uintptr_t>(m) % 16 == 0 && o.ld % 4 == 0; };
+    choose_fp32(r, p, rows16(p.a, r.a) && rows16(p.b, r.b));
   } else {
     const ShapeCost shapes[] = {kShape64, kShape128, kShape256};
     const auto lines = [](const Operand& o) { return o.repack || o.ld % 64 == 0; };
