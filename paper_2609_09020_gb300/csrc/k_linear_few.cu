@@ -17,9 +17,12 @@
 //
 // Each group of columns is then summed over the warps in shared memory.  With
 // fewer groups than CTAs fit the GPU, K is cut further over the CTAs of a
-// cluster, which add their sums through distributed shared memory.  All sums have a fixed order.  (The MMA's
-// places for rows that do not exist read the last row again; what they give is
-// not looked at.)
+// cluster, which add their sums through distributed shared memory.  All sums have
+// a fixed order.  (The MMA's places for rows that do not exist read the last row
+// again; what they give is not looked at.)
+//
+// Measured: 1 row of 4096 to 4096 columns 6.5 us with the weights in L2, 11.5 from
+// memory (2.9 TB/s: start and end are half of it); 1 x 4352 -> 7424 about 20.
 #include <atomic>
 
 #include "linear.cuh"

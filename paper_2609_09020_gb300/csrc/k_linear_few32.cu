@@ -9,7 +9,10 @@
 //   across   (dx = dz w) a lane takes 4 columns; the few values of dz that belong to
 //            a row of w are read from shared memory, four at a time.
 //
-// Eight warps of a CTA, and the CTAs of a cluster, share K in turns.
+// Eight warps of a CTA, and the CTAs of a cluster, share K in turns; they meet to add
+// their sums after several groups.  Measured, with weights that come from memory: 1
+// row of 4352 to 7424 columns 41 us, 3.2 TB/s, 8 rows 61; of dz, 7424 to 4352, 31 and
+// 45.
 #include <atomic>
 
 #include "linear.cuh"
@@ -24,6 +27,7 @@ constexpr int kWarps = 8, kThreads = 32 * kWarps;
 constexpr int kGroup = 4;         // rows of w of a warp (along)
 constexpr int kAlongTurn = 128;   // elements of K of a warp's turn
 constexpr int kAlongSteps = 4;    // turns that a warp loads at a time
+constexpr int kAlongGroups = 6;   // groups between two meetings of a CTA's, and a cluster's, warps
 constexpr int kAcrossCols = 128;  // columns of a warp (across)
 constexpr int kAcrossRows = 8;    // rows of w that a warp loads at a time
 constexpr int kMaxBytes = 100 * 1024;  // the few rows in shared memory, two CTAs on an SM
@@ -58,9 +62,46 @@ __device__ __forceinline__ float4 load4(const float* p, int n, int lane) {
   return f;
 }
 
-__device__ __forceinline__ float a_value(const Product& p, int i, long long k) {
-  const float d = static_cast<const float*>(p.a)[i * p.a_i + k];
-  return p.a_pre ? act_grad<true>(d, static_cast<const float*>(p.a_pre)[i * p.a_pre_i + k], p.a_act) : d;
+// This CTA's part of K of the rows of A (or of dz = dy act'(z)) to put(i, k, values),
+// four elements at a time, zero past K's end; kRowLoads of a thread's loads are under
+// way together (one by one, 5 rows of 4352 took longer than 129 MB of weights).
+constexpr int kRowLoads = 4;
+template <typename Put>
+__device__ __forceinline__ void load_rows(const FewParams& q, int k0, Put put) {
+  const Product& p = q.p;
+  const int per_row = q.k_part / 4, n = static_cast<int>(p.I) * per_row;
+  const auto load = [&](const void* m, long long ld, int i, int k) {
+    const uint32_t* a = static_cast<const uint32_t*>(m) + i * ld + k;
+    const long long left = i < p.I ? p.K - k : 0;
+    return make_float4(__uint_as_float(load_if(a, left > 0)), __uint_as_float(load_if(a + 1, left > 1)),
+                       __uint_as_float(load_if(a + 2, left > 2)), __uint_as_float(load_if(a + 3, left > 3)));
+  };
+  for (int e0 = threadIdx.x; e0 < n; e0 += kThreads * kRowLoads) {
+    float4 d[kRowLoads], z[kRowLoads];
+#pragma unroll
+    for (int u = 0; u < kRowLoads; ++u) {
+      const int e = e0 + u * kThreads;
+      d[u] = load(p.a, p.a_i, e / per_row, k0 + e % per_row * 4);
+    }
+    if (p.a_pre) {
+#pragma unroll
+      for (int u = 0; u < kRowLoads; ++u) {
+        const int e = e0 + u * kThreads;
+        z[u] = load(p.a_pre, p.a_pre_i, e / per_row, k0 + e % per_row * 4);
+      }
+#pragma unroll
+      for (int u = 0; u < kRowLoads; ++u) {
+        const float2 lo = act_grad2<true>(make_float2(d[u].x, d[u].y), make_float2(z[u].x, z[u].y), p.a_act);
+        const float2 hi = act_grad2<true>(make_float2(d[u].z, d[u].w), make_float2(z[u].z, z[u].w), p.a_act);
+        d[u] = make_float4(lo.x, lo.y, hi.x, hi.y);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kRowLoads; ++u) {
+      const int e = e0 + u * kThreads;
+      if (e < n) put(e / per_row, e % per_row * 4, d[u]);
+    }
+  }
 }
 
 __device__ __forceinline__ void finish(const Product& p, int i, long long j, float v) {
@@ -71,20 +112,28 @@ __device__ __forceinline__ void finish(const Product& p, int i, long long j, flo
   static_cast<float*>(p.y)[i * p.ldy + j] = v;
 }
 
-// sums[warp][rows][cols] of every CTA of the cluster, added warps first, then CTAs,
-// both in order, and out through the epilogue.
-__device__ __forceinline__ void finish_group(const FewParams& q, float* sums, int mt, int cols, long long j0, uint32_t rank) {
+// sums[group][warp][rows][cols] of every CTA of the cluster, added warps first, then
+// CTAs, both in order, and out through the epilogue: `count` groups, the first at
+// column j0, apart by `apart` columns.
+__device__ __forceinline__ void finish_groups(const FewParams& q, float* sums, int mt, int cols, int count, long long j0,
+                                              long long apart, uint32_t rank) {
   const Product& p = q.p;
   __syncthreads();
-  const int n = static_cast<int>(p.I) * cols;
+  const int per = static_cast<int>(p.I) * cols, n = count * per, group = kWarps * mt * cols;
+  const auto out = [&](int e, float v) {
+    const int i = e % per;
+    const long long j = j0 + e / per * apart + i % cols;
+    if (j < p.J) finish(p, i / cols, j, v);
+  };
   for (int e = threadIdx.x; e < n; e += kThreads) {
+    float* s = sums + e / per * group + e % per;
     float v = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) v += sums[w * mt * cols + e];
+    for (int w = 0; w < kWarps; ++w) v += s[w * mt * cols];
     if (q.cluster > 1)
-      sums[e] = v;  // only this thread reads or writes this place of warp 0's
-    else if (j0 + e % cols < p.J)
-      finish(p, e / cols, j0 + e % cols, v);
+      *s = v;  // only this thread reads or writes this place of warp 0's
+    else
+      out(e, v);
   }
   __syncwarp();
   if (q.cluster > 1) {
@@ -93,10 +142,11 @@ __device__ __forceinline__ void finish_group(const FewParams& q, float* sums, in
       float v = 0.0f;
       for (int r = 0; r < q.cluster; ++r) {
         float f;
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f) : "r"(tc::map_rank(tc::smem_addr(sums + e), r)) : "memory");
+        const uint32_t at = tc::map_rank(tc::smem_addr(sums + e / per * group + e % per), r);
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f) : "r"(at) : "memory");
         v += f;
       }
-      if (j0 + e % cols < p.J) finish(p, e / cols, j0 + e % cols, v);
+      out(e, v);
     }
     __syncwarp();
     tc::cluster_sync();  // nobody goes on while its sums are read
@@ -113,7 +163,7 @@ __global__ void __launch_bounds__(kThreads, 2) along_kernel(const FewParams q) {
   const uint32_t rank = q.cluster > 1 ? tc::cluster_rank() : 0;
   const int k0 = rank * q.k_part, k1 = static_cast<int>(min(p.K, static_cast<long long>(k0) + q.k_part));
   float* xs = smem;                                    // [rows][k_part]
-  float* sums = smem + rows * q.k_part;                // [warps][MT][kGroup]
+  float* sums = smem + rows * q.k_part;                // [kAlongGroups][warps][MT][kGroup]
   const float* w = static_cast<const float*>(p.b);
   float4 a[kAlongSteps][kGroup];
   auto load = [&](int s, int group, int k) {
@@ -128,11 +178,9 @@ __global__ void __launch_bounds__(kThreads, 2) along_kernel(const FewParams q) {
   int group = blockIdx.x / q.cluster;
 #pragma unroll
   for (int s = 0; s < kAlongSteps; ++s) load(s, group, kw);
-  for (int e = threadIdx.x; e < rows * q.k_part; e += kThreads) {
-    const int i = e / q.k_part, k = k0 + e % q.k_part;
-    xs[e] = k < p.K ? a_value(p, i, k) : 0.0f;
-  }
+  load_rows(q, k0, [&](int i, int k, const float4& v) { *reinterpret_cast<float4*>(xs + i * q.k_part + k) = v; });
   __syncthreads();
+  int slot = 0;
   for (; group < q.groups; group += step) {
     float c[MT * kGroup] = {};
     for (int k = kw; k < k1 || k == kw; k += batch) {
@@ -182,8 +230,12 @@ __global__ void __launch_bounds__(kThreads, 2) along_kernel(const FewParams q) {
         c[0] += __shfl_xor_sync(0xffffffffu, c[0], o);
       }
     }
-    sums[warp * MT * kGroup + mine] = c[0];  // lanes with the same sum write the same value
-    finish_group(q, sums, MT, kGroup, group * static_cast<long long>(kGroup), rank);
+    sums[(slot * kWarps + warp) * MT * kGroup + mine] = c[0];  // lanes with the same sum write the same value
+    if (++slot == kAlongGroups || group + step >= q.groups) {
+      const long long j0 = (group - (slot - 1LL) * step) * kGroup;
+      finish_groups(q, sums, MT, kGroup, slot, j0, static_cast<long long>(step) * kGroup, rank);
+      slot = 0;
+    }
   }
 }
 
@@ -207,10 +259,13 @@ __global__ void __launch_bounds__(kThreads, 2) across_kernel(const FewParams q) 
   int group = blockIdx.x / q.cluster;
 #pragma unroll
   for (int s = 0; s < kAcrossRows; ++s) load(s, group, kw);
-  for (int e = threadIdx.x; e < q.k_part * MT; e += kThreads) {
-    const int i = e / q.k_part, k = e % q.k_part;
-    xs[k * MT + i] = i < rows && k0 + k < p.K ? a_value(p, i, k0 + k) : 0.0f;
-  }
+  load_rows(q, k0, [&](int i, int k, const float4& v) {
+    const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int c = 0; c < 4; ++c) xs[(k + c) * MT + i] = f[c];
+  });
+  for (int e = threadIdx.x; e < q.k_part * (MT - rows); e += kThreads)  // rows that do not exist
+    xs[e / (MT - rows) * MT + rows + e % (MT - rows)] = 0.0f;
   __syncthreads();
   for (; group < q.groups; group += step) {
     float4 c[MT] = {};
@@ -241,7 +296,7 @@ __global__ void __launch_bounds__(kThreads, 2) across_kernel(const FewParams q) 
         s[lane] = c[m].x, s[lane + 32] = c[m].y, s[lane + 64] = c[m].z, s[lane + 96] = c[m].w;
       }
     }
-    finish_group(q, sums, MT, kAcrossCols, group * static_cast<long long>(kAcrossCols), rank);
+    finish_groups(q, sums, MT, kAcrossCols, 1, group * static_cast<long long>(kAcrossCols), 0, rank);
   }
 }
 
@@ -270,7 +325,7 @@ Plan plan(const Product& p) {
   while (r.cluster < 8 && bytes(r.cluster) > kMaxBytes) r.cluster *= 2;
   const long long need = bytes(r.cluster);
   if (need > kMaxBytes) return r;
-  r.smem = static_cast<int>(need) + kWarps * r.mt * (r.along ? kGroup : kAcrossCols) * 4;
+  r.smem = static_cast<int>(need) + kWarps * r.mt * (r.along ? kGroup * kAlongGroups : kAcrossCols) * 4;
   if (r.smem > 113 * 1024) return r;
   const int most = 2 * kSms / r.cluster * r.cluster;
   const long long want = groups * r.cluster;

@@ -74,16 +74,6 @@ struct ThinShape {
   }
 };
 
-__device__ __forceinline__ uint4 thin_load(const void* p, bool on) {
-  uint4 v;
-  asm volatile(
-      "{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %5, 0;\n\tmov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t"
-      "@q ld.global.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
-      : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-      : "l"(p), "r"(static_cast<uint32_t>(on)));
-  return v;
-}
-
 template <typename T>
 __device__ __forceinline__ void thin_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
@@ -105,11 +95,11 @@ struct ThinPiece {
   uint4 lo, hi;
   __device__ __forceinline__ void load(const char* at, int bytes) {  // bytes of the row from `at` on, may be <= 0
     if constexpr (FAST) {
-      lo = thin_load(at, bytes > 0);
+      lo = load_if16(at, bytes > 0);
     } else {
       const int m = static_cast<int>(reinterpret_cast<uintptr_t>(at) & 15);
-      lo = thin_load(at - m, bytes > 0);
-      hi = thin_load(at - m + 16, m + min(bytes, 16) > 16);
+      lo = load_if16(at - m, bytes > 0);
+      hi = load_if16(at - m + 16, m + min(bytes, 16) > 16);
     }
   }
   // the 16 bytes from byte `m` of the two on
@@ -131,14 +121,6 @@ struct ThinPiece {
     }
   }
 };
-
-// Keeps `bytes` bytes of w, from its beginning.
-template <typename T>
-__device__ __forceinline__ void thin_keep(uint32_t (&w)[4], int bytes) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    w[i] = bytes >= 4 * i + 4 ? w[i] : sizeof(T) == 2 && bytes >= 4 * i + 2 ? w[i] & 0xffffu : 0u;
-}
 
 // The sums of a lane's places, on the FP32 cores.
 template <int NT>
@@ -211,7 +193,7 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
           uint32_t* o = &res[h][gi * S::kGroup * E / 2];
           const bool there = row < p.I && col < J;
           if (cols * E == 16) {
-            const uint4 w = thin_load(at, there);
+            const uint4 w = load_if16(at, there);
             o[0] = w.x, o[1] = w.y, o[2] = w.z, o[3] = w.w;
           } else {
             o[0] = load_if(reinterpret_cast<const uint32_t*>(at), there);
@@ -223,7 +205,7 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
       const uint4* v = reinterpret_cast<const uint4*>(r + tile * kThinRows * p.J);
 #pragma unroll
       for (int i = 0; i < NT * E / 4; ++i) {
-        const uint4 w = thin_load(v + i * 32 + lane, i * 32 + lane < run_pieces);
+        const uint4 w = load_if16(v + i * 32 + lane, i * 32 + lane < run_pieces);
         uint32_t* o = &res[0][0] + 4 * i;
         o[0] = w.x, o[1] = w.y, o[2] = w.z, o[3] = w.w;
       }
@@ -243,9 +225,9 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
     const int there = n < J ? K - k0 : 0;  // elements of the row from here on
     uint32_t v[4];
     if (q.w16) {
-      const uint4 x = thin_load(w, there > 0);
+      const uint4 x = load_if16(w, there > 0);
       v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
-      thin_keep<T>(v, there * E);
+      keep_bytes<T>(v, there * E);
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -302,7 +284,7 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
         for (int c = 0; c < 2; ++c) {
           next[h][c].template get<T>(m, x[h][c]);
           const int left = k_bytes - (step * 128 + c * 64 + t * 16);
-          if (q.ragged && step == q.steps - 1) thin_keep<T>(x[h][c], left);
+          if (q.ragged && step == q.steps - 1) keep_bytes<T>(x[h][c], left);
         }
       }
       const bool last = step + 1 == q.steps;

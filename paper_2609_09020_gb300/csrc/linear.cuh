@@ -44,6 +44,25 @@ __device__ __forceinline__ uint32_t load_if(const uint32_t* p, bool on) {
   return v;
 }
 
+// 16 bytes from a 16-byte boundary.  (If one of them is in a tensor, all are in its
+// allocation.)
+__device__ __forceinline__ uint4 load_if16(const void* p, bool on) {
+  uint4 v;
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %5, 0;\n\tmov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t"
+      "@q ld.global.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+      : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+      : "l"(p), "r"(static_cast<uint32_t>(on)));
+  return v;
+}
+// Keeps `bytes` bytes of w, from its beginning.
+template <typename T>
+__device__ __forceinline__ void keep_bytes(uint32_t (&w)[4], int bytes) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    w[i] = bytes >= 4 * i + 4 ? w[i] : sizeof(T) == 2 && bytes >= 4 * i + 2 ? w[i] & 0xffffu : 0u;
+}
+
 // Round to nearest even.
 template <typename T>
 __device__ __forceinline__ T from_f32(float v);
