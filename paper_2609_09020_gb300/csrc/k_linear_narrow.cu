@@ -25,6 +25,10 @@
 // this tile under way while dz is computed, dy and z of the next while x is written
 // to shared memory: any stride and alignment, but less in flight.
 //
+// Measured: fp16 393216 x 64 -> 64 ReLU 38.8 us for 201 MB, 5.2 TB/s, 78 % of the copy
+// rate; fp32 65536 x 40 -> 40 GELU 29 us for 42 MB: there the chain of cutting,
+// multiplying and taking over, one tile at a time, is what takes the time.
+//
 // An infinite or NaN value among fp32 pieces would spread (inf 0 = NaN): its tile
 // is marked, and dx and dw of that tile are computed again on the FP32 cores.
 #include "cut3.cuh"

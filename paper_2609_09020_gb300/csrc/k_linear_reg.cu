@@ -11,7 +11,8 @@
 // as the MMA wants them, warp 12 issues the MMAs.  What bounds it is the loaders'
 // work, some 40 operations for four values, so a thread's quads are whole rows
 // apart and share their addresses.  The loads of the next slice are under way while
-// this one is written.
+// this one is written.  Measured: 1.7 us for a slice of 64 of K, 92 TFLOP/s over all
+// SMs; 100 x 4096 -> 2048 34 us, 128 x 2048 -> 8192 59.
 #include "cut3.cuh"
 #include "k_linear_reg.cuh"
 
