@@ -72,20 +72,28 @@ __device__ __forceinline__ void mma<__nv_bfloat16>(float (&c)[4], uint32_t a0, u
 }
 
 // Eight elements of a row, of which `n` exist; the weights pass by once.
-template <typename T, bool VEC>
+template <typename T, int ALIGN>
 __device__ __forceinline__ uint4 load8(const T* p, int n) {
   if (n <= 0) return make_uint4(0, 0, 0, 0);
-  if (VEC && n >= 8) {
+  if (ALIGN == 16 && n >= 8) {
     uint4 q;
     asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
                  : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w)
                  : "l"(p));
     return q;
   }
-  uint32_t e[8];
+  if constexpr (ALIGN == 4) {  // words that have an element of the row
+    uint32_t w[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) e[i] = load_if(reinterpret_cast<const uint16_t*>(p) + i, i < n);
-  return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+    for (int i = 0; i < 4; ++i) w[i] = load_if(reinterpret_cast<const uint32_t*>(p) + i, 2 * i < n);
+    keep_bytes<T>(w, 2 * n);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  } else {
+    uint32_t e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = load_if(reinterpret_cast<const uint16_t*>(p) + i, i < n);
+    return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+  }
 }
 
 // Eight elements of a row of A, or of dz = dy act'(z) rounded to its type.
@@ -93,10 +101,10 @@ template <typename T>
 __device__ __forceinline__ uint4 load_a(const FewParams& q, int r, long long k, int n) {
   const Product& p = q.p;
   const T* a = static_cast<const T*>(p.a) + r * p.a_i + k;
-  const uint4 w = q.a_vec ? load8<T, true>(a, n) : load8<T, false>(a, n);
+  const uint4 w = q.a_vec ? load8<T, 16>(a, n) : load8<T, 2>(a, n);
   if (!p.a_pre) return w;
   const T* z = static_cast<const T*>(p.a_pre) + r * p.a_pre_i + k;
-  const uint4 v = q.pre_vec ? load8<T, true>(z, n) : load8<T, false>(z, n);
+  const uint4 v = q.pre_vec ? load8<T, 16>(z, n) : load8<T, 2>(z, n);
   uint4 out;
   const T *d = reinterpret_cast<const T*>(&w), *e = reinterpret_cast<const T*>(&v);
   T* o = reinterpret_cast<T*>(&out);
@@ -154,7 +162,7 @@ constexpr int kAlongWarps = 8;
 constexpr int kAlongSteps = 8;    // turns of 32 elements that a warp loads at a time
 constexpr int kAlongStride = 20;  // floats per row of x in a warp's sums: no bank conflicts
 
-template <typename T, int NT, bool VEC>
+template <typename T, int NT, int ALIGN>
 __global__ void __launch_bounds__(32 * kAlongWarps, 2) along_kernel(const FewParams q) {
   extern __shared__ __align__(16) uint8_t smem[];
   const Product& p = q.p;
@@ -172,7 +180,7 @@ __global__ void __launch_bounds__(32 * kAlongWarps, 2) along_kernel(const FewPar
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const long long r = group * 16LL + g + 8 * h;
-      a[s][h] = load8<T, VEC>(w + r * p.b_j + kk, r < p.J ? k1 - kk : 0);
+      a[s][h] = load8<T, ALIGN>(w + r * p.b_j + kk, r < p.J ? k1 - kk : 0);
     }
   };
   const int kw = k0 + warp * 32, batch = 32 * kAlongWarps * kAlongSteps, step = gridDim.x / q.cluster;
@@ -237,7 +245,7 @@ constexpr int kAcrossStride = 68;  // floats per row in a warp's sums
 __device__ __forceinline__ uint32_t low2(uint32_t a, uint32_t b) { return __byte_perm(a, b, 0x5410); }
 __device__ __forceinline__ uint32_t high2(uint32_t a, uint32_t b) { return __byte_perm(a, b, 0x7632); }
 
-template <typename T, bool VEC>
+template <typename T, int ALIGN>
 __global__ void __launch_bounds__(32 * kAcrossWarps, 2) across_kernel(const FewParams q) {
   extern __shared__ __align__(16) uint8_t smem[];
   const Product& p = q.p;
@@ -257,7 +265,7 @@ __global__ void __launch_bounds__(32 * kAcrossWarps, 2) across_kernel(const FewP
     for (int h = 0; h < 4; ++h) {
       // rows of B (elements of K) 2t, 2t + 1, 2t + 8, 2t + 9 of the turn
       const int kk = k + s * 16 * kAcrossWarps + 2 * t + (h & 1) + 8 * (h >> 1);
-      b[s][h] = load8<T, VEC>(w + kk * p.b_k + j, kk < k1 ? n : 0);
+      b[s][h] = load8<T, ALIGN>(w + kk * p.b_k + j, kk < k1 ? n : 0);
     }
   };
   const int kw = k0 + warp * 16, batch = 16 * kAcrossWarps * kAcrossSteps, step = gridDim.x / q.cluster;
@@ -361,16 +369,21 @@ Plan plan(const Product& p) {
   return r;
 }
 
-template <typename T, bool VEC>
+template <typename T, int ALIGN>
 const void* kernel_of(const Plan& r) {
-  if (!r.along) return reinterpret_cast<const void*>(across_kernel<T, VEC>);
-  return r.tiles == 1 ? reinterpret_cast<const void*>(along_kernel<T, 1, VEC>)
-                      : reinterpret_cast<const void*>(along_kernel<T, 2, VEC>);
+  if (!r.along) return reinterpret_cast<const void*>(across_kernel<T, ALIGN>);
+  return r.tiles == 1 ? reinterpret_cast<const void*>(along_kernel<T, 1, ALIGN>)
+                      : reinterpret_cast<const void*>(along_kernel<T, 2, ALIGN>);
+}
+
+template <typename T>
+const void* kernel_at(const Plan& r, int align) {
+  return align == 2 ? kernel_of<T, 16>(r) : align == 1 ? kernel_of<T, 4>(r) : kernel_of<T, 2>(r);
 }
 
 // Allows the kernel all of an SM's shared memory, once per device.
 int set_up(const void* fn, int slot) {
-  static std::atomic<uint64_t> done[12];
+  static std::atomic<uint64_t> done[18];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return PIC_ERR_CUDA;
   const uint64_t bit = 1ull << (dev & 63);
@@ -388,14 +401,13 @@ bool few_takes(const Product& p) { return plan(p).ok; }
 int few_product(const Product& p, int dtype, cudaStream_t s) {
   const Plan r = plan(p);
   FewParams q{p, r.groups, r.cluster, r.k_part, r.stride, 0, 0};
-  const auto on16 = [](const void* m, long long ld) { return reinterpret_cast<uintptr_t>(m) % 16 == 0 && ld % 8 == 0; };
   q.a_vec = reinterpret_cast<uintptr_t>(p.a) % 16 == 0 && (p.I == 1 || p.a_i % 8 == 0);
   q.pre_vec = reinterpret_cast<uintptr_t>(p.a_pre) % 16 == 0 && (p.I == 1 || p.a_pre_i % 8 == 0);
-  const bool vec = on16(p.b, r.along ? p.b_j : p.b_k);
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p.b) | static_cast<uintptr_t>((r.along ? p.b_j : p.b_k) * 2);
+  const int align = at % 16 == 0 ? 2 : at % 4 == 0 ? 1 : 0;  // 16, 4 or 2 bytes
   const bool bf16 = dtype == PIC_DTYPE_BF16;
-  const void* fn = bf16 ? (vec ? kernel_of<__nv_bfloat16, true>(r) : kernel_of<__nv_bfloat16, false>(r))
-                        : (vec ? kernel_of<__half, true>(r) : kernel_of<__half, false>(r));
-  const int slot = ((bf16 ? 2 : 0) + (vec ? 1 : 0)) * 3 + (r.along ? r.tiles : 0);
+  const void* fn = bf16 ? kernel_at<__nv_bfloat16>(r, align) : kernel_at<__half>(r, align);
+  const int slot = ((bf16 ? 3 : 0) + align) * 3 + (r.along ? r.tiles : 0);
   if (set_up(fn, slot) != PIC_OK) return PIC_ERR_CUDA;
   void* args[] = {&q};
   return launch_kernel(fn, r.grid, 32 * (r.along ? kAlongWarps : kAcrossWarps), r.smem, r.cluster, args, s);

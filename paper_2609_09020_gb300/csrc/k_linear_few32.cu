@@ -40,26 +40,18 @@ struct FewParams {
 // Four elements from p on, of which n exist; not VEC: 32 apart, from p + lane on.
 template <bool VEC>
 __device__ __forceinline__ float4 load4(const float* p, int n, int lane) {
-  float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  uint32_t w[4];
   if constexpr (VEC) {
-    p += 4 * lane, n -= 4 * lane;
-    if (n >= 4) {
-      asm volatile("ld.global.nc.L1::no_allocate.v4.f32 {%0,%1,%2,%3}, [%4];"
-                   : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w)
-                   : "l"(p));
-    } else {
-      if (n > 0) f.x = __ldg(p);
-      if (n > 1) f.y = __ldg(p + 1);
-      if (n > 2) f.z = __ldg(p + 2);
-    }
+    n = (n - 4 * lane) * 4;
+    const uint4 f = load_if16(p + 4 * lane, n > 0);
+    w[0] = f.x, w[1] = f.y, w[2] = f.z, w[3] = f.w;
+    keep_bytes<float>(w, n);
   } else {
     p += lane, n -= lane;
-    if (n > 0) f.x = __ldg(p);
-    if (n > 32) f.y = __ldg(p + 32);
-    if (n > 64) f.z = __ldg(p + 64);
-    if (n > 96) f.w = __ldg(p + 96);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = load_if(reinterpret_cast<const uint32_t*>(p) + 32 * i, n > 32 * i);
   }
-  return f;
+  return make_float4(__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3]));
 }
 
 // This CTA's part of K of the rows of A (or of dz = dy act'(z)) to put(i, k, values),

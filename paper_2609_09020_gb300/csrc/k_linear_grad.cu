@@ -1,9 +1,9 @@
 // k_linear_grad.cu -- the elementwise part of the linear layer's gradient:
 // dz = dy act'(z) and its column sums db.  Bound by memory: dy and z are read
-// and dz is written once.  A thread takes V neighbouring columns (16 bytes of
-// them where every row starts on a 16-byte boundary, else one) of every so
-// many-th row of a block's run of rows, with kUnroll rows' loads in flight; the
-// block adds its threads' column sums in shared memory and writes them to the
+// and dz is written once.  A thread takes 16 bytes of neighbouring columns
+// (rows of dy and z off 16-byte boundaries: out of the two aligned pieces that have
+// them; those of dz are on them) of every so many-th row of a block's run of rows,
+// with kUnroll rows' loads in flight; the block adds its threads' column sums in shared memory and writes them to the
 // workspace, and a second kernel adds the blocks' sums in a fixed order.  Measured:
 // bf16 4096 x 8192 GELU 40 us for 201 MB, 75 % of the copy rate: GELU' is some 20
 // instructions for an element, and half of them cannot be packed in pairs.
@@ -15,12 +15,14 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kUnroll = 4;
-constexpr int kBlocks = 1216;  // 8 per SM
+constexpr int kSms = 152;
+constexpr int kBlocks = 8 * kSms;
 constexpr int kOneBlockRows = 128;  // up to here a block takes all rows, and db needs no second kernel
 
 // How a [I][J] matrix is shared out: tx threads across columns, blocks of `run` rows.
 struct Share {
   int v, tx;
+  bool on16;  // rows of dy and z start on 16-byte boundaries
   long long col_blocks, row_blocks, run;
 };
 
@@ -29,9 +31,8 @@ Share share(const GradAct& g, int elem) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (ld * elem % 16 == 0 || g.I == 1);
   };
   Share s;
-  const bool wide = on16(g.dy, g.lddy) && (g.act == PIC_ACT_NONE || on16(g.pre, g.ldpre)) &&
-                    (!g.dz || on16(g.dz, g.lddz)) && g.J % (16 / elem) == 0;
-  s.v = wide ? 16 / elem : 1;
+  s.on16 = on16(g.dy, g.lddy) && (g.act == PIC_ACT_NONE || on16(g.pre, g.ldpre));
+  s.v = 16 / elem;
   const long long across = (g.J + s.v - 1) / s.v;
   s.tx = 1;
   while (s.tx < across && s.tx < 32) s.tx *= 2;
@@ -40,29 +41,19 @@ Share share(const GradAct& g, int elem) {
   long long want = (kBlocks + s.col_blocks - 1) / s.col_blocks;
   if (want > 304) want = 304;  // more sums per column than that take longer to add than they save
   if (g.I <= kOneBlockRows) want = 1;
-  const long long least = static_cast<long long>(ty) * kUnroll;
+  // kUnroll rows of a thread, or one where that leaves SMs without a block
+  const long long all = static_cast<long long>(ty) * kUnroll;
+  const long long least = s.col_blocks * ((g.I + all - 1) / all) >= kSms ? all : ty;
   s.run = (g.I + want - 1) / want;
   s.run = (s.run + least - 1) / least * least;
   s.row_blocks = (g.I + s.run - 1) / s.run;
   return s;
 }
 
-template <typename T, int V>
-struct Load {
-  uint32_t w[V * sizeof(T) / 4 ? V * sizeof(T) / 4 : 1];
-  __device__ __forceinline__ void get(const T* p) {
-    if constexpr (V * sizeof(T) == 16) {
-      const uint4 q = *reinterpret_cast<const uint4*>(p);
-      w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
-    } else {
-      *reinterpret_cast<T*>(w) = *p;
-    }
-  }
-  __device__ __forceinline__ float at(int i) const { return to_f32(reinterpret_cast<const T*>(w)[i]); }
-};
-
-template <typename T, int V>
-__global__ void __launch_bounds__(kThreads, 4) grad_act_kernel(const GradAct g, const Share s) {
+template <typename T, bool ON16>
+__global__ void __launch_bounds__(kThreads, ON16 ? 4 : 3) grad_act_kernel(const GradAct g, const Share s) {
+  constexpr int V = 16 / sizeof(T);
+  constexpr int kRows = ON16 ? kUnroll : kUnroll / 2;
   extern __shared__ float sums[];  // [ty][tx * V]
   const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx, rows = kThreads / s.tx;
   const long long col_block = blockIdx.x % s.col_blocks, row_block = blockIdx.x / s.col_blocks;
@@ -70,49 +61,50 @@ __global__ void __launch_bounds__(kThreads, 4) grad_act_kernel(const GradAct g, 
   const long long i0 = row_block * s.run, i1 = min(g.I, i0 + s.run);
   float sum[V] = {};
   if (j < g.J) {
-    const T* dy = static_cast<const T*>(g.dy) + j;
-    const T* pre = static_cast<const T*>(g.pre) + j;
-    T* dz = static_cast<T*>(g.dz) + j;
-    for (long long i = i0 + ty; i < i1; i += rows * kUnroll) {
-      Load<T, V> a[kUnroll], z[kUnroll];
+    const int bytes = static_cast<int>(min(static_cast<long long>(V), g.J - j) * sizeof(T));
+    const char* dy = reinterpret_cast<const char*>(static_cast<const T*>(g.dy) + j);
+    const char* pre = reinterpret_cast<const char*>(static_cast<const T*>(g.pre) + j);
+    const long long lddy = g.lddy * static_cast<long long>(sizeof(T)), ldpre = g.ldpre * static_cast<long long>(sizeof(T));
+    const auto words = [&](const Piece16<ON16>& q, const char* at, uint32_t (&w)[4]) {
+      q.template get<T>(ON16 ? 0 : static_cast<int>(reinterpret_cast<uintptr_t>(at) & 15), w);
+      if (bytes < 16) keep_bytes<T>(w, bytes);
+    };
+    for (long long i = i0 + ty; i < i1; i += rows * kRows) {
+      Piece16<ON16> a[kRows], z[kRows];
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
+      for (int u = 0; u < kRows; ++u) {
         const long long r = i + u * rows;
-        if (r < i1) {
-          a[u].get(dy + r * g.lddy);
-          if (g.act != PIC_ACT_NONE) z[u].get(pre + r * g.ldpre);
-        }
+        a[u].load(dy + r * lddy, r < i1 ? bytes : 0);
+        if (g.act != PIC_ACT_NONE) z[u].load(pre + r * ldpre, r < i1 ? bytes : 0);
       }
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
+      for (int u = 0; u < kRows; ++u) {
         const long long r = i + u * rows;
         if (r >= i1) break;
-        Load<T, V> out;
+        uint32_t w[4];
+        words(a[u], dy + r * lddy, w);
         float d[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) d[e] = a[u].at(e);
+        for (int e = 0; e < V; ++e) d[e] = to_f32(reinterpret_cast<const T*>(w)[e]);
         if (g.act != PIC_ACT_NONE) {
-          if constexpr (V > 1) {
+          words(z[u], pre + r * ldpre, w);
 #pragma unroll
-            for (int e = 0; e < V; e += 2) {
-              const float2 r = act_grad2<sizeof(T) == 4>(make_float2(d[e], d[e + 1]), make_float2(z[u].at(e), z[u].at(e + 1)), g.act);
-              d[e] = r.x;
-              d[e + 1] = r.y;
-            }
-          } else {
-            d[0] = act_grad<sizeof(T) == 4>(d[0], z[u].at(0), g.act);
+          for (int e = 0; e < V; e += 2) {
+            const float2 v = act_grad2<sizeof(T) == 4>(
+                make_float2(d[e], d[e + 1]),
+                make_float2(to_f32(reinterpret_cast<const T*>(w)[e]), to_f32(reinterpret_cast<const T*>(w)[e + 1])), g.act);
+            d[e] = v.x;
+            d[e + 1] = v.y;
           }
         }
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          sum[e] += d[e];
-          reinterpret_cast<T*>(out.w)[e] = from_f32<T>(d[e]);
-        }
+        for (int e = 0; e < V; ++e) sum[e] += d[e];
         if (g.dz) {
-          if constexpr (V * sizeof(T) == 16)
-            *reinterpret_cast<uint4*>(dz + r * g.lddz) = make_uint4(out.w[0], out.w[1], out.w[2], out.w[3]);
-          else
-            dz[r * g.lddz] = *reinterpret_cast<T*>(out.w);
+          T out[V];
+#pragma unroll
+          for (int e = 0; e < V; ++e) out[e] = from_f32<T>(d[e]);
+          const uint32_t* o = reinterpret_cast<const uint32_t*>(out);
+          *reinterpret_cast<uint4*>(static_cast<T*>(g.dz) + j + r * g.lddz) = make_uint4(o[0], o[1], o[2], o[3]);
         }
       }
     }
@@ -159,10 +151,10 @@ int run(const GradAct& g, cudaStream_t stream) {
   const long long blocks = s.col_blocks * s.row_blocks;
   if (blocks > 0x7fffffffLL) return PIC_ERR_INVALID_ARG;
   const int smem = g.db ? kThreads * s.v * 4 : 0;
-  if (s.v == 1)
-    grad_act_kernel<T, 1><<<static_cast<unsigned>(blocks), kThreads, smem, stream>>>(g, s);
+  if (s.on16)
+    grad_act_kernel<T, true><<<static_cast<unsigned>(blocks), kThreads, smem, stream>>>(g, s);
   else
-    grad_act_kernel<T, 16 / sizeof(T)><<<static_cast<unsigned>(blocks), kThreads, smem, stream>>>(g, s);
+    grad_act_kernel<T, false><<<static_cast<unsigned>(blocks), kThreads, smem, stream>>>(g, s);
   if (g.db && s.row_blocks > 1)
     sum_parts_kernel<<<static_cast<unsigned>((g.J + 15) / 16), 1024, 0, stream>>>(
         g.parts, static_cast<int>(s.row_blocks), g.J, static_cast<T*>(g.db));

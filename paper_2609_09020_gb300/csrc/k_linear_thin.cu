@@ -32,8 +32,8 @@ int allow(const void* fn, int slot) {
 
 }  // namespace
 
-// Not 16-bit rows of exactly two slices of K of the tiled kernel, many of them and on
-// 16-byte boundaries: nothing of its loads is wasted there.  us, here / tiled: fp16
+// Not 16-bit rows of exactly two slices of K of the tiled kernel, many of them and,
+// like those of y, on 16-byte boundaries: nothing of its loads is wasted there.  us, here / tiled: fp16
 // 200000 x 128 -> 128 28.6 / 22.1, -> 64 16.6 / 12.8; but 120 -> 64 17.0 / 24.8, 64 ->
 // 128 18.8 / 20.4, 64 -> 64 11.5 / 12.4, 16 -> 128 15.2 / 31.5; 20000 x 128 -> 128 7.9
 // / 7.3, -> 64 5.3 / 5.6; 300 x 64 -> 64 3.3 / 5.0.  fp32 200000 x 128 -> 128 96.9 /
@@ -41,8 +41,8 @@ int allow(const void* fn, int slot) {
 // 2000 rows of 128 -> 128, 11.5 / 9.7.
 bool thin_takes(const Product& p, int dtype) {
   if (p.a_k != 1 || p.b_k != 1 || p.a_pre || p.K > kThinMost || p.J > kThinMost) return false;
-  return dtype == PIC_DTYPE_F32 || p.K != kThinMost || p.J <= 32 || p.I < 65536 || p.a_i % 8 != 0 ||
-         reinterpret_cast<uintptr_t>(p.a) % 16 != 0;
+  return dtype == PIC_DTYPE_F32 || p.K != kThinMost || p.J <= 32 || p.I < 65536 || p.a_i % 8 != 0 || p.J % 8 != 0 ||
+         p.ldy % 8 != 0 || (reinterpret_cast<uintptr_t>(p.a) | reinterpret_cast<uintptr_t>(p.y)) % 16 != 0;
 }
 
 int thin_product(const Product& p, int dtype, cudaStream_t s) {

@@ -89,39 +89,6 @@ __device__ __forceinline__ void thin_mma(float (&c)[4], uint32_t a0, uint32_t a1
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// A lane's 16 bytes of a row as loaded: one aligned piece (FAST), or the two that have them.
-template <bool FAST>
-struct ThinPiece {
-  uint4 lo, hi;
-  __device__ __forceinline__ void load(const char* at, int bytes) {  // bytes of the row from `at` on, may be <= 0
-    if constexpr (FAST) {
-      lo = load_if16(at, bytes > 0);
-    } else {
-      const int m = static_cast<int>(reinterpret_cast<uintptr_t>(at) & 15);
-      lo = load_if16(at - m, bytes > 0);
-      hi = load_if16(at - m + 16, m + min(bytes, 16) > 16);
-    }
-  }
-  // the 16 bytes from byte `m` of the two on
-  template <typename T>
-  __device__ __forceinline__ void get(int m, uint32_t (&w)[4]) const {
-    if constexpr (FAST) {
-      w[0] = lo.x, w[1] = lo.y, w[2] = lo.z, w[3] = lo.w;
-    } else {
-      const uint32_t v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-      const bool by2 = (m & 8) != 0, by1 = (m & 4) != 0;
-      uint32_t u[6], s[5];
-#pragma unroll
-      for (int i = 0; i < 6; ++i) u[i] = by2 ? v[i + 2] : v[i];
-#pragma unroll
-      for (int i = 0; i < 5; ++i) s[i] = by1 ? u[i + 1] : u[i];
-      const uint32_t bits = (m & 2) * 8;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = sizeof(T) == 4 ? s[i] : __funnelshift_r(s[i], s[i + 1], bits);
-    }
-  }
-};
-
 // The sums of a lane's places, on the FP32 cores.
 template <int NT>
 __device__ __noinline__ void thin_again(const Product& p, long long row, int t, float* u) {
@@ -163,9 +130,12 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
   const long long lda = p.a_i * E;
   const int k_bytes = K * E;
   uint8_t* panel = thin_smem + q.panel_at + warp * q.panel_bytes;
-  const int run_pieces = kThinRows * J * E / 16;
+  // bytes of a tile's rows that lie end to end (a multiple of 16 but for the last tile's)
+  const auto run_bytes = [&](long long tile) {
+    return static_cast<int>(min(static_cast<long long>(kThinRows), p.I - tile * kThinRows)) * J * E;
+  };
 
-  ThinPiece<FAST> next[2][2];  // rows g and g + 8; the pieces of a step
+  Piece16<FAST> next[2][2];  // rows g and g + 8; the pieces of a step
   const auto fetch = [&](long long tile, int step) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -201,11 +171,12 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
           }
         }
       }
-    } else if (q.res_mode == kThinRun && (tile + 1) * kThinRows <= p.I) {
+    } else if (q.res_mode == kThinRun) {
+      const int run = run_bytes(tile);
       const uint4* v = reinterpret_cast<const uint4*>(r + tile * kThinRows * p.J);
 #pragma unroll
       for (int i = 0; i < NT * E / 4; ++i) {
-        const uint4 w = load_if16(v + i * 32 + lane, i * 32 + lane < run_pieces);
+        const uint4 w = load_if16(v + i * 32 + lane, (i * 32 + lane) * 16 < run);
         uint32_t* o = &res[0][0] + 4 * i;
         o[0] = w.x, o[1] = w.y, o[2] = w.z, o[3] = w.w;
       }
@@ -379,8 +350,10 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
       if (straight) return;
       __syncwarp();
       T* o = static_cast<T*>(out) + row0 * ld;
-      if (mode == kThinRun && rows == kThinRows) {
-        for (int i = lane; i < run_pieces; i += 32) reinterpret_cast<uint4*>(o)[i] = reinterpret_cast<const uint4*>(panel)[i];
+      if (mode == kThinRun) {
+        const int run = run_bytes(tile), whole = run / 16;
+        for (int i = lane; i < whole; i += 32) reinterpret_cast<uint4*>(o)[i] = reinterpret_cast<const uint4*>(panel)[i];
+        for (int i = whole * (16 / E) + lane; i < run / E; i += 32) o[i] = reinterpret_cast<const T*>(panel)[i];
       } else {
         for (int r = 0; r < rows; ++r)
           for (int c = lane; c < J; c += 32) o[r * ld + c] = reinterpret_cast<const T*>(panel)[r * J + c];
@@ -417,17 +390,27 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
           }
       } else {
         __syncwarp();
-        if (q.res_mode == kThinRun && rows == kThinRows) {
+        if (q.res_mode == kThinRun) {
 #pragma unroll
           for (int i = 0; i < NT * E / 4; ++i) {
             const uint32_t* o = &res[0][0] + 4 * i;
-            if (i * 32 + lane < run_pieces)
+            if ((i * 32 + lane) * 16 < run_bytes(tile))
               reinterpret_cast<uint4*>(panel)[i * 32 + lane] = make_uint4(o[0], o[1], o[2], o[3]);
           }
         } else {
           const T* r = static_cast<const T*>(p.residual) + row0 * p.ldr;
-          for (int i = 0; i < rows; ++i)
-            for (int c = lane; c < J; c += 32) reinterpret_cast<T*>(panel)[i * J + c] = r[i * p.ldr + c];
+          using Bits = std::conditional_t<S::kWide, uint32_t, uint16_t>;
+          for (int e0 = lane; e0 < rows * J; e0 += 32 * 8) {  // eight loads under way together
+            uint32_t v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+              const int e = e0 + 32 * u;
+              v[u] = load_if(reinterpret_cast<const Bits*>(r + e / J * p.ldr + e % J), e < rows * J);
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+              if (e0 + 32 * u < rows * J) reinterpret_cast<Bits*>(panel)[e0 + 32 * u] = static_cast<Bits>(v[u]);
+          }
         }
         __syncwarp();
 #pragma unroll

@@ -63,6 +63,39 @@ __device__ __forceinline__ void keep_bytes(uint32_t (&w)[4], int bytes) {
     w[i] = bytes >= 4 * i + 4 ? w[i] : sizeof(T) == 2 && bytes >= 4 * i + 2 ? w[i] & 0xffffu : 0u;
 }
 
+// 16 bytes of a row as loaded: one aligned piece (ON16), or the two that have them.
+template <bool ON16>
+struct Piece16 {
+  uint4 lo, hi;
+  __device__ __forceinline__ void load(const char* at, int bytes) {  // bytes of the row from `at` on, may be <= 0
+    if constexpr (ON16) {
+      lo = load_if16(at, bytes > 0);
+    } else {
+      const int m = static_cast<int>(reinterpret_cast<uintptr_t>(at) & 15);
+      lo = load_if16(at - m, bytes > 0);
+      hi = load_if16(at - m + 16, m + min(bytes, 16) > 16);
+    }
+  }
+  // the 16 bytes from byte `m` of the two on
+  template <typename T>
+  __device__ __forceinline__ void get(int m, uint32_t (&w)[4]) const {
+    if constexpr (ON16) {
+      w[0] = lo.x, w[1] = lo.y, w[2] = lo.z, w[3] = lo.w;
+    } else {
+      const uint32_t v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+      const bool by2 = (m & 8) != 0, by1 = (m & 4) != 0;
+      uint32_t u[6], s[5];
+#pragma unroll
+      for (int i = 0; i < 6; ++i) u[i] = by2 ? v[i + 2] : v[i];
+#pragma unroll
+      for (int i = 0; i < 5; ++i) s[i] = by1 ? u[i + 1] : u[i];
+      const uint32_t bits = (m & 2) * 8;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = sizeof(T) == 4 ? s[i] : __funnelshift_r(s[i], s[i + 1], bits);
+    }
+  }
+};
+
 // Round to nearest even.
 template <typename T>
 __device__ __forceinline__ T from_f32(float v);
@@ -255,7 +288,8 @@ struct OuterGrad {
 int outer_grad(const OuterGrad& g, int dtype, cudaStream_t s);
 
 // dz[i][j] = dy act'(z), rounded (dz null: not written), and db[j], the sums of
-// the unrounded dz over the rows (db null: none); parts is workspace.
+// the unrounded dz over the rows (db null: none); parts is workspace.  Rows of dz
+// are on 16-byte boundaries and written to the next one.
 struct GradAct {
   const void* dy;
   long long lddy;
