@@ -3,10 +3,11 @@
 // and dz is written once.  A thread takes 16 bytes of neighbouring columns
 // (rows of dy and z off 16-byte boundaries: out of the two aligned pieces that have
 // them; those of dz are on them) of every so many-th row of a block's run of rows,
-// with kUnroll rows' loads in flight; the block adds its threads' column sums in shared memory and writes them to the
-// workspace, and a second kernel adds the blocks' sums in a fixed order.  Measured:
-// bf16 4096 x 8192 GELU 37 us for db alone and 134 MB, 40 with dz: GELU' is some 20
-// instructions for an element, and half of them cannot be packed in pairs.
+// with kUnroll rows' loads in flight; the block adds its threads' column sums in
+// shared memory and writes them to the workspace, and a second kernel adds the
+// blocks' sums in a fixed order.  Measured: bf16 4096 x 8192 GELU 37 us for db alone
+// and 134 MB, 40 with dz: GELU' is some 20 instructions for an element, and half of
+// them cannot be packed in pairs.
 #include "linear.cuh"
 
 namespace pic {
