@@ -297,7 +297,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         continue;
       }
       if (row0 >= p.I) continue;
-      finish_rows(v, p, turn, lane, row0, col0);
+      if (p.swapped)
+        finish_swapped(v, p, lane, row0, col0);
+      else
+        finish_rows(v, p, turn, lane, row0, col0);
     }
     __syncwarp();
   }

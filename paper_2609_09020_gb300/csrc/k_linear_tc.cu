@@ -228,6 +228,8 @@ void choose_fp32(Plan& r, const Product& p, bool rows16) {
   ShapeCost reg = kShapeReg;
   if (!rows16) reg.slice *= 1.15;
   const double on_the_way = choose(r, p, &reg, 1, 4, true);
+  r.reg = true;
+  if (p.swapped) return;
   const double elements = static_cast<double>(p.K) * static_cast<double>(p.I + p.J);
   const double first = choose(other, p, &kShapePlanes, 1, 4, true) + 4.0 + elements * 10.0 / 5e6;
   if (first < on_the_way) {
@@ -235,6 +237,21 @@ void choose_fp32(Plan& r, const Product& p, bool rows16) {
     r.planes = true;
   }
   r.reg = !r.planes;
+}
+
+// fp32 with no more rows than the smaller side of a tile through registers: w takes the
+// larger one where fewer tiles are less time, which is where there are many (us, 12 x
+// 4096 -> 8192 70 instead of 105, 48 x 2048 -> 8192 35 instead of 51).  Columns of y a
+// row apart cost a little: 33 x 2048 -> 512 14.8 instead of 13.5.
+Product oriented(const Product& p, int dtype) {
+  if (dtype != PIC_DTYPE_F32 || p.I > kRegCols || p.J <= kRegRows) return p;
+  Product q = p;
+  q.a = p.b, q.a_i = p.b_j, q.a_k = p.b_k, q.I = p.J;
+  q.b = p.a, q.b_j = p.a_i, q.b_k = p.a_k, q.J = p.I;
+  q.swapped = 1;
+  Plan r{};
+  r.k_blocks = static_cast<int>((p.K + kSlice - 1) / kSlice);
+  return choose(r, q, &kShapeReg, 1, 4, true) + 1.5 < choose(r, p, &kShapeReg, 1, 4, true) ? q : p;
 }
 
 Plan plan(const Product& p, int dtype) {
@@ -362,11 +379,12 @@ int allow_smem(const void* fn, int slot, int smem) {
 }
 
 long long tc_workspace(const Product& p, int dtype) {
-  const Plan r = plan(p, dtype);
+  const Plan r = plan(oriented(p, dtype), dtype);
   return r.a_bytes + r.b_bytes + r.part_bytes;
 }
 
-int tc_product(const Product& p, int dtype, void* ws, const Waits& waits, cudaStream_t s) {
+int tc_product(const Product& given, int dtype, void* ws, const Waits& waits, cudaStream_t s) {
+  const Product p = oriented(given, dtype);
   const Plan r = plan(p, dtype);
   const long long elem = dtype == PIC_DTYPE_F32 ? 4 : 2;
   char* w = static_cast<char*>(ws);

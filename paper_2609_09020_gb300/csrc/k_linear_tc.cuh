@@ -408,6 +408,34 @@ __device__ __forceinline__ void finish_rows(const float (&v)[64], const Product&
   }
 }
 
+// The same of a swapped product: a lane's row is a column of y, and neighbouring lanes'
+// are neighbours.
+__device__ __forceinline__ void finish_swapped(const float (&v)[64], const Product& p, int lane, long long row0,
+                                               long long col0) {
+  const long long i = row0 + lane;
+  if (i >= p.I) return;
+  const int cols = static_cast<int>(min(64LL, p.J - col0));
+  const float bias = p.bias ? static_cast<const float*>(p.bias)[i] : 0.0f;
+#pragma unroll
+  for (int c0 = 0; c0 < 64; c0 += 8) {
+    if (c0 >= cols) break;
+    float q[8] = {};
+    if (p.residual) {
+      const uint32_t* res = static_cast<const uint32_t*>(p.residual) + (col0 + c0) * p.ldr + i;
+#pragma unroll
+      for (int u = 0; u < 8; ++u, res += p.ldr) q[u] = __uint_as_float(load_if(res, c0 + u < cols));
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (c0 + u >= cols) break;
+      const long long j = col0 + c0 + u;
+      const float z = v[c0 + u] + bias;
+      if (p.pre) static_cast<float*>(p.pre)[j * p.ldpre + i] = z;
+      static_cast<float*>(p.y)[j * p.ldy + i] = act_value<true>(z, p.act) + q[u];
+    }
+  }
+}
+
 // A product cut along K: a tile's parts are [rank][panel][quarter][16][32 rows][4
 // columns] of fp32 each; an item is four columns of a row, and neighbouring items
 // are neighbouring columns.
@@ -427,6 +455,21 @@ __device__ __forceinline__ JoinItem join_place(int in, int bn, long long ti, lon
 template <typename T>
 __device__ __forceinline__ void finish_item(const Product& p, const JoinItem& m, const float4& sum) {
   const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+  if constexpr (sizeof(T) == 4) {
+    if (p.swapped) {
+      const float b = p.bias ? static_cast<const float*>(p.bias)[m.i] : 0.0f;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const long long j = m.j + c;
+        if (j >= p.J) break;
+        if (p.pre) static_cast<float*>(p.pre)[j * p.ldpre + m.i] = v[c] + b;
+        float z = act_value<true>(v[c] + b, p.act);
+        if (p.residual) z += static_cast<const float*>(p.residual)[j * p.ldr + m.i];
+        static_cast<float*>(p.y)[j * p.ldy + m.i] = z;
+      }
+      return;
+    }
+  }
   T y[4], pre[4];
   const int cols = static_cast<int>(min(4LL, p.J - m.j));
   struct alignas(4 * sizeof(T)) Four {

@@ -222,6 +222,9 @@ struct Product {
   const void* a_pre;
   long long a_pre_i;
   int a_act;
+  // A is w and B is x: C(i, j) belongs at [j][i] of y, pre and the residual, and to
+  // bias[i] (set and read by the fp32 products through registers only)
+  int swapped;
 };
 
 // Launches a kernel in clusters of `cluster` CTAs along x.

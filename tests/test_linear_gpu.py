@@ -471,3 +471,28 @@ def test_narrow_nonfinite(pad, dtype):
     y = pic.linear(x, w)
     assert bool((y[:, 49] == -math.inf).all())
     ref.check(y[:, :49], (want[:, :49], tol[:, :49]))
+
+
+@pytest.mark.parametrize("size", [(9, 700, 9000), (33, 2100, 5003), (64, 4097, 2050), (10, 130, 30000)], ids=str)
+def test_fp32_few_rows_many_columns(size):
+    """fp32 with fewer rows than a tile over wide outputs, infinities and gradients included."""
+    from paper_2609_09020_gb300 import pic
+    M, K, N = size
+    dtype = torch.float32
+    x, w = normal((M, K), dtype, 1), normal((N, K), dtype, 2, 1.4 / math.sqrt(K))
+    b, r, dy = normal((N,), dtype, 3, 0.1), normal((M, N), dtype, 4), normal((M, N), dtype, 5, 0.1)
+    for act, res in (("gelu", r), ("none", None)):
+        y, z = pic.linear(x, w, b, act=act, residual=res, save_pre=True)
+        want_y, want_z = ref.forward(x, w, b, act, res)
+        ref.check(y, want_y, "y")
+        ref.check(z, want_z, "pre")
+        assert torch.equal(y, pic.linear(x, w, b, act=act, residual=res))
+    got = pic.linear_backward(dy, x, w, act="gelu", pre=z)
+    for g, v, name in zip(got, ref.backward(dy, x, w, z, "gelu"), ("dx", "dw", "db")):
+        ref.check(g, v, name)
+    x[M - 1, 5] = math.inf
+    want = torch.sign(w[:, 5]) * math.inf
+    y2 = pic.linear(x, w, b)
+    assert torch.equal(y2[M - 1], want)
+    ref.check(y2[:M - 1], tuple(t[:M - 1] for t in ref.forward(x[:M - 1], w, b, "none", None)[0]), "y")
+    pic.linear_check()
