@@ -46,18 +46,29 @@ __device__ __forceinline__ void cut3(uint32_t a, uint32_t b, uint32_t& hi, uint3
   lo = __byte_perm(__float_as_uint(ra), __float_as_uint(rb), 0x7632);
 }
 
-// v[c] = the sum over elements [k0, k1) of K for row i and N columns from col0,
-// on the FP32 cores.  a, b: where A(0, 0) and B(0, 0) are; strides per row and per K.
+// Adds to v[c] the sum over elements [k0, k1) of K for row i
+// and N columns from col0, on the FP32 cores, eight columns at a time.  a, b: where
+// A(0, 0) and B(0, 0) are; strides per row and per K.  Its callers ask for one
+// takeover's K, 128 at most, so that the waits of a CTA's other warps do not grow with K.
 template <int N>
-__device__ __noinline__ void sum_again(float* v, const float* a, long long a_i, long long a_k, const float* b,
-                                       long long b_j, long long b_k, long long i, long long I, long long col0,
-                                       long long J, long long k0, long long k1) {
-  for (int c = 0; c < N; ++c) {
-    const long long j = col0 + c;
-    float s = 0.0f;
-    if (i < I && j < J)
-      for (long long k = k0; k < k1; ++k) s = fmaf(a[i * a_i + k * a_k], b[j * b_j + k * b_k], s);
-    v[c] = s;
+__device__ __forceinline__ void sum_again(float (&v)[N], const float* a, long long a_i, long long a_k, const float* b,
+                                          long long b_j, long long b_k, long long i, long long I, long long col0,
+                                          long long J, long long k0, long long k1) {
+  static_assert(N % 8 == 0, "columns in eights");
+  a += i * a_i + k0 * a_k, b += col0 * b_j + k0 * b_k;
+  const int n = i < I ? static_cast<int>(k1 - k0) : 0, cols = static_cast<int>(min(static_cast<long long>(N), J - col0));
+#pragma unroll
+  for (int c = 0; c < N; c += 8) {
+    float s[8] = {};
+#pragma unroll 1
+    for (int k = 0; k < n; ++k) {
+      const float x = a[k * a_k];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (c + u < cols) s[u] = fmaf(x, b[(c + u) * b_j + k * b_k], s[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[c + u] += s[u];
   }
 }
 

@@ -14,8 +14,9 @@
 // each, which takes the accumulators over after every kTakeover slices.
 //
 // An infinite or NaN value would meet the zero pieces of others (inf 0 = NaN), so
-// the first kernel marks the blocks that have one, and an epilogue warp whose
-// rows or columns are marked computes its sums again with FP32 FMAs.
+// the first kernel marks the blocks of 128 x 128 that have one, and an epilogue warp
+// computes the sums of a takeover's K, where its rows or columns are marked there,
+// again with FP32 FMAs: no wait is longer than a few such sums, however long K is.
 #include "cut3.cuh"
 #include "k_linear_planes.cuh"
 
@@ -94,6 +95,51 @@ __device__ __forceinline__ bool marked(const PlOperand& o, bool mn, long long gr
   for (int b = k0 / 2 + lane; b <= (k1 - 1) / 2; b += 32)
     bad |= o.marks[mn ? b * static_cast<long long>(o.col_blocks) + group : group * o.col_blocks + b] != 0;
   return __any_sync(0xffffffffu, bad);
+}
+__device__ __forceinline__ bool marked_in(const PlOperands& o, const TcParams& q, long long a_group, long long b_group,
+                                          int k0, int k1, int lane) {
+  return marked(o.a, q.a_mn, a_group, (q.p.I + 127) / 128, k0, k1, lane) ||
+         marked(o.b, q.b_mn, b_group, (q.p.J + 127) / 128, k0, k1, lane);
+}
+
+// The epilogue's takeovers of slices [k0, k1) where some are marked: those from memory
+// again.  A function of its own, so that it takes no registers from the usual path
+// (inlined, 2048 x 1024 -> 4096 took 92 us instead of 84).
+struct TakeMarked {
+  long long a_group, b_group, row, col0;
+  int k0, k1, lane;
+  uint32_t tmem, bar_acc, lead_free;
+  bool withhold;
+  volatile int* abort_flag;
+};
+__device__ __noinline__ bool take_marked(float* out, const TcParams& q, const PlOperands& o, const TakeMarked& m, int buf,
+                                         uint32_t phase) {
+  float v[64] = {};
+  for (int c0 = m.k0; c0 < m.k1; c0 += kTakeover) {
+    if (!__all_sync(0xffffffffu, wait_bounded(m.bar_acc + 8 * buf, phase, m.abort_flag, q.waits))) return false;
+    tc::tc_fence_after();
+    const int c1 = min(m.k1, c0 + kTakeover);
+    if (marked_in(o, q, m.a_group, m.b_group, c0, c1, m.lane)) {
+      sum_again(v, o.a.m, q.a_mn ? 1 : o.a.ld, q.a_mn ? o.a.ld : 1, o.b.m, q.b_mn ? 1 : o.b.ld, q.b_mn ? o.b.ld : 1,
+                m.row, q.p.I, m.col0, q.p.J, c0 * 64LL, min(q.p.K, c1 * 64LL));
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t r[32];
+        tc::tmem_ld32_wait(m.tmem + buf * kPlCols + 32 * h, r);
+#pragma unroll
+        for (int c = 0; c < 32; ++c)
+          v[32 * h + c] += __uint_as_float(r[c]);
+      }
+    }
+    tc::tc_fence_before();
+    __syncwarp();
+    if (m.lane == 0 && !m.withhold) tc::mbar_arrive_cluster(m.lead_free + 8 * buf);
+    if (++buf == kBufs) buf = 0, phase ^= 1;
+  }
+#pragma unroll
+  for (int c = 0; c < 64; ++c) out[c] = v[c];
+  return true;
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
@@ -231,7 +277,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int quarter = warp & 3, half = (warp - 2) >> 2;
     float* turn = reinterpret_cast<float*>(smem + kOffPanels + (warp - 2) * kTurnBytes);
     const uint32_t lead_free = tc::map_rank(bar_free, 0);
-    const long long a_groups = (p.I + 127) / 128, b_groups = (p.J + 127) / 128;
     int buf = 0;
     for (long long w = first; w < q.work && ok; w += step) {
       long long ti, tj;
@@ -240,32 +285,38 @@ __global__ void __launch_bounds__(kThreads, 1)
       int k0, k1;
       part(w, k0, k1);
       float v[64];
-      for (int c0 = k0; c0 < k1; c0 += kTakeover) {
-        ok = __all_sync(0xffffffffu, wait(bar_acc + 8 * buf, phase));
-        if (!ok) break;
-        tc::tc_fence_after();
-        const uint32_t d = tmem + buf * kPlCols + half * 64 + (static_cast<uint32_t>(quarter * 32) << 16);
+      const bool withhold = q.waits.test_fault && w == 0 && rank == 0 && warp == 2;
+      if (!marked_in(o, q, ti * 2 + rank, tj, k0, k1, lane)) {
+        for (int c0 = k0; c0 < k1; c0 += kTakeover) {
+          ok = __all_sync(0xffffffffu, wait(bar_acc + 8 * buf, phase));
+          if (!ok) break;
+          tc::tc_fence_after();
+          const uint32_t d = tmem + buf * kPlCols + half * 64 + (static_cast<uint32_t>(quarter * 32) << 16);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t r[32];
-          tc::tmem_ld32_wait(d + 32 * h, r);
+          for (int h = 0; h < 2; ++h) {
+            uint32_t r[32];
+            tc::tmem_ld32_wait(d + 32 * h, r);
 #pragma unroll
-          for (int c = 0; c < 32; ++c)
-            v[32 * h + c] = c0 == k0 ? __uint_as_float(r[c]) : v[32 * h + c] + __uint_as_float(r[c]);
+            for (int c = 0; c < 32; ++c)
+              v[32 * h + c] = c0 == k0 ? __uint_as_float(r[c]) : v[32 * h + c] + __uint_as_float(r[c]);
+          }
+          tc::tc_fence_before();
+          __syncwarp();
+          if (lane == 0 && !withhold) tc::mbar_arrive_cluster(lead_free + 8 * buf);
+          if (++buf == kBufs) buf = 0, phase ^= 1;
         }
-        tc::tc_fence_before();
-        __syncwarp();
-        if (lane == 0 && !(q.waits.test_fault && w == 0 && rank == 0 && warp == 2)) tc::mbar_arrive_cluster(lead_free + 8 * buf);
-        if (++buf == kBufs) buf = 0, phase ^= 1;
-      }
-      if (!ok) break;
-      if (marked(o.a, q.a_mn, ti * 2 + rank, a_groups, k0, k1, lane) || marked(o.b, q.b_mn, tj, b_groups, k0, k1, lane)) {
+      } else {
         float u[64];
-        sum_again<64>(u, o.a.m, q.a_mn ? 1 : o.a.ld, q.a_mn ? o.a.ld : 1, o.b.m, q.b_mn ? 1 : o.b.ld, q.b_mn ? o.b.ld : 1,
-                      row0 + lane, p.I, col0, p.J, k0 * 64LL, min(p.K, k1 * 64LL));
+        const TakeMarked m{ti * 2 + rank, tj, row0 + lane, col0, k0, k1, lane,
+                           tmem + half * 64 + (static_cast<uint32_t>(quarter * 32) << 16), bar_acc, lead_free, withhold,
+                           abort_flag};
+        ok = take_marked(u, q, o, m, buf, phase);
+        buf += (k1 - k0 + kTakeover - 1) / kTakeover;
+        phase ^= buf / kBufs & 1, buf %= kBufs;
 #pragma unroll
         for (int c = 0; c < 64; ++c) v[c] = u[c];
       }
+      if (!ok) break;
       if (q.parts) {
         float4* out = reinterpret_cast<float4*>(q.parts) + ((w * 2 + rank) * 2 + half) * (128 * 16) + quarter * (32 * 16) + lane;
 #pragma unroll

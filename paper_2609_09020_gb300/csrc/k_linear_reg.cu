@@ -3,8 +3,9 @@
 // 64; the cuts along K are those of k_linear_tc.cuh.
 //
 // An infinite or NaN value would meet the zero pieces of others (inf 0 = NaN), so
-// a loader that sees one marks the tile, and its epilogue computes the tile's
-// sums again with FP32 FMAs from global memory: right, and only then slow.
+// a loader that sees one marks the takeover (two slices) it belongs to, and the
+// epilogue computes that takeover's sums again with FP32 FMAs from global memory:
+// right, and only then slow; no wait is longer than a few such sums, however long K is.
 //
 // Roles: warps 0..3 epilogue (32 rows each), warps 4..11 load slices of A and B (16
 // bytes per lane and load where they may), cut them and write them to shared memory
@@ -22,7 +23,7 @@ namespace {
 
 constexpr int kEpiWarps = 4, kLoadWarps = 8, kMmaWarp = kEpiWarps + kLoadWarps;
 constexpr int kThreads = 32 * (kMmaWarp + 1), kLoaders = 32 * kLoadWarps;
-constexpr int kMarks = 16;  // more than the tiles that the loaders can be ahead of the epilogue
+constexpr unsigned kMarks = 16;  // more than the takeovers that the loaders can be ahead of the epilogue (5)
 constexpr int kChunk = 2;  // slices of 64 between two takeovers of the accumulators
 
 constexpr int kAPlane = kRegRows * 128, kBPlane = kRegCols * 128;  // bytes
@@ -97,6 +98,48 @@ struct Slice {
   }
 };
 
+// The epilogue's takeovers from slice c0 to the tile's end, where the first is marked: those
+// that are, added to v from memory again.  A function of its own, so that it takes no
+// registers from the usual path.
+struct TakeMarked {
+  long long row, col0;
+  int c0, k1, lane;
+  uint32_t tmem, bar_acc, bar_free;
+  bool withhold;
+  volatile int* abort_flag;
+  volatile unsigned* marks;
+};
+__device__ __noinline__ bool take_marked(float* sums, const TcParams& q, const RegOperands& o, const TakeMarked& m, int buf,
+                                         uint32_t phase, unsigned takeover) {
+  float v[64];
+#pragma unroll
+  for (int c = 0; c < 64; ++c) v[c] = sums[c];
+  for (int c0 = m.c0; c0 < m.k1; c0 += kChunk, ++takeover) {
+    if (!__all_sync(0xffffffffu, wait_bounded(m.bar_acc + 8 * buf, phase, m.abort_flag, q.waits))) return false;
+    tc::tc_fence_after();
+    if (m.marks[takeover % kMarks] == takeover + 1) {
+      sum_again(v, static_cast<const float*>(o.a), q.a_mn ? 1 : o.lda, q.a_mn ? o.lda : 1, static_cast<const float*>(o.b),
+                q.b_mn ? 1 : o.ldb, q.b_mn ? o.ldb : 1, m.row, q.p.I, m.col0, q.p.J, c0 * 64LL,
+                min(q.p.K, min(m.k1, c0 + kChunk) * 64LL));
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t r[32];
+        tc::tmem_ld32_wait(m.tmem + buf * kRegCols + 32 * h, r);
+#pragma unroll
+        for (int c = 0; c < 32; ++c) v[32 * h + c] += __uint_as_float(r[c]);
+      }
+    }
+    tc::tc_fence_before();
+    __syncwarp();
+    if (m.lane == 0 && !m.withhold) tc::mbar_arrive(m.bar_free + 8 * buf);
+    if (++buf == kBufs) buf = 0, phase ^= 1;
+  }
+#pragma unroll
+  for (int c = 0; c < 64; ++c) sums[c] = v[c];
+  return true;
+}
+
 __global__ void __launch_bounds__(kThreads, 1)
     reg_kernel(const __grid_constant__ TcParams q, const __grid_constant__ TcMaps maps, const __grid_constant__ RegOperands o) {
   extern __shared__ uint8_t smem_raw[];
@@ -109,8 +152,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                  bar_free = bar_acc + 8 * kBufs, bar_drain = bar_free + 8 * kBufs;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kOffBars + 8 * kBars);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kOffBars + 8 * kBars + 4);
-  // mark t % kMarks holds t + 1 if this CTA's t-th tile has an infinite or NaN operand
-  volatile int* marks = reinterpret_cast<volatile int*>(smem + kOffMarks);
+  // mark t % kMarks holds t + 1 if this CTA's t-th takeover has an infinite or NaN operand
+  volatile unsigned* marks = reinterpret_cast<volatile unsigned*>(smem + kOffMarks);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -123,7 +166,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     tc::mbar_init(bar_drain, 1);
     *abort_flag = 0;
-    for (int m = 0; m < kMarks; ++m) marks[m] = 0;
+    for (unsigned m = 0; m < kMarks; ++m) marks[m] = 0;
     tc::fence_mbar_init();
   }
   if (warp == kMmaWarp) tc::tmem_alloc_cg<1>(tc::smem_addr(tmem_slot), kTmemCols);
@@ -148,19 +191,20 @@ __global__ void __launch_bounds__(kThreads, 1)
     // a place in the CTA's sequence of slices; loads are one slice ahead of stores
     struct Cursor {
       long long w, ti, tj;
-      int kb, k1, tile;
+      int k0, kb, k1;
+      unsigned takeover;
     };
     auto enter = [&](Cursor& c) {
       if (c.w >= q.work) return;
-      int k0;
-      part(c.w, k0, c.k1);
+      part(c.w, c.k0, c.k1);
       tile_place<kRegRows>(c.w / q.splits, q.tiles_i, q.tiles_j, c.ti, c.tj);
-      c.kb = k0;
+      c.kb = c.k0;
     };
     auto advance = [&](Cursor& c) {
-      if (++c.kb < c.k1) return;
+      ++c.kb;
+      if (c.kb == c.k1 || (c.kb - c.k0) % kChunk == 0) ++c.takeover;
+      if (c.kb < c.k1) return;
       c.w += gridDim.x;
-      ++c.tile;
       enter(c);
     };
     auto load_a = [&](Slice<kRegRows>& x, const Cursor& c) {
@@ -179,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     };
     // a B that is the same for all tiles is written to every stage once
     const bool fixed_b = q.tiles_j == 1 && q.k_blocks == 1;
-    Cursor put{blockIdx.x, 0, 0, 0, 0, 0};
+    Cursor put{blockIdx.x, 0, 0, 0, 0, 0, 0};
     enter(put);
     Cursor get = put;
     load_a(a, get);
@@ -198,7 +242,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!fixed_b || filled < kStages) bad_b |= b.store(sa + kPieces * kAPlane, q.b_mn, p.J - put.tj * kRegCols, tid);
       ++filled;
       if (!fixed_b) load_b(b, get);
-      if (bad || bad_b) marks[put.tile % kMarks] = put.tile + 1;
+      if (bad || bad_b) marks[put.takeover % kMarks] = put.takeover + 1;
       if (!fixed_b) bad_b = false;
       if (get.w < q.work) advance(get);
       advance(put);
@@ -254,20 +298,37 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else {
     const int quarter = warp;
     float* turn = reinterpret_cast<float*>(smem + kOffPanels + warp * kTurnBytes);
-    int buf = 0, tile = 0;
+    int buf = 0;
+    unsigned takeover = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (long long w = blockIdx.x; w < q.work && ok; w += gridDim.x, ++tile) {
+    for (long long w = blockIdx.x; w < q.work && ok; w += gridDim.x) {
       long long ti, tj;
       tile_place<kRegRows>(w / q.splits, q.tiles_i, q.tiles_j, ti, tj);
       const long long row0 = ti * kRegRows + quarter * 32, col0 = tj * kRegCols;
       int k0, k1;
       part(w, k0, k1);
       float v[64];
-      for (int c0 = k0; c0 < k1; c0 += kChunk) {
+      for (int c0 = k0; c0 < k1; c0 += kChunk, ++takeover) {
         ok = __all_sync(0xffffffffu, wait(bar_acc + 8 * buf, phase));
         if (!ok) break;
         tc::tc_fence_after();
+        if (marks[takeover % kMarks] == takeover + 1) {  // the rest of the tile's
+          float u[64];
+#pragma unroll
+          for (int c = 0; c < 64; ++c) u[c] = c0 == k0 ? 0.0f : v[c];
+          const TakeMarked m{row0 + lane, col0, c0, k1, lane, tmem + (static_cast<uint32_t>(quarter * 32) << 16), bar_acc,
+                             bar_free, q.waits.test_fault && w == 0 && quarter == 0, abort_flag, marks};
+          ok = take_marked(u, q, o, m, buf, phase, takeover);
+#pragma unroll
+          for (int c = 0; c < 64; ++c) v[c] = u[c];
+          const int n = (k1 - c0 + kChunk - 1) / kChunk;
+          takeover += n - 1, buf += n;
+          phase ^= buf / kBufs & 1, buf %= kBufs;
+          c0 = k1;
+          if (!ok) break;
+          continue;
+        }
         const uint32_t d = tmem + buf * kRegCols + (static_cast<uint32_t>(quarter * 32) << 16);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -283,13 +344,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (++buf == kBufs) buf = 0, phase ^= 1;
       }
       if (!ok) break;
-      if (marks[tile % kMarks] == tile + 1) {
-        float u[64];
-        sum_again<64>(u, ma, q.a_mn ? 1 : o.lda, q.a_mn ? o.lda : 1, mb, q.b_mn ? 1 : o.ldb, q.b_mn ? o.ldb : 1, row0 + lane,
-                      p.I, col0, p.J, k0 * 64LL, min(p.K, k1 * 64LL));
-#pragma unroll
-        for (int c = 0; c < 64; ++c) v[c] = u[c];
-      }
       if (q.parts) {
         float4* out = reinterpret_cast<float4*>(q.parts) + w * (128 * 16) + quarter * (32 * 16) + lane;
 #pragma unroll
