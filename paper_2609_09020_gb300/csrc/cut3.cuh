@@ -1,21 +1,25 @@
 // cut3.cuh -- fp32 values as three bfloat16 pieces, for products on the tensor
 // cores.
 //
-// A value is hi + mid + lo, each the top 8 significant bits of what the ones
-// before left, by truncation: 24 bits in all, so the sum is the value exactly
-// (pieces below 2^-126 lose bits).  Of the nine products of pieces the six
+// A value is hi + mid + lo, each the nearest bfloat16 (8 significant bits) to what the
+// ones before left: mid is at most 2^-8 and lo at most 2^-16 of the value, and the sum is
+// the value exactly, but for bits below 2^-133, bfloat16's smallest step: values below
+// 2^-110 are held in fewer than 24 bits.  Of the nine products of pieces the six
 // largest are formed,
 //     hi hi + (hi mid + mid hi) + (mid mid + hi lo + lo hi);
-// the three left out are below 3 x 2^-24 of the product.  Six MMAs of bfloat16 at
-// 2.25 PFLOP/s nominal are 375 TFLOP/s of fp32, five times what the FP32 cores do.
+// the three left out are below 2^-23 of the product, of either sign.  (By truncation the
+// pieces would be up to 2^-7 and 2^-15, the rest up to 2^-21 and always of the product's
+// sign; it takes as many instructions.)  Six MMAs of bfloat16 at 2.25 PFLOP/s nominal are
+// 375 TFLOP/s of fp32, five times what the FP32 cores do.
 //
 // A tensor core truncates when it adds to an accumulator.  So within a slice of 64
 // of K the products of small pieces come first (cut_a, cut_b), which leaves few
 // truncations at the sum's full size, and after every 128 of K the accumulators are
 // taken over into registers and added there to nearest.  Measured on 2048 x 1024 ->
-// 4096 (root mean square error, relative): 2.1e-6 with all products of 16 of K
-// together and takeovers every 256; 7e-7 as it is; 1.6e-7 with takeovers every 64,
-// which take a quarter more time; fp32 FMAs in order give 6.2e-7.
+// 4096 (root mean square error, relative): 6.0e-7 with terms of random sign, 5.2e-7 with
+// positive ones; fp32 FMAs in order give 6.2e-7.  (With pieces by truncation: 6.8e-7 and
+// 2.1e-6; with those and all products of 16 of K together and takeovers every 256, 2.1e-6
+// and more; takeovers every 64 take a quarter more time.)
 #pragma once
 
 #include <cstdint>
@@ -34,16 +38,24 @@ __host__ __device__ constexpr int cut_b(int t) {
   return p[t];
 }
 
-// The three pieces of two finite fp32 values, packed (a in the low half).
+// From here on hi would be infinite: such values, like infinite and NaN ones, take no
+// part in products of pieces.
+constexpr uint32_t kCutLimit = 0x7f7f8000u;
+
+// Two values rounded to bfloat16, packed (a in the low half).
+__device__ __forceinline__ uint32_t nearest2(float a, float b) {
+  uint32_t d;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(b), "f"(a));
+  return d;
+}
+// The three pieces of two values below kCutLimit in size, packed (a in the low half).
 __device__ __forceinline__ void cut3(uint32_t a, uint32_t b, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
-  hi = __byte_perm(a, b, 0x7632);
-  float ra = __uint_as_float(a) - __uint_as_float(a & 0xffff0000u);
-  float rb = __uint_as_float(b) - __uint_as_float(b & 0xffff0000u);
-  const uint32_t ma = __float_as_uint(ra), mb = __float_as_uint(rb);
-  mid = __byte_perm(ma, mb, 0x7632);
-  ra -= __uint_as_float(ma & 0xffff0000u);
-  rb -= __uint_as_float(mb & 0xffff0000u);
-  lo = __byte_perm(__float_as_uint(ra), __float_as_uint(rb), 0x7632);
+  float ra = __uint_as_float(a), rb = __uint_as_float(b);
+  hi = nearest2(ra, rb);
+  ra -= __uint_as_float(hi << 16), rb -= __uint_as_float(hi & 0xffff0000u);
+  mid = nearest2(ra, rb);
+  ra -= __uint_as_float(mid << 16), rb -= __uint_as_float(mid & 0xffff0000u);
+  lo = nearest2(ra, rb);
 }
 
 // Adds to v[c] the sum over elements [k0, k1) of K for row i

@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       v.get(static_cast<const T*>(g.w) + row * g.ldw + col, row < g.N ? g.K - col : 0, vec);
       largest = max(largest, put_vec<T>(base + S::kOffW, S::kWBlock, S::kWPlane, row, col, v.w));
     }
-    if (largest >= 0x7f800000u) marks[kMarks] = 1;
+    if (largest >= kCutLimit) marks[kMarks] = 1;
   }
   tc::fence_async_smem();
   tc::tc_fence_before();
@@ -406,7 +406,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       if (!ok) break;
-      if (largest >= 0x7f800000u) marks[count % kMarks] = count + 1;
+      if (largest >= kCutLimit) marks[count % kMarks] = count + 1;
       tc::fence_async_smem();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(bar_full + 8 * s);

@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(256) cut_kernel(const CutPair q) {
     *reinterpret_cast<uint2*>(o + plane) = make_uint2(m0, m1);
     *reinterpret_cast<uint2*>(o + 2 * plane) = make_uint2(l0, l1);
   }
-  const int bad = __syncthreads_or(largest >= 0x7f800000u);
+  const int bad = __syncthreads_or(largest >= kCutLimit);
   if (threadIdx.x == 0) q.m[which].marks[block] = bad;
 }
 

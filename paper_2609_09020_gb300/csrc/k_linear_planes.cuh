@@ -14,7 +14,7 @@ constexpr int kPlBlock = 128;  // rows and columns of a stored matrix that share
 struct PlOperand {
   const float* m;
   long long ld;       // elements from one stored row to the next
-  const int* marks;   // [row blocks][col_blocks], nonzero: the block has an infinite or NaN value
+  const int* marks;   // [row blocks][col_blocks], nonzero: the block has a value from kCutLimit on
   int col_blocks;
 };
 struct PlOperands {

@@ -75,7 +75,7 @@ struct Slice {
           q[u].w[i] = load_if(reinterpret_cast<const uint32_t*>(p) + i, u * turn < left && i < n);
     }
   }
-  // true if a value is infinite or NaN.  Of the rows that do not exist (from
+  // true if a value is infinite or NaN (or from kCutLimit on).  Of the rows that do not exist (from
   // `rows` on) nothing is written: what the MMA makes of them is not looked at.
   __device__ __forceinline__ bool store(uint32_t s, bool mn, long long rows, int tid) const {
     constexpr int kPlane = ROWS * 128;
@@ -94,7 +94,7 @@ struct Slice {
       sts64(at + u * turn * 128 + kPlane, m0, m1);
       sts64(at + u * turn * 128 + 2 * kPlane, l0, l1);
     }
-    return largest >= 0x7f800000u;
+    return largest >= kCutLimit;
   }
 };
 
