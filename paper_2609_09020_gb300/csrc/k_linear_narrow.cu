@@ -9,7 +9,10 @@
 // of 128 bytes, swizzled) is both operands: read along its rows it is A of
 // dx = dz w, read across them A of dw = dz^T x.  dw stays in tensor memory from
 // tile to tile; at the end each CTA writes its dw and db, and a small second kernel
-// adds the CTAs' in order.
+// adds the CTAs' in order.  A tensor core truncates when it adds to an accumulator, so
+// a CTA takes no more than kMostTiles tiles: 1024 additions, which lose at most 2^-13
+// of a sum of terms of one sign (6e-5 on average), below the rounding of the output.
+// From 2.5 million rows on there is more than one CTA for each SM, one after another.
 //
 // Up to 128 columns on each side for 16-bit types, 64 for fp32, whose values are
 // cut into three bfloat16 pieces as in cut3.cuh (dw is then taken over into
@@ -44,6 +47,7 @@ constexpr int kMmaWarp = 6, kTmaWarp = 7;
 constexpr int kTile = 128;
 constexpr int kMarks = 8;  // more tiles than the loaders can be ahead of the others
 constexpr int kSms = 152;
+constexpr int kMostTiles = 128;  // of a CTA, where dw stays in tensor memory
 
 struct NarrowParams {
   NarrowGrad g;
@@ -645,15 +649,18 @@ __global__ void __launch_bounds__(kThreads, 1)
 // 32nd part, the first warp the warps' sums.
 template <typename T>
 __global__ void __launch_bounds__(1024) add_parts_kernel(const float* parts, int n_parts, const NarrowGrad g) {
+  constexpr int kAtOnce = (kSms + 31) / 32;  // loads of a thread under way together
   __shared__ float sums[32][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nk = g.N * g.K, per = nk + g.N;
   const int e = blockIdx.x * 32 + lane;
   float v = 0.0f;
   if (e < per) {
+    for (int s0 = warp; s0 < n_parts; s0 += 32 * kAtOnce) {
 #pragma unroll
-    for (int i = 0; i < (kSms + 31) / 32; ++i) {
-      const int s = warp + 32 * i;
-      if (s < n_parts) v += __ldcg(parts + s * static_cast<long long>(per) + e);
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int s = s0 + 32 * i;
+        if (s < n_parts) v += __ldcg(parts + s * static_cast<long long>(per) + e);
+      }
     }
   }
   sums[warp][lane] = v;
@@ -668,9 +675,11 @@ __global__ void __launch_bounds__(1024) add_parts_kernel(const float* parts, int
   }
 }
 
-int ctas(const NarrowGrad& g) {
-  const long long tiles = (g.I + kTile - 1) / kTile;
-  return static_cast<int>(tiles < kSms ? tiles : kSms);
+// As many CTAs as SMs, or a multiple of that (fp32 takes dw over after every tile).
+int ctas(const NarrowGrad& g, int dtype) {
+  const long long tiles = (g.I + kTile - 1) / kTile, each = dtype == PIC_DTYPE_F32 ? tiles : kMostTiles;
+  const long long most = kSms * ((tiles + kSms * each - 1) / (kSms * each));
+  return static_cast<int>(tiles < most ? tiles : most);
 }
 
 // The run mode's room for copies: a tile's dy, z and x, each on a 16-byte boundary
@@ -689,9 +698,9 @@ bool plan_runs(NarrowParams& q) {
 }
 
 template <typename T, bool WIDE, Source SRC>
-int run(const NarrowGrad& g, NarrowParams& q, NarrowMaps& maps, int slot, cudaStream_t s) {
+int run(const NarrowGrad& g, NarrowParams& q, NarrowMaps& maps, int grid, int slot, cudaStream_t s) {
   const void* fn = reinterpret_cast<const void*>(narrow_kernel<T, WIDE, SRC>);
-  const int fixed = Shape<T, WIDE, SRC>::kSmem, grid = ctas(g);
+  const int fixed = Shape<T, WIDE, SRC>::kSmem;
   const int smem = SRC == kRun ? 227 * 1024 : fixed;  // the attribute is set once, for runs of any width
   static_assert(Shape<T, WIDE, SRC>::kSmem <= 227 * 1024, "shared memory of an SM");
   if (allow_smem(fn, slot, smem) != PIC_OK) return PIC_ERR_CUDA;
@@ -711,11 +720,13 @@ bool narrow_takes(const NarrowGrad& g, int dtype) {
   return (g.dx || g.dw) && g.N <= most && g.K <= most && g.I >= 1024;
 }
 
-long long narrow_workspace(const NarrowGrad& g) { return ctas(g) * static_cast<long long>(g.N * g.K + g.N) * 4; }
+long long narrow_workspace(const NarrowGrad& g, int dtype) {
+  return ctas(g, dtype) * static_cast<long long>(g.N * g.K + g.N) * 4;
+}
 
 int narrow_grad(const NarrowGrad& g, int dtype, void* ws, const Waits& waits, cudaStream_t s) {
   NarrowParams q{};
-  const int elem = dtype == PIC_DTYPE_F32 ? 4 : 2;
+  const int elem = dtype == PIC_DTYPE_F32 ? 4 : 2, grid = ctas(g, dtype);
   const auto on16 = [&](const void* m, long long ld) { return reinterpret_cast<uintptr_t>(m) % 16 == 0 && ld * elem % 16 == 0; };
   q.g = g;
   q.tiles = (g.I + kTile - 1) / kTile;
@@ -737,16 +748,16 @@ int narrow_grad(const NarrowGrad& g, int dtype, void* ws, const Waits& waits, cu
   const auto packed = [](const void* m, long long ld, int cols) { return ld == cols && reinterpret_cast<uintptr_t>(m) % 16 == 0; };
   const bool runs = !tma && packed(g.dy, g.lddy, g.N) && (!has_z || packed(g.pre, g.ldpre, g.N)) && (!g.dw || packed(g.x, g.ldx, g.K));
   if (dtype == PIC_DTYPE_F32)
-    return runs && plan_runs<float, false>(q) ? run<float, false, kRun>(g, q, maps, 15, s) : run<float, false, kReg>(g, q, maps, 8, s);
+    return runs && plan_runs<float, false>(q) ? run<float, false, kRun>(g, q, maps, grid, 15, s) : run<float, false, kReg>(g, q, maps, grid, 8, s);
   if (dtype == PIC_DTYPE_F16) {
-    if (tma) return run<__half, false, kTma>(g, q, maps, 10, s);
-    if (wide) return runs && plan_runs<__half, true>(q) ? run<__half, true, kRun>(g, q, maps, 16, s) : run<__half, true, kReg>(g, q, maps, 9, s);
-    return runs && plan_runs<__half, false>(q) ? run<__half, false, kRun>(g, q, maps, 17, s) : run<__half, false, kReg>(g, q, maps, 11, s);
+    if (tma) return run<__half, false, kTma>(g, q, maps, grid, 10, s);
+    if (wide) return runs && plan_runs<__half, true>(q) ? run<__half, true, kRun>(g, q, maps, grid, 16, s) : run<__half, true, kReg>(g, q, maps, grid, 9, s);
+    return runs && plan_runs<__half, false>(q) ? run<__half, false, kRun>(g, q, maps, grid, 17, s) : run<__half, false, kReg>(g, q, maps, grid, 11, s);
   }
   using B = __nv_bfloat16;
-  if (tma) return run<B, false, kTma>(g, q, maps, 13, s);
-  if (wide) return runs && plan_runs<B, true>(q) ? run<B, true, kRun>(g, q, maps, 18, s) : run<B, true, kReg>(g, q, maps, 12, s);
-  return runs && plan_runs<B, false>(q) ? run<B, false, kRun>(g, q, maps, 19, s) : run<B, false, kReg>(g, q, maps, 14, s);
+  if (tma) return run<B, false, kTma>(g, q, maps, grid, 13, s);
+  if (wide) return runs && plan_runs<B, true>(q) ? run<B, true, kRun>(g, q, maps, grid, 18, s) : run<B, true, kReg>(g, q, maps, grid, 12, s);
+  return runs && plan_runs<B, false>(q) ? run<B, false, kRun>(g, q, maps, grid, 19, s) : run<B, false, kReg>(g, q, maps, grid, 14, s);
 }
 
 }  // namespace lin

@@ -327,7 +327,7 @@ struct NarrowGrad {
   int N, K, act;
 };
 bool narrow_takes(const NarrowGrad& g, int dtype);
-long long narrow_workspace(const NarrowGrad& g);
+long long narrow_workspace(const NarrowGrad& g, int dtype);
 int narrow_grad(const NarrowGrad& g, int dtype, void* ws, const Waits& waits, cudaStream_t s);
 
 }  // namespace lin

@@ -169,7 +169,7 @@ int backward(const pic_linear_grad_args& a, Arena& ws, bool launch, cudaStream_t
     const pic::lin::NarrowGrad g{a.dy, a.lddy, a.pre, a.ldpre, a.x, a.ldx, a.w, a.ldw, a.dx, a.lddx,
                                  a.dw, a.lddw, a.db, M, static_cast<int>(N), static_cast<int>(K), a.act};
     if (pic::lin::narrow_takes(g, a.dtype)) {
-      void* w = ws.take(pic::lin::narrow_workspace(g));
+      void* w = ws.take(pic::lin::narrow_workspace(g, a.dtype));
       if (!launch) return PIC_OK;
       pic::lin::Waits wt;
       return waits(wt) ? pic::lin::narrow_grad(g, a.dtype, w, wt, s) : PIC_ERR_CUDA;
