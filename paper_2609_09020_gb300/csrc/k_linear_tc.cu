@@ -159,7 +159,7 @@ struct Plan {
   int cg, bn;
   long long tiles_i, tiles_j;
   int k_blocks, part_blocks, splits;
-  long long a_bytes, b_bytes, part_bytes;
+  long long a_bytes, b_bytes, part_bytes, carry_bytes;
 };
 
 long long round256(long long v) { return (v + 255) / 256 * 256; }
@@ -254,6 +254,12 @@ Product oriented(const Product& p, int dtype) {
   return choose(r, q, &kShapeReg, 1, 4, true) + 1.5 < choose(r, p, &kShapeReg, 1, 4, true) ? q : p;
 }
 
+// CTAs of a launch: persistent, two on an SM for tiles of 64 columns of 16-bit types.
+long long ctas(const Plan& r) {
+  const long long want = r.tiles_i * r.tiles_j * r.splits * r.cg, most = r.bn == 64 && !r.reg ? 2 * kSms : kSms;
+  return want < most ? want : most;
+}
+
 Plan plan(const Product& p, int dtype) {
   Plan r{};
   const bool fp32 = dtype == PIC_DTYPE_F32;
@@ -276,6 +282,7 @@ Plan plan(const Product& p, int dtype) {
     r.b_bytes = planes_bytes(r.b) + marks_bytes(r.b);
   }
   if (r.splits > 1) r.part_bytes = r.tiles_i * r.tiles_j * r.splits * rows * r.bn * 4;
+  if (!fp32 && r.part_blocks > kTcTakeover) r.carry_bytes = ctas(r) * 128 * r.bn * 4;
   return r;
 }
 
@@ -380,7 +387,7 @@ int allow_smem(const void* fn, int slot, int smem) {
 
 long long tc_workspace(const Product& p, int dtype) {
   const Plan r = plan(oriented(p, dtype), dtype);
-  return r.a_bytes + r.b_bytes + r.part_bytes;
+  return r.a_bytes + r.b_bytes + r.part_bytes + r.carry_bytes;
 }
 
 int tc_product(const Product& given, int dtype, void* ws, const Waits& waits, cudaStream_t s) {
@@ -401,6 +408,7 @@ int tc_product(const Product& given, int dtype, void* ws, const Waits& waits, cu
   q.work = r.tiles_i * r.tiles_j * r.splits;
   q.a_mn = r.a.mn, q.b_mn = r.b.mn;
   q.parts = r.splits > 1 ? reinterpret_cast<float*>(w + r.a_bytes + r.b_bytes) : nullptr;
+  q.carry = r.carry_bytes ? reinterpret_cast<float*>(w + r.a_bytes + r.b_bytes + r.part_bytes) : nullptr;
   q.waits = waits;
   const auto fits = [&](const void* m, long long ld, long long rows) {
     return reinterpret_cast<uintptr_t>(m) % 16 == 0 && ((ld * elem % 16 == 0 && ld * elem < (1LL << 40)) || rows == 1);
@@ -448,18 +456,16 @@ int tc_product(const Product& given, int dtype, void* ws, const Waits& waits, cu
     fn = k.fn, threads = k.threads, smem = k.smem;
     slot = 7;
   } else {
-    fn = dtype == PIC_DTYPE_BF16 ? tc_kernel_bf16(r.bn) : tc_kernel_f16(r.bn);
+    const bool long_parts = r.carry_bytes > 0;
+    fn = dtype == PIC_DTYPE_BF16 ? tc_kernel_bf16(r.bn, long_parts) : tc_kernel_f16(r.bn, long_parts);
     const int shape = r.bn == 256 ? 2 : r.bn == 128 ? 1 : 0;
-    slot = shape + (dtype == PIC_DTYPE_BF16 ? 3 : 0);
+    slot = shape + (dtype == PIC_DTYPE_BF16 ? 3 : 0) + (long_parts ? 20 : 0);
     smem = shape == 2 ? TcShape<2, 256>::kSmem : shape == 1 ? TcShape<1, 128>::kSmem : TcShape<1, 64>::kSmem;
     threads = shape == 2 ? TcShape<2, 256>::kThreads : shape == 1 ? TcShape<1, 128>::kThreads : TcShape<1, 64>::kThreads;
   }
   if (allow_smem(fn, slot, smem) != PIC_OK) return PIC_ERR_CUDA;
-  long long grid = q.work * r.cg;
-  const long long most = r.bn == 64 && !r.reg ? 2 * kSms : kSms;
-  if (grid > most) grid = most;
   void* args[] = {&q, &maps, r.planes ? static_cast<void*>(&pl) : &o};  // 16-bit kernels take the first two
-  if (launch_kernel(fn, grid, threads, smem, r.cg, args, s) != PIC_OK) return PIC_ERR_CUDA;
+  if (launch_kernel(fn, ctas(r), threads, smem, r.cg, args, s) != PIC_OK) return PIC_ERR_CUDA;
   if (q.parts) {
     const JoinParams j{p, reinterpret_cast<const float4*>(q.parts), r.tiles_i, r.tiles_j, r.splits, 128 * r.cg, r.bn};
     if (dtype == PIC_DTYPE_F32) return join<float>(j, s);

@@ -12,7 +12,10 @@
 //               TMA where rows start and end on 16-byte boundaries, in one run
 //               where narrow rows lie end to end, else by plain stores
 // There are two sets of accumulators, so that a tile's epilogue runs under the
-// next tile's MMAs.  An operand may be contiguous along K or along its rows
+// next tile's MMAs.  A tensor core truncates when it adds to an accumulator, so one is
+// taken over after 1024 additions, 16384 of K (at most 2^-13 is lost of a sum of terms of
+// one sign, 6e-5 on average): over longer K the epilogue warps add what they take over to
+// sums of the CTA's own in the workspace, to nearest, under the next MMAs.  An operand may be contiguous along K or along its rows
 // (dz and x in dw = dz^T x): TMA then brings blocks of 64 rows x 64 of K and
 // the MMA reads them transposed.  A product that has fewer tiles than the GPU
 // has SMs is cut along K: each part's accumulators go to the workspace in fp32,
@@ -47,11 +50,13 @@ struct TcParams {
   int a_mn, b_mn;        // the operand is contiguous along its rows
   int store_tma;         // y (and pre) go out by TMA
   float* parts;          // fp32 parts, or null: the epilogue runs in the kernel
+  float* carry;          // [CTAs][128][BN] sums so far, for kernels of long parts
   Waits waits;
 };
 
 constexpr int kSlice = 64;           // K of one stage
 constexpr int kPanelBytes = 32 * 128;  // 32 rows x 64 columns of a 16-bit type
+constexpr int kTcTakeover = 256;     // slices that stay in an accumulator
 constexpr int kGroupRows = 2048;     // rows of A that neighbouring tiles share the columns of B for
 
 // At most limit polls; false (with the flags raised) if the phase does not
@@ -515,7 +520,69 @@ __device__ __forceinline__ void finish_item(const Product& p, const JoinItem& m,
   put(p.y, p.ldy, y);
 }
 
-template <typename T, int CG, int BN>
+// a[0..3], bits of floats, plus f.
+__device__ __forceinline__ void add4(uint32_t* a, const float4& f) {
+  a[0] = __float_as_uint(__uint_as_float(a[0]) + f.x);
+  a[1] = __float_as_uint(__uint_as_float(a[1]) + f.y);
+  a[2] = __float_as_uint(__uint_as_float(a[2]) + f.z);
+  a[3] = __float_as_uint(__uint_as_float(a[3]) + f.w);
+}
+
+// A tile with more K than stays in an accumulator: an epilogue warp takes the
+// accumulators over `n` times and sums them up in `sums` (panels of [16][32 lanes] x 4
+// columns, each lane's its own); the tile's last ones it adds where they are, in tensor
+// memory, for the usual path to find.  A function of its own, so that it takes no
+// registers from that path; false after an abort.
+struct Carry {
+  float4* sums;
+  uint32_t tmem, bar_acc, lead_free;
+  int from, to, n, lane;
+  bool withhold;
+  volatile int* abort_flag;
+};
+template <int CG, int BN>
+__device__ __noinline__ bool carry_sums(const Carry& m, const Waits& waits, int buf, uint32_t phase) {
+  for (int t = 0; m.n > 0 && t <= m.n; ++t) {
+    if (!__all_sync(0xffffffffu, wait_bounded(m.bar_acc + 8 * buf, phase, m.abort_flag, waits))) return false;
+    tc::tc_fence_after();
+    for (int c0 = m.from; c0 < m.to; c0 += 64) {
+      const uint32_t at = m.tmem + buf * BN + c0;
+      uint32_t r[64];
+      tc::tmem_ld64_wait(at, r);
+      if (t < m.n && c0 + 64 == m.to) {
+        tc::tc_fence_before();
+        __syncwarp();
+        if (m.lane == 0 && !m.withhold) {
+          if constexpr (CG == 2)
+            tc::mbar_arrive_cluster(m.lead_free + 8 * buf);
+          else
+            tc::mbar_arrive(m.lead_free + 8 * buf);
+        }
+      }
+      float4* o = m.sums + c0 / 64 * (128 * 16);
+      if (t > 0) {
+#pragma unroll
+        for (int c = 0; c < 16; ++c) add4(r + 4 * c, o[c * 32]);
+      }
+      if (t < m.n) {
+#pragma unroll
+        for (int c = 0; c < 16; ++c)
+          o[c * 32] = make_float4(__uint_as_float(r[4 * c]), __uint_as_float(r[4 * c + 1]), __uint_as_float(r[4 * c + 2]),
+                                  __uint_as_float(r[4 * c + 3]));
+      } else {
+#pragma unroll
+        for (int c = 0; c < 64; c += 16) tc::tmem_st16(at + c, r + c);
+        tc::tmem_st_wait();
+      }
+    }
+    if (++buf == 2) buf = 0, phase ^= 1;
+  }
+  return true;
+}
+
+// LONG: parts with more than kTcTakeover slices.  (In one kernel with the others, 4096 x
+// 512 -> 4096 with residual took 36.8 us instead of 35.6.)
+template <typename T, int CG, int BN, bool LONG>
 __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
     tc_kernel(const __grid_constant__ TcParams q, const __grid_constant__ TcMaps maps) {
   using S = TcShape<CG, BN>;
@@ -612,8 +679,16 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
         tc::tc_fence_after();
         int k0, k1;
         part(w, k0, k1);
-        const uint32_t d = tmem + buf * BN;
-        for (int kb = k0; kb < k1; ++kb) {
+        uint32_t d = tmem + buf * BN;
+        for (int kb = k0, t1 = k0 + kTcTakeover; kb < k1; ++kb) {
+          if (LONG && kb == t1) {
+            tc::mma_commit_cg<CG>(bar_acc + 8 * buf);
+            if (++buf == 2) buf = 0, free_phase ^= 1;
+            if (!(ok = wait(bar_free + 8 * buf, free_phase ^ 1))) break;
+            tc::tc_fence_after();
+            d = tmem + buf * BN;
+            k0 = kb, t1 += kTcTakeover;
+          }
           if (!(ok = wait(bar_full + 8 * s, phase))) break;
           tc::tc_fence_after();
           const uint32_t sa = base + s * S::kStageBytes, sb = sa + S::kABytes;
@@ -641,6 +716,16 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
       long long ti, tj;
       tile_place<S::kRows>(w / q.splits, q.tiles_i, q.tiles_j, ti, tj);
       const long long row0 = ti * S::kRows + rank * 128 + quarter * 32, j0 = tj * BN;
+      if constexpr (LONG) {
+        int k0, k1;
+        part(w, k0, k1);
+        const Carry c{reinterpret_cast<float4*>(q.carry) + blockIdx.x * static_cast<long long>(128 * BN / 4) + quarter * (32 * 16) + lane,
+                      tmem + (static_cast<uint32_t>(quarter * 32) << 16), bar_acc, lead_free, from, to, (k1 - k0 - 1) / kTcTakeover, lane,
+                      q.waits.test_fault && w == 0 && rank == 0 && quarter == 0, abort_flag};
+        if (!carry_sums<CG, BN>(c, q.waits, buf, phase)) break;
+        buf += c.n;
+        phase ^= buf >> 1 & 1, buf &= 1;
+      }
       // tiles of 64 columns wait for memory: their residual is on its way before they
       // are summed (for larger tiles that would take registers that they need)
       Residual<T> res;
@@ -735,18 +820,18 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
 bool encode(CUtensorMap* map, const void* m, long long rows, long long cols, long long ld, int box_rows, int dtype);
 // Allows a kernel `smem` bytes of shared memory, once per device; each kernel of
 // these files has a slot of its own below kSmemSlots.
-constexpr int kSmemSlots = 20;
+constexpr int kSmemSlots = 26;
 int allow_smem(const void* fn, int slot, int smem);
 
 // The kernel for tiles of bn columns: 64 and 128 by one CTA, 256 by a pair.
-const void* tc_kernel_f16(int bn);
-const void* tc_kernel_bf16(int bn);
+const void* tc_kernel_f16(int bn, bool long_parts);
+const void* tc_kernel_bf16(int bn, bool long_parts);
 
-template <typename T>
+template <typename T, bool LONG>
 const void* tc_kernel_of(int bn) {
-  if (bn == 256) return reinterpret_cast<const void*>(tc_kernel<T, 2, 256>);
-  if (bn == 128) return reinterpret_cast<const void*>(tc_kernel<T, 1, 128>);
-  return reinterpret_cast<const void*>(tc_kernel<T, 1, 64>);
+  if (bn == 256) return reinterpret_cast<const void*>(tc_kernel<T, 2, 256, LONG>);
+  if (bn == 128) return reinterpret_cast<const void*>(tc_kernel<T, 1, 128, LONG>);
+  return reinterpret_cast<const void*>(tc_kernel<T, 1, 64, LONG>);
 }
 
 }  // namespace lin

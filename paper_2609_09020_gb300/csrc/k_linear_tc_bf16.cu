@@ -4,7 +4,9 @@
 namespace pic {
 namespace lin {
 
-const void* tc_kernel_bf16(int bn) { return tc_kernel_of<__nv_bfloat16>(bn); }
+const void* tc_kernel_bf16(int bn, bool long_parts) {
+  return long_parts ? tc_kernel_of<__nv_bfloat16, true>(bn) : tc_kernel_of<__nv_bfloat16, false>(bn);
+}
 
 }  // namespace lin
 }  // namespace pic

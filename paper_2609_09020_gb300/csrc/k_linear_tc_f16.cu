@@ -4,7 +4,9 @@
 namespace pic {
 namespace lin {
 
-const void* tc_kernel_f16(int bn) { return tc_kernel_of<__half>(bn); }
+const void* tc_kernel_f16(int bn, bool long_parts) {
+  return long_parts ? tc_kernel_of<__half, true>(bn) : tc_kernel_of<__half, false>(bn);
+}
 
 }  // namespace lin
 }  // namespace pic
