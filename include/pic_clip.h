@@ -6,11 +6,14 @@
  *   coef = min(1, max_norm / (norm + 1e-6)),   out = coef * grad
  *
  * The squares are summed in fp32 within short runs and in fp64 across them,
- * and a run whose sum leaves fp32's range is summed again in fp64: the norm is
- * right for finite gradients of any size.  If an element is infinite or NaN,
- * so is the norm, and the outputs are what the formula gives: NaN where coef
- * or the element is NaN, or for an infinite element times coef = 0.  coef and
- * the products are computed in fp32; a product is rounded once, to nearest, to
+ * and a run whose sum leaves fp32's range is summed again in fp64: finite
+ * gradients of any size are clipped as the formula says.  The norm is returned
+ * in fp32: one above fp32's largest value is infinite there (coef is then
+ * computed from the fp64 sum).  If an element is infinite or NaN, so is the
+ * norm, and the outputs are what the formula gives: NaN where coef or the
+ * element is NaN, or for an infinite element times coef = 0.  With max_norm
+ * infinite coef is 1, whatever the norm.  coef and the products are fp32 (a
+ * coef below 2^-126 has fewer bits); a product is rounded once, to nearest, to
  * the tensor's type.
  *
  * Conventions as in pic_decode.h: device pointers owned by the caller,

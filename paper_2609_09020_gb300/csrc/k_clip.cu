@@ -255,6 +255,8 @@ __global__ void __launch_bounds__(kThreads, 2) clip_kernel(const ClipParams p) {
       if (blockIdx.x == 0) *p.norm = norm;
       // not fminf: coef is NaN where norm is
       float c = p.max_norm / (norm + 1e-6f);
+      // finite gradients with a norm above fp32's largest value
+      if (isinf(norm) && !isinf(d)) c = static_cast<float>(p.max_norm / sqrt(d));
       if (c > 1.0f || isinf(p.max_norm)) c = 1.0f;
       coef_s = c;
     }
