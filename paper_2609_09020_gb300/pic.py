@@ -427,14 +427,14 @@ def huffman_decode(words, word_off, n_bits, tab_value, tab_len, p, sym_off, stre
 
 
 # ---- the linear layer, its gradient, gradient clipping ----------------------
-_dtype_codes = {}  # torch dtype -> pic_dtype
+_dtype_codes = None  # torch dtype -> pic_dtype; whole from its assignment on, for calls of other threads
 
 
 def _dtype_code(t, name) -> int:
-    if not _dtype_codes:
+    global _dtype_codes
+    if _dtype_codes is None:
         import torch
-        for n, c in DTYPES.items():
-            _dtype_codes[getattr(torch, n.split(".")[1])] = c
+        _dtype_codes = {getattr(torch, n.split(".")[1]): c for n, c in DTYPES.items()}
     code = _dtype_codes.get(t.dtype)
     if code is None:
         raise ValueError(f"{name}: must be float32, float16 or bfloat16, not {t.dtype}")
@@ -508,7 +508,7 @@ _LINEAR_GRAD_ARGS = struct.Struct("@3q2iPqPqPqPqPqPqP")
 
 def _call_with_workspace(name, packed, torch, device):
     lib = load_library()
-    call, workspace_bytes = _linear_calls[name] if _linear_calls else _find_linear_calls(lib, name)
+    call, workspace_bytes = (_linear_calls or _find_linear_calls(lib))[name]
     stream = _current_stream()
     # a call that needs workspace refuses to do without: nothing is launched then
     rc = call(packed, None, 0, stream)
@@ -521,16 +521,19 @@ def _call_with_workspace(name, packed, torch, device):
         raise PicError(rc, name)
 
 
-_linear_calls = {}
+_linear_calls = None  # whole from its assignment on, for calls of other threads
 
 
-def _find_linear_calls(lib, name):
+def _find_linear_calls(lib):
     """The C functions with untyped pointers, which ctypes passes bytes to."""
+    global _linear_calls
+    calls = {}
     for n in ("pic_linear", "pic_linear_backward"):
         f = ctypes.CFUNCTYPE(ctypes.c_int, _P, _P, ctypes.c_size_t, _P)((n, lib))
         g = ctypes.CFUNCTYPE(ctypes.c_int64, _P)((n + "_workspace_bytes", lib))
-        _linear_calls[n] = f, g
-    return _linear_calls[name]
+        calls[n] = f, g
+    _linear_calls = calls
+    return calls
 
 
 def _linear_act(act) -> int:
