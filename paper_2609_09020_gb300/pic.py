@@ -543,6 +543,14 @@ def _linear_act(act) -> int:
     return code
 
 
+def _refuse_recorded(**tensors):
+    """Gradients that autograd would lose without a word."""
+    for name, t in tensors.items():
+        if t is not None and t.requires_grad:
+            raise ValueError(f"{name}: requires a gradient, and autograd does not record this call: detach it, or "
+                             "call under torch.no_grad(), and take the gradients from linear_backward")
+
+
 def linear(x, weight, bias=None, act="none", residual=None, out=None, save_pre=False, stream=None):
     """act(x weight^T + bias) + residual on torch CUDA tensors: x [..., in],
     weight [out, in], bias [out], residual [..., out] (or one row, expanded),
@@ -550,11 +558,19 @@ def linear(x, weight, bias=None, act="none", residual=None, out=None, save_pre=F
     (erf form).  Returns y [..., out] (``out`` if given, which may be
     ``residual``), or (y, pre) with save_pre: pre = x weight^T + bias is what
     ``linear_backward`` reads.  x and residual may be 2-D with rows further
-    apart than their width.  Enqueued on the stream, not synchronised."""
+    apart than their width.  Enqueued on the stream, not synchronised.
+
+    torch's autograd does not record the call, and tensors that require
+    gradients are refused while it records: detach them, or call under
+    ``torch.no_grad()``, and take the gradients from ``linear_backward``."""
     if stream is not None:
         with _Allocating(stream):
             return linear(x, weight, bias, act, residual, out, save_pre)
     import torch
+    if ((x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad
+         or residual is not None and residual.requires_grad or out is not None and out.requires_grad)
+            and torch.is_grad_enabled()):
+        _refuse_recorded(x=x, weight=weight, bias=bias, residual=residual, out=out)
     _on_device(x, "x")
     if weight.dim() != 2:
         raise ValueError("weight: must be 2-D")
