@@ -19,7 +19,7 @@ constexpr int kRows = 64, kWarpRows = 8;
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads, 2) outer_kernel(const OuterGrad g, long long col_blocks) {
   constexpr int kV = 16 / sizeof(T), kCols = 32 * kV;
-  __shared__ float xs[kFewRows][kCols];
+  __shared__ __align__(16) float xs[kFewRows][kCols];
   __shared__ __align__(16) float ds[kFewRows][kRows];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rows = static_cast<int>(g.I);
   const long long n0 = blockIdx.x / col_blocks * kRows, k0 = blockIdx.x % col_blocks * kCols;

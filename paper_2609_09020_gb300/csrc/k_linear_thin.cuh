@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
   using S = ThinShape<T, NT>;
   constexpr int E = S::kElem;
   extern __shared__ __align__(16) uint8_t thin_smem[];
-  __shared__ float bias[NT * 8];
+  __shared__ __align__(8) float bias[NT * 8];
   const Product& p = q.p;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int J = static_cast<int>(p.J), K = static_cast<int>(p.K);
