@@ -7,8 +7,9 @@
  *   forward   z = x w^T + b,  y = act(z) + residual
  *   backward  dz = dy * act'(z),  dx = dz w,  dw = dz^T x,  db = sum_rows dz
  *             (the residual's gradient is dy itself)
- *   act       none, ReLU (max(z, 0), derivative 0 at 0) or GELU in its erf
- *             form (z Phi(z), derivative Phi(z) + z phi(z))
+ *   act       none, ReLU (max(z, 0), derivative 1 where z > 0, else 0, at NaN
+ *             too) or GELU in its erf form (z Phi(z), derivative Phi(z) + z
+ *             phi(z)); dz is 0 where the derivative is, whatever dy is
  *
  * Matrices are row-major with unit stride inside a row and `ld` elements from
  * row to row: x [rows][in], w [out][in] (the layout of pic_decode.h's blobs),

@@ -162,8 +162,8 @@ __device__ __forceinline__ float2 gelu2(float2 z) {
   }
 }
 
-// dy act'(z): a derivative of zero gives zero whatever dy is; act' is NaN for
-// NaN.  EXACT (fp32): off by the roundings of the evaluation, about 1e-7; else by
+// dy act'(z): a derivative of zero gives zero whatever dy is.  At z = NaN GELU's is NaN,
+// and ReLU's is zero, as [z > 0] is.  EXACT (fp32): off by the roundings of the evaluation, about 1e-7; else by
 // at most 5e-7, far below the rounding of dz to 16 bits.
 template <bool EXACT>
 __device__ __forceinline__ float act_grad(float dy, float z, int act) {
