@@ -65,7 +65,8 @@ int pic_clip(pic_clipper *c, float max_norm, float *norm, void *stream);
 
 /* Synchronises `stream`; PIC_OK if the blocks of every launch of this handle
  * since the last check met in time, PIC_ERR_TIMEOUT if those of one did not (its
- * norm is NaN then, and its outs are not all written), PIC_ERR_CUDA. */
+ * outs are not all written then, and its norm is unspecified: it may look right,
+ * so a program that must know asks here), PIC_ERR_CUDA. */
 int pic_clip_check(pic_clipper *c, void *stream);
 
 void pic_clip_destroy(pic_clipper *c);

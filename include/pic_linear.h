@@ -19,6 +19,15 @@
  * nearest.  In the backward pass of a 16-bit type, dz is rounded to that type
  * before the products (but for db, and for dw of up to 15 rows).
  *
+ * Products run on the tensor cores, which truncate when they add to a sum:
+ * after at most 1024 additions of 16 terms (fp32: 48) a sum is taken over and
+ * added to nearest, so that less than 2^-13 of a 16-bit type's sum of terms of
+ * one sign is lost, below the rounding of the output.  fp32 operands (but
+ * for a few rows, which the FP32 cores take) are cut into three bfloat16 pieces,
+ * which hold 24 bits, or fewer of values below 2^-110 in size; of a product of
+ * two values less than 2^-23 is left out.  Measured, root mean square, of sums of 1024: 6e-7, as much as fp32
+ * FMAs in order.
+ *
  * Conventions as in pic_decode.h: device pointers owned by the caller and
  * aligned to their element, asynchronous on `stream`, pic_status codes, no
  * traps.  Nothing is allocated; calls that overlap on the GPU need workspaces
@@ -83,7 +92,8 @@ typedef struct {
   int64_t ldx;
   const void *w; /* read for dx; may be NULL without dx */
   int64_t ldw;
-  const void *pre; /* z of the forward pass; may be NULL with PIC_ACT_NONE */
+  const void *pre; /* z of the forward pass (ReLU without residual: y will do, it
+                      has z's sign); may be NULL with PIC_ACT_NONE */
   int64_t ldpre;
   void *dx; /* [rows][in_features], or NULL: not computed */
   int64_t lddx;

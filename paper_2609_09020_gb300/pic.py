@@ -603,7 +603,8 @@ def linear_backward(dy, x, weight, act="none", pre=None, need=("x", "weight", "b
                     dbias=None, stream=None):
     """The gradients (dx, dweight, dbias) of ``linear`` for the output gradient
     dy [..., out]; those not named in ``need`` are None.  pre is what
-    ``linear`` returned with save_pre (not read with act "none").  The
+    ``linear`` returned with save_pre (not read with act "none"; with "relu"
+    and no residual y itself will do, which saves writing pre).  The
     gradients are new tensors, or are written to those given (a slice of a
     gradient buffer, say).  The residual's gradient is dy itself.  Enqueued on
     the stream."""
