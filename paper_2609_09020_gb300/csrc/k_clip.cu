@@ -11,8 +11,9 @@
 // L2 cache still holds, and with what the warp still has in registers (its last
 // 4 KB): up to 19 MB in all are read only once.
 //
-// Measured: 805 MB of bf16 in place 381 us: 2.33 GB of traffic at 6.1 TB/s, 91 % of the
-// copy rate; 384 tensors of nets (1.3 MB) 7.5 us, the launch and the meeting.
+// Measured: 805 MB of bf16, in place or to tensors beside, 386 us: 2.33 GB of traffic at
+// 6.0 TB/s, 90 % of the copy rate (376 us one after another); 384 tensors of nets (1.3 MB)
+// 7.4 us, the launch and the meeting.
 //
 // Sums: a lane adds at most 64 squares in fp32 and goes on in fp64; where such a
 // sum leaves the range in which fp32 is good, it is added again in fp64.
