@@ -151,6 +151,15 @@ def _shapes(case):
             for _ in range(case["count"])]
 
 
+def _matrices(buffers, shapes):
+    """The matrices that lie one behind another in their types' buffers."""
+    at, out = dict.fromkeys(buffers, 0), []
+    for t, r, c in shapes:
+        out.append(buffers[t][at[t]:at[t] + r * c].view(r, c))
+        at[t] += r * c
+    return out
+
+
 def _inputs(case, seed):
     """The tensors of a case, on the GPU, from the seed alone."""
     gen = torch.Generator(device="cuda").manual_seed(seed)
@@ -159,12 +168,17 @@ def _inputs(case, seed):
         return torch.randn(shape, generator=gen, device="cuda").mul_(std).to(dtype)
 
     if case["op"] == "orth":
-        grads = []
-        for t, r, c in _shapes(case):
+        # a program's gradients are slices of one buffer for each type
+        shapes = _shapes(case)
+        buffers = {t: torch.empty(sum(r * c for u, r, c in shapes if u == t), dtype=_DTYPES[t], device="cuda")
+                   for t in sorted({t for t, _, _ in shapes})}
+        grads = _matrices(buffers, shapes)
+        for g in grads:
+            r, c = g.shape
             # a weight gradient: few directions that most samples share, and what is left of each
             k = min(r, c, 16)
             few = normal((r, k), 1.0, torch.float32) @ normal((k, c), 1.0, torch.float32)
-            grads.append(((few / math.sqrt(k) + normal((r, c), 0.5, torch.float32)) * 0.01).to(_DTYPES[t]))
+            g.copy_((few / math.sqrt(k) + normal((r, c), 0.5, torch.float32)) * 0.01)
         return {"grads": grads}
     t = _DTYPES[case["dtype"]]
     G, M, K, N = case["groups"], case["rows"], case["inp"], case["outp"]
@@ -185,10 +199,13 @@ def prepare(case, seed):
     s["case"] = case
     if case["op"] == "orth":
         # updates go to tensors of their own, so that every pass has the same gradients
-        s["out"] = [torch.zeros_like(g) for g in s["grads"]]
+        shapes = _shapes(case)
+        s["out"] = {t: torch.zeros(sum(r * c for u, r, c in shapes if u == t), dtype=_DTYPES[t], device="cuda")
+                    for t in sorted({t for t, _, _ in shapes})}
+        s["to"] = _matrices(s["out"], shapes)
         if own:
             from paper_2609_09020_gb300 import pic
-            s["orth"] = pic.Orthogonalizer(s["grads"], out=s["out"])
+            s["orth"] = pic.Orthogonalizer(s["grads"], out=s["to"])
     return s
 
 
@@ -210,7 +227,7 @@ def _plain(s):
     case = s["case"]
     if case["op"] == "orth":
         a, b, c = _COEFFICIENTS
-        for g, out in zip(s["grads"], s["out"]):
+        for g, out in zip(s["grads"], s["to"]):
             x = g.float()
             x = x / (torch.sqrt((x * x).sum()) + _EPS)
             if g.shape[0] > g.shape[1]:
@@ -271,8 +288,8 @@ def exact(case, seed):
     s = _inputs(case, seed)
     if case["op"] == "orth":
         a, b, c = _COEFFICIENTS
-        done = []
-        for g in s["grads"]:
+        done = {}
+        for (t, _, _), g in zip(_shapes(case), s["grads"]):
             x = g.double()
             x /= torch.linalg.vector_norm(x) + _EPS
             for _ in range(_STEPS):
@@ -282,8 +299,8 @@ def exact(case, seed):
                 q = b * p + c * torch.mm(p, p)
                 q.diagonal().add_(a)
                 x = torch.mm(q, x) if left else torch.mm(x, q)
-            done.append(x)
-        return {"out": done}
+            done.setdefault(t, []).append(x.reshape(-1))
+        return {"out": {t: torch.cat(done[t]) for t in sorted(done)}}
     phi = torch.distributions.Normal(0.0, 1.0, validate_args=False)
     M, K, N, act = case["rows"], case["inp"], case["outp"], case["act"]
     lens = torch.diff(s["offsets"])
