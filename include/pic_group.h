@@ -1,0 +1,121 @@
+/*
+ * pic_group.h -- C ABI of linear layers of many nets at once, and their
+ * gradient: the layers of the per-image nets of a batch (MLP^i, arxiv 2609.09020
+ * Sec. 3.1), whose images have pixels in different numbers.
+ *
+ * The rows of x are sorted by group; group g's are [offsets[g], offsets[g + 1]),
+ * and it has weights and a bias of its own:
+ *
+ *   forward   z = x w_g^T + b_g,  y = act(z)
+ *   backward  dz = dy * act'(z),  dx = dz w_g,  dw_g = dz_g^T x_g,
+ *             db_g = sum of dz over the group's rows
+ *
+ * with act, types, sums and roundings as in pic_linear.h.  Rows of one group
+ * never meet those of another: a NaN stays in its group.  A group without rows
+ * has gradients of zero.  Rows before offsets[0] and from offsets[groups] on
+ * belong to no group: nothing of them is read, and y, pre and dx are not
+ * written there.
+ *
+ * offsets are int64 on the device, read when the kernels run, so that a
+ * program need not wait for them on the host.  They must not decrease and must
+ * lie in [0, rows].  What does not is held to that (each offset is taken as
+ * the largest so far, at most rows), so that no call reads or writes out of
+ * range, and pic_grouped_linear_check reports it.
+ *
+ * Conventions as in pic_linear.h: device pointers owned by the caller and
+ * aligned to their element, asynchronous on `stream`, pic_status codes, no
+ * traps, nothing allocated; calls that overlap on the GPU need workspaces of
+ * their own.  Results do not vary from call to call.
+ */
+#ifndef PIC_GROUP_H
+#define PIC_GROUP_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "pic_linear.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+#define PIC_MAX_GROUPS 1024
+
+/* rows >= 0, in_features >= 1, out_features >= 1, each below 2^31 - 256;
+ * 1 <= groups <= PIC_MAX_GROUPS. */
+typedef struct {
+  int64_t rows, in_features, out_features;
+  int groups;
+  int dtype; /* pic_dtype */
+  int act;   /* PIC_ACT_NONE, PIC_ACT_RELU or PIC_ACT_GELU */
+  const int64_t *offsets; /* [groups + 1], 8-byte aligned */
+  const void *x;          /* [rows][in] */
+  int64_t ldx;            /* >= in_features */
+  const void *w;          /* [groups][out][in] */
+  int64_t ldw;            /* >= in_features */
+  int64_t w_group; /* elements from one group's weights to the next's: at least
+                      (out_features - 1) ldw + in_features, with more than one group */
+  const void *bias;  /* [groups][out_features], or NULL */
+  int64_t bias_group; /* >= out_features, with more than one group */
+  void *y;            /* [rows][out] */
+  int64_t ldy;
+  void *pre; /* receives z for the backward pass, or NULL */
+  int64_t ldpre;
+} pic_grouped_linear_args;
+
+/* Bytes of device workspace that pic_grouped_linear needs for these sizes, types,
+ * strides and pointers (it may be 0), or -1 for arguments it would refuse. */
+int64_t pic_grouped_linear_workspace_bytes(const pic_grouped_linear_args *a);
+
+/*
+ * The forward layers.  With rows = 0 nothing is launched.  Outputs overlap
+ * neither inputs nor each other.
+ * Errors: PIC_ERR_INVALID_ARG (NULL or misaligned pointers, sizes, strides,
+ * groups, type or activation out of range, workspace too small or not 256-byte
+ * aligned) with nothing launched; PIC_ERR_UNSUPPORTED (a device that is not
+ * sm_103); PIC_ERR_CUDA.
+ */
+int pic_grouped_linear(const pic_grouped_linear_args *a, void *workspace, size_t workspace_bytes, void *stream);
+
+typedef struct {
+  int64_t rows, in_features, out_features;
+  int groups;
+  int dtype;
+  int act;
+  const int64_t *offsets;
+  const void *dy; /* [rows][out] */
+  int64_t lddy;
+  const void *x; /* read for dw; may be NULL without dw */
+  int64_t ldx;
+  const void *w; /* read for dx; may be NULL without dx */
+  int64_t ldw;
+  int64_t w_group;
+  const void *pre; /* z of the forward pass (ReLU: y will do); may be NULL with PIC_ACT_NONE */
+  int64_t ldpre;
+  void *dx; /* [rows][in], or NULL: not computed */
+  int64_t lddx;
+  void *dw; /* [groups][out][in], or NULL */
+  int64_t lddw;
+  int64_t dw_group;
+  void *db; /* [groups][out], or NULL */
+  int64_t db_group;
+} pic_grouped_linear_grad_args;
+
+int64_t pic_grouped_linear_backward_workspace_bytes(const pic_grouped_linear_grad_args *a);
+
+/* The gradients that are asked for (at least one); every group's dw and db are
+ * written, zeros where it has no rows.  Errors as for pic_grouped_linear. */
+int pic_grouped_linear_backward(const pic_grouped_linear_grad_args *a, void *workspace, size_t workspace_bytes,
+                                void *stream);
+
+/* Synchronises `stream`; PIC_OK if since the last check, on the current device,
+ * no bounded device-side wait of these calls or of pic_linear.h's gave up
+ * (PIC_ERR_TIMEOUT if one did: its outputs are unspecified) and all offsets
+ * were as they must be (else PIC_ERR_INVALID_ARG); PIC_ERR_CUDA. */
+int pic_grouped_linear_check(void *stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* PIC_GROUP_H */

@@ -3,8 +3,8 @@
 Each translation unit is compiled by its own nvcc process, in parallel, then
 linked into one shared library with the C ABI of include/pic_decode.h,
 include/pic_izpr.h, include/pic_idct.h, include/pic_fuse.h,
-include/pic_huffman.h, include/pic_linear.h, include/pic_clip.h and
-include/pic_measure.h.
+include/pic_huffman.h, include/pic_linear.h, include/pic_clip.h,
+include/pic_group.h, include/pic_orth.h and include/pic_measure.h.
 """
 from __future__ import annotations
 
@@ -27,7 +27,8 @@ SOURCES = ["pic_decode.cu", "k_fp32.cu", "k_fp32_any.cu", "k_fp32_sweep.cu", "k_
            "k_linear_planes.cu", "k_linear_narrow.cu", "k_linear_few.cu", "k_linear_few32.cu",
            "k_linear_thin.cu", "k_linear_thin_f16.cu", "k_linear_thin_bf16.cu",
            "k_linear_thin_f32.cu",
-           "k_linear_outer.cu", "k_clip.cu"]
+           "k_linear_outer.cu", "k_clip.cu", "pic_group.cu", "k_group_any.cu",
+           "k_orth.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",
          "--expt-relaxed-constexpr", "-I", INCLUDE, "-I", CSRC]

@@ -1,0 +1,141 @@
+// group.cuh -- what the kernels of the grouped linear layer (include/pic_group.h)
+// share: the table of groups and the launch interfaces between their translation
+// units.
+#pragma once
+
+#include "linear.cuh"
+#include "pic_group.h"
+
+namespace pic {
+namespace grp {
+
+using lin::Waits;
+
+constexpr int kMaxGroups = PIC_MAX_GROUPS;
+
+// A CTA's table of groups, in shared memory: first rows, and the number of tiles of
+// `unit` rows before each group's.  An offset counts as the largest so far, within [0, rows].
+struct GroupTable {
+  int start[kMaxGroups + 1];
+  int tiles[kMaxGroups + 1];
+  int scan[32];
+
+  __device__ __forceinline__ int rows(int g) const { return start[g + 1] - start[g]; }
+  // the group that has tile t, of those in the table
+  __device__ __forceinline__ int find(int t, int groups) const {
+    int lo = 0, hi = groups - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (tiles[mid + 1] <= t)
+        lo = mid + 1;
+      else
+        hi = mid;
+    }
+    return lo;
+  }
+};
+
+// Inclusive scan over the block's threads (at most 1024, whole warps).
+template <bool MAX>
+__device__ __forceinline__ int block_scan(int v, int* scratch) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const auto join = [](int a, int b) { return MAX ? max(a, b) : a + b; };
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const int o = __shfl_up_sync(0xffffffffu, v, d);
+    if (lane >= d) v = join(v, o);
+  }
+  __syncthreads();
+  if (lane == 31) scratch[warp] = v;
+  __syncthreads();
+  int before = 0;  // offsets and counts are not negative
+  for (int w = 0; w < warp && w < warps; ++w) before = join(before, scratch[w]);
+  return join(before, v);
+}
+
+// Filled by all threads of the block; tiles of a group without rows: `least`.  Block
+// 0 reports offsets that are not as they must be.
+__device__ __forceinline__ void make_table(GroupTable& t, const long long* offsets, int groups, long long rows, int unit,
+                                           int least, int* status) {
+  const int each = (groups + blockDim.x) / blockDim.x;  // of groups + 1 offsets
+  const int first = threadIdx.x * each, last = min(first + each, groups + 1);
+  int most = 0;
+  bool bad = false;
+  for (int i = first; i < last; ++i) {
+    const long long o = offsets[i];
+    bad |= o < 0 || o > rows;
+    const int held = static_cast<int>(min(max(o, 0LL), rows));
+    bad |= held < most;
+    most = max(most, held);
+    t.start[i] = most;
+  }
+  // the largest of the threads before
+  const int upto = block_scan<true>(most, t.scan);
+  int before = __shfl_up_sync(0xffffffffu, upto, 1);
+  if ((threadIdx.x & 31) == 0) {
+    before = 0;
+    for (int w = 0; w < static_cast<int>(threadIdx.x >> 5); ++w) before = max(before, t.scan[w]);
+  }
+  for (int i = first; i < last; ++i) {
+    bad |= t.start[i] < before;
+    t.start[i] = max(t.start[i], before);
+  }
+  if (bad && blockIdx.x == 0) atomicOr(status + 1, 1);
+  __syncthreads();
+  int count = 0;
+  for (int g = first; g < min(last, groups); ++g) count += max(least, (t.rows(g) + unit - 1) / unit);
+  int at = block_scan<false>(count, t.scan) - count;
+  for (int g = first; g < last; ++g) {
+    t.tiles[g] = at;
+    if (g < groups) at += max(least, (t.rows(g) + unit - 1) / unit);
+  }
+  __syncthreads();
+}
+
+// Products of any types, strides and sizes.  ROWS: y[i][j] = sum_k a(i, k) b_g(j, k)
+// for the rows i of group g, a(i, k) at a[i * a_i + k], b_g(j, k) at b[g * b_group + j
+// * b_j + k * b_k], with the layer's epilogue.  Else y_g[i][j] = sum over the group's
+// rows k of a(k, i) b(k, j), a at a[k * a_i + i], b at b[k * b_k + j].  Where there is
+// an a_pre, a is multiplied by act'(a_pre).
+struct GroupProduct {
+  bool by_rows;
+  const void* a;
+  long long a_i;
+  const void* a_pre;
+  long long a_pre_i;
+  int a_act;
+  const void* b;
+  long long b_group, b_j, b_k;
+  long long rows;  // of all groups, and around them
+  long long I;     // columns of a that are rows of y_g (not by_rows)
+  long long J, K;  // K: by_rows
+  int groups;
+  const long long* offsets;
+  const void* bias;
+  long long bias_group;
+  void* y;
+  long long ldy, y_group;
+  void* pre;
+  long long ldpre;
+  int act;
+  int* status;
+};
+int any_product(const GroupProduct& p, int dtype, cudaStream_t s);
+
+// db_g = sum of dy act'(z) over each group's rows.
+struct GroupSums {
+  const void* dy;
+  long long lddy;
+  const void* pre;
+  long long ldpre;
+  void* db;
+  long long db_group;
+  long long rows, J;
+  int groups, act;
+  const long long* offsets;
+  int* status;
+};
+int any_sums(const GroupSums& g, int dtype, cudaStream_t s);
+
+}  // namespace grp
+}  // namespace pic

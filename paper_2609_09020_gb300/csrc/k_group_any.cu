@@ -1,0 +1,145 @@
+// k_group_any.cu -- grouped products of any type, stride and size on the FP32
+// cores: tiles of 64 x 64, 16 of K at a time through shared memory, sixteen sums a
+// thread.  CTAs are persistent, with the table of groups in shared memory, and take
+// tiles one after another.
+#include "group.cuh"
+
+namespace pic {
+namespace grp {
+namespace {
+
+using lin::act_grad;
+using lin::act_value;
+using lin::from_f32;
+using lin::to_f32;
+
+constexpr int kTile = 64, kDeep = 16, kThreads = 256;
+constexpr int kSms = 152;
+
+template <typename T, bool ROWS>
+__global__ void __launch_bounds__(kThreads) any_kernel(const GroupProduct p) {
+  constexpr bool EXACT = sizeof(T) == 4;
+  __shared__ GroupTable table;
+  __shared__ __align__(16) float sa[kDeep][kTile + 4], sb[kDeep][kTile + 4];
+  make_table(table, p.offsets, p.groups, p.rows, kTile, 0, p.status);
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const long long tiles_j = (p.J + kTile - 1) / kTile, tiles_i = (p.I + kTile - 1) / kTile;
+  const long long work = ROWS ? table.tiles[p.groups] * tiles_j : p.groups * tiles_i * tiles_j;
+  const T *a = static_cast<const T*>(p.a), *b = static_cast<const T*>(p.b), *z = static_cast<const T*>(p.a_pre);
+  for (long long w = blockIdx.x; w < work; w += gridDim.x) {
+    const long long tj = w % tiles_j, t = w / tiles_j;
+    const int g = ROWS ? table.find(static_cast<int>(t), p.groups) : static_cast<int>(t / tiles_i);
+    const long long first = table.start[g], len = table.rows(g);
+    const long long i0 = (ROWS ? t - table.tiles[g] : t % tiles_i) * kTile, j0 = tj * kTile;
+    const long long I = ROWS ? len : p.I, K = ROWS ? p.K : len;
+    const T* bg = ROWS ? b + g * p.b_group : b + first * p.b_k;
+    float acc[4][4] = {};
+    for (long long k0 = 0; k0 < K; k0 += kDeep) {
+      for (int e = threadIdx.x; e < kTile * kDeep; e += kThreads) {
+        // neighbouring threads along what is contiguous
+        const int ka = ROWS ? e % kDeep : e / kTile, ia = ROWS ? e / kDeep : e % kTile;
+        float v = 0.0f;
+        if (i0 + ia < I && k0 + ka < K) {
+          const long long row = first + (ROWS ? i0 + ia : k0 + ka), col = ROWS ? k0 + ka : i0 + ia;
+          v = to_f32(a[row * p.a_i + col]);
+          if (z) v = act_grad<EXACT>(v, to_f32(z[row * p.a_pre_i + col]), p.a_act);
+        }
+        sa[ka][ia] = v;
+        const bool along = ROWS && p.b_k == 1;
+        const int kb = along ? e % kDeep : e / kTile, jb = along ? e / kDeep : e % kTile;
+        sb[kb][jb] = j0 + jb < p.J && k0 + kb < K ? to_f32(bg[(j0 + jb) * p.b_j + (k0 + kb) * p.b_k]) : 0.0f;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < kDeep; ++k) {
+        const float4 u = *reinterpret_cast<const float4*>(&sa[k][4 * ty]), v = *reinterpret_cast<const float4*>(&sb[k][4 * tx]);
+        const float x[4] = {u.x, u.y, u.z, u.w}, y[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[r][c] = fmaf(x[r], y[c], acc[r][c]);
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const long long i = i0 + 4 * ty + r;
+      if (i >= I) break;
+      const long long row = ROWS ? first + i : i;
+      T* y = static_cast<T*>(p.y) + (ROWS ? 0 : g * p.y_group) + row * p.ldy;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const long long j = j0 + 4 * tx + c;
+        if (j >= p.J) break;
+        float v = acc[r][c];
+        if (p.bias) v += to_f32(static_cast<const T*>(p.bias)[g * p.bias_group + j]);
+        if (p.pre) static_cast<T*>(p.pre)[row * p.ldpre + j] = from_f32<T>(v);
+        y[j] = from_f32<T>(act_value<EXACT>(v, p.act));
+      }
+    }
+  }
+}
+
+// A block takes 32 columns of a group: 32 runs of its rows side by side.
+template <typename T>
+__global__ void __launch_bounds__(1024) sums_kernel(const GroupSums q) {
+  constexpr bool EXACT = sizeof(T) == 4;
+  __shared__ GroupTable table;
+  __shared__ float sums[32][33];
+  make_table(table, q.offsets, q.groups, q.rows, 1, 0, q.status);
+  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+  const long long blocks_j = (q.J + 31) / 32;
+  for (long long w = blockIdx.x; w < blocks_j * q.groups; w += gridDim.x) {
+    const int g = static_cast<int>(w / blocks_j);
+    const long long j = w % blocks_j * 32 + tx;
+    float sum = 0.0f;
+    if (j < q.J)
+      for (long long r = table.start[g] + ty; r < table.start[g + 1]; r += 32) {
+        const float d = to_f32(static_cast<const T*>(q.dy)[r * q.lddy + j]);
+        sum += q.act == PIC_ACT_NONE ? d : act_grad<EXACT>(d, to_f32(static_cast<const T*>(q.pre)[r * q.ldpre + j]), q.act);
+      }
+    sums[ty][tx] = sum;
+    __syncthreads();
+    if (ty == 0 && j < q.J) {
+      for (int r = 1; r < 32; ++r) sum += sums[r][tx];
+      static_cast<T*>(q.db)[g * q.db_group + j] = from_f32<T>(sum);
+    }
+    __syncthreads();
+  }
+}
+
+template <typename T>
+int run(const GroupProduct& p, cudaStream_t s) {
+  const long long tiles_j = (p.J + kTile - 1) / kTile, tiles_i = (p.I + kTile - 1) / kTile;
+  const long long most = p.by_rows ? ((p.rows + kTile - 1) / kTile + p.groups) * tiles_j : p.groups * tiles_i * tiles_j;
+  const unsigned grid = static_cast<unsigned>(most < 4 * kSms ? most : 4 * kSms);
+  if (p.by_rows)
+    any_kernel<T, true><<<grid, kThreads, 0, s>>>(p);
+  else
+    any_kernel<T, false><<<grid, kThreads, 0, s>>>(p);
+  return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+}
+
+template <typename T>
+int run(const GroupSums& g, cudaStream_t s) {
+  const long long most = (g.J + 31) / 32 * g.groups;
+  sums_kernel<T><<<static_cast<unsigned>(most < 2 * kSms ? most : 2 * kSms), 1024, 0, s>>>(g);
+  return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+}
+
+}  // namespace
+
+int any_product(const GroupProduct& p, int dtype, cudaStream_t s) {
+  if (dtype == PIC_DTYPE_F32) return run<float>(p, s);
+  if (dtype == PIC_DTYPE_F16) return run<__half>(p, s);
+  return run<__nv_bfloat16>(p, s);
+}
+
+int any_sums(const GroupSums& g, int dtype, cudaStream_t s) {
+  if (dtype == PIC_DTYPE_F32) return run<float>(g, s);
+  if (dtype == PIC_DTYPE_F16) return run<__half>(g, s);
+  return run<__nv_bfloat16>(g, s);
+}
+
+}  // namespace grp
+}  // namespace pic

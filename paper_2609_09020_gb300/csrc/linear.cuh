@@ -255,6 +255,26 @@ struct Waits {
   int test_fault;
 };
 
+// PIC_OK on a device that the kernels are built for.
+int device_status();
+// False if the status word has no address.
+bool call_waits(Waits& w);
+// Word 0 or 1 behind Waits::status (a wait that gave up; offsets of groups that are not
+// as they must be), which is then 0; -1 for an error.  Synchronises.
+int take_status(int word, cudaStream_t s);
+
+// Hands out 256-byte aligned pieces of a workspace; with a null base it only
+// counts.
+struct Arena {
+  char* base;
+  long long used = 0;
+  void* take(long long bytes) {
+    void* p = base ? base + used : nullptr;
+    used += (bytes + 255) / 256 * 256;
+    return p;
+  }
+};
+
 // On the tensor cores.
 long long tc_workspace(const Product& p, int dtype);
 int tc_product(const Product& p, int dtype, void* ws, const Waits& waits, cudaStream_t s);

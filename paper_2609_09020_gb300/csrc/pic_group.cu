@@ -1,0 +1,150 @@
+// pic_group.cu -- the C ABI of include/pic_group.h: checks of arguments and the
+// choice of kernels.
+#include "group.cuh"
+
+namespace {
+
+using pic::grp::GroupProduct;
+using pic::grp::GroupSums;
+
+constexpr long long kMaxDim = 0x7fffffffLL - 256;
+
+bool aligned(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+size_t elem_bytes(int dtype) { return dtype == PIC_DTYPE_F32 ? 4 : 2; }
+
+// A [rows][cols] matrix of the call, or [groups] of them, each `group` elements behind the one before.
+bool matrix_ok(const void* p, long long ld, long long rows, long long cols, int dtype) {
+  return (p || rows == 0) && aligned(p, elem_bytes(dtype)) && ld >= cols && ld <= (1LL << 40);
+}
+bool matrices_ok(const void* p, long long ld, long long group, int groups, long long rows, long long cols, int dtype) {
+  if (!matrix_ok(p, ld, rows, cols, dtype)) return false;
+  return groups == 1 || (group <= (1LL << 44) && (rows == 1 || ld <= group) && group >= (rows - 1) * ld + cols);
+}
+bool vectors_ok(const void* p, long long group, int groups, long long n, int dtype) {
+  return aligned(p, elem_bytes(dtype)) && (groups == 1 || (group >= n && group <= (1LL << 44)));
+}
+
+template <typename Args>
+bool sizes_ok(const Args* a) {
+  if (!a) return false;
+  const auto dim = [](long long v, long long least) { return v >= least && v <= kMaxDim; };
+  return dim(a->rows, 0) && dim(a->in_features, 1) && dim(a->out_features, 1) && a->groups >= 1 &&
+         a->groups <= PIC_MAX_GROUPS && (a->dtype == PIC_DTYPE_F32 || a->dtype == PIC_DTYPE_F16 || a->dtype == PIC_DTYPE_BF16) &&
+         (a->act == PIC_ACT_NONE || a->act == PIC_ACT_RELU || a->act == PIC_ACT_GELU) && a->offsets && aligned(a->offsets, 8);
+}
+
+bool args_ok(const pic_grouped_linear_args* a) {
+  if (!sizes_ok(a)) return false;
+  const long long M = a->rows, K = a->in_features, N = a->out_features;
+  return matrix_ok(a->x, a->ldx, M, K, a->dtype) && matrices_ok(a->w, a->ldw, a->w_group, a->groups, N, K, a->dtype) &&
+         (!a->bias || vectors_ok(a->bias, a->bias_group, a->groups, N, a->dtype)) && matrix_ok(a->y, a->ldy, M, N, a->dtype) &&
+         (!a->pre || matrix_ok(a->pre, a->ldpre, M, N, a->dtype));
+}
+
+bool args_ok(const pic_grouped_linear_grad_args* a) {
+  if (!sizes_ok(a) || (!a->dx && !a->dw && !a->db)) return false;
+  const long long M = a->rows, K = a->in_features, N = a->out_features;
+  if (!matrix_ok(a->dy, a->lddy, M, N, a->dtype)) return false;
+  if (a->act != PIC_ACT_NONE && !matrix_ok(a->pre, a->ldpre, M, N, a->dtype)) return false;
+  if (a->dw && (!matrix_ok(a->x, a->ldx, M, K, a->dtype) ||
+                !matrices_ok(a->dw, a->lddw, a->dw_group, a->groups, N, K, a->dtype)))
+    return false;
+  if (a->dx && (!matrices_ok(a->w, a->ldw, a->w_group, a->groups, N, K, a->dtype) || !matrix_ok(a->dx, a->lddx, M, K, a->dtype)))
+    return false;
+  return !a->db || vectors_ok(a->db, a->db_group, a->groups, N, a->dtype);
+}
+
+const long long* offsets_of(const int64_t* o) { return reinterpret_cast<const long long*>(o); }
+
+int forward(const pic_grouped_linear_args& a, pic::lin::Arena&, bool launch, const pic::lin::Waits& w, cudaStream_t s) {
+  if (a.rows == 0 || !launch) return PIC_OK;
+  GroupProduct p{};
+  p.by_rows = true;
+  p.a = a.x, p.a_i = a.ldx;
+  p.b = a.w, p.b_group = a.w_group, p.b_j = a.ldw, p.b_k = 1;
+  p.rows = a.rows, p.J = a.out_features, p.K = a.in_features;
+  p.groups = a.groups, p.offsets = offsets_of(a.offsets);
+  p.bias = a.bias, p.bias_group = a.bias_group;
+  p.y = a.y, p.ldy = a.ldy, p.pre = a.pre, p.ldpre = a.ldpre, p.act = a.act;
+  p.status = w.status;
+  return pic::grp::any_product(p, a.dtype, s);
+}
+
+int backward(const pic_grouped_linear_grad_args& a, pic::lin::Arena&, bool launch, const pic::lin::Waits& w, cudaStream_t s) {
+  if (!launch) return PIC_OK;
+  int rc = PIC_OK;
+  GroupProduct p{};
+  p.a = a.dy, p.a_i = a.lddy;
+  if (a.act != PIC_ACT_NONE) p.a_pre = a.pre, p.a_pre_i = a.ldpre, p.a_act = a.act;
+  p.rows = a.rows, p.groups = a.groups, p.offsets = offsets_of(a.offsets);
+  p.act = PIC_ACT_NONE;
+  p.status = w.status;
+  if (a.dx && a.rows > 0) {
+    p.by_rows = true;
+    p.b = a.w, p.b_group = a.w_group, p.b_j = 1, p.b_k = a.ldw;
+    p.J = a.in_features, p.K = a.out_features;
+    p.y = a.dx, p.ldy = a.lddx;
+    if ((rc = pic::grp::any_product(p, a.dtype, s)) != PIC_OK) return rc;
+  }
+  if (a.dw) {
+    p.by_rows = false;
+    p.b = a.x, p.b_j = 1, p.b_k = a.ldx;
+    p.I = a.out_features, p.J = a.in_features;
+    p.y = a.dw, p.ldy = a.lddw, p.y_group = a.dw_group;
+    if ((rc = pic::grp::any_product(p, a.dtype, s)) != PIC_OK) return rc;
+  }
+  if (a.db) {
+    const GroupSums g{a.dy, a.lddy, a.pre, a.ldpre, a.db, a.db_group, a.rows, a.out_features,
+                      a.groups, a.act, offsets_of(a.offsets), w.status};
+    rc = pic::grp::any_sums(g, a.dtype, s);
+  }
+  return rc;
+}
+
+template <typename Args, typename F>
+int64_t count_bytes(const Args* a, F f) {
+  if (!args_ok(a)) return -1;
+  pic::lin::Arena ws{nullptr};
+  f(*a, ws, false, pic::lin::Waits{}, nullptr);
+  return ws.used;
+}
+
+template <typename Args, typename F>
+int run(const Args* a, F f, void* workspace, size_t bytes, void* stream) {
+  const int64_t need = count_bytes(a, f);
+  if (need < 0 || bytes < static_cast<size_t>(need)) return PIC_ERR_INVALID_ARG;
+  if (need > 0 && (!workspace || !aligned(workspace, 256))) return PIC_ERR_INVALID_ARG;
+  const int rc = pic::lin::device_status();
+  if (rc != PIC_OK) return rc;
+  pic::lin::Waits w;
+  if (!pic::lin::call_waits(w)) return PIC_ERR_CUDA;
+  pic::lin::Arena ws{static_cast<char*>(workspace)};
+  const int r = f(*a, ws, true, w, static_cast<cudaStream_t>(stream));
+  if (r == PIC_ERR_CUDA) cudaGetLastError();
+  return r;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t pic_grouped_linear_workspace_bytes(const pic_grouped_linear_args* a) { return count_bytes(a, forward); }
+
+int pic_grouped_linear(const pic_grouped_linear_args* a, void* workspace, size_t workspace_bytes, void* stream) {
+  return run(a, forward, workspace, workspace_bytes, stream);
+}
+
+int64_t pic_grouped_linear_backward_workspace_bytes(const pic_grouped_linear_grad_args* a) { return count_bytes(a, backward); }
+
+int pic_grouped_linear_backward(const pic_grouped_linear_grad_args* a, void* workspace, size_t workspace_bytes, void* stream) {
+  return run(a, backward, workspace, workspace_bytes, stream);
+}
+
+int pic_grouped_linear_check(void* stream) {
+  const int offsets = pic::lin::take_status(1, static_cast<cudaStream_t>(stream));
+  const int waits = pic::lin::take_status(0, static_cast<cudaStream_t>(stream));
+  if (offsets < 0 || waits < 0) return PIC_ERR_CUDA;
+  return waits ? PIC_ERR_TIMEOUT : offsets ? PIC_ERR_INVALID_ARG : PIC_OK;
+}
+
+}  // extern "C"

@@ -4,8 +4,85 @@
 
 #include "linear.cuh"
 
+namespace pic {
+namespace lin {
 namespace {
 
+// The words that a kernel sets: when one of its bounded waits gives up, and when a
+// grouped call's offsets are not as they must be.  Their address on each device is
+// looked up once.
+__device__ int lin_status[2];
+
+int* status_word() {
+  static std::atomic<int*> known[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
+  int* p = known[dev].load(std::memory_order_relaxed);
+  if (!p) {
+    void* v = nullptr;
+    if (cudaGetSymbolAddress(&v, lin_status) != cudaSuccess) return nullptr;
+    p = static_cast<int*>(v);
+    known[dev].store(p, std::memory_order_relaxed);
+  }
+  return p;
+}
+
+// pic_linear_test_wait_fault's: nonzero only while a test makes a wait run out.
+std::atomic<int> test_fault{0};
+std::atomic<unsigned> test_spin_limit{0};
+
+}  // namespace
+
+// The device must be the one that the kernels are built for; looked up once
+// per device (0: not yet, 1: it is, 2: it is not).
+int device_status() {
+  static std::atomic<int> known[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) {
+    cudaGetLastError();
+    return PIC_ERR_UNSUPPORTED;
+  }
+  if (dev < 0 || dev >= 64) return PIC_ERR_UNSUPPORTED;
+  int k = known[dev].load(std::memory_order_relaxed);
+  if (k == 0) {
+    int major = 0, minor = 0;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess) {
+      cudaGetLastError();
+      return PIC_ERR_CUDA;
+    }
+    k = major == 10 && minor == 3 ? 1 : 2;
+    known[dev].store(k, std::memory_order_relaxed);
+  }
+  return k == 1 ? PIC_OK : PIC_ERR_UNSUPPORTED;
+}
+
+// False if the status word has no address.
+bool call_waits(Waits& w) {
+  const unsigned limit = test_spin_limit.load(std::memory_order_relaxed);
+  w = {status_word(), limit ? limit : pic::kWaitPolls, test_fault.load(std::memory_order_relaxed)};
+  return w.status != nullptr;
+}
+
+int take_status(int word, cudaStream_t s) {
+  int* status = status_word();
+  int flag = 0;
+  if (status) status += word;
+  if (!status || cudaMemcpyAsync(&flag, status, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess ||
+      cudaStreamSynchronize(s) != cudaSuccess ||
+      (flag && (cudaMemsetAsync(status, 0, sizeof(int), s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess))) {
+    cudaGetLastError();
+    return -1;
+  }
+  return flag;
+}
+
+}  // namespace lin
+}  // namespace pic
+
+namespace {
+
+using pic::lin::Arena;
 using pic::lin::GradAct;
 using pic::lin::Product;
 
@@ -51,59 +128,6 @@ bool args_ok(const pic_linear_grad_args* a) {
   return !a->db || aligned(a->db, elem_bytes(a->dtype));
 }
 
-// The device must be the one that the kernels are built for; looked up once
-// per device (0: not yet, 1: it is, 2: it is not).
-int device_status() {
-  static std::atomic<int> known[64];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) {
-    cudaGetLastError();
-    return PIC_ERR_UNSUPPORTED;
-  }
-  if (dev < 0 || dev >= 64) return PIC_ERR_UNSUPPORTED;
-  int k = known[dev].load(std::memory_order_relaxed);
-  if (k == 0) {
-    int major = 0, minor = 0;
-    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess) {
-      cudaGetLastError();
-      return PIC_ERR_CUDA;
-    }
-    k = major == 10 && minor == 3 ? 1 : 2;
-    known[dev].store(k, std::memory_order_relaxed);
-  }
-  return k == 1 ? PIC_OK : PIC_ERR_UNSUPPORTED;
-}
-
-// The word that a kernel sets when one of its bounded waits gives up; its
-// address on each device is looked up once.
-__device__ int lin_status;
-
-int* status_word() {
-  static std::atomic<int*> known[64];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
-  int* p = known[dev].load(std::memory_order_relaxed);
-  if (!p) {
-    void* v = nullptr;
-    if (cudaGetSymbolAddress(&v, lin_status) != cudaSuccess) return nullptr;
-    p = static_cast<int*>(v);
-    known[dev].store(p, std::memory_order_relaxed);
-  }
-  return p;
-}
-
-// pic_linear_test_wait_fault's: nonzero only while a test makes a wait run out.
-std::atomic<int> test_fault{0};
-std::atomic<unsigned> test_spin_limit{0};
-
-// False if the status word has no address.
-bool waits(pic::lin::Waits& w) {
-  const unsigned limit = test_spin_limit.load(std::memory_order_relaxed);
-  w = {status_word(), limit ? limit : pic::kWaitPolls, test_fault.load(std::memory_order_relaxed)};
-  return w.status != nullptr;
-}
-
 // Whether the kernels for few rows take a product (they need no workspace), its
 // workspace bytes, and the product.
 bool few(const Product& p, int dtype) {
@@ -119,20 +143,8 @@ int product(const Product& p, int dtype, void* ws, cudaStream_t s) {
     return dtype == PIC_DTYPE_F32 ? pic::lin::few32_product(p, s) : pic::lin::few_product(p, dtype, s);
   if (pic::lin::thin_takes(p, dtype)) return pic::lin::thin_product(p, dtype, s);
   pic::lin::Waits w;
-  return waits(w) ? pic::lin::tc_product(p, dtype, ws, w, s) : PIC_ERR_CUDA;
+  return pic::lin::call_waits(w) ? pic::lin::tc_product(p, dtype, ws, w, s) : PIC_ERR_CUDA;
 }
-
-// Hands out 256-byte aligned pieces of a workspace; with a null base it only
-// counts.
-struct Arena {
-  char* base;
-  long long used = 0;
-  void* take(long long bytes) {
-    void* p = base ? base + used : nullptr;
-    used += (bytes + 255) / 256 * 256;
-    return p;
-  }
-};
 
 Product forward_product(const pic_linear_args& a) {
   Product p{};
@@ -172,7 +184,7 @@ int backward(const pic_linear_grad_args& a, Arena& ws, bool launch, cudaStream_t
       void* w = ws.take(pic::lin::narrow_workspace(g, a.dtype));
       if (!launch) return PIC_OK;
       pic::lin::Waits wt;
-      return waits(wt) ? pic::lin::narrow_grad(g, a.dtype, w, wt, s) : PIC_ERR_CUDA;
+      return pic::lin::call_waits(wt) ? pic::lin::narrow_grad(g, a.dtype, w, wt, s) : PIC_ERR_CUDA;
     }
   }
   const auto dx_product = [&](const void* dz, long long lddz) {
@@ -241,7 +253,7 @@ int run(const Args* a, F f, void* workspace, size_t bytes, void* stream) {
   const int64_t need = count_bytes(a, f);
   if (need < 0 || bytes < static_cast<size_t>(need)) return PIC_ERR_INVALID_ARG;
   if (need > 0 && (!workspace || !aligned(workspace, 256))) return PIC_ERR_INVALID_ARG;
-  const int rc = device_status();
+  const int rc = pic::lin::device_status();
   if (rc != PIC_OK) return rc;
   Arena ws{static_cast<char*>(workspace)};
   const int r = f(*a, ws, true, static_cast<cudaStream_t>(stream));
@@ -266,22 +278,15 @@ int pic_linear_backward(const pic_linear_grad_args* a, void* workspace, size_t w
 }
 
 int pic_linear_check(void* stream) {
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  int* status = status_word();
-  int flag = 0;
-  if (!status || cudaMemcpyAsync(&flag, status, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess ||
-      cudaStreamSynchronize(s) != cudaSuccess ||
-      (flag && (cudaMemsetAsync(status, 0, sizeof(int), s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess))) {
-    cudaGetLastError();
-    return PIC_ERR_CUDA;
-  }
+  const int flag = pic::lin::take_status(0, static_cast<cudaStream_t>(stream));
+  if (flag < 0) return PIC_ERR_CUDA;
   return flag ? PIC_ERR_TIMEOUT : PIC_OK;
 }
 
 int pic_linear_test_wait_fault(int withhold_arrival, unsigned spin_limit) {
   if (withhold_arrival != 0 && withhold_arrival != 1) return PIC_ERR_INVALID_ARG;
-  test_spin_limit.store(spin_limit, std::memory_order_relaxed);
-  test_fault.store(withhold_arrival, std::memory_order_relaxed);
+  pic::lin::test_spin_limit.store(spin_limit, std::memory_order_relaxed);
+  pic::lin::test_fault.store(withhold_arrival, std::memory_order_relaxed);
   return PIC_OK;
 }
 

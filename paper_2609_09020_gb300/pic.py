@@ -91,8 +91,29 @@ class pic_linear_grad_args(ctypes.Structure):
                        ("db", _P))
 
 
+class pic_grouped_linear_args(ctypes.Structure):
+    _fields_ = _fields("rows in_features out_features", ("groups", ctypes.c_int), ("dtype", ctypes.c_int),
+                       ("act", ctypes.c_int), ("offsets", _P), ("x", _P), ("ldx", ctypes.c_int64), ("w", _P),
+                       ("ldw", ctypes.c_int64), ("w_group", ctypes.c_int64), ("bias", _P),
+                       ("bias_group", ctypes.c_int64), ("y", _P), ("ldy", ctypes.c_int64), ("pre", _P),
+                       ("ldpre", ctypes.c_int64))
+
+
+class pic_grouped_linear_grad_args(ctypes.Structure):
+    _fields_ = _fields("rows in_features out_features", ("groups", ctypes.c_int), ("dtype", ctypes.c_int),
+                       ("act", ctypes.c_int), ("offsets", _P), ("dy", _P), ("lddy", ctypes.c_int64), ("x", _P),
+                       ("ldx", ctypes.c_int64), ("w", _P), ("ldw", ctypes.c_int64), ("w_group", ctypes.c_int64),
+                       ("pre", _P), ("ldpre", ctypes.c_int64), ("dx", _P), ("lddx", ctypes.c_int64), ("dw", _P),
+                       ("lddw", ctypes.c_int64), ("dw_group", ctypes.c_int64), ("db", _P),
+                       ("db_group", ctypes.c_int64))
+
+
 class pic_clip_tensor(ctypes.Structure):
     _fields_ = [("grad", _P), ("out", _P), ("count", ctypes.c_int64), ("dtype", ctypes.c_int)]
+
+
+class pic_orth_matrix(ctypes.Structure):
+    _fields_ = [("grad", _P), ("out", _P)] + _fields("rows cols ld_grad ld_out", ("dtype", ctypes.c_int))
 
 
 _lib = None
@@ -158,7 +179,9 @@ def load_library():
     lib.pic_huffman_decode.restype = i
     lib.pic_huffman_status.argtypes = [_P, _P]
     lib.pic_huffman_status.restype = i
-    for name, args in (("pic_linear", pic_linear_args), ("pic_linear_backward", pic_linear_grad_args)):
+    for name, args in (("pic_linear", pic_linear_args), ("pic_linear_backward", pic_linear_grad_args),
+                       ("pic_grouped_linear", pic_grouped_linear_args),
+                       ("pic_grouped_linear_backward", pic_grouped_linear_grad_args)):
         f = getattr(lib, name)
         f.argtypes, f.restype = [ctypes.POINTER(args), _P, ctypes.c_size_t, _P], i
         f = getattr(lib, name + "_workspace_bytes")
@@ -167,6 +190,16 @@ def load_library():
     lib.pic_linear_check.restype = i
     lib.pic_linear_test_wait_fault.argtypes = [i, ctypes.c_uint]
     lib.pic_linear_test_wait_fault.restype = i
+    lib.pic_grouped_linear_check.argtypes = [_P]
+    lib.pic_grouped_linear_check.restype = i
+    lib.pic_orth_create.argtypes = [ctypes.POINTER(pic_orth_matrix), i, ctypes.POINTER(_P)]
+    lib.pic_orth_create.restype = i
+    lib.pic_orth.argtypes = [_P, i] + [ctypes.c_float] * 4 + [_P]
+    lib.pic_orth.restype = i
+    lib.pic_orth_check.argtypes = [_P, _P]
+    lib.pic_orth_check.restype = i
+    lib.pic_orth_destroy.argtypes = [_P]
+    lib.pic_orth_destroy.restype = None
     lib.pic_clip_create.argtypes = [ctypes.POINTER(pic_clip_tensor), i, ctypes.POINTER(_P)]
     lib.pic_clip_create.restype = i
     lib.pic_clip.argtypes = [_P, ctypes.c_float, _P, _P]
@@ -504,6 +537,8 @@ class _Allocating:
 # bytes takes a tenth of the time of filling the structure
 _LINEAR_ARGS = struct.Struct("@3q2iPqPqPPqPqPq")
 _LINEAR_GRAD_ARGS = struct.Struct("@3q2iPqPqPqPqPqPqP")
+_GROUPED_ARGS = struct.Struct("@3q3iPPqPqqPqPqPq")
+_GROUPED_GRAD_ARGS = struct.Struct("@3q3iPPqPqPqqPqPqPqqPq")
 
 
 def _call_with_workspace(name, packed, torch, device):
@@ -528,7 +563,7 @@ def _find_linear_calls(lib):
     """The C functions with untyped pointers, which ctypes passes bytes to."""
     global _linear_calls
     calls = {}
-    for n in ("pic_linear", "pic_linear_backward"):
+    for n in ("pic_linear", "pic_linear_backward", "pic_grouped_linear", "pic_grouped_linear_backward"):
         f = ctypes.CFUNCTYPE(ctypes.c_int, _P, _P, ctypes.c_size_t, _P)((n, lib))
         g = ctypes.CFUNCTYPE(ctypes.c_int64, _P)((n + "_workspace_bytes", lib))
         calls[n] = f, g
@@ -543,12 +578,12 @@ def _linear_act(act) -> int:
     return code
 
 
-def _refuse_recorded(**tensors):
+def _refuse_recorded(backward="linear_backward", **tensors):
     """Gradients that autograd would lose without a word."""
     for name, t in tensors.items():
         if t is not None and t.requires_grad:
             raise ValueError(f"{name}: requires a gradient, and autograd does not record this call: detach it, or "
-                             "call under torch.no_grad(), and take the gradients from linear_backward")
+                             f"call under torch.no_grad(), and take the gradients from {backward}")
 
 
 def linear(x, weight, bias=None, act="none", residual=None, out=None, save_pre=False, stream=None):
@@ -668,6 +703,163 @@ def linear_check(stream=None):
         raise PicError(rc, "pic_linear_check")
 
 
+def _matrices(t, name, shape, like, distinct=False):
+    """(pointer, row stride, group stride) of t as [groups][rows][cols] matrices of ``like``'s type and device."""
+    if t.dtype is not like.dtype or t.get_device() != like.get_device():
+        raise ValueError(f"{name}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    G, N, K = shape
+    if t.is_contiguous():
+        return t.data_ptr(), K, N * K
+    group, ld, one = t.stride()
+    ld = K if N == 1 else ld
+    if K > 1 and one != 1 or ld < K or G > 1 and group < (N - 1) * ld + K:
+        raise ValueError(f"{name}: rows must be contiguous, and rows and groups must not overlap")
+    return t.data_ptr(), ld, group
+
+
+def _vectors(t, name, shape, like):
+    """(pointer, stride) of t as [groups][n] vectors of ``like``'s type and device."""
+    if t.dtype is not like.dtype or t.get_device() != like.get_device() or t.shape != shape:
+        raise ValueError(f"{name}: must be a {list(shape)} tensor of {like.dtype} on {like.device}")
+    G, n = shape
+    if n > 1 and t.stride(1) != 1 or G > 1 and t.stride(0) < n:
+        raise ValueError(f"{name}: rows must be contiguous and must not overlap")
+    return t.data_ptr(), n if G == 1 else t.stride(0)
+
+
+MAX_GROUPS = 1024
+
+
+def _grouped(weight, offsets, like):
+    """(groups, out, in) of a grouped layer, and its offsets' pointer."""
+    if weight.dim() != 3 or 0 in weight.shape:
+        raise ValueError("weight: must be 3-D and not empty")
+    G, N, K = weight.shape
+    if G > MAX_GROUPS:
+        raise ValueError(f"weight: {G} groups, at most {MAX_GROUPS}")
+    if (str(offsets.dtype) != "torch.int64" or offsets.get_device() != like.get_device() or offsets.shape != (G + 1,)
+            or not offsets.is_contiguous()):
+        raise ValueError(f"offsets: must be a contiguous int64 tensor [{G + 1}] on {like.device}")
+    return G, N, K, offsets.data_ptr()
+
+
+def _two_dim(t, name, cols, like, rows=None):
+    if t.dim() != 2:
+        raise ValueError(f"{name}: must be 2-D")
+    return _rows(t, name, cols, like, rows)
+
+
+def grouped_linear(x, weight, offsets, bias=None, act="none", out=None, save_pre=False, stream=None):
+    """Linear layers of several nets at once: for the rows i of group g, which
+    are offsets[g] <= i < offsets[g + 1],
+
+        y[i] = act(x[i] @ weight[g].T + bias[g])
+
+    x is [rows, in], its rows sorted by group (contiguous, or further apart than
+    their width), weight [groups, out, in] and bias [groups, out] (slices of
+    larger buffers will do), offsets int64 [groups + 1] on the device, which do
+    not decrease and lie in [0, rows].  act and types as for ``linear``.
+    Returns y, or (y, z) with save_pre.  Rows of no group, before offsets[0]
+    and from offsets[-1] on, are not written.  Offsets are read when the
+    kernels run; ``grouped_linear_check`` reports ones that were not as they
+    must be.  Enqueued on the stream, not synchronised.
+
+    torch's autograd does not record the call; gradients come from
+    ``grouped_linear_backward``."""
+    if stream is not None:
+        with _Allocating(stream):
+            return grouped_linear(x, weight, offsets, bias, act, out, save_pre)
+    import torch
+    if ((x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad
+         or out is not None and out.requires_grad) and torch.is_grad_enabled()):
+        _refuse_recorded("grouped_linear_backward", x=x, weight=weight, bias=bias, out=out)
+    _on_device(x, "x")
+    G, N, K, po = _grouped(weight, offsets, x)
+    act_code, device = _linear_act(act), x.device
+    px, ldx = _two_dim(x, "x", K, x)
+    M = x.shape[0]
+    pw, ldw, gw = _matrices(weight, "weight", (G, N, K), x)
+    pb, gb = (0, N) if bias is None else _vectors(bias, "bias", (G, N), x)
+    if out is None:
+        out = torch.empty((M, N), dtype=x.dtype, device=device)
+    py, ldy = _two_dim(out, "out", N, x, M)
+    pre, pp = None, 0
+    if save_pre:
+        pre = torch.empty((M, N), dtype=x.dtype, device=device)
+        pp = pre.data_ptr()
+    _call_with_workspace("pic_grouped_linear",
+                         _GROUPED_ARGS.pack(M, K, N, G, _dtype_code(x, "x"), act_code, po, px, ldx, pw, ldw, gw,
+                                            pb, gb, py, ldy, pp, N), torch, device)
+    return (out, pre) if save_pre else out
+
+
+def grouped_linear_backward(dy, x, weight, offsets, act="none", pre=None, need=("x", "weight", "bias"), dx=None,
+                            dweight=None, dbias=None, stream=None):
+    """The gradients (dx, dweight, dbias) of ``grouped_linear`` for the output
+    gradient dy [rows, out]; those not named in ``need`` are None.  pre is what
+    ``grouped_linear`` returned with save_pre (not read with act "none"; with
+    "relu" y itself will do).  Groups without rows have gradients of zero; rows
+    of dx that belong to no group are not written.  The gradients are new
+    tensors, or are written to those given.  Enqueued on the stream."""
+    if stream is not None:
+        with _Allocating(stream):
+            return grouped_linear_backward(dy, x, weight, offsets, act, pre, need, dx, dweight, dbias)
+    import torch
+    _on_device(dy, "dy")
+    need = tuple(need)
+    if not need or not _GRADIENTS.issuperset(need):
+        raise ValueError('need: must name some of "x", "weight" and "bias"')
+    G, N, K, po = _grouped(weight, offsets, dy)
+    act_code, dtype, device = _linear_act(act), dy.dtype, dy.device
+    pdy, lddy = _two_dim(dy, "dy", N, dy)
+    M = dy.shape[0]
+    px, ldx = _two_dim(x, "x", K, dy, M)
+    pw, ldw, gw = _matrices(weight, "weight", (G, N, K), dy)
+    pz = ldz = 0
+    if act_code != PIC_ACT_NONE:
+        if pre is None:
+            raise ValueError(f"pre: needed for act {act!r}")
+        pz, ldz = _two_dim(pre, "pre", N, dy, M)
+    pdx = pdw = pdb = 0
+    lddx = lddw = K
+    gdw, gdb = N * K, N
+    if "x" not in need:
+        dx = None
+    else:
+        if dx is None:
+            dx = torch.empty((M, K), dtype=dtype, device=device)
+        pdx, lddx = _two_dim(dx, "dx", K, dy, M)
+    if "weight" not in need:
+        dweight = None
+    else:
+        if dweight is None:
+            dweight = torch.empty((G, N, K), dtype=dtype, device=device)
+        pdw, lddw, gdw = _matrices(dweight, "dweight", (G, N, K), dy)
+    if "bias" not in need:
+        dbias = None
+    else:
+        if dbias is None:
+            dbias = torch.empty((G, N), dtype=dtype, device=device)
+        pdb, gdb = _vectors(dbias, "dbias", (G, N), dy)
+    if M > 0 or pdw or pdb:
+        _call_with_workspace("pic_grouped_linear_backward",
+                             _GROUPED_GRAD_ARGS.pack(M, K, N, G, _dtype_code(dy, "dy"), act_code, po, pdy, lddy, px, ldx,
+                                                     pw, ldw, gw, pz, ldz, pdx, lddx, pdw, lddw, gdw, pdb, gdb),
+                             torch, device)
+    return dx, dweight, dbias
+
+
+def grouped_linear_check(stream=None):
+    """Synchronises the stream; raises if since the last check offsets of a
+    grouped call decreased or left [0, rows], or a bounded device-side wait of
+    the linear layer's kernels gave up."""
+    rc = load_library().pic_grouped_linear_check(_stream_ptr(stream))
+    if rc != PIC_OK:
+        raise PicError(rc, "pic_grouped_linear_check")
+
+
 class GradClip:
     """The global norm of a fixed list of gradient tensors, and their clipping:
     in place, or to the tensors of ``out`` (same sizes and types).  The handle
@@ -724,6 +916,84 @@ class GradClip:
     def close(self):
         if self.handle:
             load_library().pic_clip_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Orthogonalizer:
+    """Orthogonalised updates for a fixed list of matrices: each is replaced by
+    (or ``out``'s tensor of the same shape and type gets) what Newton-Schulz
+    products make of it, its singular vectors with singular values of about
+    one.  A tensor is [rows, cols], or [n, rows, cols] for n matrices, float32,
+    float16 or bfloat16, with contiguous rows, on the current device.  The
+    handle keeps the tensors, and has room for what is held between products."""
+
+    def __init__(self, tensors, out=None):
+        import torch
+        self.handle = None
+        tensors = list(tensors)
+        outs = tensors if out is None else list(out)
+        if len(outs) != len(tensors):
+            raise ValueError(f"out: {len(outs)} tensors, expected {len(tensors)}")
+        entries = []
+        for i, (t, o) in enumerate(zip(tensors, outs)):
+            for name, v in ((f"tensors[{i}]", t), (f"out[{i}]", o)):
+                _on_device(v, name)
+                if v.dim() not in (2, 3):
+                    raise ValueError(f"{name}: must be 2-D or 3-D")
+            if o.dtype != t.dtype or o.shape != t.shape:
+                raise ValueError(f"out[{i}]: {tuple(o.shape)} of {o.dtype}, expected {tuple(t.shape)} of {t.dtype}")
+            code = _dtype_code(t, f"tensors[{i}]")
+            if t.numel() == 0:
+                continue
+            shape = t.shape if t.dim() == 3 else (1, *t.shape)
+            pt, ldt, gt = _matrices(t.unsqueeze(0) if t.dim() == 2 else t, f"tensors[{i}]", shape, t)
+            po, ldo, go = _matrices(o.unsqueeze(0) if o.dim() == 2 else o, f"out[{i}]", shape, t)
+            size = t.element_size()
+            entries += [(pt + g * gt * size, po + g * go * size, shape[1], shape[2], ldt, ldo, code)
+                        for g in range(shape[0])]
+        table = (pic_orth_matrix * max(len(entries), 1))()
+        for i, e in enumerate(entries):
+            table[i] = pic_orth_matrix(*e)
+        self._tensors, self._outs = tensors, outs
+        self.device = torch.cuda.current_device()
+        h = _P()
+        rc = load_library().pic_orth_create(table, len(entries), ctypes.byref(h))
+        if rc != PIC_OK:
+            raise PicError(rc, "pic_orth_create")
+        self.handle = h.value
+        self._call = load_library().pic_orth
+
+    def orthogonalize(self, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, stream=None):
+        """X = G / (|G| + eps), then ``steps`` times, with A = X X^T (the
+        smaller of X X^T and X^T X),
+
+            X = a X + (b A + c A^2) X
+
+        and X to the out tensors.  Enqueued on the stream; calls with one handle
+        must not overlap on the GPU."""
+        if self.handle is None:
+            raise ValueError("Orthogonalizer: closed")
+        a, b, c = coefficients
+        rc = self._call(self.handle, steps, a, b, c, eps, _stream_ptr(stream))
+        if rc != PIC_OK:
+            raise PicError(rc, "pic_orth")
+
+    def check(self, stream=None):
+        """Synchronises the stream; raises if a bounded device-side wait of this
+        handle's calls gave up since the last check."""
+        rc = load_library().pic_orth_check(self.handle, _stream_ptr(stream))
+        if rc != PIC_OK:
+            raise PicError(rc, "pic_orth_check")
+
+    def close(self):
+        if self.handle:
+            load_library().pic_orth_destroy(self.handle)
             self.handle = None
 
     def __del__(self):
