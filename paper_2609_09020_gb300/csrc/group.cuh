@@ -122,20 +122,32 @@ struct GroupProduct {
 };
 int any_product(const GroupProduct& p, int dtype, cudaStream_t s);
 
-// db_g = sum of dy act'(z) over each group's rows.
-struct GroupSums {
+// On the tensor cores: 16-bit types, a as it is (no a_pre).
+constexpr long long kTcMostK = 16384;  // of K that one accumulator sums up
+bool tc_takes(const GroupProduct& p, int dtype);
+long long tc_workspace(const GroupProduct& p, int dtype);
+int tc_product(const GroupProduct& p, int dtype, void* ws, const Waits& waits, cudaStream_t s);
+
+// dz[i][j] = dy act'(pre), rounded (dz null: not written; its rows are on 16-byte
+// boundaries and written to the next one), and db_g, the sums of the unrounded dz over
+// each group's rows (db null: none).
+struct GroupGradAct {
   const void* dy;
   long long lddy;
   const void* pre;
   long long ldpre;
+  void* dz;
+  long long lddz;
   void* db;
   long long db_group;
+  float* parts;
   long long rows, J;
   int groups, act;
   const long long* offsets;
   int* status;
 };
-int any_sums(const GroupSums& g, int dtype, cudaStream_t s);
+long long grad_act_workspace(const GroupGradAct& g, int dtype);
+int grad_act(const GroupGradAct& g, int dtype, cudaStream_t s);
 
 }  // namespace grp
 }  // namespace pic

@@ -80,34 +80,6 @@ __global__ void __launch_bounds__(kThreads) any_kernel(const GroupProduct p) {
   }
 }
 
-// A block takes 32 columns of a group: 32 runs of its rows side by side.
-template <typename T>
-__global__ void __launch_bounds__(1024) sums_kernel(const GroupSums q) {
-  constexpr bool EXACT = sizeof(T) == 4;
-  __shared__ GroupTable table;
-  __shared__ float sums[32][33];
-  make_table(table, q.offsets, q.groups, q.rows, 1, 0, q.status);
-  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-  const long long blocks_j = (q.J + 31) / 32;
-  for (long long w = blockIdx.x; w < blocks_j * q.groups; w += gridDim.x) {
-    const int g = static_cast<int>(w / blocks_j);
-    const long long j = w % blocks_j * 32 + tx;
-    float sum = 0.0f;
-    if (j < q.J)
-      for (long long r = table.start[g] + ty; r < table.start[g + 1]; r += 32) {
-        const float d = to_f32(static_cast<const T*>(q.dy)[r * q.lddy + j]);
-        sum += q.act == PIC_ACT_NONE ? d : act_grad<EXACT>(d, to_f32(static_cast<const T*>(q.pre)[r * q.ldpre + j]), q.act);
-      }
-    sums[ty][tx] = sum;
-    __syncthreads();
-    if (ty == 0 && j < q.J) {
-      for (int r = 1; r < 32; ++r) sum += sums[r][tx];
-      static_cast<T*>(q.db)[g * q.db_group + j] = from_f32<T>(sum);
-    }
-    __syncthreads();
-  }
-}
-
 template <typename T>
 int run(const GroupProduct& p, cudaStream_t s) {
   const long long tiles_j = (p.J + kTile - 1) / kTile, tiles_i = (p.I + kTile - 1) / kTile;
@@ -120,25 +92,12 @@ int run(const GroupProduct& p, cudaStream_t s) {
   return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
 }
 
-template <typename T>
-int run(const GroupSums& g, cudaStream_t s) {
-  const long long most = (g.J + 31) / 32 * g.groups;
-  sums_kernel<T><<<static_cast<unsigned>(most < 2 * kSms ? most : 2 * kSms), 1024, 0, s>>>(g);
-  return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
-}
-
 }  // namespace
 
 int any_product(const GroupProduct& p, int dtype, cudaStream_t s) {
   if (dtype == PIC_DTYPE_F32) return run<float>(p, s);
   if (dtype == PIC_DTYPE_F16) return run<__half>(p, s);
   return run<__nv_bfloat16>(p, s);
-}
-
-int any_sums(const GroupSums& g, int dtype, cudaStream_t s) {
-  if (dtype == PIC_DTYPE_F32) return run<float>(g, s);
-  if (dtype == PIC_DTYPE_F16) return run<__half>(g, s);
-  return run<__nv_bfloat16>(g, s);
 }
 
 }  // namespace grp

@@ -818,9 +818,13 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
 // A [rows][cols] matrix in boxes of 128 bytes of columns and box_rows rows,
 // 128-byte swizzled; false if the driver will not make the map.
 bool encode(CUtensorMap* map, const void* m, long long rows, long long cols, long long ld, int box_rows, int dtype);
+// `count` [rows][cols] matrices, `group` elements apart, in boxes of 128 bytes of columns
+// and box_rows rows of one of them.
+bool encode_many(CUtensorMap* map, const void* m, long long rows, long long cols, long long ld, long long count,
+                 long long group, int box_rows, int dtype);
 // Allows a kernel `smem` bytes of shared memory, once per device; each kernel of
 // these files has a slot of its own below kSmemSlots.
-constexpr int kSmemSlots = 26;
+constexpr int kSmemSlots = 64;
 int allow_smem(const void* fn, int slot, int smem);
 
 // The kernel for tiles of bn columns: 64 and 128 by one CTA, 256 by a pair.

@@ -5,7 +5,7 @@
 namespace {
 
 using pic::grp::GroupProduct;
-using pic::grp::GroupSums;
+using pic::grp::GroupGradAct;
 
 constexpr long long kMaxDim = 0x7fffffffLL - 256;
 
@@ -56,8 +56,15 @@ bool args_ok(const pic_grouped_linear_grad_args* a) {
 
 const long long* offsets_of(const int64_t* o) { return reinterpret_cast<const long long*>(o); }
 
-int forward(const pic_grouped_linear_args& a, pic::lin::Arena&, bool launch, const pic::lin::Waits& w, cudaStream_t s) {
-  if (a.rows == 0 || !launch) return PIC_OK;
+long long product_workspace(const GroupProduct& p, int dtype) {
+  return pic::grp::tc_takes(p, dtype) ? pic::grp::tc_workspace(p, dtype) : 0;
+}
+int product(const GroupProduct& p, int dtype, void* ws, const pic::lin::Waits& w, cudaStream_t s) {
+  return pic::grp::tc_takes(p, dtype) ? pic::grp::tc_product(p, dtype, ws, w, s) : pic::grp::any_product(p, dtype, s);
+}
+
+int forward(const pic_grouped_linear_args& a, pic::lin::Arena& ws, bool launch, const pic::lin::Waits& w, cudaStream_t s) {
+  if (a.rows == 0) return PIC_OK;
   GroupProduct p{};
   p.by_rows = true;
   p.a = a.x, p.a_i = a.ldx;
@@ -67,38 +74,49 @@ int forward(const pic_grouped_linear_args& a, pic::lin::Arena&, bool launch, con
   p.bias = a.bias, p.bias_group = a.bias_group;
   p.y = a.y, p.ldy = a.ldy, p.pre = a.pre, p.ldpre = a.ldpre, p.act = a.act;
   p.status = w.status;
-  return pic::grp::any_product(p, a.dtype, s);
+  void* room = ws.take(product_workspace(p, a.dtype));
+  return launch ? product(p, a.dtype, room, w, s) : PIC_OK;
 }
 
-int backward(const pic_grouped_linear_grad_args& a, pic::lin::Arena&, bool launch, const pic::lin::Waits& w, cudaStream_t s) {
-  if (!launch) return PIC_OK;
+int backward(const pic_grouped_linear_grad_args& a, pic::lin::Arena& ws, bool launch, const pic::lin::Waits& w, cudaStream_t s) {
+  const long long M = a.rows, K = a.in_features, N = a.out_features;
   int rc = PIC_OK;
+  // dz: dy itself where there is no activation
+  const void* dz = a.dy;
+  long long lddz = a.lddy;
+  const bool own_dz = a.act != PIC_ACT_NONE && (a.dx || a.dw);
+  if (own_dz) {
+    lddz = (N + 63) / 64 * 64;  // rows of 16-bit values on 128-byte lines
+    dz = ws.take(M * lddz * static_cast<long long>(elem_bytes(a.dtype)));
+  }
+  if ((own_dz && M > 0) || a.db) {
+    GroupGradAct g{a.dy, a.lddy, a.pre, a.ldpre, own_dz ? const_cast<void*>(dz) : nullptr, lddz, a.db, a.db_group, nullptr,
+                   M, N, a.groups, a.act, offsets_of(a.offsets), w.status};
+    g.parts = static_cast<float*>(ws.take(pic::grp::grad_act_workspace(g, a.dtype)));
+    if (launch && (rc = pic::grp::grad_act(g, a.dtype, s)) != PIC_OK) return rc;
+  }
   GroupProduct p{};
-  p.a = a.dy, p.a_i = a.lddy;
-  if (a.act != PIC_ACT_NONE) p.a_pre = a.pre, p.a_pre_i = a.ldpre, p.a_act = a.act;
-  p.rows = a.rows, p.groups = a.groups, p.offsets = offsets_of(a.offsets);
+  p.a = dz, p.a_i = lddz;
+  p.rows = M, p.groups = a.groups, p.offsets = offsets_of(a.offsets);
   p.act = PIC_ACT_NONE;
   p.status = w.status;
-  if (a.dx && a.rows > 0) {
+  if (a.dx && M > 0) {
     p.by_rows = true;
     p.b = a.w, p.b_group = a.w_group, p.b_j = 1, p.b_k = a.ldw;
-    p.J = a.in_features, p.K = a.out_features;
+    p.J = K, p.K = N;
     p.y = a.dx, p.ldy = a.lddx;
-    if ((rc = pic::grp::any_product(p, a.dtype, s)) != PIC_OK) return rc;
+    void* room = ws.take(product_workspace(p, a.dtype));
+    if (launch && (rc = product(p, a.dtype, room, w, s)) != PIC_OK) return rc;
   }
   if (a.dw) {
     p.by_rows = false;
-    p.b = a.x, p.b_j = 1, p.b_k = a.ldx;
-    p.I = a.out_features, p.J = a.in_features;
+    p.b = a.x, p.b_group = 0, p.b_j = 1, p.b_k = a.ldx;
+    p.I = N, p.J = K, p.K = 0;
     p.y = a.dw, p.ldy = a.lddw, p.y_group = a.dw_group;
-    if ((rc = pic::grp::any_product(p, a.dtype, s)) != PIC_OK) return rc;
+    void* room = ws.take(product_workspace(p, a.dtype));
+    if (launch && (rc = product(p, a.dtype, room, w, s)) != PIC_OK) return rc;
   }
-  if (a.db) {
-    const GroupSums g{a.dy, a.lddy, a.pre, a.ldpre, a.db, a.db_group, a.rows, a.out_features,
-                      a.groups, a.act, offsets_of(a.offsets), w.status};
-    rc = pic::grp::any_sums(g, a.dtype, s);
-  }
-  return rc;
+  return PIC_OK;
 }
 
 template <typename Args, typename F>
