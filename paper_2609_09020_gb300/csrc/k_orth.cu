@@ -1,21 +1,30 @@
-// k_orth.cu -- orthogonalised updates (include/pic_orth.h): the handle, the norms,
-// and the products on the FP32 cores.
+// k_orth.cu -- orthogonalised updates (include/pic_orth.h): the handle with its
+// lists of jobs, and the norms.
 #include <algorithm>
 #include <cmath>
 #include <new>
 #include <vector>
 
+#include "k_linear_tc.cuh"
 #include "orth.cuh"
+
+// Tile shapes, by columns.
+constexpr int kShapes = 3;
+constexpr int kShapeColumns[kShapes] = {64, 128, 256};
 
 struct pic_orthogonalizer {
   int device;
-  int n_pieces, n_square, n_full;
+  int n_pieces;
   char* room;  // all of it
   pic::orth::Matrix* matrices;
+  CUtensorMap* maps;
   pic::orth::Piece* pieces;
-  pic::orth::Tile* square;  // tiles of A and b A + c A^2
-  pic::orth::Tile* full;    // tiles of X
-  double* parts;
+  pic::orth::Job* jobs[3][kShapes];  // of each stage
+  int n_jobs[3][kShapes];
+  double* squares;
+  float4* parts;
+  unsigned* counters;
+  long long n_counters;
   int* status;
 };
 
@@ -27,7 +36,6 @@ using pic::lin::to_f32;
 
 constexpr int kThreads = 256;
 constexpr int kPiece = 16384;  // elements
-constexpr int kTile = 64, kDeep = 16;
 
 template <typename F>
 __device__ __forceinline__ void for_type(int dtype, F f) {
@@ -104,78 +112,16 @@ __global__ void __launch_bounds__(kThreads) scale_kernel(const Matrix* matrices,
     for (int e = threadIdx.x; e < p.rows * p.cols; e += kThreads) {
       const long long r = p.row0 + e / p.cols, c = p.col0 + e % p.cols;
       const float v = to_f32(g[r * m.ld_grad + c]) * f0 * f1;
-      if (last)
+      if (last) {
         out[r * m.ld_out + c] = from_f32<T>(v);
-      else
-        m.x[0][r * m.ldx + c] = v;
-    }
-  });
-}
-
-// Tile (i, j) of a product: STAGE 0 A = X X^T (or X^T X), 1 B = b A + c A A, 2 X' = a X +
-// B X (or X B).  `last`: X' goes to out.
-template <int STAGE>
-__global__ void __launch_bounds__(kThreads) product_kernel(const Matrix* matrices, const Tile* tiles, Coefficients co,
-                                                           int from, int last) {
-  __shared__ __align__(16) float sa[kDeep][kTile + 4], sb[kDeep][kTile + 4];
-  const Tile t = tiles[blockIdx.x];
-  const Matrix& m = matrices[t.matrix];
-  const float* x = m.x[from];
-  const float *pa, *pb;
-  long long ai, ak, bj, bk;
-  int I, J, K;
-  if (STAGE == 0) {
-    pa = pb = x, I = J = m.m, K = m.left ? m.cols : m.rows;
-    ai = bj = m.left ? m.ldx : 1, ak = bk = m.left ? 1 : m.ldx;
-  } else if (STAGE == 1) {
-    pa = pb = m.a, I = J = K = m.m;
-    ai = bj = m.lda, ak = bk = 1;
-  } else {
-    I = m.rows, J = m.cols, K = m.m;
-    pa = m.left ? m.b : x, ai = m.left ? m.lda : m.ldx, ak = 1;
-    pb = m.left ? x : m.b, bj = m.left ? 1 : m.lda, bk = m.left ? m.ldx : 1;
-  }
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const long long i0 = t.i * kTile, j0 = t.j * kTile;
-  float acc[4][4] = {};
-  for (int k0 = 0; k0 < K; k0 += kDeep) {
-    for (int e = threadIdx.x; e < kTile * kDeep; e += kThreads) {
-      const int ka = ak == 1 ? e % kDeep : e / kTile, ia = ak == 1 ? e / kDeep : e % kTile;
-      sa[ka][ia] = i0 + ia < I && k0 + ka < K ? pa[(i0 + ia) * ai + (k0 + ka) * ak] : 0.0f;
-      const int kb = bk == 1 ? e % kDeep : e / kTile, jb = bk == 1 ? e / kDeep : e % kTile;
-      sb[kb][jb] = j0 + jb < J && k0 + kb < K ? pb[(j0 + jb) * bj + (k0 + kb) * bk] : 0.0f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kDeep; ++k) {
-      const float4 u = *reinterpret_cast<const float4*>(&sa[k][4 * ty]), v = *reinterpret_cast<const float4*>(&sb[k][4 * tx]);
-      const float p[4] = {u.x, u.y, u.z, u.w}, q[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) acc[r][c] = fmaf(p[r], q[c], acc[r][c]);
-    }
-    __syncthreads();
-  }
-  for (int r = 0; r < 4; ++r)
-    for (int c = 0; c < 4; ++c) {
-      const long long i = i0 + 4 * ty + r, j = j0 + 4 * tx + c;
-      if (i >= I || j >= J) continue;
-      if (STAGE == 0) {
-        m.a[i * m.lda + j] = acc[r][c];
-      } else if (STAGE == 1) {
-        m.b[i * m.lda + j] = co.b * m.a[i * m.lda + j] + co.c * acc[r][c];
       } else {
-        const float v = co.a * x[i * m.ldx + j] + acc[r][c];
-        if (last)
-          for_type(m.dtype, [&](auto t) {
-            using T = decltype(t);
-            static_cast<T*>(m.out)[i * m.ld_out + j] = from_f32<T>(v);
-          });
-        else
-          m.x[from ^ 1][i * m.ldx + j] = v;
+        const float x = v * kScale;
+        const __half hi = __float2half_rn(x);
+        m.x[0][r * m.ldx + c] = hi;
+        m.x[0][m.rows * m.ldx + r * m.ldx + c] = __float2half_rn(x - __half2float(hi));
       }
     }
+  });
 }
 
 long long elem_bytes(int dtype) { return dtype == PIC_DTYPE_F32 ? 4 : 2; }
@@ -246,6 +192,78 @@ bool steps_ok(int steps, double a, double b, double c) {
   return true;
 }
 
+// The jobs of each stage and tile shape, the workspace of their parts and its counters.
+//
+// Shapes: 256 columns by pairs of CTAs, with a third of the time for as many
+// operations, where the list has such tiles for most of the pairs; 64 where the
+// smaller side is no more; else 128.
+//
+// Parts: stages with fewer tiles than there are CTAs (kSlots) are cut along K, with at
+// least kLeast slices in a part; and sums of more than kMost slices, in which a tensor
+// core's truncations would show (it loses up to 2^-24 of a sum with each 16 of K).
+void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kShapes], long long& part_bytes,
+               long long& counters) {
+  constexpr int kSms = 152, kSlots[kShapes] = {2 * kSms, kSms, kSms / 2}, kLeast = 2, kMost[2] = {256, 64};
+  const auto blocks = [](long long n, long long of) { return (n + of - 1) / of; };
+  long long large = 0;
+  for (const Matrix& m : table)
+    if (m.m > 512) large += blocks(m.rows, 256) * blocks(m.cols, 256);
+  for (int s = 0; s < 3; ++s) {
+    long long tiles[kShapes] = {};
+    std::vector<Job> plain[kShapes];
+    for (size_t id = 0; id < table.size(); ++id) {
+      const Matrix& m = table[id];
+      const int shape = m.m <= 64 ? 0 : m.m > 512 && large >= 60 ? 2 : 1;
+      const int bn = kShapeColumns[shape], rows = shape == 2 ? 256 : 128;
+      Job j{};
+      j.matrix = static_cast<int>(id), j.halves = m.halves, j.parts = 1;
+      long long I = m.m, J = m.m, K = m.m;
+      if (s == kGram) {
+        j.p_map = j.q_map = kMapX, j.p_mn = j.q_mn = !m.left, K = m.left ? m.cols : m.rows;
+      } else if (s == kPolynomial) {
+        j.p_map = j.q_map = kMapA;
+      } else {
+        I = m.rows, J = m.cols;
+        j.p_map = m.left ? kMapB : kMapX, j.q_map = m.left ? kMapX : kMapB;
+        j.q_mn = m.left;
+      }
+      j.k1 = static_cast<int>(blocks(K, 64));
+      // some rows of tiles at a time, columns outermost among them, so that what they share stays in L2
+      const long long ti = blocks(I, rows), tj = blocks(J, bn), group = 2048 / rows;
+      for (long long g = 0; g < ti; g += group)
+        for (long long c = 0; c < tj; ++c)
+          for (long long r = g; r < std::min(ti, g + group); ++r) {
+            if (s != kUpdate && c * bn >= (r + 1) * rows) continue;  // above the diagonal
+            j.i = static_cast<int>(r * rows), j.j = static_cast<int>(c * bn);
+            j.mirror = s != kUpdate && (c + 1) * bn <= r * rows;
+            plain[shape].push_back(j);
+          }
+    }
+    for (int shape = 0; shape < kShapes; ++shape) {
+      tiles[shape] = static_cast<long long>(plain[shape].size());
+      const long long fill = tiles[shape] ? kSlots[shape] / tiles[shape] : 1;
+      const int cg = shape == 2 ? 2 : 1, panels = cg * (kShapeColumns[shape] / 64) * 4;
+      int slot = 0;
+      for (const Job& j : plain[shape]) {
+        const int slices = j.k1, most = kMost[j.halves - 1];
+        long long parts = std::max<long long>(std::min<long long>(fill, slices / kLeast), blocks(slices, most));
+        parts = std::max<long long>(parts, 1);
+        const int each = static_cast<int>(blocks(slices, parts));
+        parts = blocks(slices, each);
+        for (int p = 0; p < parts; ++p) {
+          Job k = j;
+          k.k0 = p * each, k.k1 = std::min(slices, k.k0 + each);
+          k.part = p, k.parts = static_cast<int>(parts), k.slot = slot;
+          jobs[s][shape].push_back(k);
+        }
+        if (parts > 1) slot += static_cast<int>(parts);
+      }
+      part_bytes = std::max(part_bytes, static_cast<long long>(slot) * panels * 512 * 16);
+      counters = std::max(counters, static_cast<long long>(slot) * panels);
+    }
+  }
+}
+
 }  // namespace
 
 extern "C" {
@@ -274,7 +292,6 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
     if (rc != PIC_OK) return rc;
     std::vector<Matrix> table;
     std::vector<Piece> pieces;
-    std::vector<Tile> square, full;
     long long bytes = 0;
     const auto take = [&](long long b) {
       const long long at = bytes;
@@ -288,7 +305,8 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
       t.grad = m.grad, t.out = m.out, t.ld_grad = m.ld_grad, t.ld_out = m.ld_out;
       t.rows = static_cast<int>(m.rows), t.cols = static_cast<int>(m.cols), t.dtype = m.dtype;
       t.m = std::min(t.rows, t.cols), t.left = t.rows <= t.cols;
-      t.ldx = (m.cols + 7) / 8 * 8, t.lda = (t.m + 7) / 8 * 8;
+      t.halves = m.dtype == PIC_DTYPE_BF16 ? 1 : 2;
+      t.ldx = (m.cols + 63) / 64 * 64, t.lda = (t.m + 63) / 64 * 64;  // whole panels
       t.part0 = static_cast<int>(pieces.size());
       const int cols = std::min(t.cols, kPiece), rows = kPiece / cols;
       for (long long r = 0; r < t.rows; r += rows)
@@ -296,40 +314,57 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
           pieces.push_back({id, static_cast<int>(r), static_cast<int>(std::min<long long>(rows, t.rows - r)),
                             static_cast<int>(c), static_cast<int>(std::min<long long>(cols, t.cols - c))});
       t.parts = static_cast<int>(pieces.size()) - t.part0;
-      for (int i = 0; i * kTile < t.m; ++i)
-        for (int j = 0; j * kTile < t.m; ++j) square.push_back({id, i, j});
-      for (int i = 0; i * static_cast<long long>(kTile) < t.rows; ++i)
-        for (int j = 0; j * static_cast<long long>(kTile) < t.cols; ++j) full.push_back({id, i, j});
-      for (int i = 0; i < 2; ++i) at.push_back(take(t.rows * t.ldx * 4));
-      for (int i = 0; i < 2; ++i) at.push_back(take(t.m * t.lda * 4));
+      for (int i = 0; i < 2; ++i) at.push_back(take(2 * t.rows * t.ldx * 2));
+      for (int i = 0; i < 2; ++i) at.push_back(take(t.halves * t.m * t.lda * 2));
       table.push_back(t);
     }
-    const long long at_matrices = take(table.size() * sizeof(Matrix)), at_pieces = take(pieces.size() * sizeof(Piece)),
-                    at_square = take(square.size() * sizeof(Tile)), at_full = take(full.size() * sizeof(Tile)),
-                    at_parts = take(pieces.size() * sizeof(double)), at_status = take(4);
+    std::vector<Job> jobs[3][kShapes];
+    long long part_bytes = 0, counters = 0;
+    make_jobs(table, jobs, part_bytes, counters);
+    const long long at_matrices = take(table.size() * sizeof(Matrix)), at_maps = take(table.size() * kMaps * sizeof(CUtensorMap)),
+                    at_pieces = take(pieces.size() * sizeof(Piece)), at_squares = take(pieces.size() * sizeof(double)),
+                    at_parts = take(part_bytes), at_counters = take(counters * 4), at_status = take(4);
+    long long at_jobs[3][kShapes];
+    for (int s = 0; s < 3; ++s)
+      for (int c = 0; c < kShapes; ++c) at_jobs[s][c] = take(jobs[s][c].size() * sizeof(Job));
     h = new pic_orthogonalizer{};
     if (cudaGetDevice(&h->device) != cudaSuccess || cudaMalloc(&h->room, bytes) != cudaSuccess) {
       cudaGetLastError();
       pic_orth_destroy(h);
       return PIC_ERR_ALLOC;
     }
+    std::vector<CUtensorMap> maps(table.size() * kMaps);
+    bool ok = true;
     for (size_t i = 0; i < table.size(); ++i) {
-      float** p[4] = {&table[i].x[0], &table[i].x[1], &table[i].a, &table[i].b};
-      for (int k = 0; k < 4; ++k) *p[k] = reinterpret_cast<float*>(h->room + at[4 * i + k]);
+      Matrix& t = table[i];
+      __half** p[4] = {&t.x[0], &t.x[1], &t.a, &t.b};
+      for (int k = 0; k < 4; ++k) {
+        *p[k] = reinterpret_cast<__half*>(h->room + at[4 * i + k]);
+        const bool x = k < 2;
+        const long long rows = x ? t.rows : t.m, cols = x ? t.cols : t.m, ld = x ? t.ldx : t.lda;
+        ok = ok && pic::lin::encode_many(&maps[i * kMaps + k], *p[k], rows, cols, ld, x ? 2 : t.halves, rows * ld, 64, PIC_DTYPE_F16);
+      }
     }
     h->matrices = reinterpret_cast<Matrix*>(h->room + at_matrices);
+    h->maps = reinterpret_cast<CUtensorMap*>(h->room + at_maps);
     h->pieces = reinterpret_cast<Piece*>(h->room + at_pieces);
-    h->square = reinterpret_cast<Tile*>(h->room + at_square);
-    h->full = reinterpret_cast<Tile*>(h->room + at_full);
-    h->parts = reinterpret_cast<double*>(h->room + at_parts);
+    h->squares = reinterpret_cast<double*>(h->room + at_squares);
+    h->parts = reinterpret_cast<float4*>(h->room + at_parts);
+    h->counters = reinterpret_cast<unsigned*>(h->room + at_counters);
+    h->n_counters = counters;
     h->status = reinterpret_cast<int*>(h->room + at_status);
     h->n_pieces = static_cast<int>(pieces.size());
-    h->n_square = static_cast<int>(square.size());
-    h->n_full = static_cast<int>(full.size());
     const auto put = [](void* to, const auto& v) {
       return v.empty() || cudaMemcpy(to, v.data(), v.size() * sizeof(v[0]), cudaMemcpyHostToDevice) == cudaSuccess;
     };
-    if (!put(h->matrices, table) || !put(h->pieces, pieces) || !put(h->square, square) || !put(h->full, full) ||
+    ok = ok && put(h->matrices, table) && put(h->maps, maps) && put(h->pieces, pieces);
+    for (int s = 0; s < 3; ++s)
+      for (int c = 0; c < kShapes; ++c) {
+        h->jobs[s][c] = reinterpret_cast<Job*>(h->room + at_jobs[s][c]);
+        h->n_jobs[s][c] = static_cast<int>(jobs[s][c].size());
+        ok = ok && put(h->jobs[s][c], jobs[s][c]);
+      }
+    if (!ok || (counters && cudaMemset(h->counters, 0, counters * 4) != cudaSuccess) ||
         cudaMemset(h->status, 0, 4) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
       cudaGetLastError();
       pic_orth_destroy(h);
@@ -357,16 +392,22 @@ int pic_orth(pic_orthogonalizer* h, int steps, float a, float b, float c, float 
   if (dev != h->device) return PIC_ERR_INVALID_ARG;
   if (h->n_pieces == 0) return PIC_OK;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const Coefficients co{a, b, c, eps};
-  squares_kernel<<<h->n_pieces, kThreads, 0, s>>>(h->matrices, h->pieces, h->parts);
-  scale_kernel<<<h->n_pieces, kThreads, 0, s>>>(h->matrices, h->pieces, h->parts, eps, steps == 0);
-  for (int k = 0; k < steps; ++k) {
-    product_kernel<0><<<h->n_square, kThreads, 0, s>>>(h->matrices, h->square, co, k & 1, 0);
-    product_kernel<1><<<h->n_square, kThreads, 0, s>>>(h->matrices, h->square, co, k & 1, 0);
-    product_kernel<2><<<h->n_full, kThreads, 0, s>>>(h->matrices, h->full, co, k & 1, k + 1 == steps);
-  }
-  if (cudaGetLastError() != cudaSuccess) return PIC_ERR_CUDA;
-  return PIC_OK;
+  pic::lin::Waits waits;
+  if (!pic::lin::call_waits(waits)) return PIC_ERR_CUDA;
+  waits.status = h->status;
+  squares_kernel<<<h->n_pieces, kThreads, 0, s>>>(h->matrices, h->pieces, h->squares);
+  scale_kernel<<<h->n_pieces, kThreads, 0, s>>>(h->matrices, h->pieces, h->squares, eps, steps == 0);
+  for (int k = 0; k < steps; ++k)
+    for (const Stage stage : {kGram, kPolynomial, kUpdate})
+      for (int shape = 0; shape < kShapes; ++shape) {
+        const StageParams q{h->matrices, h->maps, h->jobs[stage][shape], h->n_jobs[stage][shape], {a, b, c}, k & 1,
+                            k + 1 == steps, h->parts, h->counters, waits};
+        if (launch_stage(stage, kShapeColumns[shape], q, s) != PIC_OK) {
+          cudaGetLastError();
+          return PIC_ERR_CUDA;
+        }
+      }
+  return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
 }
 
 int pic_orth_check(pic_orthogonalizer* h, void* stream) {
@@ -375,7 +416,10 @@ int pic_orth_check(pic_orthogonalizer* h, void* stream) {
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (cudaMemcpyAsync(&flag, h->status, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess ||
       cudaStreamSynchronize(s) != cudaSuccess ||
-      (flag && (cudaMemsetAsync(h->status, 0, sizeof(int), s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess))) {
+      // parts that never came have left their counters where they were
+      (flag && (cudaMemsetAsync(h->status, 0, sizeof(int), s) != cudaSuccess ||
+                (h->n_counters && cudaMemsetAsync(h->counters, 0, h->n_counters * 4, s) != cudaSuccess) ||
+                cudaStreamSynchronize(s) != cudaSuccess))) {
     cudaGetLastError();
     return PIC_ERR_CUDA;
   }

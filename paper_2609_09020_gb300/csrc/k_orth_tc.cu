@@ -1,0 +1,383 @@
+// k_orth_tc.cu -- the products of orthogonalised updates on the tensor cores,
+// organised as k_linear_tc.cuh's (a ring of stages filled by TMA, one thread that
+// issues the MMAs, two sets of accumulators in tensor memory, the epilogue in the other
+// warps): all matrices of a list in one launch, each with tensor maps of its own.
+//
+// Operands are halves of kScale v.  Where values are held in two, a product is three
+// products of halves, the two small ones first: lo hi, hi lo, hi hi.  Each is a run
+// along K of its own in the same accumulators (their operands are loaded three times:
+// the loads keep up with the MMAs at 256 columns).
+//
+// A = X X^T and A^2 are symmetric: tiles on and below the diagonal are computed, and
+// those below it written twice.  A product with few tiles is cut along K: each part's
+// sums go to the workspace, and the warp that is the last to bring its part of a panel
+// adds all parts of it in order and finishes it, so that the result does not depend on
+// which is last.
+#include "k_linear_tc.cuh"
+#include "orth.cuh"
+
+namespace pic {
+namespace orth {
+namespace {
+
+using lin::kSlice;
+
+template <int CG, int BN>
+struct Shape {
+  static constexpr int kABytes = 128 * 128, kBRows = BN / CG, kBBytes = kBRows * 128;
+  static constexpr int kStageBytes = kABytes + kBBytes;
+  static constexpr int kCtas = BN == 64 ? 2 : 1;
+  static constexpr int kStages = BN == 64 ? 3 : 5;
+  static constexpr int kEpi = BN == 64 ? 4 : 8;
+  static constexpr int kThreads = 64 + 32 * kEpi;
+  static constexpr int kColumns = BN == 64 ? 64 : BN / 2;
+  static constexpr int kOffPanels = kStages * kStageBytes;
+  static constexpr int kOffBars = (kOffPanels + kEpi * lin::kTurnBytes + 15) / 16 * 16;
+  static constexpr int kBars = 2 * kStages + 4 + 1;
+  static constexpr int kSmem = kOffBars + kBars * 8 + 16 + 1024;  // 1024: the base is rounded up
+  static constexpr int kTmemCols = 2 * BN;
+};
+
+template <bool PAIR>
+__device__ __forceinline__ void load_3d(uint32_t dst, const void* tmap, int x, int y, int z, uint32_t bar) {
+  if constexpr (PAIR)
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
+        "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
+
+// 64 values of a lane's row as halves, hi and (lo not null) lo, in 16-byte stores.
+__device__ __forceinline__ void put_halves(const float (&v)[64], __half* hi, __half* lo) {
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float x = v[8 * c + 2 * e], y = v[8 * c + 2 * e + 1];
+      h[e] = lin::pack2_of<__half>(x, y);
+      const float2 f = lin::unpack2_of<__half>(h[e]);
+      l[e] = lin::pack2_of<__half>(x - f.x, y - f.y);
+    }
+    reinterpret_cast<uint4*>(hi)[c] = make_uint4(h[0], h[1], h[2], h[3]);
+    if (lo) reinterpret_cast<uint4*>(lo)[c] = make_uint4(l[0], l[1], l[2], l[3]);
+  }
+}
+// v += f times the 64 values that are held as hi and (lo not null) lo.
+__device__ __forceinline__ void add_halves(float (&v)[64], float f, const __half* hi, const __half* lo) {
+  uint4 h[8], l[8];
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    h[c] = reinterpret_cast<const uint4*>(hi)[c];
+    l[c] = lo ? reinterpret_cast<const uint4*>(lo)[c] : make_uint4(0, 0, 0, 0);
+  }
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    const uint32_t a[4] = {h[c].x, h[c].y, h[c].z, h[c].w}, b[4] = {l[c].x, l[c].y, l[c].z, l[c].w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 p = lin::unpack2_of<__half>(a[e]), q = lin::unpack2_of<__half>(b[e]);
+      v[8 * c + 2 * e] = fmaf(f, p.x + q.x, v[8 * c + 2 * e]);
+      v[8 * c + 2 * e + 1] = fmaf(f, p.y + q.y, v[8 * c + 2 * e + 1]);
+    }
+  }
+}
+// The transposed panel: columns become rows, and neighbouring lanes neighbours.
+__device__ __forceinline__ void put_mirrored(const float (&v)[64], __half* hi, __half* lo, long long ld, int cols) {
+#pragma unroll
+  for (int c = 0; c < 64; ++c) {
+    if (c >= cols) break;
+    const __half h = __float2half_rn(v[c]);
+    hi[c * ld] = h;
+    if (lo) lo[c * ld] = __float2half_rn(v[c] - __half2float(h));
+  }
+}
+
+// 32 rows x 64 columns of sums to a matrix of type T, turned in shared memory so that a
+// row's columns leave together.
+template <typename T>
+__device__ __forceinline__ void put_out(const float (&v)[64], float* turn, int lane, T* out, long long ld, int rows, int cols) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (32 * h >= cols) break;
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 32; ++c) turn[lane * lin::kTurnStride + c] = v[32 * h + c];
+    __syncwarp();
+    if (32 * h + lane < cols) {
+      T* o = out + 32 * h + lane;
+#pragma unroll 8
+      for (int r = 0; r < rows; ++r) o[r * ld] = lin::from_f32<T>(turn[r * lin::kTurnStride + lane]);
+    }
+  }
+}
+
+template <Stage STAGE, int CG, int BN>
+__global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
+    stage_kernel(const __grid_constant__ StageParams q) {
+  using S = Shape<CG, BN>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = tc::smem_addr(smem_raw);
+  uint8_t* smem = smem_raw + ((1024 - (raw & 1023)) & 1023);
+  const uint32_t base = tc::smem_addr(smem);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = CG == 2 ? tc::cluster_rank() : 0;
+  const uint32_t bars = base + S::kOffBars;
+  const uint32_t bar_full = bars, bar_empty = bars + 8 * S::kStages, bar_acc = bar_empty + 8 * S::kStages,
+                 bar_free = bar_acc + 16, bar_drain = bar_free + 16;
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + S::kOffBars + 8 * S::kBars);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::kOffBars + 8 * S::kBars + 4);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S::kStages; ++s) {
+      tc::mbar_init(bar_full + 8 * s, 1);
+      tc::mbar_init(bar_empty + 8 * s, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      tc::mbar_init(bar_acc + 8 * b, 1);
+      tc::mbar_init(bar_free + 8 * b, S::kEpi * CG);
+    }
+    tc::mbar_init(bar_drain, 1);
+    *abort_flag = 0;
+    tc::fence_mbar_init();
+  }
+  if (warp == 1) tc::tmem_alloc_cg<CG>(tc::smem_addr(tmem_slot), S::kTmemCols);
+  tc::tc_fence_before();
+  __syncthreads();
+  if constexpr (CG == 2) tc::cluster_sync();
+  tc::tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  auto wait = [&](uint32_t bar, uint32_t parity) { return lin::wait_bounded(bar, parity, abort_flag, q.waits); };
+  const int first = blockIdx.x / CG, step = gridDim.x / CG;
+
+  int s = 0;
+  uint32_t phase = 0;
+  bool ok = true;
+  if (warp == 0) {
+    if (tc::elect_one()) {
+      const uint32_t lead_full = CG == 2 ? tc::map_rank(bar_full, 0) : bar_full;
+      const CUtensorMap* known[2] = {nullptr, nullptr};
+      for (int w = first; w < q.n && ok; w += step) {
+        const Job& job = q.jobs[w];
+        const int i0 = job.i + rank * 128, j0 = job.j + rank * S::kBRows;
+        const CUtensorMap* maps = q.maps + static_cast<long long>(job.matrix) * kMaps;
+        const auto map_of = [&](int which) { return maps + (which == kMapX ? q.from : which); };
+        const CUtensorMap *mp = map_of(job.p_map), *mq = map_of(job.q_map);
+        // (made on the host, and copied before the launch)
+        if (mp != known[0]) asm volatile("fence.proxy.tensormap::generic.acquire.sys [%0], 128;" ::"l"(mp) : "memory");
+        if (mq != known[1]) asm volatile("fence.proxy.tensormap::generic.acquire.sys [%0], 128;" ::"l"(mq) : "memory");
+        known[0] = mp, known[1] = mq;
+        const int k0 = job.k0, k1 = job.k1, p_mn = job.p_mn, q_mn = job.q_mn;
+        for (int term = job.halves == 2 ? 0 : 2; term < 3 && ok; ++term) {
+          const int zp = term == 0, zq = term == 1;
+          for (int kb = k0; kb < k1; ++kb) {
+            if (!(ok = wait(bar_empty + 8 * s, phase ^ 1))) break;
+            if (rank == 0) tc::mbar_arrive_expect_tx(bar_full + 8 * s, CG * S::kStageBytes);
+            const uint32_t sa = base + s * S::kStageBytes, sb = sa + S::kABytes, bar = lead_full + 8 * s;
+            const int k = kb * kSlice;
+            // boxes of 64 x 64 either way
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              if (p_mn)
+                load_3d<CG == 2>(sa + c * 8192, mp, i0 + 64 * c, k, zp, bar);
+              else
+                load_3d<CG == 2>(sa + c * 8192, mp, k, i0 + 64 * c, zp, bar);
+            }
+#pragma unroll
+            for (int c = 0; c < S::kBRows / 64; ++c) {
+              if (q_mn)
+                load_3d<CG == 2>(sb + c * 8192, mq, j0 + 64 * c, k, zq, bar);
+              else
+                load_3d<CG == 2>(sb + c * 8192, mq, k, j0 + 64 * c, zq, bar);
+            }
+            if (++s == S::kStages) s = 0, phase ^= 1;
+          }
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (rank == 0 && tc::elect_one()) {
+      int buf = 0;
+      uint32_t free_phase = 0;
+      for (int w = first; w < q.n && ok; w += step) {
+        const Job& job = q.jobs[w];
+        const int slices = (job.k1 - job.k0) * (job.halves == 2 ? 3 : 1), p_mn = job.p_mn, q_mn = job.q_mn;
+        const uint32_t idesc = tc::idesc_16(128 * CG, BN, false, p_mn != 0, q_mn != 0);
+        // one MMA takes 16 of K: 32 bytes of a K-major row, 16 rows of an MN-major block
+        const uint32_t a_step = p_mn ? 2048 : 32, b_step = q_mn ? 2048 : 32;
+        if (!(ok = wait(bar_free + 8 * buf, free_phase ^ 1))) break;
+        tc::tc_fence_after();
+        const uint32_t d = tmem + buf * BN;
+        for (int kb = 0; kb < slices; ++kb) {
+          if (!(ok = wait(bar_full + 8 * s, phase))) break;
+          tc::tc_fence_after();
+          const uint32_t sa = base + s * S::kStageBytes, sb = sa + S::kABytes;
+#pragma unroll
+          for (int kk = 0; kk < kSlice / 16; ++kk)
+            tc::mma_16<CG>(d, tc::smem_desc_sw128(sa + kk * a_step, 8192, 1024),
+                           tc::smem_desc_sw128(sb + kk * b_step, 8192, 1024), idesc, (kb > 0 || kk > 0) ? 1u : 0u);
+          tc::mma_commit_cg<CG>(bar_empty + 8 * s);
+          if (++s == S::kStages) s = 0, phase ^= 1;
+        }
+        if (!ok) break;
+        tc::mma_commit_cg<CG>(bar_acc + 8 * buf);
+        if (++buf == 2) buf = 0, free_phase ^= 1;
+      }
+    }
+    __syncwarp();
+  } else {
+    const int quarter = warp & 3;  // the 32 lanes of tensor memory that this warp may read
+    const int from = (warp - 2) / 4 * S::kColumns, to = from + S::kColumns;
+    float* turn = reinterpret_cast<float*>(smem + S::kOffPanels + (warp - 2) * lin::kTurnBytes);
+    const uint32_t lead_free = CG == 2 ? tc::map_rank(bar_free, 0) : bar_free;
+    int buf = 0;
+    for (int w = first; w < q.n; w += step) {
+      const Job& job = q.jobs[w];
+      const Matrix& m = q.matrices[job.matrix];
+      const int I = STAGE == kUpdate ? m.rows : m.m, J = STAGE == kUpdate ? m.cols : m.m;
+      const int row0 = job.i + rank * 128 + quarter * 32, row = row0 + lane, parts = job.parts;
+      if (!__all_sync(0xffffffffu, wait(bar_acc + 8 * buf, phase))) break;
+      tc::tc_fence_after();
+      const uint32_t d = tmem + buf * BN + (static_cast<uint32_t>(quarter * 32) << 16);
+      for (int c0 = from; c0 < to; c0 += 64) {
+        float v[64];
+        {
+          uint32_t acc[64];
+          tc::tmem_ld64_wait(d + c0, acc);
+#pragma unroll
+          for (int c = 0; c < 64; ++c) v[c] = __uint_as_float(acc[c]);
+        }
+        if (c0 + 64 == to) {
+          tc::tc_fence_before();
+          __syncwarp();
+          if (lane == 0 && !(q.waits.test_fault && w == 0 && rank == 0 && quarter == 0)) {
+            if constexpr (CG == 2)
+              tc::mbar_arrive_cluster(lead_free + 8 * buf);
+            else
+              tc::mbar_arrive(bar_free + 8 * buf);
+          }
+        }
+        const int col0 = job.j + c0, cols = min(64, J - col0);
+        if (row0 >= I || cols <= 0) continue;  // nothing of this panel is inside
+        if (parts > 1) {
+          // [part][rank][panel][quarter][16][32 lanes][4 columns]
+          constexpr int kPanels = CG * (BN / 64) * 4;  // warps' panels of a tile
+          const int panel = (rank * (BN / 64) + c0 / 64) * 4 + quarter;
+          float4* mine = q.parts + (static_cast<long long>(job.slot + job.part) * kPanels + panel) * 512 + lane;
+#pragma unroll
+          for (int c = 0; c < 16; ++c) __stcg(mine + c * 32, make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]));
+          __threadfence();
+          __syncwarp();
+          unsigned* counter = q.counters + static_cast<long long>(job.slot) * kPanels + panel;
+          unsigned before = 0;
+          if (lane == 0) before = atomicAdd(counter, 1);
+          before = __shfl_sync(0xffffffffu, before, 0);
+          if (before + 1 < static_cast<unsigned>(parts)) continue;  // others bring theirs later
+          __threadfence();
+          if (lane == 0) *counter = 0;  // for the next launch
+          const float4* all = q.parts + (static_cast<long long>(job.slot) * kPanels + panel) * 512 + lane;
+#pragma unroll
+          for (int c = 0; c < 64; ++c) v[c] = 0.0f;
+          for (int p = 0; p < parts; ++p, all += kPanels * 512) {
+#pragma unroll
+            for (int c = 0; c < 16; ++c) {
+              const float4 f = __ldcg(all + c * 32);
+              v[4 * c] += f.x, v[4 * c + 1] += f.y, v[4 * c + 2] += f.z, v[4 * c + 3] += f.w;
+            }
+          }
+        }
+        const bool two = m.halves == 2;
+        if constexpr (STAGE == kGram) {
+#pragma unroll
+          for (int c = 0; c < 64; ++c) v[c] *= 1.0f / kScale;
+        } else {
+          const float f = (STAGE == kPolynomial ? q.co.c : 1.0f) / kScale;
+#pragma unroll
+          for (int c = 0; c < 64; ++c) v[c] *= f;
+          const __half* from_m = STAGE == kPolynomial ? m.a : m.x[q.from];
+          const long long ld = STAGE == kPolynomial ? m.lda : m.ldx;
+          const __half* hi = from_m + row * ld + col0;
+          if (row < I) add_halves(v, STAGE == kPolynomial ? q.co.b : q.co.a, hi, STAGE == kUpdate || two ? hi + I * ld : nullptr);
+        }
+        if (STAGE == kUpdate && q.last) {
+#pragma unroll
+          for (int c = 0; c < 64; ++c) v[c] *= 1.0f / kScale;
+          const int rows = min(32, I - row0);
+          const long long at = row0 * m.ld_out + col0;
+          if (m.dtype == PIC_DTYPE_F32)
+            put_out(v, turn, lane, static_cast<float*>(m.out) + at, m.ld_out, rows, cols);
+          else if (m.dtype == PIC_DTYPE_F16)
+            put_out(v, turn, lane, static_cast<__half*>(m.out) + at, m.ld_out, rows, cols);
+          else
+            put_out(v, turn, lane, static_cast<__nv_bfloat16*>(m.out) + at, m.ld_out, rows, cols);
+        } else if (row < I) {
+          __half* to_m = STAGE == kGram ? m.a : STAGE == kPolynomial ? m.b : m.x[q.from ^ 1];
+          const long long ld = STAGE == kUpdate ? m.ldx : m.lda;
+          const bool lo = STAGE == kUpdate || two;
+          // rows of the workspace are whole panels
+          __half* hi = to_m + row * ld + col0;
+          put_halves(v, hi, lo ? hi + I * ld : nullptr);
+          if (STAGE != kUpdate && job.mirror) {
+            __half* turned = to_m + col0 * ld + row;
+            put_mirrored(v, turned, lo ? turned + I * ld : nullptr, ld, cols);
+          }
+        }
+      }
+      if (++buf == 2) buf = 0, phase ^= 1;
+    }
+    __syncwarp();
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {
+    // the copies and MMAs in flight use shared and tensor memory.  The other CTA of a
+    // pair may have started copies that this one did not expect: it lingers for far
+    // longer than a copy takes.
+    if (warp == 0 && rank == 0 && tc::elect_one()) lin::drain_loads(bar_full, S::kStages, s, phase, q.waits);
+    if (warp == 1 && rank == 0 && tc::elect_one()) lin::drain_mmas<CG>(bar_drain, q.waits);
+    if (CG == 2) __nanosleep(200000);
+    __syncthreads();
+  }
+  if constexpr (CG == 2) tc::cluster_sync();
+  tc::tc_fence_after();
+  if (warp == 1) tc::tmem_dealloc_cg<CG>(tmem, S::kTmemCols);
+}
+
+template <Stage STAGE, int CG, int BN>
+int launch(const StageParams& q, int slot, cudaStream_t s) {
+  using S = Shape<CG, BN>;
+  static_assert((S::kSmem + 1024) * S::kCtas <= 228 * 1024, "shared memory of an SM");
+  const void* fn = reinterpret_cast<const void*>(stage_kernel<STAGE, CG, BN>);
+  if (lin::allow_smem(fn, slot, S::kSmem) != PIC_OK) return PIC_ERR_CUDA;
+  const long long want = static_cast<long long>(q.n) * CG, most = 152 * S::kCtas;
+  void* args[] = {const_cast<StageParams*>(&q)};
+  return lin::launch_kernel(fn, want < most ? want : most, S::kThreads, S::kSmem, CG, args, s);
+}
+
+template <Stage STAGE>
+int launch_bn(int bn, const StageParams& q, cudaStream_t s) {
+  if (bn == 64) return launch<STAGE, 1, 64>(q, 44 + STAGE, s);
+  if (bn == 128) return launch<STAGE, 1, 128>(q, 47 + STAGE, s);
+  return launch<STAGE, 2, 256>(q, 50 + STAGE, s);
+}
+
+}  // namespace
+
+int launch_stage(Stage stage, int bn, const StageParams& q, cudaStream_t s) {
+  if (q.n == 0) return PIC_OK;
+  if (stage == kGram) return launch_bn<kGram>(bn, q, s);
+  if (stage == kPolynomial) return launch_bn<kPolynomial>(bn, q, s);
+  return launch_bn<kUpdate>(bn, q, s);
+}
+
+}  // namespace orth
+}  // namespace pic
