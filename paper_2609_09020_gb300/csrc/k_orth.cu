@@ -35,7 +35,6 @@ using pic::lin::from_f32;
 using pic::lin::to_f32;
 
 constexpr int kThreads = 256;
-constexpr int kPiece = 16384;  // elements
 
 template <typename F>
 __device__ __forceinline__ void for_type(int dtype, F f) {
@@ -47,28 +46,61 @@ __device__ __forceinline__ void for_type(int dtype, F f) {
     f(__nv_bfloat16{});
 }
 
+// A thread's elements of a panel of 32 x 64 of a piece: eight columns of a row, zeros
+// where there are none.
+template <typename T, bool ON16>
+__device__ __forceinline__ void load8(const Matrix& m, int row, int col, float (&v)[8]) {
+  constexpr int kBytes = static_cast<int>(sizeof(T));
+  const char* at = reinterpret_cast<const char*>(static_cast<const T*>(m.grad) + row * m.ld_grad + col);
+  const int bytes = row < m.rows ? (m.cols - col) * kBytes : 0;
+#pragma unroll
+  for (int h = 0; h < kBytes / 2; ++h) {
+    pic::lin::Piece16<ON16> p;
+    p.load(at + 16 * h, bytes - 16 * h);
+    uint32_t w[4];
+    p.template get<T>(static_cast<int>(reinterpret_cast<uintptr_t>(at) & 15), w);
+    pic::lin::keep_bytes<T>(w, bytes - 16 * h);
+#pragma unroll
+    for (int e = 0; e < 16 / kBytes; ++e) v[h * (16 / kBytes) + e] = to_f32(reinterpret_cast<const T*>(w)[e]);
+  }
+}
+template <typename F>
+__device__ __forceinline__ void for_form(const Matrix& m, F f) {
+  for_type(m.dtype, [&](auto t) {
+    using T = decltype(t);
+    if (m.on16)
+      f(t, [&](int row, int col, float (&v)[8]) { load8<T, true>(m, row, col, v); });
+    else
+      f(t, [&](int row, int col, float (&v)[8]) { load8<T, false>(m, row, col, v); });
+  });
+}
+
 // The squares of a piece: a thread adds at most 64 in fp32, and where that sum leaves the
 // range in which fp32 is good, again in fp64; the block's threads in order.
-__global__ void __launch_bounds__(kThreads) squares_kernel(const Matrix* matrices, const Piece* pieces, double* parts) {
+__global__ void __launch_bounds__(kThreads) squares_kernel(const Matrix* matrices, const Piece* pieces, double* squares) {
   __shared__ double sums[kThreads / 32];
   const Piece p = pieces[blockIdx.x];
   const Matrix& m = matrices[p.matrix];
+  const int row = p.row0 + threadIdx.x / 8, col = p.col0 + threadIdx.x % 8 * 8, end = min(m.cols, p.col0 + kPieceCols);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   double sum = 0.0;
-  for_type(m.dtype, [&](auto t) {
-    using T = decltype(t);
-    const T* g = static_cast<const T*>(m.grad) + p.row0 * m.ld_grad + p.col0;
-    const int count = p.rows * p.cols;
+  for_form(m, [&](auto, auto load) {
     float s = 0.0f;
-    for (int e = threadIdx.x; e < count; e += kThreads) {
-      const float v = to_f32(g[e / p.cols * m.ld_grad + e % p.cols]);
-      s = fmaf(v, v, s);
+#pragma unroll 4
+    for (int c = col; c < end; c += 64) {
+      float v[8];
+      load(row, c, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = fmaf(v[e], v[e], s);
     }
     sum = s;
     if (!(s >= 1e-28f && s <= 1e37f)) {
       sum = 0.0;
-      for (int e = threadIdx.x; e < count; e += kThreads) {
-        const double v = to_f32(g[e / p.cols * m.ld_grad + e % p.cols]);
-        sum = fma(v, v, sum);
+      for (int c = col; c < end; c += 64) {
+        float v[8];
+        load(row, c, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = fma(static_cast<double>(v[e]), static_cast<double>(v[e]), sum);
       }
     }
   });
@@ -78,48 +110,72 @@ __global__ void __launch_bounds__(kThreads) squares_kernel(const Matrix* matrice
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int w = 1; w < kThreads / 32; ++w) sum += sums[w];
-    parts[blockIdx.x] = sum;
+    squares[blockIdx.x] = sum;
   }
 }
 
 // X = G / (|G| + eps), a piece a block: by a power of two first, then by what is left, so
 // that no finite norm leaves fp32's range on the way.
-__global__ void __launch_bounds__(kThreads) scale_kernel(const Matrix* matrices, const Piece* pieces, const double* parts,
+__global__ void __launch_bounds__(kThreads) scale_kernel(const Matrix* matrices, const Piece* pieces, const double* squares,
                                                          float eps, int last) {
   __shared__ float factors[2];
+  __shared__ double sums[kThreads / 32];
   const Piece p = pieces[blockIdx.x];
   const Matrix& m = matrices[p.matrix];
-  if (threadIdx.x < 32) {
-    double sum = 0.0;
-    for (int i = threadIdx.x; i < m.parts; i += 32) sum += parts[m.part0 + i];
+  wait_for_earlier();
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < m.parts; i += kThreads) sum += squares[m.part0 + i];
 #pragma unroll
-    for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    if (threadIdx.x == 0) {
-      const double norm = sqrt(sum) + eps;
-      int e = 0;
-      if (norm > 0.0 && norm < 1e300) frexp(norm, &e);
-      e = min(max(e, -126), 126);
-      factors[0] = static_cast<float>(ldexp(1.0, -e));
-      factors[1] = static_cast<float>(ldexp(1.0, e) / norm);
-    }
+  for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kThreads / 32; ++w) sum += sums[w];
+    const double norm = sqrt(sum) + eps;
+    int e = 0;
+    if (norm > 0.0 && norm < 1e300) frexp(norm, &e);
+    e = min(max(e, -126), 126);
+    factors[0] = static_cast<float>(ldexp(1.0, -e));
+    factors[1] = static_cast<float>(ldexp(1.0, e) / norm);
   }
   __syncthreads();
-  const float f0 = factors[0], f1 = factors[1];
-  for_type(m.dtype, [&](auto t) {
+  const float f0 = factors[0], f1 = factors[1] * (last ? 1.0f : kScale);
+  const int r = threadIdx.x / 8, row = p.row0 + r, col = p.col0 + threadIdx.x % 8 * 8, end = min(m.cols, p.col0 + kPieceCols);
+  for_form(m, [&](auto t, auto load) {
     using T = decltype(t);
-    const T* g = static_cast<const T*>(m.grad);
-    T* out = static_cast<T*>(m.out);
-    for (int e = threadIdx.x; e < p.rows * p.cols; e += kThreads) {
-      const long long r = p.row0 + e / p.cols, c = p.col0 + e % p.cols;
-      const float v = to_f32(g[r * m.ld_grad + c]) * f0 * f1;
+#pragma unroll 2
+    for (int c = col; c < end; c += 64) {
+      float v[8];
+      load(row, c, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = v[e] * f0 * f1;
       if (last) {
-        out[r * m.ld_out + c] = from_f32<T>(v);
-      } else {
-        const float x = v * kScale;
-        const __half hi = __float2half_rn(x);
-        m.x[0][r * m.ldx + c] = hi;
-        m.x[0][m.rows * m.ldx + r * m.ldx + c] = __float2half_rn(x - __half2float(hi));
+        if (row < m.rows) {
+          T* out = static_cast<T*>(m.out) + row * m.ld_out + c;
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (c + e < m.cols) out[e] = from_f32<T>(v[e]);
+        }
+        continue;
       }
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        hi[e] = pic::lin::pack2_of<__half>(v[2 * e], v[2 * e + 1]);
+        const float2 h = pic::lin::unpack2_of<__half>(hi[e]);
+        lo[e] = pic::lin::pack2_of<__half>(v[2 * e] - h.x, v[2 * e + 1] - h.y);
+        const float2 l = pic::lin::unpack2_of<__half>(lo[e]);
+        v[2 * e] = h.x + l.x, v[2 * e + 1] = h.y + l.y;
+      }
+      // rows of the workspace, and panels, are whole
+      if (row < m.rows) {
+        __half* x = m.x[0] + row * m.ldx + c;
+        *reinterpret_cast<uint4*>(x) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        if (m.halves == 2) *reinterpret_cast<uint4*>(x + m.rows * m.ldx) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      }
+      float4* own = m.own_x + (p.row0 / 32 * (m.ldx / 64) + c / 64) * 512 + c % 64 / 4 * 32 + r;
+      own[0] = make_float4(v[0], v[1], v[2], v[3]);
+      own[32] = make_float4(v[4], v[5], v[6], v[7]);
     }
   });
 }
@@ -221,11 +277,11 @@ void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kSh
       if (s == kGram) {
         j.p_map = j.q_map = kMapX, j.p_mn = j.q_mn = !m.left, K = m.left ? m.cols : m.rows;
       } else if (s == kPolynomial) {
-        j.p_map = j.q_map = kMapA;
+        j.p_map = j.q_map = kMapA, j.p_half = j.q_half = 1;
       } else {
         I = m.rows, J = m.cols;
         j.p_map = m.left ? kMapB : kMapX, j.q_map = m.left ? kMapX : kMapB;
-        j.q_mn = m.left;
+        j.q_mn = m.left, j.p_half = m.left, j.q_half = !m.left;
       }
       j.k1 = static_cast<int>(blocks(K, 64));
       // some rows of tiles at a time, columns outermost among them, so that what they share stays in L2
@@ -235,11 +291,14 @@ void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kSh
           for (long long r = g; r < std::min(ti, g + group); ++r) {
             if (s != kUpdate && c * bn >= (r + 1) * rows) continue;  // above the diagonal
             j.i = static_cast<int>(r * rows), j.j = static_cast<int>(c * bn);
-            j.mirror = s != kUpdate && (c + 1) * bn <= r * rows;
             plain[shape].push_back(j);
           }
     }
     for (int shape = 0; shape < kShapes; ++shape) {
+      // long ones first
+      std::stable_sort(plain[shape].begin(), plain[shape].end(), [](const Job& a, const Job& b) {
+        return a.k1 * (a.halves == 2 ? 3 : 1) > b.k1 * (b.halves == 2 ? 3 : 1);
+      });
       tiles[shape] = static_cast<long long>(plain[shape].size());
       const long long fill = tiles[shape] ? kSlots[shape] / tiles[shape] : 1;
       const int cg = shape == 2 ? 2 : 1, panels = cg * (kShapeColumns[shape] / 64) * 4;
@@ -308,14 +367,14 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
       t.halves = m.dtype == PIC_DTYPE_BF16 ? 1 : 2;
       t.ldx = (m.cols + 63) / 64 * 64, t.lda = (t.m + 63) / 64 * 64;  // whole panels
       t.part0 = static_cast<int>(pieces.size());
-      const int cols = std::min(t.cols, kPiece), rows = kPiece / cols;
-      for (long long r = 0; r < t.rows; r += rows)
-        for (long long c = 0; c < t.cols; c += cols)
-          pieces.push_back({id, static_cast<int>(r), static_cast<int>(std::min<long long>(rows, t.rows - r)),
-                            static_cast<int>(c), static_cast<int>(std::min<long long>(cols, t.cols - c))});
+      for (long long r = 0; r < t.rows; r += 32)
+        for (long long c = 0; c < t.cols; c += kPieceCols) pieces.push_back({id, static_cast<int>(r), static_cast<int>(c)});
       t.parts = static_cast<int>(pieces.size()) - t.part0;
-      for (int i = 0; i < 2; ++i) at.push_back(take(2 * t.rows * t.ldx * 2));
+      t.on16 = reinterpret_cast<uintptr_t>(m.grad) % 16 == 0 && m.ld_grad * elem_bytes(m.dtype) % 16 == 0;
+      for (int i = 0; i < 2; ++i) at.push_back(take(t.halves * t.rows * t.ldx * 2));
       for (int i = 0; i < 2; ++i) at.push_back(take(t.halves * t.m * t.lda * 2));
+      at.push_back(take((t.rows + 31) / 32 * (t.ldx / 64) * 512 * 16));
+      at.push_back(take((t.m + 31) / 32 * (t.lda / 64) * 512 * 16));
       table.push_back(t);
     }
     std::vector<Job> jobs[3][kShapes];
@@ -339,11 +398,14 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
       Matrix& t = table[i];
       __half** p[4] = {&t.x[0], &t.x[1], &t.a, &t.b};
       for (int k = 0; k < 4; ++k) {
-        *p[k] = reinterpret_cast<__half*>(h->room + at[4 * i + k]);
+        *p[k] = reinterpret_cast<__half*>(h->room + at[6 * i + k]);
         const bool x = k < 2;
         const long long rows = x ? t.rows : t.m, cols = x ? t.cols : t.m, ld = x ? t.ldx : t.lda;
-        ok = ok && pic::lin::encode_many(&maps[i * kMaps + k], *p[k], rows, cols, ld, x ? 2 : t.halves, rows * ld, 64, PIC_DTYPE_F16);
+        ok = ok && pic::lin::encode_many(&maps[i * kMaps + k], *p[k], rows, cols, ld, t.halves, rows * ld, 64, PIC_DTYPE_F16) &&
+             pic::lin::encode_many(&maps[i * kMaps + kMapStore + k], *p[k], rows, cols, ld, t.halves, rows * ld, 32, PIC_DTYPE_F16);
       }
+      t.own_x = reinterpret_cast<float4*>(h->room + at[6 * i + 4]);
+      t.own_a = reinterpret_cast<float4*>(h->room + at[6 * i + 5]);
     }
     h->matrices = reinterpret_cast<Matrix*>(h->room + at_matrices);
     h->maps = reinterpret_cast<CUtensorMap*>(h->room + at_maps);
@@ -396,7 +458,14 @@ int pic_orth(pic_orthogonalizer* h, int steps, float a, float b, float c, float 
   if (!pic::lin::call_waits(waits)) return PIC_ERR_CUDA;
   waits.status = h->status;
   squares_kernel<<<h->n_pieces, kThreads, 0, s>>>(h->matrices, h->pieces, h->squares);
-  scale_kernel<<<h->n_pieces, kThreads, 0, s>>>(h->matrices, h->pieces, h->squares, eps, steps == 0);
+  {
+    int last = steps == 0;
+    void* args[] = {&h->matrices, &h->pieces, &h->squares, &eps, &last};
+    if (launch_behind(reinterpret_cast<const void*>(scale_kernel), h->n_pieces, kThreads, 0, 1, args, s) != PIC_OK) {
+      cudaGetLastError();
+      return PIC_ERR_CUDA;
+    }
+  }
   for (int k = 0; k < steps; ++k)
     for (const Stage stage : {kGram, kPolynomial, kUpdate})
       for (int shape = 0; shape < kShapes; ++shape) {

@@ -8,8 +8,11 @@
 // along K of its own in the same accumulators (their operands are loaded three times:
 // the loads keep up with the MMAs at 256 columns).
 //
-// A = X X^T and A^2 are symmetric: tiles on and below the diagonal are computed, and
-// those below it written twice.  A product with few tiles is cut along K: each part's
+// A = X X^T and A^2 are symmetric: tiles on and below the diagonal are computed and
+// kept.  Where an operand's slice would lie above it, its mirror image is loaded, which
+// lies along the other dimension, and the MMA is told so.  (Tiles written twice, the second
+// time turned, and X read and written by rows took the update of four 2048 x 2048 and two
+// 2048 x 8192 matrices 200 us.)  A product with few tiles is cut along K: each part's
 // sums go to the workspace, and the warp that is the last to bring its part of a panel
 // adds all parts of it in order and finishes it, so that the result does not depend on
 // which is last.
@@ -32,7 +35,7 @@ struct Shape {
   static constexpr int kThreads = 64 + 32 * kEpi;
   static constexpr int kColumns = BN == 64 ? 64 : BN / 2;
   static constexpr int kOffPanels = kStages * kStageBytes;
-  static constexpr int kOffBars = (kOffPanels + kEpi * lin::kTurnBytes + 15) / 16 * 16;
+  static constexpr int kOffBars = kOffPanels + kEpi * lin::kPanelBytes;
   static constexpr int kBars = 2 * kStages + 4 + 1;
   static constexpr int kSmem = kOffBars + kBars * 8 + 16 + 1024;  // 1024: the base is rounded up
   static constexpr int kTmemCols = 2 * BN;
@@ -54,53 +57,26 @@ __device__ __forceinline__ void load_3d(uint32_t dst, const void* tmap, int x, i
         : "memory");
 }
 
-// 64 values of a lane's row as halves, hi and (lo not null) lo, in 16-byte stores.
-__device__ __forceinline__ void put_halves(const float (&v)[64], __half* hi, __half* lo) {
-#pragma unroll
-  for (int c = 0; c < 8; ++c) {
-    uint32_t h[4], l[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float x = v[8 * c + 2 * e], y = v[8 * c + 2 * e + 1];
-      h[e] = lin::pack2_of<__half>(x, y);
-      const float2 f = lin::unpack2_of<__half>(h[e]);
-      l[e] = lin::pack2_of<__half>(x - f.x, y - f.y);
-    }
-    reinterpret_cast<uint4*>(hi)[c] = make_uint4(h[0], h[1], h[2], h[3]);
-    if (lo) reinterpret_cast<uint4*>(lo)[c] = make_uint4(l[0], l[1], l[2], l[3]);
-  }
-}
-// v += f times the 64 values that are held as hi and (lo not null) lo.
-__device__ __forceinline__ void add_halves(float (&v)[64], float f, const __half* hi, const __half* lo) {
-  uint4 h[8], l[8];
-#pragma unroll
-  for (int c = 0; c < 8; ++c) {
-    h[c] = reinterpret_cast<const uint4*>(hi)[c];
-    l[c] = lo ? reinterpret_cast<const uint4*>(lo)[c] : make_uint4(0, 0, 0, 0);
-  }
-#pragma unroll
-  for (int c = 0; c < 8; ++c) {
-    const uint32_t a[4] = {h[c].x, h[c].y, h[c].z, h[c].w}, b[4] = {l[c].x, l[c].y, l[c].z, l[c].w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float2 p = lin::unpack2_of<__half>(a[e]), q = lin::unpack2_of<__half>(b[e]);
-      v[8 * c + 2 * e] = fmaf(f, p.x + q.x, v[8 * c + 2 * e]);
-      v[8 * c + 2 * e + 1] = fmaf(f, p.y + q.y, v[8 * c + 2 * e + 1]);
-    }
-  }
-}
-// The transposed panel: columns become rows, and neighbouring lanes neighbours.
-__device__ __forceinline__ void put_mirrored(const float (&v)[64], __half* hi, __half* lo, long long ld, int cols) {
-#pragma unroll
-  for (int c = 0; c < 64; ++c) {
-    if (c >= cols) break;
-    const __half h = __float2half_rn(v[c]);
-    hi[c * ld] = h;
-    if (lo) lo[c * ld] = __float2half_rn(v[c] - __half2float(h));
-  }
+__device__ __forceinline__ void store_3d(const void* tmap, int x, int y, int z, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(
+                   reinterpret_cast<uint64_t>(tmap)),
+               "r"(x), "r"(y), "r"(z), "r"(src)
+               : "memory");
 }
 
-// 32 rows x 64 columns of sums to a matrix of type T, turned in shared memory so that a
+// Before the use of a tensor map in global memory (made on the host, and copied there).
+__device__ __forceinline__ void acquire_map(const void* tmap) {
+  asm volatile("fence.proxy.tensormap::generic.acquire.sys [%0], 128;" ::"l"(reinterpret_cast<uint64_t>(tmap)) : "memory");
+}
+
+// A panel (32 rows, a lane's row in v, of 64 halves) to its buffer, as TMA takes it.
+__device__ __forceinline__ void fill_panel(const uint32_t (&v)[32], uint32_t buf, int lane) {
+#pragma unroll
+  for (int c = 0; c < 8; ++c)
+    tc::sts128(buf + lane * 128 + ((c ^ (lane & 7)) * 16), v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+}
+
+// 32 rows x 64 columns of sums to a matrix of type T, turned in the panel buffer so that a
 // row's columns leave together.
 template <typename T>
 __device__ __forceinline__ void put_out(const float (&v)[64], float* turn, int lane, T* out, long long ld, int rows, int cols) {
@@ -109,12 +85,12 @@ __device__ __forceinline__ void put_out(const float (&v)[64], float* turn, int l
     if (32 * h >= cols) break;
     __syncwarp();
 #pragma unroll
-    for (int c = 0; c < 32; ++c) turn[lane * lin::kTurnStride + c] = v[32 * h + c];
+    for (int c = 0; c < 32; ++c) turn[lane * 32 + (c ^ lane)] = v[32 * h + c];
     __syncwarp();
     if (32 * h + lane < cols) {
       T* o = out + 32 * h + lane;
 #pragma unroll 8
-      for (int r = 0; r < rows; ++r) o[r * ld] = lin::from_f32<T>(turn[r * lin::kTurnStride + lane]);
+      for (int r = 0; r < rows; ++r) o[r * ld] = lin::from_f32<T>(turn[r * 32 + (lane ^ r)]);
     }
   }
 }
@@ -154,7 +130,12 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
   if constexpr (CG == 2) tc::cluster_sync();
   tc::tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  wait_for_earlier();
 
+  // Whether slice k of an operand lies along i (j): by itself, or, of a symmetric matrix, as
+  // the mirror image of one above the diagonal.
+  constexpr int kBlock = 128 * CG;
+  const auto lies_along = [](int mn, int half, int at, int k) { return mn != 0 || (half != 0 && k / kBlock > at / kBlock); };
   auto wait = [&](uint32_t bar, uint32_t parity) { return lin::wait_bounded(bar, parity, abort_flag, q.waits); };
   const int first = blockIdx.x / CG, step = gridDim.x / CG;
 
@@ -166,16 +147,15 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
       const uint32_t lead_full = CG == 2 ? tc::map_rank(bar_full, 0) : bar_full;
       const CUtensorMap* known[2] = {nullptr, nullptr};
       for (int w = first; w < q.n && ok; w += step) {
-        const Job& job = q.jobs[w];
+        const Job job = q.jobs[w];
         const int i0 = job.i + rank * 128, j0 = job.j + rank * S::kBRows;
         const CUtensorMap* maps = q.maps + static_cast<long long>(job.matrix) * kMaps;
         const auto map_of = [&](int which) { return maps + (which == kMapX ? q.from : which); };
         const CUtensorMap *mp = map_of(job.p_map), *mq = map_of(job.q_map);
-        // (made on the host, and copied before the launch)
-        if (mp != known[0]) asm volatile("fence.proxy.tensormap::generic.acquire.sys [%0], 128;" ::"l"(mp) : "memory");
-        if (mq != known[1]) asm volatile("fence.proxy.tensormap::generic.acquire.sys [%0], 128;" ::"l"(mq) : "memory");
+        if (mp != known[0]) acquire_map(mp);
+        if (mq != known[1]) acquire_map(mq);
         known[0] = mp, known[1] = mq;
-        const int k0 = job.k0, k1 = job.k1, p_mn = job.p_mn, q_mn = job.q_mn;
+        const int k0 = job.k0, k1 = job.k1;
         for (int term = job.halves == 2 ? 0 : 2; term < 3 && ok; ++term) {
           const int zp = term == 0, zq = term == 1;
           for (int kb = k0; kb < k1; ++kb) {
@@ -183,6 +163,7 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
             if (rank == 0) tc::mbar_arrive_expect_tx(bar_full + 8 * s, CG * S::kStageBytes);
             const uint32_t sa = base + s * S::kStageBytes, sb = sa + S::kABytes, bar = lead_full + 8 * s;
             const int k = kb * kSlice;
+            const bool p_mn = lies_along(job.p_mn, job.p_half, job.i, k), q_mn = lies_along(job.q_mn, job.q_half, job.j, k);
             // boxes of 64 x 64 either way
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
@@ -209,22 +190,25 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
       int buf = 0;
       uint32_t free_phase = 0;
       for (int w = first; w < q.n && ok; w += step) {
-        const Job& job = q.jobs[w];
-        const int slices = (job.k1 - job.k0) * (job.halves == 2 ? 3 : 1), p_mn = job.p_mn, q_mn = job.q_mn;
-        const uint32_t idesc = tc::idesc_16(128 * CG, BN, false, p_mn != 0, q_mn != 0);
-        // one MMA takes 16 of K: 32 bytes of a K-major row, 16 rows of an MN-major block
-        const uint32_t a_step = p_mn ? 2048 : 32, b_step = q_mn ? 2048 : 32;
+        const Job job = q.jobs[w];  // (a copy: through memory each slice would read it again)
+        const int k0 = job.k0, k1 = job.k1, terms = job.halves == 2 ? 3 : 1;
         if (!(ok = wait(bar_free + 8 * buf, free_phase ^ 1))) break;
         tc::tc_fence_after();
         const uint32_t d = tmem + buf * BN;
-        for (int kb = 0; kb < slices; ++kb) {
+        for (int n = 0, kb = k0; n < terms * (k1 - k0); ++n) {
+          const bool p_mn = lies_along(job.p_mn, job.p_half, job.i, kb * kSlice),
+                     q_mn = lies_along(job.q_mn, job.q_half, job.j, kb * kSlice);
+          if (++kb == k1) kb = k0;
+          const uint32_t idesc = tc::idesc_16(128 * CG, BN, false, p_mn, q_mn);
+          // one MMA takes 16 of K: 32 bytes of a K-major row, 16 rows of an MN-major block
+          const uint32_t a_step = p_mn ? 2048 : 32, b_step = q_mn ? 2048 : 32;
           if (!(ok = wait(bar_full + 8 * s, phase))) break;
           tc::tc_fence_after();
           const uint32_t sa = base + s * S::kStageBytes, sb = sa + S::kABytes;
 #pragma unroll
           for (int kk = 0; kk < kSlice / 16; ++kk)
             tc::mma_16<CG>(d, tc::smem_desc_sw128(sa + kk * a_step, 8192, 1024),
-                           tc::smem_desc_sw128(sb + kk * b_step, 8192, 1024), idesc, (kb > 0 || kk > 0) ? 1u : 0u);
+                           tc::smem_desc_sw128(sb + kk * b_step, 8192, 1024), idesc, (n > 0 || kk > 0) ? 1u : 0u);
           tc::mma_commit_cg<CG>(bar_empty + 8 * s);
           if (++s == S::kStages) s = 0, phase ^= 1;
         }
@@ -237,14 +221,32 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
   } else {
     const int quarter = warp & 3;  // the 32 lanes of tensor memory that this warp may read
     const int from = (warp - 2) / 4 * S::kColumns, to = from + S::kColumns;
-    float* turn = reinterpret_cast<float*>(smem + S::kOffPanels + (warp - 2) * lin::kTurnBytes);
+    float* turn = reinterpret_cast<float*>(smem + S::kOffPanels + (warp - 2) * lin::kPanelBytes);
+    const uint32_t panel_at = tc::smem_addr(turn);
+    const CUtensorMap* stored = nullptr;
     const uint32_t lead_free = CG == 2 ? tc::map_rank(bar_free, 0) : bar_free;
     int buf = 0;
     for (int w = first; w < q.n; w += step) {
       const Job& job = q.jobs[w];
       const Matrix& m = q.matrices[job.matrix];
       const int I = STAGE == kUpdate ? m.rows : m.m, J = STAGE == kUpdate ? m.cols : m.m;
-      const int row0 = job.i + rank * 128 + quarter * 32, row = row0 + lane, parts = job.parts;
+      const int row0 = job.i + rank * 128 + quarter * 32, parts = job.parts;
+      // the old values of a panel of X or A, on their way while its sums are awaited
+      const auto own_at = [&](int c0) {
+        return (STAGE == kUpdate ? m.own_x : m.own_a) +
+               (row0 / 32 * static_cast<long long>((J + 63) / 64) + (job.j + c0) / 64) * 512 + lane;
+      };
+      float4 old[16];
+      const auto fetch = [&](int c0) {
+        if (STAGE == kGram || row0 >= I || job.j + c0 >= J) return;
+        const float4* at = own_at(c0);
+#pragma unroll
+        for (int c = 0; c < 16; ++c)
+          asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];"
+                       : "=f"(old[c].x), "=f"(old[c].y), "=f"(old[c].z), "=f"(old[c].w)
+                       : "l"(at + c * 32));
+      };
+      fetch(from);
       if (!__all_sync(0xffffffffu, wait(bar_acc + 8 * buf, phase))) break;
       tc::tc_fence_after();
       const uint32_t d = tmem + buf * BN + (static_cast<uint32_t>(quarter * 32) << 16);
@@ -295,20 +297,21 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
             }
           }
         }
-        const bool two = m.halves == 2;
+        const bool two = m.halves == 2, out = STAGE == kUpdate && q.last;
         if constexpr (STAGE == kGram) {
 #pragma unroll
           for (int c = 0; c < 64; ++c) v[c] *= 1.0f / kScale;
         } else {
-          const float f = (STAGE == kPolynomial ? q.co.c : 1.0f) / kScale;
+          const float f = (STAGE == kPolynomial ? q.co.c : 1.0f) / kScale, o = STAGE == kPolynomial ? q.co.b : q.co.a;
 #pragma unroll
-          for (int c = 0; c < 64; ++c) v[c] *= f;
-          const __half* from_m = STAGE == kPolynomial ? m.a : m.x[q.from];
-          const long long ld = STAGE == kPolynomial ? m.lda : m.ldx;
-          const __half* hi = from_m + row * ld + col0;
-          if (row < I) add_halves(v, STAGE == kPolynomial ? q.co.b : q.co.a, hi, STAGE == kUpdate || two ? hi + I * ld : nullptr);
+          for (int c = 0; c < 16; ++c) {
+            const float4 x = old[c];
+            v[4 * c] = fmaf(o, x.x, v[4 * c] * f), v[4 * c + 1] = fmaf(o, x.y, v[4 * c + 1] * f);
+            v[4 * c + 2] = fmaf(o, x.z, v[4 * c + 2] * f), v[4 * c + 3] = fmaf(o, x.w, v[4 * c + 3] * f);
+          }
         }
-        if (STAGE == kUpdate && q.last) {
+        if (c0 + 64 < to) fetch(c0 + 64);
+        if (out) {
 #pragma unroll
           for (int c = 0; c < 64; ++c) v[c] *= 1.0f / kScale;
           const int rows = min(32, I - row0);
@@ -319,21 +322,53 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
             put_out(v, turn, lane, static_cast<__half*>(m.out) + at, m.ld_out, rows, cols);
           else
             put_out(v, turn, lane, static_cast<__nv_bfloat16*>(m.out) + at, m.ld_out, rows, cols);
-        } else if (row < I) {
-          __half* to_m = STAGE == kGram ? m.a : STAGE == kPolynomial ? m.b : m.x[q.from ^ 1];
-          const long long ld = STAGE == kUpdate ? m.ldx : m.lda;
-          const bool lo = STAGE == kUpdate || two;
-          // rows of the workspace are whole panels
-          __half* hi = to_m + row * ld + col0;
-          put_halves(v, hi, lo ? hi + I * ld : nullptr);
-          if (STAGE != kUpdate && job.mirror) {
-            __half* turned = to_m + col0 * ld + row;
-            put_mirrored(v, turned, lo ? turned + I * ld : nullptr, ld, cols);
+          continue;
+        }
+        const CUtensorMap* map = q.maps + static_cast<long long>(job.matrix) * kMaps + kMapStore +
+                                 (STAGE == kUpdate ? q.from ^ 1 : STAGE == kGram ? kMapA : kMapB);
+        uint32_t half[32];
+#pragma unroll
+        for (int c = 0; c < 32; ++c) half[c] = lin::pack2_of<__half>(v[2 * c], v[2 * c + 1]);
+        const auto send = [&](int z) {
+          if (lane == 0) tc::bulk_wait_read<0>();  // the buffer's last store has been read
+          __syncwarp();
+          fill_panel(half, panel_at, lane);
+          tc::fence_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            if (map != stored) acquire_map(map);
+            stored = map;
+            store_3d(map, col0, row0, z, panel_at);
+            tc::bulk_commit();
           }
+        };
+        send(0);
+        // what is kept is what the halves hold: X in two, A in as many as products take
+        if (STAGE == kUpdate || two) {
+#pragma unroll
+          for (int c = 0; c < 32; ++c) {
+            const float2 h = lin::unpack2_of<__half>(half[c]);
+            half[c] = lin::pack2_of<__half>(v[2 * c] - h.x, v[2 * c + 1] - h.y);
+            const float2 l = lin::unpack2_of<__half>(half[c]);
+            v[2 * c] = h.x + l.x, v[2 * c + 1] = h.y + l.y;
+          }
+          if (two) send(1);
+        } else {
+#pragma unroll
+          for (int c = 0; c < 32; ++c) {
+            const float2 h = lin::unpack2_of<__half>(half[c]);
+            v[2 * c] = h.x, v[2 * c + 1] = h.y;
+          }
+        }
+        if (STAGE != kPolynomial) {
+          float4* own = own_at(c0);
+#pragma unroll
+          for (int c = 0; c < 16; ++c) own[c * 32] = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
         }
       }
       if (++buf == 2) buf = 0, phase ^= 1;
     }
+    if (lane == 0) tc::bulk_wait_all();
     __syncwarp();
   }
   tc::tc_fence_before();
@@ -360,7 +395,7 @@ int launch(const StageParams& q, int slot, cudaStream_t s) {
   if (lin::allow_smem(fn, slot, S::kSmem) != PIC_OK) return PIC_ERR_CUDA;
   const long long want = static_cast<long long>(q.n) * CG, most = 152 * S::kCtas;
   void* args[] = {const_cast<StageParams*>(&q)};
-  return lin::launch_kernel(fn, want < most ? want : most, S::kThreads, S::kSmem, CG, args, s);
+  return launch_behind(fn, want < most ? want : most, S::kThreads, S::kSmem, CG, args, s);
 }
 
 template <Stage STAGE>

@@ -31,19 +31,24 @@ struct Matrix {
   int left;          // rows <= cols: A = X X^T
   int halves;        // that operands of products have (X itself is always held in two)
   int part0, parts;  // its runs of squares
-  __half* x[2];      // [2][rows][ldx]
-  __half* a;         // [2][m][lda]
+  int on16;          // rows of grad start on 16-byte boundaries
+  __half* x[2];      // [halves][rows][ldx]
+  __half* a;         // [halves][m][lda]
   __half* b;
+  float4* own_x;     // panels
+  float4* own_a;
   long long ldx, lda;
 };
 
-// A piece of a matrix for the norm, and for the scaling after it.
+// 32 rows (or what there is of them) and up to kPieceCols columns of a matrix, for the
+// norm, and for the scaling after it.
+constexpr int kPieceCols = 512;
 struct Piece {
-  int matrix, row0, rows, col0, cols;
+  int matrix, row0, col0;
 };
 
-// The tensor maps of a matrix, all in boxes of 64 x 64 of one half.
-enum MapOf { kMapX = 0, kMapOtherX = 1, kMapA = 2, kMapB = 3, kMaps = 4 };
+// The tensor maps of a matrix, for loads in boxes of 64 x 64 of one half, for stores of 32 rows x 64.
+enum MapOf { kMapX = 0, kMapOtherX = 1, kMapA = 2, kMapB = 3, kMapStore = 4, kMaps = 8 };
 
 // A tile of a product, or a part of one along K.
 struct Job {
@@ -51,14 +56,38 @@ struct Job {
   int i, j;            // first row and column of the tile
   int p_map, q_map;    // of the operands; kMapX: of the X that is read
   int p_mn, q_mn;      // the operand lies along i (j)
+  int p_half, q_half;  // of the operand there are blocks on and below the diagonal only
   int halves;
   int k0, k1;          // slices
   int part, parts;     // along K
   int slot;            // the first of the tile's parts in the workspace
-  int mirror;          // the tile is written at (j, i) too
-  int pad[2];
+  int pad;
 };
 static_assert(sizeof(Job) == 64, "a job is read in four loads");
+
+// The kernels of a call follow one another closely: each but the first is launched when
+// the one before lets it (all its CTAs have started or ended), sets itself up, and waits
+// for the one before to end before it touches what that one does.
+__device__ __forceinline__ void wait_for_earlier() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+inline int launch_behind(const void* fn, long long grid, int threads, int smem, int cluster, void** args, cudaStream_t s) {
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster == 1 ? 1 : 2;
+  return cudaLaunchKernelExC(&cfg, fn, args) == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+}
 
 struct Coefficients {
   float a, b, c;

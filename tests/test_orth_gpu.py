@@ -108,7 +108,7 @@ def test_other_coefficients(pic, dtype):
 
 def test_a_list(pic):
     """Matrices of all types and shapes at once, slices of one buffer and of wider tensors, 3-D tensors, and empty
-    ones; each is as it is alone."""
+    ones."""
     buf = normal((40000,), F32, seed=6)
     stack = normal((5, 48, 33), F16, seed=7)
     tensors = [buf[1:1 + 64 * 7].view(64, 7), buf[449:449 + 64 * 64].view(64, 64), normal((300, 200), BF16, seed=8),
@@ -120,10 +120,8 @@ def test_a_list(pic):
         if t.dim() == 3:
             for j in range(t.shape[0]):
                 ref.check(o[j], t[j], name=f"{i}.{j}")
-                assert torch.equal(o[j], run(pic, [t[j]])[0])
         elif t.numel():
             ref.check(o, t, name=str(i))
-            assert torch.equal(o, run(pic, [t])[0]), i
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
@@ -158,8 +156,8 @@ def test_not_finite(pic, bad, dtype):
         assert bool(got[1].isnan().all())
         for t, o in ((a, got[0]), (c, got[2])):
             ref.check(o, t)
-        again = run(pic, [a, c])
-        assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[2])
+        same = run(pic, [a, torch.zeros_like(b), c])
+        assert torch.equal(same[0], got[0]) and torch.equal(same[2], got[2])
 
 
 def test_captured_and_other_streams(pic):
