@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(kThreads) scale_kernel(const Matrix* matrices,
   }
   __syncthreads();
   const float f0 = factors[0], f1 = factors[1] * (last ? 1.0f : kScale);
-  const int r = threadIdx.x / 8, row = p.row0 + r, col = p.col0 + threadIdx.x % 8 * 8, end = min(m.cols, p.col0 + kPieceCols);
+  const int row = p.row0 + threadIdx.x / 8, col = p.col0 + threadIdx.x % 8 * 8, end = min(m.cols, p.col0 + kPieceCols);
   for_form(m, [&](auto t, auto load) {
     using T = decltype(t);
 #pragma unroll 2
@@ -164,18 +164,13 @@ __global__ void __launch_bounds__(kThreads) scale_kernel(const Matrix* matrices,
         hi[e] = pic::lin::pack2_of<__half>(v[2 * e], v[2 * e + 1]);
         const float2 h = pic::lin::unpack2_of<__half>(hi[e]);
         lo[e] = pic::lin::pack2_of<__half>(v[2 * e] - h.x, v[2 * e + 1] - h.y);
-        const float2 l = pic::lin::unpack2_of<__half>(lo[e]);
-        v[2 * e] = h.x + l.x, v[2 * e + 1] = h.y + l.y;
       }
-      // rows of the workspace, and panels, are whole
+      // rows of the workspace are whole
       if (row < m.rows) {
         __half* x = m.x[0] + row * m.ldx + c;
         *reinterpret_cast<uint4*>(x) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        if (m.halves == 2) *reinterpret_cast<uint4*>(x + m.rows * m.ldx) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        *reinterpret_cast<uint4*>(x + m.rows * m.ldx) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
       }
-      float4* own = m.own_x + (p.row0 / 32 * (m.ldx / 64) + c / 64) * 512 + c % 64 / 4 * 32 + r;
-      own[0] = make_float4(v[0], v[1], v[2], v[3]);
-      own[32] = make_float4(v[4], v[5], v[6], v[7]);
     }
   });
 }
@@ -371,10 +366,8 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
         for (long long c = 0; c < t.cols; c += kPieceCols) pieces.push_back({id, static_cast<int>(r), static_cast<int>(c)});
       t.parts = static_cast<int>(pieces.size()) - t.part0;
       t.on16 = reinterpret_cast<uintptr_t>(m.grad) % 16 == 0 && m.ld_grad * elem_bytes(m.dtype) % 16 == 0;
-      for (int i = 0; i < 2; ++i) at.push_back(take(t.halves * t.rows * t.ldx * 2));
+      for (int i = 0; i < 2; ++i) at.push_back(take(2 * t.rows * t.ldx * 2));
       for (int i = 0; i < 2; ++i) at.push_back(take(t.halves * t.m * t.lda * 2));
-      at.push_back(take((t.rows + 31) / 32 * (t.ldx / 64) * 512 * 16));
-      at.push_back(take((t.m + 31) / 32 * (t.lda / 64) * 512 * 16));
       table.push_back(t);
     }
     std::vector<Job> jobs[3][kShapes];
@@ -398,14 +391,12 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
       Matrix& t = table[i];
       __half** p[4] = {&t.x[0], &t.x[1], &t.a, &t.b};
       for (int k = 0; k < 4; ++k) {
-        *p[k] = reinterpret_cast<__half*>(h->room + at[6 * i + k]);
+        *p[k] = reinterpret_cast<__half*>(h->room + at[4 * i + k]);
         const bool x = k < 2;
-        const long long rows = x ? t.rows : t.m, cols = x ? t.cols : t.m, ld = x ? t.ldx : t.lda;
-        ok = ok && pic::lin::encode_many(&maps[i * kMaps + k], *p[k], rows, cols, ld, t.halves, rows * ld, 64, PIC_DTYPE_F16) &&
-             pic::lin::encode_many(&maps[i * kMaps + kMapStore + k], *p[k], rows, cols, ld, t.halves, rows * ld, 32, PIC_DTYPE_F16);
+        const long long rows = x ? t.rows : t.m, cols = x ? t.cols : t.m, ld = x ? t.ldx : t.lda, n = x ? 2 : t.halves;
+        ok = ok && pic::lin::encode_many(&maps[i * kMaps + k], *p[k], rows, cols, ld, n, rows * ld, 64, PIC_DTYPE_F16) &&
+             pic::lin::encode_many(&maps[i * kMaps + kMapPanel + k], *p[k], rows, cols, ld, n, rows * ld, 32, PIC_DTYPE_F16);
       }
-      t.own_x = reinterpret_cast<float4*>(h->room + at[6 * i + 4]);
-      t.own_a = reinterpret_cast<float4*>(h->room + at[6 * i + 5]);
     }
     h->matrices = reinterpret_cast<Matrix*>(h->room + at_matrices);
     h->maps = reinterpret_cast<CUtensorMap*>(h->room + at_maps);

@@ -10,9 +10,11 @@
 //
 // A = X X^T and A^2 are symmetric: tiles on and below the diagonal are computed and
 // kept.  Where an operand's slice would lie above it, its mirror image is loaded, which
-// lies along the other dimension, and the MMA is told so.  (Tiles written twice, the second
-// time turned, and X read and written by rows took the update of four 2048 x 2048 and two
-// 2048 x 8192 matrices 200 us.)  A product with few tiles is cut along K: each part's
+// lies along the other dimension, and the MMA is told so.  An epilogue reads the old
+// X (or A) of its panel, and writes the new one, by TMA through the panel's buffers: the next
+// panel is on its way while its sums are awaited.  (By lanes, a row each, the update of four
+// 2048 x 2048 and two 2048 x 8192 matrices took 200 us; from and to a copy of its own in fp32
+// 175.)  A product with few tiles is cut along K: each part's
 // sums go to the workspace, and the warp that is the last to bring its part of a panel
 // adds all parts of it in order and finishes it, so that the result does not depend on
 // which is last.
@@ -34,9 +36,9 @@ struct Shape {
   static constexpr int kEpi = BN == 64 ? 4 : 8;
   static constexpr int kThreads = 64 + 32 * kEpi;
   static constexpr int kColumns = BN == 64 ? 64 : BN / 2;
-  static constexpr int kOffPanels = kStages * kStageBytes;
-  static constexpr int kOffBars = kOffPanels + kEpi * lin::kPanelBytes;
-  static constexpr int kBars = 2 * kStages + 4 + 1;
+  static constexpr int kOffPanels = kStages * kStageBytes;  // two halves of each warp
+  static constexpr int kOffBars = kOffPanels + kEpi * 2 * lin::kPanelBytes;
+  static constexpr int kBars = 2 * kStages + 4 + 1 + kEpi;
   static constexpr int kSmem = kOffBars + kBars * 8 + 16 + 1024;  // 1024: the base is rounded up
   static constexpr int kTmemCols = 2 * BN;
 };
@@ -69,6 +71,23 @@ __device__ __forceinline__ void acquire_map(const void* tmap) {
   asm volatile("fence.proxy.tensormap::generic.acquire.sys [%0], 128;" ::"l"(reinterpret_cast<uint64_t>(tmap)) : "memory");
 }
 
+// 64 halves of a lane's row from a panel's buffer: v += f times them.
+__device__ __forceinline__ void add_panel(float (&v)[64], float f, uint32_t buf, int lane) {
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    uint32_t w[4];
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                 : "r"(buf + lane * 128 + ((c ^ (lane & 7)) * 16))
+                 : "memory");
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 x = lin::unpack2_of<__half>(w[e]);
+      v[8 * c + 2 * e] = fmaf(f, x.x, v[8 * c + 2 * e]);
+      v[8 * c + 2 * e + 1] = fmaf(f, x.y, v[8 * c + 2 * e + 1]);
+    }
+  }
+}
 // A panel (32 rows, a lane's row in v, of 64 halves) to its buffer, as TMA takes it.
 __device__ __forceinline__ void fill_panel(const uint32_t (&v)[32], uint32_t buf, int lane) {
 #pragma unroll
@@ -107,7 +126,7 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
   const uint32_t rank = CG == 2 ? tc::cluster_rank() : 0;
   const uint32_t bars = base + S::kOffBars;
   const uint32_t bar_full = bars, bar_empty = bars + 8 * S::kStages, bar_acc = bar_empty + 8 * S::kStages,
-                 bar_free = bar_acc + 16, bar_drain = bar_free + 16;
+                 bar_free = bar_acc + 16, bar_drain = bar_free + 16, bar_in = bar_drain + 8;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + S::kOffBars + 8 * S::kBars);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::kOffBars + 8 * S::kBars + 4);
 
@@ -121,6 +140,7 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
       tc::mbar_init(bar_free + 8 * b, S::kEpi * CG);
     }
     tc::mbar_init(bar_drain, 1);
+    for (int e = 0; e < S::kEpi; ++e) tc::mbar_init(bar_in + 8 * e, 1);
     *abort_flag = 0;
     tc::fence_mbar_init();
   }
@@ -221,36 +241,47 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
   } else {
     const int quarter = warp & 3;  // the 32 lanes of tensor memory that this warp may read
     const int from = (warp - 2) / 4 * S::kColumns, to = from + S::kColumns;
-    float* turn = reinterpret_cast<float*>(smem + S::kOffPanels + (warp - 2) * lin::kPanelBytes);
-    const uint32_t panel_at = tc::smem_addr(turn);
-    const CUtensorMap* stored = nullptr;
+    uint8_t* buffers = smem + S::kOffPanels + (warp - 2) * 2 * lin::kPanelBytes;
+    const uint32_t buffer = tc::smem_addr(buffers), here = bar_in + 8 * (warp - 2);
     const uint32_t lead_free = CG == 2 ? tc::map_rank(bar_free, 0) : bar_free;
+    const int below = rank * 128 + quarter * 32;  // rows of the tile above this warp's
     int buf = 0;
+    uint32_t in_phase = 0;
+    bool coming = false;  // the old values of the panel that is next
+    const CUtensorMap *read = nullptr, *written = nullptr;
+    const auto inside = [&](const Job& job, const Matrix& m, int c0) {
+      return job.i + below < (STAGE == kUpdate ? m.rows : m.m) && job.j + c0 < (STAGE == kUpdate ? m.cols : m.m);
+    };
+    // sends for the old values of a panel: X, or A
+    const auto fetch = [&](const Job& job, const Matrix& m, int c0) {
+      coming = true;
+      if (lane != 0) return;
+      const CUtensorMap* map = q.maps + static_cast<long long>(job.matrix) * kMaps + kMapPanel + (STAGE == kUpdate ? q.from : kMapA);
+      if (map != read) acquire_map(map);
+      read = map;
+      const int n = STAGE == kUpdate ? 2 : m.halves;
+      tc::bulk_wait_read<0>();  // the buffers' last stores have been read
+      tc::mbar_arrive_expect_tx(here, n * lin::kPanelBytes);
+      for (int z = 0; z < n; ++z) load_3d<false>(buffer + z * lin::kPanelBytes, map, job.j + c0, job.i + below, z, here);
+    };
+    // whether a panel's old values can be sent for before its sums are there
+    const auto ahead = [&](const Job& job, const Matrix& m, int c0) {
+      return STAGE != kGram && job.parts == 1 && inside(job, m, c0);
+    };
+    if (first < q.n) {
+      const Job& job = q.jobs[first];
+      const Matrix& m = q.matrices[job.matrix];
+      if (ahead(job, m, from)) fetch(job, m, from);
+    }
     for (int w = first; w < q.n; w += step) {
       const Job& job = q.jobs[w];
       const Matrix& m = q.matrices[job.matrix];
       const int I = STAGE == kUpdate ? m.rows : m.m, J = STAGE == kUpdate ? m.cols : m.m;
-      const int row0 = job.i + rank * 128 + quarter * 32, parts = job.parts;
-      // the old values of a panel of X or A, on their way while its sums are awaited
-      const auto own_at = [&](int c0) {
-        return (STAGE == kUpdate ? m.own_x : m.own_a) +
-               (row0 / 32 * static_cast<long long>((J + 63) / 64) + (job.j + c0) / 64) * 512 + lane;
-      };
-      float4 old[16];
-      const auto fetch = [&](int c0) {
-        if (STAGE == kGram || row0 >= I || job.j + c0 >= J) return;
-        const float4* at = own_at(c0);
-#pragma unroll
-        for (int c = 0; c < 16; ++c)
-          asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];"
-                       : "=f"(old[c].x), "=f"(old[c].y), "=f"(old[c].z), "=f"(old[c].w)
-                       : "l"(at + c * 32));
-      };
-      fetch(from);
+      const int row0 = job.i + below, parts = job.parts;
       if (!__all_sync(0xffffffffu, wait(bar_acc + 8 * buf, phase))) break;
       tc::tc_fence_after();
       const uint32_t d = tmem + buf * BN + (static_cast<uint32_t>(quarter * 32) << 16);
-      for (int c0 = from; c0 < to; c0 += 64) {
+      for (int c0 = from; c0 < to && ok; c0 += 64) {
         float v[64];
         {
           uint32_t acc[64];
@@ -269,106 +300,113 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
           }
         }
         const int col0 = job.j + c0, cols = min(64, J - col0);
-        if (row0 >= I || cols <= 0) continue;  // nothing of this panel is inside
-        if (parts > 1) {
+        bool mine = inside(job, m, c0);
+        if (mine && parts > 1) {
           // [part][rank][panel][quarter][16][32 lanes][4 columns]
           constexpr int kPanels = CG * (BN / 64) * 4;  // warps' panels of a tile
           const int panel = (rank * (BN / 64) + c0 / 64) * 4 + quarter;
-          float4* mine = q.parts + (static_cast<long long>(job.slot + job.part) * kPanels + panel) * 512 + lane;
+          float4* o = q.parts + (static_cast<long long>(job.slot + job.part) * kPanels + panel) * 512 + lane;
 #pragma unroll
-          for (int c = 0; c < 16; ++c) __stcg(mine + c * 32, make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]));
+          for (int c = 0; c < 16; ++c) __stcg(o + c * 32, make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]));
           __threadfence();
           __syncwarp();
           unsigned* counter = q.counters + static_cast<long long>(job.slot) * kPanels + panel;
           unsigned before = 0;
           if (lane == 0) before = atomicAdd(counter, 1);
           before = __shfl_sync(0xffffffffu, before, 0);
-          if (before + 1 < static_cast<unsigned>(parts)) continue;  // others bring theirs later
-          __threadfence();
-          if (lane == 0) *counter = 0;  // for the next launch
-          const float4* all = q.parts + (static_cast<long long>(job.slot) * kPanels + panel) * 512 + lane;
+          mine = before + 1 == static_cast<unsigned>(parts);  // else others bring theirs later
+          if (mine) {
+            if (STAGE != kGram) fetch(job, m, c0);
+            __threadfence();
+            if (lane == 0) *counter = 0;  // for the next launch
+            const float4* all = q.parts + (static_cast<long long>(job.slot) * kPanels + panel) * 512 + lane;
 #pragma unroll
-          for (int c = 0; c < 64; ++c) v[c] = 0.0f;
-          for (int p = 0; p < parts; ++p, all += kPanels * 512) {
+            for (int c = 0; c < 64; ++c) v[c] = 0.0f;
+            for (int p = 0; p < parts; ++p, all += kPanels * 512) {
 #pragma unroll
-            for (int c = 0; c < 16; ++c) {
-              const float4 f = __ldcg(all + c * 32);
-              v[4 * c] += f.x, v[4 * c + 1] += f.y, v[4 * c + 2] += f.z, v[4 * c + 3] += f.w;
+              for (int c = 0; c < 16; ++c) {
+                const float4 f = __ldcg(all + c * 32);
+                v[4 * c] += f.x, v[4 * c + 1] += f.y, v[4 * c + 2] += f.z, v[4 * c + 3] += f.w;
+              }
             }
           }
         }
-        const bool two = m.halves == 2, out = STAGE == kUpdate && q.last;
-        if constexpr (STAGE == kGram) {
+        if (mine) {
+          const bool two = STAGE == kUpdate || m.halves == 2;
+          const float f = (STAGE == kPolynomial ? q.co.c : 1.0f) / kScale;
 #pragma unroll
-          for (int c = 0; c < 64; ++c) v[c] *= 1.0f / kScale;
-        } else {
-          const float f = (STAGE == kPolynomial ? q.co.c : 1.0f) / kScale, o = STAGE == kPolynomial ? q.co.b : q.co.a;
-#pragma unroll
-          for (int c = 0; c < 16; ++c) {
-            const float4 x = old[c];
-            v[4 * c] = fmaf(o, x.x, v[4 * c] * f), v[4 * c + 1] = fmaf(o, x.y, v[4 * c + 1] * f);
-            v[4 * c + 2] = fmaf(o, x.z, v[4 * c + 2] * f), v[4 * c + 3] = fmaf(o, x.w, v[4 * c + 3] * f);
+          for (int c = 0; c < 64; ++c) v[c] *= f;
+          if constexpr (STAGE != kGram) {
+            if (!__all_sync(0xffffffffu, wait(here, in_phase))) {
+              ok = false;
+              break;
+            }
+            in_phase ^= 1;
+            coming = false;
+            const float o = STAGE == kPolynomial ? q.co.b : q.co.a;
+            if (two) add_panel(v, o, buffer + lin::kPanelBytes, lane);
+            add_panel(v, o, buffer, lane);
+          } else {
+            if (lane == 0) tc::bulk_wait_read<0>();
           }
-        }
-        if (c0 + 64 < to) fetch(c0 + 64);
-        if (out) {
-#pragma unroll
-          for (int c = 0; c < 64; ++c) v[c] *= 1.0f / kScale;
-          const int rows = min(32, I - row0);
-          const long long at = row0 * m.ld_out + col0;
-          if (m.dtype == PIC_DTYPE_F32)
-            put_out(v, turn, lane, static_cast<float*>(m.out) + at, m.ld_out, rows, cols);
-          else if (m.dtype == PIC_DTYPE_F16)
-            put_out(v, turn, lane, static_cast<__half*>(m.out) + at, m.ld_out, rows, cols);
-          else
-            put_out(v, turn, lane, static_cast<__nv_bfloat16*>(m.out) + at, m.ld_out, rows, cols);
-          continue;
-        }
-        const CUtensorMap* map = q.maps + static_cast<long long>(job.matrix) * kMaps + kMapStore +
-                                 (STAGE == kUpdate ? q.from ^ 1 : STAGE == kGram ? kMapA : kMapB);
-        uint32_t half[32];
-#pragma unroll
-        for (int c = 0; c < 32; ++c) half[c] = lin::pack2_of<__half>(v[2 * c], v[2 * c + 1]);
-        const auto send = [&](int z) {
-          if (lane == 0) tc::bulk_wait_read<0>();  // the buffer's last store has been read
           __syncwarp();
-          fill_panel(half, panel_at, lane);
-          tc::fence_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            if (map != stored) acquire_map(map);
-            stored = map;
-            store_3d(map, col0, row0, z, panel_at);
-            tc::bulk_commit();
-          }
-        };
-        send(0);
-        // what is kept is what the halves hold: X in two, A in as many as products take
-        if (STAGE == kUpdate || two) {
+          if (STAGE == kUpdate && q.last) {
 #pragma unroll
-          for (int c = 0; c < 32; ++c) {
-            const float2 h = lin::unpack2_of<__half>(half[c]);
-            half[c] = lin::pack2_of<__half>(v[2 * c] - h.x, v[2 * c + 1] - h.y);
-            const float2 l = lin::unpack2_of<__half>(half[c]);
-            v[2 * c] = h.x + l.x, v[2 * c + 1] = h.y + l.y;
-          }
-          if (two) send(1);
-        } else {
+            for (int c = 0; c < 64; ++c) v[c] *= 1.0f / kScale;
+            const int rows = min(32, I - row0);
+            const long long at = row0 * m.ld_out + col0;
+            float* turn = reinterpret_cast<float*>(buffers);
+            if (m.dtype == PIC_DTYPE_F32)
+              put_out(v, turn, lane, static_cast<float*>(m.out) + at, m.ld_out, rows, cols);
+            else if (m.dtype == PIC_DTYPE_F16)
+              put_out(v, turn, lane, static_cast<__half*>(m.out) + at, m.ld_out, rows, cols);
+            else
+              put_out(v, turn, lane, static_cast<__nv_bfloat16*>(m.out) + at, m.ld_out, rows, cols);
+            tc::fence_async_smem();
+            __syncwarp();
+          } else {
+            uint32_t half[32];
 #pragma unroll
-          for (int c = 0; c < 32; ++c) {
-            const float2 h = lin::unpack2_of<__half>(half[c]);
-            v[2 * c] = h.x, v[2 * c + 1] = h.y;
+            for (int c = 0; c < 32; ++c) half[c] = lin::pack2_of<__half>(v[2 * c], v[2 * c + 1]);
+            fill_panel(half, buffer, lane);
+            if (two) {
+#pragma unroll
+              for (int c = 0; c < 32; ++c) {
+                const float2 h = lin::unpack2_of<__half>(half[c]);
+                half[c] = lin::pack2_of<__half>(v[2 * c] - h.x, v[2 * c + 1] - h.y);
+              }
+              fill_panel(half, buffer + lin::kPanelBytes, lane);
+            }
+            tc::fence_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              const CUtensorMap* map = q.maps + static_cast<long long>(job.matrix) * kMaps + kMapPanel +
+                                       (STAGE == kUpdate ? q.from ^ 1 : STAGE == kGram ? kMapA : kMapB);
+              if (map != written) acquire_map(map);
+              written = map;
+              store_3d(map, col0, row0, 0, buffer);
+              if (two) store_3d(map, col0, row0, 1, buffer + lin::kPanelBytes);
+              tc::bulk_commit();
+            }
           }
         }
-        if (STAGE != kPolynomial) {
-          float4* own = own_at(c0);
-#pragma unroll
-          for (int c = 0; c < 16; ++c) own[c * 32] = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+        if (c0 + 64 < to) {
+          if (ahead(job, m, c0 + 64)) fetch(job, m, c0 + 64);
+        } else if (w + step < q.n) {
+          const Job& next = q.jobs[w + step];
+          const Matrix& nm = q.matrices[next.matrix];
+          if (ahead(next, nm, from)) fetch(next, nm, from);
         }
       }
+      if (!ok) break;
       if (++buf == 2) buf = 0, phase ^= 1;
     }
-    if (lane == 0) tc::bulk_wait_all();
+    if (lane == 0) {
+      tc::bulk_wait_all();
+      // after an abort: what has been sent for and not awaited
+      for (uint32_t i = 0; coming && i < q.waits.spin_limit && !tc::mbar_try_wait(here, in_phase); ++i) {
+      }
+    }
     __syncwarp();
   }
   tc::tc_fence_before();

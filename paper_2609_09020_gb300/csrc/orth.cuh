@@ -7,6 +7,9 @@
 // |c s^4| of at most 12 bound every element, so that none reaches the largest half; with
 // kScale = 4096 an element of the usual size, 1 / sqrt(max(rows, cols)), is far above
 // the smallest.
+//
+// A and b A + c A^2 are symmetric, and only their blocks on and below the diagonal are
+// kept (blocks as high as a tile); operands above it are loaded turned.
 #pragma once
 
 #include <cuda.h>
@@ -29,14 +32,12 @@ struct Matrix {
   int rows, cols, dtype;
   int m;             // the smaller side
   int left;          // rows <= cols: A = X X^T
-  int halves;        // that operands of products have (X itself is always held in two)
+  int halves;        // that A, b A + c A^2 and operands of products have
   int part0, parts;  // its runs of squares
   int on16;          // rows of grad start on 16-byte boundaries
-  __half* x[2];      // [halves][rows][ldx]
+  __half* x[2];      // [2][rows][ldx]
   __half* a;         // [halves][m][lda]
   __half* b;
-  float4* own_x;     // panels
-  float4* own_a;
   long long ldx, lda;
 };
 
@@ -47,8 +48,9 @@ struct Piece {
   int matrix, row0, col0;
 };
 
-// The tensor maps of a matrix, for loads in boxes of 64 x 64 of one half, for stores of 32 rows x 64.
-enum MapOf { kMapX = 0, kMapOtherX = 1, kMapA = 2, kMapB = 3, kMapStore = 4, kMaps = 8 };
+// The tensor maps of a matrix: of operands in boxes of 64 x 64 of one half, of epilogues'
+// panels in boxes of 32 rows x 64.
+enum MapOf { kMapX = 0, kMapOtherX = 1, kMapA = 2, kMapB = 3, kMapPanel = 4, kMaps = 8 };
 
 // A tile of a product, or a part of one along K.
 struct Job {
