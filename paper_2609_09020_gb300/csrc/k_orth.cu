@@ -11,13 +11,19 @@
 // Tile shapes, by columns.
 constexpr int kShapes = 3;
 constexpr int kShapeColumns[kShapes] = {64, 128, 256};
+// Small matrices of up to so much shared memory are launched together.
+constexpr int kSmallLists = 3;
+constexpr int kSmallBytes[kSmallLists] = {56 * 1024, 112 * 1024, pic::orth::kSmallMost};
 
 struct pic_orthogonalizer {
   int device;
   int n_pieces;
+  int* small[kSmallLists];  // matrices that a CTA each takes, by the shared memory that they need
+  int n_small[kSmallLists], small_bytes[kSmallLists];
   char* room;  // all of it
   pic::orth::Matrix* matrices;
   CUtensorMap* maps;
+  int n_maps;
   pic::orth::Piece* pieces;
   pic::orth::Job* jobs[3][kShapes];  // of each stage
   int n_jobs[3][kShapes];
@@ -86,15 +92,16 @@ __global__ void __launch_bounds__(kThreads) squares_kernel(const Matrix* matrice
   double sum = 0.0;
   for_form(m, [&](auto, auto load) {
     float s = 0.0f;
+    bool some = false;  // values that are not zero
 #pragma unroll 4
     for (int c = col; c < end; c += 64) {
       float v[8];
       load(row, c, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s = fmaf(v[e], v[e], s);
+      for (int e = 0; e < 8; ++e) s = fmaf(v[e], v[e], s), some |= v[e] != 0.0f;
     }
     sum = s;
-    if (!(s >= 1e-28f && s <= 1e37f)) {
+    if (some && !(s >= 1e-28f && s <= 1e37f)) {
       sum = 0.0;
       for (int c = col; c < end; c += 64) {
         float v[8];
@@ -114,8 +121,7 @@ __global__ void __launch_bounds__(kThreads) squares_kernel(const Matrix* matrice
   }
 }
 
-// X = G / (|G| + eps), a piece a block: by a power of two first, then by what is left, so
-// that no finite norm leaves fp32's range on the way.
+// X = G / (|G| + eps), a piece a block.
 __global__ void __launch_bounds__(kThreads) scale_kernel(const Matrix* matrices, const Piece* pieces, const double* squares,
                                                          float eps, int last) {
   __shared__ float factors[2];
@@ -131,12 +137,7 @@ __global__ void __launch_bounds__(kThreads) scale_kernel(const Matrix* matrices,
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int w = 1; w < kThreads / 32; ++w) sum += sums[w];
-    const double norm = sqrt(sum) + eps;
-    int e = 0;
-    if (norm > 0.0 && norm < 1e300) frexp(norm, &e);
-    e = min(max(e, -126), 126);
-    factors[0] = static_cast<float>(ldexp(1.0, -e));
-    factors[1] = static_cast<float>(ldexp(1.0, e) / norm);
+    norm_factors(sum, eps, factors[0], factors[1]);
   }
   __syncthreads();
   const float f0 = factors[0], f1 = factors[1] * (last ? 1.0f : kScale);
@@ -217,6 +218,14 @@ bool outputs_disjoint(const std::vector<pic_orth_matrix>& list) {
   return true;
 }
 
+// What five steps of a matrix take one CTA, in us (measured, of fp32: 32 x 32 15, 32 x 1000
+// 100, 64 x 64 25, 64 x 256 62, 64 x 512 109, 128 x 128 115; by tiles 200 x 200 takes 127,
+// 512 x 512 168; bfloat16 three quarters of that).
+double small_time(const Matrix& m) {
+  const double n = std::max(m.rows, m.cols);
+  return (m.m <= 32 ? 12 + 0.09 * n : m.m <= 64 ? 13 + 0.19 * n : 50 + 0.6 * n) * (m.halves == 2 ? 1.0 : 0.75);
+}
+
 // Whether the singular values that steps meet, from [0, 1], stay in [-2, 2], and b s^2 + c
 // s^4 within 12: what X and b A + c A^2 are held in has room for no more.
 bool steps_ok(int steps, double a, double b, double c) {
@@ -250,20 +259,22 @@ bool steps_ok(int steps, double a, double b, double c) {
 // smaller side is no more; else 128.
 //
 // Parts: stages with fewer tiles than there are CTAs (kSlots) are cut along K, with at
-// least kLeast slices in a part; and sums of more than kMost slices, in which a tensor
+// least kLeast slices (of all three products of halves) in a part, as a part more costs 3
+// us; and sums of more than kMost slices, in which a tensor
 // core's truncations would show (it loses up to 2^-24 of a sum with each 16 of K).
 void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kShapes], long long& part_bytes,
                long long& counters) {
-  constexpr int kSms = 152, kSlots[kShapes] = {2 * kSms, kSms, kSms / 2}, kLeast = 2, kMost[2] = {256, 64};
+  constexpr int kSms = 152, kSlots[kShapes] = {2 * kSms, kSms, kSms / 2}, kLeast = 16, kMost[2] = {256, 64};
   const auto blocks = [](long long n, long long of) { return (n + of - 1) / of; };
   long long large = 0;
   for (const Matrix& m : table)
-    if (m.m > 512) large += blocks(m.rows, 256) * blocks(m.cols, 256);
+    if (m.parts > 0 && m.m > 512) large += blocks(m.rows, 256) * blocks(m.cols, 256);
   for (int s = 0; s < 3; ++s) {
     long long tiles[kShapes] = {};
     std::vector<Job> plain[kShapes];
     for (size_t id = 0; id < table.size(); ++id) {
       const Matrix& m = table[id];
+      if (m.parts == 0) continue;  // a CTA's
       const int shape = m.m <= 64 ? 0 : m.m > 512 && large >= 60 ? 2 : 1;
       const int bn = kShapeColumns[shape], rows = shape == 2 ? 256 : 128;
       Job j{};
@@ -300,7 +311,8 @@ void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kSh
       int slot = 0;
       for (const Job& j : plain[shape]) {
         const int slices = j.k1, most = kMost[j.halves - 1];
-        long long parts = std::max<long long>(std::min<long long>(fill, slices / kLeast), blocks(slices, most));
+        const int passes = j.halves == 2 ? 3 : 1;
+        long long parts = std::max<long long>(std::min<long long>(fill, slices * passes / kLeast), blocks(slices, most));
         parts = std::max<long long>(parts, 1);
         const int each = static_cast<int>(blocks(slices, parts));
         parts = blocks(slices, each);
@@ -346,6 +358,8 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
     if (rc != PIC_OK) return rc;
     std::vector<Matrix> table;
     std::vector<Piece> pieces;
+    std::vector<int> small[kSmallLists];
+    int small_most[kSmallLists] = {};
     long long bytes = 0;
     const auto take = [&](long long b) {
       const long long at = bytes;
@@ -353,6 +367,10 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
       return at;
     };
     std::vector<long long> at;
+    // by a CTA each: what is sooner done so than by tiles, or, beside others that go by
+    // tiles, where it takes a fraction of their time
+    const bool tiles = std::any_of(list.begin(), list.end(), [](const pic_orth_matrix& m) { return std::min(m.rows, m.cols) > 128; });
+    const double worth = tiles ? 30.0 : 100.0;
     for (const pic_orth_matrix& m : list) {
       const int id = static_cast<int>(table.size());
       Matrix t{};
@@ -361,6 +379,16 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
       t.m = std::min(t.rows, t.cols), t.left = t.rows <= t.cols;
       t.halves = m.dtype == PIC_DTYPE_BF16 ? 1 : 2;
       t.ldx = (m.cols + 63) / 64 * 64, t.lda = (t.m + 63) / 64 * 64;  // whole panels
+      const long long need = t.m <= 128 ? small_bytes(t.m, t.left ? t.cols : t.rows) : kSmallMost + 1LL;
+      if (need <= kSmallMost && small_time(t) <= worth) {
+        int which = 0;
+        while (need > kSmallBytes[which]) ++which;
+        small[which].push_back(id);
+        small_most[which] = std::max(small_most[which], static_cast<int>(need));
+        at.resize(at.size() + 4);
+        table.push_back(t);
+        continue;
+      }
       t.part0 = static_cast<int>(pieces.size());
       for (long long r = 0; r < t.rows; r += 32)
         for (long long c = 0; c < t.cols; c += kPieceCols) pieces.push_back({id, static_cast<int>(r), static_cast<int>(c)});
@@ -379,6 +407,8 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
     long long at_jobs[3][kShapes];
     for (int s = 0; s < 3; ++s)
       for (int c = 0; c < kShapes; ++c) at_jobs[s][c] = take(jobs[s][c].size() * sizeof(Job));
+    long long at_small[kSmallLists];
+    for (int i = 0; i < kSmallLists; ++i) at_small[i] = take(small[i].size() * sizeof(int));
     h = new pic_orthogonalizer{};
     if (cudaGetDevice(&h->device) != cudaSuccess || cudaMalloc(&h->room, bytes) != cudaSuccess) {
       cudaGetLastError();
@@ -389,6 +419,7 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
     bool ok = true;
     for (size_t i = 0; i < table.size(); ++i) {
       Matrix& t = table[i];
+      if (t.parts == 0) continue;
       __half** p[4] = {&t.x[0], &t.x[1], &t.a, &t.b};
       for (int k = 0; k < 4; ++k) {
         *p[k] = reinterpret_cast<__half*>(h->room + at[4 * i + k]);
@@ -400,6 +431,7 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
     }
     h->matrices = reinterpret_cast<Matrix*>(h->room + at_matrices);
     h->maps = reinterpret_cast<CUtensorMap*>(h->room + at_maps);
+    h->n_maps = static_cast<int>(std::min<size_t>(maps.size(), 0x7fffffff));
     h->pieces = reinterpret_cast<Piece*>(h->room + at_pieces);
     h->squares = reinterpret_cast<double*>(h->room + at_squares);
     h->parts = reinterpret_cast<float4*>(h->room + at_parts);
@@ -411,6 +443,12 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
       return v.empty() || cudaMemcpy(to, v.data(), v.size() * sizeof(v[0]), cudaMemcpyHostToDevice) == cudaSuccess;
     };
     ok = ok && put(h->matrices, table) && put(h->maps, maps) && put(h->pieces, pieces);
+    for (int i = 0; i < kSmallLists; ++i) {
+      h->small[i] = reinterpret_cast<int*>(h->room + at_small[i]);
+      h->n_small[i] = static_cast<int>(small[i].size());
+      h->small_bytes[i] = small_most[i];
+      ok = ok && put(h->small[i], small[i]);
+    }
     for (int s = 0; s < 3; ++s)
       for (int c = 0; c < kShapes; ++c) {
         h->jobs[s][c] = reinterpret_cast<Job*>(h->room + at_jobs[s][c]);
@@ -443,8 +481,13 @@ int pic_orth(pic_orthogonalizer* h, int steps, float a, float b, float c, float 
     return PIC_ERR_CUDA;
   }
   if (dev != h->device) return PIC_ERR_INVALID_ARG;
-  if (h->n_pieces == 0) return PIC_OK;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  for (int i = kSmallLists - 1; i >= 0; --i)
+    if (launch_small(h->matrices, h->small[i], h->n_small[i], h->small_bytes[i], steps, {a, b, c}, eps, s) != PIC_OK) {
+      cudaGetLastError();
+      return PIC_ERR_CUDA;
+    }
+  if (h->n_pieces == 0) return PIC_OK;
   pic::lin::Waits waits;
   if (!pic::lin::call_waits(waits)) return PIC_ERR_CUDA;
   waits.status = h->status;
@@ -460,7 +503,7 @@ int pic_orth(pic_orthogonalizer* h, int steps, float a, float b, float c, float 
   for (int k = 0; k < steps; ++k)
     for (const Stage stage : {kGram, kPolynomial, kUpdate})
       for (int shape = 0; shape < kShapes; ++shape) {
-        const StageParams q{h->matrices, h->maps, h->jobs[stage][shape], h->n_jobs[stage][shape], {a, b, c}, k & 1,
+        const StageParams q{h->matrices, h->maps, h->n_maps, h->jobs[stage][shape], h->n_jobs[stage][shape], {a, b, c}, k & 1,
                             k + 1 == steps, h->parts, h->counters, waits};
         if (launch_stage(stage, kShapeColumns[shape], q, s) != PIC_OK) {
           cudaGetLastError();

@@ -145,12 +145,16 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
     tc::fence_mbar_init();
   }
   if (warp == 1) tc::tmem_alloc_cg<CG>(tc::smem_addr(tmem_slot), S::kTmemCols);
+  if (q.n_maps <= kAcquiredFirst)
+    for (int i = threadIdx.x; i < q.n_maps; i += blockDim.x) acquire_map(q.maps + i);
   tc::tc_fence_before();
   __syncthreads();
   if constexpr (CG == 2) tc::cluster_sync();
   tc::tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   wait_for_earlier();
+  // (a fence takes half a microsecond)
+  const bool acquired = q.n_maps <= kAcquiredFirst;
 
   // Whether slice k of an operand lies along i (j): by itself, or, of a symmetric matrix, as
   // the mirror image of one above the diagonal.
@@ -172,8 +176,8 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
         const CUtensorMap* maps = q.maps + static_cast<long long>(job.matrix) * kMaps;
         const auto map_of = [&](int which) { return maps + (which == kMapX ? q.from : which); };
         const CUtensorMap *mp = map_of(job.p_map), *mq = map_of(job.q_map);
-        if (mp != known[0]) acquire_map(mp);
-        if (mq != known[1]) acquire_map(mq);
+        if (!acquired && mp != known[0]) acquire_map(mp);
+        if (!acquired && mq != known[1]) acquire_map(mq);
         known[0] = mp, known[1] = mq;
         const int k0 = job.k0, k1 = job.k1;
         for (int term = job.halves == 2 ? 0 : 2; term < 3 && ok; ++term) {
@@ -257,7 +261,7 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
       coming = true;
       if (lane != 0) return;
       const CUtensorMap* map = q.maps + static_cast<long long>(job.matrix) * kMaps + kMapPanel + (STAGE == kUpdate ? q.from : kMapA);
-      if (map != read) acquire_map(map);
+      if (!acquired && map != read) acquire_map(map);
       read = map;
       const int n = STAGE == kUpdate ? 2 : m.halves;
       tc::bulk_wait_read<0>();  // the buffers' last stores have been read
@@ -382,7 +386,7 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
             if (lane == 0) {
               const CUtensorMap* map = q.maps + static_cast<long long>(job.matrix) * kMaps + kMapPanel +
                                        (STAGE == kUpdate ? q.from ^ 1 : STAGE == kGram ? kMapA : kMapB);
-              if (map != written) acquire_map(map);
+              if (!acquired && map != written) acquire_map(map);
               written = map;
               store_3d(map, col0, row0, 0, buffer);
               if (two) store_3d(map, col0, row0, 1, buffer + lin::kPanelBytes);

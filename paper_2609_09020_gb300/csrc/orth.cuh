@@ -14,6 +14,7 @@
 
 #include <cuda.h>
 
+#include "k_linear_tc.cuh"
 #include "linear.cuh"
 #include "pic_orth.h"
 
@@ -95,12 +96,41 @@ struct Coefficients {
   float a, b, c;
 };
 
+// |G| + eps from the sum of squares: X is G times f0 times f1, a power of two first, then
+// what is left, so that no finite norm leaves fp32's range on the way.
+__device__ __forceinline__ void norm_factors(double sum, float eps, float& f0, float& f1) {
+  const double norm = sqrt(sum) + eps;
+  int e = 0;
+  if (norm > 0.0 && norm < 1e300) frexp(norm, &e);
+  e = min(max(e, -126), 126);
+  f0 = static_cast<float>(ldexp(1.0, -e));
+  f1 = static_cast<float>(ldexp(1.0, e) / norm);
+}
+
+// Matrices that one CTA takes through all steps by itself: the smaller side at most 128,
+// and X, A and b A + c A^2, in two halves each, within kSmallMost bytes of shared memory.
+struct SmallShape {
+  int rows, cols;  // of X in shared memory, and 8 more halves from row to row
+};
+__host__ __device__ inline SmallShape small_shape(int m, int n) {
+  return {m <= 32 ? 32 : m <= 64 ? 64 : 128, (n + 31) / 32 * 32};
+}
+constexpr int kSmallMost = 220 * 1024;
+__host__ inline long long small_bytes(int m, int n) {
+  const SmallShape s = small_shape(m, n);
+  return 4LL * s.rows * (s.cols + 8) + 8LL * s.rows * (s.rows + 8);
+}
+int launch_small(const Matrix* matrices, const int* list, int n, int smem, int steps, const Coefficients& co, float eps,
+                 cudaStream_t s);
+
 // Stages of a step: A = X X^T, B = b A + c A^2, X = a X + B X.
 enum Stage { kGram = 0, kPolynomial = 1, kUpdate = 2 };
 
+constexpr int kAcquiredFirst = 512;  // up to so many maps, a CTA's threads acquire them all while it waits for the kernel before
 struct StageParams {
   const Matrix* matrices;
   const CUtensorMap* maps;  // [matrices][kMaps]
+  int n_maps;
   const Job* jobs;
   int n;
   Coefficients co;
