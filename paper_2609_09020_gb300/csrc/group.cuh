@@ -82,12 +82,13 @@ __device__ __forceinline__ void make_table(GroupTable& t, const long long* offse
   }
   if (bad && blockIdx.x == 0) atomicOr(status + 1, 1);
   __syncthreads();
+  const auto tiles_of = [&](int g) { return t.rows(g) == 0 ? least : (t.rows(g) - 1) / unit + 1; };
   int count = 0;
-  for (int g = first; g < min(last, groups); ++g) count += max(least, (t.rows(g) + unit - 1) / unit);
+  for (int g = first; g < min(last, groups); ++g) count += tiles_of(g);
   int at = block_scan<false>(count, t.scan) - count;
   for (int g = first; g < last; ++g) {
     t.tiles[g] = at;
-    if (g < groups) at += max(least, (t.rows(g) + unit - 1) / unit);
+    if (g < groups) at += tiles_of(g);
   }
   __syncthreads();
 }
@@ -127,6 +128,33 @@ constexpr long long kTcMostK = 16384;  // of K that one accumulator sums up
 bool tc_takes(const GroupProduct& p, int dtype);
 long long tc_workspace(const GroupProduct& p, int dtype);
 int tc_product(const GroupProduct& p, int dtype, void* ws, const Waits& waits, cudaStream_t s);
+
+// Where part `item` of group g is among the parts of the groups that have several; the
+// calling warp's lanes count together.
+__device__ __forceinline__ long long part_slot(const GroupTable& t, int g, int item, int chunk, int lane) {
+  int whole = 0;
+  for (int i = lane; i < g; i += 32) whole += t.rows(i) <= chunk;
+  return item - __reduce_add_sync(0xffffffffu, whole);
+}
+
+// The sums of the groups' parts (of groups with more than `chunk` rows), in order.  A
+// tile's part is [rank][panel of 64 columns][quarter][16][32 rows][4 columns].
+struct JoinParams {
+  const long long* offsets;
+  long long rows, I, J, tiles_i, tiles_j;
+  int groups, chunk, bn;
+  const float4* parts;
+  void* y;
+  long long ldy, y_group;
+  int* status;
+};
+// rows: of a tile.
+void join_parts(const JoinParams& q, int rows, int dtype, cudaStream_t s);
+
+// fp32 on the tensor cores, cut into planes first.
+bool planes_takes(const GroupProduct& p, int dtype);
+long long planes_workspace(const GroupProduct& p);
+int planes_product(const GroupProduct& p, void* ws, const Waits& waits, cudaStream_t s);
 
 // dz[i][j] = dy act'(pre), rounded (dz null: not written; its rows are on 16-byte
 // boundaries and written to the next one), and db_g, the sums of the unrounded dz over

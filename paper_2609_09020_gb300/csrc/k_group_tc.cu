@@ -79,16 +79,7 @@ __global__ void __launch_bounds__(32) maps_kernel(const MakeMaps q, const __grid
                  : "memory");
 }
 
-// The sums of a group's parts, in order: a thread finishes four columns of a row.
-struct JoinParams {
-  const long long* offsets;
-  long long rows, I, J, tiles_i, tiles_j;
-  int groups, chunk, bn;
-  const float4* parts;
-  void* y;
-  long long ldy, y_group;
-  int* status;
-};
+// (group.cuh)
 template <typename T, int ROWS>
 __global__ void __launch_bounds__(256) join_kernel(const JoinParams q) {
   __shared__ GroupTable table;
@@ -220,15 +211,24 @@ void pad(const Operand& o, long long ld, long long group, void* to, cudaStream_t
 }
 
 template <typename T>
-void join(const JoinParams& q, int cg, cudaStream_t s) {
-  const dim3 grid(static_cast<unsigned>(q.tiles_i * q.tiles_j * 128 * cg * q.bn / 4 / 256), q.groups);
-  if (cg == 1)
+void join(const JoinParams& q, int rows, cudaStream_t s) {
+  const dim3 grid(static_cast<unsigned>(q.tiles_i * q.tiles_j * rows * q.bn / 4 / 256), q.groups);
+  if (rows == 128)
     join_kernel<T, 128><<<grid, 256, 0, s>>>(q);
   else
     join_kernel<T, 256><<<grid, 256, 0, s>>>(q);
 }
 
 }  // namespace
+
+void join_parts(const JoinParams& q, int rows, int dtype, cudaStream_t s) {
+  if (dtype == PIC_DTYPE_F32)
+    join<float>(q, rows, s);
+  else if (dtype == PIC_DTYPE_F16)
+    join<__half>(q, rows, s);
+  else
+    join<__nv_bfloat16>(q, rows, s);
+}
 
 bool tc_takes(const GroupProduct& p, int dtype) {
   if (dtype == PIC_DTYPE_F32 || p.a_pre) return false;
@@ -300,10 +300,7 @@ int tc_product(const GroupProduct& p, int dtype, void* ws, const Waits& waits, c
   if (!p.by_rows && r.part_bytes > 0) {
     const JoinParams j{p.offsets, p.rows, p.I, p.J, r.tiles_i, r.tiles_j, p.groups, r.chunk, r.bn,
                        reinterpret_cast<const float4*>(q.parts), p.y, p.ldy, p.y_group, waits.status};
-    if (dtype == PIC_DTYPE_BF16)
-      join<__nv_bfloat16>(j, r.cg, s);
-    else
-      join<__half>(j, r.cg, s);
+    join_parts(j, 128 * r.cg, dtype, s);
   }
   return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
 }

@@ -157,14 +157,6 @@ struct GtItem {
   bool whole;           // kSums: the group's only one
 };
 
-// Where part `item` of group g is among the parts of the groups that have several; the
-// calling warp's lanes count together.
-__device__ __forceinline__ long long part_slot(const GroupTable& t, int g, int item, int chunk, int lane) {
-  int whole = 0;
-  for (int i = lane; i < g; i += 32) whole += t.rows(i) <= chunk;
-  return item - __reduce_add_sync(0xffffffffu, whole);
-}
-
 template <int CG, int BN, TcMode MODE>
 __device__ __forceinline__ long long work_of(const GtParams& q, const GroupTable& t) {
   if constexpr (MODE == kRows) return t.tiles[q.groups] * q.tiles_j;

@@ -822,6 +822,9 @@ bool encode(CUtensorMap* map, const void* m, long long rows, long long cols, lon
 // and box_rows rows of one of them.
 bool encode_many(CUtensorMap* map, const void* m, long long rows, long long cols, long long ld, long long count,
                  long long group, int box_rows, int dtype);
+// The three planes of a matrix, in boxes of box_cols columns (64, 128-byte swizzled,
+// or 32, 64-byte swizzled), box_rows rows and all planes.
+bool encode_planes(CUtensorMap* map, const void* m, long long rows, long long cols, long long ld, int box_cols, int box_rows);
 // Allows a kernel `smem` bytes of shared memory, once per device; each kernel of
 // these files has a slot of its own below kSmemSlots.
 constexpr int kSmemSlots = 64;

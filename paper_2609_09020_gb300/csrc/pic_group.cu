@@ -57,10 +57,13 @@ bool args_ok(const pic_grouped_linear_grad_args* a) {
 const long long* offsets_of(const int64_t* o) { return reinterpret_cast<const long long*>(o); }
 
 long long product_workspace(const GroupProduct& p, int dtype) {
-  return pic::grp::tc_takes(p, dtype) ? pic::grp::tc_workspace(p, dtype) : 0;
+  if (pic::grp::tc_takes(p, dtype)) return pic::grp::tc_workspace(p, dtype);
+  return pic::grp::planes_takes(p, dtype) ? pic::grp::planes_workspace(p) : 0;
 }
 int product(const GroupProduct& p, int dtype, void* ws, const pic::lin::Waits& w, cudaStream_t s) {
-  return pic::grp::tc_takes(p, dtype) ? pic::grp::tc_product(p, dtype, ws, w, s) : pic::grp::any_product(p, dtype, s);
+  if (pic::grp::tc_takes(p, dtype)) return pic::grp::tc_product(p, dtype, ws, w, s);
+  if (pic::grp::planes_takes(p, dtype)) return pic::grp::planes_product(p, ws, w, s);
+  return pic::grp::any_product(p, dtype, s);
 }
 
 int forward(const pic_grouped_linear_args& a, pic::lin::Arena& ws, bool launch, const pic::lin::Waits& w, cudaStream_t s) {

@@ -353,3 +353,59 @@ def test_rows_past_32_bits(pic):
     ref.check(dw, ww, "dw")
     ref.check(db, wb, "db")
     pic.grouped_linear_check()
+
+
+@pytest.mark.parametrize("inp,outp", [(512, 384), (1000, 130), (136, 640)], ids=str)
+def test_large_fp32(pic, inp, outp):
+    """fp32 layers large enough for the tensor cores: against the definition, and sums of 512
+    and more about as good as fp32 FMAs in order (6.2e-7 of 1024), not worse than 1.5e-6."""
+    offsets = [3, 700, 700, 1500, 1629, 2600, 2601]
+    check_forward(pic, offsets, 2610, inp, outp, F32, "gelu")
+    check_backward(pic, offsets, 2610, inp, outp, F32, "gelu")
+    x, w, b = case(2610, 6, inp, outp, F32, 7, bias=False)
+    y = pic.grouped_linear(x, w, offsets_tensor(offsets))
+    dx, dw, _ = pic.grouped_linear_backward(y, x, w, offsets_tensor(offsets))
+    for g, i, j in group_ref.spans(offsets):
+        if j - i > 128:
+            for got, want in ((y[i:j], x[i:j].double() @ w[g].double().t()), (dx[i:j], y[i:j].double() @ w[g].double()),
+                              (dw[g], y[i:j].double().t() @ x[i:j].double())):
+                d = (got.double() - want).square().mean().sqrt() / want.square().mean().sqrt()
+                assert float(d) <= 1.5e-6
+
+
+def test_large_fp32_not_finite(pic):
+    """In large fp32 layers too, rows that are not finite stay in their group, and an infinity
+    or a value that its first piece would round to one is as the formula has it."""
+    offsets, rows = [0, 300, 301, 701, 1100], 1100
+    x, w, _ = case(rows, 4, 520, 392, F32, 0, bias=False)
+    x[300:301], x[701:705], w[3, 17, 5] = float("nan"), float("inf"), float("nan")
+    x[10, 100], x[450, 7] = 3.4e38, float("-inf")
+    o = offsets_tensor(offsets)
+    y = pic.grouped_linear(x, w, o)
+    dy = normal((rows, 392), F32, 4)
+    dx, dw, db = pic.grouped_linear_backward(dy, x, w, o)
+    pic.grouped_linear_check()
+    finite = torch.isfinite(x).all(1)
+    wy, _ = group_ref.forward(x, w, None, offsets, "none")
+    ok = finite.clone()
+    ok[701:] = False
+    ok[10] = False  # beside fp32's range in places
+    ref.check(y[ok], (wy[0][ok], wy[1][ok]), "y")
+    assert bool(y[300].isnan().all()) and bool(y[701:, 17].isnan().all())
+    others = [c for c in range(392) if c != 17]
+    assert torch.isfinite(y[705:][:, others]).all()
+    assert torch.equal(y[450].sign(), -w[2, :, 7].sign()) and torch.isinf(y[450]).all()
+    near = wy[0][10].abs() < 3e38
+    ref.check(y[10][near], (wy[0][10][near], wy[1][10][near]), "y")
+    wx, ww, wb = group_ref.backward(dy, x, w, None, offsets, "none")
+    ref.check(dx[:701], (wx[0][:701], wx[1][:701]), "dx")
+    bad = [c for c in range(520) if c != 5]
+    ref.check(dx[701:][:, bad], (wx[0][701:][:, bad], wx[1][701:][:, bad]), "dx")
+    assert bool(dx[701:, 5].isnan().all())
+    most = [c for c in range(520) if c != 100]
+    ref.check(dw[0][:, most], (ww[0][0][:, most], ww[1][0][:, most]), "dw")
+    ref.check(db, wb, "db")
+    assert bool(dw[1].isnan().all()) and not torch.isfinite(dw[3]).any()
+    most = [c for c in range(520) if c != 7]
+    ref.check(dw[2][:, most], (ww[0][2][:, most], ww[1][2][:, most]), "dw")
+    assert torch.isinf(dw[2][:, 7]).all()
