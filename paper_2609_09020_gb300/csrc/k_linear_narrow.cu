@@ -34,7 +34,13 @@
 //
 // An infinite or NaN value among fp32 pieces would spread (inf 0 = NaN): its tile
 // is marked, and dx and dw of that tile are computed again on the FP32 cores.
+//
+// GROUPED (include/pic_group.h): a tile is 128 rows of one group, and a CTA has a piece of
+// one group's tiles.  Pieces are about as long as can be for as many of them as there are
+// CTAs at once (or a multiple of that).  A group's last tile ends with it: what is behind is
+// zero in dz and x, and dx is not written there.
 #include "cut3.cuh"
+#include "group.cuh"
 #include "k_linear_tc.cuh"
 
 namespace pic {
@@ -57,6 +63,11 @@ struct NarrowParams {
   int raw_z, raw_x;         // where z and x begin in it
   float* parts;  // [CTAs][N K + N]
   Waits waits;
+  // grouped
+  const long long* offsets;
+  int groups;
+  int pieces;  // at most, and so many CTAs
+  long long w_group, dw_group, db_group;
 };
 
 // How dy, z and x arrive: through registers, by TMA, as runs of memory.
@@ -214,7 +225,28 @@ struct NarrowMaps {
   CUtensorMap dx, dy, z, x;
 };
 
-template <typename T, bool WIDE, Source SRC>
+// The pieces of a grouped call: the table's tiles become pieces.  Their longest length, in
+// tiles, is the least of 32 between the even share of all tiles and one with which there
+// certainly are no more than `pieces` (every group has one that is not full).  Whole warps.
+__device__ __forceinline__ void make_pieces(grp::GroupTable& table, const NarrowParams& q, long long rows, int* scratch) {
+  grp::make_table(table, q.offsets, q.groups, rows, kTile, 0, q.waits.status);
+  const int all = table.tiles[q.groups], lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const int lo = max(1, (all + q.pieces - 1) / q.pieces), hi = max(lo, (all + q.pieces - q.groups) / (q.pieces - q.groups + 1));
+  if (threadIdx.x == 0) *scratch = hi;
+  __syncthreads();
+  for (int i = threadIdx.x >> 5; i < 32; i += warps) {
+    const int length = lo + static_cast<int>((hi - lo) * static_cast<long long>(i) / 32);
+    int n = 0;
+    for (int g = lane; g < q.groups; g += 32) n += (table.tiles[g + 1] - table.tiles[g] + length - 1) / length;
+    if (__reduce_add_sync(0xffffffffu, n) <= q.pieces && lane == 0) atomicMin(scratch, length);
+  }
+  __syncthreads();
+  const int length = *scratch;
+  __syncthreads();
+  grp::make_table(table, q.offsets, q.groups, rows, kTile * length, 0, q.waits.status);
+}
+
+template <typename T, bool WIDE, Source SRC, bool GROUPED>
 __global__ void __launch_bounds__(kThreads, 1)
     narrow_kernel(const __grid_constant__ NarrowParams q, const __grid_constant__ NarrowMaps maps) {
   using S = Shape<T, WIDE, SRC>;
@@ -223,7 +255,23 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* smem = smem_raw + ((1024 - (raw & 1023)) & 1023);
   const uint32_t base = tc::smem_addr(smem);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const NarrowGrad& g = q.g;
+  // this CTA's tiles, every step-th: rows origin + tile kTile and on
+  long long first = blockIdx.x, last = q.tiles, step = gridDim.x, origin = 0;
+  NarrowGrad of_group;  // I is the group's end, and w its weights
+  if constexpr (GROUPED) {
+    grp::GroupTable& table = *reinterpret_cast<grp::GroupTable*>(smem);  // (where the stages will be)
+    make_pieces(table, q, q.g.I, reinterpret_cast<int*>(smem + sizeof(grp::GroupTable)));
+    if (static_cast<int>(blockIdx.x) >= table.tiles[q.groups]) return;
+    const int at = table.find(blockIdx.x, q.groups);
+    const long long pieces = table.tiles[at + 1] - table.tiles[at], piece = blockIdx.x - table.tiles[at],
+                    tiles = (table.rows(at) + kTile - 1) / kTile;
+    first = piece * tiles / pieces, last = (piece + 1) * tiles / pieces, step = 1, origin = table.start[at];
+    of_group = q.g;
+    of_group.I = table.start[at + 1];
+    of_group.w = static_cast<const T*>(q.g.w) + at * q.w_group;
+    __syncthreads();
+  }
+  const NarrowGrad& g = GROUPED ? of_group : q.g;
   const uint32_t bars = base + S::kOffBars;
   const uint32_t bar_full = bars, bar_empty = bars + 8 * S::kStages, bar_landed = bar_empty + 8 * S::kStages,
                  bar_taken = bar_landed + 8 * kMaxRing, bar_dx = bar_taken + 8 * kMaxRing,
@@ -302,9 +350,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     int s = 0, count = 0;
     uint32_t phase = 0;
     if constexpr (SRC == kTma) {
-      for (long long tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
+      for (long long tile = first; tile < last; tile += step) {
         if (!__all_sync(0xffffffffu, wait(bar_landed + 8 * s, phase))) break;
         const uint32_t sdz = base + s * S::kStageBytes, sz = sdz + 2 * S::kPlaneBytes;
+        bool gone[4] = {};
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const int r = row + u * S::kPassRows;
@@ -316,6 +365,15 @@ __global__ void __launch_bounds__(kThreads, 1)
             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                          : "=r"(vz[u].w[0]), "=r"(vz[u].w[1]), "=r"(vz[u].w[2]), "=r"(vz[u].w[3])
                          : "r"(sz + at));
+          // rows behind the group's
+          if constexpr (GROUPED) {
+            gone[u] = origin + tile * kTile + r >= g.I;
+            if (gone[u]) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) vy[u].w[i] = vz[u].w[i] = 0;
+              if (g.dw) tc::sts128(sdz + S::kPlaneBytes + at, 0, 0, 0, 0);
+            }
+          }
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -328,6 +386,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[i] = pack2_of<T>(d[2 * i], d[2 * i + 1]);
             put_vec<T>(sdz, S::kBlockBytes, S::kPlaneBytes, row + u * S::kPassRows, col, w);
+          } else if (GROUPED && gone[u]) {
+            put_vec<T>(sdz, S::kBlockBytes, S::kPlaneBytes, row + u * S::kPassRows, col, vy[u].w);
           }
 #pragma unroll
           for (int e = 0; e < S::kPer; ++e) sum[e] += d[e];
@@ -338,16 +398,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (++s == S::kStages) s = 0, phase ^= 1;
       }
     } else {
-    if (SRC == kReg && blockIdx.x < q.tiles) load_dz(blockIdx.x * static_cast<long long>(kTile));
+    if (SRC == kReg && first < last) load_dz(origin + first * kTile);
     int raw = 0;
     uint32_t raw_phase = 0;
-    for (long long tile = blockIdx.x; tile < q.tiles; tile += gridDim.x, ++count) {
+    for (long long tile = first; tile < last; tile += step, ++count) {
       uint32_t largest = 0;
       bool ok = true;
       if (SRC == kRun && !__all_sync(0xffffffffu, wait(bar_landed + 8 * raw, raw_phase))) break;
 #pragma unroll
       for (int unit = 0; unit < S::kUnits; ++unit) {
-        const long long i0 = tile * kTile + unit * S::kUnitRows;
+        const long long i0 = origin + tile * kTile + unit * S::kUnitRows;
         if constexpr (SRC == kRun) {
           const uint32_t from = base + S::kOffRaw + raw * q.raw_bytes;
           constexpr int kElem = sizeof(T);
@@ -399,8 +459,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (SRC == kRun) {
         } else if (unit + 1 < S::kUnits)
           load_dz(i0 + S::kUnitRows);
-        else if (tile + gridDim.x < q.tiles)
-          load_dz((tile + gridDim.x) * kTile);
+        else if (tile + step < last)
+          load_dz(origin + (tile + step) * kTile);
         if (g.dw) {
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
@@ -438,8 +498,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t dz_lbo = WIDE && g.N > 64 ? S::kBlockBytes : 0;
       int s = 0, buf = 0;
       uint32_t phase = 0, free_phase = 0;
-      bool ok = true, first = true;
-      for (long long tile = blockIdx.x; tile < q.tiles && ok; tile += gridDim.x) {
+      bool ok = true, begin = true;
+      for (long long tile = first; tile < last && ok; tile += step) {
         if (!(ok = wait(bar_full + 8 * s, phase) && (SRC != kTma || wait(bar_landed + 8 * s, phase)))) break;
         tc::tc_fence_after();
         const uint32_t sdz = base + s * S::kStageBytes, sx = sdz + S::kPlanes * S::kPlaneBytes, sw = base + S::kOffW;
@@ -471,10 +531,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int kk = 0; kk < kTile / 16; ++kk)
               tc::mma_16<1>(d, tc::smem_desc_sw128(sdz + pa * S::kPlaneBytes + kk * 2048, dz_lbo, 1024),
                             tc::smem_desc_sw128(sx + pb * S::kPlaneBytes + kk * 2048, S::kBlockBytes, 1024), idesc_dw,
-                            ((S::kPlanes == 1 && !first) || t > 0 || kk > 0) ? 1u : 0u);
+                            ((S::kPlanes == 1 && !begin) || t > 0 || kk > 0) ? 1u : 0u);
           }
           if (S::kPlanes == 3) tc::mma_commit(bar_dw + 8 * buf);
-          first = false;
+          begin = false;
         }
         tc::mma_commit(bar_empty + 8 * s);
         if (++s == S::kStages) s = 0, phase ^= 1;
@@ -486,7 +546,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (SRC == kRun && warp == kTmaWarp) {
     if (tc::elect_one()) {
       constexpr long long kElem = sizeof(T);
-      for (long long tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
+      for (long long tile = first; tile < last; tile += step) {
         if (!wait(bar_taken + 8 * ring_s, ring_phase ^ 1)) break;
         const uint32_t at = base + S::kOffRaw + ring_s * q.raw_bytes, bar = bar_landed + 8 * ring_s;
         const long long rows = min(static_cast<long long>(kTile), g.I - tile * kTile);
@@ -519,10 +579,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (tc::elect_one()) {
       const bool has_z = g.act != PIC_ACT_NONE;
       const uint32_t bytes = S::kPlaneBytes * (1 + (g.dw ? 1 : 0) + (has_z ? 1 : 0));
-      for (long long tile = blockIdx.x; tile < q.tiles; tile += gridDim.x) {
+      for (long long tile = first; tile < last; tile += step) {
         if (!wait(bar_empty + 8 * ring_s, ring_phase ^ 1)) break;
         const uint32_t at = base + ring_s * S::kStageBytes, bar = bar_landed + 8 * ring_s;
-        const int i = static_cast<int>(tile * kTile);
+        const int i = static_cast<int>(origin + tile * kTile);
         tc::mbar_arrive_expect_tx(bar, bytes);
         tc::tma_load_2d<false>(at, &maps.dy, 0, i, bar);
         if (has_z) tc::tma_load_2d<false>(at + 2 * S::kPlaneBytes, &maps.z, 0, i, bar);
@@ -539,11 +599,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     int buf = 0, pb = 0, count = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (long long tile = blockIdx.x; g.dx && tile < q.tiles; tile += gridDim.x, ++count) {
+    for (long long tile = first; g.dx && tile < last; tile += step, ++count) {
       ok = __all_sync(0xffffffffu, wait(bar_dx + 8 * buf, phase));
       if (!ok) break;
       tc::tc_fence_after();
-      const long long row0 = tile * kTile + warp * 32;
+      const long long row0 = origin + tile * kTile + warp * 32;
 #pragma unroll
       for (int b = 0; b < S::kBlocks; ++b) {
         uint32_t r[64];
@@ -576,7 +636,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           if (lane == 0) tc::bulk_wait_read<S::kPanels - 1>();
           __syncwarp();
-          put_panel<T>(out, panels + pb * kPanelBytes, lane, row0, 64 * b + 32 * h, p, g.dx, g.lddx, &maps.dx, q.store_tma);
+          put_panel<T>(out, panels + pb * kPanelBytes, lane, row0, 64 * b + 32 * h, p, g.dx, g.lddx, &maps.dx,
+                       q.store_tma && (!GROUPED || row0 + 32 <= g.I));
           if (++pb == S::kPanels) pb = 0;
         }
       }
@@ -605,12 +666,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     float v[64] = {};
     int buf = 0, count = 0;
     uint32_t phase = 0;
-    for (long long tile = blockIdx.x; tile < q.tiles; tile += gridDim.x, ++count) {
+    for (long long tile = first; tile < last; tile += step, ++count) {
       if (!__all_sync(0xffffffffu, wait(bar_dw + 8 * buf, phase))) break;
       tc::tc_fence_after();
       if (marks[count % kMarks] == count + 1) {
         float u[64];
-        dw_again(u, g, tile * kTile, n);
+        dw_again(u, g, origin + tile * kTile, n);
 #pragma unroll
         for (int c = 0; c < 64; ++c) v[c] += u[c];
       } else {
@@ -699,7 +760,7 @@ bool plan_runs(NarrowParams& q) {
 
 template <typename T, bool WIDE, Source SRC>
 int run(const NarrowGrad& g, NarrowParams& q, NarrowMaps& maps, int grid, int slot, cudaStream_t s) {
-  const void* fn = reinterpret_cast<const void*>(narrow_kernel<T, WIDE, SRC>);
+  const void* fn = reinterpret_cast<const void*>(narrow_kernel<T, WIDE, SRC, false>);
   const int fixed = Shape<T, WIDE, SRC>::kSmem;
   const int smem = SRC == kRun ? 227 * 1024 : fixed;  // the attribute is set once, for runs of any width
   static_assert(Shape<T, WIDE, SRC>::kSmem <= 227 * 1024, "shared memory of an SM");
@@ -713,7 +774,107 @@ int run(const NarrowGrad& g, NarrowParams& q, NarrowMaps& maps, int grid, int sl
   return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
 }
 
+// Pieces of a grouped call, at most: as many CTAs as are there at once, or a multiple of
+// that, so that every second one may be a group's rest and (16-bit types) none has to
+// be longer than kMostTiles.  With few tiles, one each.
+long long pieces_of(const NarrowGrad& g, int groups, int dtype) {
+  const long long tiles = g.I / kTile + groups;
+  long long least = 2LL * groups;
+  if (dtype != PIC_DTYPE_F32 && tiles / kMostTiles + groups > least) least = tiles / kMostTiles + groups;
+  const long long want = (least + kSms - 1) / kSms * kSms;
+  return tiles < want ? tiles : want;
+}
+
+// dw and db of the groups from their pieces' parts.  MANY of a group: a block finishes 32
+// values, its warps add every 32nd part; else a thread a value.
+template <typename T, bool MANY>
+__global__ void __launch_bounds__(MANY ? 1024 : 256) add_group_parts_kernel(const NarrowParams q) {
+  __shared__ grp::GroupTable table;
+  __shared__ float sums[MANY ? 32 : 1][32];
+  __shared__ int scratch;
+  const NarrowGrad& g = q.g;
+  make_pieces(table, q, g.I, &scratch);
+  const int at = blockIdx.y, nk = g.N * g.K, per = nk + g.N;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int e = MANY ? blockIdx.x * 32 + lane : blockIdx.x * 256 + threadIdx.x;
+  float v = 0.0f;
+  if (e < per) {
+#pragma unroll 5
+    for (int c = table.tiles[at] + (MANY ? warp : 0); c < table.tiles[at + 1]; c += MANY ? 32 : 1)
+      v += __ldcg(q.parts + c * static_cast<long long>(per) + e);
+  }
+  if (MANY) {
+    sums[warp][lane] = v;
+    __syncthreads();
+    if (warp > 0) return;
+#pragma unroll
+    for (int w = 1; w < 32; ++w) v += sums[w][lane];
+  }
+  if (e >= per) return;
+  if (e >= nk) {
+    if (g.db) static_cast<T*>(g.db)[at * q.db_group + e - nk] = from_f32<T>(v);
+  } else if (g.dw) {
+    static_cast<T*>(g.dw)[at * q.dw_group + e / g.K * g.lddw + e % g.K] = from_f32<T>(v);
+  }
+}
+
+template <typename T, bool WIDE, Source SRC>
+int run_groups(NarrowParams& q, NarrowMaps& maps, int slot, cudaStream_t s) {
+  const void* fn = reinterpret_cast<const void*>(narrow_kernel<T, WIDE, SRC, true>);
+  constexpr int smem = Shape<T, WIDE, SRC>::kSmem;
+  static_assert(smem <= 227 * 1024 && sizeof(grp::GroupTable) + 4 <= Shape<T, WIDE, SRC>::kOffW, "shared memory of an SM");
+  if (allow_smem(fn, slot, smem) != PIC_OK) return PIC_ERR_CUDA;
+  void* args[] = {&q, &maps};
+  if (cudaLaunchKernel(fn, dim3(q.pieces), dim3(kThreads), args, smem, s) != cudaSuccess) return PIC_ERR_CUDA;
+  if (q.g.dw || q.g.db) {
+    const int per = q.g.N * q.g.K + q.g.N;
+    if (q.pieces / q.groups >= 16)
+      add_group_parts_kernel<T, true><<<dim3((per + 31) / 32, q.groups), 1024, 0, s>>>(q);
+    else
+      add_group_parts_kernel<T, false><<<dim3((per + 255) / 256, q.groups), 256, 0, s>>>(q);
+  }
+  return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+}
+
 }  // namespace
+
+bool narrow_group_takes(const NarrowGrad& g, int groups, int dtype) { return g.I > 0 && narrow_takes(g, dtype); }
+
+long long narrow_group_workspace(const NarrowGrad& g, int groups, int dtype) {
+  return pieces_of(g, groups, dtype) * (g.N * g.K + g.N) * 4LL;
+}
+
+int narrow_group_grad(const NarrowGroups& a, int dtype, void* ws, const Waits& waits, cudaStream_t s) {
+  const NarrowGrad& g = a.g;
+  NarrowParams q{};
+  const int elem = dtype == PIC_DTYPE_F32 ? 4 : 2;
+  const auto on16 = [&](const void* m, long long ld) { return reinterpret_cast<uintptr_t>(m) % 16 == 0 && ld * elem % 16 == 0; };
+  const auto far = [&](long long ld) { return ld * elem >= (1LL << 40); };
+  q.g = g;
+  q.vec_dy = on16(g.dy, g.lddy), q.vec_z = on16(g.pre, g.ldpre), q.vec_x = on16(g.x, g.ldx);
+  q.store_tma = g.dx && g.K * elem % 16 == 0 && on16(g.dx, g.lddx) && !far(g.lddx);
+  q.parts = static_cast<float*>(ws);
+  q.waits = waits;
+  q.pieces = static_cast<int>(pieces_of(g, a.groups, dtype));
+  q.offsets = a.offsets, q.groups = a.groups, q.w_group = a.w_group, q.dw_group = a.dw_group, q.db_group = a.db_group;
+  NarrowMaps maps{};
+  if (q.store_tma && !encode(&maps.dx, g.dx, g.I, g.K, g.lddx, 32, dtype)) return PIC_ERR_CUDA;
+  const bool wide = g.N > 64 || g.K > 64, has_z = g.act != PIC_ACT_NONE;
+  const bool tma = dtype != PIC_DTYPE_F32 && !wide && q.vec_dy && !far(g.lddy) && (!has_z || (q.vec_z && !far(g.ldpre))) &&
+                   (!g.dw || (q.vec_x && !far(g.ldx)));
+  if (tma && !(encode(&maps.dy, g.dy, g.I, g.N, g.lddy, kTile, dtype) &&
+               (!has_z || encode(&maps.z, g.pre, g.I, g.N, g.ldpre, kTile, dtype)) &&
+               (!g.dw || encode(&maps.x, g.x, g.I, g.K, g.ldx, kTile, dtype))))
+    return PIC_ERR_CUDA;
+  if (dtype == PIC_DTYPE_F32) return run_groups<float, false, kReg>(q, maps, 55, s);
+  if (dtype == PIC_DTYPE_F16) {
+    if (tma) return run_groups<__half, false, kTma>(q, maps, 56, s);
+    return wide ? run_groups<__half, true, kReg>(q, maps, 57, s) : run_groups<__half, false, kReg>(q, maps, 58, s);
+  }
+  using B = __nv_bfloat16;
+  if (tma) return run_groups<B, false, kTma>(q, maps, 59, s);
+  return wide ? run_groups<B, true, kReg>(q, maps, 60, s) : run_groups<B, false, kReg>(q, maps, 61, s);
+}
 
 bool narrow_takes(const NarrowGrad& g, int dtype) {
   const int most = dtype == PIC_DTYPE_F32 ? 64 : 128;

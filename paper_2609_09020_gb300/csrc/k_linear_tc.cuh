@@ -161,7 +161,7 @@ template <typename T>
 __device__ __forceinline__ void put_panel(const uint32_t (&v)[32], uint32_t buf, int lane, long long row0, long long col0,
                                           const Product& p, void* out, long long ld, const CUtensorMap* map,
                                           bool by_tma) {
-  if (!by_tma && row0 + 32 <= p.I && packed_rows<T>(out, ld, p)) {
+  if (!by_tma && row0 + 32 <= p.I && packed_rows<T>(out, ld, p) && row0 * p.J * static_cast<int>(sizeof(T)) % 16 == 0) {
     // as the rows lie in memory, and out in one copy
     const int n = static_cast<int>(p.J);
     const uint32_t row = buf + lane * n * sizeof(T);

@@ -350,5 +350,17 @@ bool narrow_takes(const NarrowGrad& g, int dtype);
 long long narrow_workspace(const NarrowGrad& g, int dtype);
 int narrow_grad(const NarrowGrad& g, int dtype, void* ws, const Waits& waits, cudaStream_t s);
 
+// The same for the groups of include/pic_group.h: g's matrices are those of all rows, w, dw
+// and db the first group's.
+struct NarrowGroups {
+  NarrowGrad g;
+  const long long* offsets;
+  int groups;
+  long long w_group, dw_group, db_group;
+};
+bool narrow_group_takes(const NarrowGrad& g, int groups, int dtype);
+long long narrow_group_workspace(const NarrowGrad& g, int groups, int dtype);
+int narrow_group_grad(const NarrowGroups& a, int dtype, void* ws, const Waits& waits, cudaStream_t s);
+
 }  // namespace lin
 }  // namespace pic

@@ -84,6 +84,15 @@ int forward(const pic_grouped_linear_args& a, pic::lin::Arena& ws, bool launch, 
 int backward(const pic_grouped_linear_grad_args& a, pic::lin::Arena& ws, bool launch, const pic::lin::Waits& w, cudaStream_t s) {
   const long long M = a.rows, K = a.in_features, N = a.out_features;
   int rc = PIC_OK;
+  if (N <= 128 && K <= 128) {
+    const pic::lin::NarrowGroups n{{a.dy, a.lddy, a.pre, a.ldpre, a.x, a.ldx, a.w, a.ldw, a.dx, a.lddx, a.dw, a.lddw, a.db, M,
+                                    static_cast<int>(N), static_cast<int>(K), a.act},
+                                   offsets_of(a.offsets), a.groups, a.w_group, a.dw_group, a.db_group};
+    if (pic::lin::narrow_group_takes(n.g, a.groups, a.dtype)) {
+      void* room = ws.take(pic::lin::narrow_group_workspace(n.g, a.groups, a.dtype));
+      return launch ? pic::lin::narrow_group_grad(n, a.dtype, room, w, s) : PIC_OK;
+    }
+  }
   // dz: dy itself where there is no activation
   const void* dz = a.dy;
   long long lddz = a.lddy;

@@ -409,3 +409,44 @@ def test_large_fp32_not_finite(pic):
     most = [c for c in range(520) if c != 7]
     ref.check(dw[2][:, most], (ww[0][2][:, most], ww[1][2][:, most]), "dw")
     assert torch.isinf(dw[2][:, 7]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("inp,outp", [(64, 64), (40, 24), (7, 64), (128, 96), (64, 3)], ids=str)
+def test_narrow_gradients(pic, inp, outp, dtype):
+    """Narrow layers over many rows: groups of one row, of none, that end on and off tiles, more groups than
+    CTAs, fewer tiles than CTAs, and one group of all."""
+    rng = random.Random(inp)
+    many = [5]
+    for _ in range(700):
+        many.append(many[-1] + rng.choice([0, 1, 2, 3, 40, 127, 128, 129]))
+    for offsets in ([0, 1, 1, 2, 130, 1153, 2000, 2001], [0, 0, 1024, 1024], [0, 30000], many, [3, 900, 1500]):
+        rows = offsets[-1] + 4
+        check_backward(pic, offsets, rows, inp, outp, dtype, "gelu", seed=outp)
+    check_backward(pic, [0, 700, 1800], 1900, inp, outp, dtype, "none")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_narrow_groups_keep_to_themselves(pic, bad, dtype):
+    """As test_groups_keep_to_themselves, over enough rows for the one-pass gradient."""
+    offsets, rows = [2, 537, 1100, 1100, 2235], 2240
+    for inp, outp in ((64, 64), (24, 40), (128, 72)):
+        x, w, b = case(rows, 4, inp, outp, dtype, 0)
+        dy, z = normal((rows, outp), dtype, 4), normal((rows, outp), dtype, 5)
+        for t in (x, dy, z):
+            t[:2] = bad
+            t[537:1100] = bad
+            t[2235:] = bad
+        w[1], w[2] = bad, bad
+        for act in ("gelu", "none"):
+            dx, dw, db = pic.grouped_linear_backward(dy, x, w, offsets_tensor(offsets), act=act, pre=z)
+            wx, ww, wb = group_ref.backward(dy, x, w, z, offsets, act)
+            for i, j in ((2, 537), (1100, 2235)):
+                ref.check(dx[i:j], (wx[0][i:j], wx[1][i:j]), "dx")
+            for g in (0, 3):
+                ref.check(dw[g], (ww[0][g], ww[1][g]), "dw")
+                ref.check(db[g], (wb[0][g], wb[1][g]), "db")
+            assert not dw[2].any() and not db[2].any()
+            assert not torch.isfinite(dw[1]).any() and not torch.isfinite(db[1]).any()
+        pic.grouped_linear_check()
