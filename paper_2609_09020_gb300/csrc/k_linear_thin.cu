@@ -19,13 +19,13 @@ int mode_of(const void* m, long long ld, const Product& p, int elem) {
 }
 
 // A kernel's shared memory allowed once per device.
-int allow(const void* fn, int slot) {
-  static std::atomic<uint64_t> done[3 * 2 * 16];
+int allow(const void* fn, int slot, int fixed) {
+  static std::atomic<uint64_t> done[2 * 3 * 2 * 16];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return PIC_ERR_CUDA;
   const uint64_t bit = 1ull << (dev & 63);
   if (done[slot].load(std::memory_order_acquire) & bit) return PIC_OK;
-  if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemSm - 2048) != cudaSuccess) return PIC_ERR_CUDA;
+  if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemSm - fixed) != cudaSuccess) return PIC_ERR_CUDA;
   done[slot].fetch_or(bit, std::memory_order_release);
   return PIC_OK;
 }
@@ -45,7 +45,9 @@ bool thin_takes(const Product& p, int dtype) {
          p.ldy % 8 != 0 || (reinterpret_cast<uintptr_t>(p.a) | reinterpret_cast<uintptr_t>(p.y)) % 16 != 0;
 }
 
-int thin_product(const Product& p, int dtype, cudaStream_t s) {
+namespace {
+// groups: null, or those of a grouped call
+int launch_thin(const Product& p, int dtype, const ThinGroups* groups, cudaStream_t s) {
   const int elem = dtype == PIC_DTYPE_F32 ? 4 : 2;
   const int columns = static_cast<int>(p.J);
   ThinParams q{};
@@ -55,24 +57,53 @@ int thin_product(const Product& p, int dtype, cudaStream_t s) {
   q.res_mode = mode_of(p.residual, p.ldr, p, elem);
   const bool x16 = reinterpret_cast<uintptr_t>(p.a) % 16 == 0 && p.a_i * elem % 16 == 0;
   const bool fast = x16 && q.y_mode == kThinVector && q.pre_mode == kThinVector && q.res_mode == kThinVector;
-  const ThinKernel k = dtype == PIC_DTYPE_F32   ? thin_kernel_f32(columns, fast)
+  const ThinKernel k = groups ? dtype == PIC_DTYPE_F32   ? thin_group_kernel_f32(columns, fast)
+                                : dtype == PIC_DTYPE_F16 ? thin_group_kernel_f16(columns, fast)
+                                                         : thin_group_kernel_bf16(columns, fast)
+                       : dtype == PIC_DTYPE_F32 ? thin_kernel_f32(columns, fast)
                        : dtype == PIC_DTYPE_F16 ? thin_kernel_f16(columns, fast)
                                                 : thin_kernel_bf16(columns, fast);
   q.steps = static_cast<int>((p.K * elem + 127) / 128);
   q.pieces = static_cast<int>((p.K * elem + 63) / 64);
   q.ragged = p.K * elem % 16 != 0;
   q.w16 = reinterpret_cast<uintptr_t>(p.b) % 16 == 0 && p.b_j * elem % 16 == 0;
+  long long tiles = (p.I + kThinRows - 1) / kThinRows;
+  if (groups) {
+    q.w16 = q.w16 && (groups->groups == 1 || groups->w_group * elem % 16 == 0);
+    q.offsets = groups->offsets, q.groups = groups->groups, q.status = groups->status;
+    q.w_group = groups->w_group, q.bias_group = groups->bias_group;
+    tiles = p.I / kThinRows + groups->groups;
+  }
   const bool panels = q.y_mode != kThinVector || q.pre_mode != kThinVector || q.res_mode != kThinVector;
   q.panel_at = q.steps * k.step_bytes;
   q.panel_bytes = panels ? kThinRows * columns * elem : 0;
-  q.tiles = (p.I + kThinRows - 1) / kThinRows;
+  q.tiles = tiles;
   const int smem = q.panel_at + kThinWarps * q.panel_bytes;
-  const int slot = (dtype * 2 + fast) * 16 + k.tiles - 1;
-  if (smem > 46 * 1024 && allow(k.fn, slot) != PIC_OK) return PIC_ERR_CUDA;
-  const long long ctas = std::min(k.ctas, kSmemSm / (smem + 2048));
+  const int slot = ((groups != nullptr) * 3 * 2 + dtype * 2 + fast) * 16 + k.tiles - 1;
+  const int fixed = groups ? 11 * 1024 : 2048;  // of a CTA, beside that
+  if (smem + fixed > 48 * 1024 && allow(k.fn, slot, fixed) != PIC_OK) return PIC_ERR_CUDA;
+  const long long ctas = std::min(k.ctas, kSmemSm / (smem + fixed));
   const long long grid = std::min(kSms * ctas, q.tiles);
   void* args[] = {&q};
   return launch_kernel(k.fn, grid, kThinThreads, smem, 1, args, s);
+}
+}  // namespace
+
+int thin_product(const Product& p, int dtype, cudaStream_t s) { return launch_thin(p, dtype, nullptr, s); }
+
+// Not many 16-bit rows of whole slices of K that, like those of y and pre, start on 16-byte
+// boundaries: the tiled kernel wastes nothing there.  us, here / tiled, fp16, 24 groups:
+// 1000000 x 64 -> 64 keeping z 77.5 / 67.4, 200000 x 128 -> 128 28.9 / 28.9; but 40 -> 40 14.6 /
+// 22.3, 7 -> 64 20.8 / 24.2, 64 -> 3 28.2 / 33.0, 2000 x 64 -> 64 7.0 / 9.1.
+bool thin_group_takes(const Product& p, int dtype) {
+  if (!thin_takes(p, dtype)) return false;
+  const auto on16 = [](const void* m, long long ld) { return reinterpret_cast<uintptr_t>(m) % 16 == 0 && ld % 8 == 0; };
+  return dtype == PIC_DTYPE_F32 || p.K % 64 != 0 || p.J % 8 != 0 || p.I < 16384 || !on16(p.a, p.a_i) || !on16(p.y, p.ldy) ||
+         (p.pre && !on16(p.pre, p.ldpre));
+}
+
+int thin_group_product(const Product& p, int dtype, const ThinGroups& groups, cudaStream_t s) {
+  return launch_thin(p, dtype, &groups, s);
 }
 
 }  // namespace lin

@@ -30,9 +30,14 @@
 //
 // While a step (128 bytes of each row) is multiplied, the next, of this tile or the
 // warp's next, is on its way.
+//
+// GROUPED (include/pic_group.h): a tile is 16 rows of one group.  A CTA has a piece of the
+// tiles of one group after another: it makes that group's fragments of the weights, and its
+// warps take the piece's tiles.
 #pragma once
 
 #include "cut3.cuh"
+#include "group.cuh"
 #include "linear.cuh"
 #include "linear_ptx.cuh"
 
@@ -54,6 +59,11 @@ struct ThinParams {
   int y_mode, pre_mode, res_mode;  // a FAST kernel's are kThinVector
   int panel_at, panel_bytes;  // a warp's panel, where a mode needs it
   long long tiles;
+  // grouped
+  const long long* offsets;
+  int groups;
+  long long w_group, bias_group;
+  int* status;
 };
 
 // Groups of neighbouring columns: 32 of a 16-bit type (the last may have 16), 16 of fp32.
@@ -115,33 +125,55 @@ constexpr int thin_ctas() {
   return NT <= 8 || !FAST ? 2 : 1;
 }
 
+template <bool GROUPED>
+struct ThinTable {
+  using Type = grp::GroupTable;
+};
+template <>
+struct ThinTable<false> {
+  struct Type {};
+};
+
 // FAST: rows of every matrix start and end on 16-byte boundaries (x's may end anywhere).
-template <typename T, int NT, bool FAST>
+template <typename T, int NT, bool FAST, bool GROUPED>
 __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_kernel(const __grid_constant__ ThinParams q) {
   using S = ThinShape<T, NT>;
   constexpr int E = S::kElem;
   extern __shared__ __align__(16) uint8_t thin_smem[];
   __shared__ __align__(8) float bias[NT * 8];
-  const Product& p = q.p;
+  Product of_group;  // grouped: I is the group's end
+  if constexpr (GROUPED) of_group = q.p;
+  const Product& p = GROUPED ? of_group : q.p;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int J = static_cast<int>(p.J), K = static_cast<int>(p.K);
 
-  const long long first = warp * static_cast<long long>(gridDim.x) + blockIdx.x;  // few tiles: over all SMs
-  const long long stride = gridDim.x * static_cast<long long>(kThinWarps);
+  // this warp's tiles: rows origin + 16 tile and on
+  long long first = warp * static_cast<long long>(gridDim.x) + blockIdx.x, last = q.tiles;  // few tiles: over all SMs
+  const long long stride = GROUPED ? kThinWarps : gridDim.x * static_cast<long long>(kThinWarps);
+  long long origin = 0;
+  // grouped: the CTA's tiles of all groups'
+  __shared__ typename ThinTable<GROUPED>::Type table;
+  long long next_piece = 0, end_piece = 1;
+  if constexpr (GROUPED) {
+    grp::make_table(table, q.offsets, q.groups, q.p.I, kThinRows, 0, q.status);
+    const long long all = table.tiles[q.groups];
+    next_piece = blockIdx.x * all / gridDim.x;
+    end_piece = (blockIdx.x + 1LL) * all / gridDim.x;
+  }
   const char* a = static_cast<const char*>(p.a);
   const long long lda = p.a_i * E;
   const int k_bytes = K * E;
   uint8_t* panel = thin_smem + q.panel_at + warp * q.panel_bytes;
   // bytes of a tile's rows that lie end to end (a multiple of 16 but for the last tile's)
   const auto run_bytes = [&](long long tile) {
-    return static_cast<int>(min(static_cast<long long>(kThinRows), p.I - tile * kThinRows)) * J * E;
+    return static_cast<int>(min(static_cast<long long>(kThinRows), p.I - origin - tile * kThinRows)) * J * E;
   };
 
   Piece16<FAST> next[2][2];  // rows g and g + 8; the pieces of a step
   const auto fetch = [&](long long tile, int step) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const long long row = tile * kThinRows + g + 8 * h;
+      const long long row = origin + tile * kThinRows + g + 8 * h;
       const char* r = a + row * lda;
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
@@ -184,7 +216,27 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
       }
     }
   };
-  if (first < q.tiles) {
+  while (next_piece < end_piece) {
+  int y_mode = q.y_mode, pre_mode = q.pre_mode;
+  if constexpr (GROUPED) {
+    const int at = table.find(static_cast<int>(next_piece), q.groups);
+    first = next_piece - table.tiles[at] + warp;
+    next_piece = min(end_piece, static_cast<long long>(table.tiles[at + 1]));
+    last = next_piece - table.tiles[at];
+    origin = table.start[at];
+    of_group.I = table.start[at + 1];
+    of_group.b = static_cast<const T*>(q.p.b) + at * q.w_group;
+    if (q.p.bias) of_group.bias = static_cast<const T*>(q.p.bias) + at * q.bias_group;
+    // 16 rows are a run on a boundary only where the group begins on one
+    if (!FAST && origin * J * E % 16 != 0) {
+      if (y_mode == kThinRun) y_mode = kThinElements;
+      if (pre_mode == kThinRun) pre_mode = kThinElements;
+    }
+    __syncthreads();  // the group's before is done with
+  } else {
+    next_piece = end_piece;
+  }
+  if (first < last) {
     fetch(first, 0);
     if (p.residual) fetch_residual(first);
   }
@@ -238,8 +290,8 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
       acc[j][0] += b.x, acc[j][1] += b.y, acc[j][2] += b.x, acc[j][3] += b.y;
     }
   };
-  for (long long tile = first; tile < q.tiles; tile += stride) {
-    const long long row0 = tile * kThinRows, row = row0 + g;
+  for (long long tile = first; tile < last; tile += stride) {
+    const long long row0 = origin + tile * kThinRows, row = row0 + g;
     float acc[NT][4];
 #pragma unroll
     for (int j = 0; j < NT; ++j)
@@ -260,9 +312,9 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
           if (q.ragged && step == q.steps - 1) keep_bytes<T>(x[h][c], left);
         }
       }
-      const bool last = step + 1 == q.steps;
-      const long long next_tile = last ? tile + stride : tile;
-      if (next_tile < q.tiles) fetch(next_tile, last ? 0 : step + 1);
+      const bool done = step + 1 == q.steps;
+      const long long next_tile = done ? tile + stride : tile;
+      if (next_tile < last) fetch(next_tile, done ? 0 : step + 1);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         if (step * 2 + c >= q.pieces) break;
@@ -366,7 +418,7 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
           for (int c = lane; c < J; c += 32) o[r * ld + c] = reinterpret_cast<const T*>(panel)[r * J + c];
       }
     };
-    if (p.pre) put(p.pre, p.ldpre, q.pre_mode);
+    if (p.pre) put(p.pre, p.ldpre, pre_mode);
     if (p.act == PIC_ACT_RELU) {
 #pragma unroll
       for (int j = 0; j < NT; ++j)
@@ -430,9 +482,10 @@ __global__ void __launch_bounds__(kThinThreads, thin_ctas<T, NT, FAST>()) thin_k
               if (col < J) acc[j][2 * h + e] += to_f32(reinterpret_cast<const T*>(panel)[(g + 8 * h) * J + col]);
             }
       }
-      if (tile + stride < q.tiles) fetch_residual(tile + stride);
+      if (tile + stride < last) fetch_residual(tile + stride);
     }
-    put(p.y, p.ldy, q.y_mode);
+    put(p.y, p.ldy, y_mode);
+  }
   }
 }
 
@@ -441,23 +494,27 @@ struct ThinKernel {
   const void* fn;
   int tiles, step_bytes, ctas;
 };
-template <typename T, int NT>
+template <typename T, int NT, bool GROUPED>
 ThinKernel thin_kernel_at(bool fast) {
-  return {fast ? reinterpret_cast<const void*>(thin_kernel<T, NT, true>) : reinterpret_cast<const void*>(thin_kernel<T, NT, false>),
+  return {fast ? reinterpret_cast<const void*>(thin_kernel<T, NT, true, GROUPED>)
+               : reinterpret_cast<const void*>(thin_kernel<T, NT, false, GROUPED>),
           NT, ThinShape<T, NT>::kStepBytes, fast ? thin_ctas<T, NT, true>() : thin_ctas<T, NT, false>()};
 }
-template <typename T>
+template <typename T, bool GROUPED>
 ThinKernel thin_kernel_of(int columns, bool fast) {
-  if (columns <= 16) return thin_kernel_at<T, 2>(fast);
-  if (columns <= 32) return thin_kernel_at<T, 4>(fast);
-  if (columns <= 48) return thin_kernel_at<T, 6>(fast);
-  if (columns <= 64) return thin_kernel_at<T, 8>(fast);
-  if (columns <= 96) return thin_kernel_at<T, 12>(fast);
-  return thin_kernel_at<T, 16>(fast);
+  if (columns <= 16) return thin_kernel_at<T, 2, GROUPED>(fast);
+  if (columns <= 32) return thin_kernel_at<T, 4, GROUPED>(fast);
+  if (columns <= 48) return thin_kernel_at<T, 6, GROUPED>(fast);
+  if (columns <= 64) return thin_kernel_at<T, 8, GROUPED>(fast);
+  if (columns <= 96) return thin_kernel_at<T, 12, GROUPED>(fast);
+  return thin_kernel_at<T, 16, GROUPED>(fast);
 }
 ThinKernel thin_kernel_f32(int columns, bool fast);
 ThinKernel thin_kernel_f16(int columns, bool fast);
 ThinKernel thin_kernel_bf16(int columns, bool fast);
+ThinKernel thin_group_kernel_f32(int columns, bool fast);
+ThinKernel thin_group_kernel_f16(int columns, bool fast);
+ThinKernel thin_group_kernel_bf16(int columns, bool fast);
 
 }  // namespace lin
 }  // namespace pic

@@ -4,7 +4,7 @@
 namespace pic {
 namespace lin {
 
-ThinKernel thin_kernel_bf16(int columns, bool fast) { return thin_kernel_of<__nv_bfloat16>(columns, fast); }
+ThinKernel thin_kernel_bf16(int columns, bool fast) { return thin_kernel_of<__nv_bfloat16, false>(columns, fast); }
 
 }  // namespace lin
 }  // namespace pic

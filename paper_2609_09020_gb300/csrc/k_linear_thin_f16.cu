@@ -4,7 +4,7 @@
 namespace pic {
 namespace lin {
 
-ThinKernel thin_kernel_f16(int columns, bool fast) { return thin_kernel_of<__half>(columns, fast); }
+ThinKernel thin_kernel_f16(int columns, bool fast) { return thin_kernel_of<__half, false>(columns, fast); }
 
 }  // namespace lin
 }  // namespace pic

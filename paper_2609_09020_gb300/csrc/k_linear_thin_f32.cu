@@ -4,7 +4,7 @@
 namespace pic {
 namespace lin {
 
-ThinKernel thin_kernel_f32(int columns, bool fast) { return thin_kernel_of<float>(columns, fast); }
+ThinKernel thin_kernel_f32(int columns, bool fast) { return thin_kernel_of<float, false>(columns, fast); }
 
 }  // namespace lin
 }  // namespace pic

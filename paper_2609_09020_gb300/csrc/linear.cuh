@@ -350,6 +350,16 @@ bool narrow_takes(const NarrowGrad& g, int dtype);
 long long narrow_workspace(const NarrowGrad& g, int dtype);
 int narrow_grad(const NarrowGrad& g, int dtype, void* ws, const Waits& waits, cudaStream_t s);
 
+// The groups of a thin product (include/pic_group.h), whose b and bias are the first group's.
+struct ThinGroups {
+  const long long* offsets;
+  int groups;
+  long long w_group, bias_group;
+  int* status;
+};
+bool thin_group_takes(const Product& p, int dtype);
+int thin_group_product(const Product& p, int dtype, const ThinGroups& groups, cudaStream_t s);
+
 // The same for the groups of include/pic_group.h: g's matrices are those of all rows, w, dw
 // and db the first group's.
 struct NarrowGroups {

@@ -77,6 +77,16 @@ int forward(const pic_grouped_linear_args& a, pic::lin::Arena& ws, bool launch, 
   p.bias = a.bias, p.bias_group = a.bias_group;
   p.y = a.y, p.ldy = a.ldy, p.pre = a.pre, p.ldpre = a.ldpre, p.act = a.act;
   p.status = w.status;
+  pic::lin::Product t{};
+  t.a = a.x, t.a_i = a.ldx, t.a_k = 1;
+  t.b = a.w, t.b_j = a.ldw, t.b_k = 1;
+  t.I = a.rows, t.J = a.out_features, t.K = a.in_features;
+  t.bias = a.bias;
+  t.y = a.y, t.ldy = a.ldy, t.pre = a.pre, t.ldpre = a.ldpre, t.act = a.act;
+  if (pic::lin::thin_group_takes(t, a.dtype)) {
+    const pic::lin::ThinGroups g{p.offsets, a.groups, a.w_group, a.bias_group, w.status};
+    return launch ? pic::lin::thin_group_product(t, a.dtype, g, s) : PIC_OK;
+  }
   void* room = ws.take(product_workspace(p, a.dtype));
   return launch ? product(p, a.dtype, room, w, s) : PIC_OK;
 }
