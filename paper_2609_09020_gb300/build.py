@@ -28,7 +28,7 @@ SOURCES = ["pic_decode.cu", "k_fp32.cu", "k_fp32_any.cu", "k_fp32_sweep.cu", "k_
            "k_linear_thin.cu", "k_linear_thin_f16.cu", "k_linear_thin_bf16.cu",
            "k_linear_thin_f32.cu",
            "k_linear_outer.cu", "k_clip.cu", "pic_group.cu", "k_group_any.cu",
-           "k_group_grad.cu", "k_group_tc.cu", "k_group_tc_f16.cu", "k_group_tc_bf16.cu", "k_group_planes.cu",
+           "k_group_grad.cu", "k_group_tc.cu", "k_group_tc_f16.cu", "k_group_tc_bf16.cu", "k_group_planes.cu", "k_group_few.cu",
            "k_group_thin_f16.cu", "k_group_thin_bf16.cu", "k_group_thin_f32.cu",
            "k_orth.cu", "k_orth_tc.cu", "k_orth_small.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

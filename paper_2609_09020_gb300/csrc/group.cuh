@@ -123,6 +123,12 @@ struct GroupProduct {
 };
 int any_product(const GroupProduct& p, int dtype, cudaStream_t s);
 
+// Few rows in a group, eight at a time: any types, strides and sizes.  The gradients take a
+// and a_pre as any_product does; few_dw makes db too (y or db null: not that one).
+int few_forward(const GroupProduct& p, int dtype, cudaStream_t s);
+int few_dx(const GroupProduct& p, int dtype, cudaStream_t s);
+int few_dw(const GroupProduct& p, void* db, long long db_group, int dtype, cudaStream_t s);
+
 // On the tensor cores: 16-bit types, a as it is (no a_pre).
 constexpr long long kTcMostK = 16384;  // of K that one accumulator sums up
 bool tc_takes(const GroupProduct& p, int dtype);

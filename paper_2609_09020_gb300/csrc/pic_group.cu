@@ -66,6 +66,27 @@ int product(const GroupProduct& p, int dtype, void* ws, const pic::lin::Waits& w
   return pic::grp::any_product(p, dtype, s);
 }
 
+// Few rows in the groups: up to `most` on average.
+bool few(long long rows, int groups, int most) { return rows <= static_cast<long long>(most) * groups; }
+
+// The forward of 16-bit types whose weights TMA can read goes by tiles that read them at the
+// memory's rate; others would be laid out first.
+bool few_forward(const pic_grouped_linear_args& a) {
+  if (a.dtype == PIC_DTYPE_F32) return few(a.rows, a.groups, 24);
+  const bool tma = aligned(a.w, 16) && a.ldw % 8 == 0 && (a.groups == 1 || a.w_group % 8 == 0) && a.ldw < (1LL << 39) && a.w_group < (1LL << 39);
+  return !tma && few(a.rows, a.groups, 8);
+}
+// The gradient of 16-bit types: a row or two on average, or weights, x or dw that TMA cannot
+// read or write.
+bool few_backward(const pic_grouped_linear_grad_args& a) {
+  if (a.dtype == PIC_DTYPE_F32) return few(a.rows, a.groups, 24);
+  const auto tma = [&](const void* m, long long ld, long long group) {
+    return !m || (aligned(m, 16) && ld % 8 == 0 && (a.groups == 1 || group % 8 == 0));
+  };
+  const bool all = (!a.dx || tma(a.w, a.ldw, a.w_group)) && (!a.dw || (tma(a.x, a.ldx, 0) && tma(a.dw, a.lddw, a.dw_group)));
+  return few(a.rows, a.groups, all ? 1 : 4);
+}
+
 int forward(const pic_grouped_linear_args& a, pic::lin::Arena& ws, bool launch, const pic::lin::Waits& w, cudaStream_t s) {
   if (a.rows == 0) return PIC_OK;
   GroupProduct p{};
@@ -87,6 +108,7 @@ int forward(const pic_grouped_linear_args& a, pic::lin::Arena& ws, bool launch, 
     const pic::lin::ThinGroups g{p.offsets, a.groups, a.w_group, a.bias_group, w.status};
     return launch ? pic::lin::thin_group_product(t, a.dtype, g, s) : PIC_OK;
   }
+  if (few_forward(a)) return launch ? pic::grp::few_forward(p, a.dtype, s) : PIC_OK;
   void* room = ws.take(product_workspace(p, a.dtype));
   return launch ? product(p, a.dtype, room, w, s) : PIC_OK;
 }
@@ -102,6 +124,26 @@ int backward(const pic_grouped_linear_grad_args& a, pic::lin::Arena& ws, bool la
       void* room = ws.take(pic::lin::narrow_group_workspace(n.g, a.groups, a.dtype));
       return launch ? pic::lin::narrow_group_grad(n, a.dtype, room, w, s) : PIC_OK;
     }
+  }
+  if (M == 0 || few_backward(a)) {
+    if (!launch) return PIC_OK;
+    GroupProduct p{};
+    p.a = a.dy, p.a_i = a.lddy;
+    if (a.act != PIC_ACT_NONE) p.a_pre = a.pre, p.a_pre_i = a.ldpre, p.a_act = a.act;
+    p.rows = M, p.groups = a.groups, p.offsets = offsets_of(a.offsets), p.status = w.status;
+    if (a.dx && M > 0) {
+      p.b = a.w, p.b_group = a.w_group, p.b_j = 1, p.b_k = a.ldw;
+      p.J = K, p.K = N;
+      p.y = a.dx, p.ldy = a.lddx;
+      if ((rc = pic::grp::few_dx(p, a.dtype, s)) != PIC_OK) return rc;
+    }
+    if (a.dw || a.db) {
+      p.b = a.x, p.b_group = 0, p.b_j = 1, p.b_k = a.ldx;
+      p.I = N, p.J = K;
+      p.y = a.dw, p.ldy = a.lddw, p.y_group = a.dw_group;
+      rc = pic::grp::few_dw(p, a.db, a.db_group, a.dtype, s);
+    }
+    return rc;
   }
   // dz: dy itself where there is no activation
   const void* dz = a.dy;

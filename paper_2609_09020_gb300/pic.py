@@ -730,6 +730,16 @@ def _vectors(t, name, shape, like):
 
 
 MAX_GROUPS = 1024
+_int64_type = None
+
+
+def _int64():
+    global _int64_type
+    if _int64_type is None:
+        import torch
+        _int64_type = torch.int64
+    return _int64_type
+
 
 
 def _grouped(weight, offsets, like):
@@ -739,7 +749,7 @@ def _grouped(weight, offsets, like):
     G, N, K = weight.shape
     if G > MAX_GROUPS:
         raise ValueError(f"weight: {G} groups, at most {MAX_GROUPS}")
-    if (str(offsets.dtype) != "torch.int64" or offsets.get_device() != like.get_device() or offsets.shape != (G + 1,)
+    if (offsets.dtype is not _int64() or offsets.get_device() != like.get_device() or offsets.shape != (G + 1,)
             or not offsets.is_contiguous()):
         raise ValueError(f"offsets: must be a contiguous int64 tensor [{G + 1}] on {like.device}")
     return G, N, K, offsets.data_ptr()
