@@ -9,6 +9,8 @@
 namespace pic {
 namespace grp {
 
+using lin::Chain;
+using lin::wait_for_earlier;
 using lin::Waits;
 
 constexpr int kMaxGroups = PIC_MAX_GROUPS;
@@ -121,19 +123,19 @@ struct GroupProduct {
   int act;
   int* status;
 };
-int any_product(const GroupProduct& p, int dtype, cudaStream_t s);
+int any_product(const GroupProduct& p, int dtype, Chain& s);
 
 // Few rows in a group, eight at a time: any types, strides and sizes.  The gradients take a
 // and a_pre as any_product does; few_dw makes db too (y or db null: not that one).
-int few_forward(const GroupProduct& p, int dtype, cudaStream_t s);
-int few_dx(const GroupProduct& p, int dtype, cudaStream_t s);
-int few_dw(const GroupProduct& p, void* db, long long db_group, int dtype, cudaStream_t s);
+int few_forward(const GroupProduct& p, int dtype, Chain& s);
+int few_dx(const GroupProduct& p, int dtype, Chain& s);
+int few_dw(const GroupProduct& p, void* db, long long db_group, int dtype, Chain& s);
 
 // On the tensor cores: 16-bit types, a as it is (no a_pre).
 constexpr long long kTcMostK = 16384;  // of K that one accumulator sums up
 bool tc_takes(const GroupProduct& p, int dtype);
 long long tc_workspace(const GroupProduct& p, int dtype);
-int tc_product(const GroupProduct& p, int dtype, void* ws, const Waits& waits, cudaStream_t s);
+int tc_product(const GroupProduct& p, int dtype, void* ws, const Waits& waits, Chain& s);
 
 // Where part `item` of group g is among the parts of the groups that have several; the
 // calling warp's lanes count together.
@@ -155,12 +157,13 @@ struct JoinParams {
   int* status;
 };
 // rows: of a tile.
-void join_parts(const JoinParams& q, int rows, int dtype, cudaStream_t s);
+int join_parts(const JoinParams& q, int rows, int dtype, Chain& s);
 
 // fp32 on the tensor cores, cut into planes first.
 bool planes_takes(const GroupProduct& p, int dtype);
-long long planes_workspace(const GroupProduct& p);
-int planes_product(const GroupProduct& p, void* ws, const Waits& waits, cudaStream_t s);
+int planes_product(const GroupProduct& p, lin::Arena& ws, bool launch, const Waits& waits, Chain& s);
+// dx and dw of the same dz (their a).
+int planes_gradients(const GroupProduct& dx, const GroupProduct& dw, lin::Arena& ws, bool launch, const Waits& waits, Chain& s);
 
 // dz[i][j] = dy act'(pre), rounded (dz null: not written; its rows are on 16-byte
 // boundaries and written to the next one), and db_g, the sums of the unrounded dz over
@@ -181,7 +184,7 @@ struct GroupGradAct {
   int* status;
 };
 long long grad_act_workspace(const GroupGradAct& g, int dtype);
-int grad_act(const GroupGradAct& g, int dtype, cudaStream_t s);
+int grad_act(const GroupGradAct& g, int dtype, Chain& s);
 
 }  // namespace grp
 }  // namespace pic

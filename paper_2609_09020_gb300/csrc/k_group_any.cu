@@ -22,6 +22,7 @@ __global__ void __launch_bounds__(kThreads) any_kernel(const GroupProduct p) {
   __shared__ GroupTable table;
   __shared__ __align__(16) float sa[kDeep][kTile + 4], sb[kDeep][kTile + 4];
   make_table(table, p.offsets, p.groups, p.rows, kTile, 0, p.status);
+  wait_for_earlier();
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const long long tiles_j = (p.J + kTile - 1) / kTile, tiles_i = (p.I + kTile - 1) / kTile;
   const long long work = ROWS ? table.tiles[p.groups] * tiles_j : p.groups * tiles_i * tiles_j;
@@ -34,22 +35,38 @@ __global__ void __launch_bounds__(kThreads) any_kernel(const GroupProduct p) {
     const long long I = ROWS ? len : p.I, K = ROWS ? p.K : len;
     const T* bg = ROWS ? b + g * p.b_group : b + first * p.b_k;
     float acc[4][4] = {};
-    for (long long k0 = 0; k0 < K; k0 += kDeep) {
-      for (int e = threadIdx.x; e < kTile * kDeep; e += kThreads) {
-        // neighbouring threads along what is contiguous
+    // a thread's elements of the next 16 of K, on their way while these are multiplied
+    constexpr int kEach = kTile * kDeep / kThreads;
+    const bool along = ROWS && p.b_k == 1;  // neighbouring threads along what is contiguous
+    T na[kEach], nz[kEach], nb[kEach];
+    const auto fetch = [&](long long k0) {
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) {
+        const int e = threadIdx.x + u * kThreads;
         const int ka = ROWS ? e % kDeep : e / kTile, ia = ROWS ? e / kDeep : e % kTile;
-        float v = 0.0f;
+        na[u] = nz[u] = nb[u] = from_f32<T>(0.0f);
         if (i0 + ia < I && k0 + ka < K) {
           const long long row = first + (ROWS ? i0 + ia : k0 + ka), col = ROWS ? k0 + ka : i0 + ia;
-          v = to_f32(a[row * p.a_i + col]);
-          if (z) v = act_grad<EXACT>(v, to_f32(z[row * p.a_pre_i + col]), p.a_act);
+          na[u] = a[row * p.a_i + col];
+          if (z) nz[u] = z[row * p.a_pre_i + col];
         }
-        sa[ka][ia] = v;
-        const bool along = ROWS && p.b_k == 1;
         const int kb = along ? e % kDeep : e / kTile, jb = along ? e / kDeep : e % kTile;
-        sb[kb][jb] = j0 + jb < p.J && k0 + kb < K ? to_f32(bg[(j0 + jb) * p.b_j + (k0 + kb) * p.b_k]) : 0.0f;
+        if (j0 + jb < p.J && k0 + kb < K) nb[u] = bg[(j0 + jb) * p.b_j + (k0 + kb) * p.b_k];
+      }
+    };
+    if (K > 0) fetch(0);
+    for (long long k0 = 0; k0 < K; k0 += kDeep) {
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) {
+        const int e = threadIdx.x + u * kThreads;
+        const int ka = ROWS ? e % kDeep : e / kTile, ia = ROWS ? e / kDeep : e % kTile;
+        const int kb = along ? e % kDeep : e / kTile, jb = along ? e / kDeep : e % kTile;
+        const float v = to_f32(na[u]);
+        sa[ka][ia] = z ? act_grad<EXACT>(v, to_f32(nz[u]), p.a_act) : v;
+        sb[kb][jb] = to_f32(nb[u]);
       }
       __syncthreads();
+      if (k0 + kDeep < K) fetch(k0 + kDeep);
 #pragma unroll
       for (int k = 0; k < kDeep; ++k) {
         const float4 u = *reinterpret_cast<const float4*>(&sa[k][4 * ty]), v = *reinterpret_cast<const float4*>(&sb[k][4 * tx]);
@@ -81,20 +98,16 @@ __global__ void __launch_bounds__(kThreads) any_kernel(const GroupProduct p) {
 }
 
 template <typename T>
-int run(const GroupProduct& p, cudaStream_t s) {
+int run(const GroupProduct& p, Chain& s) {
   const long long tiles_j = (p.J + kTile - 1) / kTile, tiles_i = (p.I + kTile - 1) / kTile;
   const long long most = p.by_rows ? ((p.rows + kTile - 1) / kTile + p.groups) * tiles_j : p.groups * tiles_i * tiles_j;
   const unsigned grid = static_cast<unsigned>(most < 4 * kSms ? most : 4 * kSms);
-  if (p.by_rows)
-    any_kernel<T, true><<<grid, kThreads, 0, s>>>(p);
-  else
-    any_kernel<T, false><<<grid, kThreads, 0, s>>>(p);
-  return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+  return s.launch(p.by_rows ? any_kernel<T, true> : any_kernel<T, false>, dim3(grid), kThreads, 0, p);
 }
 
 }  // namespace
 
-int any_product(const GroupProduct& p, int dtype, cudaStream_t s) {
+int any_product(const GroupProduct& p, int dtype, Chain& s) {
   if (dtype == PIC_DTYPE_F32) return run<float>(p, s);
   if (dtype == PIC_DTYPE_F16) return run<__half>(p, s);
   return run<__nv_bfloat16>(p, s);

@@ -114,6 +114,7 @@ __global__ void __launch_bounds__(kThreads, 2) forward_kernel(const FewParams q)
   __shared__ GroupTable table;
   __shared__ __align__(16) float xs[kRows][kDeep];
   make_table(table, q.offsets, q.groups, q.rows, kRows, 0, q.status);
+  wait_for_earlier();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long blocks = (q.N + kOuts * kWarps - 1) / (kOuts * kWarps), work = table.tiles[q.groups] * blocks;
   for (long long item = blockIdx.x; item < work; item += gridDim.x) {
@@ -204,6 +205,7 @@ __global__ void __launch_bounds__(kThreads, 2) dx_kernel(const FewParams q) {
   __shared__ __align__(16) float ds[kDeep * kRows];  // [n][row]; at the end four warps' sums
   static_assert(4 * kRows * kCols <= kDeep * kRows, "sums in the place of dz");
   make_table(table, q.offsets, q.groups, q.rows, kRows, 0, q.status);
+  wait_for_earlier();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long blocks = (q.K + kCols - 1) / kCols, work = table.tiles[q.groups] * blocks;
   for (long long item = blockIdx.x; item < work; item += gridDim.x) {
@@ -267,6 +269,7 @@ __global__ void __launch_bounds__(kThreads, 3) dw_kernel(const FewParams q) {
   __shared__ GroupTable table;
   __shared__ __align__(16) float ds[2][kRows][kHigh];
   make_table(table, q.offsets, q.groups, q.rows, kRows, 0, q.status);
+  wait_for_earlier();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long across = q.y ? (q.K + kCols - 1) / kCols : 1, blocks = (q.N + kHigh - 1) / kHigh * across;
   for (long long item = blockIdx.x; item < q.groups * blocks; item += gridDim.x) {
@@ -324,35 +327,29 @@ unsigned grid(long long work, int ctas) {
 }
 
 template <typename T>
-int forward(const FewParams& q, cudaStream_t s) {
+int forward(FewParams q, Chain& s) {
   const long long work = (q.rows / kRows + q.groups) * ((q.N + kOuts * kWarps - 1) / (kOuts * kWarps));
   if (on16(q.w, q.ldw, q.w_group, q.groups, sizeof(T)))
-    forward_kernel<T, true><<<grid(work, 2), kThreads, 0, s>>>(q);
-  else
-    forward_kernel<T, false><<<grid(work, 2), kThreads, 0, s>>>(q);
-  return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+    return s.launch(forward_kernel<T, true>, dim3(grid(work, 2)), kThreads, 0, q);
+  return s.launch(forward_kernel<T, false>, dim3(grid(work, 2)), kThreads, 0, q);
 }
 template <typename T>
-int backward_x(FewParams q, cudaStream_t s) {
+int backward_x(FewParams q, Chain& s) {
   constexpr int kCols = 32 * 16 / sizeof(T);
   const long long work = (q.rows / kRows + q.groups) * ((q.K + kCols - 1) / kCols);
   q.out16 = on16(q.y, q.ldy, 0, 1, sizeof(T));
   if (on16(q.w, q.ldw, q.w_group, q.groups, sizeof(T)))
-    dx_kernel<T, true><<<grid(work, 2), kThreads, 0, s>>>(q);
-  else
-    dx_kernel<T, false><<<grid(work, 2), kThreads, 0, s>>>(q);
-  return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+    return s.launch(dx_kernel<T, true>, dim3(grid(work, 2)), kThreads, 0, q);
+  return s.launch(dx_kernel<T, false>, dim3(grid(work, 2)), kThreads, 0, q);
 }
 template <typename T>
-int backward_w(FewParams q, cudaStream_t s) {
+int backward_w(FewParams q, Chain& s) {
   constexpr int kCols = 32 * 16 / sizeof(T), kHigh = kOuts * kWarps;
   const long long work = q.groups * ((q.N + kHigh - 1) / kHigh) * (q.y ? (q.K + kCols - 1) / kCols : 1);
   q.out16 = on16(q.y, q.ldy, q.y_group, q.groups, sizeof(T));
   if (on16(q.x, q.ldx, 0, 1, sizeof(T)) && q.out16)
-    dw_kernel<T, true><<<grid(work, 3), kThreads, 0, s>>>(q);
-  else
-    dw_kernel<T, false><<<grid(work, 3), kThreads, 0, s>>>(q);
-  return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+    return s.launch(dw_kernel<T, true>, dim3(grid(work, 3)), kThreads, 0, q);
+  return s.launch(dw_kernel<T, false>, dim3(grid(work, 3)), kThreads, 0, q);
 }
 
 FewParams params(const GroupProduct& p) {
@@ -365,7 +362,7 @@ FewParams params(const GroupProduct& p) {
 
 }  // namespace
 
-int few_forward(const GroupProduct& p, int dtype, cudaStream_t s) {
+int few_forward(const GroupProduct& p, int dtype, Chain& s) {
   FewParams q = params(p);
   q.x = p.a, q.ldx = p.a_i;
   q.K = p.K, q.N = p.J;
@@ -375,7 +372,7 @@ int few_forward(const GroupProduct& p, int dtype, cudaStream_t s) {
   return forward<__nv_bfloat16>(q, s);
 }
 
-int few_dx(const GroupProduct& p, int dtype, cudaStream_t s) {
+int few_dx(const GroupProduct& p, int dtype, Chain& s) {
   FewParams q = params(p);
   q.dy = p.a, q.lddy = p.a_i, q.pre = p.a_pre, q.ldpre = p.a_pre_i, q.act = p.a_pre ? p.a_act : PIC_ACT_NONE;
   q.K = p.J, q.N = p.K;
@@ -384,7 +381,7 @@ int few_dx(const GroupProduct& p, int dtype, cudaStream_t s) {
   return backward_x<__nv_bfloat16>(q, s);
 }
 
-int few_dw(const GroupProduct& p, void* db, long long db_group, int dtype, cudaStream_t s) {
+int few_dw(const GroupProduct& p, void* db, long long db_group, int dtype, Chain& s) {
   FewParams q = params(p);
   q.dy = p.a, q.lddy = p.a_i, q.pre = p.a_pre, q.ldpre = p.a_pre_i, q.act = p.a_pre ? p.a_act : PIC_ACT_NONE;
   q.x = p.b, q.ldx = p.b_k;

@@ -44,14 +44,22 @@ Share share(const GroupGradAct& g, int elem) {
   return s;
 }
 
+// Where the first kernel leaves its table of runs for the second, behind the sums.
+__host__ __device__ inline int* table_of(const GroupGradAct& g, const Share& s) {
+  return reinterpret_cast<int*>(g.parts + s.items * g.J);
+}
+
 template <typename T, bool ON16>
 __global__ void __launch_bounds__(kThreads, ON16 ? 4 : 3) grad_act_kernel(const GroupGradAct g, const Share s) {
   constexpr int V = 16 / sizeof(T);
   __shared__ GroupTable table;
   __shared__ float sums[kThreads * V];
   make_table(table, g.offsets, g.groups, g.rows, s.run, 1, g.status);
+  wait_for_earlier();
   const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx, rows = kThreads / s.tx, width = s.tx * V;
   const long long work = table.tiles[g.groups] * s.col_blocks;
+  if (g.db && g.rows > s.run && blockIdx.x == 0)
+    for (int i = threadIdx.x; i <= g.groups; i += kThreads) table_of(g, s)[i] = table.tiles[i];
   for (long long w = blockIdx.x; w < work; w += gridDim.x) {
     const int item = static_cast<int>(w / s.col_blocks), at = table.find(item, g.groups);
     const long long col_block = w % s.col_blocks, j = (col_block * s.tx + tx) * V;
@@ -128,52 +136,49 @@ __global__ void __launch_bounds__(kThreads, ON16 ? 4 : 3) grad_act_kernel(const 
   }
 }
 
-// A block takes 16 columns of a group that has several runs.
+// A block takes 64 columns of a group that has several runs, four threads a column.
+// `tiles`: the first kernel's table of runs.
 template <typename T>
-__global__ void __launch_bounds__(512) sum_parts_kernel(const GroupGradAct g, int run) {
-  __shared__ GroupTable table;
-  __shared__ float sums[32][17];
-  make_table(table, g.offsets, g.groups, g.rows, run, 1, g.status);
-  const int at = blockIdx.y, tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  const int p0 = table.tiles[at], p1 = table.tiles[at + 1];
+__global__ void __launch_bounds__(256) sum_parts_kernel(const GroupGradAct g, const int* tiles) {
+  __shared__ float sums[4][64];
+  wait_for_earlier();
+  const int at = blockIdx.y, tx = threadIdx.x % 64, ty = threadIdx.x / 64;
+  const int p0 = tiles[at], p1 = tiles[at + 1];
   if (p1 - p0 < 2) return;
-  const long long j = blockIdx.x * 16LL + tx;
+  const long long j = blockIdx.x * 64LL + tx;
   float sum = 0.0f;
   if (j < g.J) {
-#pragma unroll 4
-    for (int p = p0 + ty; p < p1; p += 32) sum += g.parts[p * g.J + j];
+#pragma unroll 8
+    for (int p = p0 + ty; p < p1; p += 4) sum += __ldcg(g.parts + p * g.J + j);
   }
   sums[ty][tx] = sum;
   __syncthreads();
   if (ty == 0 && j < g.J) {
 #pragma unroll
-    for (int r = 1; r < 32; ++r) sum += sums[r][tx];
+    for (int r = 1; r < 4; ++r) sum += sums[r][tx];
     static_cast<T*>(g.db)[at * g.db_group + j] = lin::from_f32<T>(sum);
   }
 }
 
 template <typename T>
-int run(const GroupGradAct& g, cudaStream_t stream) {
+int run(GroupGradAct g, Chain& chain) {
   const Share s = share(g, sizeof(T));
   const long long most = s.items * s.col_blocks, slots = (s.on16 ? 4 : 3) * kSms;
   const unsigned blocks = static_cast<unsigned>(most < slots ? most : slots);
-  if (s.on16)
-    grad_act_kernel<T, true><<<blocks, kThreads, 0, stream>>>(g, s);
-  else
-    grad_act_kernel<T, false><<<blocks, kThreads, 0, stream>>>(g, s);
-  if (g.db && g.rows > s.run)
-    sum_parts_kernel<T><<<dim3(static_cast<unsigned>((g.J + 15) / 16), g.groups), 512, 0, stream>>>(g, s.run);
-  return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+  const int rc = chain.launch(s.on16 ? grad_act_kernel<T, true> : grad_act_kernel<T, false>, dim3(blocks), kThreads, 0, g, s);
+  if (rc != PIC_OK || !g.db || g.rows <= s.run) return rc;
+  return chain.launch(sum_parts_kernel<T>, dim3(static_cast<unsigned>((g.J + 63) / 64), g.groups), 256, 0, g,
+                      static_cast<const int*>(table_of(g, s)));
 }
 
 }  // namespace
 
 long long grad_act_workspace(const GroupGradAct& g, int dtype) {
   const Share s = share(g, dtype == PIC_DTYPE_F32 ? 4 : 2);
-  return g.db && g.rows > s.run ? s.items * g.J * 4 : 0;
+  return g.db && g.rows > s.run ? (s.items * g.J + g.groups + 1) * 4 : 0;
 }
 
-int grad_act(const GroupGradAct& g, int dtype, cudaStream_t s) {
+int grad_act(const GroupGradAct& g, int dtype, Chain& s) {
   if (dtype == PIC_DTYPE_F32) return run<float>(g, s);
   if (dtype == PIC_DTYPE_F16) return run<__half>(g, s);
   return run<__nv_bfloat16>(g, s);

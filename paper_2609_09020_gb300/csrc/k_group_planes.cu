@@ -233,6 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1) planes_kernel(const __grid_consta
   tc::cluster_sync();
   tc::tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  wait_for_earlier();
   auto wait = [&](uint32_t bar, uint32_t parity) { return lin::wait_bounded(bar, parity, abort_flag, q.waits); };
   const long long first = blockIdx.x / 2, step = gridDim.x / 2;
   const long long work = tiles[q.groups] * (q.sums ? q.tiles_i * q.tiles_j : q.tiles_j);
@@ -409,10 +410,16 @@ struct Cut {
   long long plane, ld_out;  // elements of a plane
   int* marks;
 };
-__global__ void __launch_bounds__(256) cut_kernel(const Cut q, int* status) {
+struct Cuts {
+  Cut m[3];
+};
+// The y-th row of blocks takes the y-th matrix.
+__global__ void __launch_bounds__(256) cut_kernel(const __grid_constant__ Cuts cuts, int* status) {
   __shared__ GroupTable table;
+  const Cut& q = cuts.m[blockIdx.y];
   const bool grouped = q.offsets != nullptr;
   if (grouped) make_table(table, q.offsets, q.groups, q.rows, kAlign, 0, status);
+  wait_for_earlier();
   const long long all = grouped ? table.tiles[q.groups] * static_cast<long long>(kAlign) : static_cast<long long>(q.groups) * q.padded;
   const unsigned col_blocks = static_cast<unsigned>((q.cols + kPlBlock - 1) / kPlBlock);
   const long long work = (all + kPlBlock - 1) / kPlBlock * col_blocks;
@@ -535,27 +542,53 @@ Plan plan(const GroupProduct& p) {
 
 }  // namespace
 
-// (k_group_any.cu's kernel, measured: 17 TFLOP/s of whole tiles of 64 x 64, with 4 CTAs on an
-// SM; 0.35 us for 16 of K)
+// (k_group_any.cu's kernel, measured: 16 of K take from 1.3 us with few tiles of 64 x 64 to 4
+// with four on each SM)
 bool planes_takes(const GroupProduct& p, int dtype) {
   if (dtype != PIC_DTYPE_F32 || p.a_pre || p.rows == 0) return false;
   const double each = static_cast<double>(p.rows) / p.groups;
   const auto up = [](double a, double b) { return static_cast<double>(static_cast<long long>((a + b - 1) / b)); };
   const double k = p.by_rows ? static_cast<double>(p.K) : each;
   const double tiles = p.groups * (p.by_rows ? up(each, 64) : up(static_cast<double>(p.I), 64)) * up(static_cast<double>(p.J), 64);
-  const double any = 4.0 + (tiles < 4 * kSms ? up(k, 16) * 0.35 * (0.5 + 0.5 * tiles / (4 * kSms)) : tiles * 64 * 64 * 2 * up(k, 16) * 16 / 17e6);
+  const double full = tiles / (4 * kSms);
+  const double any = 4.0 + up(k, 16) * (full <= 1 ? 1.0 + 3.0 * full : 4.0 * up(full, 1));
   return plan(p).time < any;
 }
 
-long long planes_workspace(const GroupProduct& p) {
-  const Plan r = plan(p);
-  return r.a.bytes + r.b.bytes + r.a.mark_bytes + r.b.mark_bytes + r.part_bytes;
+namespace {
+
+int blocks_of(long long cols) { return static_cast<int>((cols + kPlBlock - 1) / kPlBlock); }
+
+// The planes and marks of an operand, and the job of making them.
+struct Made {
+  Planes l;
+  char *planes, *marks;
+  Cut cut;
+};
+// grouped: of rows by group; else of p's weights.
+Made made(const GroupProduct& p, const Planes& l, bool grouped, const void* m, long long ld, long long group, lin::Arena& ws) {
+  Made o{l, static_cast<char*>(ws.take(l.bytes)), static_cast<char*>(ws.take(l.mark_bytes)), {}};
+  const long long rows = p.b_k == 1 ? p.J : p.K;  // of a group's weights
+  o.cut = {static_cast<const float*>(m), ld, group, grouped ? p.rows : rows, l.cols, static_cast<int>(round_up(rows, kAlign)), p.groups,
+           grouped ? p.offsets : nullptr, reinterpret_cast<uint16_t*>(o.planes), l.rows * l.ld, l.ld, reinterpret_cast<int*>(o.marks)};
+  return o;
+}
+Made made_a(const GroupProduct& p, const Plan& r, lin::Arena& ws) { return made(p, r.a, true, p.a, p.a_i, 0, ws); }
+Made made_b(const GroupProduct& p, const Plan& r, lin::Arena& ws) {
+  return made(p, r.b, !p.by_rows, p.b, p.by_rows && p.b_k == 1 ? p.b_j : p.b_k, p.b_group, ws);
+}
+int cut_all(const Made* const* m, int n, int* status, Chain& s) {
+  Cuts c{};
+  long long most = 1;
+  for (int i = 0; i < n; ++i) {
+    c.m[i] = m[i]->cut;
+    const long long want = (m[i]->l.rows + kPlBlock - 1) / kPlBlock * blocks_of(m[i]->l.cols);
+    if (want > most) most = want;
+  }
+  return s.launch(cut_kernel, dim3(static_cast<unsigned>(most < 6 * kSms ? most : 6 * kSms), n), 256, 0, c, status);
 }
 
-int planes_product(const GroupProduct& p, void* ws, const Waits& waits, cudaStream_t s) {
-  const Plan r = plan(p);
-  char* w = static_cast<char*>(ws);
-  char *pa = w, *pb = pa + r.a.bytes, *ma = pb + r.b.bytes, *mb = ma + r.a.mark_bytes, *parts = mb + r.b.mark_bytes;
+int multiply(const GroupProduct& p, const Plan& r, const Made& a, const Made& b, float* parts, const Waits& waits, Chain& s) {
   GpParams q{};
   GpMaps maps;
   q.rows = p.rows, q.I = p.I, q.J = p.J, q.K = p.K;
@@ -563,42 +596,54 @@ int planes_product(const GroupProduct& p, void* ws, const Waits& waits, cudaStre
   q.groups = p.groups, q.offsets = p.offsets;
   q.sums = !p.by_rows;
   q.b_mn = p.by_rows && p.b_k != 1;
-  const long long w_rows = q.b_mn ? p.K : p.J;
-  q.w_rows = static_cast<int>(round_up(w_rows, kAlign));
+  q.w_rows = b.cut.padded;
   q.chunk = r.chunk;
-  q.parts = reinterpret_cast<float*>(parts);
-  const auto blocks = [](long long cols) { return static_cast<int>((cols + kPlBlock - 1) / kPlBlock); };
-  q.a = {static_cast<const float*>(p.a), p.a_i, 0, reinterpret_cast<int*>(ma), blocks(r.a.cols)};
-  q.b = {static_cast<const float*>(p.b), p.by_rows && p.b_k == 1 ? p.b_j : p.b_k, p.b_group, reinterpret_cast<int*>(mb), blocks(r.b.cols)};
+  q.parts = parts;
+  const auto source = [](const Made& o) { return Source{o.cut.m, o.cut.ld, o.cut.group, o.cut.marks, blocks_of(o.l.cols)}; };
+  q.a = source(a), q.b = source(b);
   q.bias = static_cast<const float*>(p.bias), q.bias_group = p.bias_group;
   q.y = static_cast<float*>(p.y), q.ldy = p.ldy, q.y_group = p.y_group;
   q.pre = static_cast<float*>(p.pre), q.ldpre = p.ldpre, q.act = p.act;
   q.waits = waits;
-  const auto cut = [&](const Source& o, const Planes& l, bool grouped, char* planes) {
-    const Cut c{o.m, o.ld, o.group, grouped ? p.rows : w_rows, l.cols, q.w_rows, p.groups, grouped ? p.offsets : nullptr,
-                reinterpret_cast<uint16_t*>(planes), l.rows * l.ld, l.ld, const_cast<int*>(o.marks)};
-    const long long want = (l.rows + kPlBlock - 1) / kPlBlock * blocks(l.cols);
-    cut_kernel<<<static_cast<unsigned>(want < 6 * kSms ? want : 6 * kSms), 256, 0, s>>>(c, waits.status);
-  };
-  cut(q.a, r.a, true, pa);
-  cut(q.b, r.b, q.sums, pb);
   // 32 of K: along K a box of the CTA's rows, else blocks of 64 rows
-  if (!(q.sums ? lin::encode_planes(&maps.a, pa, r.a.rows, r.a.cols, r.a.ld, 64, 32)
-               : lin::encode_planes(&maps.a, pa, r.a.rows, r.a.cols, r.a.ld, 32, 128)) ||
-      !(q.sums || q.b_mn ? lin::encode_planes(&maps.b, pb, r.b.rows, r.b.cols, r.b.ld, 64, 32)
-                         : lin::encode_planes(&maps.b, pb, r.b.rows, r.b.cols, r.b.ld, 32, 64)))
+  if (!(q.sums ? lin::encode_planes(&maps.a, a.planes, a.l.rows, a.l.cols, a.l.ld, 64, 32)
+               : lin::encode_planes(&maps.a, a.planes, a.l.rows, a.l.cols, a.l.ld, 32, 128)) ||
+      !(q.sums || q.b_mn ? lin::encode_planes(&maps.b, b.planes, b.l.rows, b.l.cols, b.l.ld, 64, 32)
+                         : lin::encode_planes(&maps.b, b.planes, b.l.rows, b.l.cols, b.l.ld, 32, 64)))
     return PIC_ERR_CUDA;
   const void* fn = reinterpret_cast<const void*>(planes_kernel);
   if (lin::allow_smem(fn, 54, kSmem) != PIC_OK) return PIC_ERR_CUDA;
   const long long want = 2 * r.work;
   void* args[] = {&q, &maps};
-  if (lin::launch_kernel(fn, want < kSms ? want : kSms, kThreads, kSmem, 2, args, s) != PIC_OK) return PIC_ERR_CUDA;
-  if (r.part_bytes > 0) {
-    const JoinParams j{p.offsets, p.rows, p.I, p.J, r.tiles_i, r.tiles_j, p.groups, r.chunk, kPlCols,
-                       reinterpret_cast<const float4*>(q.parts), p.y, p.ldy, p.y_group, waits.status};
-    join_parts(j, kPlRows, PIC_DTYPE_F32, s);
-  }
-  return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+  if (s.launch(fn, dim3(static_cast<unsigned>(want < kSms ? want : kSms)), kThreads, kSmem, 2, args) != PIC_OK) return PIC_ERR_CUDA;
+  if (r.part_bytes == 0) return PIC_OK;
+  const JoinParams j{p.offsets, p.rows, p.I, p.J, r.tiles_i, r.tiles_j, p.groups, r.chunk, kPlCols,
+                     reinterpret_cast<const float4*>(q.parts), p.y, p.ldy, p.y_group, waits.status};
+  return join_parts(j, kPlRows, PIC_DTYPE_F32, s);
+}
+
+}  // namespace
+
+int planes_product(const GroupProduct& p, lin::Arena& ws, bool launch, const Waits& waits, Chain& s) {
+  const Plan r = plan(p);
+  const Made a = made_a(p, r, ws), b = made_b(p, r, ws);
+  float* parts = static_cast<float*>(ws.take(r.part_bytes));
+  if (!launch) return PIC_OK;
+  const Made* both[] = {&a, &b};
+  const int rc = cut_all(both, 2, waits.status, s);
+  return rc == PIC_OK ? multiply(p, r, a, b, parts, waits, s) : rc;
+}
+
+int planes_gradients(const GroupProduct& dx, const GroupProduct& dw, lin::Arena& ws, bool launch, const Waits& waits, Chain& s) {
+  const Plan rx = plan(dx), rw = plan(dw);
+  // the same planes of dz serve both
+  const Made dz = made_a(dx, rx, ws), w = made_b(dx, rx, ws), x = made_b(dw, rw, ws);
+  float* parts = static_cast<float*>(ws.take(rw.part_bytes));
+  if (!launch) return PIC_OK;
+  const Made* all[] = {&dz, &w, &x};
+  int rc = cut_all(all, 3, waits.status, s);
+  if (rc == PIC_OK) rc = multiply(dx, rx, dz, w, nullptr, waits, s);
+  return rc == PIC_OK ? multiply(dw, rw, dz, x, parts, waits, s) : rc;
 }
 
 }  // namespace grp

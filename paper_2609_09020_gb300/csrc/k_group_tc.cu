@@ -22,6 +22,7 @@ struct Pad {
   int ld_out;
 };
 __global__ void __launch_bounds__(256) pad_kernel(const Pad q) {
+  wait_for_earlier();
   const int chunks = (q.cols + 7) / 8;
   const long long all = q.rows * q.count * chunks;
   for (long long e = blockIdx.x * 256LL + threadIdx.x; e < all; e += gridDim.x * 256LL) {
@@ -50,6 +51,7 @@ struct MakeMaps {
 __global__ void __launch_bounds__(32) maps_kernel(const MakeMaps q, const __grid_constant__ GtMaps maps) {
   __shared__ __align__(128) uint32_t sm[2][32];
   const int g = blockIdx.x, lane = threadIdx.x;
+  wait_for_earlier();
   // an offset counts as the largest so far, within [0, rows]
   long long first = 0;
   for (int i = lane; i <= g; i += 32) first = max(first, q.offsets[i]);
@@ -84,6 +86,7 @@ template <typename T, int ROWS>
 __global__ void __launch_bounds__(256) join_kernel(const JoinParams q) {
   __shared__ GroupTable table;
   make_table(table, q.offsets, q.groups, q.rows, q.chunk, 1, q.status);
+  wait_for_earlier();
   const int g = blockIdx.y;
   const int parts = table.tiles[g + 1] - table.tiles[g];
   if (parts < 2) return;
@@ -203,31 +206,25 @@ Plan plan(const GroupProduct& p) {
   return r;
 }
 
-void pad(const Operand& o, long long ld, long long group, void* to, cudaStream_t s) {
+int pad(const Operand& o, long long ld, long long group, void* to, Chain& s) {
   const Pad q{static_cast<const uint16_t*>(o.m), ld, group, o.rows, o.count, static_cast<int>(o.cols),
               static_cast<uint4*>(to), static_cast<int>(o.ld)};
   const long long blocks = (o.rows * o.count * ((o.cols + 7) / 8) + 255) / 256;
-  pad_kernel<<<static_cast<unsigned>(blocks < 16 * kSms ? blocks : 16 * kSms), 256, 0, s>>>(q);
+  return s.launch(pad_kernel, dim3(static_cast<unsigned>(blocks < 16 * kSms ? blocks : 16 * kSms)), 256, 0, q);
 }
 
 template <typename T>
-void join(const JoinParams& q, int rows, cudaStream_t s) {
+int join(JoinParams q, int rows, Chain& s) {
   const dim3 grid(static_cast<unsigned>(q.tiles_i * q.tiles_j * rows * q.bn / 4 / 256), q.groups);
-  if (rows == 128)
-    join_kernel<T, 128><<<grid, 256, 0, s>>>(q);
-  else
-    join_kernel<T, 256><<<grid, 256, 0, s>>>(q);
+  return s.launch(rows == 128 ? join_kernel<T, 128> : join_kernel<T, 256>, grid, 256, 0, q);
 }
 
 }  // namespace
 
-void join_parts(const JoinParams& q, int rows, int dtype, cudaStream_t s) {
-  if (dtype == PIC_DTYPE_F32)
-    join<float>(q, rows, s);
-  else if (dtype == PIC_DTYPE_F16)
-    join<__half>(q, rows, s);
-  else
-    join<__nv_bfloat16>(q, rows, s);
+int join_parts(const JoinParams& q, int rows, int dtype, Chain& s) {
+  if (dtype == PIC_DTYPE_F32) return join<float>(q, rows, s);
+  if (dtype == PIC_DTYPE_F16) return join<__half>(q, rows, s);
+  return join<__nv_bfloat16>(q, rows, s);
 }
 
 bool tc_takes(const GroupProduct& p, int dtype) {
@@ -240,16 +237,16 @@ long long tc_workspace(const GroupProduct& p, int) {
   return r.a.bytes + r.b.bytes + r.map_bytes + r.part_bytes;
 }
 
-int tc_product(const GroupProduct& p, int dtype, void* ws, const Waits& waits, cudaStream_t s) {
+int tc_product(const GroupProduct& p, int dtype, void* ws, const Waits& waits, Chain& s) {
   const Plan r = plan(p);
   char* w = static_cast<char*>(ws);
   Operand a = r.a, b = r.b;
   if (a.pad) {
-    pad(a, p.a_i, 0, w, s);
+    if (pad(a, p.a_i, 0, w, s) != PIC_OK) return PIC_ERR_CUDA;
     a.m = w;
   }
   if (b.pad) {
-    pad(b, p.by_rows && p.b_k == 1 ? p.b_j : p.b_k, p.b_group, w + a.bytes, s);
+    if (pad(b, p.by_rows && p.b_k == 1 ? p.b_j : p.b_k, p.b_group, w + a.bytes, s) != PIC_OK) return PIC_ERR_CUDA;
     b.m = w + a.bytes;
   }
   GtParams q{};
@@ -290,19 +287,19 @@ int tc_product(const GroupProduct& p, int dtype, void* ws, const Waits& waits, c
   if (!p.by_rows && p.rows > 0) {
     const MakeMaps mk{p.offsets, p.rows, {static_cast<const char*>(a.m), static_cast<const char*>(b.m)}, {a.ld * 2, b.ld * 2},
                       const_cast<CUtensorMap*>(q.maps)};
-    maps_kernel<<<p.groups, 32, 0, s>>>(mk, maps);
+    if (s.launch(maps_kernel, dim3(p.groups), 32, 0, mk, maps) != PIC_OK) return PIC_ERR_CUDA;
   }
   const GtKernel k = dtype == PIC_DTYPE_BF16 ? group_kernel_bf16(r.mode, r.bn) : group_kernel_f16(r.mode, r.bn);
   if (lin::allow_smem(k.fn, k.slot, k.smem) != PIC_OK) return PIC_ERR_CUDA;
   const long long slots = static_cast<long long>(kSms) * k.ctas, want = r.work * r.cg;
   void* args[] = {&q, &maps};
-  if (lin::launch_kernel(k.fn, want < slots ? want : slots, k.threads, k.smem, r.cg, args, s) != PIC_OK) return PIC_ERR_CUDA;
+  if (s.launch(k.fn, dim3(static_cast<unsigned>(want < slots ? want : slots)), k.threads, k.smem, r.cg, args) != PIC_OK) return PIC_ERR_CUDA;
   if (!p.by_rows && r.part_bytes > 0) {
     const JoinParams j{p.offsets, p.rows, p.I, p.J, r.tiles_i, r.tiles_j, p.groups, r.chunk, r.bn,
                        reinterpret_cast<const float4*>(q.parts), p.y, p.ldy, p.y_group, waits.status};
-    join_parts(j, 128 * r.cg, dtype, s);
+    return join_parts(j, 128 * r.cg, dtype, s);
   }
-  return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+  return PIC_OK;
 }
 
 }  // namespace grp

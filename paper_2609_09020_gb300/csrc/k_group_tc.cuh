@@ -232,6 +232,7 @@ __global__ void __launch_bounds__(GtShape<CG, BN, MODE>::kThreads, GtShape<CG, B
   if constexpr (CG == 2) tc::cluster_sync();
   tc::tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  wait_for_earlier();
 
   auto wait = [&](uint32_t bar, uint32_t parity) { return lin::wait_bounded(bar, parity, abort_flag, q.waits); };
   const long long first = blockIdx.x / CG, step = gridDim.x / CG, work = work_of<CG, BN, MODE>(q, table);

@@ -67,6 +67,7 @@ struct NarrowParams {
   const long long* offsets;
   int groups;
   int pieces;  // at most, and so many CTAs
+  int* piece_table;  // [groups + 1]: pieces before each group's
   long long w_group, dw_group, db_group;
 };
 
@@ -259,8 +260,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   long long first = blockIdx.x, last = q.tiles, step = gridDim.x, origin = 0;
   NarrowGrad of_group;  // I is the group's end, and w its weights
   if constexpr (GROUPED) {
+    wait_for_earlier();
     grp::GroupTable& table = *reinterpret_cast<grp::GroupTable*>(smem);  // (where the stages will be)
     make_pieces(table, q, q.g.I, reinterpret_cast<int*>(smem + sizeof(grp::GroupTable)));
+    if (blockIdx.x == 0)  // for the kernel that adds the parts
+      for (int i = threadIdx.x; i <= q.groups; i += kThreads) q.piece_table[i] = table.tiles[i];
     if (static_cast<int>(blockIdx.x) >= table.tiles[q.groups]) return;
     const int at = table.find(blockIdx.x, q.groups);
     const long long pieces = table.tiles[at + 1] - table.tiles[at], piece = blockIdx.x - table.tiles[at],
@@ -789,18 +793,16 @@ long long pieces_of(const NarrowGrad& g, int groups, int dtype) {
 // values, its warps add every 32nd part; else a thread a value.
 template <typename T, bool MANY>
 __global__ void __launch_bounds__(MANY ? 1024 : 256) add_group_parts_kernel(const NarrowParams q) {
-  __shared__ grp::GroupTable table;
   __shared__ float sums[MANY ? 32 : 1][32];
-  __shared__ int scratch;
   const NarrowGrad& g = q.g;
-  make_pieces(table, q, g.I, &scratch);
+  wait_for_earlier();
   const int at = blockIdx.y, nk = g.N * g.K, per = nk + g.N;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int e = MANY ? blockIdx.x * 32 + lane : blockIdx.x * 256 + threadIdx.x;
   float v = 0.0f;
   if (e < per) {
 #pragma unroll 5
-    for (int c = table.tiles[at] + (MANY ? warp : 0); c < table.tiles[at + 1]; c += MANY ? 32 : 1)
+    for (int c = q.piece_table[at] + (MANY ? warp : 0), c1 = q.piece_table[at + 1]; c < c1; c += MANY ? 32 : 1)
       v += __ldcg(q.parts + c * static_cast<long long>(per) + e);
   }
   if (MANY) {
@@ -819,21 +821,17 @@ __global__ void __launch_bounds__(MANY ? 1024 : 256) add_group_parts_kernel(cons
 }
 
 template <typename T, bool WIDE, Source SRC>
-int run_groups(NarrowParams& q, NarrowMaps& maps, int slot, cudaStream_t s) {
+int run_groups(NarrowParams q, NarrowMaps& maps, int slot, Chain& s) {
   const void* fn = reinterpret_cast<const void*>(narrow_kernel<T, WIDE, SRC, true>);
   constexpr int smem = Shape<T, WIDE, SRC>::kSmem;
   static_assert(smem <= 227 * 1024 && sizeof(grp::GroupTable) + 4 <= Shape<T, WIDE, SRC>::kOffW, "shared memory of an SM");
   if (allow_smem(fn, slot, smem) != PIC_OK) return PIC_ERR_CUDA;
   void* args[] = {&q, &maps};
-  if (cudaLaunchKernel(fn, dim3(q.pieces), dim3(kThreads), args, smem, s) != cudaSuccess) return PIC_ERR_CUDA;
-  if (q.g.dw || q.g.db) {
-    const int per = q.g.N * q.g.K + q.g.N;
-    if (q.pieces / q.groups >= 16)
-      add_group_parts_kernel<T, true><<<dim3((per + 31) / 32, q.groups), 1024, 0, s>>>(q);
-    else
-      add_group_parts_kernel<T, false><<<dim3((per + 255) / 256, q.groups), 256, 0, s>>>(q);
-  }
-  return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+  if (s.launch(fn, dim3(q.pieces), kThreads, smem, 1, args) != PIC_OK) return PIC_ERR_CUDA;
+  if (!q.g.dw && !q.g.db) return PIC_OK;
+  const int per = q.g.N * q.g.K + q.g.N;
+  if (q.pieces / q.groups >= 16) return s.launch(add_group_parts_kernel<T, true>, dim3((per + 31) / 32, q.groups), 1024, 0, q);
+  return s.launch(add_group_parts_kernel<T, false>, dim3((per + 255) / 256, q.groups), 256, 0, q);
 }
 
 }  // namespace
@@ -841,10 +839,10 @@ int run_groups(NarrowParams& q, NarrowMaps& maps, int slot, cudaStream_t s) {
 bool narrow_group_takes(const NarrowGrad& g, int groups, int dtype) { return g.I > 0 && narrow_takes(g, dtype); }
 
 long long narrow_group_workspace(const NarrowGrad& g, int groups, int dtype) {
-  return pieces_of(g, groups, dtype) * (g.N * g.K + g.N) * 4LL;
+  return pieces_of(g, groups, dtype) * (g.N * g.K + g.N) * 4LL + (groups + 1) * 4;
 }
 
-int narrow_group_grad(const NarrowGroups& a, int dtype, void* ws, const Waits& waits, cudaStream_t s) {
+int narrow_group_grad(const NarrowGroups& a, int dtype, void* ws, const Waits& waits, Chain& s) {
   const NarrowGrad& g = a.g;
   NarrowParams q{};
   const int elem = dtype == PIC_DTYPE_F32 ? 4 : 2;
@@ -856,6 +854,7 @@ int narrow_group_grad(const NarrowGroups& a, int dtype, void* ws, const Waits& w
   q.parts = static_cast<float*>(ws);
   q.waits = waits;
   q.pieces = static_cast<int>(pieces_of(g, a.groups, dtype));
+  q.piece_table = reinterpret_cast<int*>(q.parts + q.pieces * static_cast<long long>(g.N * g.K + g.N));
   q.offsets = a.offsets, q.groups = a.groups, q.w_group = a.w_group, q.dw_group = a.dw_group, q.db_group = a.db_group;
   NarrowMaps maps{};
   if (q.store_tma && !encode(&maps.dx, g.dx, g.I, g.K, g.lddx, 32, dtype)) return PIC_ERR_CUDA;

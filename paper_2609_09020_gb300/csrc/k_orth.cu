@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(kThreads) squares_kernel(const Matrix* matrice
   const Piece p = pieces[blockIdx.x];
   const Matrix& m = matrices[p.matrix];
   const int row = p.row0 + threadIdx.x / 8, col = p.col0 + threadIdx.x % 8 * 8, end = min(m.cols, p.col0 + kPieceCols);
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  wait_for_earlier();
   double sum = 0.0;
   for_form(m, [&](auto, auto load) {
     float s = 0.0f;
@@ -481,7 +481,7 @@ int pic_orth(pic_orthogonalizer* h, int steps, float a, float b, float c, float 
     return PIC_ERR_CUDA;
   }
   if (dev != h->device) return PIC_ERR_INVALID_ARG;
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  pic::lin::Chain s{static_cast<cudaStream_t>(stream)};
   for (int i = kSmallLists - 1; i >= 0; --i)
     if (launch_small(h->matrices, h->small[i], h->n_small[i], h->small_bytes[i], steps, {a, b, c}, eps, s) != PIC_OK) {
       cudaGetLastError();
@@ -491,14 +491,15 @@ int pic_orth(pic_orthogonalizer* h, int steps, float a, float b, float c, float 
   pic::lin::Waits waits;
   if (!pic::lin::call_waits(waits)) return PIC_ERR_CUDA;
   waits.status = h->status;
-  squares_kernel<<<h->n_pieces, kThreads, 0, s>>>(h->matrices, h->pieces, h->squares);
-  {
-    int last = steps == 0;
-    void* args[] = {&h->matrices, &h->pieces, &h->squares, &eps, &last};
-    if (launch_behind(reinterpret_cast<const void*>(scale_kernel), h->n_pieces, kThreads, 0, 1, args, s) != PIC_OK) {
-      cudaGetLastError();
-      return PIC_ERR_CUDA;
-    }
+  const Matrix* matrices = h->matrices;
+  const Piece* pieces = h->pieces;
+  int rc = s.launch(squares_kernel, dim3(h->n_pieces), kThreads, 0, matrices, pieces, h->squares);
+  if (rc == PIC_OK)
+    rc = s.launch(scale_kernel, dim3(h->n_pieces), kThreads, 0, matrices, pieces, static_cast<const double*>(h->squares), eps,
+                  static_cast<int>(steps == 0));
+  if (rc != PIC_OK) {
+    cudaGetLastError();
+    return rc;
   }
   for (int k = 0; k < steps; ++k)
     for (const Stage stage : {kGram, kPolynomial, kUpdate})

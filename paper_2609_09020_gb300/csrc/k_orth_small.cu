@@ -235,6 +235,7 @@ __global__ void __launch_bounds__(kThreads) small_kernel(const Matrix* matrices,
   const Held x{halves, s.cols + 8, s.rows * (s.cols + 8)};
   const Held a{halves + 2 * s.rows * (s.cols + 8), s.rows + 8, s.rows * (s.rows + 8)};
   const Held b{a.hi + 2 * s.rows * (s.rows + 8), a.ld, a.lo};
+  lin::wait_for_earlier();
   for (int i = threadIdx.x; i < 2 * s.rows * (s.cols + 8) / 8; i += kThreads) reinterpret_cast<uint4*>(halves)[i] = make_uint4(0, 0, 0, 0);
   // (load_scaled has a barrier before it writes to x)
   if (m.dtype == PIC_DTYPE_F32)
@@ -262,11 +263,10 @@ __global__ void __launch_bounds__(kThreads) small_kernel(const Matrix* matrices,
 }  // namespace
 
 int launch_small(const Matrix* matrices, const int* list, int n, int smem, int steps, const Coefficients& co, float eps,
-                 cudaStream_t s) {
+                 lin::Chain& s) {
   if (n == 0) return PIC_OK;
   if (lin::allow_smem(reinterpret_cast<const void*>(small_kernel), 53, kSmallMost) != PIC_OK) return PIC_ERR_CUDA;
-  small_kernel<<<n, kThreads, smem, s>>>(matrices, list, steps, co, eps);
-  return cudaGetLastError() == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+  return s.launch(small_kernel, dim3(n), kThreads, smem, matrices, list, steps, co, eps);
 }
 
 }  // namespace orth

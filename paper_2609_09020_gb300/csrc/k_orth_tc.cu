@@ -430,18 +430,18 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
 }
 
 template <Stage STAGE, int CG, int BN>
-int launch(const StageParams& q, int slot, cudaStream_t s) {
+int launch(const StageParams& q, int slot, lin::Chain& s) {
   using S = Shape<CG, BN>;
   static_assert((S::kSmem + 1024) * S::kCtas <= 228 * 1024, "shared memory of an SM");
   const void* fn = reinterpret_cast<const void*>(stage_kernel<STAGE, CG, BN>);
   if (lin::allow_smem(fn, slot, S::kSmem) != PIC_OK) return PIC_ERR_CUDA;
   const long long want = static_cast<long long>(q.n) * CG, most = 152 * S::kCtas;
   void* args[] = {const_cast<StageParams*>(&q)};
-  return launch_behind(fn, want < most ? want : most, S::kThreads, S::kSmem, CG, args, s);
+  return s.launch(fn, dim3(static_cast<unsigned>(want < most ? want : most)), S::kThreads, S::kSmem, CG, args);
 }
 
 template <Stage STAGE>
-int launch_bn(int bn, const StageParams& q, cudaStream_t s) {
+int launch_bn(int bn, const StageParams& q, lin::Chain& s) {
   if (bn == 64) return launch<STAGE, 1, 64>(q, 44 + STAGE, s);
   if (bn == 128) return launch<STAGE, 1, 128>(q, 47 + STAGE, s);
   return launch<STAGE, 2, 256>(q, 50 + STAGE, s);
@@ -449,7 +449,7 @@ int launch_bn(int bn, const StageParams& q, cudaStream_t s) {
 
 }  // namespace
 
-int launch_stage(Stage stage, int bn, const StageParams& q, cudaStream_t s) {
+int launch_stage(Stage stage, int bn, const StageParams& q, lin::Chain& s) {
   if (q.n == 0) return PIC_OK;
   if (stage == kGram) return launch_bn<kGram>(bn, q, s);
   if (stage == kPolynomial) return launch_bn<kPolynomial>(bn, q, s);

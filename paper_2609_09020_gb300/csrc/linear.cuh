@@ -245,6 +245,44 @@ inline int launch_kernel(const void* fn, long long grid, int threads, int smem, 
   return cudaLaunchKernelExC(&cfg, fn, args) == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
 }
 
+// A call's kernels on a stream.  Each but the first is launched so that it may set itself up
+// while the one before still runs: it calls wait_for_earlier before it touches anything
+// that an earlier one reads or writes.
+struct Chain {
+  cudaStream_t stream;
+  bool begun = false;
+  int launch(const void* fn, dim3 grid, int threads, int smem, int cluster, void** args) {
+    cudaLaunchAttribute attr[2] = {};
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    if (begun) {
+      attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+      attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (cluster > 1) {
+      attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+      attr[cfg.numAttrs].val.clusterDim.x = cluster;
+      attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
+      ++cfg.numAttrs;
+    }
+    begun = true;
+    return cudaLaunchKernelExC(&cfg, fn, args) == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
+  }
+  template <typename... P>
+  int launch(void (*fn)(P...), dim3 grid, int threads, int smem, P... args) {
+    void* a[] = {&args...};
+    return launch(reinterpret_cast<const void*>(fn), grid, threads, smem, 1, a);
+  }
+};
+__device__ __forceinline__ void wait_for_earlier() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // Every function returns a pic_status; `ws` is device workspace.
 // What the kernels' bounded waits share: polls that one makes, the device word that
 // is set to 1 when one gives up, and the test hook, which has one epilogue warp of
@@ -370,7 +408,7 @@ struct NarrowGroups {
 };
 bool narrow_group_takes(const NarrowGrad& g, int groups, int dtype);
 long long narrow_group_workspace(const NarrowGrad& g, int groups, int dtype);
-int narrow_group_grad(const NarrowGroups& a, int dtype, void* ws, const Waits& waits, cudaStream_t s);
+int narrow_group_grad(const NarrowGroups& a, int dtype, void* ws, const Waits& waits, Chain& s);
 
 }  // namespace lin
 }  // namespace pic

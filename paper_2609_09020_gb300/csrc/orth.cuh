@@ -68,29 +68,7 @@ struct Job {
 };
 static_assert(sizeof(Job) == 64, "a job is read in four loads");
 
-// The kernels of a call follow one another closely: each but the first is launched when
-// the one before lets it (all its CTAs have started or ended), sets itself up, and waits
-// for the one before to end before it touches what that one does.
-__device__ __forceinline__ void wait_for_earlier() {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-}
-inline int launch_behind(const void* fn, long long grid, int threads, int smem, int cluster, void** args, cudaStream_t s) {
-  cudaLaunchAttribute attr[2] = {};
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = cluster;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(grid));
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cfg.attrs = attr;
-  cfg.numAttrs = cluster == 1 ? 1 : 2;
-  return cudaLaunchKernelExC(&cfg, fn, args) == cudaSuccess ? PIC_OK : PIC_ERR_CUDA;
-}
+using lin::wait_for_earlier;
 
 struct Coefficients {
   float a, b, c;
@@ -121,7 +99,7 @@ __host__ inline long long small_bytes(int m, int n) {
   return 4LL * s.rows * (s.cols + 8) + 8LL * s.rows * (s.rows + 8);
 }
 int launch_small(const Matrix* matrices, const int* list, int n, int smem, int steps, const Coefficients& co, float eps,
-                 cudaStream_t s);
+                 lin::Chain& s);
 
 // Stages of a step: A = X X^T, B = b A + c A^2, X = a X + B X.
 enum Stage { kGram = 0, kPolynomial = 1, kUpdate = 2 };
@@ -141,7 +119,7 @@ struct StageParams {
   Waits waits;
 };
 // With tiles of bn columns: 64 and 128 by one CTA, 256 by a pair.
-int launch_stage(Stage stage, int bn, const StageParams& q, cudaStream_t s);
+int launch_stage(Stage stage, int bn, const StageParams& q, lin::Chain& s);
 
 }  // namespace orth
 }  // namespace pic

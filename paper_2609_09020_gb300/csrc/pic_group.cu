@@ -4,6 +4,7 @@
 
 namespace {
 
+using pic::grp::Chain;
 using pic::grp::GroupProduct;
 using pic::grp::GroupGradAct;
 
@@ -56,14 +57,13 @@ bool args_ok(const pic_grouped_linear_grad_args* a) {
 
 const long long* offsets_of(const int64_t* o) { return reinterpret_cast<const long long*>(o); }
 
-long long product_workspace(const GroupProduct& p, int dtype) {
-  if (pic::grp::tc_takes(p, dtype)) return pic::grp::tc_workspace(p, dtype);
-  return pic::grp::planes_takes(p, dtype) ? pic::grp::planes_workspace(p) : 0;
-}
-int product(const GroupProduct& p, int dtype, void* ws, const pic::lin::Waits& w, cudaStream_t s) {
-  if (pic::grp::tc_takes(p, dtype)) return pic::grp::tc_product(p, dtype, ws, w, s);
-  if (pic::grp::planes_takes(p, dtype)) return pic::grp::planes_product(p, ws, w, s);
-  return pic::grp::any_product(p, dtype, s);
+int product(const GroupProduct& p, int dtype, pic::lin::Arena& ws, bool launch, const pic::lin::Waits& w, Chain& s) {
+  if (pic::grp::tc_takes(p, dtype)) {
+    void* room = ws.take(pic::grp::tc_workspace(p, dtype));
+    return launch ? pic::grp::tc_product(p, dtype, room, w, s) : PIC_OK;
+  }
+  if (pic::grp::planes_takes(p, dtype)) return pic::grp::planes_product(p, ws, launch, w, s);
+  return launch ? pic::grp::any_product(p, dtype, s) : PIC_OK;
 }
 
 // Few rows in the groups: up to `most` on average.
@@ -87,7 +87,7 @@ bool few_backward(const pic_grouped_linear_grad_args& a) {
   return few(a.rows, a.groups, all ? 1 : 4);
 }
 
-int forward(const pic_grouped_linear_args& a, pic::lin::Arena& ws, bool launch, const pic::lin::Waits& w, cudaStream_t s) {
+int forward(const pic_grouped_linear_args& a, pic::lin::Arena& ws, bool launch, const pic::lin::Waits& w, Chain& s) {
   if (a.rows == 0) return PIC_OK;
   GroupProduct p{};
   p.by_rows = true;
@@ -106,14 +106,13 @@ int forward(const pic_grouped_linear_args& a, pic::lin::Arena& ws, bool launch, 
   t.y = a.y, t.ldy = a.ldy, t.pre = a.pre, t.ldpre = a.ldpre, t.act = a.act;
   if (pic::lin::thin_group_takes(t, a.dtype)) {
     const pic::lin::ThinGroups g{p.offsets, a.groups, a.w_group, a.bias_group, w.status};
-    return launch ? pic::lin::thin_group_product(t, a.dtype, g, s) : PIC_OK;
+    return launch ? pic::lin::thin_group_product(t, a.dtype, g, s.stream) : PIC_OK;
   }
   if (few_forward(a)) return launch ? pic::grp::few_forward(p, a.dtype, s) : PIC_OK;
-  void* room = ws.take(product_workspace(p, a.dtype));
-  return launch ? product(p, a.dtype, room, w, s) : PIC_OK;
+  return product(p, a.dtype, ws, launch, w, s);
 }
 
-int backward(const pic_grouped_linear_grad_args& a, pic::lin::Arena& ws, bool launch, const pic::lin::Waits& w, cudaStream_t s) {
+int backward(const pic_grouped_linear_grad_args& a, pic::lin::Arena& ws, bool launch, const pic::lin::Waits& w, Chain& s) {
   const long long M = a.rows, K = a.in_features, N = a.out_features;
   int rc = PIC_OK;
   if (N <= 128 && K <= 128) {
@@ -159,35 +158,31 @@ int backward(const pic_grouped_linear_grad_args& a, pic::lin::Arena& ws, bool la
     g.parts = static_cast<float*>(ws.take(pic::grp::grad_act_workspace(g, a.dtype)));
     if (launch && (rc = pic::grp::grad_act(g, a.dtype, s)) != PIC_OK) return rc;
   }
-  GroupProduct p{};
-  p.a = dz, p.a_i = lddz;
-  p.rows = M, p.groups = a.groups, p.offsets = offsets_of(a.offsets);
-  p.act = PIC_ACT_NONE;
-  p.status = w.status;
-  if (a.dx && M > 0) {
-    p.by_rows = true;
-    p.b = a.w, p.b_group = a.w_group, p.b_j = 1, p.b_k = a.ldw;
-    p.J = K, p.K = N;
-    p.y = a.dx, p.ldy = a.lddx;
-    void* room = ws.take(product_workspace(p, a.dtype));
-    if (launch && (rc = product(p, a.dtype, room, w, s)) != PIC_OK) return rc;
-  }
-  if (a.dw) {
-    p.by_rows = false;
-    p.b = a.x, p.b_group = 0, p.b_j = 1, p.b_k = a.ldx;
-    p.I = N, p.J = K, p.K = 0;
-    p.y = a.dw, p.ldy = a.lddw, p.y_group = a.dw_group;
-    void* room = ws.take(product_workspace(p, a.dtype));
-    if (launch && (rc = product(p, a.dtype, room, w, s)) != PIC_OK) return rc;
-  }
-  return PIC_OK;
+  GroupProduct x{};
+  x.a = dz, x.a_i = lddz;
+  x.rows = M, x.groups = a.groups, x.offsets = offsets_of(a.offsets);
+  x.act = PIC_ACT_NONE;
+  x.status = w.status;
+  GroupProduct v = x;
+  x.by_rows = true;
+  x.b = a.w, x.b_group = a.w_group, x.b_j = 1, x.b_k = a.ldw;
+  x.J = K, x.K = N;
+  x.y = a.dx, x.ldy = a.lddx;
+  v.b = a.x, v.b_j = 1, v.b_k = a.ldx;
+  v.I = N, v.J = K;
+  v.y = a.dw, v.ldy = a.lddw, v.y_group = a.dw_group;
+  if (a.dx && a.dw && pic::grp::planes_takes(x, a.dtype) && pic::grp::planes_takes(v, a.dtype))
+    return pic::grp::planes_gradients(x, v, ws, launch, w, s);
+  if (a.dx && (rc = product(x, a.dtype, ws, launch, w, s)) != PIC_OK) return rc;
+  return a.dw ? product(v, a.dtype, ws, launch, w, s) : PIC_OK;
 }
 
 template <typename Args, typename F>
 int64_t count_bytes(const Args* a, F f) {
   if (!args_ok(a)) return -1;
   pic::lin::Arena ws{nullptr};
-  f(*a, ws, false, pic::lin::Waits{}, nullptr);
+  Chain none{nullptr};
+  f(*a, ws, false, pic::lin::Waits{}, none);
   return ws.used;
 }
 
@@ -201,7 +196,8 @@ int run(const Args* a, F f, void* workspace, size_t bytes, void* stream) {
   pic::lin::Waits w;
   if (!pic::lin::call_waits(w)) return PIC_ERR_CUDA;
   pic::lin::Arena ws{static_cast<char*>(workspace)};
-  const int r = f(*a, ws, true, w, static_cast<cudaStream_t>(stream));
+  Chain s{static_cast<cudaStream_t>(stream)};
+  const int r = f(*a, ws, true, w, s);
   if (r == PIC_ERR_CUDA) cudaGetLastError();
   return r;
 }
