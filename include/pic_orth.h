@@ -12,14 +12,15 @@
  * With the usual coefficients, 3.4445, -4.7750 and 2.0315, five steps take
  * singular values above 0.01 of the largest to between 0.7 and 1.2.
  *
- * The norm is summed as pic_clip.h's.  Between products X is held in two IEEE
- * halves scaled by 4096 (22 bits), sums are fp32, and out is rounded once, to
- * nearest.  Matrices of fp32 and fp16: X, A and b A + c A^2 are held in two
- * halves each, of whose four products three are formed; the fourth is below
- * 2^-22 of a product.  Matrices of bfloat16: products take halves of 11 bits.
- * Measured for full matrices, root mean square error of out's own: fp32 1e-6,
- * bfloat16 2.3e-3 of which its rounding is 1.7e-3.  An infinite or NaN element
- * makes all of its matrix's out NaN (steps > 0), and no other's.
+ * The norm is summed as pic_clip.h's, sums are fp32, and out is rounded once, to
+ * nearest.  Matrices of fp32 and fp16: between products X, A and b A + c A^2 are
+ * held in two IEEE halves each (22 bits, scaled by 4096), of whose four products
+ * three are formed; the fourth is below 2^-22 of a product.  Matrices of
+ * bfloat16: products take halves of 11 bits, and X has a second one, which is
+ * added to a X, but before the last two steps.  Elements of X below 2^-37
+ * are lost.  Measured for full matrices, root mean square error of out's own:
+ * fp32 1e-6, bfloat16 2.3e-3 of which its rounding is 1.7e-3.  An infinite or
+ * NaN element makes all of its matrix's out NaN (steps > 0), and no other's.
  *
  * Conventions as in pic_decode.h: device pointers owned by the caller,
  * asynchronous on `stream`, pic_status codes, no traps.  Results do not vary

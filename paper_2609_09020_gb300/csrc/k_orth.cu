@@ -92,17 +92,23 @@ __global__ void __launch_bounds__(kThreads) squares_kernel(const Matrix* matrice
   double sum = 0.0;
   for_form(m, [&](auto, auto load) {
     float s = 0.0f;
-    bool some = false;  // values that are not zero
+    uint32_t some = 0;  // bits of values that are not zero
 #pragma unroll 4
     for (int c = col; c < end; c += 64) {
       float v[8];
       load(row, c, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s = fmaf(v[e], v[e], s), some |= v[e] != 0.0f;
+      for (int e = 0; e < 8; ++e) s = fmaf(v[e], v[e], s), some |= __float_as_uint(v[e]);
     }
-    sum = s;
-    if (some && !(s >= 1e-28f && s <= 1e37f)) {
-      sum = 0.0;
+    const bool again = some << 1 != 0 && !(s >= 1e-28f && s <= 1e37f);
+    if (!__any_sync(0xffffffffu, again)) {
+      // (fp64 is slow: the first eight lanes' sums in fp32)
+#pragma unroll
+      for (int d = 1; d < 8; d *= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
+      if ((threadIdx.x & 7) == 0) sum = s;
+    } else if (!again) {
+      sum = s;
+    } else {
       for (int c = col; c < end; c += 64) {
         float v[8];
         load(row, c, v);
@@ -140,7 +146,8 @@ __global__ void __launch_bounds__(kThreads) scale_kernel(const Matrix* matrices,
     norm_factors(sum, eps, factors[0], factors[1]);
   }
   __syncthreads();
-  const float f0 = factors[0], f1 = factors[1] * (last ? 1.0f : kScale);
+  const float f0 = factors[0], f1 = last ? factors[1] : kScale;
+  if (threadIdx.x == 0 && p.row0 == 0 && p.col0 == 0) *m.rest = factors[1];
   const int row = p.row0 + threadIdx.x / 8, col = p.col0 + threadIdx.x % 8 * 8, end = min(m.cols, p.col0 + kPieceCols);
   for_form(m, [&](auto t, auto load) {
     using T = decltype(t);
@@ -170,7 +177,8 @@ __global__ void __launch_bounds__(kThreads) scale_kernel(const Matrix* matrices,
       if (row < m.rows) {
         __half* x = m.x[0] + row * m.ldx + c;
         *reinterpret_cast<uint4*>(x) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        *reinterpret_cast<uint4*>(x + m.rows * m.ldx) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        // (16-bit values have no second half, but for subnormal ones of half)
+        if (m.halves == 2) *reinterpret_cast<uint4*>(x + m.rows * m.ldx) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
       }
     }
   });
@@ -401,6 +409,7 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
     std::vector<Job> jobs[3][kShapes];
     long long part_bytes = 0, counters = 0;
     make_jobs(table, jobs, part_bytes, counters);
+    const long long at_rest = take(table.size() * sizeof(float));
     const long long at_matrices = take(table.size() * sizeof(Matrix)), at_maps = take(table.size() * kMaps * sizeof(CUtensorMap)),
                     at_pieces = take(pieces.size() * sizeof(Piece)), at_squares = take(pieces.size() * sizeof(double)),
                     at_parts = take(part_bytes), at_counters = take(counters * 4), at_status = take(4);
@@ -419,6 +428,7 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
     bool ok = true;
     for (size_t i = 0; i < table.size(); ++i) {
       Matrix& t = table[i];
+      t.rest = reinterpret_cast<float*>(h->room + at_rest) + i;
       if (t.parts == 0) continue;
       __half** p[4] = {&t.x[0], &t.x[1], &t.a, &t.b};
       for (int k = 0; k < 4; ++k) {
@@ -505,7 +515,7 @@ int pic_orth(pic_orthogonalizer* h, int steps, float a, float b, float c, float 
     for (const Stage stage : {kGram, kPolynomial, kUpdate})
       for (int shape = 0; shape < kShapes; ++shape) {
         const StageParams q{h->matrices, h->maps, h->n_maps, h->jobs[stage][shape], h->n_jobs[stage][shape], {a, b, c}, k & 1,
-                            k + 1 == steps, h->parts, h->counters, waits};
+                            k == 0, k + 1 == steps, k > 0 && steps - k >= 3, steps - k - 1 >= 3, h->parts, h->counters, waits};
         if (launch_stage(stage, kShapeColumns[shape], q, s) != PIC_OK) {
           cudaGetLastError();
           return PIC_ERR_CUDA;

@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
       const CUtensorMap* map = q.maps + static_cast<long long>(job.matrix) * kMaps + kMapPanel + (STAGE == kUpdate ? q.from : kMapA);
       if (!acquired && map != read) acquire_map(map);
       read = map;
-      const int n = STAGE == kUpdate ? 2 : m.halves;
+      const int n = STAGE == kUpdate ? (m.halves == 2 || q.lo_from ? 2 : 1) : m.halves;
       tc::bulk_wait_read<0>();  // the buffers' last stores have been read
       tc::mbar_arrive_expect_tx(here, n * lin::kPanelBytes);
       for (int z = 0; z < n; ++z) load_3d<false>(buffer + z * lin::kPanelBytes, map, job.j + c0, job.i + below, z, here);
@@ -336,8 +336,10 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
           }
         }
         if (mine) {
-          const bool two = STAGE == kUpdate || m.halves == 2;
-          const float f = (STAGE == kPolynomial ? q.co.c : 1.0f) / kScale;
+          const bool two = m.halves == 2 || (STAGE == kUpdate && q.lo_to), two_old = m.halves == 2 || (STAGE == kUpdate && q.lo_from);
+          // X is the first one's times `rest`
+          const float rest = STAGE != kPolynomial && q.first ? *m.rest : 1.0f;
+          const float f = (STAGE == kPolynomial ? q.co.c : STAGE == kGram ? rest * rest : rest) / kScale;
 #pragma unroll
           for (int c = 0; c < 64; ++c) v[c] *= f;
           if constexpr (STAGE != kGram) {
@@ -347,8 +349,8 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
             }
             in_phase ^= 1;
             coming = false;
-            const float o = STAGE == kPolynomial ? q.co.b : q.co.a;
-            if (two) add_panel(v, o, buffer + lin::kPanelBytes, lane);
+            const float o = STAGE == kPolynomial ? q.co.b : q.co.a * rest;
+            if (two_old) add_panel(v, o, buffer + lin::kPanelBytes, lane);
             add_panel(v, o, buffer, lane);
           } else {
             if (lane == 0) tc::bulk_wait_read<0>();

@@ -8,6 +8,13 @@
 // kScale = 4096 an element of the usual size, 1 / sqrt(max(rows, cols)), is far above
 // the smallest.
 //
+// The first X is G times a power of two, of which bfloat16's and half's values are exact; the
+// rest of 1 / (|G| + eps), `rest` in [1, 2], is in the factors of the first step.  What X's
+// second half is for: the steps multiply what is lost by rounding X outside the singular
+// vectors that G has by a = 3.44 each, and where G has few directions that would show.  With
+// operands of one half (bfloat16) the last two steps but one leave it out: 2^-12 times 12 is
+// no more than out's rounding.
+//
 // A and b A + c A^2 are symmetric, and only their blocks on and below the diagonal are
 // kept (blocks as high as a tile); operands above it are loaded turned.
 #pragma once
@@ -36,6 +43,7 @@ struct Matrix {
   int halves;        // that A, b A + c A^2 and operands of products have
   int part0, parts;  // its runs of squares
   int on16;          // rows of grad start on 16-byte boundaries
+  float* rest;       // of 1 / (|G| + eps)
   __half* x[2];      // [2][rows][ldx]
   __half* a;         // [halves][m][lda]
   __half* b;
@@ -113,7 +121,8 @@ struct StageParams {
   int n;
   Coefficients co;
   int from;   // which X is read
-  int last;   // X goes to out
+  int first, last;  // of the steps: X is still to be multiplied by `rest`; X goes to out
+  int lo_from, lo_to;  // whether X has second halves, of matrices with operands of one half
   float4* parts;
   unsigned* counters;
   Waits waits;

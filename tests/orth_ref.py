@@ -5,7 +5,8 @@ Bounds.  The steps amplify what is rounded on the way by a factor that depends
 on the matrix's singular values, so there is none in closed form that is of use.
 The bound is four times the largest of what two evaluations of the same steps
 are off by, plus the rounding of out:
-  emulated   with the halves that X, A and b A + c A^2 are held in, products and
+  emulated   with the halves that X, A and b A + c A^2 are held in (of bfloat16: X
+             in one before the last two steps, or, by a CTA, in two), products and
              sums otherwise in fp64
   single     all in fp32 (for what sums in fp32 add; a kernel's are other sums
              of the same kind)
@@ -49,8 +50,8 @@ def emulated(g, steps=5, coefficients=USUAL, eps=1e-7):
     x = x / (torch.sqrt((x * x).sum()) + eps)
     flip = x.shape[0] > x.shape[1]
     x = x.t() if flip else x
-    for _ in range(steps):
-        held = halves(x, 2)
+    for k in range(steps):
+        held = halves(x, 2 if n == 2 or steps - k >= 3 else 1)
         u = held if n == 2 else halves(x, 1)
         p = halves(product(u, (u[0].t(), u[1].t())), n)
         q = halves(b * (p[0] + p[1]) + c * product(p, p), n)
