@@ -262,9 +262,10 @@ bool steps_ok(int steps, double a, double b, double c) {
 
 // The jobs of each stage and tile shape, the workspace of their parts and its counters.
 //
-// Shapes: 256 columns by pairs of CTAs, with a third of the time for as many
-// operations, where the list has such tiles for most of the pairs; 64 where the
-// smaller side is no more; else 128.
+// Shapes: 256 columns by pairs of CTAs, which load half as much for as many operations,
+// where the list has such tiles for the pairs twice or nearly; 64 where the smaller side is
+// no more; else 128.  us, 128 / 256 columns: bfloat16 2048 x 2048 243 / 374, two of them 410 /
+// 343, four 757 / 584, 2048 x 8192 608 / 605; fp32 541 / 523, 1029 / 757, 1901 / 1416, 1563 / 1369.
 //
 // Parts: stages with fewer tiles than there are CTAs (kSlots) are cut along K, with at
 // least kLeast slices (of all three products of halves) in a part, as a part more costs 3
@@ -273,6 +274,7 @@ bool steps_ok(int steps, double a, double b, double c) {
 void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kShapes], long long& part_bytes,
                long long& counters) {
   constexpr int kSms = 152, kSlots[kShapes] = {2 * kSms, kSms, kSms / 2}, kLeast = 16, kMost[2] = {256, 64};
+  constexpr long long kLarge = 120;
   const auto blocks = [](long long n, long long of) { return (n + of - 1) / of; };
   long long large = 0;
   for (const Matrix& m : table)
@@ -283,7 +285,7 @@ void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kSh
     for (size_t id = 0; id < table.size(); ++id) {
       const Matrix& m = table[id];
       if (m.parts == 0) continue;  // a CTA's
-      const int shape = m.m <= 64 ? 0 : m.m > 512 && large >= 60 ? 2 : 1;
+      const int shape = m.m <= 64 ? 0 : m.m > 512 && large >= kLarge ? 2 : 1;
       const int bn = kShapeColumns[shape], rows = shape == 2 ? 256 : 128;
       Job j{};
       j.matrix = static_cast<int>(id), j.halves = m.halves, j.parts = 1;
