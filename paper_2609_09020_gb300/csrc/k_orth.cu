@@ -27,6 +27,7 @@ struct pic_orthogonalizer {
   pic::orth::Piece* pieces;
   pic::orth::Job* jobs[3][kShapes];  // of each stage
   int n_jobs[3][kShapes];
+  bool both[kShapes];  // a matrix of the shape has operands of two halves
   double* squares;
   float4* parts;
   unsigned* counters;
@@ -264,28 +265,37 @@ bool steps_ok(int steps, double a, double b, double c) {
 //
 // Shapes: 256 columns by pairs of CTAs, which load half as much for as many operations,
 // where the list has such tiles for the pairs twice or nearly; 64 where the smaller side is
-// no more; else 128.  us, 128 / 256 columns: bfloat16 2048 x 2048 243 / 374, two of them 410 /
+// no more, or where there are few tiles of 128 (us, 64 / 128 columns: fp32 512 x 512 133 /
+// 166, 1024 x 1024 196 / 237, 1500 x 1500 372 / 330; bfloat16 512 x 512 101 / 105, 1024 x 1024
+// 182 / 165); else 128.  us, 128 / 256 columns: bfloat16 2048 x 2048 243 / 374, two of them 410 /
 // 343, four 757 / 584, 2048 x 8192 608 / 605; fp32 541 / 523, 1029 / 757, 1901 / 1416, 1563 / 1369.
 //
 // Parts: stages with fewer tiles than there are CTAs (kSlots) are cut along K, with at
 // least kLeast slices (of all three products of halves) in a part, as a part more costs 3
 // us; and sums of more than kMost slices, in which a tensor
 // core's truncations would show (it loses up to 2^-24 of a sum with each 16 of K).
-void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kShapes], long long& part_bytes,
+void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kShapes], bool (&both)[kShapes], long long& part_bytes,
                long long& counters) {
   constexpr int kSms = 152, kSlots[kShapes] = {2 * kSms, kSms, kSms / 2}, kLeast = 16, kMost[2] = {256, 64};
   constexpr long long kLarge = 120;
   const auto blocks = [](long long n, long long of) { return (n + of - 1) / of; };
-  long long large = 0;
-  for (const Matrix& m : table)
-    if (m.parts > 0 && m.m > 512) large += blocks(m.rows, 256) * blocks(m.cols, 256);
+  long long large = 0, middle = 0;
+  bool two = false;
+  for (const Matrix& m : table) {
+    if (m.parts == 0) continue;
+    if (m.m > 512) large += blocks(m.rows, 256) * blocks(m.cols, 256);
+    middle += blocks(m.rows, 128) * blocks(m.cols, 128);
+    two |= m.halves == 2;
+  }
+  const bool few = middle <= (two ? 110 : 16);
   for (int s = 0; s < 3; ++s) {
     long long tiles[kShapes] = {};
     std::vector<Job> plain[kShapes];
     for (size_t id = 0; id < table.size(); ++id) {
       const Matrix& m = table[id];
       if (m.parts == 0) continue;  // a CTA's
-      const int shape = m.m <= 64 ? 0 : m.m > 512 && large >= kLarge ? 2 : 1;
+      const int shape = m.m <= 64 || few ? 0 : m.m > 512 && large >= kLarge ? 2 : 1;
+      both[shape] |= m.halves == 2;
       const int bn = kShapeColumns[shape], rows = shape == 2 ? 256 : 128;
       Job j{};
       j.matrix = static_cast<int>(id), j.halves = m.halves, j.parts = 1;
@@ -316,7 +326,8 @@ void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kSh
         return a.k1 * (a.halves == 2 ? 3 : 1) > b.k1 * (b.halves == 2 ? 3 : 1);
       });
       tiles[shape] = static_cast<long long>(plain[shape].size());
-      const long long fill = tiles[shape] ? kSlots[shape] / tiles[shape] : 1;
+      const long long slots = both[shape] && shape == 0 ? kSms : kSlots[shape];
+      const long long fill = tiles[shape] ? slots / tiles[shape] : 1;
       const int cg = shape == 2 ? 2 : 1, panels = cg * (kShapeColumns[shape] / 64) * 4;
       int slot = 0;
       for (const Job& j : plain[shape]) {
@@ -410,7 +421,8 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
     }
     std::vector<Job> jobs[3][kShapes];
     long long part_bytes = 0, counters = 0;
-    make_jobs(table, jobs, part_bytes, counters);
+    bool both[kShapes] = {};
+    make_jobs(table, jobs, both, part_bytes, counters);
     const long long at_rest = take(table.size() * sizeof(float));
     const long long at_matrices = take(table.size() * sizeof(Matrix)), at_maps = take(table.size() * kMaps * sizeof(CUtensorMap)),
                     at_pieces = take(pieces.size() * sizeof(Piece)), at_squares = take(pieces.size() * sizeof(double)),
@@ -465,6 +477,7 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
       for (int c = 0; c < kShapes; ++c) {
         h->jobs[s][c] = reinterpret_cast<Job*>(h->room + at_jobs[s][c]);
         h->n_jobs[s][c] = static_cast<int>(jobs[s][c].size());
+        h->both[c] = both[c];
         ok = ok && put(h->jobs[s][c], jobs[s][c]);
       }
     if (!ok || (counters && cudaMemset(h->counters, 0, counters * 4) != cudaSuccess) ||
@@ -518,7 +531,7 @@ int pic_orth(pic_orthogonalizer* h, int steps, float a, float b, float c, float 
       for (int shape = 0; shape < kShapes; ++shape) {
         const StageParams q{h->matrices, h->maps, h->n_maps, h->jobs[stage][shape], h->n_jobs[stage][shape], {a, b, c}, k & 1,
                             k == 0, k + 1 == steps, k > 0 && steps - k >= 3, steps - k - 1 >= 3, h->parts, h->counters, waits};
-        if (launch_stage(stage, kShapeColumns[shape], q, s) != PIC_OK) {
+        if (launch_stage(stage, kShapeColumns[shape], h->both[shape], q, s) != PIC_OK) {
           cudaGetLastError();
           return PIC_ERR_CUDA;
         }

@@ -4,9 +4,12 @@
 // warps): all matrices of a list in one launch, each with tensor maps of its own.
 //
 // Operands are halves of kScale v.  Where values are held in two, a product is three
-// products of halves, the two small ones first: lo hi, hi lo, hi hi.  Each is a run
-// along K of its own in the same accumulators (their operands are loaded three times:
-// the loads keep up with the MMAs at 256 columns).
+// products of halves, lo hi, hi lo and hi hi.  At 256 columns each is a run along K of its
+// own in the same accumulators, the small ones first: their operands are loaded three
+// times, and the loads, 64 bytes a clock into an SM, keep up with the MMAs.  At fewer columns they would
+// not (1024 x 1024 fp32, a call: 245 us): both halves of a slice are loaded together, and
+// the small products have accumulators of their own, so that as few truncating additions as
+// there are slices meet the sums of full size.
 //
 // A = X X^T and A^2 are symmetric: tiles on and below the diagonal are computed and
 // kept.  Where an operand's slice would lie above it, its mirror image is loaded, which
@@ -27,12 +30,14 @@ namespace {
 
 using lin::kSlice;
 
-template <int CG, int BN>
+// BOTH: a stage has both halves of its slices.
+template <int CG, int BN, bool BOTH>
 struct Shape {
   static constexpr int kABytes = 128 * 128, kBRows = BN / CG, kBBytes = kBRows * 128;
-  static constexpr int kStageBytes = kABytes + kBBytes;
-  static constexpr int kCtas = BN == 64 ? 2 : 1;
-  static constexpr int kStages = BN == 64 ? 3 : 5;
+  static constexpr int kHalves = BOTH ? 2 : 1;
+  static constexpr int kStageBytes = kHalves * (kABytes + kBBytes);
+  static constexpr int kCtas = BN == 64 && !BOTH ? 2 : 1;
+  static constexpr int kStages = BOTH ? (BN == 64 ? 4 : 2) : BN == 64 ? 3 : 5;
   static constexpr int kEpi = BN == 64 ? 4 : 8;
   static constexpr int kThreads = 64 + 32 * kEpi;
   static constexpr int kColumns = BN == 64 ? 64 : BN / 2;
@@ -40,7 +45,8 @@ struct Shape {
   static constexpr int kOffBars = kOffPanels + kEpi * 2 * lin::kPanelBytes;
   static constexpr int kBars = 2 * kStages + 4 + 1 + kEpi;
   static constexpr int kSmem = kOffBars + kBars * 8 + 16 + 1024;  // 1024: the base is rounded up
-  static constexpr int kTmemCols = 2 * BN;
+  static constexpr int kBufCols = kHalves * BN;  // BOTH: the sums, and those of the small products
+  static constexpr int kTmemCols = 2 * kBufCols;
 };
 
 template <bool PAIR>
@@ -114,10 +120,10 @@ __device__ __forceinline__ void put_out(const float (&v)[64], float* turn, int l
   }
 }
 
-template <Stage STAGE, int CG, int BN>
-__global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
+template <Stage STAGE, int CG, int BN, bool BOTH>
+__global__ void __launch_bounds__(Shape<CG, BN, BOTH>::kThreads, Shape<CG, BN, BOTH>::kCtas)
     stage_kernel(const __grid_constant__ StageParams q) {
-  using S = Shape<CG, BN>;
+  using S = Shape<CG, BN, BOTH>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = tc::smem_addr(smem_raw);
   uint8_t* smem = smem_raw + ((1024 - (raw & 1023)) & 1023);
@@ -180,28 +186,32 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
         if (!acquired && mq != known[1]) acquire_map(mq);
         known[0] = mp, known[1] = mq;
         const int k0 = job.k0, k1 = job.k1;
-        for (int term = job.halves == 2 ? 0 : 2; term < 3 && ok; ++term) {
-          const int zp = term == 0, zq = term == 1;
+        for (int term = !BOTH && job.halves == 2 ? 0 : 2; term < 3 && ok; ++term) {
+          const int zp = term == 0, zq = term == 1, halves = BOTH ? job.halves : 1;
           for (int kb = k0; kb < k1; ++kb) {
             if (!(ok = wait(bar_empty + 8 * s, phase ^ 1))) break;
-            if (rank == 0) tc::mbar_arrive_expect_tx(bar_full + 8 * s, CG * S::kStageBytes);
-            const uint32_t sa = base + s * S::kStageBytes, sb = sa + S::kABytes, bar = lead_full + 8 * s;
+            if (rank == 0) tc::mbar_arrive_expect_tx(bar_full + 8 * s, CG * halves * (S::kABytes + S::kBBytes));
+            const uint32_t bar = lead_full + 8 * s;
             const int k = kb * kSlice;
             const bool p_mn = lies_along(job.p_mn, job.p_half, job.i, k), q_mn = lies_along(job.q_mn, job.q_half, job.j, k);
             // boxes of 64 x 64 either way
+            for (int h = 0; h < halves; ++h) {
+              const uint32_t sa = base + s * S::kStageBytes + h * S::kABytes,
+                             sb = base + s * S::kStageBytes + S::kHalves * S::kABytes + h * S::kBBytes;
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              if (p_mn)
-                load_3d<CG == 2>(sa + c * 8192, mp, i0 + 64 * c, k, zp, bar);
-              else
-                load_3d<CG == 2>(sa + c * 8192, mp, k, i0 + 64 * c, zp, bar);
-            }
+              for (int c = 0; c < 2; ++c) {
+                if (p_mn)
+                  load_3d<CG == 2>(sa + c * 8192, mp, i0 + 64 * c, k, zp + h, bar);
+                else
+                  load_3d<CG == 2>(sa + c * 8192, mp, k, i0 + 64 * c, zp + h, bar);
+              }
 #pragma unroll
-            for (int c = 0; c < S::kBRows / 64; ++c) {
-              if (q_mn)
-                load_3d<CG == 2>(sb + c * 8192, mq, j0 + 64 * c, k, zq, bar);
-              else
-                load_3d<CG == 2>(sb + c * 8192, mq, k, j0 + 64 * c, zq, bar);
+              for (int c = 0; c < S::kBRows / 64; ++c) {
+                if (q_mn)
+                  load_3d<CG == 2>(sb + c * 8192, mq, j0 + 64 * c, k, zq + h, bar);
+                else
+                  load_3d<CG == 2>(sb + c * 8192, mq, k, j0 + 64 * c, zq + h, bar);
+              }
             }
             if (++s == S::kStages) s = 0, phase ^= 1;
           }
@@ -215,10 +225,10 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
       uint32_t free_phase = 0;
       for (int w = first; w < q.n && ok; w += step) {
         const Job job = q.jobs[w];  // (a copy: through memory each slice would read it again)
-        const int k0 = job.k0, k1 = job.k1, terms = job.halves == 2 ? 3 : 1;
+        const int k0 = job.k0, k1 = job.k1, terms = !BOTH && job.halves == 2 ? 3 : 1;
         if (!(ok = wait(bar_free + 8 * buf, free_phase ^ 1))) break;
         tc::tc_fence_after();
-        const uint32_t d = tmem + buf * BN;
+        const uint32_t d = tmem + buf * S::kBufCols;
         for (int n = 0, kb = k0; n < terms * (k1 - k0); ++n) {
           const bool p_mn = lies_along(job.p_mn, job.p_half, job.i, kb * kSlice),
                      q_mn = lies_along(job.q_mn, job.q_half, job.j, kb * kSlice);
@@ -228,11 +238,18 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
           const uint32_t a_step = p_mn ? 2048 : 32, b_step = q_mn ? 2048 : 32;
           if (!(ok = wait(bar_full + 8 * s, phase))) break;
           tc::tc_fence_after();
-          const uint32_t sa = base + s * S::kStageBytes, sb = sa + S::kABytes;
+          const uint32_t sa = base + s * S::kStageBytes, sb = sa + S::kHalves * S::kABytes;
+          const auto multiply = [&](uint32_t to, uint32_t a, uint32_t b, bool begin) {
 #pragma unroll
-          for (int kk = 0; kk < kSlice / 16; ++kk)
-            tc::mma_16<CG>(d, tc::smem_desc_sw128(sa + kk * a_step, 8192, 1024),
-                           tc::smem_desc_sw128(sb + kk * b_step, 8192, 1024), idesc, (n > 0 || kk > 0) ? 1u : 0u);
+            for (int kk = 0; kk < kSlice / 16; ++kk)
+              tc::mma_16<CG>(to, tc::smem_desc_sw128(a + kk * a_step, 8192, 1024),
+                             tc::smem_desc_sw128(b + kk * b_step, 8192, 1024), idesc, (!begin || kk > 0) ? 1u : 0u);
+          };
+          if (BOTH && job.halves == 2) {
+            multiply(d + BN, sa + S::kABytes, sb, n == 0);
+            multiply(d + BN, sa, sb + S::kBBytes, false);
+          }
+          multiply(d, sa, sb, n == 0);
           tc::mma_commit_cg<CG>(bar_empty + 8 * s);
           if (++s == S::kStages) s = 0, phase ^= 1;
         }
@@ -284,7 +301,7 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
       const int row0 = job.i + below, parts = job.parts;
       if (!__all_sync(0xffffffffu, wait(bar_acc + 8 * buf, phase))) break;
       tc::tc_fence_after();
-      const uint32_t d = tmem + buf * BN + (static_cast<uint32_t>(quarter * 32) << 16);
+      const uint32_t d = tmem + buf * S::kBufCols + (static_cast<uint32_t>(quarter * 32) << 16);
       for (int c0 = from; c0 < to && ok; c0 += 64) {
         float v[64];
         {
@@ -292,6 +309,15 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
           tc::tmem_ld64_wait(d + c0, acc);
 #pragma unroll
           for (int c = 0; c < 64; ++c) v[c] = __uint_as_float(acc[c]);
+        }
+        if (BOTH && job.halves == 2) {
+#pragma unroll
+          for (int h = 0; h < 64; h += 32) {
+            uint32_t small[32];
+            tc::tmem_ld32_wait(d + BN + c0 + h, small);
+#pragma unroll
+            for (int c = 0; c < 32; ++c) v[h + c] += __uint_as_float(small[c]);
+          }
         }
         if (c0 + 64 == to) {
           tc::tc_fence_before();
@@ -431,11 +457,11 @@ __global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
   if (warp == 1) tc::tmem_dealloc_cg<CG>(tmem, S::kTmemCols);
 }
 
-template <Stage STAGE, int CG, int BN>
+template <Stage STAGE, int CG, int BN, bool BOTH>
 int launch(const StageParams& q, int slot, lin::Chain& s) {
-  using S = Shape<CG, BN>;
+  using S = Shape<CG, BN, BOTH>;
   static_assert((S::kSmem + 1024) * S::kCtas <= 228 * 1024, "shared memory of an SM");
-  const void* fn = reinterpret_cast<const void*>(stage_kernel<STAGE, CG, BN>);
+  const void* fn = reinterpret_cast<const void*>(stage_kernel<STAGE, CG, BN, BOTH>);
   if (lin::allow_smem(fn, slot, S::kSmem) != PIC_OK) return PIC_ERR_CUDA;
   const long long want = static_cast<long long>(q.n) * CG, most = 152 * S::kCtas;
   void* args[] = {const_cast<StageParams*>(&q)};
@@ -443,19 +469,19 @@ int launch(const StageParams& q, int slot, lin::Chain& s) {
 }
 
 template <Stage STAGE>
-int launch_bn(int bn, const StageParams& q, lin::Chain& s) {
-  if (bn == 64) return launch<STAGE, 1, 64>(q, 44 + STAGE, s);
-  if (bn == 128) return launch<STAGE, 1, 128>(q, 47 + STAGE, s);
-  return launch<STAGE, 2, 256>(q, 50 + STAGE, s);
+int launch_bn(int bn, bool both, const StageParams& q, lin::Chain& s) {
+  if (bn == 64) return both ? launch<STAGE, 1, 64, true>(q, 64 + STAGE, s) : launch<STAGE, 1, 64, false>(q, 44 + STAGE, s);
+  if (bn == 128) return both ? launch<STAGE, 1, 128, true>(q, 67 + STAGE, s) : launch<STAGE, 1, 128, false>(q, 47 + STAGE, s);
+  return launch<STAGE, 2, 256, false>(q, 50 + STAGE, s);
 }
 
 }  // namespace
 
-int launch_stage(Stage stage, int bn, const StageParams& q, lin::Chain& s) {
+int launch_stage(Stage stage, int bn, bool both, const StageParams& q, lin::Chain& s) {
   if (q.n == 0) return PIC_OK;
-  if (stage == kGram) return launch_bn<kGram>(bn, q, s);
-  if (stage == kPolynomial) return launch_bn<kPolynomial>(bn, q, s);
-  return launch_bn<kUpdate>(bn, q, s);
+  if (stage == kGram) return launch_bn<kGram>(bn, both, q, s);
+  if (stage == kPolynomial) return launch_bn<kPolynomial>(bn, both, q, s);
+  return launch_bn<kUpdate>(bn, both, q, s);
 }
 
 }  // namespace orth

@@ -127,8 +127,9 @@ struct StageParams {
   unsigned* counters;
   Waits waits;
 };
-// With tiles of bn columns: 64 and 128 by one CTA, 256 by a pair.
-int launch_stage(Stage stage, int bn, const StageParams& q, lin::Chain& s);
+// With tiles of bn columns: 64 and 128 by one CTA, 256 by a pair.  both: some matrices have
+// operands of two halves.
+int launch_stage(Stage stage, int bn, bool both, const StageParams& q, lin::Chain& s);
 
 }  // namespace orth
 }  // namespace pic
