@@ -276,6 +276,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncthreads();
   }
   const NarrowGrad& g = GROUPED ? of_group : q.g;
+  // kRun: what a copy has before a tile's rows, which are on 16-byte boundaries only if the group is
+  const int before_dz = GROUPED ? static_cast<int>(origin * g.N * static_cast<int>(sizeof(T)) & 15) : 0;
+  const int before_x = GROUPED ? static_cast<int>(origin * g.K * static_cast<int>(sizeof(T)) & 15) : 0;
   const uint32_t bars = base + S::kOffBars;
   const uint32_t bar_full = bars, bar_empty = bars + 8 * S::kStages, bar_landed = bar_empty + 8 * S::kStages,
                  bar_taken = bar_landed + 8 * kMaxRing, bar_dx = bar_taken + 8 * kMaxRing,
@@ -418,10 +421,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             const int r = unit * S::kUnitRows + row + u * S::kPassRows;
-            const bool here = tile * kTile + r < g.I;
-            vy[u].get_shared(from + (r * g.N + col) * kElem, here ? n_dz : 0);
-            if (has_act) vz[u].get_shared(from + q.raw_z + (r * g.N + col) * kElem, here ? n_dz : 0);
-            if (g.dw) vx[u].get_shared(from + q.raw_x + (r * g.K + col) * kElem, here ? n_x : 0);
+            const bool here = origin + tile * kTile + r < g.I;
+            vy[u].get_shared(from + before_dz + (r * g.N + col) * kElem, here ? n_dz : 0);
+            if (has_act) vz[u].get_shared(from + q.raw_z + before_dz + (r * g.N + col) * kElem, here ? n_dz : 0);
+            if (g.dw) vx[u].get_shared(from + q.raw_x + before_x + (r * g.K + col) * kElem, here ? n_x : 0);
           }
           if (unit + 1 == S::kUnits) {
             __syncwarp();
@@ -553,12 +556,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (long long tile = first; tile < last; tile += step) {
         if (!wait(bar_taken + 8 * ring_s, ring_phase ^ 1)) break;
         const uint32_t at = base + S::kOffRaw + ring_s * q.raw_bytes, bar = bar_landed + 8 * ring_s;
-        const long long rows = min(static_cast<long long>(kTile), g.I - tile * kTile);
+        const long long rows = min(static_cast<long long>(kTile), g.I - origin - tile * kTile);
         uint32_t bytes = 0;
         // whole 16 bytes by an asynchronous copy; the last tile's last few by themselves
-        const auto copy = [&](const void* m, long long cols, uint32_t to, bool go) {
-          const char* from = static_cast<const char*>(m) + tile * kTile * cols * kElem;
-          const int all = static_cast<int>(rows * cols * kElem), whole = all / 16 * 16;
+        const auto copy = [&](const void* m, long long cols, int before, uint32_t to, bool go) {
+          const char* from = static_cast<const char*>(m) + (origin + tile * kTile) * cols * kElem - before;
+          const int all = static_cast<int>(rows * cols * kElem) + before, whole = all / 16 * 16;
           if (!go) {
             bytes += whole;
             for (int e = whole; e < all; e += 2) {
@@ -570,9 +573,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         };
         for (int go = 0; go < 2; ++go) {
-          copy(g.dy, g.N, at, go);
-          if (g.act != PIC_ACT_NONE) copy(g.pre, g.N, at + q.raw_z, go);
-          if (g.dw) copy(g.x, g.K, at + q.raw_x, go);
+          copy(g.dy, g.N, before_dz, at, go);
+          if (g.act != PIC_ACT_NONE) copy(g.pre, g.N, before_dz, at + q.raw_z, go);
+          if (g.dw) copy(g.x, g.K, before_x, at + q.raw_x, go);
           if (!go) tc::mbar_arrive_expect_tx(bar, bytes);
         }
         if (++ring_s == q.raw_ring) ring_s = 0, ring_phase ^= 1;
@@ -752,8 +755,9 @@ int ctas(const NarrowGrad& g, int dtype) {
 template <typename T, bool WIDE>
 bool plan_runs(NarrowParams& q) {
   const NarrowGrad& g = q.g;
-  const int dz = (kTile * g.N * static_cast<int>(sizeof(T)) + 47) / 16 * 16;
-  const int x = (kTile * g.K * static_cast<int>(sizeof(T)) + 47) / 16 * 16;
+  const int more = q.groups > 0 ? 63 : 47;  // grouped: up to 15 bytes before
+  const int dz = (kTile * g.N * static_cast<int>(sizeof(T)) + more) / 16 * 16;
+  const int x = (kTile * g.K * static_cast<int>(sizeof(T)) + more) / 16 * 16;
   q.raw_z = dz;
   q.raw_x = g.act != PIC_ACT_NONE ? 2 * dz : dz;
   q.raw_bytes = (q.raw_x + (g.dw ? x : 0) + 127) / 128 * 128;
@@ -823,7 +827,7 @@ __global__ void __launch_bounds__(MANY ? 1024 : 256) add_group_parts_kernel(cons
 template <typename T, bool WIDE, Source SRC>
 int run_groups(NarrowParams q, NarrowMaps& maps, int slot, Chain& s) {
   const void* fn = reinterpret_cast<const void*>(narrow_kernel<T, WIDE, SRC, true>);
-  constexpr int smem = Shape<T, WIDE, SRC>::kSmem;
+  constexpr int smem = SRC == kRun ? 227 * 1024 : Shape<T, WIDE, SRC>::kSmem;
   static_assert(smem <= 227 * 1024 && sizeof(grp::GroupTable) + 4 <= Shape<T, WIDE, SRC>::kOffW, "shared memory of an SM");
   if (allow_smem(fn, slot, smem) != PIC_OK) return PIC_ERR_CUDA;
   void* args[] = {&q, &maps};
@@ -865,14 +869,21 @@ int narrow_group_grad(const NarrowGroups& a, int dtype, void* ws, const Waits& w
                (!has_z || encode(&maps.z, g.pre, g.I, g.N, g.ldpre, kTile, dtype)) &&
                (!g.dw || encode(&maps.x, g.x, g.I, g.K, g.ldx, kTile, dtype))))
     return PIC_ERR_CUDA;
-  if (dtype == PIC_DTYPE_F32) return run_groups<float, false, kReg>(q, maps, 55, s);
+  // rows end to end, the first on a 16-byte boundary
+  const auto packed = [](const void* m, long long ld, int cols) { return ld == cols && reinterpret_cast<uintptr_t>(m) % 16 == 0; };
+  const bool runs = !tma && packed(g.dy, g.lddy, g.N) && (!has_z || packed(g.pre, g.ldpre, g.N)) && (!g.dw || packed(g.x, g.ldx, g.K));
+  if (dtype == PIC_DTYPE_F32)
+    return runs && plan_runs<float, false>(q) ? run_groups<float, false, kRun>(q, maps, 70, s) : run_groups<float, false, kReg>(q, maps, 55, s);
   if (dtype == PIC_DTYPE_F16) {
-    if (tma) return run_groups<__half, false, kTma>(q, maps, 56, s);
-    return wide ? run_groups<__half, true, kReg>(q, maps, 57, s) : run_groups<__half, false, kReg>(q, maps, 58, s);
+    using H = __half;
+    if (tma) return run_groups<H, false, kTma>(q, maps, 56, s);
+    if (wide) return runs && plan_runs<H, true>(q) ? run_groups<H, true, kRun>(q, maps, 71, s) : run_groups<H, true, kReg>(q, maps, 57, s);
+    return runs && plan_runs<H, false>(q) ? run_groups<H, false, kRun>(q, maps, 72, s) : run_groups<H, false, kReg>(q, maps, 58, s);
   }
   using B = __nv_bfloat16;
   if (tma) return run_groups<B, false, kTma>(q, maps, 59, s);
-  return wide ? run_groups<B, true, kReg>(q, maps, 60, s) : run_groups<B, false, kReg>(q, maps, 61, s);
+  if (wide) return runs && plan_runs<B, true>(q) ? run_groups<B, true, kRun>(q, maps, 73, s) : run_groups<B, true, kReg>(q, maps, 60, s);
+  return runs && plan_runs<B, false>(q) ? run_groups<B, false, kRun>(q, maps, 74, s) : run_groups<B, false, kReg>(q, maps, 61, s);
 }
 
 bool narrow_takes(const NarrowGrad& g, int dtype) {

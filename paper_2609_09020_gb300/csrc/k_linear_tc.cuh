@@ -827,7 +827,7 @@ bool encode_many(CUtensorMap* map, const void* m, long long rows, long long cols
 bool encode_planes(CUtensorMap* map, const void* m, long long rows, long long cols, long long ld, int box_cols, int box_rows);
 // Allows a kernel `smem` bytes of shared memory, once per device; each kernel of
 // these files has a slot of its own below kSmemSlots.
-constexpr int kSmemSlots = 72;
+constexpr int kSmemSlots = 80;
 int allow_smem(const void* fn, int slot, int smem);
 
 // The kernel for tiles of bn columns: 64 and 128 by one CTA, 256 by a pair.
