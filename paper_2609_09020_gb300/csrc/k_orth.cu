@@ -419,6 +419,9 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
       for (int i = 0; i < 2; ++i) at.push_back(take(t.halves * t.m * t.lda * 2));
       table.push_back(t);
     }
+    // long ones first, for CTAs of their own
+    for (std::vector<int>& ids : small)
+      std::stable_sort(ids.begin(), ids.end(), [&](int a, int b) { return small_time(table[a]) > small_time(table[b]); });
     std::vector<Job> jobs[3][kShapes];
     long long part_bytes = 0, counters = 0;
     bool both[kShapes] = {};
