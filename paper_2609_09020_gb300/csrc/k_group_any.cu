@@ -1,7 +1,8 @@
 // k_group_any.cu -- grouped products of any type, stride and size on the FP32
 // cores: tiles of 64 x 64, 16 of K at a time through shared memory, sixteen sums a
 // thread.  CTAs are persistent, with the table of groups in shared memory, and take
-// tiles one after another.
+// tiles one after another.  Measured: 16 of K of such a tile take from 1.3 us to 4 with four
+// CTAs on each SM; fp32 400 x 300 -> 300 in four groups 23 us.
 #include "group.cuh"
 
 namespace pic {

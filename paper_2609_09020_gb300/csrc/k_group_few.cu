@@ -15,7 +15,10 @@
 // Weights (and in the gradients x and dw) whose rows are not on 16-byte boundaries: in the
 // forward the two aligned pieces that have the 16 bytes, shifted; in the gradients lanes
 // have columns 32 apart instead.  Nothing is laid out first, which for weights would be
-// three times their traffic (bf16, 120 groups of 1687 -> 3869 with 76 rows: 654 us so).
+// three times their traffic.
+//
+// Measured: 64 groups with 96 rows (half of the groups have none) fp32 2048 -> 2048 110 us, 4.6
+// TB/s of weights (tiles of 64 x 64 703); bf16 2047 -> 4096 203 us (laid out first 458).
 #include "group.cuh"
 
 namespace pic {

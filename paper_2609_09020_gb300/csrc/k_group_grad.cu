@@ -2,7 +2,8 @@
 // act'(z), and its column sums over each group's rows.  As k_linear_grad.cu, bound by
 // memory: a thread takes 16 bytes of neighbouring columns of every so many-th row of a
 // run of rows of one group; the block adds its threads' sums in shared memory, and a
-// second kernel the sums of a group's runs in order.
+// second kernel the sums of a group's runs in order.  Measured: bf16 8192 x 4096 GELU with dz
+// 45 us for 201 MB, 4.5 TB/s (GELU' is some 20 instructions an element).
 #include "group.cuh"
 
 namespace pic {

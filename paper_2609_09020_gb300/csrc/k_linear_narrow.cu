@@ -38,7 +38,9 @@
 // GROUPED (include/pic_group.h): a tile is 128 rows of one group, and a CTA has a piece of
 // one group's tiles.  Pieces are about as long as can be for as many of them as there are
 // CTAs at once (or a multiple of that).  A group's last tile ends with it: what is behind is
-// zero in dz and x, and dx is not written there.
+// zero in dz and x, and dx is not written there.  Measured: fp16 1000000 x 64 -> 64 ReLU in
+// 24 groups 92 us, 5.6 TB/s (a CTA that goes through its share group by group 110; twice as
+// many, shorter pieces 122).
 #include "cut3.cuh"
 #include "group.cuh"
 #include "k_linear_tc.cuh"

@@ -1,5 +1,6 @@
 // k_orth.cu -- orthogonalised updates (include/pic_orth.h): the handle with its
-// lists of jobs, and the norms.
+// lists of jobs, and the norms.  Measured: squares and first X of 50 million bf16 elements 43 and
+// 45 us.
 #include <algorithm>
 #include <cmath>
 #include <new>

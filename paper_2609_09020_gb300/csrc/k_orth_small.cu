@@ -3,8 +3,7 @@
 // memory as halves (orth.cuh), whichever side is the smaller one first, and warp-level
 // MMAs (m16n8k16).  What bounds it is the chain: five steps are 15 products that wait on
 // one another, some 0.6 us each for 64 x 64, where launches of the tiled kernels are 6 us
-// each.  Measured: 192 matrices of 64 nets (64 x 7, 64 x 64, 3 x 64), fp32, in all 105 us
-// by tiles.
+// each.  Measured: 192 matrices of 64 nets (64 x 7, 64 x 64, 3 x 64), fp32, 29 us (by tiles 105).
 //
 //   A, and b A + c A^2   a warp has 16 rows x 32 columns at a time
 //   X = a X + B X        a warp has eight columns of all rows: what it reads of X is what
