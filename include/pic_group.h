@@ -10,7 +10,8 @@
  *   backward  dz = dy * act'(z),  dx = dz w_g,  dw_g = dz_g^T x_g,
  *             db_g = sum of dz over the group's rows
  *
- * with act, types, sums and roundings as in pic_linear.h.  Rows of one group
+ * with act, types, sums and roundings as in pic_linear.h (dz of a 16-bit type
+ * may be rounded to it before the products or not; db sums it unrounded).  Rows of one group
  * never meet those of another: a NaN stays in its group.  A group without rows
  * has gradients of zero.  Rows before offsets[0] and from offsets[groups] on
  * belong to no group: nothing of them is read, and y, pre and dx are not

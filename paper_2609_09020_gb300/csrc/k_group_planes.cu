@@ -549,6 +549,9 @@ Plan plan(const GroupProduct& p) {
 // with four on each SM)
 bool planes_takes(const GroupProduct& p, int dtype) {
   if (dtype != PIC_DTYPE_F32 || p.a_pre || p.rows == 0) return false;
+  // rows of the planes are counted in 32 bits
+  const long long w_rows = p.by_rows ? p.groups * round_up(p.b_k == 1 ? p.J : p.K, kAlign) : 0;
+  if (w_rows > 0x7fffffffLL - kPlRows || p.rows + static_cast<long long>(p.groups) * kAlign > 0x7fffffffLL - kPlRows) return false;
   const double each = static_cast<double>(p.rows) / p.groups;
   const auto up = [](double a, double b) { return static_cast<double>(static_cast<long long>((a + b - 1) / b)); };
   const double k = p.by_rows ? static_cast<double>(p.K) : each;

@@ -60,7 +60,7 @@ template <typename T, bool ON16>
 __device__ __forceinline__ void load8(const Matrix& m, int row, int col, float (&v)[8]) {
   constexpr int kBytes = static_cast<int>(sizeof(T));
   const char* at = reinterpret_cast<const char*>(static_cast<const T*>(m.grad) + row * m.ld_grad + col);
-  const int bytes = row < m.rows ? (m.cols - col) * kBytes : 0;
+  const int bytes = row < m.rows ? min(8, m.cols - col) * kBytes : 0;
 #pragma unroll
   for (int h = 0; h < kBytes / 2; ++h) {
     pic::lin::Piece16<ON16> p;
@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(kThreads) squares_kernel(const Matrix* matrice
   __shared__ double sums[kThreads / 32];
   const Piece p = pieces[blockIdx.x];
   const Matrix& m = matrices[p.matrix];
-  const int row = p.row0 + threadIdx.x / 8, col = p.col0 + threadIdx.x % 8 * 8, end = min(m.cols, p.col0 + kPieceCols);
+  const int row = p.row0 + threadIdx.x / 8, col = p.col0 + threadIdx.x % 8 * 8, end = p.col0 + min(m.cols - p.col0, kPieceCols);
   wait_for_earlier();
   double sum = 0.0;
   for_form(m, [&](auto, auto load) {
@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(kThreads) scale_kernel(const Matrix* matrices,
   __syncthreads();
   const float f0 = factors[0], f1 = last ? factors[1] : kScale;
   if (threadIdx.x == 0 && p.row0 == 0 && p.col0 == 0) *m.rest = factors[1];
-  const int row = p.row0 + threadIdx.x / 8, col = p.col0 + threadIdx.x % 8 * 8, end = min(m.cols, p.col0 + kPieceCols);
+  const int row = p.row0 + threadIdx.x / 8, col = p.col0 + threadIdx.x % 8 * 8, end = p.col0 + min(m.cols - p.col0, kPieceCols);
   for_form(m, [&](auto t, auto load) {
     using T = decltype(t);
 #pragma unroll 2

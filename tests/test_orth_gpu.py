@@ -189,6 +189,23 @@ def test_many_matrices(pic):
         ref.check(o, t)
 
 
+def test_offsets_past_32_bits(pic):
+    """A matrix of more than 2^31 elements: zeros but for columns at both ends, which come to
+    what the matrix of these columns alone does."""
+    rows, cols = 20, 2 ** 27 + 40
+    at = torch.cat([torch.arange(0, 77), torch.arange(cols - 300, cols)]).cuda()
+    few = normal((rows, len(at)), BF16, seed=22)
+    g = torch.zeros((rows, cols), dtype=BF16, device="cuda")
+    g[:, at] = few
+    h = pic.Orthogonalizer([g])
+    h.orthogonalize()
+    h.check()
+    h.close()
+    ref.check(g[:, at], few)
+    g[:, at] = 0
+    assert not g.any()
+
+
 def test_refusals(pic):
     z = lambda *s, **o: torch.zeros(s, device="cuda", **o)
     buf = z(100)
