@@ -54,32 +54,50 @@ struct Held {
   }
 };
 
-// Rows 16 i.. and columns 32 j.. of P P^T.
+// Rows 16 i.. and columns 32 j.. of P P^T.  An MMA truncates what it adds: the products of
+// small halves have sums of their own, and those of the others are 64 of K long and added to
+// nearest (4 x 572, fp32, five steps: out is off by 1.1e-5 if all go into one, and by 1.8e-6 so).
+constexpr int kRun = 64;
 template <bool TWO>
 __device__ __forceinline__ void square(float (&acc)[4][4], const Held p, int i, int j, int deep, int lane) {
+  float low[4][4] = {};
 #pragma unroll
   for (int n = 0; n < 4; ++n)
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[n][e] = 0.0f;
   const __half* pa = p.hi + (16 * i + (lane & 15)) * p.ld + (lane >> 4) * 8;
   const __half* pb = p.hi + (32 * j + (lane & 7) + (lane >> 4) * 8) * p.ld + (lane >> 3 & 1) * 8;
+  for (int k0 = 0; k0 < deep; k0 += kRun) {
+    float run[4][4] = {};
+    const int k1 = min(deep, k0 + kRun);
 #pragma unroll 2
-  for (int k = 0; k < deep; k += 16) {
-    uint32_t a[4], al[4], b[2][4], bl[2][4];
-    ldsm4(a, pa + k);
+    for (int k = k0; k < k1; k += 16) {
+      uint32_t a[4], al[4], b[2][4], bl[2][4];
+      ldsm4(a, pa + k);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) ldsm4(b[h], pb + 16 * h * p.ld + k);
-    if (TWO) {
-      ldsm4(al, pa + p.lo + k);
+      for (int h = 0; h < 2; ++h) ldsm4(b[h], pb + 16 * h * p.ld + k);
+      if (TWO) {
+        ldsm4(al, pa + p.lo + k);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) ldsm4(bl[h], pb + p.lo + 16 * h * p.ld + k);
+        for (int h = 0; h < 2; ++h) ldsm4(bl[h], pb + p.lo + 16 * h * p.ld + k);
 #pragma unroll
-      for (int n = 0; n < 4; ++n) mma(acc[n], al, b[n / 2][n % 2 * 2], b[n / 2][n % 2 * 2 + 1]);
+        for (int n = 0; n < 4; ++n) mma(low[n], al, b[n / 2][n % 2 * 2], b[n / 2][n % 2 * 2 + 1]);
 #pragma unroll
-      for (int n = 0; n < 4; ++n) mma(acc[n], a, bl[n / 2][n % 2 * 2], bl[n / 2][n % 2 * 2 + 1]);
+        for (int n = 0; n < 4; ++n) mma(low[n], a, bl[n / 2][n % 2 * 2], bl[n / 2][n % 2 * 2 + 1]);
+      }
+#pragma unroll
+      for (int n = 0; n < 4; ++n) mma(run[n], a, b[n / 2][n % 2 * 2], b[n / 2][n % 2 * 2 + 1]);
     }
 #pragma unroll
-    for (int n = 0; n < 4; ++n) mma(acc[n], a, b[n / 2][n % 2 * 2], b[n / 2][n % 2 * 2 + 1]);
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[n][e] += run[n][e];
+  }
+  if (TWO) {
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[n][e] += low[n][e];
   }
 }
 

@@ -49,6 +49,15 @@ def test_larger(pic, shape, dtype):
     ref.check(run(pic, [g])[0], g)
 
 
+@pytest.mark.parametrize("steps", [1, 5])
+@pytest.mark.parametrize("shape", [(4, 572), (4, 454), (2, 900), (639, 4), (779, 2), (4, 9000), (2000, 16000)], ids=str)
+def test_long_sums(pic, shape, steps):
+    """Sums far longer than they are many: what each addition loses adds up."""
+    for seed in range(1 if shape[0] == 2000 else 4):
+        g = normal(shape, F32, seed=seed, scale=0.02)
+        ref.check(run(pic, [g], steps=steps)[0], g, steps=steps, name=f"seed {seed}")
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("shape", [(64, 64), (48, 100), (160, 160), (320, 200)], ids=str)
 def test_few_directions(pic, shape, dtype):
