@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(256) sum_parts_kernel(const GroupGradAct g, co
   __shared__ float sums[4][64];
   wait_for_earlier();
   const int at = blockIdx.y, tx = threadIdx.x % 64, ty = threadIdx.x / 64;
-  const int p0 = tiles[at], p1 = tiles[at + 1];
+  const int p0 = __ldcg(tiles + at), p1 = __ldcg(tiles + at + 1);
   if (p1 - p0 < 2) return;
   const long long j = blockIdx.x * 64LL + tx;
   float sum = 0.0f;

@@ -288,6 +288,9 @@ int tc_product(const GroupProduct& p, int dtype, void* ws, const Waits& waits, C
     const MakeMaps mk{p.offsets, p.rows, {static_cast<const char*>(a.m), static_cast<const char*>(b.m)}, {a.ld * 2, b.ld * 2},
                       const_cast<CUtensorMap*>(q.maps)};
     if (s.launch(maps_kernel, dim3(p.groups), 32, 0, mk, maps) != PIC_OK) return PIC_ERR_CUDA;
+    // maps that change under a kernel that has begun are as good as unmapped addresses if
+    // one is read too early: no more is built on than that a kernel sees what ended before it
+    s.settle();
   }
   const GtKernel k = dtype == PIC_DTYPE_BF16 ? group_kernel_bf16(r.mode, r.bn) : group_kernel_f16(r.mode, r.bn);
   if (lin::allow_smem(k.fn, k.slot, k.smem) != PIC_OK) return PIC_ERR_CUDA;

@@ -216,8 +216,10 @@ __global__ void __launch_bounds__(GtShape<CG, BN, MODE>::kThreads, GtShape<CG, B
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::kOffBars + 8 * S::kBars + 4);
 
   if (threadIdx.x == 0) {
-    tc::prefetch_map(&maps.b);
-    if (MODE != kSums) tc::prefetch_map(&maps.a);
+    if (MODE != kSums) {
+      tc::prefetch_map(&maps.a);
+      tc::prefetch_map(&maps.b);
+    }
     for (int s = 0; s < S::kStages; ++s) {
       tc::mbar_init(bar_full + 8 * s, 1);
       tc::mbar_init(bar_empty + 8 * s, 1);
