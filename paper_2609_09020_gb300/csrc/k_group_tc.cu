@@ -39,13 +39,14 @@ __global__ void __launch_bounds__(256) pad_kernel(const Pad q) {
   }
 }
 
-// The groups' tensor maps: those of the whole matrices with each group's first row and
-// number of rows.
+// The groups' tensor maps: those of the whole matrices, cut off behind each group's last
+// row.  Their base stays the matrix's, and a group's first row is a coordinate: a map that
+// was encoded for more than 128 KB may be used by the copy engine as if that much were
+// mapped from its base on, and behind a later row it need not be (with the group's first
+// row as the base, sums over a last small group faulted where memory ended behind them).
 struct MakeMaps {
   const long long* offsets;
   long long rows;
-  const char* m[2];
-  long long row_bytes[2];
   CUtensorMap* out;  // [groups][2]
 };
 __global__ void __launch_bounds__(32) maps_kernel(const MakeMaps q, const __grid_constant__ GtMaps maps) {
@@ -63,15 +64,10 @@ __global__ void __launch_bounds__(32) maps_kernel(const MakeMaps q, const __grid
   sm[0][lane] = reinterpret_cast<const uint32_t*>(&maps.a)[lane];
   sm[1][lane] = reinterpret_cast<const uint32_t*>(&maps.b)[lane];
   __syncwarp();
-  if (lane < 2) {
-    const uint32_t at = tc::smem_addr(sm[lane]);
-    asm volatile("tensormap.replace.tile.global_address.shared::cta.b1024.b64 [%0], %1;" ::"r"(at),
-                 "l"(reinterpret_cast<uint64_t>(q.m[lane] + first * q.row_bytes[lane]))
+  if (lane < 2)
+    asm volatile("tensormap.replace.tile.global_dim.shared::cta.b1024.b32 [%0], 1, %1;" ::"r"(tc::smem_addr(sm[lane])),
+                 "r"(static_cast<uint32_t>(last))
                  : "memory");
-    asm volatile("tensormap.replace.tile.global_dim.shared::cta.b1024.b32 [%0], 1, %1;" ::"r"(at),
-                 "r"(static_cast<uint32_t>(last - first))
-                 : "memory");
-  }
   __syncwarp();
 #pragma unroll
   for (int i = 0; i < 2; ++i)
@@ -285,12 +281,8 @@ int tc_product(const GroupProduct& p, int dtype, void* ws, const Waits& waits, C
   }
   if (!ok) return PIC_ERR_CUDA;
   if (!p.by_rows && p.rows > 0) {
-    const MakeMaps mk{p.offsets, p.rows, {static_cast<const char*>(a.m), static_cast<const char*>(b.m)}, {a.ld * 2, b.ld * 2},
-                      const_cast<CUtensorMap*>(q.maps)};
+    const MakeMaps mk{p.offsets, p.rows, const_cast<CUtensorMap*>(q.maps)};
     if (s.launch(maps_kernel, dim3(p.groups), 32, 0, mk, maps) != PIC_OK) return PIC_ERR_CUDA;
-    // maps that change under a kernel that has begun are as good as unmapped addresses if
-    // one is read too early: no more is built on than that a kernel sees what ended before it
-    s.settle();
   }
   const GtKernel k = dtype == PIC_DTYPE_BF16 ? group_kernel_bf16(r.mode, r.bn) : group_kernel_f16(r.mode, r.bn);
   if (lin::allow_smem(k.fn, k.slot, k.smem) != PIC_OK) return PIC_ERR_CUDA;

@@ -273,9 +273,10 @@ __global__ void __launch_bounds__(GtShape<CG, BN, MODE>::kThreads, GtShape<CG, B
           const int k = kb * kSlice;
           if constexpr (MODE == kSums) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c) tc::tma_load_2d<CG == 2>(sa + c * 8192, ma, i0 + 64 * c, k, bar);
+            for (int c = 0; c < 2; ++c) tc::tma_load_2d<CG == 2>(sa + c * 8192, ma, i0 + 64 * c, m.first + k, bar);
 #pragma unroll
-            for (int c = 0; c < S::kBRows / 64; ++c) tc::tma_load_2d<CG == 2>(sb + c * 8192, mb, j0 + 64 * c, k, bar);
+            for (int c = 0; c < S::kBRows / 64; ++c)
+              tc::tma_load_2d<CG == 2>(sb + c * 8192, mb, j0 + 64 * c, m.first + k, bar);
           } else if constexpr (MODE == kRows) {
             tc::tma_load_2d<CG == 2>(sa, ma, k, i0, bar);
             if (q.b_mn) {

@@ -251,7 +251,6 @@ inline int launch_kernel(const void* fn, long long grid, int threads, int smem, 
 struct Chain {
   cudaStream_t stream;
   bool begun = false;
-  void settle() { begun = false; }  // the next kernel begins when all before it have ended
   int launch(const void* fn, dim3 grid, int threads, int smem, int cluster, void** args) {
     cudaLaunchAttribute attr[2] = {};
     cudaLaunchConfig_t cfg{};

@@ -450,3 +450,23 @@ def test_narrow_groups_keep_to_themselves(pic, bad, dtype):
             assert not dw[2].any() and not db[2].any()
             assert not torch.isfinite(dw[1]).any() and not torch.isfinite(db[1]).any()
         pic.grouped_linear_check()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=str)
+@pytest.mark.parametrize("last", [1, 28, 70])
+def test_rows_at_the_end_of_an_allocation(pic, dtype, last):
+    """x and dy end where the allocator's segments of memory do, with a small group's rows."""
+    rows, inp, outp = 500, 232, 376
+    offsets = [0, 200, rows - last, rows]
+
+    def at_end(cols, seed):
+        held = torch.empty(6 << 20, dtype=dtype, device="cuda")  # 12 MB: a segment of its own
+        t = held[held.numel() - rows * cols:].view(rows, cols)
+        return t.copy_(normal((rows, cols), dtype, seed))
+
+    x, dy, w = at_end(inp, 1), at_end(outp, 2), normal((3, outp, inp), dtype, 3, inp ** -0.5)
+    _, dw, db = pic.grouped_linear_backward(dy, x, w, offsets_tensor(offsets), need=("weight", "bias"))
+    pic.grouped_linear_check()
+    _, ww, wb = group_ref.backward(dy, x, w, None, offsets, "none")
+    ref.check(dw, ww, "dw")
+    ref.check(db, wb, "db")
