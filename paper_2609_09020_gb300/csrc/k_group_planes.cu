@@ -15,7 +15,8 @@
 // that its rows or columns meet there is marked.
 //
 // Measured: the gradient of 16 groups of 256 -> 512 with 4096 rows 82 us (by FP32 FMAs 143):
-// six launches, of which the two products are 12 us each; 16000 x 300 -> 1000 91 us (435).
+// six launches (with cold caches dz and db 17 us, the cut 18, the products 29 and 30, parts
+// 12), whose 100 or so tiles are less than two rounds; 16000 x 300 -> 1000 91 us (435).
 #include "cut3.cuh"
 #include "group.cuh"
 #include "k_linear_planes.cuh"
