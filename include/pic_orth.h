@@ -16,12 +16,13 @@
  * nearest.  Matrices of fp32 and fp16: between products X, A and b A + c A^2 are
  * held in two IEEE halves each (22 bits, scaled by 4096), of whose four products
  * three are formed; the fourth is below 2^-22 of a product.  Matrices of
- * bfloat16: products take halves of 11 bits, and X has a second one, which is
- * added to a X, but before the last two steps.  Elements of X below 2^-37
+ * bfloat16 do so too where they are small, all of up to 64 on the smaller side
+ * among them; of others products take halves of 11 bits, and X has a second one,
+ * which is added to a X, but before the last two steps.  Elements of X below 2^-37
  * are lost.  Measured for full matrices, root mean square error of out's own:
  * fp32 1e-6 (64 x 64), 6e-6 (256 x 2048), 4e-5 (4000 x 12000), of which all but
- * 1e-6, 3e-6 and 8e-6 are the tensor cores' truncating additions; bfloat16
- * 2.3e-3 of which its rounding is 1.7e-3.  An infinite or
+ * 1e-6, 3e-6 and 8e-6 are the tensor cores' truncating additions; bfloat16 1.7e-3
+ * to 2.3e-3, of which its rounding is 1.7e-3.  An infinite or
  * NaN element makes all of its matrix's out NaN (steps > 0), and no other's.
  *
  * Conventions as in pic_decode.h: device pointers owned by the caller,

@@ -230,10 +230,10 @@ bool outputs_disjoint(const std::vector<pic_orth_matrix>& list) {
 
 // What five steps of a matrix take one CTA, in us (measured, of fp32: 32 x 32 15, 32 x 1000
 // 100, 64 x 64 25, 64 x 256 62, 64 x 512 109, 128 x 128 115; by tiles 200 x 200 takes 127,
-// 512 x 512 168; bfloat16 three quarters of that).
+// 512 x 512 168).
 double small_time(const Matrix& m) {
   const double n = std::max(m.rows, m.cols);
-  return (m.m <= 32 ? 12 + 0.09 * n : m.m <= 64 ? 13 + 0.19 * n : 50 + 0.6 * n) * (m.halves == 2 ? 1.0 : 0.75);
+  return m.m <= 32 ? 12 + 0.09 * n : m.m <= 64 ? 13 + 0.19 * n : 50 + 0.6 * n;
 }
 
 // Whether the singular values that steps meet, from [0, 1], stay in [-2, 2], and b s^2 + c
@@ -276,10 +276,11 @@ bool steps_ok(int steps, double a, double b, double c) {
 // us; and sums of more than kMost slices, in which a tensor core's truncations show (it
 // loses up to 2^-24 of a sum with each 16 of K; one half's own roundings are larger).  fp32
 // 4000 x 12000, out's error and time: 64 slices 8.5e-5, 6.5 ms; 32 4.4e-5, 7.2 ms; 16
-// 2.3e-5, 11.1 ms.
+// 2.3e-5, 11.1 ms.  With 128 columns 24 matrices of three types, sides up to 1500: 32 2.0e-6,
+// 170 us, 8 1.7e-6, 170 us, but four 700 x 700 alone 209 and 324 us; 16 leaves those at 209.
 void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kShapes], bool (&both)[kShapes], long long& part_bytes,
                long long& counters) {
-  constexpr int kSms = 152, kSlots[kShapes] = {2 * kSms, kSms, kSms / 2}, kLeast = 16, kMost[2] = {256, 32};
+  constexpr int kSms = 152, kSlots[kShapes] = {2 * kSms, kSms, kSms / 2}, kLeast = 16, kMost[2][kShapes] = {{256, 256, 256}, {32, 16, 32}};
   constexpr long long kLarge = 120;
   const auto blocks = [](long long n, long long of) { return (n + of - 1) / of; };
   long long large = 0, middle = 0;
@@ -334,7 +335,7 @@ void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kSh
       const int cg = shape == 2 ? 2 : 1, panels = cg * (kShapeColumns[shape] / 64) * 4;
       int slot = 0;
       for (const Job& j : plain[shape]) {
-        const int slices = j.k1, most = kMost[j.halves - 1];
+        const int slices = j.k1, most = kMost[j.halves - 1][shape];
         const int passes = j.halves == 2 ? 3 : 1;
         long long parts = std::max<long long>(std::min<long long>(fill, slices * passes / kLeast), blocks(slices, most));
         parts = std::max<long long>(parts, 1);
@@ -401,6 +402,8 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
       t.grad = m.grad, t.out = m.out, t.ld_grad = m.ld_grad, t.ld_out = m.ld_out;
       t.rows = static_cast<int>(m.rows), t.cols = static_cast<int>(m.cols), t.dtype = m.dtype;
       t.m = std::min(t.rows, t.cols), t.left = t.rows <= t.cols;
+      // (for a CTA by itself no difference: it takes products of both halves always, as 192
+      // bfloat16 matrices of 64 nets take 29 us so and 23 in one half, but 8 x 8 2.7e-3 of error)
       t.halves = m.dtype == PIC_DTYPE_BF16 ? 1 : 2;
       t.ldx = (m.cols + 63) / 64 * 64, t.lda = (t.m + 63) / 64 * 64;  // whole panels
       const long long need = t.m <= 128 ? small_bytes(t.m, t.left ? t.cols : t.rows) : kSmallMost + 1LL;
@@ -413,6 +416,10 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
         table.push_back(t);
         continue;
       }
+      // bfloat16 in one half, out's error of five steps (its rounding alone 1.7e-3) and time:
+      // 64 x 1000 2.4e-3, 300 x 1500 2.3e-3, 1500 x 1500 1.9e-3; eight 64 x 4096 129 us, in two
+      // 167, eight 128 x 4096 140 and 191
+      if (t.m <= 64) t.halves = 2;
       t.part0 = static_cast<int>(pieces.size());
       for (long long r = 0; r < t.rows; r += 32)
         for (long long c = 0; c < t.cols; c += kPieceCols) pieces.push_back({id, static_cast<int>(r), static_cast<int>(c)});

@@ -58,7 +58,6 @@ struct Held {
 // small halves have sums of their own, and those of the others are 64 of K long and added to
 // nearest (4 x 572, fp32, five steps: out is off by 1.1e-5 if all go into one, and by 1.8e-6 so).
 constexpr int kRun = 64;
-template <bool TWO>
 __device__ __forceinline__ void square(float (&acc)[4][4], const Held p, int i, int j, int deep, int lane) {
   float low[4][4] = {};
 #pragma unroll
@@ -76,15 +75,13 @@ __device__ __forceinline__ void square(float (&acc)[4][4], const Held p, int i, 
       ldsm4(a, pa + k);
 #pragma unroll
       for (int h = 0; h < 2; ++h) ldsm4(b[h], pb + 16 * h * p.ld + k);
-      if (TWO) {
-        ldsm4(al, pa + p.lo + k);
+      ldsm4(al, pa + p.lo + k);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) ldsm4(bl[h], pb + p.lo + 16 * h * p.ld + k);
+      for (int h = 0; h < 2; ++h) ldsm4(bl[h], pb + p.lo + 16 * h * p.ld + k);
 #pragma unroll
-        for (int n = 0; n < 4; ++n) mma(low[n], al, b[n / 2][n % 2 * 2], b[n / 2][n % 2 * 2 + 1]);
+      for (int n = 0; n < 4; ++n) mma(low[n], al, b[n / 2][n % 2 * 2], b[n / 2][n % 2 * 2 + 1]);
 #pragma unroll
-        for (int n = 0; n < 4; ++n) mma(low[n], a, bl[n / 2][n % 2 * 2], bl[n / 2][n % 2 * 2 + 1]);
-      }
+      for (int n = 0; n < 4; ++n) mma(low[n], a, bl[n / 2][n % 2 * 2], bl[n / 2][n % 2 * 2 + 1]);
 #pragma unroll
       for (int n = 0; n < 4; ++n) mma(run[n], a, b[n / 2][n % 2 * 2], b[n / 2][n % 2 * 2 + 1]);
     }
@@ -93,16 +90,14 @@ __device__ __forceinline__ void square(float (&acc)[4][4], const Held p, int i, 
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[n][e] += run[n][e];
   }
-  if (TWO) {
 #pragma unroll
-    for (int n = 0; n < 4; ++n)
+  for (int n = 0; n < 4; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[n][e] += low[n][e];
-  }
+    for (int e = 0; e < 4; ++e) acc[n][e] += low[n][e];
 }
 
 // STRIPS x 16 rows are those of X.
-template <int STRIPS, bool TWO>
+template <int STRIPS>
 __device__ __forceinline__ void steps_of(const Held x, const Held a, const Held b, const int cols, const int steps, const Coefficients co) {
   constexpr int M = 16 * STRIPS;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -110,7 +105,7 @@ __device__ __forceinline__ void steps_of(const Held x, const Held a, const Held 
     for (int u = warp; u < STRIPS * (M / 32); u += kWarps) {
       const int i = u % STRIPS, j = u / STRIPS;
       float acc[4][4];
-      square<TWO>(acc, x, i, j, cols, lane);
+      square(acc, x, i, j, cols, lane);
 #pragma unroll
       for (int n = 0; n < 4; ++n)
 #pragma unroll
@@ -122,15 +117,13 @@ __device__ __forceinline__ void steps_of(const Held x, const Held a, const Held 
     for (int u = warp; u < STRIPS * (M / 32); u += kWarps) {
       const int i = u % STRIPS, j = u / STRIPS;
       float acc[4][4];
-      square<TWO>(acc, a, i, j, M, lane);
+      square(acc, a, i, j, M, lane);
 #pragma unroll
       for (int n = 0; n < 4; ++n)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int at = (16 * i + g + 8 * h) * a.ld + 32 * j + 8 * n + 2 * t;
-          float2 old = a.get(at);
-          // what the other path holds of an A in one half
-          if (!TWO) old = __half22float2(*reinterpret_cast<const __half2*>(a.hi + at));
+          const float2 old = a.get(at);
           b.put(at, fmaf(co.b, old.x, acc[n][2 * h] * (co.c / kScale)), fmaf(co.b, old.y, acc[n][2 * h + 1] * (co.c / kScale)));
         }
     }
@@ -142,18 +135,16 @@ __device__ __forceinline__ void steps_of(const Held x, const Held a, const Held 
         uint32_t q[2], ql[2];
         const __half* pq = x.hi + (k + (lane & 15)) * x.ld + 8 * j;
         ldsm2_turned(q, pq);
-        if (TWO) ldsm2_turned(ql, pq + x.lo);
+        ldsm2_turned(ql, pq + x.lo);
 #pragma unroll
         for (int i = 0; i < STRIPS; ++i) {
           uint32_t p[4];
           const __half* pp = b.hi + (16 * i + (lane & 15)) * b.ld + (lane >> 4) * 8 + k;
           ldsm4(p, pp);
-          if (TWO) {
-            uint32_t pl[4];
-            ldsm4(pl, pp + b.lo);
-            mma(acc[i], pl, q[0], q[1]);
-            mma(acc[i], p, ql[0], ql[1]);
-          }
+          uint32_t pl[4];
+          ldsm4(pl, pp + b.lo);
+          mma(acc[i], pl, q[0], q[1]);
+          mma(acc[i], p, ql[0], ql[1]);
           mma(acc[i], p, q[0], q[1]);
         }
       }
@@ -262,13 +253,12 @@ __global__ void __launch_bounds__(kThreads) small_kernel(const Matrix* matrices,
   else
     load_scaled<__nv_bfloat16>(m, x, eps, sums, factors);
   __syncthreads();
-  const bool two = m.halves == 2;
   if (s.rows == 32)
-    two ? steps_of<2, true>(x, a, b, s.cols, steps, co) : steps_of<2, false>(x, a, b, s.cols, steps, co);
+    steps_of<2>(x, a, b, s.cols, steps, co);
   else if (s.rows == 64)
-    two ? steps_of<4, true>(x, a, b, s.cols, steps, co) : steps_of<4, false>(x, a, b, s.cols, steps, co);
+    steps_of<4>(x, a, b, s.cols, steps, co);
   else
-    two ? steps_of<8, true>(x, a, b, s.cols, steps, co) : steps_of<8, false>(x, a, b, s.cols, steps, co);
+    steps_of<8>(x, a, b, s.cols, steps, co);
   if (m.dtype == PIC_DTYPE_F32)
     store_out<float>(m, x);
   else if (m.dtype == PIC_DTYPE_F16)

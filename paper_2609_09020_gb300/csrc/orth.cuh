@@ -12,7 +12,7 @@
 // rest of 1 / (|G| + eps), `rest` in [1, 2], is in the factors of the first step.  What X's
 // second half is for: the steps multiply what is lost by rounding X outside the singular
 // vectors that G has by a = 3.44 each, and where G has few directions that would show.  With
-// operands of one half (bfloat16) the last two steps but one leave it out: 2^-12 times 12 is
+// operands of one half (bfloat16, if not small) the last two steps but one leave it out: 2^-12 times 12 is
 // no more than out's rounding.
 //
 // A and b A + c A^2 are symmetric, and only their blocks on and below the diagonal are

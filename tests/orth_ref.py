@@ -5,9 +5,9 @@ Bounds.  The steps amplify what is rounded on the way by a factor that depends
 on the matrix's singular values, so there is none in closed form that is of use.
 The bound is four times the largest of what two evaluations of the same steps
 are off by, plus the rounding of out:
-  emulated   with the halves that X, A and b A + c A^2 are held in (of bfloat16: X
-             in one before the last two steps, or, by a CTA, in two), products and
-             sums otherwise in fp64
+  emulated   with the halves that X, A and b A + c A^2 are held in (of bfloat16 one,
+             X in two but before the last two steps; small matrices have two),
+             products and sums otherwise in fp64
   single     all in fp32 (for what sums in fp32 add; a kernel's are other sums
              of the same kind)
 and 2^-18 of the largest singular value beside them, for matrices so small that

@@ -49,6 +49,17 @@ def test_larger(pic, shape, dtype):
     ref.check(run(pic, [g])[0], g)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("steps", [0, 1, 2, 3, 4, 5])
+def test_steps_of_long_and_small_matrices(pic, dtype, steps):
+    """By tiles and by one CTA, and how many halves a product has goes by the step."""
+    cases = [normal(s, dtype, seed=3, scale=0.02) for s in ((64, 4096), (6000, 48), (128, 1100), (64, 64), (8, 500), (100, 90))]
+    for g in cases:
+        ref.check(run(pic, [g], steps=steps)[0], g, steps=steps, name=f"{tuple(g.shape)}")
+    for g, o in zip(cases, run(pic, cases, steps=steps)):
+        ref.check(o, g, steps=steps, name=f"{tuple(g.shape)} of several")
+
+
 @pytest.mark.parametrize("steps", [1, 5])
 @pytest.mark.parametrize("shape", [(4, 572), (4, 454), (2, 900), (639, 4), (779, 2), (4, 9000), (2000, 16000)], ids=str)
 def test_long_sums(pic, shape, steps):
