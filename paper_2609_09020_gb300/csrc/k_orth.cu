@@ -274,13 +274,15 @@ bool steps_ok(int steps, double a, double b, double c) {
 // Parts: stages with fewer tiles than there are CTAs (kSlots) are cut along K, with at
 // least kLeast slices (of all three products of halves) in a part, as a part more costs 3
 // us; and sums of more than kMost slices, in which a tensor core's truncations show (it
-// loses up to 2^-24 of a sum with each 16 of K; one half's own roundings are larger).  fp32
+// loses up to 2^-24 of a sum with each 16 of K; one half's own roundings are larger).  In
+// A of up to 64 rows, whose sums are long and all of one sign on the diagonal, parts of four
+// slices where there are CTAs for them (24 matrices of three types: 1.5 of elementary fp32's
+// error before, 1.2 so, in the same time).  fp32
 // 4000 x 12000, out's error and time: 64 slices 8.5e-5, 6.5 ms; 32 4.4e-5, 7.2 ms; 16
-// 2.3e-5, 11.1 ms.  With 128 columns 24 matrices of three types, sides up to 1500: 32 2.0e-6,
-// 170 us, 8 1.7e-6, 170 us, but four 700 x 700 alone 209 and 324 us; 16 leaves those at 209.
+// 2.3e-5, 11.1 ms.
 void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kShapes], bool (&both)[kShapes], long long& part_bytes,
                long long& counters) {
-  constexpr int kSms = 152, kSlots[kShapes] = {2 * kSms, kSms, kSms / 2}, kLeast = 16, kMost[2][kShapes] = {{256, 256, 256}, {32, 16, 32}};
+  constexpr int kSms = 152, kSlots[kShapes] = {2 * kSms, kSms, kSms / 2}, kLeast = 16, kMost[2] = {256, 32};
   constexpr long long kLarge = 120;
   const auto blocks = [](long long n, long long of) { return (n + of - 1) / of; };
   long long large = 0, middle = 0;
@@ -335,9 +337,11 @@ void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kSh
       const int cg = shape == 2 ? 2 : 1, panels = cg * (kShapeColumns[shape] / 64) * 4;
       int slot = 0;
       for (const Job& j : plain[shape]) {
-        const int slices = j.k1, most = kMost[j.halves - 1][shape];
+        const int slices = j.k1, most = kMost[j.halves - 1];
         const int passes = j.halves == 2 ? 3 : 1;
-        long long parts = std::max<long long>(std::min<long long>(fill, slices * passes / kLeast), blocks(slices, most));
+        const bool thin = s == kGram && j.halves == 2 && table[j.matrix].m <= 64;
+        const long long worth = thin ? blocks(slices, 4) : slices * passes / kLeast;
+        long long parts = std::max(std::min(fill, worth), blocks(slices, most));
         parts = std::max<long long>(parts, 1);
         const int each = static_cast<int>(blocks(slices, parts));
         parts = blocks(slices, each);
