@@ -54,13 +54,22 @@ typedef struct {
 
 typedef struct pic_orthogonalizer pic_orthogonalizer; /* opaque: the list, and room for X, A and b A + c A^2 */
 
+/* Bytes of device memory that a handle for these matrices holds between calls for X, A and
+ * b A + c A^2, of those that are not taken by one CTA each: 8 for every element, each row
+ * rounded up to 64 columns, and 4 (bfloat16 above 64 on the smaller side) or 8 for every
+ * element of a square matrix of the smaller side.  (Its lists of work and the parts of
+ * products take more beside that.)  At most 2^50 or a little above; -1 for a list that
+ * pic_orth_create refuses. */
+int64_t pic_orth_room_bytes(const pic_orth_matrix *matrices, int n);
+
 /*
  * Creates a handle for n (>= 0) matrices on the current device.  The list is
  * copied; the matrices stay the caller's, and the handle is to be destroyed
  * before they are freed.  Synchronises.
  * Errors: PIC_ERR_INVALID_ARG (NULL or misaligned pointers, sizes or strides
  * out of range, an unknown type, outputs that overlap), PIC_ERR_UNSUPPORTED (a
- * device that is not sm_103), PIC_ERR_ALLOC, PIC_ERR_CUDA.
+ * device that is not sm_103), PIC_ERR_ALLOC (the matrices' room does not fit
+ * the device, among others), PIC_ERR_CUDA.
  */
 int pic_orth_create(const pic_orth_matrix *matrices, int n, pic_orthogonalizer **out);
 

@@ -359,98 +359,143 @@ void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kSh
   }
 }
 
+// Places in one allocation, on 256-byte boundaries.  `bytes` stays at about kMost, which no
+// device has, where it would be more.
+struct Room {
+  static constexpr long long kMost = 1LL << 50;
+  long long bytes = 0;
+  long long take(long long count, long long size) {
+    const long long at = bytes;
+    if (size > 0 && count > (kMost - bytes) / size)
+      bytes = kMost;
+    else
+      bytes += (count * size + 255) / 256 * 256;
+    return at;
+  }
+};
+
+// The matrices of a list that are not empty, and where X (twice), A and b A + c A^2 of the
+// i-th are: at[4 i] and on, -1 for those that a CTA takes by itself (`small`).
+struct Layout {
+  std::vector<Matrix> table;
+  std::vector<long long> at;
+  std::vector<int> small[kSmallLists];
+  int small_most[kSmallLists] = {};
+  Room room;
+};
+// False for a list that is refused.
+bool lay_out(const pic_orth_matrix* matrices, int n, Layout& l) {
+  if (n < 0 || (n > 0 && !matrices)) return false;
+  std::vector<pic_orth_matrix> list;
+  for (int i = 0; i < n; ++i) {
+    const pic_orth_matrix& m = matrices[i];
+    constexpr long long most = 0x7fffffffLL - 256;
+    if (m.dtype != PIC_DTYPE_F32 && m.dtype != PIC_DTYPE_F16 && m.dtype != PIC_DTYPE_BF16) return false;
+    if (m.rows < 0 || m.cols < 0 || m.rows > most || m.cols > most) return false;
+    if (m.rows == 0 || m.cols == 0) continue;
+    const auto bad = [&](const void* p, long long ld) {
+      return !p || reinterpret_cast<uintptr_t>(p) % elem_bytes(m.dtype) || ld < m.cols || ld > (1LL << 40);
+    };
+    if (bad(m.grad, m.ld_grad) || bad(m.out, m.ld_out)) return false;
+    list.push_back(m);
+  }
+  if (!outputs_disjoint(list)) return false;
+  // by a CTA each: what is sooner done so than by tiles, or, beside others that go by
+  // tiles, where it takes a fraction of their time
+  const bool tiles = std::any_of(list.begin(), list.end(), [](const pic_orth_matrix& m) { return std::min(m.rows, m.cols) > 128; });
+  const double worth = tiles ? 30.0 : 100.0;
+  for (const pic_orth_matrix& m : list) {
+    const int id = static_cast<int>(l.table.size());
+    Matrix t{};
+    t.grad = m.grad, t.out = m.out, t.ld_grad = m.ld_grad, t.ld_out = m.ld_out;
+    t.rows = static_cast<int>(m.rows), t.cols = static_cast<int>(m.cols), t.dtype = m.dtype;
+    t.m = std::min(t.rows, t.cols), t.left = t.rows <= t.cols;
+    // (for a CTA by itself no difference: it takes products of both halves always, as 192
+    // bfloat16 matrices of 64 nets take 29 us so and 23 in one half, but 8 x 8 2.7e-3 of error)
+    t.halves = m.dtype == PIC_DTYPE_BF16 ? 1 : 2;
+    t.ldx = (m.cols + 63) / 64 * 64, t.lda = (t.m + 63LL) / 64 * 64;  // whole panels
+    const long long need = t.m <= 128 ? small_bytes(t.m, t.left ? t.cols : t.rows) : kSmallMost + 1LL;
+    if (need <= kSmallMost && small_time(t) <= worth) {
+      int which = 0;
+      while (need > kSmallBytes[which]) ++which;
+      l.small[which].push_back(id);
+      l.small_most[which] = std::max(l.small_most[which], static_cast<int>(need));
+      l.at.resize(l.at.size() + 4, -1);
+      l.table.push_back(t);
+      continue;
+    }
+    // bfloat16 in one half, out's error of five steps (its rounding alone 1.7e-3) and time:
+    // 64 x 1000 2.4e-3, 300 x 1500 2.3e-3, 1500 x 1500 1.9e-3; eight 64 x 4096 129 us, in two
+    // 167, eight 128 x 4096 140 and 191
+    if (t.m <= 64) t.halves = 2;
+    t.on16 = reinterpret_cast<uintptr_t>(m.grad) % 16 == 0 && m.ld_grad * elem_bytes(m.dtype) % 16 == 0;
+    // (both halves of X, of every type: rows are counted in 64 bits, as up to 2^31 of them are)
+    for (int i = 0; i < 2; ++i) l.at.push_back(l.room.take(2LL * t.rows, t.ldx * 2));
+    for (int i = 0; i < 2; ++i) l.at.push_back(l.room.take(static_cast<long long>(t.halves) * t.m, t.lda * 2));
+    l.table.push_back(t);
+  }
+  // long ones first, for CTAs of their own
+  for (std::vector<int>& ids : l.small)
+    std::stable_sort(ids.begin(), ids.end(), [&](int a, int b) { return small_time(l.table[a]) > small_time(l.table[b]); });
+  return true;
+}
+
 }  // namespace
 
 extern "C" {
 
+int64_t pic_orth_room_bytes(const pic_orth_matrix* matrices, int n) {
+  try {
+    Layout l;
+    return lay_out(matrices, n, l) ? l.room.bytes : -1;
+  } catch (...) {
+    return -1;
+  }
+}
+
 int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer** out) {
   if (!out) return PIC_ERR_INVALID_ARG;
   *out = nullptr;
-  if (n < 0 || (n > 0 && !matrices)) return PIC_ERR_INVALID_ARG;
   pic_orthogonalizer* h = nullptr;
   try {
-    std::vector<pic_orth_matrix> list;
-    for (int i = 0; i < n; ++i) {
-      const pic_orth_matrix& m = matrices[i];
-      constexpr long long most = 0x7fffffffLL - 256;
-      if (m.dtype != PIC_DTYPE_F32 && m.dtype != PIC_DTYPE_F16 && m.dtype != PIC_DTYPE_BF16) return PIC_ERR_INVALID_ARG;
-      if (m.rows < 0 || m.cols < 0 || m.rows > most || m.cols > most) return PIC_ERR_INVALID_ARG;
-      if (m.rows == 0 || m.cols == 0) continue;
-      const auto bad = [&](const void* p, long long ld) {
-        return !p || reinterpret_cast<uintptr_t>(p) % elem_bytes(m.dtype) || ld < m.cols || ld > (1LL << 40);
-      };
-      if (bad(m.grad, m.ld_grad) || bad(m.out, m.ld_out)) return PIC_ERR_INVALID_ARG;
-      list.push_back(m);
-    }
-    if (!outputs_disjoint(list)) return PIC_ERR_INVALID_ARG;
+    Layout l;
+    if (!lay_out(matrices, n, l)) return PIC_ERR_INVALID_ARG;
     const int rc = pic::lin::device_status();
     if (rc != PIC_OK) return rc;
-    std::vector<Matrix> table;
+    // (before the lists of work are made, which are long for matrices that do not fit)
+    size_t unused = 0, device_bytes = 0;
+    if (cudaMemGetInfo(&unused, &device_bytes) != cudaSuccess) {
+      cudaGetLastError();
+      return PIC_ERR_CUDA;
+    }
+    if (static_cast<size_t>(l.room.bytes) > device_bytes) return PIC_ERR_ALLOC;
+    std::vector<Matrix>& table = l.table;
+    const std::vector<long long>& at = l.at;
     std::vector<Piece> pieces;
-    std::vector<int> small[kSmallLists];
-    int small_most[kSmallLists] = {};
-    long long bytes = 0;
-    const auto take = [&](long long b) {
-      const long long at = bytes;
-      bytes += (b + 255) / 256 * 256;
-      return at;
-    };
-    std::vector<long long> at;
-    // by a CTA each: what is sooner done so than by tiles, or, beside others that go by
-    // tiles, where it takes a fraction of their time
-    const bool tiles = std::any_of(list.begin(), list.end(), [](const pic_orth_matrix& m) { return std::min(m.rows, m.cols) > 128; });
-    const double worth = tiles ? 30.0 : 100.0;
-    for (const pic_orth_matrix& m : list) {
-      const int id = static_cast<int>(table.size());
-      Matrix t{};
-      t.grad = m.grad, t.out = m.out, t.ld_grad = m.ld_grad, t.ld_out = m.ld_out;
-      t.rows = static_cast<int>(m.rows), t.cols = static_cast<int>(m.cols), t.dtype = m.dtype;
-      t.m = std::min(t.rows, t.cols), t.left = t.rows <= t.cols;
-      // (for a CTA by itself no difference: it takes products of both halves always, as 192
-      // bfloat16 matrices of 64 nets take 29 us so and 23 in one half, but 8 x 8 2.7e-3 of error)
-      t.halves = m.dtype == PIC_DTYPE_BF16 ? 1 : 2;
-      t.ldx = (m.cols + 63) / 64 * 64, t.lda = (t.m + 63) / 64 * 64;  // whole panels
-      const long long need = t.m <= 128 ? small_bytes(t.m, t.left ? t.cols : t.rows) : kSmallMost + 1LL;
-      if (need <= kSmallMost && small_time(t) <= worth) {
-        int which = 0;
-        while (need > kSmallBytes[which]) ++which;
-        small[which].push_back(id);
-        small_most[which] = std::max(small_most[which], static_cast<int>(need));
-        at.resize(at.size() + 4);
-        table.push_back(t);
-        continue;
-      }
-      // bfloat16 in one half, out's error of five steps (its rounding alone 1.7e-3) and time:
-      // 64 x 1000 2.4e-3, 300 x 1500 2.3e-3, 1500 x 1500 1.9e-3; eight 64 x 4096 129 us, in two
-      // 167, eight 128 x 4096 140 and 191
-      if (t.m <= 64) t.halves = 2;
+    for (size_t id = 0; id < table.size(); ++id) {
+      Matrix& t = table[id];
+      if (at[4 * id] < 0) continue;
       t.part0 = static_cast<int>(pieces.size());
       for (long long r = 0; r < t.rows; r += 32)
-        for (long long c = 0; c < t.cols; c += kPieceCols) pieces.push_back({id, static_cast<int>(r), static_cast<int>(c)});
+        for (long long c = 0; c < t.cols; c += kPieceCols) pieces.push_back({static_cast<int>(id), static_cast<int>(r), static_cast<int>(c)});
       t.parts = static_cast<int>(pieces.size()) - t.part0;
-      t.on16 = reinterpret_cast<uintptr_t>(m.grad) % 16 == 0 && m.ld_grad * elem_bytes(m.dtype) % 16 == 0;
-      for (int i = 0; i < 2; ++i) at.push_back(take(2 * t.rows * t.ldx * 2));
-      for (int i = 0; i < 2; ++i) at.push_back(take(t.halves * t.m * t.lda * 2));
-      table.push_back(t);
     }
-    // long ones first, for CTAs of their own
-    for (std::vector<int>& ids : small)
-      std::stable_sort(ids.begin(), ids.end(), [&](int a, int b) { return small_time(table[a]) > small_time(table[b]); });
     std::vector<Job> jobs[3][kShapes];
     long long part_bytes = 0, counters = 0;
     bool both[kShapes] = {};
     make_jobs(table, jobs, both, part_bytes, counters);
-    const long long at_rest = take(table.size() * sizeof(float));
-    const long long at_matrices = take(table.size() * sizeof(Matrix)), at_maps = take(table.size() * kMaps * sizeof(CUtensorMap)),
-                    at_pieces = take(pieces.size() * sizeof(Piece)), at_squares = take(pieces.size() * sizeof(double)),
-                    at_parts = take(part_bytes), at_counters = take(counters * 4), at_status = take(4);
+    const auto take = [&](long long count, size_t size) { return l.room.take(count, static_cast<long long>(size)); };
+    const long long at_rest = take(table.size(), sizeof(float));
+    const long long at_matrices = take(table.size(), sizeof(Matrix)), at_maps = take(table.size(), kMaps * sizeof(CUtensorMap)),
+                    at_pieces = take(pieces.size(), sizeof(Piece)), at_squares = take(pieces.size(), sizeof(double)),
+                    at_parts = take(part_bytes, 1), at_counters = take(counters, 4), at_status = take(1, 4);
     long long at_jobs[3][kShapes];
     for (int s = 0; s < 3; ++s)
-      for (int c = 0; c < kShapes; ++c) at_jobs[s][c] = take(jobs[s][c].size() * sizeof(Job));
+      for (int c = 0; c < kShapes; ++c) at_jobs[s][c] = take(jobs[s][c].size(), sizeof(Job));
     long long at_small[kSmallLists];
-    for (int i = 0; i < kSmallLists; ++i) at_small[i] = take(small[i].size() * sizeof(int));
+    for (int i = 0; i < kSmallLists; ++i) at_small[i] = take(l.small[i].size(), sizeof(int));
     h = new pic_orthogonalizer{};
-    if (cudaGetDevice(&h->device) != cudaSuccess || cudaMalloc(&h->room, bytes) != cudaSuccess) {
+    if (cudaGetDevice(&h->device) != cudaSuccess || cudaMalloc(&h->room, l.room.bytes) != cudaSuccess) {
       cudaGetLastError();
       pic_orth_destroy(h);
       return PIC_ERR_ALLOC;
@@ -486,9 +531,9 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
     ok = ok && put(h->matrices, table) && put(h->maps, maps) && put(h->pieces, pieces);
     for (int i = 0; i < kSmallLists; ++i) {
       h->small[i] = reinterpret_cast<int*>(h->room + at_small[i]);
-      h->n_small[i] = static_cast<int>(small[i].size());
-      h->small_bytes[i] = small_most[i];
-      ok = ok && put(h->small[i], small[i]);
+      h->n_small[i] = static_cast<int>(l.small[i].size());
+      h->small_bytes[i] = l.small_most[i];
+      ok = ok && put(h->small[i], l.small[i]);
     }
     for (int s = 0; s < 3; ++s)
       for (int c = 0; c < kShapes; ++c) {

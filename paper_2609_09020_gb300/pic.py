@@ -194,6 +194,8 @@ def load_library():
     lib.pic_grouped_linear_check.restype = i
     lib.pic_orth_create.argtypes = [ctypes.POINTER(pic_orth_matrix), i, ctypes.POINTER(_P)]
     lib.pic_orth_create.restype = i
+    lib.pic_orth_room_bytes.argtypes = [ctypes.POINTER(pic_orth_matrix), i]
+    lib.pic_orth_room_bytes.restype = ctypes.c_int64
     lib.pic_orth.argtypes = [_P, i] + [ctypes.c_float] * 4 + [_P]
     lib.pic_orth.restype = i
     lib.pic_orth_check.argtypes = [_P, _P]
