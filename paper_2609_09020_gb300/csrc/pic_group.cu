@@ -14,12 +14,14 @@ bool aligned(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p)
 size_t elem_bytes(int dtype) { return dtype == PIC_DTYPE_F32 ? 4 : 2; }
 
 // A [rows][cols] matrix of the call, or [groups] of them, each `group` elements behind the one before.
+// (No address space has one whose last row is 2^60 elements from its first; up to there nothing wraps.)
 bool matrix_ok(const void* p, long long ld, long long rows, long long cols, int dtype) {
-  return (p || rows == 0) && aligned(p, elem_bytes(dtype)) && ld >= cols && ld <= (1LL << 40);
+  return (p || rows == 0) && aligned(p, elem_bytes(dtype)) && ld >= cols && ld <= (1LL << 40) &&
+         (rows <= 1 || ld <= (1LL << 60) / rows);
 }
 bool matrices_ok(const void* p, long long ld, long long group, int groups, long long rows, long long cols, int dtype) {
   if (!matrix_ok(p, ld, rows, cols, dtype)) return false;
-  return groups == 1 || (group <= (1LL << 44) && (rows == 1 || ld <= group) && group >= (rows - 1) * ld + cols);
+  return groups == 1 || (group <= (1LL << 44) && group >= (rows - 1) * ld + cols);
 }
 bool vectors_ok(const void* p, long long group, int groups, long long n, int dtype) {
   return aligned(p, elem_bytes(dtype)) && (groups == 1 || (group >= n && group <= (1LL << 44)));
