@@ -394,7 +394,8 @@ bool lay_out(const pic_orth_matrix* matrices, int n, Layout& l) {
     if (m.rows < 0 || m.cols < 0 || m.rows > most || m.cols > most) return false;
     if (m.rows == 0 || m.cols == 0) continue;
     const auto bad = [&](const void* p, long long ld) {
-      return !p || reinterpret_cast<uintptr_t>(p) % elem_bytes(m.dtype) || ld < m.cols || ld > (1LL << 40);
+      return !p || reinterpret_cast<uintptr_t>(p) % elem_bytes(m.dtype) || ld < m.cols || ld > (1LL << 40) ||
+             ld > INT64_MAX / elem_bytes(m.dtype) / m.rows;  // (so that no end wraps)
     };
     if (bad(m.grad, m.ld_grad) || bad(m.out, m.ld_out)) return false;
     list.push_back(m);

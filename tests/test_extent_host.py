@@ -45,3 +45,15 @@ def test_weight_gradients(pic, rows, ld):
     a.dtype, a.act, a.offsets = pic.PIC_DTYPE_F32, pic.PIC_ACT_NONE, P
     a.dy, a.lddy, a.x, a.ldx, a.dw, a.lddw, a.dw_group = P, rows, P, 16, P, ld, 2 ** 44
     assert pic.load_library().pic_grouped_linear_backward_workspace_bytes(ctypes.byref(a)) == -1
+
+
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+@pytest.mark.parametrize("rows,ld", FAR, ids=str)
+def test_updates(pic, rows, ld, dtype):
+    """Their ends would wrap to before their beginnings, and what they overlap would pass."""
+    inside = P + 64
+    make = lambda *m: (pic.pic_orth_matrix * len(m))(*m)
+    room = pic.load_library().pic_orth_room_bytes
+    far = pic.pic_orth_matrix(P, P, rows, 16, ld, ld, dtype)
+    assert room(make(far), 1) == -1
+    assert room(make(pic.pic_orth_matrix(inside, inside, 4, 4, 4, 4, dtype), far), 2) == -1
