@@ -84,13 +84,18 @@ __device__ __forceinline__ void for_form(const Matrix& m, F f) {
 }
 
 // The squares of a piece: a thread adds at most 64 in fp32, and where that sum leaves the
-// range in which fp32 is good, again in fp64; the block's threads in order.
-__global__ void __launch_bounds__(kThreads) squares_kernel(const Matrix* matrices, const Piece* pieces, double* squares) {
+// range in which fp32 is good, again in fp64; the block's threads in order.  Being the
+// first kernel of a call by tiles, it also sets the parts' counters to zero: a call whose
+// waits gave up leaves them where its last parts came.
+__global__ void __launch_bounds__(kThreads) squares_kernel(const Matrix* matrices, const Piece* pieces, double* squares,
+                                                           unsigned* counters, long long n_counters) {
   __shared__ double sums[kThreads / 32];
   const Piece p = pieces[blockIdx.x];
   const Matrix& m = matrices[p.matrix];
   const int row = p.row0 + threadIdx.x / 8, col = p.col0 + threadIdx.x % 8 * 8, end = p.col0 + min(m.cols - p.col0, kPieceCols);
   wait_for_earlier();
+  for (long long i = blockIdx.x * static_cast<long long>(kThreads) + threadIdx.x; i < n_counters; i += static_cast<long long>(gridDim.x) * kThreads)
+    counters[i] = 0;
   double sum = 0.0;
   for_form(m, [&](auto, auto load) {
     float s = 0.0f;
@@ -543,8 +548,7 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
         h->both[c] = both[c];
         ok = ok && put(h->jobs[s][c], jobs[s][c]);
       }
-    if (!ok || (counters && cudaMemset(h->counters, 0, counters * 4) != cudaSuccess) ||
-        cudaMemset(h->status, 0, 4) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
+    if (!ok || cudaMemset(h->status, 0, 4) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
       cudaGetLastError();
       pic_orth_destroy(h);
       return PIC_ERR_CUDA;
@@ -581,7 +585,7 @@ int pic_orth(pic_orthogonalizer* h, int steps, float a, float b, float c, float 
   waits.status = h->status;
   const Matrix* matrices = h->matrices;
   const Piece* pieces = h->pieces;
-  int rc = s.launch(squares_kernel, dim3(h->n_pieces), kThreads, 0, matrices, pieces, h->squares);
+  int rc = s.launch(squares_kernel, dim3(h->n_pieces), kThreads, 0, matrices, pieces, h->squares, h->counters, h->n_counters);
   if (rc == PIC_OK)
     rc = s.launch(scale_kernel, dim3(h->n_pieces), kThreads, 0, matrices, pieces, static_cast<const double*>(h->squares), eps,
                   static_cast<int>(steps == 0));
@@ -608,10 +612,7 @@ int pic_orth_check(pic_orthogonalizer* h, void* stream) {
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (cudaMemcpyAsync(&flag, h->status, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess ||
       cudaStreamSynchronize(s) != cudaSuccess ||
-      // parts that never came have left their counters where they were
-      (flag && (cudaMemsetAsync(h->status, 0, sizeof(int), s) != cudaSuccess ||
-                (h->n_counters && cudaMemsetAsync(h->counters, 0, h->n_counters * 4, s) != cudaSuccess) ||
-                cudaStreamSynchronize(s) != cudaSuccess))) {
+      (flag && (cudaMemsetAsync(h->status, 0, sizeof(int), s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess))) {
     cudaGetLastError();
     return PIC_ERR_CUDA;
   }
