@@ -195,32 +195,43 @@ long long elem_bytes(int dtype) { return dtype == PIC_DTYPE_F32 ? 4 : 2; }
 
 // What a matrix of the call covers.
 struct Span {
-  uintptr_t first, end, ld, width;
-  int matrix;
+  uintptr_t first, end, ld, width, rows;
   bool out;
 };
 
-// Whether two matrices have an element in common, taking rows for whole spans where
-// they are not the same distance apart.
+// Whether two matrices have a byte in common.
 bool meet(const Span& a, const Span& b) {
   if (a.first >= b.end || b.first >= a.end) return false;
-  if (a.ld != b.ld) return true;
-  // b's first column, counted along a's rows
-  const uintptr_t at = b.first >= a.first ? (b.first - a.first) % a.ld : (a.ld - (a.first - b.first) % a.ld) % a.ld;
-  return !(at >= a.width && at + b.width <= a.ld);
+  if (a.ld == b.ld) {
+    // b's first column, counted along a's rows
+    const uintptr_t at = b.first >= a.first ? (b.first - a.first) % a.ld : (a.ld - (a.first - b.first) % a.ld) % a.ld;
+    return !(at >= a.width && at + b.width <= a.ld);
+  }
+  // rows of different distances (a single row has any): each of the one that has fewer
+  // against the last of the other's to begin before it, and the next
+  const bool swap = b.rows < a.rows;
+  const Span &few = swap ? b : a, &many = swap ? a : b;
+  for (uintptr_t r = 0; r < few.rows; ++r) {
+    const uintptr_t from = few.first + r * few.ld, to = from + few.width;
+    if (to <= many.first || from >= many.end) continue;
+    if (from < many.first) return true;
+    const uintptr_t row = (from - many.first) / many.ld;
+    if (from < many.first + row * many.ld + many.width) return true;
+    if (row + 1 < many.rows && to > many.first + (row + 1) * many.ld) return true;
+  }
+  return false;
 }
 
 bool outputs_disjoint(const std::vector<pic_orth_matrix>& list) {
   std::vector<Span> spans;
-  for (size_t i = 0; i < list.size(); ++i) {
-    const pic_orth_matrix& m = list[i];
+  for (const pic_orth_matrix& m : list) {
     const uintptr_t e = elem_bytes(m.dtype);
     const auto add = [&](const void* p, long long ld, bool out) {
       const uintptr_t first = reinterpret_cast<uintptr_t>(p);
-      spans.push_back({first, first + ((m.rows - 1) * ld + m.cols) * e, ld * e, m.cols * e, static_cast<int>(i), out});
+      spans.push_back({first, first + ((m.rows - 1) * ld + m.cols) * e, ld * e, m.cols * e, static_cast<uintptr_t>(m.rows), out});
     };
     add(m.out, m.ld_out, true);
-    if (m.grad != m.out || m.ld_grad != m.ld_out) add(m.grad, m.ld_grad, false);
+    if (m.grad != m.out || (m.rows > 1 && m.ld_grad != m.ld_out)) add(m.grad, m.ld_grad, false);
   }
   std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.first < b.first; });
   std::vector<Span> open;
