@@ -581,11 +581,22 @@ def _linear_act(act) -> int:
 
 
 def _refuse_recorded(backward="linear_backward", **tensors):
-    """Gradients that autograd would lose without a word."""
+    """Derivatives that autograd would lose without a word.  backward: what makes them; None
+    of a call that makes gradients or updates itself, which takes parameters (leaves of the
+    graph) as they are."""
+    import torch
+    reverse, forward = torch.is_grad_enabled(), torch.autograd.forward_ad._current_level >= 0
     for name, t in tensors.items():
-        if t is not None and t.requires_grad:
+        if t is None:
+            continue
+        if reverse and t.requires_grad and backward:
             raise ValueError(f"{name}: requires a gradient, and autograd does not record this call: detach it, or "
                              f"call under torch.no_grad(), and take the gradients from {backward}")
+        if reverse and t.grad_fn is not None:
+            raise ValueError(f"{name}: is part of a graph, and autograd does not record this call: detach it, or "
+                             "call under torch.no_grad()")
+        if forward and torch.autograd.forward_ad.unpack_dual(t).tangent is not None:
+            raise ValueError(f"{name}: has a tangent, and autograd does not carry it through this call: detach it")
 
 
 def linear(x, weight, bias=None, act="none", residual=None, out=None, save_pre=False, stream=None):
@@ -598,15 +609,16 @@ def linear(x, weight, bias=None, act="none", residual=None, out=None, save_pre=F
     apart than their width.  Enqueued on the stream, not synchronised.
 
     torch's autograd does not record the call, and tensors that require
-    gradients are refused while it records: detach them, or call under
-    ``torch.no_grad()``, and take the gradients from ``linear_backward``."""
+    gradients are refused while it records (tensors with tangents, always):
+    detach them, or call under ``torch.no_grad()``, and take the gradients from
+    ``linear_backward``."""
     if stream is not None:
         with _Allocating(stream):
             return linear(x, weight, bias, act, residual, out, save_pre)
     import torch
     if ((x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad
          or residual is not None and residual.requires_grad or out is not None and out.requires_grad)
-            and torch.is_grad_enabled()):
+            and torch.is_grad_enabled() or torch.autograd.forward_ad._current_level >= 0):
         _refuse_recorded(x=x, weight=weight, bias=bias, residual=residual, out=out)
     _on_device(x, "x")
     if weight.dim() != 2:
@@ -778,14 +790,16 @@ def grouped_linear(x, weight, offsets, bias=None, act="none", out=None, save_pre
     kernels run; ``grouped_linear_check`` reports ones that were not as they
     must be.  Enqueued on the stream, not synchronised.
 
-    torch's autograd does not record the call; gradients come from
-    ``grouped_linear_backward``."""
+    torch's autograd does not record the call, and tensors that require
+    gradients, or have tangents, are refused as by ``linear``; gradients come
+    from ``grouped_linear_backward``."""
     if stream is not None:
         with _Allocating(stream):
             return grouped_linear(x, weight, offsets, bias, act, out, save_pre)
     import torch
     if ((x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad
-         or out is not None and out.requires_grad) and torch.is_grad_enabled()):
+         or out is not None and out.requires_grad)
+            and torch.is_grad_enabled() or torch.autograd.forward_ad._current_level >= 0):
         _refuse_recorded("grouped_linear_backward", x=x, weight=weight, bias=bias, out=out)
     _on_device(x, "x")
     G, N, K, po = _grouped(weight, offsets, x)
@@ -814,11 +828,20 @@ def grouped_linear_backward(dy, x, weight, offsets, act="none", pre=None, need=(
     ``grouped_linear`` returned with save_pre (not read with act "none"; with
     "relu" y itself will do).  Groups without rows have gradients of zero; rows
     of dx that belong to no group are not written.  The gradients are new
-    tensors, or are written to those given.  Enqueued on the stream."""
+    tensors, or are written to those given.  Enqueued on the stream.
+
+    Nor does autograd record this call: there are no second derivatives, and
+    tensors that it has recorded, or that have tangents, are refused (parameters
+    are not: their gradients are what this makes)."""
     if stream is not None:
         with _Allocating(stream):
             return grouped_linear_backward(dy, x, weight, offsets, act, pre, need, dx, dweight, dbias)
     import torch
+    if ((dy.requires_grad or x.requires_grad or weight.requires_grad or pre is not None and pre.requires_grad
+         or dx is not None and dx.requires_grad or dweight is not None and dweight.requires_grad
+         or dbias is not None and dbias.requires_grad)
+            and torch.is_grad_enabled() or torch.autograd.forward_ad._current_level >= 0):
+        _refuse_recorded(None, dy=dy, x=x, weight=weight, pre=pre, dx=dx, dweight=dweight, dbias=dbias)
     _on_device(dy, "dy")
     need = tuple(need)
     if not need or not _GRADIENTS.issuperset(need):
@@ -943,7 +966,10 @@ class Orthogonalizer:
     products make of it, its singular vectors with singular values of about
     one.  A tensor is [rows, cols], or [n, rows, cols] for n matrices, float32,
     float16 or bfloat16, with contiguous rows, on the current device.  The
-    handle keeps the tensors, and has room for what is held between products."""
+    handle keeps the tensors, and has room for what is held between products
+    (8 bytes an element, of matrices that are not small).  Autograd records
+    nothing of it: tensors that are part of a graph, or have tangents, are
+    refused."""
 
     def __init__(self, tensors, out=None):
         import torch
@@ -954,6 +980,7 @@ class Orthogonalizer:
             raise ValueError(f"out: {len(outs)} tensors, expected {len(tensors)}")
         entries = []
         for i, (t, o) in enumerate(zip(tensors, outs)):
+            _refuse_recorded(None, **{f"tensors[{i}]": t, f"out[{i}]": o})
             for name, v in ((f"tensors[{i}]", t), (f"out[{i}]", o)):
                 _on_device(v, name)
                 if v.dim() not in (2, 3):

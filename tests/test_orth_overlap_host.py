@@ -43,7 +43,7 @@ LEFT, RIGHT = (0, 6, 7, 20), (7, 6, 5, 20)
     ((0, 2, 8, 60), False),
     ((12, 2, 10, 60), True),          # the rest of a row and two of the next
     ((1, 3, 6, 19), True),            # rows 1 to 6, 20 to 25, 39 to 44
-    ((3, 4, 4, 21), False),           # 3, 24, 45, 66 and on: the third is over the right columns
+    ((3, 4, 4, 21), False),           # 3, 24, 45, 66: the second is over one of the right columns
 ], ids=str)
 def test_beside_columns(pic, other, ok):
     assert accepted(pic, RIGHT, other) == ok
