@@ -95,16 +95,15 @@ __device__ __forceinline__ void make_table(GroupTable& t, const long long* offse
   __syncthreads();
 }
 
-// Products of any types, strides and sizes.  ROWS: y[i][j] = sum_k a(i, k) b_g(j, k)
+// Products of any types, strides and sizes.  By rows: y[i][j] = sum_k a(i, k) b_g(j, k)
 // for the rows i of group g, a(i, k) at a[i * a_i + k], b_g(j, k) at b[g * b_group + j
 // * b_j + k * b_k], with the layer's epilogue.  Else y_g[i][j] = sum over the group's
-// rows k of a(k, i) b(k, j), a at a[k * a_i + i], b at b[k * b_k + j].  Where there is
-// an a_pre, a is multiplied by act'(a_pre).
+// rows k of a(k, i) b(k, j), a at a[k * a_i + i], b at b[k * b_k + j].
 struct GroupProduct {
   bool by_rows;
   const void* a;
   long long a_i;
-  const void* a_pre;
+  const void* a_pre;  // of few rows' gradients: a is multiplied by act'(a_pre); or null
   long long a_pre_i;
   int a_act;
   const void* b;
@@ -123,15 +122,16 @@ struct GroupProduct {
   int act;
   int* status;
 };
+// (16-bit types by rows only: tc_product takes all their sums.)
 int any_product(const GroupProduct& p, int dtype, Chain& s);
 
-// Few rows in a group, eight at a time: any types, strides and sizes.  The gradients take a
-// and a_pre as any_product does; few_dw makes db too (y or db null: not that one).
+// Few rows in a group, eight at a time: any types, strides and sizes.  few_dw makes db too (y
+// or db null: not that one).
 int few_forward(const GroupProduct& p, int dtype, Chain& s);
 int few_dx(const GroupProduct& p, int dtype, Chain& s);
 int few_dw(const GroupProduct& p, void* db, long long db_group, int dtype, Chain& s);
 
-// On the tensor cores: 16-bit types, a as it is (no a_pre).
+// On the tensor cores: 16-bit types.
 constexpr long long kTcMostK = 16384;  // of K that one accumulator sums up
 bool tc_takes(const GroupProduct& p, int dtype);
 long long tc_workspace(const GroupProduct& p, int dtype);

@@ -1,5 +1,5 @@
-// k_group_any.cu -- grouped products of any type, stride and size on the FP32
-// cores: tiles of 64 x 64, 16 of K at a time through shared memory, sixteen sums a
+// k_group_any.cu -- grouped products of any stride and size on the FP32 cores (products
+// of rows of every type, sums over rows of fp32): tiles of 64 x 64, 16 of K at a time through shared memory, sixteen sums a
 // thread.  CTAs are persistent, with the table of groups in shared memory, and take
 // tiles one after another.  Measured: 16 of K of such a tile take from 1.3 us to 4 with four
 // CTAs on each SM; fp32 400 x 300 -> 300 in four groups 23 us.
@@ -9,7 +9,6 @@ namespace pic {
 namespace grp {
 namespace {
 
-using lin::act_grad;
 using lin::act_value;
 using lin::from_f32;
 using lin::to_f32;
@@ -27,7 +26,7 @@ __global__ void __launch_bounds__(kThreads) any_kernel(const GroupProduct p) {
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const long long tiles_j = (p.J + kTile - 1) / kTile, tiles_i = (p.I + kTile - 1) / kTile;
   const long long work = ROWS ? table.tiles[p.groups] * tiles_j : p.groups * tiles_i * tiles_j;
-  const T *a = static_cast<const T*>(p.a), *b = static_cast<const T*>(p.b), *z = static_cast<const T*>(p.a_pre);
+  const T *a = static_cast<const T*>(p.a), *b = static_cast<const T*>(p.b);
   for (long long w = blockIdx.x; w < work; w += gridDim.x) {
     const long long tj = w % tiles_j, t = w / tiles_j;
     const int g = ROWS ? table.find(static_cast<int>(t), p.groups) : static_cast<int>(t / tiles_i);
@@ -39,17 +38,16 @@ __global__ void __launch_bounds__(kThreads) any_kernel(const GroupProduct p) {
     // a thread's elements of the next 16 of K, on their way while these are multiplied
     constexpr int kEach = kTile * kDeep / kThreads;
     const bool along = ROWS && p.b_k == 1;  // neighbouring threads along what is contiguous
-    T na[kEach], nz[kEach], nb[kEach];
+    T na[kEach], nb[kEach];
     const auto fetch = [&](long long k0) {
 #pragma unroll
       for (int u = 0; u < kEach; ++u) {
         const int e = threadIdx.x + u * kThreads;
         const int ka = ROWS ? e % kDeep : e / kTile, ia = ROWS ? e / kDeep : e % kTile;
-        na[u] = nz[u] = nb[u] = from_f32<T>(0.0f);
+        na[u] = nb[u] = from_f32<T>(0.0f);
         if (i0 + ia < I && k0 + ka < K) {
           const long long row = first + (ROWS ? i0 + ia : k0 + ka), col = ROWS ? k0 + ka : i0 + ia;
           na[u] = a[row * p.a_i + col];
-          if (z) nz[u] = z[row * p.a_pre_i + col];
         }
         const int kb = along ? e % kDeep : e / kTile, jb = along ? e / kDeep : e % kTile;
         if (j0 + jb < p.J && k0 + kb < K) nb[u] = bg[(j0 + jb) * p.b_j + (k0 + kb) * p.b_k];
@@ -62,8 +60,7 @@ __global__ void __launch_bounds__(kThreads) any_kernel(const GroupProduct p) {
         const int e = threadIdx.x + u * kThreads;
         const int ka = ROWS ? e % kDeep : e / kTile, ia = ROWS ? e / kDeep : e % kTile;
         const int kb = along ? e % kDeep : e / kTile, jb = along ? e / kDeep : e % kTile;
-        const float v = to_f32(na[u]);
-        sa[ka][ia] = z ? act_grad<EXACT>(v, to_f32(nz[u]), p.a_act) : v;
+        sa[ka][ia] = to_f32(na[u]);
         sb[kb][jb] = to_f32(nb[u]);
       }
       __syncthreads();
@@ -98,20 +95,21 @@ __global__ void __launch_bounds__(kThreads) any_kernel(const GroupProduct p) {
   }
 }
 
-template <typename T>
+template <typename T, bool ROWS>
 int run(const GroupProduct& p, Chain& s) {
   const long long tiles_j = (p.J + kTile - 1) / kTile, tiles_i = (p.I + kTile - 1) / kTile;
-  const long long most = p.by_rows ? ((p.rows + kTile - 1) / kTile + p.groups) * tiles_j : p.groups * tiles_i * tiles_j;
+  const long long most = ROWS ? ((p.rows + kTile - 1) / kTile + p.groups) * tiles_j : p.groups * tiles_i * tiles_j;
   const unsigned grid = static_cast<unsigned>(most < 4 * kSms ? most : 4 * kSms);
-  return s.launch(p.by_rows ? any_kernel<T, true> : any_kernel<T, false>, dim3(grid), kThreads, 0, p);
+  return s.launch(any_kernel<T, ROWS>, dim3(grid), kThreads, 0, p);
 }
 
 }  // namespace
 
 int any_product(const GroupProduct& p, int dtype, Chain& s) {
-  if (dtype == PIC_DTYPE_F32) return run<float>(p, s);
-  if (dtype == PIC_DTYPE_F16) return run<__half>(p, s);
-  return run<__nv_bfloat16>(p, s);
+  if (dtype == PIC_DTYPE_F32) return p.by_rows ? run<float, true>(p, s) : run<float, false>(p, s);
+  // (sums of 16-bit types are the tensor cores', whatever their size)
+  if (!p.by_rows) return PIC_ERR_INVALID_ARG;
+  return dtype == PIC_DTYPE_F16 ? run<__half, true>(p, s) : run<__nv_bfloat16, true>(p, s);
 }
 
 }  // namespace grp

@@ -549,7 +549,7 @@ Plan plan(const GroupProduct& p) {
 // (k_group_any.cu's kernel, measured: 16 of K take from 1.3 us with few tiles of 64 x 64 to 4
 // with four on each SM)
 bool planes_takes(const GroupProduct& p, int dtype) {
-  if (dtype != PIC_DTYPE_F32 || p.a_pre || p.rows == 0) return false;
+  if (dtype != PIC_DTYPE_F32 || p.rows == 0) return false;
   // rows of the planes are counted in 32 bits
   const long long w_rows = p.by_rows ? p.groups * round_up(p.b_k == 1 ? p.J : p.K, kAlign) : 0;
   if (w_rows > 0x7fffffffLL - kPlRows || p.rows + static_cast<long long>(p.groups) * kAlign > 0x7fffffffLL - kPlRows) return false;

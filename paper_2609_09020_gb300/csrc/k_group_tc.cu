@@ -224,7 +224,7 @@ int join_parts(const JoinParams& q, int rows, int dtype, Chain& s) {
 }
 
 bool tc_takes(const GroupProduct& p, int dtype) {
-  if (dtype == PIC_DTYPE_F32 || p.a_pre) return false;
+  if (dtype == PIC_DTYPE_F32) return false;
   return p.by_rows ? p.K <= kTcMostK : p.rows > 0;
 }
 

@@ -376,13 +376,10 @@ bool encode_many(CUtensorMap* map, const void* m, long long rows, long long cols
                  long long group, int box_rows, int dtype) {
   const PFN_cuTensorMapEncodeTiled_v12000 enc = encoder();
   if (!enc) return false;
-  const unsigned e = dtype == PIC_DTYPE_F32 ? 4 : 2;
-  const CUtensorMapDataType type = dtype == PIC_DTYPE_F32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
-                                   : dtype == PIC_DTYPE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
-                                                            : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  const CUtensorMapDataType type = dtype == PIC_DTYPE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   const cuuint64_t dim[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(count)};
-  const cuuint64_t stride[2] = {static_cast<cuuint64_t>(ld * e), static_cast<cuuint64_t>(group * e)};
-  const cuuint32_t box[3] = {128u / e, static_cast<cuuint32_t>(box_rows), 1};
+  const cuuint64_t stride[2] = {static_cast<cuuint64_t>(ld * 2), static_cast<cuuint64_t>(group * 2)};
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_rows), 1};
   const cuuint32_t elem[3] = {1, 1, 1};
   return enc(map, type, 3, const_cast<void*>(m), dim, stride, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;

@@ -818,8 +818,8 @@ __global__ void __launch_bounds__(TcShape<CG, BN>::kThreads, BN == 64 ? 2 : 1)
 // A [rows][cols] matrix in boxes of 128 bytes of columns and box_rows rows,
 // 128-byte swizzled; false if the driver will not make the map.
 bool encode(CUtensorMap* map, const void* m, long long rows, long long cols, long long ld, int box_rows, int dtype);
-// `count` [rows][cols] matrices, `group` elements apart, in boxes of 128 bytes of columns
-// and box_rows rows of one of them.
+// `count` [rows][cols] matrices of a 16-bit type, `group` elements apart, in boxes of 64
+// columns and box_rows rows of one of them.
 bool encode_many(CUtensorMap* map, const void* m, long long rows, long long cols, long long ld, long long count,
                  long long group, int box_rows, int dtype);
 // The three planes of a matrix, in boxes of box_cols columns (64, 128-byte swizzled,

@@ -717,7 +717,7 @@ def linear_check(stream=None):
         raise PicError(rc, "pic_linear_check")
 
 
-def _matrices(t, name, shape, like, distinct=False):
+def _matrices(t, name, shape, like):
     """(pointer, row stride, group stride) of t as [groups][rows][cols] matrices of ``like``'s type and device."""
     if t.dtype is not like.dtype or t.get_device() != like.get_device():
         raise ValueError(f"{name}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
@@ -753,7 +753,6 @@ def _int64():
         import torch
         _int64_type = torch.int64
     return _int64_type
-
 
 
 def _grouped(weight, offsets, like):
