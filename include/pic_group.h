@@ -14,8 +14,15 @@
  * may be rounded to it before the products or not; db sums it unrounded).  Rows of one group
  * never meet those of another: a NaN stays in its group.  A group without rows
  * has gradients of zero.  Rows before offsets[0] and from offsets[groups] on
- * belong to no group: nothing of them is read, and y, pre and dx are not
- * written there.
+ * belong to no group: y, pre and dx are not written there, and what x, dy and
+ * pre hold there reaches no result.  All `rows` rows of them are to be readable
+ * all the same: tiles, and the pieces of memory that they are copied in, may
+ * begin before a group's first row and end behind its last.
+ *
+ * Sums of more than 16384 products of 16-bit values (in_features in the forward,
+ * out_features in dx) go by FP32 FMAs, as one accumulator of the tensor cores
+ * takes no more: bf16, 8 groups of 2048 rows together to 1024 outputs take 96 us
+ * with 16384 inputs and 3260 with 16392.
  *
  * offsets are int64 on the device, read when the kernels run, so that a
  * program need not wait for them on the host.  They must not decrease and must
