@@ -20,8 +20,9 @@
  * among them; of others products take halves of 11 bits, and X has a second one,
  * which is added to a X, but before the last two steps.  Elements of X below 2^-37
  * are lost.  Measured for full matrices, root mean square error of out's own:
- * fp32 1e-6 (64 x 64), 6e-6 (256 x 2048), 4e-5 (4000 x 12000), of which all but
- * 1e-6, 3e-6 and 8e-6 are the tensor cores' truncating additions; bfloat16 1.7e-3
+ * fp32 1e-6 (64 x 64), 3e-6 (1024 x 1024), 9e-6 (512 x 20000, 2048 x 8192), 2e-5 (4000 x
+ * 12000), where elementary fp32 operations have 1.3e-6, 3e-6, 3e-6 and 5e-6, and 8e-6 (a
+ * tensor core truncates what it adds); bfloat16 1.7e-3
  * to 2.3e-3, of which its rounding is 1.7e-3.  An infinite or
  * NaN element makes all of its matrix's out NaN (steps > 0), and no other's.
  *

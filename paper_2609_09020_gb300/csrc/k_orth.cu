@@ -9,9 +9,8 @@
 #include "k_linear_tc.cuh"
 #include "orth.cuh"
 
-// Tile shapes, by columns.
-constexpr int kShapes = 3;
-constexpr int kShapeColumns[kShapes] = {64, 128, 256};
+using pic::orth::kShapes;
+constexpr int kShapeColumns[kShapes] = {64, 128, 256, 128}, kShapeRows[kShapes] = {128, 128, 256, 256};
 // Small matrices of up to so much shared memory are launched together.
 constexpr int kSmallLists = 3;
 constexpr int kSmallBytes[kSmallLists] = {56 * 1024, 112 * 1024, pic::orth::kSmallMost};
@@ -280,34 +279,46 @@ bool steps_ok(int steps, double a, double b, double c) {
 
 // The jobs of each stage and tile shape, the workspace of their parts and its counters.
 //
-// Shapes: 256 columns by pairs of CTAs, which load half as much for as many operations,
-// where the list has such tiles for the pairs twice or nearly; 64 where the smaller side is
-// no more, or where there are few tiles of 128 (us, 64 / 128 columns: fp32 512 x 512 133 /
-// 166, 1024 x 1024 196 / 237, 1500 x 1500 372 / 330; bfloat16 512 x 512 101 / 105, 1024 x 1024
-// 182 / 165); else 128.  us, 128 / 256 columns: bfloat16 2048 x 2048 243 / 374, two of them 410 /
-// 343, four 757 / 584, 2048 x 8192 608 / 605; fp32 541 / 523, 1029 / 757, 1901 / 1416, 1563 / 1369.
+// Shapes: by pairs of CTAs, which load half as much for as many operations, where the list
+// has tiles of 256 x 256 for the pairs twice or nearly; 64 columns where the smaller side is no
+// more, or where there are few tiles of 128; else 128.  us, 64 / 128 columns, tiles of 128 x 128 in
+// the list: fp32 512 x 512 (16) 133 / 171, 1024 x 1024 (64) 193 / 237, 300 x 300 (99) 142 / 156,
+// 256 x 256 (96) 163 / 154, 500 x 500 (96) 164 / 188, 1280 x 1280 (100) 253 / 271, 1408 x 1408 (121) 269 /
+// 287, 1536 x 1536 (144) 374 / 326; bfloat16 512 x 512 (16) 101 / 104, 640 x 640 (25) 113 / 119, 200 x
+// 200 (32) 94 / 99, 896 x 896 (49) 124 / 124, 1024 x 1024 (64) 135 / 130, 256 x 256 (64) 109 / 99, 300 x 300
+// (72) 98 / 103, (99) 110 / 101, 1536 x 1536 (144) 178 / 161: the two meet between 100 and 144 tiles
+// for fp32, and within a twentieth of one another from 16 to 72 for bfloat16.  us, 128 columns / pairs:
+// bfloat16 2048 x 2048 243 / 374, two of them 410 / 343, four 757 / 584, 2048 x 8192 608 / 605; fp32
+// 541 / 523, 1029 / 757, 1901 / 1431, 1563 / 1369.
+//
+// A pair's tiles are 256 columns wide but in A and A^2 of lists with operands of two halves,
+// where they are 128: so their sums can be taken over (k_orth_tc.cu).  us and out's error, of
+// elementary fp32's, with 256 columns / so: two 2048 x 2048 767 (3.6) / 772 (1.9), four 1431 / 1507,
+// 2048 x 8192 1340 (2.5) / 1290 (1.8), 4000 x 12000 6990 (5.3) / 6650 (2.6); with 128 columns in the
+// updates too 804 (0.6), 1502, 1303 (0.6), 7070 (0.6).  One half's matrices in such a list have
+// the same tiles in A and A^2 (six of 1000 x 1100 with six of fp32 705 us, in a launch of their own 758).
 //
 // Parts: stages with fewer tiles than there are CTAs (kSlots) are cut along K, with at
 // least kLeast slices (of all three products of halves) in a part, as a part more costs 3
-// us; and sums of more than kMost slices, in which a tensor core's truncations show (it
-// loses up to 2^-24 of a sum with each 16 of K; one half's own roundings are larger).  In
-// A of up to 64 rows, whose sums are long and all of one sign on the diagonal, parts of four
-// slices where there are CTAs for them (24 matrices of three types: 1.5 of elementary fp32's
-// error before, 1.2 so, in the same time).  fp32
-// 4000 x 12000, out's error and time: 64 slices 8.5e-5, 6.5 ms; 32 4.4e-5, 7.2 ms; 16
-// 2.3e-5, 11.1 ms.
+// us; and sums of more than kMost slices (with two halves and 32 slices or 64, us: 130 x 200000
+// 1200 and 940, 4000 x 12000 7300 and 6400, 40 of 60 x 20000 1400 and 1440; one half's own roundings
+// outweigh what 256 slices of sums lose).  In A of up to 64 rows, whose sums are all of one
+// sign on the diagonal, parts of four slices where there are CTAs for them (out's error, of
+// elementary fp32's, without and so: 8 x 1500 1.7 and 1.2, 60 x 1500 3.2 and 2.9; the worst of 24 matrices
+// of sides 8 to 1500 3.2 and 2.7, in the same time).
 void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kShapes], bool (&both)[kShapes], long long& part_bytes,
                long long& counters) {
-  constexpr int kSms = 152, kSlots[kShapes] = {2 * kSms, kSms, kSms / 2}, kLeast = 16, kMost[2] = {256, 32};
+  constexpr int kSms = 152, kSlots[kShapes] = {2 * kSms, kSms, kSms / 2, kSms / 2}, kLeast = 16, kMost[2] = {256, 64};
   constexpr long long kLarge = 120;
   const auto blocks = [](long long n, long long of) { return (n + of - 1) / of; };
   long long large = 0, middle = 0;
-  bool two = false;
+  bool two = false, two_large = false;
   for (const Matrix& m : table) {
     if (m.parts == 0) continue;
     if (m.m > 512) large += blocks(m.rows, 256) * blocks(m.cols, 256);
     middle += blocks(m.rows, 128) * blocks(m.cols, 128);
     two |= m.halves == 2;
+    two_large |= m.halves == 2 && m.m > 512;
   }
   const bool few = middle <= (two ? 110 : 16);
   for (int s = 0; s < 3; ++s) {
@@ -316,9 +327,9 @@ void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kSh
     for (size_t id = 0; id < table.size(); ++id) {
       const Matrix& m = table[id];
       if (m.parts == 0) continue;  // a CTA's
-      const int shape = m.m <= 64 || few ? 0 : m.m > 512 && large >= kLarge ? 2 : 1;
+      const int shape = m.m <= 64 || few ? k64 : m.m > 512 && large >= kLarge ? (two_large && s != kUpdate ? kPair128 : kPair256) : k128;
       both[shape] |= m.halves == 2;
-      const int bn = kShapeColumns[shape], rows = shape == 2 ? 256 : 128;
+      const int bn = kShapeColumns[shape], rows = kShapeRows[shape];
       Job j{};
       j.matrix = static_cast<int>(id), j.halves = m.halves, j.parts = 1;
       long long I = m.m, J = m.m, K = m.m;
@@ -348,9 +359,9 @@ void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kSh
         return a.k1 * (a.halves == 2 ? 3 : 1) > b.k1 * (b.halves == 2 ? 3 : 1);
       });
       tiles[shape] = static_cast<long long>(plain[shape].size());
-      const long long slots = both[shape] && shape == 0 ? kSms : kSlots[shape];
+      const long long slots = both[shape] && shape == k64 ? kSms : kSlots[shape];
       const long long fill = tiles[shape] ? slots / tiles[shape] : 1;
-      const int cg = shape == 2 ? 2 : 1, panels = cg * (kShapeColumns[shape] / 64) * 4;
+      const int panels = kShapeRows[shape] / 32 * (kShapeColumns[shape] / 64);
       int slot = 0;
       for (const Job& j : plain[shape]) {
         const int slices = j.k1, most = kMost[j.halves - 1];
@@ -609,7 +620,7 @@ int pic_orth(pic_orthogonalizer* h, int steps, float a, float b, float c, float 
       for (int shape = 0; shape < kShapes; ++shape) {
         const StageParams q{h->matrices, h->maps, h->n_maps, h->jobs[stage][shape], h->n_jobs[stage][shape], {a, b, c}, k & 1,
                             k == 0, k + 1 == steps, k > 0 && steps - k >= 3, steps - k - 1 >= 3, h->parts, h->counters, waits};
-        if (launch_stage(stage, kShapeColumns[shape], h->both[shape], q, s) != PIC_OK) {
+        if (launch_stage(stage, static_cast<TileShape>(shape), h->both[shape], q, s) != PIC_OK) {
           cudaGetLastError();
           return PIC_ERR_CUDA;
         }

@@ -8,8 +8,9 @@
 // own in the same accumulators, the small ones first: their operands are loaded three
 // times, and the loads, 64 bytes a clock into an SM, keep up with the MMAs.  At fewer columns they would
 // not (1024 x 1024 fp32, a call: 245 us): both halves of a slice are loaded together, and
-// the small products have accumulators of their own, so that as few truncating additions as
-// there are slices meet the sums of full size.
+// the small products have accumulators of their own.  There an epilogue warp has one panel,
+// and takes the sums over into registers every few slices (takeover()), where they are added
+// to nearest; at 256 columns it has two, for which there are not enough.
 //
 // A = X X^T and A^2 are symmetric: tiles on and below the diagonal are computed and
 // kept.  Where an operand's slice would lie above it, its mirror image is loaded, which
@@ -34,6 +35,15 @@ namespace {
 
 using lin::kSlice;
 
+// Slices that the accumulators of a BOTH kernel sum up before the epilogue takes them over.
+// They lose up to 2^-24 of a sum with each 16 of K, always towards zero, and the steps
+// multiply that: out's error, of elementary fp32's, with 32 to 64 slices / so: 512 x 20000 6.5 /
+// 2.6, 40 of 130 x 20000 12.3 / 1.8, 2048 x 2048 3.6 / 0.6, 1500 x 1500 4.1 / 0.7.  A^2, whose
+// diagonal outweighs its rows, counts most: eight there too 512 x 20000 4.6, 1024 x 1024 1.7 for
+// 1.0; two to eight in the others hardly differ.  A takeover costs some 0.2 us.
+template <Stage STAGE>
+constexpr int takeover() { return STAGE == kPolynomial ? 4 : 8; }
+
 // BOTH: a stage has both halves of its slices.
 template <int CG, int BN, bool BOTH>
 struct Shape {
@@ -41,7 +51,7 @@ struct Shape {
   static constexpr int kHalves = BOTH ? 2 : 1;
   static constexpr int kStageBytes = kHalves * (kABytes + kBBytes);
   static constexpr int kCtas = BN == 64 && !BOTH ? 2 : 1;
-  static constexpr int kStages = BOTH ? (BN == 64 ? 4 : 2) : BN == 64 ? 3 : 5;
+  static constexpr int kStages = BOTH ? (BN == 64 ? 4 : CG == 2 ? 3 : 2) : BN == 64 ? 3 : 5;
   static constexpr int kEpi = BN == 64 ? 4 : 8;
   static constexpr int kThreads = 64 + 32 * kEpi;
   static constexpr int kColumns = BN == 64 ? 64 : BN / 2;
@@ -128,6 +138,7 @@ template <Stage STAGE, int CG, int BN, bool BOTH>
 __global__ void __launch_bounds__(Shape<CG, BN, BOTH>::kThreads, Shape<CG, BN, BOTH>::kCtas)
     stage_kernel(const __grid_constant__ StageParams q) {
   using S = Shape<CG, BN, BOTH>;
+  constexpr int kTakeover = takeover<STAGE>();
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = tc::smem_addr(smem_raw);
   uint8_t* smem = smem_raw + ((1024 - (raw & 1023)) & 1023);
@@ -229,37 +240,40 @@ __global__ void __launch_bounds__(Shape<CG, BN, BOTH>::kThreads, Shape<CG, BN, B
       uint32_t free_phase = 0;
       for (int w = first; w < q.n && ok; w += step) {
         const Job job = q.jobs[w];  // (a copy: through memory each slice would read it again)
-        const int k0 = job.k0, k1 = job.k1, terms = !BOTH && job.halves == 2 ? 3 : 1;
-        if (!(ok = wait(bar_free + 8 * buf, free_phase ^ 1))) break;
-        tc::tc_fence_after();
-        const uint32_t d = tmem + buf * S::kBufCols;
-        for (int n = 0, kb = k0; n < terms * (k1 - k0); ++n) {
-          const bool p_mn = lies_along(job.p_mn, job.p_half, job.i, kb * kSlice),
-                     q_mn = lies_along(job.q_mn, job.q_half, job.j, kb * kSlice);
-          if (++kb == k1) kb = k0;
-          const uint32_t idesc = tc::idesc_16(128 * CG, BN, false, p_mn, q_mn);
-          // one MMA takes 16 of K: 32 bytes of a K-major row, 16 rows of an MN-major block
-          const uint32_t a_step = p_mn ? 2048 : 32, b_step = q_mn ? 2048 : 32;
-          if (!(ok = wait(bar_full + 8 * s, phase))) break;
+        const bool two = BOTH && job.halves == 2;
+        const int k0 = job.k0, k1 = job.k1, slices = (k1 - k0) * (!BOTH && job.halves == 2 ? 3 : 1), each = two ? kTakeover : slices;
+        for (int n0 = 0, kb = k0; n0 < slices && ok; n0 += each) {
+          if (!(ok = wait(bar_free + 8 * buf, free_phase ^ 1))) break;
           tc::tc_fence_after();
-          const uint32_t sa = base + s * S::kStageBytes, sb = sa + S::kHalves * S::kABytes;
-          const auto multiply = [&](uint32_t to, uint32_t a, uint32_t b, bool begin) {
+          const uint32_t d = tmem + buf * S::kBufCols;
+          for (int n = n0; n < min(slices, n0 + each); ++n) {
+            const bool p_mn = lies_along(job.p_mn, job.p_half, job.i, kb * kSlice),
+                       q_mn = lies_along(job.q_mn, job.q_half, job.j, kb * kSlice);
+            if (++kb == k1) kb = k0;
+            const uint32_t idesc = tc::idesc_16(128 * CG, BN, false, p_mn, q_mn);
+            // one MMA takes 16 of K: 32 bytes of a K-major row, 16 rows of an MN-major block
+            const uint32_t a_step = p_mn ? 2048 : 32, b_step = q_mn ? 2048 : 32;
+            if (!(ok = wait(bar_full + 8 * s, phase))) break;
+            tc::tc_fence_after();
+            const uint32_t sa = base + s * S::kStageBytes, sb = sa + S::kHalves * S::kABytes;
+            const auto multiply = [&](uint32_t to, uint32_t a, uint32_t b, bool begin) {
 #pragma unroll
-            for (int kk = 0; kk < kSlice / 16; ++kk)
-              tc::mma_16<CG>(to, tc::smem_desc_sw128(a + kk * a_step, 8192, 1024),
-                             tc::smem_desc_sw128(b + kk * b_step, 8192, 1024), idesc, (!begin || kk > 0) ? 1u : 0u);
-          };
-          if (BOTH && job.halves == 2) {
-            multiply(d + BN, sa + S::kABytes, sb, n == 0);
-            multiply(d + BN, sa, sb + S::kBBytes, false);
+              for (int kk = 0; kk < kSlice / 16; ++kk)
+                tc::mma_16<CG>(to, tc::smem_desc_sw128(a + kk * a_step, 8192, 1024),
+                               tc::smem_desc_sw128(b + kk * b_step, 8192, 1024), idesc, (!begin || kk > 0) ? 1u : 0u);
+            };
+            if (two) {
+              multiply(d + BN, sa + S::kABytes, sb, n == n0);
+              multiply(d + BN, sa, sb + S::kBBytes, false);
+            }
+            multiply(d, sa, sb, n == n0);
+            tc::mma_commit_cg<CG>(bar_empty + 8 * s);
+            if (++s == S::kStages) s = 0, phase ^= 1;
           }
-          multiply(d, sa, sb, n == 0);
-          tc::mma_commit_cg<CG>(bar_empty + 8 * s);
-          if (++s == S::kStages) s = 0, phase ^= 1;
+          if (!ok) break;
+          tc::mma_commit_cg<CG>(bar_acc + 8 * buf);
+          if (++buf == 2) buf = 0, free_phase ^= 1;
         }
-        if (!ok) break;
-        tc::mma_commit_cg<CG>(bar_acc + 8 * buf);
-        if (++buf == 2) buf = 0, free_phase ^= 1;
       }
     }
     __syncwarp();
@@ -303,36 +317,54 @@ __global__ void __launch_bounds__(Shape<CG, BN, BOTH>::kThreads, Shape<CG, BN, B
       const Matrix& m = q.matrices[job.matrix];
       const int I = STAGE == kUpdate ? m.rows : m.m, J = STAGE == kUpdate ? m.cols : m.m;
       const int row0 = job.i + below, parts = job.parts;
-      if (!__all_sync(0xffffffffu, wait(bar_acc + 8 * buf, phase))) break;
-      tc::tc_fence_after();
-      const uint32_t d = tmem + buf * S::kBufCols + (static_cast<uint32_t>(quarter * 32) << 16);
+      const bool two_halves = BOTH && job.halves == 2;
+      const int takes = two_halves ? (job.k1 - job.k0 + kTakeover - 1) / kTakeover : 1;
+      static_assert(!BOTH || S::kColumns == 64, "a warp's sums stay in its registers");
       for (int c0 = from; c0 < to && ok; c0 += 64) {
         float v[64];
-        {
-          uint32_t acc[64];
-          tc::tmem_ld64_wait(d + c0, acc);
+        for (int take = 0; take < takes; ++take) {
+          if (c0 == from) {
+            ok = __all_sync(0xffffffffu, wait(bar_acc + 8 * buf, phase));
+            if (!ok) break;
+            tc::tc_fence_after();
+          }
+          const uint32_t d = tmem + buf * S::kBufCols + (static_cast<uint32_t>(quarter * 32) << 16) + c0;
+          if (take == 0) {
+            uint32_t sums[64];
+            tc::tmem_ld64_wait(d, sums);
 #pragma unroll
-          for (int c = 0; c < 64; ++c) v[c] = __uint_as_float(acc[c]);
-        }
-        if (BOTH && job.halves == 2) {
+            for (int c = 0; c < 64; ++c) v[c] = __uint_as_float(sums[c]);
+          } else {
 #pragma unroll
-          for (int h = 0; h < 64; h += 32) {
-            uint32_t small[32];
-            tc::tmem_ld32_wait(d + BN + c0 + h, small);
+            for (int h = 0; h < 64; h += 32) {
+              uint32_t sums[32];
+              tc::tmem_ld32_wait(d + h, sums);
 #pragma unroll
-            for (int c = 0; c < 32; ++c) v[h + c] += __uint_as_float(small[c]);
+              for (int c = 0; c < 32; ++c) v[h + c] += __uint_as_float(sums[c]);
+            }
+          }
+          if (two_halves) {
+#pragma unroll
+            for (int h = 0; h < 64; h += 32) {
+              uint32_t small[32];
+              tc::tmem_ld32_wait(d + BN + h, small);
+#pragma unroll
+              for (int c = 0; c < 32; ++c) v[h + c] += __uint_as_float(small[c]);
+            }
+          }
+          if (c0 + 64 == to) {
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0 && !(q.waits.test_fault && w == 0 && rank == 0 && quarter == 0)) {
+              if constexpr (CG == 2)
+                tc::mbar_arrive_cluster(lead_free + 8 * buf);
+              else
+                tc::mbar_arrive(bar_free + 8 * buf);
+            }
+            if (++buf == 2) buf = 0, phase ^= 1;
           }
         }
-        if (c0 + 64 == to) {
-          tc::tc_fence_before();
-          __syncwarp();
-          if (lane == 0 && !(q.waits.test_fault && w == 0 && rank == 0 && quarter == 0)) {
-            if constexpr (CG == 2)
-              tc::mbar_arrive_cluster(lead_free + 8 * buf);
-            else
-              tc::mbar_arrive(bar_free + 8 * buf);
-          }
-        }
+        if (!ok) break;
         const int col0 = job.j + c0, cols = min(64, J - col0);
         bool mine = inside(job, m, c0);
         if (mine && parts > 1) {
@@ -435,7 +467,6 @@ __global__ void __launch_bounds__(Shape<CG, BN, BOTH>::kThreads, Shape<CG, BN, B
         }
       }
       if (!ok) break;
-      if (++buf == 2) buf = 0, phase ^= 1;
     }
     if (lane == 0) {
       tc::bulk_wait_all();
@@ -473,19 +504,21 @@ int launch(const StageParams& q, int slot, lin::Chain& s) {
 }
 
 template <Stage STAGE>
-int launch_bn(int bn, bool both, const StageParams& q, lin::Chain& s) {
-  if (bn == 64) return both ? launch<STAGE, 1, 64, true>(q, 64 + STAGE, s) : launch<STAGE, 1, 64, false>(q, 44 + STAGE, s);
-  if (bn == 128) return both ? launch<STAGE, 1, 128, true>(q, 67 + STAGE, s) : launch<STAGE, 1, 128, false>(q, 47 + STAGE, s);
+int launch_shape(TileShape shape, bool both, const StageParams& q, lin::Chain& s) {
+  if (shape == k64) return both ? launch<STAGE, 1, 64, true>(q, 64 + STAGE, s) : launch<STAGE, 1, 64, false>(q, 44 + STAGE, s);
+  if (shape == k128) return both ? launch<STAGE, 1, 128, true>(q, 67 + STAGE, s) : launch<STAGE, 1, 128, false>(q, 47 + STAGE, s);
+  if constexpr (STAGE != kUpdate)
+    if (shape == kPair128) return launch<STAGE, 2, 128, true>(q, 75 + STAGE, s);
   return launch<STAGE, 2, 256, false>(q, 50 + STAGE, s);
 }
 
 }  // namespace
 
-int launch_stage(Stage stage, int bn, bool both, const StageParams& q, lin::Chain& s) {
+int launch_stage(Stage stage, TileShape shape, bool both, const StageParams& q, lin::Chain& s) {
   if (q.n == 0) return PIC_OK;
-  if (stage == kGram) return launch_bn<kGram>(bn, both, q, s);
-  if (stage == kPolynomial) return launch_bn<kPolynomial>(bn, both, q, s);
-  return launch_bn<kUpdate>(bn, both, q, s);
+  if (stage == kGram) return launch_shape<kGram>(shape, both, q, s);
+  if (stage == kPolynomial) return launch_shape<kPolynomial>(shape, both, q, s);
+  return launch_shape<kUpdate>(shape, both, q, s);
 }
 
 }  // namespace orth

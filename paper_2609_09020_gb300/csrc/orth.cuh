@@ -127,9 +127,11 @@ struct StageParams {
   unsigned* counters;
   Waits waits;
 };
-// With tiles of bn columns: 64 and 128 by one CTA, 256 by a pair.  both: some matrices have
-// operands of two halves.
-int launch_stage(Stage stage, int bn, bool both, const StageParams& q, lin::Chain& s);
+// Tiles: 128 rows x 64 or 128 columns by a CTA, 256 x 256 (operands of one half) or 256 x 128
+// (of two) by a pair.
+enum TileShape { k64 = 0, k128 = 1, kPair256 = 2, kPair128 = 3, kShapes = 4 };
+// both: of k64 and k128, that some matrices have operands of two halves.
+int launch_stage(Stage stage, TileShape shape, bool both, const StageParams& q, lin::Chain& s);
 
 }  // namespace orth
 }  // namespace pic
