@@ -53,3 +53,33 @@ def test_the_next_call_is_right(pic, shape, dtype):
     assert torch.equal(out, want)
     h.close()
     other.close()
+
+
+# tiles whose sums are taken over, by pairs of CTAs and by one, in lists of one type and of two
+@pytest.mark.parametrize("shape,count,types", [((1024, 1100), 14, [F32]), ((1024, 1100), 14, [F32, torch.bfloat16]),
+                                               ((300, 5000), 40, [F32]), ((60, 20000), 60, [F32, F16])], ids=str)
+def test_sums_that_are_taken_over(pic, shape, count, types):
+    g = [torch.empty(shape, dtype=types[i % len(types)], device="cuda") for i in range(count)]
+    for i, t in enumerate(g):
+        fill(t, i)
+    out, want = [torch.zeros_like(t) for t in g], [torch.zeros_like(t) for t in g]
+    h, other = pic.Orthogonalizer(g, out=out), pic.Orthogonalizer(g, out=want)
+    lib = pic.load_library()
+    other.orthogonalize()
+    other.check()
+    assert lib.pic_linear_test_wait_fault(1, SHORT_LIMIT) == pic.PIC_OK
+    try:
+        h.orthogonalize()
+        torch.cuda.synchronize()
+    finally:
+        lib.pic_linear_test_wait_fault(0, 0)
+    for _ in range(2):
+        h.orthogonalize()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+    with pytest.raises(pic.PicError) as e:
+        h.check()
+    assert e.value.status == pic.PIC_ERR_TIMEOUT
+    h.check()
+    h.close()
+    other.close()
