@@ -24,6 +24,20 @@ constexpr int kMaxDim = 128;
 constexpr int kTcTile = 128;
 constexpr int kTmaRowBox = kTcTile + 4;
 
+// Whether `encode`, which makes a tensor map, did.  The driver refuses where no context is
+// current, as in a thread whose first CUDA call this is (the runtime makes the device's
+// current at its own first use of it): then once more with it.
+template <typename F>
+inline bool encoded(F encode) {
+  if (encode() == CUDA_SUCCESS) return true;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(dev) != cudaSuccess) {
+    cudaGetLastError();
+    return false;
+  }
+  return encode() == CUDA_SUCCESS;
+}
+
 // Geometry of one pyramid level (Eq. 1 with the ceiling rule): size, offset
 // of the level inside one image's latent block, and the size ratios
 // W_l / W, H_l / H that map output pixel centres to source coordinates.

@@ -157,9 +157,11 @@ bool encode_latent_map(pic::TmaParams& tp, const DecodeParams& p) {
   const cuuint64_t stride[1] = {4};  // unused for a 1-D tensor
   const cuuint32_t box[1] = {static_cast<cuuint32_t>(pic::kTmaRowBox)};
   const cuuint32_t elem_stride[1] = {1u};
-  return enc(&tp.lat, CU_TENSOR_MAP_DATA_TYPE_INT32, 1, const_cast<int32_t*>(p.latents), dim, stride,
-             box, elem_stride, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
-             CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return pic::encoded([&] {
+    return enc(&tp.lat, CU_TENSOR_MAP_DATA_TYPE_INT32, 1, const_cast<int32_t*>(p.latents), dim, stride,
+               box, elem_stride, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  });
 }
 
 void fill_params(const pic_decoder* h, DecodeParams& p, int B, const int32_t* latents,
