@@ -583,7 +583,7 @@ def _linear_act(act) -> int:
 def _refuse_recorded(backward="linear_backward", **tensors):
     """Derivatives that autograd would lose without a word.  backward: what makes them; None
     of a call that makes gradients or updates itself, which takes parameters (leaves of the
-    graph) as they are."""
+    graph, and views of them) as they are."""
     import torch
     reverse, forward = torch.is_grad_enabled(), torch.autograd.forward_ad._current_level >= 0
     for name, t in tensors.items():
@@ -592,7 +592,7 @@ def _refuse_recorded(backward="linear_backward", **tensors):
         if reverse and t.requires_grad and backward:
             raise ValueError(f"{name}: requires a gradient, and autograd does not record this call: detach it, or "
                              f"call under torch.no_grad(), and take the gradients from {backward}")
-        if reverse and t.grad_fn is not None:
+        if reverse and t.grad_fn is not None and (t._base is None or t._base.grad_fn is not None):
             raise ValueError(f"{name}: is part of a graph, and autograd does not record this call: detach it, or "
                              "call under torch.no_grad()")
         if forward and torch.autograd.forward_ad.unpack_dual(t).tangent is not None:

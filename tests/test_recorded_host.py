@@ -67,6 +67,24 @@ def test_forwards(pic, name, which):
             call(**a)
 
 
+def test_views_of_parameters(pic):
+    """A layer's slice of a buffer of parameters is one; a slice of a result is not."""
+    a = arguments()["grouped_linear_backward"]
+    blob = torch.zeros(2, 3 * 8 + 3, requires_grad=True)
+    weights = lambda t: t[:, :24].unflatten(1, (3, 8))
+    a["weight"] = weights(blob)
+    assert a["weight"].grad_fn is not None
+    with pytest.raises(ValueError, match=CPU):
+        pic.grouped_linear_backward(**a)
+    a["weight"] = weights(blob * 2)
+    with pytest.raises(ValueError, match="^weight: is part of a graph"):
+        pic.grouped_linear_backward(**a)
+    with pytest.raises(ValueError, match=CPU):
+        pic.Orthogonalizer([weights(blob)])
+    with pytest.raises(ValueError, match="is part of a graph"):
+        pic.Orthogonalizer([weights(blob * 2)])
+
+
 def test_a_second_derivative(pic):
     """Inside of an autograd.Function whose backward is itself recorded."""
     a = arguments()["grouped_linear_backward"]
