@@ -119,7 +119,8 @@ int pic_grouped_linear_backward(const pic_grouped_linear_grad_args *a, void *wor
 /* Synchronises `stream`; PIC_OK if since the last check, on the current device,
  * no bounded device-side wait of these calls or of pic_linear.h's gave up
  * (PIC_ERR_TIMEOUT if one did: its outputs are unspecified) and all offsets
- * were as they must be (else PIC_ERR_INVALID_ARG); PIC_ERR_CUDA. */
+ * were as they must be (else PIC_ERR_INVALID_ARG, from the next check if a wait
+ * gave up too); PIC_ERR_CUDA. */
 int pic_grouped_linear_check(void *stream);
 
 #ifdef __cplusplus

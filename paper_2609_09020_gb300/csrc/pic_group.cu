@@ -221,10 +221,13 @@ int pic_grouped_linear_backward(const pic_grouped_linear_grad_args* a, void* wor
 }
 
 int pic_grouped_linear_check(void* stream) {
-  const int offsets = pic::lin::take_status(1, static_cast<cudaStream_t>(stream));
-  const int waits = pic::lin::take_status(0, static_cast<cudaStream_t>(stream));
-  if (offsets < 0 || waits < 0) return PIC_ERR_CUDA;
-  return waits ? PIC_ERR_TIMEOUT : offsets ? PIC_ERR_INVALID_ARG : PIC_OK;
+  // (after a timeout the offsets' word is left for the next check: one code tells of one)
+  for (const int word : {0, 1}) {
+    const int flag = pic::lin::take_status(word, static_cast<cudaStream_t>(stream));
+    if (flag < 0) return PIC_ERR_CUDA;
+    if (flag) return word == 0 ? PIC_ERR_TIMEOUT : PIC_ERR_INVALID_ARG;
+  }
+  return PIC_OK;
 }
 
 }  // extern "C"
