@@ -277,6 +277,14 @@ bool steps_ok(int steps, double a, double b, double c) {
   return true;
 }
 
+// After how many slices sums of two halves are taken over.  An accumulator loses up to 2^-24
+// of a sum with each 16 of K, always towards zero, and the steps multiply that: out's error, of
+// elementary fp32's, with 32 to 64 slices in one / with takeovers: 512 x 20000 6.5 / 2.6, 40 of 130 x
+// 20000 12.3 / 1.8, 2048 x 2048 3.6 / 0.6, 1500 x 1500 4.1 / 0.7.  A^2, whose diagonal outweighs its rows,
+// counts most: eight there too 512 x 20000 4.6, 1024 x 1024 1.7 for 1.0; two to eight in the others
+// hardly differ, but in A of few rows (1 x 2^24 4.8e-6 with eight).  A takeover costs some 0.2 us.
+int takeover(int stage, const Matrix& m) { return stage == kPolynomial || (stage == kGram && m.m <= 64) ? 4 : 8; }
+
 // The jobs of each stage and tile shape, the workspace of their parts and its counters.
 //
 // Shapes: by pairs of CTAs, which load half as much for as many operations, where the list
@@ -301,14 +309,14 @@ bool steps_ok(int steps, double a, double b, double c) {
 // Parts: stages with fewer tiles than there are CTAs (kSlots) are cut along K, with at
 // least kLeast slices (of all three products of halves) in a part, as a part more costs 3
 // us; and sums of more than kMost slices (with two halves and 32 slices or 64, us: 130 x 200000
-// 1200 and 940, 4000 x 12000 7300 and 6400, 40 of 60 x 20000 1400 and 1440; one half's own roundings
-// outweigh what 256 slices of sums lose).  In A of up to 64 rows, whose sums are all of one
+// 1200 and 940, 4000 x 12000 7300 and 6400, but 40 of 60 x 20000 1400 and 1440: 32 up to 64 rows; one
+// half's own roundings outweigh what 256 slices of sums lose).  In A of up to 64 rows, whose sums are all of one
 // sign on the diagonal, parts of four slices where there are CTAs for them (out's error, of
 // elementary fp32's, without and so: 8 x 1500 1.7 and 1.2, 60 x 1500 3.2 and 2.9; the worst of 24 matrices
 // of sides 8 to 1500 3.2 and 2.7, in the same time).
 void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kShapes], bool (&both)[kShapes], long long& part_bytes,
                long long& counters) {
-  constexpr int kSms = 152, kSlots[kShapes] = {2 * kSms, kSms, kSms / 2, kSms / 2}, kLeast = 16, kMost[2] = {256, 64};
+  constexpr int kSms = 152, kSlots[kShapes] = {2 * kSms, kSms, kSms / 2, kSms / 2}, kLeast = 16, kMost[2] = {256, 64}, kMostThin = 32;
   constexpr long long kLarge = 120;
   const auto blocks = [](long long n, long long of) { return (n + of - 1) / of; };
   long long large = 0, middle = 0;
@@ -331,7 +339,7 @@ void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kSh
       both[shape] |= m.halves == 2;
       const int bn = kShapeColumns[shape], rows = kShapeRows[shape];
       Job j{};
-      j.matrix = static_cast<int>(id), j.halves = m.halves, j.parts = 1;
+      j.matrix = static_cast<int>(id), j.halves = m.halves, j.parts = 1, j.take = takeover(s, m);
       long long I = m.m, J = m.m, K = m.m;
       if (s == kGram) {
         j.p_map = j.q_map = kMapX, j.p_mn = j.q_mn = !m.left, K = m.left ? m.cols : m.rows;
@@ -364,9 +372,9 @@ void make_jobs(const std::vector<Matrix>& table, std::vector<Job> (&jobs)[3][kSh
       const int panels = kShapeRows[shape] / 32 * (kShapeColumns[shape] / 64);
       int slot = 0;
       for (const Job& j : plain[shape]) {
-        const int slices = j.k1, most = kMost[j.halves - 1];
-        const int passes = j.halves == 2 ? 3 : 1;
+        const int slices = j.k1, passes = j.halves == 2 ? 3 : 1;
         const bool thin = s == kGram && j.halves == 2 && table[j.matrix].m <= 64;
+        const int most = thin ? kMostThin : kMost[j.halves - 1];
         const long long worth = thin ? blocks(slices, 4) : slices * passes / kLeast;
         long long parts = std::max(std::min(fill, worth), blocks(slices, most));
         parts = std::max<long long>(parts, 1);

@@ -9,7 +9,7 @@
 // times, and the loads, 64 bytes a clock into an SM, keep up with the MMAs.  At fewer columns they would
 // not (1024 x 1024 fp32, a call: 245 us): both halves of a slice are loaded together, and
 // the small products have accumulators of their own.  There an epilogue warp has one panel,
-// and takes the sums over into registers every few slices (takeover()), where they are added
+// and takes the sums over into registers every few slices (Job::take), where they are added
 // to nearest; at 256 columns it has two, for which there are not enough.
 //
 // A = X X^T and A^2 are symmetric: tiles on and below the diagonal are computed and
@@ -34,15 +34,6 @@ namespace orth {
 namespace {
 
 using lin::kSlice;
-
-// Slices that the accumulators of a BOTH kernel sum up before the epilogue takes them over.
-// They lose up to 2^-24 of a sum with each 16 of K, always towards zero, and the steps
-// multiply that: out's error, of elementary fp32's, with 32 to 64 slices / so: 512 x 20000 6.5 /
-// 2.6, 40 of 130 x 20000 12.3 / 1.8, 2048 x 2048 3.6 / 0.6, 1500 x 1500 4.1 / 0.7.  A^2, whose
-// diagonal outweighs its rows, counts most: eight there too 512 x 20000 4.6, 1024 x 1024 1.7 for
-// 1.0; two to eight in the others hardly differ.  A takeover costs some 0.2 us.
-template <Stage STAGE>
-constexpr int takeover() { return STAGE == kPolynomial ? 4 : 8; }
 
 // BOTH: a stage has both halves of its slices.
 template <int CG, int BN, bool BOTH>
@@ -138,7 +129,6 @@ template <Stage STAGE, int CG, int BN, bool BOTH>
 __global__ void __launch_bounds__(Shape<CG, BN, BOTH>::kThreads, Shape<CG, BN, BOTH>::kCtas)
     stage_kernel(const __grid_constant__ StageParams q) {
   using S = Shape<CG, BN, BOTH>;
-  constexpr int kTakeover = takeover<STAGE>();
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = tc::smem_addr(smem_raw);
   uint8_t* smem = smem_raw + ((1024 - (raw & 1023)) & 1023);
@@ -241,7 +231,7 @@ __global__ void __launch_bounds__(Shape<CG, BN, BOTH>::kThreads, Shape<CG, BN, B
       for (int w = first; w < q.n && ok; w += step) {
         const Job job = q.jobs[w];  // (a copy: through memory each slice would read it again)
         const bool two = BOTH && job.halves == 2;
-        const int k0 = job.k0, k1 = job.k1, slices = (k1 - k0) * (!BOTH && job.halves == 2 ? 3 : 1), each = two ? kTakeover : slices;
+        const int k0 = job.k0, k1 = job.k1, slices = (k1 - k0) * (!BOTH && job.halves == 2 ? 3 : 1), each = two ? job.take : slices;
         for (int n0 = 0, kb = k0; n0 < slices && ok; n0 += each) {
           if (!(ok = wait(bar_free + 8 * buf, free_phase ^ 1))) break;
           tc::tc_fence_after();
@@ -318,18 +308,18 @@ __global__ void __launch_bounds__(Shape<CG, BN, BOTH>::kThreads, Shape<CG, BN, B
       const int I = STAGE == kUpdate ? m.rows : m.m, J = STAGE == kUpdate ? m.cols : m.m;
       const int row0 = job.i + below, parts = job.parts;
       const bool two_halves = BOTH && job.halves == 2;
-      const int takes = two_halves ? (job.k1 - job.k0 + kTakeover - 1) / kTakeover : 1;
+      const int k0 = job.k0, k1 = job.k1, each = two_halves ? job.take : k1 - k0;
       static_assert(!BOTH || S::kColumns == 64, "a warp's sums stay in its registers");
       for (int c0 = from; c0 < to && ok; c0 += 64) {
         float v[64];
-        for (int take = 0; take < takes; ++take) {
+        for (int k = k0; k < k1; k += each) {
           if (c0 == from) {
             ok = __all_sync(0xffffffffu, wait(bar_acc + 8 * buf, phase));
             if (!ok) break;
             tc::tc_fence_after();
           }
           const uint32_t d = tmem + buf * S::kBufCols + (static_cast<uint32_t>(quarter * 32) << 16) + c0;
-          if (take == 0) {
+          if (k == k0) {
             uint32_t sums[64];
             tc::tmem_ld64_wait(d, sums);
 #pragma unroll

@@ -72,7 +72,7 @@ struct Job {
   int k0, k1;          // slices
   int part, parts;     // along K
   int slot;            // the first of the tile's parts in the workspace
-  int pad;
+  int take;            // slices that an accumulator of two halves sums up before it is taken over
 };
 static_assert(sizeof(Job) == 64, "a job is read in four loads");
 

@@ -43,3 +43,15 @@ def test_long(pic, shape, count):
         assert mean(out[i].double() - want) <= 4 * plain + 2.0 ** -20 * mean(want)
     for t, o in zip(beside, out[count:]):
         orth_ref.check(o, t)
+
+
+@pytest.mark.parametrize("shape", [(1, 2 ** 24 + 5), (3, 5000001), (2 ** 22, 2), (64, 300000)], ids=str)
+def test_few_rows(pic, shape):
+    """Within orth_ref's bounds where A is a handful of very long sums of squares."""
+    g = normal(shape, torch.float32, 2)
+    out = torch.zeros_like(g)
+    h = pic.Orthogonalizer([g], out=[out])
+    h.orthogonalize()
+    h.check()
+    h.close()
+    orth_ref.check(out, g)
