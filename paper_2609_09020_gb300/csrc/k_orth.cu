@@ -18,6 +18,7 @@ constexpr int kSmallBytes[kSmallLists] = {56 * 1024, 112 * 1024, pic::orth::kSma
 struct pic_orthogonalizer {
   int device;
   int n_pieces;
+  int n_totals;  // matrices, if one has more than kMostSquares pieces, or 0
   int* small[kSmallLists];  // matrices that a CTA each takes, by the shared memory that they need
   int n_small[kSmallLists], small_bytes[kSmallLists];
   char* room;  // all of it
@@ -133,6 +134,31 @@ __global__ void __launch_bounds__(kThreads) squares_kernel(const Matrix* matrice
   }
 }
 
+// The sum of `n` squares, by a block: in warp 0's lane 0.
+__device__ __forceinline__ double sum_squares(const double* squares, int n, double* sums) {
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < n; i += kThreads) sum += squares[i];
+#pragma unroll
+  for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0)
+    for (int w = 1; w < kThreads / 32; ++w) sum += sums[w];
+  return sum;
+}
+
+// Matrices of more than kMostSquares pieces: a block adds up one's squares into the first, so
+// that the blocks that scale them need not all (1 x 2^29: 2.1 s of scaling, in 2^40 additions).
+constexpr int kMostSquares = 4096;
+__global__ void __launch_bounds__(kThreads) total_kernel(const Matrix* matrices, double* squares) {
+  __shared__ double sums[kThreads / 32];
+  const Matrix& m = matrices[blockIdx.x];
+  wait_for_earlier();
+  if (m.parts <= kMostSquares) return;
+  const double sum = sum_squares(squares + m.part0, m.parts, sums);
+  if (threadIdx.x == 0) squares[m.part0] = sum;
+}
+
 // X = G / (|G| + eps), a piece a block.
 __global__ void __launch_bounds__(kThreads) scale_kernel(const Matrix* matrices, const Piece* pieces, const double* squares,
                                                          float eps, int last) {
@@ -141,16 +167,8 @@ __global__ void __launch_bounds__(kThreads) scale_kernel(const Matrix* matrices,
   const Piece p = pieces[blockIdx.x];
   const Matrix& m = matrices[p.matrix];
   wait_for_earlier();
-  double sum = 0.0;
-  for (int i = threadIdx.x; i < m.parts; i += kThreads) sum += squares[m.part0 + i];
-#pragma unroll
-  for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < kThreads / 32; ++w) sum += sums[w];
-    norm_factors(sum, eps, factors[0], factors[1]);
-  }
+  const double sum = sum_squares(squares + m.part0, m.parts > kMostSquares ? 1 : m.parts, sums);
+  if (threadIdx.x == 0) norm_factors(sum, eps, factors[0], factors[1]);
   __syncthreads();
   const float f0 = factors[0], f1 = last ? factors[1] : kScale;
   if (threadIdx.x == 0 && p.row0 == 0 && p.col0 == 0) *m.rest = factors[1];
@@ -561,6 +579,8 @@ int pic_orth_create(const pic_orth_matrix* matrices, int n, pic_orthogonalizer**
     h->n_counters = counters;
     h->status = reinterpret_cast<int*>(h->room + at_status);
     h->n_pieces = static_cast<int>(pieces.size());
+    if (std::any_of(table.begin(), table.end(), [](const Matrix& t) { return t.parts > kMostSquares; }))
+      h->n_totals = static_cast<int>(table.size());
     const auto put = [](void* to, const auto& v) {
       return v.empty() || cudaMemcpy(to, v.data(), v.size() * sizeof(v[0]), cudaMemcpyHostToDevice) == cudaSuccess;
     };
@@ -616,6 +636,7 @@ int pic_orth(pic_orthogonalizer* h, int steps, float a, float b, float c, float 
   const Matrix* matrices = h->matrices;
   const Piece* pieces = h->pieces;
   int rc = s.launch(squares_kernel, dim3(h->n_pieces), kThreads, 0, matrices, pieces, h->squares, h->counters, h->n_counters);
+  if (rc == PIC_OK && h->n_totals > 0) rc = s.launch(total_kernel, dim3(h->n_totals), kThreads, 0, matrices, h->squares);
   if (rc == PIC_OK)
     rc = s.launch(scale_kernel, dim3(h->n_pieces), kThreads, 0, matrices, pieces, static_cast<const double*>(h->squares), eps,
                   static_cast<int>(steps == 0));
