@@ -127,8 +127,8 @@ struct StageParams {
   unsigned* counters;
   Waits waits;
 };
-// Tiles: 128 rows x 64 or 128 columns by a CTA, 256 x 256 (operands of one half) or 256 x 128
-// (of two) by a pair.
+// Tiles: 128 rows x 64 or 128 columns by a CTA; 256 x 256, or, in A and A^2 of lists with
+// operands of two halves, 256 x 128, by a pair.
 enum TileShape { k64 = 0, k128 = 1, kPair256 = 2, kPair128 = 3, kShapes = 4 };
 // both: of k64 and k128, that some matrices have operands of two halves.
 int launch_stage(Stage stage, TileShape shape, bool both, const StageParams& q, lin::Chain& s);
